@@ -647,6 +647,144 @@ fc_status fc_rope_heads(const void* d_in, int in_stride, void* d_out, int batch,
                         const int32_t* d_pos, float base, fc_stream s);
 
 /* ------------------------------------------------------------------------
+ * Serving in four bits (no counterpart in the paper, whose target models keep
+ * their caches and weights in 16 bits): a paged KV cache held in 4 bits, the
+ * verification attention over it, and products of a few rows with weights in
+ * 4 bits.  A step of a serving loop: fc_kv_pages_plan (where the new tokens
+ * go) -> per layer fc_w4_matvec, fc_kv4_attn, fc_kv4_write.
+ *
+ * Quantisation.  A row x of D values (or a group of one column's weights) is
+ * held as one scale s = bf16(max|x| / 7) and whole numbers
+ * c = clamp(rint(x / s), -7, 7), ties to even (all 0 when s = 0); it stands
+ * for c * s.  In memory a number is c + 8, two to a byte, the first in the
+ * low half.  A row with a NaN or an infinity gets a NaN scale and stands for
+ * NaN.
+ * ------------------------------------------------------------------------ */
+typedef struct {
+  void* k_codes;     /* device, [n_pages][Hkv][page_size][D / 2] bytes, 16-byte aligned */
+  void* v_codes;
+  void* k_scale;     /* device, [n_pages][Hkv][page_size] bf16, 16-byte aligned */
+  void* v_scale;
+  int32_t n_pages;   /* >= 1; n_pages * page_size < 2^31 */
+  int32_t page_size; /* tokens a page: 16, 32, 64, 128 or 256 */
+  int32_t Hkv;
+  int32_t D;         /* 128 */
+} fc_kv4_cache;
+
+/*
+ * Block tables and slot maps of one step, from the requests' lengths.
+ * Request b holds kv_len[b] tokens in the pages table[b][0 ..
+ * ceil(kv_len / page_size)) and gets n_new[b] more.  Pages it lacks come from
+ * the end of the free list, in request order: with n_free pages free and o
+ * pages taken by the requests before it, its j-th new page is
+ * free[n_free - 1 - o - j].  The new tokens form the rows of the step, request
+ * by request:
+ *   d_cu   [batch + 1] first row of each request, then the number of rows
+ *   d_seq  [rows_cap] the request of a row; d_pos its position (kv_len + its
+ *          index among the new); d_slot its place in the cache, page *
+ *          page_size + offset.  Rows past the last hold -1 in every array.
+ *   d_src  optional [rows_cap]: where the row's key comes from, seq *
+ *          n_per_seq + node, the node being d_path[b][index] (the accepted
+ *          path [batch][path_cap] of fc_accept) or, with d_path NULL, the
+ *          index itself; -1 where the path has none.  For fc_kv4_write.
+ *   d_kv_len_out, d_n_free_out  the lengths and the free count afterwards
+ *          (not the arrays they come from)
+ *   d_table entries of new pages are written, the others left.
+ * A request that is not served keeps its length and its rows get slot -1: one
+ * whose pages would pass max_pages, the free list's end or (rows) rows_cap
+ * records FC_ERR_CAPACITY, one with a negative length FC_ERR_INVALID_ARG (as
+ * does a free count outside 0..n_pages, read as 0, or a page id outside the
+ * pool).  The same inputs give the same outputs, so a call can be repeated.
+ * One launch.
+ */
+fc_status fc_kv_pages_plan(const int32_t* d_kv_len, const int32_t* d_n_new, int batch, int page_size,
+                           int32_t* d_table, int max_pages, const int32_t* d_free, int n_pages,
+                           const int32_t* d_n_free_in, const int32_t* d_path, int path_cap, int n_per_seq,
+                           int rows_cap, int32_t* d_cu, int32_t* d_seq, int32_t* d_pos, int32_t* d_slot,
+                           int32_t* d_src, int32_t* d_kv_len_out, int32_t* d_n_free_out, fc_stream s);
+
+/*
+ * Gives pages back: request b keeps its first min(keep[b], kv_len[b]) tokens
+ * (0: it is finished); the pages past them go on the end of the free list
+ * [n_pages], in request order.  d_kv_len_out, d_n_free_out as above.  More
+ * pages than the pool holds, or a negative length, record FC_ERR_INVALID_ARG
+ * (what does not fit is not given back).
+ */
+fc_status fc_kv_pages_release(const int32_t* d_kv_len, const int32_t* d_keep, int batch, int page_size,
+                              const int32_t* d_table, int max_pages, int32_t* d_free, int n_pages,
+                              const int32_t* d_n_free_in, int32_t* d_kv_len_out, int32_t* d_n_free_out, fc_stream s);
+
+/*
+ * Quantises rows of keys and values into the cache.  Row r goes to slot
+ * d_slot[r] (page * page_size + offset; negative: the row is left out); the
+ * slots of a call differ.  Its key of head h is the D values at element
+ *   d_k + (x / n_per_seq) * seq_stride + (x % n_per_seq) * row_stride + h * head_stride
+ * with x = d_src[r] (d_src NULL: x = r) in 0..n_seq * n_per_seq, the value
+ * likewise in d_v, so that parts of a fused projection's rows and head-major
+ * tensors are read where they are.  bf16, 16-byte aligned, strides multiples
+ * of 8 elements.  A slot or a d_src entry out of range records
+ * FC_ERR_INVALID_ARG and its row is left out.
+ */
+fc_status fc_kv4_write(const fc_kv4_cache* cache, const void* d_k, const void* d_v, int n_seq, int n_per_seq,
+                       int64_t seq_stride, int64_t row_stride, int64_t head_stride, const int32_t* d_src,
+                       const int32_t* d_slot, int rows, fc_stream s);
+
+/* The values that cached rows stand for, rounded to bf16: d_k, d_v
+ * [rows][Hkv][D] from slots d_slot[r] (negative: zeros). */
+fc_status fc_kv4_read(const fc_kv4_cache* cache, const int32_t* d_slot, int rows, void* d_k, void* d_v, fc_stream s);
+
+/*
+ * fc_tree_attn over the paged 4-bit cache, for 1 to 128 new tokens a request:
+ * single tokens, chunks and draft trees.  Node i of request b attends to the
+ * cached tokens [0, kv_len[b]) and to the new tokens of its mask row.
+ *   d_q         bf16 [batch][n_pad][H][D], position-encoded
+ *   d_table     [batch][max_pages] int32 page ids
+ *   d_kv_len    [batch] int32, 0 .. max_pages * page_size
+ *   d_k_new, d_v_new  bf16 [batch][Hkv][n_pad][D]: the new tokens' own keys and
+ *               values; both NULL: none, the cache alone
+ *   d_mask      [batch][n_pad][(n_pad + 63) / 64] uint64 (bit j: node i sees
+ *               node j); NULL: node i sees nodes 0..i
+ *   d_n_nodes   [batch] int32 in 0..n_pad; NULL: n_pad everywhere
+ *   d_out       bf16 [batch][n_pad][H][D]; rows past n_nodes, and rows that
+ *               see no key at all, are zeros
+ *   d_ws        workspace of fc_kv4_attn_workspace() bytes, 256-byte aligned,
+ *               ZEROED before its first use; every call leaves it fit for the
+ *               next.  Less, or none (NULL), splits the keys less, or not.
+ *               Calls that may overlap need one each.
+ * D = 128, 1 <= n_pad <= 128, H a multiple of Hkv, H / Hkv <= 16.  The tensor
+ * cores' products of numbers and bf16 queries are exact, sums, scales and the
+ * softmax are fp32; probabilities are rounded to bf16 for the second product.
+ * A length or node count out of range, or a page id outside the pool, records
+ * FC_ERR_INVALID_ARG (that request's rows are zeros; that page's keys are
+ * left out).  What a page holds past a request's end is not looked at.
+ */
+fc_status fc_kv4_attn(const void* d_q, const fc_kv4_cache* cache, const int32_t* d_table, int max_pages,
+                      const int32_t* d_kv_len, const void* d_k_new, const void* d_v_new, const uint64_t* d_mask,
+                      const int32_t* d_n_nodes, int batch, int n_pad, int H, float scale, void* d_out, void* d_ws,
+                      size_t ws_bytes, fc_stream s);
+
+/* Workspace bytes for fc_kv4_attn's largest key split at this shape (0 for an
+ * unsupported shape). */
+size_t fc_kv4_attn_workspace(int batch, int n_pad, int H, int Hkv);
+
+/*
+ * Weights in 4 bits for fc_w4_matvec (once, at load): d_w bf16 [K][N] to
+ * d_codes (fc_w4_codes_bytes(K, N) bytes, laid out for the kernel) and d_scale
+ * [K / group][N] bf16, a scale for each `group` weights of a column.  group 32,
+ * 64 or 128; K a multiple of 64 and of group; any N.  16-byte aligned.
+ */
+size_t fc_w4_codes_bytes(int K, int N);
+fc_status fc_w4_pack(const void* d_w, int K, int N, int group, void* d_codes, void* d_scale, fc_stream s);
+
+/*
+ * y[M][N] = x[M][K] W for a few rows (M <= 16), W the bf16 [K][N] weights that
+ * (d_codes, d_scale) stand for.  x and y bf16 row-major, x 16-byte and y 2-byte
+ * aligned; sums in fp32, y rounded once.
+ */
+fc_status fc_w4_matvec(const void* d_x, const void* d_codes, const void* d_scale, int M, int K, int N, int group,
+                       void* d_y, fc_stream s);
+
+/* ------------------------------------------------------------------------
  * Acceptance (Section IV-D: every correct token from the start is accepted,
  * everything after the first error rejected; Eq. 7 counts tokens per step).
  * ------------------------------------------------------------------------ */

@@ -1,0 +1,448 @@
+// The paged 4-bit KV cache: block tables and slot maps built from request
+// lengths (fc_kv_pages_plan, fc_kv_pages_release), and keys and values
+// quantised into the pages and read back (fc_kv4_write, fc_kv4_read).
+//
+// A cached row x (128 values of one token and kv head) is held as
+//   s = bf16(max|x| / 7),  c_d = clamp(rint(x_d / s), -7, 7)  (ties to even; all 0 when s = 0),
+// the numbers c_d + 8 two to a byte (dimension 2i in byte i's low half), and
+// stands for c_d * s.  One scale a row keeps both attention products exact in
+// the tensor cores: a number in -7..7 is a bf16 value, and the scale
+// multiplies a whole key's score or probability instead of its 128 elements.
+#include <algorithm>
+
+#include "fc_common.cuh"
+#include "kv4.cuh"
+
+FC_DEFINE_ERROR_WORD(kv4)
+
+namespace {
+
+constexpr int HD = KV4_D;
+
+// ---------------------------------------------------------------------------
+// Pages.
+// ---------------------------------------------------------------------------
+constexpr int PL_THREADS = 512;
+constexpr int PL_CHUNK = PL_THREADS;  // requests scanned at a time, one a thread
+constexpr int PL_MIN_ROWS = 512;      // rows a CTA takes at least
+
+struct PlanArgs {
+  const int32_t *kv_len, *n_new;
+  int batch, shift, max_pages;
+  int32_t* table;
+  const int32_t* free_list;
+  int n_pages;
+  const int32_t* n_free_in;
+  const int32_t* path;
+  int path_cap, n_per_seq, rows_cap;
+  int32_t *cu, *seq, *pos, *slot, *src, *kv_out, *n_free_out;
+  unsigned int* err;
+};
+
+// Inclusive sums of two values over the block's threads (64-bit: lengths are
+// the caller's data, and their sum may pass 32 bits before it is refused).
+__device__ __forceinline__ void block_scan2(long long& a, long long& b, long long (*s_part)[2]) {
+  const int lane = threadIdx.x & 31, wp = threadIdx.x >> 5;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const long long x = __shfl_up_sync(0xFFFFFFFFu, a, o), y = __shfl_up_sync(0xFFFFFFFFu, b, o);
+    if (lane >= o) a += x, b += y;
+  }
+  if (lane == 31) s_part[wp][0] = a, s_part[wp][1] = b;
+  __syncthreads();
+  long long pa = 0, pb = 0;
+  for (int w = 0; w < wp; ++w) pa += s_part[w][0], pb += s_part[w][1];
+  a += pa, b += pb;
+}
+
+// Every CTA sums over all requests itself, a chunk of PL_CHUNK at a time, and
+// fills its own rows and its own requests' table entries, so one launch does
+// the whole plan with no CTA waiting for another.  The lengths are a few KB
+// that L2 serves; bound by latency at every size that a step has.
+__global__ void __launch_bounds__(PL_THREADS) k_pages_plan(PlanArgs a, int rows_per_cta) {
+  __shared__ long long s_part[PL_THREADS / 32][2];
+  __shared__ int32_t s_cu[PL_CHUNK + 1], s_kv[PL_CHUNK], s_have[PL_CHUNK], s_off[PL_CHUNK], s_more[PL_CHUNK];
+  const int tid = threadIdx.x;
+  const long long page = 1ll << a.shift;
+  int n_free = *a.n_free_in;
+  if (n_free < 0 || n_free > a.n_pages) {
+    if (blockIdx.x == 0 && tid == 0) fc_flag(FC_ERR_WORD(a.err), FC_EBIT_INVALID);
+    n_free = 0;
+  }
+  const int r_lo = (int)std::min<long long>((long long)blockIdx.x * rows_per_cta, a.rows_cap);
+  const int r_hi = (int)std::min<long long>((long long)r_lo + rows_per_cta, a.rows_cap);
+  long long row_base = 0, page_base = 0;
+  long long taken = 0;  // pages of the requests served so far (CTA 0)
+  for (int b0 = 0; b0 < a.batch; b0 += PL_CHUNK) {
+    const int b = b0 + tid;
+    long long kv = 0, n = 0;
+    bool ok = b < a.batch, bad = false;
+    if (ok) {
+      kv = a.kv_len[b];
+      n = a.n_new[b];
+      bad = kv < 0 || n < 0;
+      kv = std::max(kv, 0ll);
+      n = std::max(n, 0ll);
+    }
+    const long long have = (kv + page - 1) >> a.shift, need = (kv + n + page - 1) >> a.shift;
+    const bool fits = ok && !bad && need <= a.max_pages && kv + n <= 0x7FFFFFFFll;
+    long long rows_end = n, page_end = fits ? need - have : 0;
+    const long long more = page_end;
+    block_scan2(rows_end, page_end, s_part);
+    rows_end += row_base;
+    page_end += page_base;
+    const bool served = fits && rows_end <= a.rows_cap && (more == 0 || page_end <= n_free);
+    if (ok) {
+      s_cu[tid + 1] = (int32_t)std::min<long long>(rows_end, a.rows_cap);
+      s_kv[tid] = (int32_t)kv;
+      s_have[tid] = (int32_t)have;
+      s_off[tid] = (int32_t)std::min<long long>(page_end - more, n_free);
+      s_more[tid] = served ? (int32_t)more : -1;
+    }
+    if (tid == 0) s_cu[0] = (int32_t)std::min<long long>(row_base, a.rows_cap);
+    if (blockIdx.x == 0 && ok) {
+      a.cu[b + 1] = (int32_t)std::min<long long>(rows_end, a.rows_cap);
+      a.kv_out[b] = (int32_t)(served ? kv + n : kv);
+      if (b == 0) a.cu[0] = 0;
+      if (!served) fc_flag(FC_ERR_WORD(a.err), bad ? FC_EBIT_INVALID : FC_EBIT_CAPACITY);
+    }
+    const int in_chunk = min(PL_CHUNK, a.batch - b0);
+    // the last thread holds the chunk's sums
+    __syncthreads();  // s_part is read, the chunk's arrays are written
+    if (tid == PL_THREADS - 1) s_part[0][0] = rows_end, s_part[0][1] = page_end;
+    if (blockIdx.x == 0) taken += served ? more : 0;
+    // table entries of new pages: a warp a request
+    for (int i = (tid >> 5) * gridDim.x + blockIdx.x; i < in_chunk; i += (PL_THREADS / 32) * gridDim.x) {
+      const int m = s_more[i];
+      for (int j = tid & 31; j < m; j += 32)
+        a.table[(size_t)(b0 + i) * a.max_pages + s_have[i] + j] = a.free_list[n_free - 1 - s_off[i] - j];
+    }
+    // rows of this chunk's requests in [r_lo, r_hi)
+    const int lo = std::max(r_lo, s_cu[0]), hi = std::min(r_hi, s_cu[in_chunk]);
+    for (int r = lo + tid; r < hi; r += PL_THREADS) {
+      int x = 0, y = in_chunk;  // s_cu[x] <= r < s_cu[y]
+      while (y - x > 1) {
+        const int m = (x + y) >> 1;
+        if (s_cu[m] <= r) x = m;
+        else y = m;
+      }
+      const int q = b0 + x, j = r - s_cu[x], p = (int)((uint32_t)s_kv[x] + (uint32_t)j);
+      int slot = -1;
+      if (s_more[x] >= 0) {
+        const int pg = p >> a.shift;
+        const int id = pg < s_have[x] ? a.table[(size_t)q * a.max_pages + pg]
+                                      : a.free_list[n_free - 1 - s_off[x] - (pg - s_have[x])];
+        slot = id < 0 || id >= a.n_pages ? -1 : (id << a.shift) + (p & ((1 << a.shift) - 1));
+        if (id < 0 || id >= a.n_pages) fc_flag(FC_ERR_WORD(a.err), FC_EBIT_INVALID);
+      }
+      a.seq[r] = q;
+      a.pos[r] = p;
+      a.slot[r] = slot;
+      if (a.src) {
+        const int node = a.path ? (j < a.path_cap ? a.path[(size_t)q * a.path_cap + j] : -1) : j;
+        a.src[r] = node < 0 || node >= a.n_per_seq ? -1 : q * a.n_per_seq + node;
+      }
+    }
+    __syncthreads();
+    row_base = s_part[0][0];
+    page_base = s_part[0][1];
+    __syncthreads();
+  }
+  // rows past the last request's
+  const int total = (int)std::min<long long>(row_base, a.rows_cap);
+  for (int r = std::max(r_lo, total) + tid; r < r_hi; r += PL_THREADS) {
+    a.seq[r] = -1;
+    a.pos[r] = -1;
+    a.slot[r] = -1;
+    if (a.src) a.src[r] = -1;
+  }
+  if (blockIdx.x == 0) {
+    long long t2 = 0;
+    block_scan2(taken, t2, s_part);
+    if (tid == PL_THREADS - 1) *a.n_free_out = n_free - (int32_t)taken;
+    if (a.batch == 0 && tid == 0) a.cu[0] = 0;
+  }
+}
+
+// One CTA: the pages of request b past ceil(keep / page) go back on the free
+// list in request order.
+__global__ void __launch_bounds__(PL_THREADS) k_pages_release(const int32_t* kv_len, const int32_t* keep, int batch,
+                                                              int shift, const int32_t* table, int max_pages,
+                                                              int32_t* free_list, int n_pages,
+                                                              const int32_t* n_free_in, int32_t* n_free_out,
+                                                              int32_t* kv_out, unsigned int* err) {
+  __shared__ long long s_part[PL_THREADS / 32][2];
+  __shared__ long long s_base;
+  __shared__ int32_t s_first[PL_THREADS], s_n[PL_THREADS], s_at[PL_THREADS];
+  const int tid = threadIdx.x;
+  const long long page = 1ll << shift;
+  int n_free = *n_free_in;
+  bool flag = n_free < 0 || n_free > n_pages;
+  if (flag) n_free = n_pages;  // nothing can be given back
+  if (tid == 0) s_base = n_free;
+  __syncthreads();
+  for (int b0 = 0; b0 < batch; b0 += PL_THREADS) {
+    const int b = b0 + tid;
+    long long first = 0, n = 0, kv = 0, kp = 0;
+    if (b < batch) {
+      kv = kv_len[b];
+      kp = keep[b];
+      if (kv < 0 || kp < 0) flag = true;
+      kv = std::max(kv, 0ll);
+      kp = std::min(std::max(kp, 0ll), kv);
+      first = (kp + page - 1) >> shift;
+      const long long held = (kv + page - 1) >> shift;
+      if (held > max_pages) flag = true;
+      n = std::max(std::min<long long>(held, max_pages) - first, 0ll);
+    }
+    long long end = n, dummy = 0;
+    block_scan2(end, dummy, s_part);
+    const long long base = s_base;
+    const bool fits = b < batch && base + end <= n_pages;  // else the tables are not this pool's
+    if (b < batch) {
+      if (!fits && n > 0) flag = true;
+      kv_out[b] = (int32_t)(fits ? kp : kv);
+    }
+    s_first[tid] = (int32_t)first;
+    s_n[tid] = fits ? (int32_t)n : 0;
+    s_at[tid] = fits ? (int32_t)(base + end - n) : 0;
+    __syncthreads();
+    for (int i = tid >> 5; i < min(PL_THREADS, batch - b0); i += PL_THREADS / 32)  // a warp a request
+      for (int j = tid & 31; j < s_n[i]; j += 32)
+        free_list[s_at[i] + j] = table[(size_t)(b0 + i) * max_pages + s_first[i] + j];
+    // the requests that fit are a prefix of those with pages to give
+    long long given = fits ? n : 0, d2 = 0;
+    block_scan2(given, d2, s_part);
+    __syncthreads();
+    if (tid == PL_THREADS - 1) s_base = base + given;
+    __syncthreads();
+  }
+  if (flag) fc_flag(FC_ERR_WORD(err), FC_EBIT_INVALID);
+  if (tid == 0) *n_free_out = (*n_free_in < 0 || *n_free_in > n_pages) ? 0 : (int32_t)s_base;
+}
+
+// ---------------------------------------------------------------------------
+// Write and read.
+// ---------------------------------------------------------------------------
+constexpr int WR_THREADS = 128;
+constexpr int WR_LANES = HD / 8;                     // lanes a row: 8 dimensions (16 bytes of bf16) each
+constexpr int WR_GROUPS = WR_THREADS / WR_LANES;     // rows in flight a CTA
+
+struct KvRows {
+  const __nv_bfloat16 *k, *v;
+  int n_per_seq, n_src;
+  long long seq_stride, row_stride, head_stride;
+};
+
+// 8 values of a row (4 words of two) to 8 numbers of 4 bits, given the row's
+// scale.  x * (1 / s) is rounded onto a grid of 2^-11 before the rounding to
+// whole numbers.  x and s have 8 significant bits: with x = X 2^a, s = S 2^b
+// (X, S in 128..255) the quotient's distance from a tie (2k+1)/2 is
+// |2X 2^(a-b) - (2k+1) S| / 2S, and near a tie of at most 7.1 a - b >= -2, so
+// the numerator is 0 or at least 1/2 and the distance 0 or above 2^-10.  The
+// grid holds every tie and moves a value by at most 2^-12, so this is
+// rint(x / s) exactly, in three operations where a division takes about ten.
+__device__ __forceinline__ uint32_t quantise8(const uint4& x, float s) {
+  const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+  uint32_t out = 0;
+  if (s >= 0x1p-100f && s <= 0x1p100f) {
+    const float r = __frcp_rn(s);
+    constexpr float GRID = 6144.f;             // 1.5 * 2^12: neighbours are 2^-11 apart
+    constexpr float WHOLE = 12582912.f + 8.f;  // 1.5 * 2^23: neighbours are 1 apart; and the bias
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float lo = __uint_as_float(w[i] << 16), hi = __uint_as_float(w[i] & 0xFFFF0000u);
+      const float a = __fadd_rn(__fadd_rn(__fmaf_rn(lo, r, GRID), -GRID), WHOLE);
+      const float b = __fadd_rn(__fadd_rn(__fmaf_rn(hi, r, GRID), -GRID), WHOLE);
+      out |= (__float_as_uint(a) & 15u) << (8 * i);
+      out |= (__float_as_uint(b) & 15u) << (8 * i + 4);
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float lo = __uint_as_float(w[i] << 16), hi = __uint_as_float(w[i] & 0xFFFF0000u);
+      const float a = s > 0.f ? fminf(fmaxf(rintf(__fdiv_rn(lo, s)), -7.f), 7.f) : 0.f;
+      const float b = s > 0.f ? fminf(fmaxf(rintf(__fdiv_rn(hi, s)), -7.f), 7.f) : 0.f;
+      out |= (uint32_t)((int)a + 8) << (8 * i);
+      out |= (uint32_t)((int)b + 8) << (8 * i + 4);
+    }
+  }
+  return out;
+}
+
+// 16 lanes a (row, head, K or V): the largest magnitude from the bf16 bits
+// (as unsigned numbers they order like the magnitudes, infinities and NaN on
+// top), the scale, the numbers.
+__global__ void __launch_bounds__(WR_THREADS) k_kv4_write(KvRows x, const int32_t* __restrict__ src,
+                                                          const int32_t* __restrict__ slot, int rows, int Hkv,
+                                                          int shift, long long n_slots, uint32_t* __restrict__ kc,
+                                                          uint32_t* __restrict__ vc, __nv_bfloat16* __restrict__ ks,
+                                                          __nv_bfloat16* __restrict__ vs, unsigned int* err) {
+  const int lane = threadIdx.x % WR_LANES;
+  const long long items = (long long)rows * Hkv;
+  for (long long e = (long long)blockIdx.x * WR_GROUPS + threadIdx.x / WR_LANES; e < items;
+       e += (long long)gridDim.x * WR_GROUPS) {
+    const int r = (int)(e / Hkv), h = (int)(e - (long long)r * Hkv);
+    const int sl = slot[r];
+    const int at = src ? src[r] : r;
+    const bool live = sl >= 0 && sl < n_slots && at >= 0 && at < x.n_src;
+    if (!live && lane == 0 && h == 0 && (sl >= n_slots || (sl >= 0 && (at < 0 || at >= x.n_src))))
+      fc_flag(FC_ERR_WORD(err), FC_EBIT_INVALID);
+    if (!live) continue;  // the 16 lanes of a row agree
+    const int q = at / x.n_per_seq, i = at - q * x.n_per_seq;
+    const long long off = q * x.seq_stride + i * x.row_stride + h * x.head_stride;
+    const uint4 kx = reinterpret_cast<const uint4*>(x.k + off)[lane];
+    const uint4 vx = reinterpret_cast<const uint4*>(x.v + off)[lane];
+    auto top = [](const uint4& u) {
+      const uint32_t m = __vmaxu2(__vmaxu2(u.x & 0x7FFF7FFFu, u.y & 0x7FFF7FFFu),
+                                  __vmaxu2(u.z & 0x7FFF7FFFu, u.w & 0x7FFF7FFFu));
+      return std::max(m & 0xFFFFu, m >> 16);
+    };
+    uint32_t m = top(kx) | (top(vx) << 16);
+    const uint32_t group = 0xFFFFu << (threadIdx.x & 16);
+#pragma unroll
+    for (int o = 1; o < WR_LANES; o <<= 1) m = __vmaxu2(m, __shfl_xor_sync(group, m, o));
+    const long long row = ((long long)(sl >> shift) * Hkv + h) * (1 << shift) + (sl & ((1 << shift) - 1));
+    auto scale = [](uint32_t top_bits) {
+      const float t = __uint_as_float(top_bits << 16);
+      return top_bits >= 0x7F80u ? __ushort_as_bfloat16(0x7FC0) : __float2bfloat16_rn(__fdiv_rn(t, 7.f));
+    };
+    const __nv_bfloat16 sk = scale(m & 0xFFFFu), sv = scale(m >> 16);
+    kc[row * WR_LANES + lane] = quantise8(kx, __bfloat162float(sk));
+    vc[row * WR_LANES + lane] = quantise8(vx, __bfloat162float(sv));
+    if (lane == 0) ks[row] = sk;
+    if (lane == 1) vs[row] = sv;
+  }
+}
+
+__global__ void __launch_bounds__(WR_THREADS) k_kv4_read(const int32_t* __restrict__ slot, int rows, int Hkv, int shift,
+                                                         long long n_slots, const uint32_t* __restrict__ kc,
+                                                         const uint32_t* __restrict__ vc,
+                                                         const __nv_bfloat16* __restrict__ ks,
+                                                         const __nv_bfloat16* __restrict__ vs, uint4* __restrict__ k,
+                                                         uint4* __restrict__ v, unsigned int* err) {
+  const int lane = threadIdx.x % WR_LANES;
+  const long long items = (long long)rows * Hkv;
+  for (long long e = (long long)blockIdx.x * WR_GROUPS + threadIdx.x / WR_LANES; e < items;
+       e += (long long)gridDim.x * WR_GROUPS) {
+    const int r = (int)(e / Hkv), h = (int)(e - (long long)r * Hkv);
+    const int sl = slot[r];
+    if (sl >= n_slots && lane == 0 && h == 0) fc_flag(FC_ERR_WORD(err), FC_EBIT_INVALID);
+    uint4 ko = make_uint4(0, 0, 0, 0), vo = ko;
+    if (sl >= 0 && sl < n_slots) {
+      const long long row = ((long long)(sl >> shift) * Hkv + h) * (1 << shift) + (sl & ((1 << shift) - 1));
+      const uint32_t a = kc[row * WR_LANES + lane], b = vc[row * WR_LANES + lane];
+      const float sk = __bfloat162float(ks[row]), sv = __bfloat162float(vs[row]);
+      uint32_t* kw = &ko.x;
+      uint32_t* vw = &vo.x;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        auto val = [&](uint32_t w, int n, float s) { return (float)((int)((w >> (4 * n)) & 15u) - 8) * s; };
+        kw[i] = pack_bf16x2(val(a, 2 * i, sk), val(a, 2 * i + 1, sk));
+        vw[i] = pack_bf16x2(val(b, 2 * i, sv), val(b, 2 * i + 1, sv));
+      }
+    }
+    k[e * WR_LANES + lane] = ko;
+    v[e * WR_LANES + lane] = vo;
+  }
+}
+
+bool aligned(const void* p, uintptr_t n) { return reinterpret_cast<uintptr_t>(p) % n == 0; }
+
+unsigned grid_for(long long items) {
+  // at most 16 CTAs an SM: 2048 threads
+  return (unsigned)std::max<long long>(1, std::min<long long>((items + WR_GROUPS - 1) / WR_GROUPS, 152 * 16));
+}
+
+}  // namespace
+
+fc_status fc_kv4_check(const fc_kv4_cache* c) {
+  if (!c || c->n_pages < 1 || c->Hkv < 1) return FC_ERR_INVALID_ARG;
+  if (c->D != HD || kv4_page_shift(c->page_size) < 0 || (long long)c->n_pages * c->page_size > 0x7FFFFFFFll)
+    return FC_ERR_UNSUPPORTED;
+  if (!c->k_codes || !c->v_codes || !c->k_scale || !c->v_scale || !aligned(c->k_codes, 16) ||
+      !aligned(c->v_codes, 16) || !aligned(c->k_scale, 16) || !aligned(c->v_scale, 16))
+    return FC_ERR_INVALID_ARG;
+  return FC_OK;
+}
+
+extern "C" fc_status fc_kv_pages_plan(const int32_t* d_kv_len, const int32_t* d_n_new, int batch, int page_size,
+                                      int32_t* d_table, int max_pages, const int32_t* d_free, int n_pages,
+                                      const int32_t* d_n_free_in, const int32_t* d_path, int path_cap, int n_per_seq,
+                                      int rows_cap, int32_t* d_cu, int32_t* d_seq, int32_t* d_pos, int32_t* d_slot,
+                                      int32_t* d_src, int32_t* d_kv_len_out, int32_t* d_n_free_out,
+                                      fc_stream stream) {
+  FC_NVTX_RANGE();
+  const int shift = kv4_page_shift(page_size);
+  if (shift < 0) return FC_ERR_UNSUPPORTED;
+  if (batch < 0 || max_pages < 1 || n_pages < 1 || rows_cap < 0 || (long long)n_pages << shift > 0x7FFFFFFFll)
+    return FC_ERR_INVALID_ARG;
+  if (batch == 0 && rows_cap == 0) return FC_OK;
+  if ((batch && (!d_kv_len || !d_n_new || !d_table || !d_free || !d_kv_len_out)) || !d_n_free_in || !d_n_free_out ||
+      !d_cu || d_n_free_in == d_n_free_out || (batch && d_kv_len == d_kv_len_out))
+    return FC_ERR_INVALID_ARG;
+  if (rows_cap && (!d_seq || !d_pos || !d_slot)) return FC_ERR_INVALID_ARG;
+  if (d_src && (n_per_seq < 1 || (long long)batch * n_per_seq > 0x7FFFFFFFll || (d_path && path_cap < 1)))
+    return FC_ERR_INVALID_ARG;
+  PlanArgs a{d_kv_len, d_n_new,    batch,    shift,     max_pages, d_table, d_free, n_pages, d_n_free_in,
+             d_path,   path_cap,   n_per_seq, rows_cap, d_cu,      d_seq,   d_pos,  d_slot,  d_src,
+             d_kv_len_out, d_n_free_out, fc_error_slot()};
+  const int ctas = std::max(1, std::min((rows_cap + PL_MIN_ROWS - 1) / PL_MIN_ROWS, 152 * 4));
+  const int per = std::max(1, (rows_cap + ctas - 1) / ctas);
+  k_pages_plan<<<ctas, PL_THREADS, 0, static_cast<cudaStream_t>(stream)>>>(a, per);
+  return FC_CHECK_LAUNCH();
+}
+
+extern "C" fc_status fc_kv_pages_release(const int32_t* d_kv_len, const int32_t* d_keep, int batch, int page_size,
+                                         const int32_t* d_table, int max_pages, int32_t* d_free, int n_pages,
+                                         const int32_t* d_n_free_in, int32_t* d_kv_len_out, int32_t* d_n_free_out,
+                                         fc_stream stream) {
+  FC_NVTX_RANGE();
+  const int shift = kv4_page_shift(page_size);
+  if (shift < 0) return FC_ERR_UNSUPPORTED;
+  if (batch < 0 || max_pages < 1 || n_pages < 1) return FC_ERR_INVALID_ARG;
+  if (batch == 0) return FC_OK;
+  if (!d_kv_len || !d_keep || !d_table || !d_free || !d_n_free_in || !d_kv_len_out || !d_n_free_out ||
+      d_n_free_in == d_n_free_out || d_kv_len == d_kv_len_out)
+    return FC_ERR_INVALID_ARG;
+  k_pages_release<<<1, PL_THREADS, 0, static_cast<cudaStream_t>(stream)>>>(
+      d_kv_len, d_keep, batch, shift, d_table, max_pages, d_free, n_pages, d_n_free_in, d_n_free_out, d_kv_len_out,
+      fc_error_slot());
+  return FC_CHECK_LAUNCH();
+}
+
+extern "C" fc_status fc_kv4_write(const fc_kv4_cache* cache, const void* d_k, const void* d_v, int n_seq, int n_per_seq,
+                                  int64_t seq_stride, int64_t row_stride, int64_t head_stride, const int32_t* d_src,
+                                  const int32_t* d_slot, int rows, fc_stream stream) {
+  FC_NVTX_RANGE();
+  if (const fc_status st = fc_kv4_check(cache)) return st;
+  if (rows < 0 || n_seq < 0 || n_per_seq < 1 || seq_stride < 0 || row_stride < 0 || head_stride < 0 ||
+      (long long)n_seq * n_per_seq > 0x7FFFFFFFll)
+    return FC_ERR_INVALID_ARG;
+  if (rows == 0) return FC_OK;
+  if (!d_k || !d_v || !d_slot || !aligned(d_k, 16) || !aligned(d_v, 16) || seq_stride % 8 || row_stride % 8 ||
+      head_stride % 8 || (!d_src && rows > n_seq * n_per_seq))
+    return FC_ERR_INVALID_ARG;
+  KvRows x{static_cast<const __nv_bfloat16*>(d_k), static_cast<const __nv_bfloat16*>(d_v), n_per_seq,
+           n_seq * n_per_seq, seq_stride, row_stride, head_stride};
+  k_kv4_write<<<grid_for((long long)rows * cache->Hkv), WR_THREADS, 0, static_cast<cudaStream_t>(stream)>>>(
+      x, d_src, d_slot, rows, cache->Hkv, kv4_page_shift(cache->page_size), (long long)cache->n_pages * cache->page_size,
+      static_cast<uint32_t*>(cache->k_codes), static_cast<uint32_t*>(cache->v_codes),
+      static_cast<__nv_bfloat16*>(cache->k_scale), static_cast<__nv_bfloat16*>(cache->v_scale), fc_error_slot());
+  return FC_CHECK_LAUNCH();
+}
+
+extern "C" fc_status fc_kv4_read(const fc_kv4_cache* cache, const int32_t* d_slot, int rows, void* d_k, void* d_v,
+                                 fc_stream stream) {
+  FC_NVTX_RANGE();
+  if (const fc_status st = fc_kv4_check(cache)) return st;
+  if (rows < 0) return FC_ERR_INVALID_ARG;
+  if (rows == 0) return FC_OK;
+  if (!d_slot || !d_k || !d_v || !aligned(d_k, 16) || !aligned(d_v, 16)) return FC_ERR_INVALID_ARG;
+  k_kv4_read<<<grid_for((long long)rows * cache->Hkv), WR_THREADS, 0, static_cast<cudaStream_t>(stream)>>>(
+      d_slot, rows, cache->Hkv, kv4_page_shift(cache->page_size), (long long)cache->n_pages * cache->page_size,
+      static_cast<const uint32_t*>(cache->k_codes), static_cast<const uint32_t*>(cache->v_codes),
+      static_cast<const __nv_bfloat16*>(cache->k_scale), static_cast<const __nv_bfloat16*>(cache->v_scale),
+      static_cast<uint4*>(d_k), static_cast<uint4*>(d_v), fc_error_slot());
+  return FC_CHECK_LAUNCH();
+}

@@ -73,6 +73,11 @@ class fc_pipeline_desc(C.Structure):
                 ("n_parts", C.c_int32), ("parts", C.POINTER(fc_pipeline_part)), ("cache_weight", C.c_uint32)]
 
 
+class fc_kv4_cache(C.Structure):
+    _fields_ = [("k_codes", C.c_void_p), ("v_codes", C.c_void_p), ("k_scale", C.c_void_p), ("v_scale", C.c_void_p),
+                ("n_pages", C.c_int32), ("page_size", C.c_int32), ("Hkv", C.c_int32), ("D", C.c_int32)]
+
+
 EXPORTS = ["fc_status_string", "fc_version", "fc_get_error", "fc_datastore_build_workspace", "fc_datastore_build",
            "fc_datastore_build_noalloc", "fc_datastore_keys", "fc_datastore_save", "fc_datastore_file_info", "fc_datastore_load",
            "fc_retrieve", "fc_retrieve_all", "fc_retrieve_rev", "fc_reverse_tokens", "fc_rcache_bytes", "fc_rcache_init", "fc_rcache_lookup", "fc_rcache_insert", "fc_retrieve_cached",
@@ -81,7 +86,8 @@ EXPORTS = ["fc_status_string", "fc_version", "fc_get_error", "fc_datastore_build
            "fc_add_rmsnorm", "fc_silu_mul", "fc_rope_heads", "fc_selftest_wait", "fc_accept", "fc_argmax_accept", "fc_kv_append", "fc_synth_argmax",
            "fc_pipeline_create", "fc_pipeline_step", "fc_pipeline_step_part", "fc_pipeline_join_part", "fc_pipeline_stream", "fc_pipeline_error", "fc_pipeline_join",
            "fc_pipeline_capture_part", "fc_pipeline_graph_launch", "fc_pipeline_graph_kernels", "fc_pipeline_graph_destroy",
-           "fc_pipeline_destroy"]
+           "fc_pipeline_destroy", "fc_kv_pages_plan", "fc_kv_pages_release", "fc_kv4_write", "fc_kv4_read", "fc_kv4_attn",
+           "fc_kv4_attn_workspace", "fc_w4_codes_bytes", "fc_w4_pack", "fc_w4_matvec"]
 
 
 def _load():
@@ -165,6 +171,16 @@ def _load():
         "fc_pipeline_graph_launch": (C.c_int, [vp, vp]),
         "fc_pipeline_graph_kernels": (C.c_int, [vp, C.POINTER(C.c_int), C.POINTER(C.c_int)]),
         "fc_pipeline_graph_destroy": (None, [vp]),
+        "fc_kv_pages_plan": (C.c_int, [vp, vp, i32, i32, vp, i32, vp, i32, vp, vp, i32, i32, i32, vp, vp, vp, vp, vp, vp,
+                                       vp, vp]),
+        "fc_kv_pages_release": (C.c_int, [vp, vp, i32, i32, vp, i32, vp, i32, vp, vp, vp, vp]),
+        "fc_kv4_write": (C.c_int, [vp, vp, vp, i32, i32, C.c_int64, C.c_int64, C.c_int64, vp, vp, i32, vp]),
+        "fc_kv4_read": (C.c_int, [vp, vp, i32, vp, vp, vp]),
+        "fc_kv4_attn": (C.c_int, [vp, vp, vp, i32, vp, vp, vp, vp, vp, i32, i32, i32, C.c_float, vp, vp, sz, vp]),
+        "fc_kv4_attn_workspace": (sz, [i32, i32, i32, i32]),
+        "fc_w4_codes_bytes": (sz, [i32, i32]),
+        "fc_w4_pack": (C.c_int, [vp, i32, i32, i32, vp, vp, vp]),
+        "fc_w4_matvec": (C.c_int, [vp, vp, vp, i32, i32, i32, i32, vp, vp]),
     }
     for name, (res, args) in sig.items():
         f = getattr(lib, name)
@@ -773,6 +789,223 @@ def fc_rope_heads(x, col0, stride, out, B, n_pad, heads, D, pos, base):
     ptr = C.c_void_p(x.data_ptr() + col0 * x.element_size())
     _check("fc_rope_heads", LIB.fc_rope_heads(ptr, stride, _ptr(out), B, n_pad, heads, D, _ptr(pos), C.c_float(base),
                                               _stream()))
+    return out
+
+
+# ------------------------------------------------------ serving in four bits
+class KvPages:
+    """A pool of cache pages: the block tables [B, max_pages] and the free
+    list [n_pages] (int32 tensors owned by the caller; fc_kv_pages_plan and
+    fc_kv_pages_release update them).  ``page_size`` tokens a page."""
+
+    def __init__(self, page_size, table, free):
+        _need(table, torch.int32, "table")
+        _need(free, torch.int32, "free")
+        if table.dim() != 2 or free.dim() != 1:
+            raise ValueError("table must be [B, max_pages] and free [n_pages]")
+        self.page_size, self.table, self.free = int(page_size), table, free
+        self.batch, self.max_pages = table.shape
+        self.n_pages = free.numel()
+
+
+def kv_pages_outputs(batch, rows_cap, device, src=False):
+    """Output tensors of fc_kv_pages_plan (``src`` too when wanted)."""
+    e = lambda n: torch.empty(n, dtype=torch.int32, device=device)
+    o = dict(cu=e(batch + 1), seq=e(rows_cap), pos=e(rows_cap), slot=e(rows_cap), kv_len=e(batch), n_free=e(1))
+    if src:
+        o["src"] = e(rows_cap)
+    return o
+
+
+def fc_kv_pages_plan(pages: KvPages, kv_len, n_new, n_free, rows_cap=None, path=None, n_per_seq=0, out=None):
+    """Where a step's new tokens go: kv_len, n_new [B] and n_free [1] (int32)
+    to dict(cu [B + 1], seq, pos, slot [rows_cap], kv_len [B], n_free [1]);
+    pages.table gets the new pages.  With n_per_seq, also src [rows_cap] (see
+    fc_kv_pages_plan in the header; path [B, path_cap]: an accepted path).
+    Give ``rows_cap`` or ``out``."""
+    B = pages.batch
+    _need(kv_len, torch.int32, "kv_len", (B,))
+    _need(n_new, torch.int32, "n_new", (B,))
+    _need(n_free, torch.int32, "n_free", (1,))
+    if path is not None:
+        _need(path, torch.int32, "path")
+        if path.dim() != 2 or path.shape[0] != B or not n_per_seq:
+            raise ValueError("path must be [B, path_cap], with n_per_seq")
+    if out is None:
+        if rows_cap is None:
+            raise ValueError("give rows_cap or out")
+        out = kv_pages_outputs(B, rows_cap, kv_len.device, src=bool(n_per_seq))
+    src = out.get("src") if n_per_seq else None
+    if n_per_seq and src is None:
+        raise ValueError("out has no src")
+    _check("fc_kv_pages_plan", LIB.fc_kv_pages_plan(
+        kv_len.data_ptr(), n_new.data_ptr(), B, pages.page_size, pages.table.data_ptr(), pages.max_pages,
+        pages.free.data_ptr(), pages.n_pages, n_free.data_ptr(), None if path is None else path.data_ptr(),
+        0 if path is None else path.shape[1], n_per_seq, out["seq"].numel(), out["cu"].data_ptr(),
+        out["seq"].data_ptr(), out["pos"].data_ptr(), out["slot"].data_ptr(), None if src is None else src.data_ptr(),
+        out["kv_len"].data_ptr(), out["n_free"].data_ptr(), _stream()))
+    return out
+
+
+def fc_kv_pages_release(pages: KvPages, kv_len, keep, n_free, out=None):
+    """Request b keeps min(keep[b], kv_len[b]) tokens; the pages past them go
+    back to pages.free.  Returns (kv_len, n_free) afterwards."""
+    B = pages.batch
+    _need(kv_len, torch.int32, "kv_len", (B,))
+    _need(keep, torch.int32, "keep", (B,))
+    _need(n_free, torch.int32, "n_free", (1,))
+    kv_out, free_out = out if out is not None else (torch.empty_like(kv_len), torch.empty_like(n_free))
+    _check("fc_kv_pages_release", LIB.fc_kv_pages_release(
+        kv_len.data_ptr(), keep.data_ptr(), B, pages.page_size, pages.table.data_ptr(), pages.max_pages,
+        pages.free.data_ptr(), pages.n_pages, n_free.data_ptr(), kv_out.data_ptr(), free_out.data_ptr(), _stream()))
+    return kv_out, free_out
+
+
+class Kv4Cache:
+    """One layer's paged cache in 4 bits: k_codes, v_codes uint8 [n_pages,
+    Hkv, page_size, D / 2] and k_scale, v_scale bf16 [n_pages, Hkv, page_size]
+    (device tensors owned here)."""
+
+    def __init__(self, k_codes, v_codes, k_scale, v_scale):
+        _need(k_codes, torch.uint8, "k_codes")
+        if k_codes.dim() != 4:
+            raise ValueError("k_codes must be [n_pages, Hkv, page_size, D / 2]")
+        _need(v_codes, torch.uint8, "v_codes", k_codes.shape)
+        _need(k_scale, torch.bfloat16, "k_scale", k_codes.shape[:3])
+        _need(v_scale, torch.bfloat16, "v_scale", k_codes.shape[:3])
+        self.k_codes, self.v_codes, self.k_scale, self.v_scale = k_codes, v_codes, k_scale, v_scale
+        self.n_pages, self.Hkv, self.page_size = k_codes.shape[:3]
+        self.D = 2 * k_codes.shape[3]
+        self.view = fc_kv4_cache(k_codes.data_ptr(), v_codes.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr(),
+                                 self.n_pages, self.page_size, self.Hkv, self.D)
+        self.ref = C.c_void_p(C.addressof(self.view))
+
+    @classmethod
+    def empty(cls, n_pages, Hkv, page_size=64, D=128, device="cuda"):
+        return cls(*(torch.zeros((n_pages, Hkv, page_size, D // 2), dtype=torch.uint8, device=device) for _ in range(2)),
+                   *(torch.zeros((n_pages, Hkv, page_size), dtype=torch.bfloat16, device=device) for _ in range(2)))
+
+
+def fc_kv4_write(cache: Kv4Cache, k, v, slot, src=None):
+    """Quantise rows into the cache: k, v bf16 [rows, Hkv, D] or [B, n, Hkv, D]
+    of equal strides (any, the last dimension dense: parts of a fused
+    projection, or head-major tensors transposed), slot [rows] int32 (negative:
+    left out); src [rows] int32: the row of k, v (of B * n) that goes to a slot."""
+    if k.dtype is not torch.bfloat16 or v.dtype is not torch.bfloat16:
+        raise TypeError("k and v must be torch.bfloat16")
+    st, shape = k.stride(), k.shape
+    if not (k.is_cuda and v.is_cuda):
+        raise ValueError("k and v must be on a CUDA device")
+    if v.shape != shape or v.stride() != st:
+        raise ValueError("k and v must have the same shape and strides")
+    if len(shape) not in (3, 4) or shape[-2] != cache.Hkv or shape[-1] != cache.D or st[-1] != 1:
+        raise ValueError("k and v must be [rows, Hkv, D] or [B, n, Hkv, D] with a dense last dimension")
+    _need(slot, torch.int32, "slot")
+    rows = slot.numel()
+    if src is not None:
+        _need(src, torch.int32, "src", (rows,))
+    B, n = (1, shape[0]) if len(shape) == 3 else shape[:2]
+    if src is None and rows > B * n:
+        raise ValueError("more slots than rows")
+    _check("fc_kv4_write", LIB.fc_kv4_write(cache.ref, k.data_ptr(), v.data_ptr(), B, max(n, 1),
+                                            0 if len(shape) == 3 else st[0], st[-3], st[-2],
+                                            None if src is None else src.data_ptr(), slot.data_ptr(), rows, _stream()))
+
+
+def fc_kv4_read(cache: Kv4Cache, slot, out=None):
+    """The values that the rows at ``slot`` [rows] stand for, as bf16 (k, v),
+    each [rows, Hkv, D]; negative slots give zeros."""
+    _need(slot, torch.int32, "slot")
+    shape = (slot.numel(), cache.Hkv, cache.D)
+    if out is None:
+        out = tuple(torch.empty(shape, dtype=torch.bfloat16, device=slot.device) for _ in range(2))
+    k, v = out
+    _need(k, torch.bfloat16, "k", shape)
+    _need(v, torch.bfloat16, "v", shape)
+    _check("fc_kv4_read", LIB.fc_kv4_read(cache.ref, slot.data_ptr(), shape[0], k.data_ptr(), v.data_ptr(), _stream()))
+    return out
+
+
+def kv4_attn_workspace(B, n_pad, H, Hkv, device):
+    """A zeroed workspace for fc_kv4_attn at this shape.  Calls that may overlap
+    on different streams need one each."""
+    n = int(LIB.fc_kv4_attn_workspace(B, n_pad, H, Hkv))
+    return torch.zeros(max(n, 256), dtype=torch.uint8, device=device)
+
+
+def fc_kv4_attn(q, cache: Kv4Cache, table, kv_len, k_new=None, v_new=None, mask=None, n_nodes=None, scale=None, out=None,
+                workspace=None):
+    """Attention of q [B, n_pad, H, D] over the cache's tokens [0, kv_len[b]) in
+    pages table [B, max_pages] and the new tokens k_new, v_new [B, Hkv, n_pad,
+    D] (bf16; None: none) by mask [B, n_pad, ceil(n_pad / 64)] (int64 bits;
+    None: causal among the new).  n_nodes [B] (None: all n_pad).  workspace:
+    kv4_attn_workspace(...) or None (no key split)."""
+    _need(q, torch.bfloat16, "q")
+    B, Np, H, D = q.shape
+    Hkv = cache.Hkv
+    if D != cache.D:
+        raise ValueError("q and the cache differ in head dimension")
+    _need(table, torch.int32, "table")
+    if table.dim() != 2 or table.shape[0] != B:
+        raise ValueError("table must be [B, max_pages]")
+    _need(kv_len, torch.int32, "kv_len", (B,))
+    kp = vp = mp = np_ = None
+    if k_new is not None:
+        _need(k_new, torch.bfloat16, "k_new", (B, Hkv, Np, D))
+        _need(v_new, torch.bfloat16, "v_new", (B, Hkv, Np, D))
+        kp, vp = k_new.data_ptr(), v_new.data_ptr()
+    elif v_new is not None:
+        raise ValueError("k_new and v_new go together")
+    if mask is not None:
+        _need(mask, torch.int64, "mask", (B, Np, (Np + 63) // 64))
+        mp = mask.data_ptr()
+    if n_nodes is not None:
+        _need(n_nodes, torch.int32, "n_nodes", (B,))
+        np_ = n_nodes.data_ptr()
+    if out is None:
+        out = torch.empty_like(q)
+    else:
+        _need(out, torch.bfloat16, "out", q.shape)
+    ws, ws_bytes = (None, 0) if workspace is None else (workspace.data_ptr(), workspace.numel() * workspace.element_size())
+    _check("fc_kv4_attn", LIB.fc_kv4_attn(q.data_ptr(), cache.ref, table.data_ptr(), table.shape[1], kv_len.data_ptr(), kp,
+                                          vp, mp, np_, B, Np, H, D ** -0.5 if scale is None else float(scale),
+                                          out.data_ptr(), ws, ws_bytes, _stream()))
+    return out
+
+
+class W4Weight:
+    """Weights [K, N] in 4 bits, as fc_w4_pack lays them out for fc_w4_matvec:
+    codes (uint8), scale bf16 [K / group, N]."""
+
+    def __init__(self, codes, scale, K, N, group):
+        self.codes, self.scale, self.K, self.N, self.group = codes, scale, int(K), int(N), int(group)
+
+
+def fc_w4_pack(w, group=128) -> W4Weight:
+    """w bf16 [K, N] -> W4Weight, one scale for ``group`` weights of a column."""
+    _need(w, torch.bfloat16, "w")
+    K, N = w.shape
+    n = int(LIB.fc_w4_codes_bytes(K, N))
+    if n == 0:
+        raise ValueError("K must be a multiple of 64")
+    codes = torch.empty(n, dtype=torch.uint8, device=w.device)
+    scale = torch.empty((max(1, K // group), N), dtype=torch.bfloat16, device=w.device)
+    _check("fc_w4_pack", LIB.fc_w4_pack(w.data_ptr(), K, N, group, codes.data_ptr(), scale.data_ptr(), _stream()))
+    return W4Weight(codes, scale, K, N, group)
+
+
+def fc_w4_matvec(x, w: W4Weight, out=None):
+    """x bf16 [M, K] (M <= 16) times the weights: [M, N] bf16."""
+    _need(x, torch.bfloat16, "x")
+    M, K = x.shape
+    if K != w.K:
+        raise ValueError("inner dimensions differ")
+    if out is None:
+        out = torch.empty((M, w.N), dtype=torch.bfloat16, device=x.device)
+    else:
+        _need(out, torch.bfloat16, "out", (M, w.N))
+    _check("fc_w4_matvec", LIB.fc_w4_matvec(x.data_ptr(), w.codes.data_ptr(), w.scale.data_ptr(), M, K, w.N, w.group,
+                                            out.data_ptr(), _stream()))
     return out
 
 

@@ -1,0 +1,474 @@
+"""Serving in four bits on the GPU against the 64-bit oracle (oracle/kv4.py).
+
+Whole numbers (plans, numbers, scales) are equal.  bf16 has 8 significant
+bits, so a rounding to it moves a value by at most 2^-8 of itself.  Floating
+tolerances, per element:
+* attention: the output's rounding, 2^-8 |out|; each p's rounding, 2^-8 of A =
+  the mean of |v| under the same probabilities; and a score's fp32 error
+  (numbers may enter the product with a surplus of up to 136, sums of 128
+  terms: below 2^-22 * 136 * sum|q| * s * scale < 2^-12 here), which changes p
+  by as much again relative to the row sum: 2^-10 A.
+* product: the fp32 sums' error e, whose terms carry a surplus of 136, is
+  below 2^-20 * 136 * sum |x| s; the output lies between the roundings of
+  y - e and y + e.
+"""
+import numpy as np
+import pytest
+import torch
+
+from oracle import kv4 as o4
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def fc():
+    import paper_2502_17139_gb300.fastcoder as m
+    assert m.fc_get_error() == "FC_OK"
+    return m
+
+
+def dev(a):
+    return torch.from_numpy(np.ascontiguousarray(a)).cuda()
+
+
+def bf(rng, *shape, scale=1.0):
+    return torch.from_numpy((rng.standard_normal(shape) * scale).astype(np.float32)).bfloat16()
+
+
+def num(t):
+    return t.double().cpu().numpy()
+
+
+# ------------------------------------------------------------------ pages
+def pool(rng, kv, new, page, spare):
+    """Tables that hold kv, and a free list of what new needs plus spare pages."""
+    held = [-(-int(max(k, 0)) // page) for k in kv]
+    need = [-(-int(max(k, 0) + max(n, 0)) // page) for k, n in zip(kv, new)]
+    n_free = max(0, sum(need) - sum(held) + spare)
+    n_pages = sum(held) + n_free + 3
+    order = rng.permutation(n_pages).astype(np.int32)
+    table = np.full((len(kv), max(need) + 1), -1, np.int32)
+    at = n_free
+    for b, h in enumerate(held):
+        table[b, :h] = order[at:at + h]
+        at += h
+    free = np.full(n_pages, -1, np.int32)
+    free[:n_free] = order[:n_free]
+    return table, free, n_free
+
+
+def check_plan(fc, kv, new, page, table, free, n_free, rows_cap, path=None, n_per_seq=0, status="FC_OK"):
+    ref, _ = o4.pages_plan(kv, new, page, table, free, n_free, rows_cap, path, n_per_seq)
+    pages = fc.KvPages(page, dev(table), dev(free))
+    out = fc.fc_kv_pages_plan(pages, dev(kv), dev(new), dev(np.array([n_free], np.int32)), rows_cap=rows_cap,
+                              path=None if path is None else dev(path), n_per_seq=n_per_seq)
+    again = fc.fc_kv_pages_plan(pages, dev(kv), dev(new), dev(np.array([n_free], np.int32)), rows_cap=rows_cap,
+                                path=None if path is None else dev(path), n_per_seq=n_per_seq)
+    assert fc.fc_get_error() == status
+    for k in out:
+        assert np.array_equal(out[k].cpu().numpy(), ref[k]), k
+        assert torch.equal(out[k], again[k])
+    assert np.array_equal(pages.table.cpu().numpy(), ref["table"])
+    return pages, out
+
+
+@pytest.mark.parametrize("B,most_kv,most_new,page", [(1, 0, 1, 16), (1, 5000, 700, 64), (32, 16384, 1, 64), (33, 300, 40, 16),
+                                                     (512, 200, 9, 128), (513, 100, 90, 32), (1500, 70, 5, 256),
+                                                     (2, 100, 30000, 16)])
+def test_plan(fc, B, most_kv, most_new, page):
+    rng = np.random.default_rng(B + page)
+    kv = rng.integers(0, most_kv + 1, B).astype(np.int32)
+    new = rng.integers(0, most_new + 1, B).astype(np.int32)
+    new[0] = most_new
+    table, free, n_free = pool(rng, kv, new, page, 2)
+    check_plan(fc, kv, new, page, table, free, n_free, int(new.sum()) + (B % 3) * 7)
+
+
+def test_plan_paths_name_the_source_rows(fc):
+    rng = np.random.default_rng(7)
+    B, cap = 40, 12
+    kv, new = rng.integers(0, 90, B).astype(np.int32), rng.integers(1, 11, B).astype(np.int32)
+    path = np.full((B, cap), -1, np.int32)
+    for b in range(B):
+        path[b, :new[b]] = np.sort(rng.choice(64, new[b], replace=False))
+    path[3, 0] = 64  # outside its tree
+    table, free, n_free = pool(rng, kv, new, 16, 0)
+    check_plan(fc, kv, new, 16, table, free, n_free, int(new.sum()), path, 64)
+    check_plan(fc, kv, new, 16, table, free, n_free, int(new.sum()), None, 8)
+
+
+@pytest.mark.parametrize("case", ["pool", "table", "rows", "negative"])
+def test_plan_refuses_what_does_not_fit(fc, case):
+    rng = np.random.default_rng(11)
+    B, page = 700, 16
+    kv, new = rng.integers(0, 60, B).astype(np.int32), rng.integers(0, 60, B).astype(np.int32)
+    new[600:640] = 0
+    if case == "negative":
+        kv[5], new[650] = -3, -1
+    table, free, n_free = pool(rng, kv, new, page, -40 if case == "pool" else 0)
+    rows = int(np.maximum(new, 0).sum())
+    if case == "table":
+        table = np.ascontiguousarray(table[:, :6])
+    if case == "rows":
+        rows -= 100
+    check_plan(fc, kv, new, page, table, free, n_free, rows,
+               status="FC_ERR_INVALID_ARG" if case == "negative" else "FC_ERR_CAPACITY")
+
+
+def test_release_gives_the_pages_back_in_order(fc):
+    rng = np.random.default_rng(13)
+    B, page = 900, 16
+    kv, new = rng.integers(0, 80, B).astype(np.int32), np.zeros(B, np.int32)
+    table, free, n_free = pool(rng, kv, new, page, 5)
+    keep = np.where(rng.random(B) < 0.4, rng.integers(0, 90, B), kv).astype(np.int32)
+    want, at = free.copy(), n_free
+    for b in range(B):
+        k = min(keep[b], kv[b])
+        for j in range(-(-int(k) // page), -(-int(kv[b]) // page)):
+            want[at] = table[b, j]
+            at += 1
+    pages = fc.KvPages(page, dev(table), dev(free))
+    kv_out, free_out = fc.fc_kv_pages_release(pages, dev(kv), dev(keep), dev(np.array([n_free], np.int32)))
+    assert fc.fc_get_error() == "FC_OK"
+    assert np.array_equal(pages.free.cpu().numpy(), want) and free_out.item() == at
+    assert np.array_equal(kv_out.cpu().numpy(), np.minimum(keep, kv))
+    # a free count that leaves no room: nothing is written past the list
+    full = dev(np.array([len(free) - 4], np.int32))
+    pages = fc.KvPages(page, dev(table), dev(free))
+    _, free_out = fc.fc_kv_pages_release(pages, dev(kv), dev(np.zeros(B, np.int32)), full)
+    assert fc.fc_get_error() == "FC_ERR_INVALID_ARG" and len(free) - 4 <= free_out.item() <= len(free)
+
+
+# ------------------------------------------------------------- write, read
+def rows_of(rng, kind, R, H):
+    """(k, v) tensors of three layouts that hold the same kind of rows."""
+    if kind == "fused":
+        qkv = bf(rng, R, (2 * H + 2 * H) * 128).cuda()
+        return qkv[:, 2 * H * 128:3 * H * 128].view(R, H, 128), qkv[:, 3 * H * 128:].view(R, H, 128)
+    if kind == "heads":  # [B, Hkv, n, D], transposed in place
+        n = -(-R // 3)
+        k, v = bf(rng, 3, H, n, 128).cuda(), bf(rng, 3, H, n, 128).cuda()
+        return k.transpose(1, 2), v.transpose(1, 2)
+    return bf(rng, R, H, 128).cuda(), bf(rng, R, H, 128).cuda()
+
+
+@pytest.mark.parametrize("kind", ["dense", "fused", "heads"])
+@pytest.mark.parametrize("R,H,page", [(1, 1, 16), (7, 3, 16), (33, 8, 64), (300, 2, 256)])
+def test_write_and_read(fc, kind, R, H, page):
+    rng = np.random.default_rng(R * 7 + H)
+    k, v = rows_of(rng, kind, R, H)
+    k, v = k.clone(memory_format=torch.preserve_format) if kind == "dense" else k, v
+    flat = lambda t: num(t.reshape(-1, H, 128))
+    n_pages = -(-R // page) + 2
+    slot = rng.permutation(n_pages * page)[:R].astype(np.int32)
+    src = rng.permutation(flat(k).shape[0])[:R].astype(np.int32)
+    slot[R // 2] = -1 if R > 2 else slot[R // 2]
+    cache = fc.Kv4Cache.empty(n_pages, H, page)
+    fc.fc_kv4_write(cache, k, v, dev(slot), src=dev(src))
+    rk, rv = fc.fc_kv4_read(cache, dev(slot))
+    assert fc.fc_get_error() == "FC_OK"
+    for x, codes, scale, back in ((k, cache.k_codes, cache.k_scale, rk), (v, cache.v_codes, cache.v_scale, rv)):
+        c, s = o4.quantise(flat(x)[src])
+        want_c = np.zeros((n_pages, H, page, 64), np.uint8)
+        want_s = np.zeros((n_pages, H, page))
+        live = slot >= 0
+        want_c[slot[live] // page, :, slot[live] % page] = o4.pack(c)[live]
+        want_s[slot[live] // page, :, slot[live] % page] = s[live]
+        assert np.array_equal(codes.cpu().numpy(), want_c)  # and nothing else is written
+        assert np.array_equal(num(scale), want_s)
+        want = np.where(live[:, None, None], o4.bf16_round(c * s[..., None]), 0)
+        assert np.array_equal(num(back), want)
+
+
+def test_quantiser_at_ties_and_extremes(fc):
+    """Every bf16 mantissa against every scale mantissa: exact ties, values
+    just beside them, tiny and huge rows, zeros, NaN and infinities."""
+    rng = np.random.default_rng(17)
+    m = np.arange(128, 256)
+    rows = []
+    for top in m:  # the row's maximum; the others sweep mantissas and exponents
+        for e in (-1, -2, -3, -4):
+            r = np.zeros(128)
+            r[:128] = m * 2.0 ** e * rng.choice([-1, 1], 128)
+            r = np.where(np.abs(r) > top, 0, r)
+            r[rng.integers(128)] = top
+            rows.append(r)
+    rows = np.array(rows)
+    rows = np.concatenate([rows, rows[:40] * 2.0 ** 118, rows[40:80] * 2.0 ** -110, rows[80:120] * 2.0 ** -130,
+                           np.zeros((2, 128)), np.full((1, 128), 2.0 ** -133), rng.standard_normal((5, 128))])
+    x = torch.from_numpy(rows.astype(np.float32)).bfloat16()[:, None].cuda()
+    R = len(rows)
+    cache = fc.Kv4Cache.empty(-(-R // 16), 1, 16)
+    slot = torch.arange(R, dtype=torch.int32).cuda()
+    fc.fc_kv4_write(cache, x, -x, slot)
+    c, s = o4.quantise(num(x)[:, 0])
+    got = o4.unpack(cache.k_codes.cpu().numpy()).reshape(-1, 128)[:R]
+    assert np.array_equal(num(cache.k_scale).reshape(-1)[:R], s)
+    assert np.array_equal(got, c)
+    assert np.array_equal(o4.unpack(cache.v_codes.cpu().numpy()).reshape(-1, 128)[:R], -c)
+    x[3, 0, 5], x[4, 0, 6], x[5, 0, 7] = float("nan"), float("inf"), -float("inf")
+    fc.fc_kv4_write(cache, x, x, slot)
+    rk, rv = fc.fc_kv4_read(cache, slot[:8])
+    for t in (rk, rv):
+        assert torch.isnan(t[3:6]).all() and torch.isfinite(t[:3]).all() and torch.isfinite(t[6:]).all()
+    assert fc.fc_get_error() == "FC_OK"
+
+
+def test_write_and_read_leave_out_what_is_out_of_range(fc):
+    rng = np.random.default_rng(19)
+    k = bf(rng, 6, 2, 128).cuda()
+    cache = fc.Kv4Cache.empty(2, 2, 16)
+    fc.fc_kv4_write(cache, k, k, dev(np.array([0, 32, 5], np.int32)))  # two pages of 16: slot 32 is past the pool
+    assert fc.fc_get_error() == "FC_ERR_INVALID_ARG"
+    fc.fc_kv4_write(cache, k, k, dev(np.array([6, 7], np.int32)), src=dev(np.array([6, -1], np.int32)))
+    assert fc.fc_get_error() == "FC_ERR_INVALID_ARG"
+    c = cache.k_codes.cpu().numpy().reshape(2, 2, 16, 64)
+    assert c[0, :, [0, 5]].any() and not c[0, :, 6:].any() and not c[1].any()
+    out, _ = fc.fc_kv4_read(cache, dev(np.array([0, 1 << 20], np.int32)))
+    assert fc.fc_get_error() == "FC_ERR_INVALID_ARG" and not out[1].any()
+
+
+def test_write_binding_checks(fc):
+    cache = fc.Kv4Cache.empty(2, 2, 16)
+    k = torch.zeros((4, 2, 128), dtype=torch.bfloat16, device="cuda")
+    slot = torch.arange(4, dtype=torch.int32, device="cuda")
+    with pytest.raises(ValueError):
+        fc.fc_kv4_write(cache, k, k[:2], slot)
+    with pytest.raises(ValueError):
+        fc.fc_kv4_write(cache, k[:2], k[:2], slot)
+    with pytest.raises(ValueError):
+        fc.fc_kv4_write(cache, k[:, :1], k[:, :1], slot)
+    with pytest.raises(TypeError):
+        fc.fc_kv4_write(cache, k.float(), k.float(), slot)
+    with pytest.raises(TypeError):
+        fc.fc_kv4_write(cache, k, k, slot.long())
+
+
+# --------------------------------------------------------------- attention
+def random_cache(rng, n_pages, G, page):
+    codes = [np.clip(np.rint(rng.standard_normal((n_pages, G, page, 128)) * 2.6), -7, 7).astype(np.int64) for _ in range(2)]
+    scales = [o4.bf16_round(0.3 + 0.2 * rng.random((n_pages, G, page))) for _ in range(2)]
+    return codes, scales
+
+
+def tree_sees(rng, B, n):
+    """Ancestors and itself, random parents."""
+    s = np.zeros((B, n, n), bool)
+    for b in range(B):
+        for i in range(n):
+            if i:
+                s[b, i] = s[b, rng.integers(max(0, i - 6), i)]
+            s[b, i, i] = True
+    return s
+
+
+def mask_words(sees):
+    B, n, _ = sees.shape
+    w = np.zeros((B, n, (n + 63) // 64), np.uint64)
+    for j in range(n):
+        w[..., j // 64] |= sees[..., j].astype(np.uint64) << np.uint64(j % 64)
+    return w.view(np.int64)
+
+
+def attn_case(seed, B, n, H, G, lens, page, nodes=None, kind="tree", scale=None, spare=1, stale=True, qscale=1.0):
+    rng = np.random.default_rng(seed)
+    held = [-(-L // page) for L in lens]
+    n_pages, most = sum(held) + 1, max(held) + spare
+    codes, scales = random_cache(rng, n_pages, G, page)
+    order = rng.permutation(n_pages).astype(np.int32)
+    table = np.full((B, max(most, 1)), 0, np.int32)
+    at = 0
+    for b, h in enumerate(held):
+        table[b, :h] = order[at:at + h]
+        at += h
+        if stale and lens[b] % page:  # what stands past a request's end
+            for s in scales:
+                s[table[b, h - 1], :, lens[b] % page:] = np.nan
+    sees = tree_sees(rng, B, n) if kind == "tree" else np.broadcast_to(np.tril(np.ones((n, n), bool)), (B, n, n)).copy()
+    return dict(q=bf(rng, B, n, H, 128, scale=qscale), codes=codes, scales=scales, table=table, lens=np.asarray(lens, np.int32),
+                k_new=bf(rng, B, G, n, 128), v_new=bf(rng, B, G, n, 128), sees=sees, kind=kind,
+                nodes=np.asarray(nodes if nodes is not None else [n] * B, np.int32), scale=128 ** -0.5 if scale is None else scale)
+
+
+def gpu_cache(fc, c):
+    return fc.Kv4Cache(*(dev(o4.pack(x)) for x in c["codes"]),
+                       *(torch.from_numpy(s).to(torch.bfloat16).cuda() for s in c["scales"]))
+
+
+def run_attn(fc, c, new=True, ws=True, nodes=True, cache=None):
+    B, n, H, _ = c["q"].shape
+    cache = cache or gpu_cache(fc, c)
+    return fc.fc_kv4_attn(c["q"].cuda(), cache, dev(c["table"]), dev(c["lens"]), c["k_new"].cuda() if new else None,
+                          c["v_new"].cuda() if new else None, dev(mask_words(c["sees"])) if c["kind"] == "tree" else None,
+                          dev(c["nodes"]) if nodes else None, scale=c["scale"],
+                          workspace=fc.kv4_attn_workspace(B, n, H, cache.Hkv, "cuda") if ws else None)
+
+
+def check_attn(fc, c, new=True, **kw):
+    out = run_attn(fc, c, new=new, **kw)
+    assert fc.fc_get_error() == "FC_OK"
+    kn, vn = (num(c["k_new"]), num(c["v_new"])) if new else (None, None)
+    ref, size = o4.attn(num(c["q"]), *(o4.pack(x) for x in c["codes"]), *c["scales"], c["table"], c["lens"], kn, vn,
+                        c["sees"], c["nodes"], c["scale"])
+    got = num(out)
+    assert np.isfinite(got).all()
+    bad = np.abs(got - ref) - 2.0 ** -8 * np.abs(ref) - size * (2.0 ** -8 + 2.0 ** -10)
+    assert bad.max() <= 0, (bad.max(), np.unravel_index(bad.argmax(), bad.shape))
+    return out
+
+
+@pytest.mark.parametrize("lens", [[0], [1], [15, 16, 17], [63, 64, 65], [500, 0, 1, 129], [127, 128, 257]])
+@pytest.mark.parametrize("G,rep", [(1, 1), (2, 4), (1, 8), (1, 16)])
+def test_attn_one_token(fc, lens, G, rep):
+    check_attn(fc, attn_case(len(lens) + rep, len(lens), 1, G * rep, G, lens, 16 if len(lens) % 2 else 64))
+
+
+@pytest.mark.parametrize("n,H,G,page", [(2, 8, 2, 16), (5, 4, 4, 64), (8, 2, 1, 32), (9, 8, 2, 128), (16, 1, 1, 16),
+                                        (17, 4, 1, 64), (33, 2, 2, 256), (64, 4, 1, 64), (65, 6, 2, 16), (100, 4, 2, 32),
+                                        (127, 4, 1, 64), (128, 4, 1, 128), (128, 16, 1, 64)])
+@pytest.mark.parametrize("kind", ["tree", "causal"])
+def test_attn_trees(fc, n, H, G, page, kind):
+    lens = [300, 0, 131]
+    check_attn(fc, attn_case(n * 3 + H, 3, n, H, G, lens, page, nodes=[n, max(1, n // 2), max(1, n - 1)], kind=kind))
+
+
+@pytest.mark.parametrize("n,H,G", [(1, 8, 2), (3, 4, 4), (40, 4, 2), (128, 4, 1)])
+def test_attn_without_new_keys_and_without_any(fc, n, H, G):
+    """The cache alone; a request with no cache then has rows that see nothing."""
+    c = attn_case(n, 3, n, H, G, [200, 0, 33], 16)
+    out = check_attn(fc, c, new=False)
+    assert not out[1].any()
+
+
+@pytest.mark.parametrize("n,H,G", [(1, 8, 2), (12, 4, 4), (128, 4, 1)])
+def test_attn_masks_that_leave_a_row_empty(fc, n, H, G):
+    c = attn_case(n + 50, 2, n, H, G, [0, 40], 16, nodes=[max(1, n - 1), n])
+    c["sees"][:, 0] = False
+    out = check_attn(fc, c)
+    assert not out[0, 0].any() and out[1, 0].any()
+
+
+def test_attn_rows_past_the_nodes_and_a_request_without_nodes(fc):
+    c = attn_case(61, 3, 20, 4, 2, [70, 64, 5], 16, nodes=[0, 20, 3])
+    out = check_attn(fc, c)
+    assert not out[0].any() and not out[2, 3:].any() and out[1].any()
+
+
+@pytest.mark.parametrize("n,L", [(1, 40000), (4, 20000), (70, 6000)])
+def test_attn_long_and_split(fc, n, L):
+    """Few requests with many keys: the keys are split and the parts joined,
+    the same way every time, and alike without a workspace."""
+    c = attn_case(L, 2, n, 4, 1, [L, L // 3 + 1], 64)
+    if n > 1:
+        c["q"], c["nodes"] = c["q"], c["nodes"]
+    cache = gpu_cache(fc, c)
+    out = check_attn(fc, c, cache=cache)
+    for _ in range(4):
+        assert torch.equal(run_attn(fc, c, cache=cache), out)
+    one = run_attn(fc, c, cache=cache, ws=False)
+    assert (one.float() - out.float()).abs().max() <= 2 ** -6 * out.float().abs().max()
+
+
+@pytest.mark.parametrize("n", [1, 30])
+def test_attn_sharp_and_shifted_scores(fc, n):
+    """Queries that put all weight on few keys, late ones among them: the
+    running maximum has to move."""
+    c = attn_case(71 + n, 2, n, 4, 2, [700, 333], 32, qscale=12.0)
+    c["lens"] = np.asarray([700, 333], np.int32)
+    out = run_attn(fc, c)
+    ref, size = o4.attn(num(c["q"]), *(o4.pack(x) for x in c["codes"]), *c["scales"], c["table"], c["lens"],
+                        num(c["k_new"]), num(c["v_new"]), c["sees"], c["nodes"], c["scale"])
+    # scores reach 60: their fp32 errors (2^-22 * 136 * sum|q| s scale < 2^-8) are relative errors of p
+    assert np.all(np.abs(num(out) - ref) <= 2.0 ** -8 * np.abs(ref) + size * (2.0 ** -8 + 2.0 ** -7))
+
+
+@pytest.mark.parametrize("n", [1, 8, 90])
+def test_attn_refuses_bad_lengths_and_pages(fc, n):
+    c = attn_case(81, 3, n, 4, 2, [64, 64, 64], 16, spare=0)
+    good = run_attn(fc, c)
+    bad = dict(c, lens=np.asarray([64, 65, -1], np.int32))  # tables of four pages
+    out = run_attn(fc, bad)
+    assert fc.fc_get_error() == "FC_ERR_INVALID_ARG"
+    assert torch.equal(out[0], good[0]) and not out[1:].any()
+    bad = dict(c, nodes=np.asarray([n, n + 1, -1], np.int32))
+    out = run_attn(fc, bad)
+    assert fc.fc_get_error() == "FC_ERR_INVALID_ARG"
+    assert torch.equal(out[0], good[0]) and not out[1:].any()
+    # a page outside the pool: its keys are left out
+    t = c["table"].copy()
+    t[1, 3], t[2, 3] = 13, -5
+    out = run_attn(fc, dict(c, table=t))
+    assert fc.fc_get_error() == "FC_ERR_INVALID_ARG"
+    short = run_attn(fc, dict(c, lens=np.asarray([64, 48, 48], np.int32)))
+    assert (out.float() - short.float()).abs().max() <= 2 ** -6 * short.float().abs().max()
+    assert fc.fc_get_error() == "FC_OK"
+
+
+def test_attn_on_another_stream_and_in_a_graph(fc):
+    c = attn_case(91, 2, 3, 8, 2, [3000, 1000], 64)
+    cache, want = gpu_cache(fc, c), run_attn(fc, c)
+    args = [c["q"].cuda(), cache, dev(c["table"]), dev(c["lens"]), c["k_new"].cuda(), c["v_new"].cuda(),
+            dev(mask_words(c["sees"])), dev(c["nodes"])]
+    kw = dict(scale=c["scale"], out=torch.empty_like(args[0]), workspace=fc.kv4_attn_workspace(2, 3, 8, 2, "cuda"))
+    torch.cuda.synchronize()
+    s = torch.cuda.Stream()
+    with torch.cuda.stream(s):
+        assert torch.equal(fc.fc_kv4_attn(*args, **kw), want)
+    s.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        fc.fc_kv4_attn(*args, **kw)
+    for _ in range(3):
+        kw["out"].zero_()
+        g.replay()
+        assert torch.equal(kw["out"], want)
+
+
+# ------------------------------------------------------------------ product
+@pytest.mark.parametrize("M", [1, 2, 7, 8, 9, 16])
+@pytest.mark.parametrize("K,N,group", [(64, 1, 32), (64, 16, 64), (128, 33, 128), (320, 100, 64), (2048, 50, 32),
+                                       (448, 2500, 64), (1024, 2049, 128)])
+def test_matvec(fc, M, K, N, group):
+    rng = np.random.default_rng(M * K + N)
+    w, x = bf(rng, K, N, scale=K ** -0.5), bf(rng, M, K)
+    h = fc.fc_w4_pack(w.cuda(), group)
+    c, s = o4.quantise(num(w).reshape(K // group, group, N), 1)
+    assert np.array_equal(num(h.scale), s)
+    out = fc.fc_w4_matvec(x.cuda(), h)
+    assert fc.fc_get_error() == "FC_OK"
+    y, size = o4.matvec(num(x), num(w), group)
+    e = 2.0 ** -20 * 136 * size
+    got = num(out)
+    assert np.all((o4.bf16_round(y - e) <= got) & (got <= o4.bf16_round(y + e)))
+
+
+def test_matvec_of_unit_rows_reads_the_weights_back(fc):
+    """x = a unit row: the product is one row of the weights, so every number
+    of the packed layout is checked by itself."""
+    rng = np.random.default_rng(5)
+    K, N, group = 192, 37, 64
+    w = bf(rng, K, N)
+    c, s = o4.quantise(num(w).reshape(K // group, group, N), 1)
+    want = o4.bf16_round((c * s[:, None]).reshape(K, N))
+    h = fc.fc_w4_pack(w.cuda(), group)
+    eye = torch.eye(K, dtype=torch.bfloat16, device="cuda")
+    got = torch.cat([fc.fc_w4_matvec(eye[i:i + 16].contiguous(), h) for i in range(0, K, 16)])
+    assert np.array_equal(num(got), want)
+
+
+def test_matvec_extremes_and_refusals(fc):
+    K, N = 128, 40
+    w = torch.zeros((K, N), dtype=torch.bfloat16, device="cuda")
+    w[:, 1], w[3, 2], w[4, 3] = 2.0 ** -120, float("nan"), float("inf")
+    out = fc.fc_w4_matvec(torch.ones((2, K), dtype=torch.bfloat16, device="cuda"), fc.fc_w4_pack(w, 64))
+    assert not out[:, 0].any() and torch.isnan(out[:, 2:4]).all() and not out[:, 4:].any()
+    assert (out[:, 1].double() / (128 * 2.0 ** -120) - 1).abs().max() < 0.01
+    with pytest.raises(fc.FastCoderError):
+        fc.fc_w4_matvec(torch.ones((17, K), dtype=torch.bfloat16, device="cuda"), fc.fc_w4_pack(w, 64))
+    with pytest.raises(ValueError):
+        fc.fc_w4_matvec(torch.ones((2, 64), dtype=torch.bfloat16, device="cuda"), fc.fc_w4_pack(w, 64))
+    with pytest.raises(ValueError):
+        fc.fc_w4_pack(torch.zeros((100, 8), dtype=torch.bfloat16, device="cuda"), 32)
+    with pytest.raises(fc.FastCoderError):
+        fc.fc_w4_pack(w, 48)
