@@ -89,6 +89,602 @@ __global__ void __launch_bounds__(128) k_kv4_attn_row(Kv4Args a) {
       make_uint2(pack_bf16x2(o[0] * inv, o[1] * inv), pack_bf16x2(o[2] * inv, o[3] * inv));
 }
 
+
+// ---------------------------------------------------------------------------
+// Few query rows for a kv head (n_pad * H / Hkv <= 16: single tokens, small
+// trees).  The cache's read bounds this, so the work is what it costs to turn
+// 4-bit numbers into tensor-core operands as fast as they arrive.
+//
+// Keys and dimensions are the rows of mma.m16n8k16 (operand A, from the
+// cache), query rows its 8 columns:
+//   S^T [16 keys][8 rows] = K Q^T,   O^T [128 dims][8 rows] += V^T P^T.
+// fp16 operands: a number c + 8 in a 16-bit half's low bits IS the fp16
+// subnormal (c + 8) 2^-24, in the next four bits (c + 8) 2^-20, so a mask is
+// all that a pair needs, and a shift every second.  The products are exact.
+//   * The 8 too much comes off in the accumulators' start for S (-8 times the
+//     sum of the query) and through one more product a tile for O (-8 P^T).
+//   * Queries enter as fp16 times one power of two for the unit (its largest
+//     query value below 2^15) and, for the odd dimensions, 1/16.
+//   * The second product takes w = p * (value scale) * T in fp16, T a power of
+//     two per row that keeps the largest w seen between 2^6 and 2^14, moved
+//     lazily like the softmax's running maximum.
+// A warp takes every FEW_WARPS-th step of 16 keys (2112 bytes, one page's
+// rows in a row), four steps in flight by 16-byte asynchronous copies.  S^T
+// becomes P^T's operand by two 8x8 transposes in registers.
+// ---------------------------------------------------------------------------
+constexpr int FEW_WARPS = 8, FEW_THREADS = FEW_WARPS * 32;
+constexpr int STEP = 16;         // keys a step
+constexpr int FEW_STAGES = 4;    // steps in flight a warp
+constexpr int STEP_BYTES = 2 * STEP * KV4_ROW + 2 * STEP * 2;  // K rows, V rows, K scales, V scales
+constexpr int FEW_MIN_STEPS = 2 * FEW_WARPS;  // steps worth a CTA of their own
+constexpr float W_MAX = 16384.f;
+constexpr int T_START = 100;     // log2 T before the first key with a value
+
+template <int NT>
+struct FewSmem {
+  static constexpr int ROWS = 8 * NT;
+  static constexpr int RING = FEW_WARPS * FEW_STAGES * STEP_BYTES;
+  static constexpr int OUT_PITCH = HD + 4;  // floats a row of a warp's partial
+  static constexpr int MERGE = FEW_WARPS * ROWS * (OUT_PITCH + 2) * 4;
+  static constexpr int BYTES = RING > MERGE ? RING : MERGE;  // the partials take the ring's place
+};
+
+struct FewArgs {
+  Kv4Args a;
+  int split;         // 1: units are cut anywhere, by steps; 0: a CTA takes whole units
+  int* cnt;          // [units] arrivals at a cut unit, zero between calls
+  float* part;       // [grid][2][ROWS][HD + 2]: O unnormalised, m, l of a CTA's first and last piece
+};
+
+__device__ __forceinline__ void cp_async16(uint32_t dst, const void* src) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;\n" ::"r"(dst), "l"(src) : "memory");
+}
+__device__ __forceinline__ void cp_async_commit() { asm volatile("cp.async.commit_group;\n" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void cp_async_wait() {
+  asm volatile("cp.async.wait_group %0;\n" ::"n"(N) : "memory");
+}
+__device__ __forceinline__ void mma_f16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0,
+                                        uint32_t b1) {
+  asm volatile(
+      "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+      : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+      : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ void mma_bf16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0,
+                                         uint32_t b1) {
+  asm volatile(
+      "mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+      : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+      : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ uint32_t transpose8x8(uint32_t v) {
+  uint32_t r;
+  asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(v));
+  return r;
+}
+__device__ __forceinline__ uint32_t pack_f16x2(float lo, float hi) {
+  uint32_t r;
+  asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+  return r;
+}
+__device__ __forceinline__ float exp2_fast(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+__device__ __forceinline__ float pow2i(int e) { return __uint_as_float((uint32_t)(e + 127) << 23); }  // -126 <= e <= 127
+__device__ __forceinline__ int expo(float x) { return (int)((__float_as_uint(x) >> 23) & 255u) - 127; }
+__device__ __forceinline__ float lo_f(uint32_t w) { return __uint_as_float(w << 16); }
+__device__ __forceinline__ float hi_f(uint32_t w) { return __uint_as_float(w & 0xFFFF0000u); }
+
+// Byte offset of 16-byte chunk c (0..3) of row r (0..15) in a staged step:
+// rows 2j and 2j + 1 change places when j is odd, chunks by bit 1 of j, so
+// that four rows two apart (the V operand's) lie in different banks.
+__device__ __forceinline__ int swz(int r, int c) {
+  const int j = r >> 1;
+  return j * 128 + (((r ^ j) & 1) << 6) + ((c ^ (j & 2)) << 4);
+}
+
+struct FewUnit {
+  int b, g, nn, kvl, c_steps, steps;  // cached steps, all steps (>= 1)
+  bool fresh;                         // the last step holds the new tokens
+};
+
+__device__ __forceinline__ int few_steps(const Kv4Args& a, int b, int& nn, int& kvl, bool& bad) {
+  kvl = a.kv_len[b];
+  nn = a.n_nodes ? a.n_nodes[b] : a.n_pad;
+  bad = nn < 0 || nn > a.n_pad || kvl < 0 || kvl > (long long)a.max_pages << a.shift;
+  if (bad) nn = kvl = 0;
+  return nn == 0 ? 1 : max(1, (kvl + STEP - 1) / STEP + (a.k_new ? 1 : 0));
+}
+
+template <int NT>
+__global__ void __launch_bounds__(FEW_THREADS, NT == 1 ? 2 : 1) k_kv4_attn_few(FewArgs f) {
+  using L = FewSmem<NT>;
+  extern __shared__ __align__(1024) unsigned char smem[];
+  __shared__ long long s_total, s_begin;
+  __shared__ int s_b, s_last;
+  const Kv4Args& a = f.a;
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t = lane & 3;
+  const uint32_t ring = smem_u32(smem) + warp * (FEW_STAGES * STEP_BYTES);
+  const unsigned char* ring_p = smem + warp * (FEW_STAGES * STEP_BYTES);
+
+  // This CTA's share of all units' steps: [begin, end), from every request's length.
+  long long cur, end;
+  int b, n_cta = gridDim.x;
+  long long total = 0;
+  if (f.split) {
+    if (warp == 0) {
+      long long sum = 0;
+      int nn, kvl;
+      bool bad;
+      for (int i = lane; i < a.B; i += 32) sum += few_steps(a, i, nn, kvl, bad);
+#pragma unroll
+      for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, o);
+      const long long T = sum * a.Hkv;
+      const int n = (int)max(1ll, min((long long)gridDim.x, T / FEW_MIN_STEPS));
+      const long long start = (long long)blockIdx.x * T / n;
+      long long base = 0;  // steps of the requests before b0, times Hkv
+      int found = 0;
+      for (int b0 = 0; b0 < a.B; b0 += 32) {
+        long long mine = b0 + lane < a.B ? (long long)few_steps(a, b0 + lane, nn, kvl, bad) * a.Hkv : 0;
+        long long inc = mine;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+          const long long v = __shfl_up_sync(0xFFFFFFFFu, inc, o);
+          if (lane >= o) inc += v;
+        }
+        const uint32_t hit = __ballot_sync(0xFFFFFFFFu, mine > 0 && base + inc > start);
+        if (hit) {
+          const int w = __ffs(hit) - 1;
+          found = b0 + w;
+          base += __shfl_sync(0xFFFFFFFFu, inc - mine, w);
+          break;
+        }
+        base += __shfl_sync(0xFFFFFFFFu, inc, 31);
+      }
+      if (lane == 0) s_total = T, s_begin = base, s_b = found;
+    }
+    __syncthreads();
+    total = s_total;
+    n_cta = (int)max(1ll, min((long long)gridDim.x, total / FEW_MIN_STEPS));
+    if ((int)blockIdx.x >= n_cta) return;
+    cur = (long long)blockIdx.x * total / n_cta;
+    end = ((long long)blockIdx.x + 1) * total / n_cta;
+    b = s_b;
+  } else {
+    cur = blockIdx.x;  // a unit, not a step
+    end = (long long)a.B * a.Hkv;
+    b = 0;
+  }
+  long long req_base = f.split ? s_begin : 0;  // first step of request b
+
+  while (cur < end) {
+    // ---- the unit that cur lies in, and this CTA's steps [s0, s1) of it
+    int nn, kvl, gh, s0, s1, steps;
+    bool bad;
+    long long unit_base = 0;
+    if (f.split) {
+      steps = few_steps(a, b, nn, kvl, bad);
+      while (cur - req_base >= (long long)steps * a.Hkv) {
+        req_base += (long long)steps * a.Hkv;
+        ++b;
+        steps = few_steps(a, b, nn, kvl, bad);
+      }
+      gh = (int)((cur - req_base) / steps);
+      unit_base = req_base + (long long)gh * steps;
+      s0 = (int)(cur - unit_base);
+      s1 = (int)min((long long)steps, end - unit_base);
+      cur = unit_base + s1;
+    } else {
+      b = (int)(cur / a.Hkv);
+      gh = (int)(cur - (long long)b * a.Hkv);
+      steps = few_steps(a, b, nn, kvl, bad);
+      s0 = 0;
+      s1 = steps;
+      cur += gridDim.x;
+    }
+    if (bad && gh == 0 && s0 == 0 && tid == 0) fc_flag(FC_ERR_WORD(a.err), FC_EBIT_INVALID);
+    const int c_steps = nn == 0 ? 0 : (kvl + STEP - 1) / STEP;
+    const int R = nn * a.G;  // rows in use: node-major, r = node * G + head in group
+    auto q_row = [&](int r) { return a.q + (((size_t)b * a.n_pad + r / a.G) * a.H + gh * a.G + r % a.G) * HD; };
+
+    // ---- queries: the unit's power of two, then the operand registers
+    // k-step 2i of word i of a key's 16-byte quarter t: dimensions 32t + 8i +
+    // {0, 4} and {1, 5} / 16; k-step 2i + 1: {2, 6} and {3, 7} / 16
+    uint4 qw[NT][4];
+    uint32_t top = 0;
+#pragma unroll
+    for (int n = 0; n < NT; ++n)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        qw[n][i] = 8 * n + g < R ? reinterpret_cast<const uint4*>(q_row(8 * n + g))[4 * t + i] : make_uint4(0, 0, 0, 0);
+        const uint32_t* w = &qw[n][i].x;
+#pragma unroll
+        for (int x = 0; x < 4; ++x) {
+          const uint32_t l = w[x] & 0x7FFFu, h = (w[x] >> 16) & 0x7FFFu;  // finite values only
+          if (l < 0x7F80u) top = max(top, l);
+          if (h < 0x7F80u) top = max(top, h);
+        }
+      }
+    top = __reduce_max_sync(0xFFFFFFFFu, top);
+    const int qe = top ? min(max((int)(top >> 7) - 127, -100), 100) : 0;  // largest |q| < 2^(qe + 1) (or it overflows)
+    const float q_mul = pow2i(14 - qe), q_odd = q_mul * 0.0625f;
+    const float z_mul = a.scale_log2 * pow2i(qe + 10);  // undoes 2^(14 - qe) 2^-24
+    uint32_t qf[NT][8][2];
+    float s_init[NT][2];  // rows 8n + 2t, + 1: -8 2^-24 times the sum of the row
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+      float sum = 0.f;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const uint4 w = qw[n][i];
+        const float d0 = lo_f(w.x) * q_mul, d1 = hi_f(w.x) * q_odd, d2 = lo_f(w.y) * q_mul, d3 = hi_f(w.y) * q_odd;
+        const float d4 = lo_f(w.z) * q_mul, d5 = hi_f(w.z) * q_odd, d6 = lo_f(w.w) * q_mul, d7 = hi_f(w.w) * q_odd;
+        qf[n][2 * i][0] = pack_f16x2(d0, d4);
+        qf[n][2 * i][1] = pack_f16x2(d1, d5);
+        qf[n][2 * i + 1][0] = pack_f16x2(d2, d6);
+        qf[n][2 * i + 1][1] = pack_f16x2(d3, d7);
+        sum += ((d0 + d2) + (d4 + d6)) + 16.f * ((d1 + d3) + (d5 + d7));
+      }
+      sum += __shfl_xor_sync(0xFFFFFFFFu, sum, 1);
+      sum += __shfl_xor_sync(0xFFFFFFFFu, sum, 2);  // row g of the tile, in all four lanes t
+      sum *= -0x1p-21f;
+      s_init[n][0] = __shfl_sync(0xFFFFFFFFu, sum, 8 * t);      // row 2t is lane group g = 2t
+      s_init[n][1] = __shfl_sync(0xFFFFFFFFu, sum, 8 * t + 4);
+    }
+
+    float o[NT][8][4];  // [tile of 16 dims][c]: rows 2t + (c & 1), dims 16g + 2 mt + (c >> 1)
+    float m[NT][2], l[NT][2];
+    int te[NT][2];      // log2 T
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+#pragma unroll
+      for (int mt = 0; mt < 8; ++mt)
+#pragma unroll
+        for (int c = 0; c < 4; ++c) o[n][mt][c] = 0.f;
+      m[n][0] = m[n][1] = -INFINITY;
+      l[n][0] = l[n][1] = 0.f;
+      te[n][0] = te[n][1] = T_START;
+    }
+
+    // One step's softmax: scores z[c] (base 2, masked ones -inf) of keys g (c
+    // = 0, 1) and g + 8 (c = 2, 3), rows 2t + (c & 1), to probabilities; moves
+    // the running maximum when a score passes it by more than 8.
+    auto softmax = [&](int n, float (&z)[4], float (&p)[4]) {
+      const bool move = z[0] > m[n][0] + 8.f || z[2] > m[n][0] + 8.f || z[1] > m[n][1] + 8.f || z[3] > m[n][1] + 8.f;
+      if (__any_sync(0xFFFFFFFFu, move)) {
+#pragma unroll
+        for (int r = 0; r < 2; ++r) {
+          float mx = fmaxf(z[r], z[2 + r]);
+#pragma unroll
+          for (int x = 4; x < 32; x <<= 1) mx = fmaxf(mx, __shfl_xor_sync(0xFFFFFFFFu, mx, x));
+          const float mn = fmaxf(m[n][r], mx);
+          const float al = mn == -INFINITY ? 1.f : exp2_fast(m[n][r] - mn);
+          m[n][r] = mn;
+          l[n][r] *= al;
+#pragma unroll
+          for (int mt = 0; mt < 8; ++mt) o[n][mt][r] *= al, o[n][mt][2 + r] *= al;
+        }
+      }
+#pragma unroll
+      for (int r = 0; r < 2; ++r) {
+        const float mu = m[n][r] == -INFINITY ? 0.f : m[n][r];
+        p[r] = exp2_fast(z[r] - mu);
+        p[2 + r] = exp2_fast(z[2 + r] - mu);
+        l[n][r] += p[r] + p[2 + r];
+      }
+    };
+
+    // ---- cached steps of this warp: s0 + warp, s0 + warp + 8, ...
+    const int cs1 = min(s1, c_steps);
+    const int n_it = cs1 > s0 + warp ? (cs1 - s0 - warp + FEW_WARPS - 1) / FEW_WARPS : 0;
+    int ids = 0;            // page ids of the warp's next 32 steps, one a lane
+    uint32_t outside = 0;   // bit per stage: its step's page is not in the pool
+    auto issue = [&](int it) {
+      if (it < n_it) {
+        if ((it & 31) == 0) {
+          const int s = s0 + warp + (it + lane) * FEW_WARPS;
+          ids = s < cs1 ? a.table[(size_t)b * a.max_pages + (((long long)s * STEP) >> a.shift)] : 0;
+          if (ids < 0 || ids >= a.n_pages) ids = -1;
+        }
+        int id = __shfl_sync(0xFFFFFFFFu, ids, it & 31);
+        outside = (outside & ~(1u << (it % FEW_STAGES))) | ((id < 0 ? 1u : 0u) << (it % FEW_STAGES));
+        if (id < 0) id = 0;  // its keys are left out below
+        const int s = s0 + warp + it * FEW_WARPS;
+        const size_t row = (((size_t)id * a.Hkv + gh) << a.shift) + ((s * STEP) & ((1 << a.shift) - 1));
+        const uint32_t st = ring + (it % FEW_STAGES) * STEP_BYTES;
+        const int r = lane >> 2, c = lane & 3;
+        const uint32_t d0 = st + swz(r, c), d1 = st + swz(r + 8, c);
+        const uint8_t* k = a.kc + row * KV4_ROW + lane * 16;
+        const uint8_t* v = a.vc + row * KV4_ROW + lane * 16;
+        cp_async16(d0, k);
+        cp_async16(d1, k + 512);
+        cp_async16(d0 + STEP * KV4_ROW, v);
+        cp_async16(d1 + STEP * KV4_ROW, v + 512);
+        if (lane < 4)
+          cp_async16(st + 2 * STEP * KV4_ROW + lane * 16, (lane < 2 ? a.ks : a.vs) + row + (lane & 1) * 8);
+      }
+      cp_async_commit();
+    };
+#pragma unroll
+    for (int it = 0; it < FEW_STAGES - 1; ++it) issue(it);
+    for (int it = 0; it < n_it; ++it) {
+      cp_async_wait<FEW_STAGES - 2>();
+      __syncwarp();
+      const int s = s0 + warp + it * FEW_WARPS;
+      const unsigned char* st = ring_p + (it % FEW_STAGES) * STEP_BYTES;
+      const uint4 k0 = *reinterpret_cast<const uint4*>(st + swz(g, t));
+      const uint4 k1 = *reinterpret_cast<const uint4*>(st + swz(g + 8, t));
+      const uint16_t* sc = reinterpret_cast<const uint16_t*>(st + 2 * STEP * KV4_ROW);
+      float ks0 = __uint_as_float((uint32_t)sc[g] << 16) * z_mul, ks1 = __uint_as_float((uint32_t)sc[g + 8] << 16) * z_mul;
+      float vs0 = __uint_as_float((uint32_t)sc[16 + g] << 16), vs1 = __uint_as_float((uint32_t)sc[24 + g] << 16);
+      float z[NT][4];
+#pragma unroll
+      for (int n = 0; n < NT; ++n) z[n][0] = z[n][2] = s_init[n][0], z[n][1] = z[n][3] = s_init[n][1];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const uint32_t x = (&k0.x)[i], y = (&k1.x)[i];
+        const uint32_t x8 = x >> 8, y8 = y >> 8;
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+          mma_f16(z[n], x & 0x000F000Fu, y & 0x000F000Fu, x & 0x00F000F0u, y & 0x00F000F0u, qf[n][2 * i][0],
+                  qf[n][2 * i][1]);
+          mma_f16(z[n], x8 & 0x000F000Fu, y8 & 0x000F000Fu, x8 & 0x00F000F0u, y8 & 0x00F000F0u, qf[n][2 * i + 1][0],
+                  qf[n][2 * i + 1][1]);
+        }
+      }
+#pragma unroll
+      for (int n = 0; n < NT; ++n) z[n][0] *= ks0, z[n][1] *= ks0, z[n][2] *= ks1, z[n][3] *= ks1;
+      // keys past the request's end, or in a page outside the pool: no weight, whatever stands there
+      const int left = (outside >> (it % FEW_STAGES)) & 1u ? 0 : kvl - s * STEP;
+      if (left < STEP) {
+        if (left <= 0 && lane == 0) fc_flag(FC_ERR_WORD(a.err), FC_EBIT_INVALID);
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+          if (g >= left) z[n][0] = z[n][1] = -INFINITY;
+          if (g + 8 >= left) z[n][2] = z[n][3] = -INFINITY;
+        }
+        if (g >= left) vs0 = 0.f;
+        if (g + 8 >= left) vs1 = 0.f;
+      }
+      issue(it + FEW_STAGES - 1);
+      uint32_t pb[NT][2];
+#pragma unroll
+      for (int n = 0; n < NT; ++n) {
+        float p[4], w[4];
+        softmax(n, z[n], p);
+        auto weigh = [&]() {
+          const float t0 = pow2i(te[n][0]), t1 = pow2i(te[n][1]);
+          w[0] = p[0] * vs0 * t0;
+          w[1] = p[1] * vs0 * t1;
+          w[2] = p[2] * vs1 * t0;
+          w[3] = p[3] * vs1 * t1;
+        };
+        weigh();
+        if (__any_sync(0xFFFFFFFFu, w[0] > W_MAX || w[1] > W_MAX || w[2] > W_MAX || w[3] > W_MAX)) {
+#pragma unroll
+          for (int r = 0; r < 2; ++r) {
+            int e = max(w[r] > 0.f ? expo(p[r]) + expo(vs0) : -1000, w[2 + r] > 0.f ? expo(p[2 + r]) + expo(vs1) : -1000);
+#pragma unroll
+            for (int x = 4; x < 32; x <<= 1) e = max(e, __shfl_xor_sync(0xFFFFFFFFu, e, x));
+            const int tn = max(-90, min(te[n][r], 6 - e));
+            const float down = pow2i(max(tn - te[n][r], -126));
+#pragma unroll
+            for (int mt = 0; mt < 8; ++mt) o[n][mt][r] *= down, o[n][mt][2 + r] *= down;
+            te[n][r] = tn;
+          }
+          weigh();
+        }
+        pb[n][0] = transpose8x8(pack_f16x2(w[0], w[1]));
+        pb[n][1] = transpose8x8(pack_f16x2(w[2], w[3]));
+      }
+      // O^T: numbers of keys (2t, 2t + 1) and (2t + 8, 2t + 9), dims 16g ..
+      const unsigned char* vst = st + STEP * KV4_ROW + (g & 1) * 8;
+      const uint2 va = *reinterpret_cast<const uint2*>(vst + swz(2 * t, g >> 1));
+      const uint2 vb = *reinterpret_cast<const uint2*>(vst + swz(2 * t + 1, g >> 1));
+      const uint2 vc = *reinterpret_cast<const uint2*>(vst + swz(2 * t + 8, g >> 1));
+      const uint2 vd = *reinterpret_cast<const uint2*>(vst + swz(2 * t + 9, g >> 1));
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {  // four dims: a 16-bit part of each key's word
+        const uint32_t sel = (u & 1) ? 0x7632u : 0x5410u;
+        const uint32_t x = __byte_perm((&va.x)[u >> 1], (&vb.x)[u >> 1], sel);
+        const uint32_t y = __byte_perm((&vc.x)[u >> 1], (&vd.x)[u >> 1], sel);
+        const uint32_t x8 = x >> 8, y8 = y >> 8;
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+          mma_f16(o[n][2 * u], 0x80088008u, 0x80808080u, 0x80088008u, 0x80808080u, pb[n][0], pb[n][1]);
+          mma_f16(o[n][2 * u], x & 0x000F000Fu, x & 0x00F000F0u, y & 0x000F000Fu, y & 0x00F000F0u, pb[n][0], pb[n][1]);
+          mma_f16(o[n][2 * u + 1], 0x80088008u, 0x80808080u, 0x80088008u, 0x80808080u, pb[n][0], pb[n][1]);
+          mma_f16(o[n][2 * u + 1], x8 & 0x000F000Fu, x8 & 0x00F000F0u, y8 & 0x000F000Fu, y8 & 0x00F000F0u, pb[n][0],
+                  pb[n][1]);
+        }
+      }
+    }
+    cp_async_wait<0>();
+
+    // ---- the new tokens' step, in bf16: the warp whose turn it would be
+    if (a.k_new && nn > 0 && s1 == steps && warp == (steps - 1 - s0) % FEW_WARPS) {
+      const size_t nrow = ((size_t)b * a.Hkv + gh) * a.n_pad;
+      const uint4 zero = make_uint4(0, 0, 0, 0);
+      float z[NT][4];
+#pragma unroll
+      for (int n = 0; n < NT; ++n) z[n][0] = z[n][1] = z[n][2] = z[n][3] = 0.f;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const uint4 x = g < nn ? reinterpret_cast<const uint4*>(a.k_new + (nrow + g) * HD)[4 * t + i] : zero;
+        const uint4 y = g + 8 < nn ? reinterpret_cast<const uint4*>(a.k_new + (nrow + g + 8) * HD)[4 * t + i] : zero;
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+          const uint4 w = 8 * n + g < R ? reinterpret_cast<const uint4*>(q_row(8 * n + g))[4 * t + i] : zero;
+          mma_bf16(z[n], x.x, y.x, x.y, y.y, w.x, w.y);
+          mma_bf16(z[n], x.z, y.z, x.w, y.w, w.z, w.w);
+        }
+      }
+      const int words = (a.n_pad + 63) / 64;
+      uint32_t pb[NT][2];
+#pragma unroll
+      for (int n = 0; n < NT; ++n) {
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+          const int r = 8 * n + 2 * t + (c & 1), j = g + 8 * (c >> 1), i = r / a.G;
+          bool sees = r < R && j < nn;
+          if (sees) sees = a.mask ? (a.mask[((size_t)b * a.n_pad + i) * words] >> j) & 1 : j <= i;
+          z[n][c] = sees ? z[n][c] * a.scale_log2 : -INFINITY;
+        }
+        float p[4];
+        softmax(n, z[n], p);
+        // O holds O 2^-24 T (2^-20 T at odd dims): the weights take 2^-24 T, the odd dims' values 16
+        const float t0 = pow2i(te[n][0] - 24), t1 = pow2i(te[n][1] - 24);
+        pb[n][0] = transpose8x8(pack_bf16x2(p[0] * t0, p[1] * t1));
+        pb[n][1] = transpose8x8(pack_bf16x2(p[2] * t0, p[3] * t1));
+      }
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {  // 8 of the lane's 16 dims
+        uint4 v[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          const int j = 2 * t + (k & 1) + 8 * (k >> 1);
+          v[k] = j < nn ? reinterpret_cast<const uint4*>(a.v_new + (nrow + j) * HD)[2 * g + h] : zero;
+        }
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+          auto odd = [](uint32_t w) { return pack_bf16x2(lo_f(w) * 16.f, hi_f(w) * 16.f); };
+          const uint32_t a0 = __byte_perm((&v[0].x)[u], (&v[1].x)[u], 0x5410), a1 = odd(__byte_perm((&v[0].x)[u], (&v[1].x)[u], 0x7632));
+          const uint32_t a2 = __byte_perm((&v[2].x)[u], (&v[3].x)[u], 0x5410), a3 = odd(__byte_perm((&v[2].x)[u], (&v[3].x)[u], 0x7632));
+#pragma unroll
+          for (int n = 0; n < NT; ++n) mma_bf16(o[n][4 * h + u], a0, a1, a2, a3, pb[n][0], pb[n][1]);
+        }
+      }
+    }
+
+    // ---- join the warps, then the CTAs of a cut unit
+    __syncthreads();  // every warp is done with the ring
+    float* po = reinterpret_cast<float*>(smem);
+    float2* pml = reinterpret_cast<float2*>(po + FEW_WARPS * L::ROWS * L::OUT_PITCH);
+#pragma unroll
+    for (int n = 0; n < NT; ++n)
+#pragma unroll
+      for (int r = 0; r < 2; ++r) {
+        float sum = l[n][r];
+#pragma unroll
+        for (int x = 4; x < 32; x <<= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, x);
+        const int row = warp * L::ROWS + 8 * n + 2 * t + r;
+        const float up = pow2i(24 - te[n][r]), up_odd = up * 0.0625f;
+        float* dst = po + row * L::OUT_PITCH + 16 * g;
+#pragma unroll
+        for (int mt = 0; mt < 8; mt += 2)
+          *reinterpret_cast<float4*>(dst + 2 * mt) = make_float4(o[n][mt][r] * up, o[n][mt][2 + r] * up_odd,
+                                                                 o[n][mt + 1][r] * up, o[n][mt + 1][2 + r] * up_odd);
+        if (g == 0) pml[row] = make_float2(m[n][r], sum);
+      }
+    __syncthreads();
+    const bool whole = s0 == 0 && s1 == steps;
+    const int rows_all = a.n_pad * a.G;  // rows past the nodes are written as zeros
+    float* slot = whole ? nullptr
+                        : f.part + ((size_t)2 * blockIdx.x + ((long long)blockIdx.x * total / n_cta < unit_base ? 1 : 0)) *
+                                       (L::ROWS * (HD + 2));
+    auto put = [&](int r, int d4, const float4& v) {
+      const int i = r / a.G;
+      __nv_bfloat16* dst = a.out + (((size_t)b * a.n_pad + i) * a.H + gh * a.G + (r - i * a.G)) * HD + 4 * d4;
+      *reinterpret_cast<uint2*>(dst) = make_uint2(pack_bf16x2(v.x, v.y), pack_bf16x2(v.z, v.w));
+    };
+    for (int e = tid; e < rows_all * (HD / 4); e += FEW_THREADS) {
+      const int r = e / (HD / 4), d4 = e % (HD / 4);
+      if (r >= R) {
+        if (s0 == 0) put(r, d4, make_float4(0.f, 0.f, 0.f, 0.f));
+        continue;
+      }
+      float mx = -INFINITY;
+#pragma unroll
+      for (int w = 0; w < FEW_WARPS; ++w) mx = fmaxf(mx, pml[w * L::ROWS + r].x);
+      float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+      float sum = 0.f;
+#pragma unroll
+      for (int w = 0; w < FEW_WARPS; ++w) {
+        const float2 ml = pml[w * L::ROWS + r];
+        const float k = ml.x == -INFINITY ? 0.f : exp2_fast(ml.x - mx);
+        const float4 v = *reinterpret_cast<const float4*>(po + (w * L::ROWS + r) * L::OUT_PITCH + 4 * d4);
+        sum += ml.y * k;
+        acc.x += v.x * k, acc.y += v.y * k, acc.z += v.z * k, acc.w += v.w * k;
+      }
+      if (whole) {
+        const float inv = sum == 0.f ? 0.f : 1.f / sum;
+        put(r, d4, make_float4(acc.x * inv, acc.y * inv, acc.z * inv, acc.w * inv));
+      } else {
+        __stcg(reinterpret_cast<float4*>(slot + r * HD) + d4, acc);
+        if (d4 == 0) __stcg(reinterpret_cast<float2*>(slot + L::ROWS * HD) + r, make_float2(mx, sum));
+      }
+    }
+    if (!whole) {
+      // The last CTA to arrive adds up the pieces, in CTA order whichever it is.
+      __threadfence();
+      __syncthreads();
+      const long long last = unit_base + steps - 1;
+      const int c0 = (int)(((unit_base + 1) * n_cta - 1) / total), c1 = (int)(((last + 1) * n_cta - 1) / total);
+      const int unit = b * a.Hkv + gh;
+      if (tid == 0) s_last = atomicAdd(f.cnt + unit, 1) == c1 - c0;
+      __syncthreads();
+      if (s_last) {
+        __threadfence();
+        if (tid == 0) f.cnt[unit] = 0;  // fit for the next call
+        for (int e = tid; e < R * (HD / 4); e += FEW_THREADS) {
+          const int r = e / (HD / 4), d4 = e % (HD / 4);
+          float mx = -INFINITY, sum = 0.f;
+          float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+          for (int c = c0; c <= c1; ++c) {
+            const float* sl = f.part + ((size_t)2 * c + ((long long)c * total / n_cta < unit_base ? 1 : 0)) *
+                                           (L::ROWS * (HD + 2));
+            const float2 ml = __ldcg(reinterpret_cast<const float2*>(sl + L::ROWS * HD) + r);
+            const float4 v = __ldcg(reinterpret_cast<const float4*>(sl + r * HD) + d4);
+            const float mn = fmaxf(mx, ml.x);
+            const float ka = mx == -INFINITY ? 0.f : exp2_fast(mx - mn), kb = ml.x == -INFINITY ? 0.f : exp2_fast(ml.x - mn);
+            mx = mn;
+            sum = sum * ka + ml.y * kb;
+            acc.x = acc.x * ka + v.x * kb, acc.y = acc.y * ka + v.y * kb;
+            acc.z = acc.z * ka + v.z * kb, acc.w = acc.w * ka + v.w * kb;
+          }
+          const float inv = sum == 0.f ? 0.f : 1.f / sum;
+          put(r, d4, make_float4(acc.x * inv, acc.y * inv, acc.z * inv, acc.w * inv));
+        }
+      }
+    }
+    __syncthreads();  // the partials are read; the ring is free again
+  }
+}
+
+constexpr int FEW_GRID = 152 * 2;
+
+size_t few_cnt_bytes(int batch, int Hkv) { return ((size_t)batch * Hkv * sizeof(int) + 255) / 256 * 256; }
+
+template <int NT>
+fc_status launch_few(const Kv4Args& a, void* ws, size_t ws_bytes, cudaStream_t s) {
+  static std::atomic<unsigned long long> done{0};
+  const fc_status st = fc_once_per_device(done, [](int) {
+    return fc_cuda_status(cudaFuncSetAttribute(k_kv4_attn_few<NT>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                               FewSmem<NT>::BYTES));
+  });
+  if (st != FC_OK) return st;
+  const int full = NT == 1 ? FEW_GRID : FEW_GRID / 2;
+  const size_t cnt = few_cnt_bytes(a.B, a.Hkv), one = (size_t)2 * FewSmem<NT>::ROWS * (HD + 2) * sizeof(float);
+  const long long units = (long long)a.B * a.Hkv;
+  // at most what the tables could hold, in steps worth a CTA
+  const long long most = units * ((((long long)a.max_pages << a.shift) + STEP - 1) / STEP + 1);
+  int grid = (int)std::max<long long>(1, std::min<long long>(full, most / FEW_MIN_STEPS));
+  FewArgs f{a, 1, nullptr, nullptr};
+  if (ws && ws_bytes > cnt) grid = (int)std::min<size_t>(grid, (ws_bytes - cnt) / one);
+  if (!ws || ws_bytes <= cnt || grid < 1) {
+    f.split = 0;
+    grid = (int)std::min<long long>(units, 1 << 20);
+  } else {
+    f.cnt = static_cast<int*>(ws);
+    f.part = reinterpret_cast<float*>(static_cast<unsigned char*>(ws) + cnt);
+  }
+  k_kv4_attn_few<NT><<<grid, FEW_THREADS, FewSmem<NT>::BYTES, s>>>(f);
+  return FC_CHECK_LAUNCH();
+}
+
 bool aligned(const void* p, uintptr_t n) { return reinterpret_cast<uintptr_t>(p) % n == 0; }
 
 bool shape_ok(int n_pad, int H, int Hkv) {
@@ -99,7 +695,9 @@ bool shape_ok(int n_pad, int H, int Hkv) {
 
 extern "C" size_t fc_kv4_attn_workspace(int batch, int n_pad, int H, int Hkv) {
   if (batch < 1 || !shape_ok(n_pad, H, Hkv)) return 0;
-  return 256;
+  const int rows = n_pad * (H / Hkv);
+  if (rows > 16) return 256;
+  return few_cnt_bytes(batch, Hkv) + (size_t)FEW_GRID * 2 * 8 * (HD + 2) * sizeof(float);
 }
 
 extern "C" fc_status fc_kv4_attn(const void* d_q, const fc_kv4_cache* cache, const int32_t* d_table, int max_pages,
@@ -136,8 +734,12 @@ extern "C" fc_status fc_kv4_attn(const void* d_q, const fc_kv4_cache* cache, con
             kv4_page_shift(cache->page_size),
             scale * 1.4426950408889634f,
             fc_error_slot()};
+  cudaStream_t s = static_cast<cudaStream_t>(stream);
+  if ((long long)batch * a.Hkv > 0x7FFFFFFFll) return FC_ERR_UNSUPPORTED;
+  if (n_pad * a.G <= 8) return launch_few<1>(a, d_ws, ws_bytes, s);
+  if (n_pad * a.G <= 16) return launch_few<2>(a, d_ws, ws_bytes, s);
   const long long rows = (long long)batch * n_pad * H;
   if ((rows + 3) / 4 > 0x7FFFFFFFll) return FC_ERR_UNSUPPORTED;
-  k_kv4_attn_row<<<(unsigned)((rows + 3) / 4), 128, 0, static_cast<cudaStream_t>(stream)>>>(a);
+  k_kv4_attn_row<<<(unsigned)((rows + 3) / 4), 128, 0, s>>>(a);
   return FC_CHECK_LAUNCH();
 }
