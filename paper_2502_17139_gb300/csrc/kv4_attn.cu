@@ -101,24 +101,38 @@ __global__ void __launch_bounds__(128) k_kv4_attn_row(Kv4Args a) {
 // fp16 operands: a number c + 8 in a 16-bit half's low bits IS the fp16
 // subnormal (c + 8) 2^-24, in the next four bits (c + 8) 2^-20, so a mask is
 // all that a pair needs, and a shift every second.  The products are exact.
-//   * The 8 too much comes off in the accumulators' start for S (-8 times the
-//     sum of the query) and through one more product a tile for O (-8 P^T).
+//   * The 8 too much comes off S in the accumulators' start (-8 times the sum
+//     of the query), V by an addition a pair: off O by a second product it
+//     would leave errors of a large weight's size on dimensions where that
+//     key holds 0.
 //   * Queries enter as fp16 times one power of two for the unit (its largest
 //     query value below 2^15) and, for the odd dimensions, 1/16.
-//   * The second product takes w = p * (value scale) * T in fp16, T a power of
-//     two per row that keeps the largest w seen between 2^6 and 2^14, moved
-//     lazily like the softmax's running maximum.
-// A warp takes every FEW_WARPS-th step of 16 keys (2112 bytes, one page's
-// rows in a row), four steps in flight by 16-byte asynchronous copies.  S^T
-// becomes P^T's operand by two 8x8 transposes in registers.
+//   * The second product takes w = 2^(z - m) * (value scale) in fp16.  The
+//     row's reference m (O and the row sum are relative to it) moves when a w
+//     passes 2^15, to where the largest is 2^11 to 2^12: a running maximum of
+//     z + log2(value scale), moved lazily.  (High in fp16's range, so that a
+//     weight of 2^-25 of the largest keeps 11 bits.)  A key's scale counts as at least
+//     2^-80 in w, which no number of a row with a smaller one can show, so
+//     that 2^(z - m) stays below 2^95 in the row sum.
+// A warp takes every FEW_WARPS-th step of 32 keys (4224 bytes, two runs of 16
+// rows in a page), three steps in flight by 16-byte asynchronous copies.  S^T
+// becomes P^T's operand by 8x8 transposes in registers.
+//
+// Key 4g + i of a step (g = lane / 4) is row g of 8-row group i; groups 0, 1
+// and 2, 3 make the two products of 16 keys, so that a lane's scales are four
+// in a row.  Dimensions 32t .. 32t + 31 (t = lane % 4) are the lane's part of
+// K, 16g .. 16g + 15 its part of V, each as they lie in memory; the queries
+// are permuted to match.
 // ---------------------------------------------------------------------------
 constexpr int FEW_WARPS = 8, FEW_THREADS = FEW_WARPS * 32;
-constexpr int STEP = 16;         // keys a step
-constexpr int FEW_STAGES = 4;    // steps in flight a warp
-constexpr int STEP_BYTES = 2 * STEP * KV4_ROW + 2 * STEP * 2;  // K rows, V rows, K scales, V scales
-constexpr int FEW_MIN_STEPS = 2 * FEW_WARPS;  // steps worth a CTA of their own
-constexpr float W_MAX = 16384.f;
-constexpr int T_START = 100;     // log2 T before the first key with a value
+constexpr int STEP = 32;         // keys a step
+constexpr int FEW_STAGES = 3;    // steps in flight a warp
+constexpr int OFF_VROWS = STEP * KV4_ROW, OFF_KSC = 2 * STEP * KV4_ROW, OFF_VSC = OFF_KSC + STEP * 2;
+constexpr int STEP_BYTES = OFF_VSC + STEP * 2;
+constexpr int FEW_MIN_STEPS = FEW_WARPS;  // steps worth a CTA of their own
+constexpr float W_MAX = 32768.f;
+constexpr float VS_MIN = 0x1p-80f;
+constexpr float M_START = -1e30f;  // a reference before any key: 2^(z + 1e30) passes W_MAX, 2^(-1e30 - m) is 0
 
 template <int NT>
 struct FewSmem {
@@ -126,7 +140,8 @@ struct FewSmem {
   static constexpr int RING = FEW_WARPS * FEW_STAGES * STEP_BYTES;
   static constexpr int OUT_PITCH = HD + 4;  // floats a row of a warp's partial
   static constexpr int MERGE = FEW_WARPS * ROWS * (OUT_PITCH + 2) * 4;
-  static constexpr int BYTES = RING > MERGE ? RING : MERGE;  // the partials take the ring's place
+  static constexpr int JOIN = (ROWS * 152 * 2 + FEW_THREADS * 4) * 4;  // pieces' weights, subsets' sums
+  static constexpr int BYTES = RING > MERGE ? (RING > JOIN ? RING : JOIN) : (MERGE > JOIN ? MERGE : JOIN);
 };
 
 struct FewArgs {
@@ -168,6 +183,12 @@ __device__ __forceinline__ uint32_t pack_f16x2(float lo, float hi) {
   asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
   return r;
 }
+// The sum of two fp16 pairs (subnormals kept).
+__device__ __forceinline__ uint32_t less8(uint32_t v, uint32_t minus) {
+  uint32_t r;
+  asm("add.rn.f16x2 %0, %1, %2;" : "=r"(r) : "r"(v), "r"(minus));
+  return r;
+}
 __device__ __forceinline__ float exp2_fast(float x) {
   float y;
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
@@ -178,18 +199,13 @@ __device__ __forceinline__ int expo(float x) { return (int)((__float_as_uint(x) 
 __device__ __forceinline__ float lo_f(uint32_t w) { return __uint_as_float(w << 16); }
 __device__ __forceinline__ float hi_f(uint32_t w) { return __uint_as_float(w & 0xFFFF0000u); }
 
-// Byte offset of 16-byte chunk c (0..3) of row r (0..15) in a staged step:
-// rows 2j and 2j + 1 change places when j is odd, chunks by bit 1 of j, so
-// that four rows two apart (the V operand's) lie in different banks.
+// Byte offset of 16-byte chunk c (0..3) of row r (0..31) in a staged step:
+// two rows a 128-byte line, such that a quarter warp's 16-byte reads (rows
+// 8x + i and 8x + 4 + i) and a half warp's 8-byte reads (rows 8t + i, t =
+// 0..3, two chunks) each fall in different banks.
 __device__ __forceinline__ int swz(int r, int c) {
-  const int j = r >> 1;
-  return j * 128 + (((r ^ j) & 1) << 6) + ((c ^ (j & 2)) << 4);
+  return (((r & 3) | ((r >> 3) << 2)) << 7) | ((((r >> 2) ^ (r >> 3)) & 1) << 6) | ((c ^ (((r >> 4) & 1) << 1)) << 4);
 }
-
-struct FewUnit {
-  int b, g, nn, kvl, c_steps, steps;  // cached steps, all steps (>= 1)
-  bool fresh;                         // the last step holds the new tokens
-};
 
 __device__ __forceinline__ int few_steps(const Kv4Args& a, int b, int& nn, int& kvl, bool& bad) {
   kvl = a.kv_len[b];
@@ -337,170 +353,187 @@ __global__ void __launch_bounds__(FEW_THREADS, NT == 1 ? 2 : 1) k_kv4_attn_few(F
 
     float o[NT][8][4];  // [tile of 16 dims][c]: rows 2t + (c & 1), dims 16g + 2 mt + (c >> 1)
     float m[NT][2], l[NT][2];
-    int te[NT][2];      // log2 T
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
 #pragma unroll
       for (int mt = 0; mt < 8; ++mt)
 #pragma unroll
         for (int c = 0; c < 4; ++c) o[n][mt][c] = 0.f;
-      m[n][0] = m[n][1] = -INFINITY;
+      m[n][0] = m[n][1] = M_START;
       l[n][0] = l[n][1] = 0.f;
-      te[n][0] = te[n][1] = T_START;
     }
 
-    // One step's softmax: scores z[c] (base 2, masked ones -inf) of keys g (c
-    // = 0, 1) and g + 8 (c = 2, 3), rows 2t + (c & 1), to probabilities; moves
-    // the running maximum when a score passes it by more than 8.
-    auto softmax = [&](int n, float (&z)[4], float (&p)[4]) {
-      const bool move = z[0] > m[n][0] + 8.f || z[2] > m[n][0] + 8.f || z[1] > m[n][1] + 8.f || z[3] > m[n][1] + 8.f;
-      if (__any_sync(0xFFFFFFFFu, move)) {
+    // Scores z (base 2, masked ones -inf; z[i][r] of the lane's key i, row 2t
+    // + r) and value scales to w = 2^(z - m) vs; adds 2^(z - m) to the row
+    // sums; moves the references when a w is too large.
+    auto weigh = [&](int n, const float (&z)[4][2], const float (&vs)[4], float (&w)[4][2]) {
+      float p[4][2], sum = 0.f;
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
 #pragma unroll
         for (int r = 0; r < 2; ++r) {
-          float mx = fmaxf(z[r], z[2 + r]);
+          p[i][r] = exp2_fast(z[i][r] - m[n][r]);
+          w[i][r] = p[i][r] * vs[i];
+          sum += w[i][r];
+        }
+      if (__any_sync(0xFFFFFFFFu, sum > W_MAX)) {
 #pragma unroll
-          for (int x = 4; x < 32; x <<= 1) mx = fmaxf(mx, __shfl_xor_sync(0xFFFFFFFFu, mx, x));
-          const float mn = fmaxf(m[n][r], mx);
-          const float al = mn == -INFINITY ? 1.f : exp2_fast(m[n][r] - mn);
+        for (int r = 0; r < 2; ++r) {
+          float top = M_START;
+#pragma unroll
+          for (int i = 0; i < 4; ++i) top = fmaxf(top, z[i][r] + (float)(expo(vs[i]) - 11));
+#pragma unroll
+          for (int x = 4; x < 32; x <<= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, x));
+          const float mn = fmaxf(m[n][r], top), al = exp2_fast(m[n][r] - mn);
           m[n][r] = mn;
           l[n][r] *= al;
 #pragma unroll
           for (int mt = 0; mt < 8; ++mt) o[n][mt][r] *= al, o[n][mt][2 + r] *= al;
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            p[i][r] = exp2_fast(z[i][r] - mn);
+            w[i][r] = p[i][r] * vs[i];
+          }
         }
       }
 #pragma unroll
-      for (int r = 0; r < 2; ++r) {
-        const float mu = m[n][r] == -INFINITY ? 0.f : m[n][r];
-        p[r] = exp2_fast(z[r] - mu);
-        p[2 + r] = exp2_fast(z[2 + r] - mu);
-        l[n][r] += p[r] + p[2 + r];
-      }
+      for (int r = 0; r < 2; ++r) l[n][r] += (p[0][r] + p[1][r]) + (p[2][r] + p[3][r]);
     };
 
     // ---- cached steps of this warp: s0 + warp, s0 + warp + 8, ...
     const int cs1 = min(s1, c_steps);
     const int n_it = cs1 > s0 + warp ? (cs1 - s0 - warp + FEW_WARPS - 1) / FEW_WARPS : 0;
-    int ids = 0;            // page ids of the warp's next 32 steps, one a lane
-    uint32_t outside = 0;   // bit per stage: its step's page is not in the pool
-    auto issue = [&](int it) {
+    int id_a = 0, id_b = 0;  // page ids of the two runs of 16 keys of the warp's next 32 steps, one a lane
+    uint32_t outside = 0;    // bits 2 x stage, + 1: that run's page is not in the pool
+    const int32_t* tab = a.table + (size_t)b * a.max_pages;
+    auto issue = [&](int it, int stage) {
       if (it < n_it) {
-        if ((it & 31) == 0) {
-          const int s = s0 + warp + (it + lane) * FEW_WARPS;
-          ids = s < cs1 ? a.table[(size_t)b * a.max_pages + (((long long)s * STEP) >> a.shift)] : 0;
-          if (ids < 0 || ids >= a.n_pages) ids = -1;
-        }
-        int id = __shfl_sync(0xFFFFFFFFu, ids, it & 31);
-        outside = (outside & ~(1u << (it % FEW_STAGES))) | ((id < 0 ? 1u : 0u) << (it % FEW_STAGES));
-        if (id < 0) id = 0;  // its keys are left out below
         const int s = s0 + warp + it * FEW_WARPS;
-        const size_t row = (((size_t)id * a.Hkv + gh) << a.shift) + ((s * STEP) & ((1 << a.shift) - 1));
-        const uint32_t st = ring + (it % FEW_STAGES) * STEP_BYTES;
+        if ((it & 31) == 0) {
+          const long long key = (long long)(s + lane * FEW_WARPS) * STEP;
+          id_a = key < kvl ? tab[key >> a.shift] : 0;
+          id_b = key + 16 < kvl ? tab[(key + 16) >> a.shift] : 0;
+        }
+        int ia = __shfl_sync(0xFFFFFFFFu, id_a, it & 31), ib = __shfl_sync(0xFFFFFFFFu, id_b, it & 31);
+        const bool xa = (unsigned)ia >= (unsigned)a.n_pages, xb = (unsigned)ib >= (unsigned)a.n_pages;
+        outside &= ~(3u << (2 * stage));
+        if (xa || xb) {  // its keys are left out below
+          outside |= ((xa ? 1u : 0u) | (xb ? 2u : 0u)) << (2 * stage);
+          ia = xa ? 0 : ia;
+          ib = xb ? 0 : ib;
+          if (lane == 0) fc_flag(FC_ERR_WORD(a.err), FC_EBIT_INVALID);
+        }
+        const int in_page = (1 << a.shift) - 1;
+        const size_t ra = (((size_t)ia * a.Hkv + gh) << a.shift) + ((s * STEP) & in_page);
+        const size_t rb = (((size_t)ib * a.Hkv + gh) << a.shift) + ((s * STEP + 16) & in_page);
+        const uint32_t st = ring + stage * STEP_BYTES;
+        const uint8_t *ka = a.kc + ra * KV4_ROW + lane * 16, *kb = a.kc + rb * KV4_ROW + lane * 16;
+        const uint8_t *va = a.vc + ra * KV4_ROW + lane * 16, *vb = a.vc + rb * KV4_ROW + lane * 16;
         const int r = lane >> 2, c = lane & 3;
-        const uint32_t d0 = st + swz(r, c), d1 = st + swz(r + 8, c);
-        const uint8_t* k = a.kc + row * KV4_ROW + lane * 16;
-        const uint8_t* v = a.vc + row * KV4_ROW + lane * 16;
-        cp_async16(d0, k);
-        cp_async16(d1, k + 512);
-        cp_async16(d0 + STEP * KV4_ROW, v);
-        cp_async16(d1 + STEP * KV4_ROW, v + 512);
-        if (lane < 4)
-          cp_async16(st + 2 * STEP * KV4_ROW + lane * 16, (lane < 2 ? a.ks : a.vs) + row + (lane & 1) * 8);
+        cp_async16(st + swz(r, c), ka);
+        cp_async16(st + swz(r + 8, c), ka + 512);
+        cp_async16(st + swz(r + 16, c), kb);
+        cp_async16(st + swz(r + 24, c), kb + 512);
+        cp_async16(st + OFF_VROWS + swz(r, c), va);
+        cp_async16(st + OFF_VROWS + swz(r + 8, c), va + 512);
+        cp_async16(st + OFF_VROWS + swz(r + 16, c), vb);
+        cp_async16(st + OFF_VROWS + swz(r + 24, c), vb + 512);
+        if (lane < 8)  // K scales of the two runs, then V scales
+          cp_async16(st + OFF_KSC + lane * 16, (lane < 4 ? a.ks : a.vs) + ((lane & 2) ? rb : ra) + (lane & 1) * 8);
       }
       cp_async_commit();
     };
 #pragma unroll
-    for (int it = 0; it < FEW_STAGES - 1; ++it) issue(it);
+    for (int it = 0; it < FEW_STAGES - 1; ++it) issue(it, it);
+    int stage = 0;
     for (int it = 0; it < n_it; ++it) {
       cp_async_wait<FEW_STAGES - 2>();
       __syncwarp();
-      const int s = s0 + warp + it * FEW_WARPS;
-      const unsigned char* st = ring_p + (it % FEW_STAGES) * STEP_BYTES;
-      const uint4 k0 = *reinterpret_cast<const uint4*>(st + swz(g, t));
-      const uint4 k1 = *reinterpret_cast<const uint4*>(st + swz(g + 8, t));
-      const uint16_t* sc = reinterpret_cast<const uint16_t*>(st + 2 * STEP * KV4_ROW);
-      float ks0 = __uint_as_float((uint32_t)sc[g] << 16) * z_mul, ks1 = __uint_as_float((uint32_t)sc[g + 8] << 16) * z_mul;
-      float vs0 = __uint_as_float((uint32_t)sc[16 + g] << 16), vs1 = __uint_as_float((uint32_t)sc[24 + g] << 16);
-      float z[NT][4];
+      const unsigned char* st = ring_p + stage * STEP_BYTES;
+      const int left = kvl - (s0 + warp + it * FEW_WARPS) * STEP;  // keys of the request from here on
+      const uint32_t out_now = (outside >> (2 * stage)) & 3u;
+      {
+        const int ahead = stage == 0 ? FEW_STAGES - 1 : stage - 1;  // the stage read in the last turn
+        issue(it + FEW_STAGES - 1, ahead);
+      }
+      const uint2 ks2 = *reinterpret_cast<const uint2*>(st + OFF_KSC + 8 * g);
+      const uint2 vs2 = *reinterpret_cast<const uint2*>(st + OFF_VSC + 8 * g);
+      const float ks[4] = {lo_f(ks2.x), hi_f(ks2.x), lo_f(ks2.y), hi_f(ks2.y)};
+      float vs[4] = {lo_f(vs2.x), hi_f(vs2.x), lo_f(vs2.y), hi_f(vs2.y)};
+      float z[NT][4][2];
 #pragma unroll
-      for (int n = 0; n < NT; ++n) z[n][0] = z[n][2] = s_init[n][0], z[n][1] = z[n][3] = s_init[n][1];
+      for (int h = 0; h < 2; ++h) {  // keys 4g + 2h, 4g + 2h + 1
+        const uint4 k0 = *reinterpret_cast<const uint4*>(st + swz(4 * g + 2 * h, t));
+        const uint4 k1 = *reinterpret_cast<const uint4*>(st + swz(4 * g + 2 * h + 1, t));
+        float d[NT][4];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const uint32_t x = (&k0.x)[i], y = (&k1.x)[i];
-        const uint32_t x8 = x >> 8, y8 = y >> 8;
+        for (int n = 0; n < NT; ++n) d[n][0] = d[n][2] = s_init[n][0], d[n][1] = d[n][3] = s_init[n][1];
 #pragma unroll
-        for (int n = 0; n < NT; ++n) {
-          mma_f16(z[n], x & 0x000F000Fu, y & 0x000F000Fu, x & 0x00F000F0u, y & 0x00F000F0u, qf[n][2 * i][0],
-                  qf[n][2 * i][1]);
-          mma_f16(z[n], x8 & 0x000F000Fu, y8 & 0x000F000Fu, x8 & 0x00F000F0u, y8 & 0x00F000F0u, qf[n][2 * i + 1][0],
-                  qf[n][2 * i + 1][1]);
+        for (int i = 0; i < 4; ++i) {
+          const uint32_t x = (&k0.x)[i], y = (&k1.x)[i];
+          const uint32_t x8 = x >> 8, y8 = y >> 8;
+#pragma unroll
+          for (int n = 0; n < NT; ++n) {
+            mma_f16(d[n], x & 0x000F000Fu, y & 0x000F000Fu, x & 0x00F000F0u, y & 0x00F000F0u, qf[n][2 * i][0],
+                    qf[n][2 * i][1]);
+            mma_f16(d[n], x8 & 0x000F000Fu, y8 & 0x000F000Fu, x8 & 0x00F000F0u, y8 & 0x00F000F0u, qf[n][2 * i + 1][0],
+                    qf[n][2 * i + 1][1]);
+          }
         }
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+          for (int c = 0; c < 4; ++c) z[n][2 * h + (c >> 1)][c & 1] = d[n][c] * (ks[2 * h + (c >> 1)] * z_mul);
       }
 #pragma unroll
-      for (int n = 0; n < NT; ++n) z[n][0] *= ks0, z[n][1] *= ks0, z[n][2] *= ks1, z[n][3] *= ks1;
-      // keys past the request's end, or in a page outside the pool: no weight, whatever stands there
-      const int left = (outside >> (it % FEW_STAGES)) & 1u ? 0 : kvl - s * STEP;
-      if (left < STEP) {
-        if (left <= 0 && lane == 0) fc_flag(FC_ERR_WORD(a.err), FC_EBIT_INVALID);
+      for (int i = 0; i < 4; ++i) vs[i] = vs[i] < VS_MIN ? VS_MIN : vs[i];  // a NaN stays
+      if (left < STEP || out_now) {
+        // keys past the request's end, or in a page outside the pool: no weight, whatever stands there
 #pragma unroll
-        for (int n = 0; n < NT; ++n) {
-          if (g >= left) z[n][0] = z[n][1] = -INFINITY;
-          if (g + 8 >= left) z[n][2] = z[n][3] = -INFINITY;
+        for (int i = 0; i < 4; ++i) {
+          const int j = 4 * g + i;
+          if (j >= left || ((out_now >> (j >> 4)) & 1u)) {
+            vs[i] = VS_MIN;
+#pragma unroll
+            for (int n = 0; n < NT; ++n) z[n][i][0] = z[n][i][1] = -INFINITY;
+          }
         }
-        if (g >= left) vs0 = 0.f;
-        if (g + 8 >= left) vs1 = 0.f;
       }
-      issue(it + FEW_STAGES - 1);
-      uint32_t pb[NT][2];
+      uint32_t pb[NT][4];
 #pragma unroll
       for (int n = 0; n < NT; ++n) {
-        float p[4], w[4];
-        softmax(n, z[n], p);
-        auto weigh = [&]() {
-          const float t0 = pow2i(te[n][0]), t1 = pow2i(te[n][1]);
-          w[0] = p[0] * vs0 * t0;
-          w[1] = p[1] * vs0 * t1;
-          w[2] = p[2] * vs1 * t0;
-          w[3] = p[3] * vs1 * t1;
-        };
-        weigh();
-        if (__any_sync(0xFFFFFFFFu, w[0] > W_MAX || w[1] > W_MAX || w[2] > W_MAX || w[3] > W_MAX)) {
+        float w[4][2];
+        weigh(n, z[n], vs, w);
 #pragma unroll
-          for (int r = 0; r < 2; ++r) {
-            int e = max(w[r] > 0.f ? expo(p[r]) + expo(vs0) : -1000, w[2 + r] > 0.f ? expo(p[2 + r]) + expo(vs1) : -1000);
+        for (int i = 0; i < 4; ++i) pb[n][i] = transpose8x8(pack_f16x2(w[i][0], w[i][1]));
+      }
+      // O^T: in product h, k 2t, 2t + 1 are rows 2t, 2t + 1 of group 2h (keys
+      // 8t + 2h, 8t + 4 + 2h), k 2t + 8, + 9 those of group 2h + 1
 #pragma unroll
-            for (int x = 4; x < 32; x <<= 1) e = max(e, __shfl_xor_sync(0xFFFFFFFFu, e, x));
-            const int tn = max(-90, min(te[n][r], 6 - e));
-            const float down = pow2i(max(tn - te[n][r], -126));
+      for (int h = 0; h < 2; ++h) {
+        const unsigned char* vst = st + OFF_VROWS + (g & 1) * 8;
+        const uint2 va = *reinterpret_cast<const uint2*>(vst + swz(8 * t + 2 * h, g >> 1));
+        const uint2 vb = *reinterpret_cast<const uint2*>(vst + swz(8 * t + 4 + 2 * h, g >> 1));
+        const uint2 vc = *reinterpret_cast<const uint2*>(vst + swz(8 * t + 1 + 2 * h, g >> 1));
+        const uint2 vd = *reinterpret_cast<const uint2*>(vst + swz(8 * t + 5 + 2 * h, g >> 1));
 #pragma unroll
-            for (int mt = 0; mt < 8; ++mt) o[n][mt][r] *= down, o[n][mt][2 + r] *= down;
-            te[n][r] = tn;
+        for (int u = 0; u < 4; ++u) {  // four dims: a 16-bit part of each key's word
+          const uint32_t sel = (u & 1) ? 0x7632u : 0x5410u;
+          const uint32_t x = __byte_perm((&va.x)[u >> 1], (&vb.x)[u >> 1], sel);
+          const uint32_t y = __byte_perm((&vc.x)[u >> 1], (&vd.x)[u >> 1], sel);
+          const uint32_t x8 = x >> 8, y8 = y >> 8;
+          const uint32_t v0 = less8(x & 0x000F000Fu, 0x80088008u), v1 = less8(x & 0x00F000F0u, 0x80808080u);
+          const uint32_t v2 = less8(y & 0x000F000Fu, 0x80088008u), v3 = less8(y & 0x00F000F0u, 0x80808080u);
+          const uint32_t v4 = less8(x8 & 0x000F000Fu, 0x80088008u), v5 = less8(x8 & 0x00F000F0u, 0x80808080u);
+          const uint32_t v6 = less8(y8 & 0x000F000Fu, 0x80088008u), v7 = less8(y8 & 0x00F000F0u, 0x80808080u);
+#pragma unroll
+          for (int n = 0; n < NT; ++n) {
+            mma_f16(o[n][2 * u], v0, v1, v2, v3, pb[n][2 * h], pb[n][2 * h + 1]);
+            mma_f16(o[n][2 * u + 1], v4, v5, v6, v7, pb[n][2 * h], pb[n][2 * h + 1]);
           }
-          weigh();
-        }
-        pb[n][0] = transpose8x8(pack_f16x2(w[0], w[1]));
-        pb[n][1] = transpose8x8(pack_f16x2(w[2], w[3]));
-      }
-      // O^T: numbers of keys (2t, 2t + 1) and (2t + 8, 2t + 9), dims 16g ..
-      const unsigned char* vst = st + STEP * KV4_ROW + (g & 1) * 8;
-      const uint2 va = *reinterpret_cast<const uint2*>(vst + swz(2 * t, g >> 1));
-      const uint2 vb = *reinterpret_cast<const uint2*>(vst + swz(2 * t + 1, g >> 1));
-      const uint2 vc = *reinterpret_cast<const uint2*>(vst + swz(2 * t + 8, g >> 1));
-      const uint2 vd = *reinterpret_cast<const uint2*>(vst + swz(2 * t + 9, g >> 1));
-#pragma unroll
-      for (int u = 0; u < 4; ++u) {  // four dims: a 16-bit part of each key's word
-        const uint32_t sel = (u & 1) ? 0x7632u : 0x5410u;
-        const uint32_t x = __byte_perm((&va.x)[u >> 1], (&vb.x)[u >> 1], sel);
-        const uint32_t y = __byte_perm((&vc.x)[u >> 1], (&vd.x)[u >> 1], sel);
-        const uint32_t x8 = x >> 8, y8 = y >> 8;
-#pragma unroll
-        for (int n = 0; n < NT; ++n) {
-          mma_f16(o[n][2 * u], 0x80088008u, 0x80808080u, 0x80088008u, 0x80808080u, pb[n][0], pb[n][1]);
-          mma_f16(o[n][2 * u], x & 0x000F000Fu, x & 0x00F000F0u, y & 0x000F000Fu, y & 0x00F000F0u, pb[n][0], pb[n][1]);
-          mma_f16(o[n][2 * u + 1], 0x80088008u, 0x80808080u, 0x80088008u, 0x80808080u, pb[n][0], pb[n][1]);
-          mma_f16(o[n][2 * u + 1], x8 & 0x000F000Fu, x8 & 0x00F000F0u, y8 & 0x000F000Fu, y8 & 0x00F000F0u, pb[n][0],
-                  pb[n][1]);
         }
       }
+      stage = stage == FEW_STAGES - 1 ? 0 : stage + 1;
     }
     cp_async_wait<0>();
 
@@ -524,21 +557,22 @@ __global__ void __launch_bounds__(FEW_THREADS, NT == 1 ? 2 : 1) k_kv4_attn_few(F
       }
       const int words = (a.n_pad + 63) / 64;
       uint32_t pb[NT][2];
+      const float one[4] = {1.f, 1.f, VS_MIN, VS_MIN};
 #pragma unroll
       for (int n = 0; n < NT; ++n) {
+        float zz[4][2], w[4][2];
 #pragma unroll
         for (int c = 0; c < 4; ++c) {
           const int r = 8 * n + 2 * t + (c & 1), j = g + 8 * (c >> 1), i = r / a.G;
           bool sees = r < R && j < nn;
           if (sees) sees = a.mask ? (a.mask[((size_t)b * a.n_pad + i) * words] >> j) & 1 : j <= i;
-          z[n][c] = sees ? z[n][c] * a.scale_log2 : -INFINITY;
+          zz[c >> 1][c & 1] = sees ? z[n][c] * a.scale_log2 : -INFINITY;
+          zz[2 + (c >> 1)][c & 1] = -INFINITY;
         }
-        float p[4];
-        softmax(n, z[n], p);
-        // O holds O 2^-24 T (2^-20 T at odd dims): the weights take 2^-24 T, the odd dims' values 16
-        const float t0 = pow2i(te[n][0] - 24), t1 = pow2i(te[n][1] - 24);
-        pb[n][0] = transpose8x8(pack_bf16x2(p[0] * t0, p[1] * t1));
-        pb[n][1] = transpose8x8(pack_bf16x2(p[2] * t0, p[3] * t1));
+        weigh(n, zz, one, w);
+        // O is held times 2^-24 (2^-20 at odd dims): the weights take 2^-24, the odd dims' values 16
+        pb[n][0] = transpose8x8(pack_bf16x2(w[0][0] * 0x1p-24f, w[0][1] * 0x1p-24f));
+        pb[n][1] = transpose8x8(pack_bf16x2(w[1][0] * 0x1p-24f, w[1][1] * 0x1p-24f));
       }
 #pragma unroll
       for (int h = 0; h < 2; ++h) {  // 8 of the lane's 16 dims
@@ -571,7 +605,7 @@ __global__ void __launch_bounds__(FEW_THREADS, NT == 1 ? 2 : 1) k_kv4_attn_few(F
 #pragma unroll
         for (int x = 4; x < 32; x <<= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, x);
         const int row = warp * L::ROWS + 8 * n + 2 * t + r;
-        const float up = pow2i(24 - te[n][r]), up_odd = up * 0.0625f;
+        constexpr float up = 0x1p24f, up_odd = 0x1p20f;
         float* dst = po + row * L::OUT_PITCH + 16 * g;
 #pragma unroll
         for (int mt = 0; mt < 8; mt += 2)
@@ -604,7 +638,7 @@ __global__ void __launch_bounds__(FEW_THREADS, NT == 1 ? 2 : 1) k_kv4_attn_few(F
 #pragma unroll
       for (int w = 0; w < FEW_WARPS; ++w) {
         const float2 ml = pml[w * L::ROWS + r];
-        const float k = ml.x == -INFINITY ? 0.f : exp2_fast(ml.x - mx);
+        const float k = exp2_fast(ml.x - mx);
         const float4 v = *reinterpret_cast<const float4*>(po + (w * L::ROWS + r) * L::OUT_PITCH + 4 * d4);
         sum += ml.y * k;
         acc.x += v.x * k, acc.y += v.y * k, acc.z += v.z * k, acc.w += v.w * k;
@@ -629,24 +663,55 @@ __global__ void __launch_bounds__(FEW_THREADS, NT == 1 ? 2 : 1) k_kv4_attn_few(F
       if (s_last) {
         __threadfence();
         if (tid == 0) f.cnt[unit] = 0;  // fit for the next call
-        for (int e = tid; e < R * (HD / 4); e += FEW_THREADS) {
-          const int r = e / (HD / 4), d4 = e % (HD / 4);
+        // each piece's weight in a row, a warp a row ...
+        const int nc = c1 - c0 + 1;
+        float* wt = reinterpret_cast<float*>(smem);  // [R][nc]
+        float* red = wt + ((R * nc + 3) & ~3);       // [subsets][R][HD]
+        auto piece = [&](int c) {
+          return f.part + ((size_t)2 * c + ((long long)c * total / n_cta < unit_base ? 1 : 0)) * (L::ROWS * (HD + 2));
+        };
+        for (int r = warp; r < R; r += FEW_WARPS) {
           float mx = -INFINITY, sum = 0.f;
-          float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-          for (int c = c0; c <= c1; ++c) {
-            const float* sl = f.part + ((size_t)2 * c + ((long long)c * total / n_cta < unit_base ? 1 : 0)) *
-                                           (L::ROWS * (HD + 2));
-            const float2 ml = __ldcg(reinterpret_cast<const float2*>(sl + L::ROWS * HD) + r);
-            const float4 v = __ldcg(reinterpret_cast<const float4*>(sl + r * HD) + d4);
-            const float mn = fmaxf(mx, ml.x);
-            const float ka = mx == -INFINITY ? 0.f : exp2_fast(mx - mn), kb = ml.x == -INFINITY ? 0.f : exp2_fast(ml.x - mn);
-            mx = mn;
-            sum = sum * ka + ml.y * kb;
-            acc.x = acc.x * ka + v.x * kb, acc.y = acc.y * ka + v.y * kb;
-            acc.z = acc.z * ka + v.z * kb, acc.w = acc.w * ka + v.w * kb;
+          for (int c = lane; c < nc; c += 32)
+            mx = fmaxf(mx, __ldcg(reinterpret_cast<const float2*>(piece(c0 + c) + L::ROWS * HD) + r).x);
+#pragma unroll
+          for (int x = 16; x > 0; x >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xFFFFFFFFu, mx, x));
+          for (int c = lane; c < nc; c += 32) {
+            const float2 ml = __ldcg(reinterpret_cast<const float2*>(piece(c0 + c) + L::ROWS * HD) + r);
+            const float k = exp2_fast(ml.x - mx);
+            wt[r * nc + c] = k;
+            sum += ml.y * k;
           }
+#pragma unroll
+          for (int x = 16; x > 0; x >>= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, x);
           const float inv = sum == 0.f ? 0.f : 1.f / sum;
-          put(r, d4, make_float4(acc.x * inv, acc.y * inv, acc.z * inv, acc.w * inv));
+          for (int c = lane; c < nc; c += 32) wt[r * nc + c] *= inv;
+        }
+        __syncthreads();
+        // ... then its values, the pieces dealt out to as many subsets as there are threads for
+        const int quads = R * (HD / 4), subsets = max(1, FEW_THREADS / quads);
+        for (int e = tid; e < quads * subsets; e += FEW_THREADS) {
+          const int sub = e / quads, q = e - sub * quads, r = q / (HD / 4), d4 = q % (HD / 4);
+          float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 8
+          for (int c = sub; c < nc; c += subsets) {
+            const float k = wt[r * nc + c];
+            const float4 v = __ldcg(reinterpret_cast<const float4*>(piece(c0 + c) + r * HD) + d4);
+            acc.x += v.x * k, acc.y += v.y * k, acc.z += v.z * k, acc.w += v.w * k;
+          }
+          if (subsets == 1) put(r, d4, acc);
+          else reinterpret_cast<float4*>(red)[e] = acc;
+        }
+        if (subsets > 1) {
+          __syncthreads();
+          for (int q = tid; q < quads; q += FEW_THREADS) {
+            float4 acc = reinterpret_cast<const float4*>(red)[q];
+            for (int sub = 1; sub < subsets; ++sub) {
+              const float4 v = reinterpret_cast<const float4*>(red)[sub * quads + q];
+              acc.x += v.x, acc.y += v.y, acc.z += v.z, acc.w += v.w;
+            }
+            put(q / (HD / 4), q % (HD / 4), acc);
+          }
         }
       }
     }
