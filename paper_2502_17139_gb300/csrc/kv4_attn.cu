@@ -189,6 +189,11 @@ __device__ __forceinline__ uint32_t less8(uint32_t v, uint32_t minus) {
   asm("add.rn.f16x2 %0, %1, %2;" : "=r"(r) : "r"(v), "r"(minus));
   return r;
 }
+__device__ __forceinline__ float max_nan(float a, float b) {  // a NaN stays
+  float r;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+  return r;
+}
 __device__ __forceinline__ float exp2_fast(float x) {
   float y;
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
@@ -199,13 +204,12 @@ __device__ __forceinline__ int expo(float x) { return (int)((__float_as_uint(x) 
 __device__ __forceinline__ float lo_f(uint32_t w) { return __uint_as_float(w << 16); }
 __device__ __forceinline__ float hi_f(uint32_t w) { return __uint_as_float(w & 0xFFFF0000u); }
 
-// Byte offset of 16-byte chunk c (0..3) of row r (0..31) in a staged step:
-// two rows a 128-byte line, such that a quarter warp's 16-byte reads (rows
-// 8x + i and 8x + 4 + i) and a half warp's 8-byte reads (rows 8t + i, t =
-// 0..3, two chunks) each fall in different banks.
-__device__ __forceinline__ int swz(int r, int c) {
-  return (((r & 3) | ((r >> 3) << 2)) << 7) | ((((r >> 2) ^ (r >> 3)) & 1) << 6) | ((c ^ (((r >> 4) & 1) << 1)) << 4);
-}
+// A staged step keeps row r's 16-byte chunk c at
+//   (r % 4 + 4 (r / 8)) * 128 + ((r / 4 + r / 8) % 2) * 64 + (c ^ 2 (r / 16)) * 16:
+// two rows a 128-byte line, such that a quarter warp's 16-byte reads (rows 8x
+// + i and 8x + 4 + i) and a half warp's 8-byte reads (rows 8t + i, t = 0..3,
+// two chunks) each fall in different banks.  Every address below is one of
+// three lane constants plus an immediate.
 
 __device__ __forceinline__ int few_steps(const Kv4Args& a, int b, int& nn, int& kvl, bool& bad) {
   kvl = a.kv_len[b];
@@ -215,43 +219,56 @@ __device__ __forceinline__ int few_steps(const Kv4Args& a, int b, int& nn, int& 
   return nn == 0 ? 1 : max(1, (kvl + STEP - 1) / STEP + (a.k_new ? 1 : 0));
 }
 
+// total steps cut into n shares of equal size, the first rem one longer.
+struct FewCut {
+  int n, q, rem;
+  __device__ __forceinline__ FewCut(int total, int grid) {
+    n = max(1, min(grid, total / FEW_MIN_STEPS));
+    q = total / n;
+    rem = total - q * n;
+  }
+  __device__ __forceinline__ int start(int c) const { return c * q + min(c, rem); }
+  __device__ __forceinline__ int share_of(int step) const {
+    const int longer = rem * (q + 1);
+    return step < longer ? step / (q + 1) : rem + (step - longer) / q;
+  }
+};
+
 template <int NT>
 __global__ void __launch_bounds__(FEW_THREADS, NT == 1 ? 2 : 1) k_kv4_attn_few(FewArgs f) {
   using L = FewSmem<NT>;
   extern __shared__ __align__(1024) unsigned char smem[];
-  __shared__ long long s_total, s_begin;
-  __shared__ int s_b, s_last;
+  __shared__ int s_total, s_begin, s_b, s_last;
   const Kv4Args& a = f.a;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t = lane & 3;
   const uint32_t ring = smem_u32(smem) + warp * (FEW_STAGES * STEP_BYTES);
   const unsigned char* ring_p = smem + warp * (FEW_STAGES * STEP_BYTES);
 
-  // This CTA's share of all units' steps: [begin, end), from every request's length.
-  long long cur, end;
-  int b, n_cta = gridDim.x;
-  long long total = 0;
+  // This CTA's share of all units' steps: [cur, end), from every request's
+  // length (the host has seen to it that the sum fits 32 bits).
+  int cur, end, b = 0, req_base = 0;  // req_base: first step of request b
   if (f.split) {
     if (warp == 0) {
-      long long sum = 0;
       int nn, kvl;
       bool bad;
-      for (int i = lane; i < a.B; i += 32) sum += few_steps(a, i, nn, kvl, bad);
-#pragma unroll
-      for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, o);
-      const long long T = sum * a.Hkv;
-      const int n = (int)max(1ll, min((long long)gridDim.x, T / FEW_MIN_STEPS));
-      const long long start = (long long)blockIdx.x * T / n;
-      long long base = 0;  // steps of the requests before b0, times Hkv
-      int found = 0;
+      const int first = lane < a.B ? few_steps(a, lane, nn, kvl, bad) * a.Hkv : 0;
+      int sum = first;
+#pragma unroll 1
+      for (int i = lane + 32; i < a.B; i += 32) sum += few_steps(a, i, nn, kvl, bad) * a.Hkv;
+      const int total = __reduce_add_sync(0xFFFFFFFFu, sum);
+      const FewCut cut(total, gridDim.x);
+      const int start = cut.start(blockIdx.x);
+      int base = 0, found = 0;
+#pragma unroll 1
       for (int b0 = 0; b0 < a.B; b0 += 32) {
-        long long mine = b0 + lane < a.B ? (long long)few_steps(a, b0 + lane, nn, kvl, bad) * a.Hkv : 0;
-        long long inc = mine;
+        const int mine = b0 == 0 ? first : (b0 + lane < a.B ? few_steps(a, b0 + lane, nn, kvl, bad) * a.Hkv : 0);
+        int inc = mine;
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) {
-          const long long v = __shfl_up_sync(0xFFFFFFFFu, inc, o);
+          const int v = __shfl_up_sync(0xFFFFFFFFu, inc, o);
           if (lane >= o) inc += v;
         }
-        const uint32_t hit = __ballot_sync(0xFFFFFFFFu, mine > 0 && base + inc > start);
+        const uint32_t hit = __ballot_sync(0xFFFFFFFFu, base + inc > start);
         if (hit) {
           const int w = __ffs(hit) - 1;
           found = b0 + w;
@@ -260,44 +277,44 @@ __global__ void __launch_bounds__(FEW_THREADS, NT == 1 ? 2 : 1) k_kv4_attn_few(F
         }
         base += __shfl_sync(0xFFFFFFFFu, inc, 31);
       }
-      if (lane == 0) s_total = T, s_begin = base, s_b = found;
+      if (lane == 0) s_total = total, s_begin = base, s_b = found;
     }
     __syncthreads();
-    total = s_total;
-    n_cta = (int)max(1ll, min((long long)gridDim.x, total / FEW_MIN_STEPS));
-    if ((int)blockIdx.x >= n_cta) return;
-    cur = (long long)blockIdx.x * total / n_cta;
-    end = ((long long)blockIdx.x + 1) * total / n_cta;
     b = s_b;
+    req_base = s_begin;
+  }
+  const FewCut cut(f.split ? s_total : 1, gridDim.x);
+  if (f.split) {
+    if ((int)blockIdx.x >= cut.n) return;
+    cur = cut.start(blockIdx.x);
+    end = cut.start(blockIdx.x + 1);
   } else {
     cur = blockIdx.x;  // a unit, not a step
-    end = (long long)a.B * a.Hkv;
-    b = 0;
+    end = a.B * a.Hkv;
   }
-  long long req_base = f.split ? s_begin : 0;  // first step of request b
 
+#pragma unroll 1
   while (cur < end) {
     // ---- the unit that cur lies in, and this CTA's steps [s0, s1) of it
-    int nn, kvl, gh, s0, s1, steps;
+    int nn, kvl, gh, s0 = 0, s1, steps, unit_base = 0;
     bool bad;
-    long long unit_base = 0;
     if (f.split) {
       steps = few_steps(a, b, nn, kvl, bad);
-      while (cur - req_base >= (long long)steps * a.Hkv) {
-        req_base += (long long)steps * a.Hkv;
+#pragma unroll 1
+      while (cur - req_base >= steps * a.Hkv) {
+        req_base += steps * a.Hkv;
         ++b;
         steps = few_steps(a, b, nn, kvl, bad);
       }
-      gh = (int)((cur - req_base) / steps);
-      unit_base = req_base + (long long)gh * steps;
-      s0 = (int)(cur - unit_base);
-      s1 = (int)min((long long)steps, end - unit_base);
+      gh = (cur - req_base) / steps;
+      unit_base = req_base + gh * steps;
+      s0 = cur - unit_base;
+      s1 = min(steps, end - unit_base);
       cur = unit_base + s1;
     } else {
-      b = (int)(cur / a.Hkv);
-      gh = (int)(cur - (long long)b * a.Hkv);
+      b = cur / a.Hkv;
+      gh = cur - b * a.Hkv;
       steps = few_steps(a, b, nn, kvl, bad);
-      s0 = 0;
       s1 = steps;
       cur += gridDim.x;
     }
@@ -306,6 +323,57 @@ __global__ void __launch_bounds__(FEW_THREADS, NT == 1 ? 2 : 1) k_kv4_attn_few(F
     const int R = nn * a.G;  // rows in use: node-major, r = node * G + head in group
     auto q_row = [&](int r) { return a.q + (((size_t)b * a.n_pad + r / a.G) * a.H + gh * a.G + r % a.G) * HD; };
 
+    const uint8_t *k_lane = a.kc + lane * 16, *v_lane = a.vc + lane * 16;
+    const __nv_bfloat16* sc0 = (lane & 4) ? a.vs : a.ks;
+    const uint8_t* sc_lane = reinterpret_cast<const uint8_t*>(sc0) + (lane & 1) * 16;
+    const uint32_t put0 = ring + ((lane >> 2) & 3) * 128 + (lane >> 4) * 64 + (lane & 3) * 16;
+    const int get_k = (g >> 1) * 512 + ((g ^ (g >> 1)) & 1) * 64 + ((t ^ ((g >> 2) << 1)) << 4);
+    const int get_v = OFF_VROWS + t * 512 + (t & 1) * 64 + (((g >> 1) ^ ((t >> 1) << 1)) << 4) + (g & 1) * 8;
+    // ---- cached steps of this warp: s0 + warp, s0 + warp + 8, ...
+    const int cs1 = min(s1, c_steps);
+    const int n_it = cs1 > s0 + warp ? (cs1 - s0 - warp + FEW_WARPS - 1) / FEW_WARPS : 0;
+    int id_a = 0, id_b = 0;  // page ids of the two runs of 16 keys of the warp's next 32 steps, one a lane
+    uint32_t outside = 0;    // bits 2 x stage, + 1: that run's page is not in the pool
+    const int32_t* tab = a.table + (size_t)b * a.max_pages;
+    // runs of 16 rows are counted in 32 bits (1024 bytes each: 4 TB)
+    const uint32_t runs_page = (uint32_t)a.Hkv << (a.shift - 4), run0 = (uint32_t)gh << (a.shift - 4);
+    const uint32_t run_mask = (1u << (a.shift - 4)) - 1u;
+    auto issue = [&](int it, int stage) {
+      if (it < n_it) {
+        const int s = s0 + warp + it * FEW_WARPS;
+        if ((it & 31) == 0) {
+          const long long key = (long long)(s + lane * FEW_WARPS) * STEP;
+          id_a = key < kvl ? tab[key >> a.shift] : 0;
+          id_b = key + 16 < kvl ? tab[(key + 16) >> a.shift] : 0;
+        }
+        int ia = __shfl_sync(0xFFFFFFFFu, id_a, it & 31), ib = __shfl_sync(0xFFFFFFFFu, id_b, it & 31);
+        if (max((unsigned)ia, (unsigned)ib) >= (unsigned)a.n_pages) {  // its keys are left out below
+          const bool xa = (unsigned)ia >= (unsigned)a.n_pages, xb = (unsigned)ib >= (unsigned)a.n_pages;
+          outside |= ((xa ? 1u : 0u) | (xb ? 2u : 0u)) << (2 * stage);
+          ia = xa ? 0 : ia;
+          ib = xb ? 0 : ib;
+          if (lane == 0) fc_flag(FC_ERR_WORD(a.err), FC_EBIT_INVALID);
+        }
+        const uint32_t ra = ia * runs_page + (run0 + ((uint32_t)(2 * s) & run_mask));
+        const uint32_t rb = ib * runs_page + (run0 + ((uint32_t)(2 * s + 1) & run_mask));
+        const uint32_t d0 = put0 + stage * STEP_BYTES, d1 = d0 ^ 64u, d2 = d0 ^ 32u, d3 = d0 ^ 96u;
+        const uint8_t *ka = k_lane + (uint64_t)ra * 1024u, *kb = k_lane + (uint64_t)rb * 1024u;
+        const uint8_t *va = v_lane + (uint64_t)ra * 1024u, *vb = v_lane + (uint64_t)rb * 1024u;
+        cp_async16(d0, ka);
+        cp_async16(d1 + 512, ka + 512);
+        cp_async16(d2 + 1024, kb);
+        cp_async16(d3 + 1536, kb + 512);
+        cp_async16(d0 + OFF_VROWS, va);
+        cp_async16(d1 + OFF_VROWS + 512, va + 512);
+        cp_async16(d2 + OFF_VROWS + 1024, vb);
+        cp_async16(d3 + OFF_VROWS + 1536, vb + 512);
+        if (lane < 8)  // K scales of the two runs, then V scales
+          cp_async16(ring + stage * STEP_BYTES + OFF_KSC + lane * 16, sc_lane + (uint64_t)((lane & 2) ? rb : ra) * 32u);
+      }
+      cp_async_commit();
+    };
+#pragma unroll 1
+    for (int it = 0; it < FEW_STAGES - 1; ++it) issue(it, it);
     // ---- queries: the unit's power of two, then the operand registers
     // k-step 2i of word i of a key's 16-byte quarter t: dimensions 32t + 8i +
     // {0, 4} and {1, 5} / 16; k-step 2i + 1: {2, 6} and {3, 7} / 16
@@ -318,13 +386,12 @@ __global__ void __launch_bounds__(FEW_THREADS, NT == 1 ? 2 : 1) k_kv4_attn_few(F
         qw[n][i] = 8 * n + g < R ? reinterpret_cast<const uint4*>(q_row(8 * n + g))[4 * t + i] : make_uint4(0, 0, 0, 0);
         const uint32_t* w = &qw[n][i].x;
 #pragma unroll
-        for (int x = 0; x < 4; ++x) {
-          const uint32_t l = w[x] & 0x7FFFu, h = (w[x] >> 16) & 0x7FFFu;  // finite values only
-          if (l < 0x7F80u) top = max(top, l);
-          if (h < 0x7F80u) top = max(top, h);
+        for (int x = 0; x < 4; ++x) {  // magnitudes of finite values, both halves at once
+          const uint32_t mag = w[x] & 0x7FFF7FFFu;
+          top = __vmaxu2(top, mag & ~__vcmpgeu2(mag, 0x7F807F80u));
         }
       }
-    top = __reduce_max_sync(0xFFFFFFFFu, top);
+    top = __reduce_max_sync(0xFFFFFFFFu, max(top & 0xFFFFu, top >> 16));
     const int qe = top ? min(max((int)(top >> 7) - 127, -100), 100) : 0;  // largest |q| < 2^(qe + 1) (or it overflows)
     const float q_mul = pow2i(14 - qe), q_odd = q_mul * 0.0625f;
     const float z_mul = a.scale_log2 * pow2i(qe + 10);  // undoes 2^(14 - qe) 2^-24
@@ -363,25 +430,25 @@ __global__ void __launch_bounds__(FEW_THREADS, NT == 1 ? 2 : 1) k_kv4_attn_few(F
       l[n][0] = l[n][1] = 0.f;
     }
 
-    // Scores z (base 2, masked ones -inf; z[i][r] of the lane's key i, row 2t
-    // + r) and value scales to w = 2^(z - m) vs; adds 2^(z - m) to the row
-    // sums; moves the references when a w is too large.
-    auto weigh = [&](int n, const float (&z)[4][2], const float (&vs)[4], float (&w)[4][2]) {
-      float p[4][2], sum = 0.f;
+    // Scores d * ks (base 2; masked keys: d -inf, ks 1; d[i][r] of the lane's
+    // key i, row 2t + r) and value scales to w = 2^(d ks - m) vs; adds the
+    // powers to the row sums; moves the references when a w is too large.
+    auto weigh = [&](int n, const float (&d)[4][2], const float (&ks)[4], const float (&vs)[4], float (&w)[4][2]) {
+      float p[4][2];
 #pragma unroll
       for (int i = 0; i < 4; ++i)
 #pragma unroll
         for (int r = 0; r < 2; ++r) {
-          p[i][r] = exp2_fast(z[i][r] - m[n][r]);
+          p[i][r] = exp2_fast(fmaf(d[i][r], ks[i], -m[n][r]));
           w[i][r] = p[i][r] * vs[i];
-          sum += w[i][r];
         }
+      const float sum = ((w[0][0] + w[0][1]) + (w[1][0] + w[1][1])) + ((w[2][0] + w[2][1]) + (w[3][0] + w[3][1]));
       if (__any_sync(0xFFFFFFFFu, sum > W_MAX)) {
 #pragma unroll
         for (int r = 0; r < 2; ++r) {
           float top = M_START;
 #pragma unroll
-          for (int i = 0; i < 4; ++i) top = fmaxf(top, z[i][r] + (float)(expo(vs[i]) - 11));
+          for (int i = 0; i < 4; ++i) top = fmaxf(top, fmaf(d[i][r], ks[i], (float)(expo(vs[i]) - 11)));
 #pragma unroll
           for (int x = 4; x < 32; x <<= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, x));
           const float mn = fmaxf(m[n][r], top), al = exp2_fast(m[n][r] - mn);
@@ -391,7 +458,7 @@ __global__ void __launch_bounds__(FEW_THREADS, NT == 1 ? 2 : 1) k_kv4_attn_few(F
           for (int mt = 0; mt < 8; ++mt) o[n][mt][r] *= al, o[n][mt][2 + r] *= al;
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
-            p[i][r] = exp2_fast(z[i][r] - mn);
+            p[i][r] = exp2_fast(fmaf(d[i][r], ks[i], -mn));
             w[i][r] = p[i][r] * vs[i];
           }
         }
@@ -400,51 +467,7 @@ __global__ void __launch_bounds__(FEW_THREADS, NT == 1 ? 2 : 1) k_kv4_attn_few(F
       for (int r = 0; r < 2; ++r) l[n][r] += (p[0][r] + p[1][r]) + (p[2][r] + p[3][r]);
     };
 
-    // ---- cached steps of this warp: s0 + warp, s0 + warp + 8, ...
-    const int cs1 = min(s1, c_steps);
-    const int n_it = cs1 > s0 + warp ? (cs1 - s0 - warp + FEW_WARPS - 1) / FEW_WARPS : 0;
-    int id_a = 0, id_b = 0;  // page ids of the two runs of 16 keys of the warp's next 32 steps, one a lane
-    uint32_t outside = 0;    // bits 2 x stage, + 1: that run's page is not in the pool
-    const int32_t* tab = a.table + (size_t)b * a.max_pages;
-    auto issue = [&](int it, int stage) {
-      if (it < n_it) {
-        const int s = s0 + warp + it * FEW_WARPS;
-        if ((it & 31) == 0) {
-          const long long key = (long long)(s + lane * FEW_WARPS) * STEP;
-          id_a = key < kvl ? tab[key >> a.shift] : 0;
-          id_b = key + 16 < kvl ? tab[(key + 16) >> a.shift] : 0;
-        }
-        int ia = __shfl_sync(0xFFFFFFFFu, id_a, it & 31), ib = __shfl_sync(0xFFFFFFFFu, id_b, it & 31);
-        const bool xa = (unsigned)ia >= (unsigned)a.n_pages, xb = (unsigned)ib >= (unsigned)a.n_pages;
-        outside &= ~(3u << (2 * stage));
-        if (xa || xb) {  // its keys are left out below
-          outside |= ((xa ? 1u : 0u) | (xb ? 2u : 0u)) << (2 * stage);
-          ia = xa ? 0 : ia;
-          ib = xb ? 0 : ib;
-          if (lane == 0) fc_flag(FC_ERR_WORD(a.err), FC_EBIT_INVALID);
-        }
-        const int in_page = (1 << a.shift) - 1;
-        const size_t ra = (((size_t)ia * a.Hkv + gh) << a.shift) + ((s * STEP) & in_page);
-        const size_t rb = (((size_t)ib * a.Hkv + gh) << a.shift) + ((s * STEP + 16) & in_page);
-        const uint32_t st = ring + stage * STEP_BYTES;
-        const uint8_t *ka = a.kc + ra * KV4_ROW + lane * 16, *kb = a.kc + rb * KV4_ROW + lane * 16;
-        const uint8_t *va = a.vc + ra * KV4_ROW + lane * 16, *vb = a.vc + rb * KV4_ROW + lane * 16;
-        const int r = lane >> 2, c = lane & 3;
-        cp_async16(st + swz(r, c), ka);
-        cp_async16(st + swz(r + 8, c), ka + 512);
-        cp_async16(st + swz(r + 16, c), kb);
-        cp_async16(st + swz(r + 24, c), kb + 512);
-        cp_async16(st + OFF_VROWS + swz(r, c), va);
-        cp_async16(st + OFF_VROWS + swz(r + 8, c), va + 512);
-        cp_async16(st + OFF_VROWS + swz(r + 16, c), vb);
-        cp_async16(st + OFF_VROWS + swz(r + 24, c), vb + 512);
-        if (lane < 8)  // K scales of the two runs, then V scales
-          cp_async16(st + OFF_KSC + lane * 16, (lane < 4 ? a.ks : a.vs) + ((lane & 2) ? rb : ra) + (lane & 1) * 8);
-      }
-      cp_async_commit();
-    };
-#pragma unroll
-    for (int it = 0; it < FEW_STAGES - 1; ++it) issue(it, it);
+    // ---- the loop over the steps
     int stage = 0;
     for (int it = 0; it < n_it; ++it) {
       cp_async_wait<FEW_STAGES - 2>();
@@ -452,19 +475,17 @@ __global__ void __launch_bounds__(FEW_THREADS, NT == 1 ? 2 : 1) k_kv4_attn_few(F
       const unsigned char* st = ring_p + stage * STEP_BYTES;
       const int left = kvl - (s0 + warp + it * FEW_WARPS) * STEP;  // keys of the request from here on
       const uint32_t out_now = (outside >> (2 * stage)) & 3u;
-      {
-        const int ahead = stage == 0 ? FEW_STAGES - 1 : stage - 1;  // the stage read in the last turn
-        issue(it + FEW_STAGES - 1, ahead);
-      }
+      outside &= ~(3u << (2 * stage));
+      issue(it + FEW_STAGES - 1, stage == 0 ? FEW_STAGES - 1 : stage - 1);  // into the stage read in the last turn
       const uint2 ks2 = *reinterpret_cast<const uint2*>(st + OFF_KSC + 8 * g);
       const uint2 vs2 = *reinterpret_cast<const uint2*>(st + OFF_VSC + 8 * g);
-      const float ks[4] = {lo_f(ks2.x), hi_f(ks2.x), lo_f(ks2.y), hi_f(ks2.y)};
+      float ks[4] = {lo_f(ks2.x) * z_mul, hi_f(ks2.x) * z_mul, lo_f(ks2.y) * z_mul, hi_f(ks2.y) * z_mul};
       float vs[4] = {lo_f(vs2.x), hi_f(vs2.x), lo_f(vs2.y), hi_f(vs2.y)};
       float z[NT][4][2];
 #pragma unroll
       for (int h = 0; h < 2; ++h) {  // keys 4g + 2h, 4g + 2h + 1
-        const uint4 k0 = *reinterpret_cast<const uint4*>(st + swz(4 * g + 2 * h, t));
-        const uint4 k1 = *reinterpret_cast<const uint4*>(st + swz(4 * g + 2 * h + 1, t));
+        const uint4 k0 = *reinterpret_cast<const uint4*>(st + get_k + h * 256);
+        const uint4 k1 = *reinterpret_cast<const uint4*>(st + get_k + h * 256 + 128);
         float d[NT][4];
 #pragma unroll
         for (int n = 0; n < NT; ++n) d[n][0] = d[n][2] = s_init[n][0], d[n][1] = d[n][3] = s_init[n][1];
@@ -483,10 +504,10 @@ __global__ void __launch_bounds__(FEW_THREADS, NT == 1 ? 2 : 1) k_kv4_attn_few(F
 #pragma unroll
         for (int n = 0; n < NT; ++n)
 #pragma unroll
-          for (int c = 0; c < 4; ++c) z[n][2 * h + (c >> 1)][c & 1] = d[n][c] * (ks[2 * h + (c >> 1)] * z_mul);
+          for (int c = 0; c < 4; ++c) z[n][2 * h + (c >> 1)][c & 1] = d[n][c];
       }
 #pragma unroll
-      for (int i = 0; i < 4; ++i) vs[i] = vs[i] < VS_MIN ? VS_MIN : vs[i];  // a NaN stays
+      for (int i = 0; i < 4; ++i) vs[i] = max_nan(vs[i], VS_MIN);
       if (left < STEP || out_now) {
         // keys past the request's end, or in a page outside the pool: no weight, whatever stands there
 #pragma unroll
@@ -494,6 +515,7 @@ __global__ void __launch_bounds__(FEW_THREADS, NT == 1 ? 2 : 1) k_kv4_attn_few(F
           const int j = 4 * g + i;
           if (j >= left || ((out_now >> (j >> 4)) & 1u)) {
             vs[i] = VS_MIN;
+            ks[i] = 1.f;
 #pragma unroll
             for (int n = 0; n < NT; ++n) z[n][i][0] = z[n][i][1] = -INFINITY;
           }
@@ -503,7 +525,7 @@ __global__ void __launch_bounds__(FEW_THREADS, NT == 1 ? 2 : 1) k_kv4_attn_few(F
 #pragma unroll
       for (int n = 0; n < NT; ++n) {
         float w[4][2];
-        weigh(n, z[n], vs, w);
+        weigh(n, z[n], ks, vs, w);
 #pragma unroll
         for (int i = 0; i < 4; ++i) pb[n][i] = transpose8x8(pack_f16x2(w[i][0], w[i][1]));
       }
@@ -511,11 +533,10 @@ __global__ void __launch_bounds__(FEW_THREADS, NT == 1 ? 2 : 1) k_kv4_attn_few(F
       // 8t + 2h, 8t + 4 + 2h), k 2t + 8, + 9 those of group 2h + 1
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
-        const unsigned char* vst = st + OFF_VROWS + (g & 1) * 8;
-        const uint2 va = *reinterpret_cast<const uint2*>(vst + swz(8 * t + 2 * h, g >> 1));
-        const uint2 vb = *reinterpret_cast<const uint2*>(vst + swz(8 * t + 4 + 2 * h, g >> 1));
-        const uint2 vc = *reinterpret_cast<const uint2*>(vst + swz(8 * t + 1 + 2 * h, g >> 1));
-        const uint2 vd = *reinterpret_cast<const uint2*>(vst + swz(8 * t + 5 + 2 * h, g >> 1));
+        const uint2 va = *reinterpret_cast<const uint2*>(st + get_v + h * 256);
+        const uint2 vb = *reinterpret_cast<const uint2*>(st + (get_v ^ 64) + h * 256);
+        const uint2 vc = *reinterpret_cast<const uint2*>(st + get_v + h * 256 + 128);
+        const uint2 vd = *reinterpret_cast<const uint2*>(st + (get_v ^ 64) + h * 256 + 128);
 #pragma unroll
         for (int u = 0; u < 4; ++u) {  // four dims: a 16-bit part of each key's word
           const uint32_t sel = (u & 1) ? 0x7632u : 0x5410u;
@@ -558,6 +579,7 @@ __global__ void __launch_bounds__(FEW_THREADS, NT == 1 ? 2 : 1) k_kv4_attn_few(F
       const int words = (a.n_pad + 63) / 64;
       uint32_t pb[NT][2];
       const float one[4] = {1.f, 1.f, VS_MIN, VS_MIN};
+      const float by[4] = {a.scale_log2, a.scale_log2, 1.f, 1.f};
 #pragma unroll
       for (int n = 0; n < NT; ++n) {
         float zz[4][2], w[4][2];
@@ -566,10 +588,10 @@ __global__ void __launch_bounds__(FEW_THREADS, NT == 1 ? 2 : 1) k_kv4_attn_few(F
           const int r = 8 * n + 2 * t + (c & 1), j = g + 8 * (c >> 1), i = r / a.G;
           bool sees = r < R && j < nn;
           if (sees) sees = a.mask ? (a.mask[((size_t)b * a.n_pad + i) * words] >> j) & 1 : j <= i;
-          zz[c >> 1][c & 1] = sees ? z[n][c] * a.scale_log2 : -INFINITY;
+          zz[c >> 1][c & 1] = sees ? z[n][c] : -INFINITY;
           zz[2 + (c >> 1)][c & 1] = -INFINITY;
         }
-        weigh(n, zz, one, w);
+        weigh(n, zz, by, one, w);
         // O is held times 2^-24 (2^-20 at odd dims): the weights take 2^-24, the odd dims' values 16
         pb[n][0] = transpose8x8(pack_bf16x2(w[0][0] * 0x1p-24f, w[0][1] * 0x1p-24f));
         pb[n][1] = transpose8x8(pack_bf16x2(w[1][0] * 0x1p-24f, w[1][1] * 0x1p-24f));
@@ -617,13 +639,13 @@ __global__ void __launch_bounds__(FEW_THREADS, NT == 1 ? 2 : 1) k_kv4_attn_few(F
     const bool whole = s0 == 0 && s1 == steps;
     const int rows_all = a.n_pad * a.G;  // rows past the nodes are written as zeros
     float* slot = whole ? nullptr
-                        : f.part + ((size_t)2 * blockIdx.x + ((long long)blockIdx.x * total / n_cta < unit_base ? 1 : 0)) *
-                                       (L::ROWS * (HD + 2));
+                        : f.part + (2 * blockIdx.x + (cut.start(blockIdx.x) < unit_base ? 1 : 0)) * (L::ROWS * (HD + 2));
     auto put = [&](int r, int d4, const float4& v) {
       const int i = r / a.G;
       __nv_bfloat16* dst = a.out + (((size_t)b * a.n_pad + i) * a.H + gh * a.G + (r - i * a.G)) * HD + 4 * d4;
       *reinterpret_cast<uint2*>(dst) = make_uint2(pack_bf16x2(v.x, v.y), pack_bf16x2(v.z, v.w));
     };
+#pragma unroll 1
     for (int e = tid; e < rows_all * (HD / 4); e += FEW_THREADS) {
       const int r = e / (HD / 4), d4 = e % (HD / 4);
       if (r >= R) {
@@ -655,8 +677,7 @@ __global__ void __launch_bounds__(FEW_THREADS, NT == 1 ? 2 : 1) k_kv4_attn_few(F
       // The last CTA to arrive adds up the pieces, in CTA order whichever it is.
       __threadfence();
       __syncthreads();
-      const long long last = unit_base + steps - 1;
-      const int c0 = (int)(((unit_base + 1) * n_cta - 1) / total), c1 = (int)(((last + 1) * n_cta - 1) / total);
+      const int c0 = cut.share_of(unit_base), c1 = cut.share_of(unit_base + steps - 1);
       const int unit = b * a.Hkv + gh;
       if (tid == 0) s_last = atomicAdd(f.cnt + unit, 1) == c1 - c0;
       __syncthreads();
@@ -668,14 +689,17 @@ __global__ void __launch_bounds__(FEW_THREADS, NT == 1 ? 2 : 1) k_kv4_attn_few(F
         float* wt = reinterpret_cast<float*>(smem);  // [R][nc]
         float* red = wt + ((R * nc + 3) & ~3);       // [subsets][R][HD]
         auto piece = [&](int c) {
-          return f.part + ((size_t)2 * c + ((long long)c * total / n_cta < unit_base ? 1 : 0)) * (L::ROWS * (HD + 2));
+          return f.part + (2 * c + (cut.start(c) < unit_base ? 1 : 0)) * (L::ROWS * (HD + 2));
         };
+#pragma unroll 1
         for (int r = warp; r < R; r += FEW_WARPS) {
           float mx = -INFINITY, sum = 0.f;
+#pragma unroll 2
           for (int c = lane; c < nc; c += 32)
             mx = fmaxf(mx, __ldcg(reinterpret_cast<const float2*>(piece(c0 + c) + L::ROWS * HD) + r).x);
 #pragma unroll
           for (int x = 16; x > 0; x >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xFFFFFFFFu, mx, x));
+#pragma unroll 2
           for (int c = lane; c < nc; c += 32) {
             const float2 ml = __ldcg(reinterpret_cast<const float2*>(piece(c0 + c) + L::ROWS * HD) + r);
             const float k = exp2_fast(ml.x - mx);
@@ -685,15 +709,17 @@ __global__ void __launch_bounds__(FEW_THREADS, NT == 1 ? 2 : 1) k_kv4_attn_few(F
 #pragma unroll
           for (int x = 16; x > 0; x >>= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, x);
           const float inv = sum == 0.f ? 0.f : 1.f / sum;
+#pragma unroll 1
           for (int c = lane; c < nc; c += 32) wt[r * nc + c] *= inv;
         }
         __syncthreads();
         // ... then its values, the pieces dealt out to as many subsets as there are threads for
         const int quads = R * (HD / 4), subsets = max(1, FEW_THREADS / quads);
+#pragma unroll 1
         for (int e = tid; e < quads * subsets; e += FEW_THREADS) {
           const int sub = e / quads, q = e - sub * quads, r = q / (HD / 4), d4 = q % (HD / 4);
           float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 8
+#pragma unroll 4
           for (int c = sub; c < nc; c += subsets) {
             const float k = wt[r * nc + c];
             const float4 v = __ldcg(reinterpret_cast<const float4*>(piece(c0 + c) + r * HD) + d4);
@@ -704,8 +730,10 @@ __global__ void __launch_bounds__(FEW_THREADS, NT == 1 ? 2 : 1) k_kv4_attn_few(F
         }
         if (subsets > 1) {
           __syncthreads();
+#pragma unroll 1
           for (int q = tid; q < quads; q += FEW_THREADS) {
             float4 acc = reinterpret_cast<const float4*>(red)[q];
+#pragma unroll 1
             for (int sub = 1; sub < subsets; ++sub) {
               const float4 v = reinterpret_cast<const float4*>(red)[sub * quads + q];
               acc.x += v.x, acc.y += v.y, acc.z += v.z, acc.w += v.w;
@@ -734,12 +762,12 @@ fc_status launch_few(const Kv4Args& a, void* ws, size_t ws_bytes, cudaStream_t s
   const int full = NT == 1 ? FEW_GRID : FEW_GRID / 2;
   const size_t cnt = few_cnt_bytes(a.B, a.Hkv), one = (size_t)2 * FewSmem<NT>::ROWS * (HD + 2) * sizeof(float);
   const long long units = (long long)a.B * a.Hkv;
-  // at most what the tables could hold, in steps worth a CTA
+  // at most what the tables could hold, in steps (past 32 bits there are units enough without cutting them)
   const long long most = units * ((((long long)a.max_pages << a.shift) + STEP - 1) / STEP + 1);
   int grid = (int)std::max<long long>(1, std::min<long long>(full, most / FEW_MIN_STEPS));
   FewArgs f{a, 1, nullptr, nullptr};
   if (ws && ws_bytes > cnt) grid = (int)std::min<size_t>(grid, (ws_bytes - cnt) / one);
-  if (!ws || ws_bytes <= cnt || grid < 1) {
+  if (!ws || ws_bytes <= cnt || grid < 1 || most > 0x7FFFFFFFll) {
     f.split = 0;
     grid = (int)std::min<long long>(units, 1 << 20);
   } else {
