@@ -129,7 +129,9 @@ constexpr int STEP = 32;         // keys a step
 constexpr int FEW_STAGES = 3;    // steps in flight a warp
 constexpr int OFF_VROWS = STEP * KV4_ROW, OFF_KSC = 2 * STEP * KV4_ROW, OFF_VSC = OFF_KSC + STEP * 2;
 constexpr int STEP_BYTES = OFF_VSC + STEP * 2;
-constexpr int FEW_MIN_STEPS = FEW_WARPS;  // steps worth a CTA of their own
+// A unit's start and end take a CTA about 6 us, 0.2 us a step at full
+// bandwidth; joining two parts of a unit about 4 us.
+constexpr int UNIT_COST = 30, PART_STEPS = 16;
 constexpr float W_MAX = 32768.f;
 constexpr float VS_MIN = 0x1p-80f;
 constexpr float M_START = -1e30f;  // a reference before any key: 2^(z + 1e30) passes W_MAX, 2^(-1e30 - m) is 0
@@ -219,11 +221,11 @@ __device__ __forceinline__ int few_steps(const Kv4Args& a, int b, int& nn, int& 
   return nn == 0 ? 1 : max(1, (kvl + STEP - 1) / STEP + (a.k_new ? 1 : 0));
 }
 
-// total steps cut into n shares of equal size, the first rem one longer.
+// A total cost cut into n shares of equal size, the first rem one longer.
 struct FewCut {
   int n, q, rem;
   __device__ __forceinline__ FewCut(int total, int grid) {
-    n = max(1, min(grid, total / FEW_MIN_STEPS));
+    n = max(1, min(grid, total / (UNIT_COST + PART_STEPS)));
     q = total / n;
     rem = total - q * n;
   }
@@ -238,86 +240,111 @@ template <int NT>
 __global__ void __launch_bounds__(FEW_THREADS, NT == 1 ? 2 : 1) k_kv4_attn_few(FewArgs f) {
   using L = FewSmem<NT>;
   extern __shared__ __align__(1024) unsigned char smem[];
-  __shared__ int s_total, s_begin, s_b, s_last;
+  __shared__ int s_last;
   const Kv4Args& a = f.a;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t = lane & 3;
   const uint32_t ring = smem_u32(smem) + warp * (FEW_STAGES * STEP_BYTES);
   const unsigned char* ring_p = smem + warp * (FEW_STAGES * STEP_BYTES);
 
-  // This CTA's share of all units' steps: [cur, end), from every request's
-  // length (the host has seen to it that the sum fits 32 bits).
-  int cur, end, b = 0, req_base = 0;  // req_base: first step of request b
-  if (f.split) {
-    if (warp == 0) {
-      int nn, kvl;
-      bool bad;
-      const int first = lane < a.B ? few_steps(a, lane, nn, kvl, bad) * a.Hkv : 0;
-      int sum = first;
+  // How the units' steps are dealt out, from every request's length (the host
+  // has seen to it that the sums fit 32 bits):
+  //   even     every unit in the same number of parts, a CTA each: no CTA
+  //            works on two units, the longest unit sets the time;
+  //   balanced shares of equal cost, cut anywhere, a unit costing its steps
+  //            and UNIT_COST for its start and end.
+  int cur, end, b = 0, req_base = 0;  // req_base: first cost of request b
+  int parts = 0;                      // even: parts a unit; 0: balanced
+  const int units = a.B * a.Hkv;
+  FewCut cut(1, 1);
+  if (f.split) {  // every warp for itself
+    int nn, kvl;
+    bool bad;
+    const int first = lane < a.B ? few_steps(a, lane, nn, kvl, bad) + UNIT_COST : 0;
+    int sum = first, longest = first;
 #pragma unroll 1
-      for (int i = lane + 32; i < a.B; i += 32) sum += few_steps(a, i, nn, kvl, bad) * a.Hkv;
-      const int total = __reduce_add_sync(0xFFFFFFFFu, sum);
-      const FewCut cut(total, gridDim.x);
-      const int start = cut.start(blockIdx.x);
-      int base = 0, found = 0;
+    for (int i = lane + 32; i < a.B; i += 32) {
+      const int st = few_steps(a, i, nn, kvl, bad) + UNIT_COST;
+      sum += st;
+      longest = max(longest, st);
+    }
+    cut = FewCut(__reduce_add_sync(0xFFFFFFFFu, sum) * a.Hkv, gridDim.x);
+    longest = __reduce_max_sync(0xFFFFFFFFu, longest);
+    if (units <= (int)gridDim.x) {
+      const int k = max(1, min((int)gridDim.x / units, (longest - UNIT_COST) / PART_STEPS));
+      if ((longest - UNIT_COST) / k <= cut.q) parts = k;
+    }
+    if (parts) {
+      cur = blockIdx.x;  // a part
+      end = min(units * parts, cur + 1);
+    } else {
+      cur = (int)blockIdx.x < cut.n ? cut.start(blockIdx.x) : 0;
+      end = (int)blockIdx.x < cut.n ? cut.start(blockIdx.x + 1) : 0;
 #pragma unroll 1
       for (int b0 = 0; b0 < a.B; b0 += 32) {
-        const int mine = b0 == 0 ? first : (b0 + lane < a.B ? few_steps(a, b0 + lane, nn, kvl, bad) * a.Hkv : 0);
+        const int mine =
+            (b0 == 0 ? first : (b0 + lane < a.B ? few_steps(a, b0 + lane, nn, kvl, bad) + UNIT_COST : 0)) * a.Hkv;
         int inc = mine;
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) {
           const int v = __shfl_up_sync(0xFFFFFFFFu, inc, o);
           if (lane >= o) inc += v;
         }
-        const uint32_t hit = __ballot_sync(0xFFFFFFFFu, base + inc > start);
+        const uint32_t hit = __ballot_sync(0xFFFFFFFFu, req_base + inc > cur);
         if (hit) {
           const int w = __ffs(hit) - 1;
-          found = b0 + w;
-          base += __shfl_sync(0xFFFFFFFFu, inc - mine, w);
+          b = b0 + w;
+          req_base += __shfl_sync(0xFFFFFFFFu, inc - mine, w);
           break;
         }
-        base += __shfl_sync(0xFFFFFFFFu, inc, 31);
+        req_base += __shfl_sync(0xFFFFFFFFu, inc, 31);
       }
-      if (lane == 0) s_total = total, s_begin = base, s_b = found;
     }
-    __syncthreads();
-    b = s_b;
-    req_base = s_begin;
-  }
-  const FewCut cut(f.split ? s_total : 1, gridDim.x);
-  if (f.split) {
-    if ((int)blockIdx.x >= cut.n) return;
-    cur = cut.start(blockIdx.x);
-    end = cut.start(blockIdx.x + 1);
   } else {
-    cur = blockIdx.x;  // a unit, not a step
-    end = a.B * a.Hkv;
+    cur = blockIdx.x;  // a unit
+    end = units;
   }
 
 #pragma unroll 1
   while (cur < end) {
-    // ---- the unit that cur lies in, and this CTA's steps [s0, s1) of it
-    int nn, kvl, gh, s0 = 0, s1, steps, unit_base = 0;
+    // ---- the next unit, this CTA's steps [s0, s1) of it, and the CTAs [c0, c0 + nc) that share it
+    int nn, kvl, gh, s0 = 0, s1, steps, c0 = 0, nc = 1, unit_base = 0;
     bool bad;
-    if (f.split) {
+    if (f.split && !parts) {
       steps = few_steps(a, b, nn, kvl, bad);
 #pragma unroll 1
-      while (cur - req_base >= steps * a.Hkv) {
-        req_base += steps * a.Hkv;
+      while (cur - req_base >= (steps + UNIT_COST) * a.Hkv) {
+        req_base += (steps + UNIT_COST) * a.Hkv;
         ++b;
         steps = few_steps(a, b, nn, kvl, bad);
       }
-      gh = (cur - req_base) / steps;
-      unit_base = req_base + gh * steps;
-      s0 = cur - unit_base;
-      s1 = min(steps, end - unit_base);
-      cur = unit_base + s1;
+      gh = (cur - req_base) / (steps + UNIT_COST);
+      unit_base = req_base + gh * (steps + UNIT_COST);
+      s0 = max(0, cur - unit_base - UNIT_COST);
+      cur = min(unit_base + UNIT_COST + steps, end);
+      s1 = cur - unit_base - UNIT_COST;
+      if (s1 <= s0) break;  // the share ends before the unit's first step
+      c0 = cut.share_of(unit_base + UNIT_COST);
+      nc = cut.share_of(unit_base + UNIT_COST + steps - 1) - c0 + 1;
     } else {
-      b = cur / a.Hkv;
-      gh = cur - b * a.Hkv;
+      const int unit = f.split ? cur / parts : cur;
+      b = unit / a.Hkv;
+      gh = unit - b * a.Hkv;
       steps = few_steps(a, b, nn, kvl, bad);
       s1 = steps;
       cur += gridDim.x;
+      if (f.split) {
+        c0 = unit * parts;
+        nc = max(1, min(parts, steps / PART_STEPS));  // a short unit in fewer parts
+        const int part = (int)blockIdx.x - c0, q = steps / nc, rem = steps - q * nc;
+        if (part >= nc) break;
+        s0 = part * q + min(part, rem);
+        s1 = s0 + q + (part < rem ? 1 : 0);
+      }
     }
+    // where CTA c keeps its piece of this unit: a balanced share's second piece apart from its first
+    auto piece = [&](int c) {
+      return f.part + (2 * c + (!parts && cut.start(c) < unit_base ? 1 : 0)) * (L::ROWS * (HD + 2));
+    };
     if (bad && gh == 0 && s0 == 0 && tid == 0) fc_flag(FC_ERR_WORD(a.err), FC_EBIT_INVALID);
     const int c_steps = nn == 0 ? 0 : (kvl + STEP - 1) / STEP;
     const int R = nn * a.G;  // rows in use: node-major, r = node * G + head in group
@@ -638,8 +665,7 @@ __global__ void __launch_bounds__(FEW_THREADS, NT == 1 ? 2 : 1) k_kv4_attn_few(F
     __syncthreads();
     const bool whole = s0 == 0 && s1 == steps;
     const int rows_all = a.n_pad * a.G;  // rows past the nodes are written as zeros
-    float* slot = whole ? nullptr
-                        : f.part + (2 * blockIdx.x + (cut.start(blockIdx.x) < unit_base ? 1 : 0)) * (L::ROWS * (HD + 2));
+    float* slot = piece(blockIdx.x);
     auto put = [&](int r, int d4, const float4& v) {
       const int i = r / a.G;
       __nv_bfloat16* dst = a.out + (((size_t)b * a.n_pad + i) * a.H + gh * a.G + (r - i * a.G)) * HD + 4 * d4;
@@ -677,20 +703,15 @@ __global__ void __launch_bounds__(FEW_THREADS, NT == 1 ? 2 : 1) k_kv4_attn_few(F
       // The last CTA to arrive adds up the pieces, in CTA order whichever it is.
       __threadfence();
       __syncthreads();
-      const int c0 = cut.share_of(unit_base), c1 = cut.share_of(unit_base + steps - 1);
       const int unit = b * a.Hkv + gh;
-      if (tid == 0) s_last = atomicAdd(f.cnt + unit, 1) == c1 - c0;
+      if (tid == 0) s_last = atomicAdd(f.cnt + unit, 1) == nc - 1;
       __syncthreads();
       if (s_last) {
         __threadfence();
         if (tid == 0) f.cnt[unit] = 0;  // fit for the next call
         // each piece's weight in a row, a warp a row ...
-        const int nc = c1 - c0 + 1;
         float* wt = reinterpret_cast<float*>(smem);  // [R][nc]
         float* red = wt + ((R * nc + 3) & ~3);       // [subsets][R][HD]
-        auto piece = [&](int c) {
-          return f.part + (2 * c + (cut.start(c) < unit_base ? 1 : 0)) * (L::ROWS * (HD + 2));
-        };
 #pragma unroll 1
         for (int r = warp; r < R; r += FEW_WARPS) {
           float mx = -INFINITY, sum = 0.f;
@@ -763,8 +784,8 @@ fc_status launch_few(const Kv4Args& a, void* ws, size_t ws_bytes, cudaStream_t s
   const size_t cnt = few_cnt_bytes(a.B, a.Hkv), one = (size_t)2 * FewSmem<NT>::ROWS * (HD + 2) * sizeof(float);
   const long long units = (long long)a.B * a.Hkv;
   // at most what the tables could hold, in steps (past 32 bits there are units enough without cutting them)
-  const long long most = units * ((((long long)a.max_pages << a.shift) + STEP - 1) / STEP + 1);
-  int grid = (int)std::max<long long>(1, std::min<long long>(full, most / FEW_MIN_STEPS));
+  const long long longest = (((long long)a.max_pages << a.shift) + STEP - 1) / STEP + 1, most = units * (longest + UNIT_COST);
+  int grid = (int)std::min<long long>(full, units * std::max<long long>(1, longest / PART_STEPS));
   FewArgs f{a, 1, nullptr, nullptr};
   if (ws && ws_bytes > cnt) grid = (int)std::min<size_t>(grid, (ws_bytes - cnt) / one);
   if (!ws || ws_bytes <= cnt || grid < 1 || most > 0x7FFFFFFFll) {
