@@ -111,9 +111,9 @@ __global__ void __launch_bounds__(128) k_kv4_attn_row(Kv4Args a) {
 //     row's reference m (O and the row sum are relative to it) moves when a w
 //     passes 2^15, to where the largest is 2^11 to 2^12: a running maximum of
 //     z + log2(value scale), moved lazily.  (High in fp16's range, so that a
-//     weight of 2^-25 of the largest keeps 11 bits.)  A key's scale counts as at least
-//     2^-80 in w, which no number of a row with a smaller one can show, so
-//     that 2^(z - m) stays below 2^95 in the row sum.
+//     weight of 2^-25 of the largest keeps 11 bits.)  For the
+//     reference a value scale counts as at least 2^-80, so that 2^(z - m), and
+//     the row sum, stay in fp32's range where a row of V is all zeros.
 // A warp takes every FEW_WARPS-th step of 32 keys (4224 bytes, two runs of 16
 // rows in a page), three steps in flight by 16-byte asynchronous copies.  S^T
 // becomes P^T's operand by 8x8 transposes in registers.
@@ -133,6 +133,7 @@ constexpr int STEP_BYTES = OFF_VSC + STEP * 2;
 // bandwidth; joining two parts of a unit about 4 us.
 constexpr int UNIT_COST = 30, PART_STEPS = 16;
 constexpr float W_MAX = 32768.f;
+constexpr int VS_MIN_EXP = -80;
 constexpr float VS_MIN = 0x1p-80f;
 constexpr float M_START = -1e30f;  // a reference before any key: 2^(z + 1e30) passes W_MAX, 2^(-1e30 - m) is 0
 
@@ -189,11 +190,6 @@ __device__ __forceinline__ uint32_t pack_f16x2(float lo, float hi) {
 __device__ __forceinline__ uint32_t less8(uint32_t v, uint32_t minus) {
   uint32_t r;
   asm("add.rn.f16x2 %0, %1, %2;" : "=r"(r) : "r"(v), "r"(minus));
-  return r;
-}
-__device__ __forceinline__ float max_nan(float a, float b) {  // a NaN stays
-  float r;
-  asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
   return r;
 }
 __device__ __forceinline__ float exp2_fast(float x) {
@@ -365,25 +361,35 @@ __global__ void __launch_bounds__(FEW_THREADS, NT == 1 ? 2 : 1) k_kv4_attn_few(F
     // runs of 16 rows are counted in 32 bits (1024 bytes each: 4 TB)
     const uint32_t runs_page = (uint32_t)a.Hkv << (a.shift - 4), run0 = (uint32_t)gh << (a.shift - 4);
     const uint32_t run_mask = (1u << (a.shift - 4)) - 1u;
-    auto issue = [&](int it, int stage) {
+    auto issue = [&](int it, int stage, uint32_t at) {
       if (it < n_it) {
         const int s = s0 + warp + it * FEW_WARPS;
         if ((it & 31) == 0) {
           const long long key = (long long)(s + lane * FEW_WARPS) * STEP;
           id_a = key < kvl ? tab[key >> a.shift] : 0;
-          id_b = key + 16 < kvl ? tab[(key + 16) >> a.shift] : 0;
+          id_b = a.shift == 4 && key + 16 < kvl ? tab[(key + 16) >> 4] : 0;
         }
-        int ia = __shfl_sync(0xFFFFFFFFu, id_a, it & 31), ib = __shfl_sync(0xFFFFFFFFu, id_b, it & 31);
-        if (max((unsigned)ia, (unsigned)ib) >= (unsigned)a.n_pages) {  // its keys are left out below
-          const bool xa = (unsigned)ia >= (unsigned)a.n_pages, xb = (unsigned)ib >= (unsigned)a.n_pages;
-          outside |= ((xa ? 1u : 0u) | (xb ? 2u : 0u)) << (2 * stage);
-          ia = xa ? 0 : ia;
-          ib = xb ? 0 : ib;
-          if (lane == 0) fc_flag(FC_ERR_WORD(a.err), FC_EBIT_INVALID);
+        int ia = __shfl_sync(0xFFFFFFFFu, id_a, it & 31);
+        uint32_t ra, rb;
+        if (a.shift > 4) {  // both runs in one page
+          if ((unsigned)ia >= (unsigned)a.n_pages) {  // its keys are left out below
+            outside |= 3u << (2 * stage);
+            ia = 0;
+          }
+          ra = ia * runs_page + (run0 + ((uint32_t)(2 * s) & run_mask));
+          rb = ra + 1;
+        } else {
+          int ib = __shfl_sync(0xFFFFFFFFu, id_b, it & 31);
+          if (max((unsigned)ia, (unsigned)ib) >= (unsigned)a.n_pages) {
+            const bool xa = (unsigned)ia >= (unsigned)a.n_pages, xb = (unsigned)ib >= (unsigned)a.n_pages;
+            outside |= ((xa ? 1u : 0u) | (xb ? 2u : 0u)) << (2 * stage);
+            ia = xa ? 0 : ia;
+            ib = xb ? 0 : ib;
+          }
+          ra = ia * runs_page + run0;
+          rb = ib * runs_page + run0;
         }
-        const uint32_t ra = ia * runs_page + (run0 + ((uint32_t)(2 * s) & run_mask));
-        const uint32_t rb = ib * runs_page + (run0 + ((uint32_t)(2 * s + 1) & run_mask));
-        const uint32_t d0 = put0 + stage * STEP_BYTES, d1 = d0 ^ 64u, d2 = d0 ^ 32u, d3 = d0 ^ 96u;
+        const uint32_t d0 = put0 + at, d1 = d0 ^ 64u, d2 = d0 ^ 32u, d3 = d0 ^ 96u;
         const uint8_t *ka = k_lane + (uint64_t)ra * 1024u, *kb = k_lane + (uint64_t)rb * 1024u;
         const uint8_t *va = v_lane + (uint64_t)ra * 1024u, *vb = v_lane + (uint64_t)rb * 1024u;
         cp_async16(d0, ka);
@@ -395,12 +401,12 @@ __global__ void __launch_bounds__(FEW_THREADS, NT == 1 ? 2 : 1) k_kv4_attn_few(F
         cp_async16(d2 + OFF_VROWS + 1024, vb);
         cp_async16(d3 + OFF_VROWS + 1536, vb + 512);
         if (lane < 8)  // K scales of the two runs, then V scales
-          cp_async16(ring + stage * STEP_BYTES + OFF_KSC + lane * 16, sc_lane + (uint64_t)((lane & 2) ? rb : ra) * 32u);
+          cp_async16(ring + at + OFF_KSC + lane * 16, sc_lane + (uint64_t)((lane & 2) ? rb : ra) * 32u);
       }
       cp_async_commit();
     };
 #pragma unroll 1
-    for (int it = 0; it < FEW_STAGES - 1; ++it) issue(it, it);
+    for (int it = 0; it < FEW_STAGES - 1; ++it) issue(it, it, it * STEP_BYTES);
     // ---- queries: the unit's power of two, then the operand registers
     // k-step 2i of word i of a key's 16-byte quarter t: dimensions 32t + 8i +
     // {0, 4} and {1, 5} / 16; k-step 2i + 1: {2, 6} and {3, 7} / 16
@@ -469,13 +475,14 @@ __global__ void __launch_bounds__(FEW_THREADS, NT == 1 ? 2 : 1) k_kv4_attn_few(F
           p[i][r] = exp2_fast(fmaf(d[i][r], ks[i], -m[n][r]));
           w[i][r] = p[i][r] * vs[i];
         }
+      float ps[2] = {(p[0][0] + p[1][0]) + (p[2][0] + p[3][0]), (p[0][1] + p[1][1]) + (p[2][1] + p[3][1])};
       const float sum = ((w[0][0] + w[0][1]) + (w[1][0] + w[1][1])) + ((w[2][0] + w[2][1]) + (w[3][0] + w[3][1]));
-      if (__any_sync(0xFFFFFFFFu, sum > W_MAX)) {
+      if (__any_sync(0xFFFFFFFFu, fmaf(ps[0] + ps[1], VS_MIN, sum) > W_MAX)) {
 #pragma unroll
         for (int r = 0; r < 2; ++r) {
           float top = M_START;
 #pragma unroll
-          for (int i = 0; i < 4; ++i) top = fmaxf(top, fmaf(d[i][r], ks[i], (float)(expo(vs[i]) - 11)));
+          for (int i = 0; i < 4; ++i) top = fmaxf(top, fmaf(d[i][r], ks[i], (float)(max(expo(vs[i]), VS_MIN_EXP) - 11)));
 #pragma unroll
           for (int x = 4; x < 32; x <<= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, x));
           const float mn = fmaxf(m[n][r], top), al = exp2_fast(m[n][r] - mn);
@@ -488,10 +495,11 @@ __global__ void __launch_bounds__(FEW_THREADS, NT == 1 ? 2 : 1) k_kv4_attn_few(F
             p[i][r] = exp2_fast(fmaf(d[i][r], ks[i], -mn));
             w[i][r] = p[i][r] * vs[i];
           }
+          ps[r] = (p[0][r] + p[1][r]) + (p[2][r] + p[3][r]);
         }
       }
-#pragma unroll
-      for (int r = 0; r < 2; ++r) l[n][r] += (p[0][r] + p[1][r]) + (p[2][r] + p[3][r]);
+      l[n][0] += ps[0];
+      l[n][1] += ps[1];
     };
 
     // ---- the loop over the steps
@@ -503,7 +511,10 @@ __global__ void __launch_bounds__(FEW_THREADS, NT == 1 ? 2 : 1) k_kv4_attn_few(F
       const int left = kvl - (s0 + warp + it * FEW_WARPS) * STEP;  // keys of the request from here on
       const uint32_t out_now = (outside >> (2 * stage)) & 3u;
       outside &= ~(3u << (2 * stage));
-      issue(it + FEW_STAGES - 1, stage == 0 ? FEW_STAGES - 1 : stage - 1);  // into the stage read in the last turn
+      {  // into the stage read in the last turn
+        const int last = stage == 0 ? FEW_STAGES - 1 : stage - 1;
+        issue(it + FEW_STAGES - 1, last, last * STEP_BYTES);
+      }
       const uint2 ks2 = *reinterpret_cast<const uint2*>(st + OFF_KSC + 8 * g);
       const uint2 vs2 = *reinterpret_cast<const uint2*>(st + OFF_VSC + 8 * g);
       float ks[4] = {lo_f(ks2.x) * z_mul, hi_f(ks2.x) * z_mul, lo_f(ks2.y) * z_mul, hi_f(ks2.y) * z_mul};
@@ -533,15 +544,14 @@ __global__ void __launch_bounds__(FEW_THREADS, NT == 1 ? 2 : 1) k_kv4_attn_few(F
 #pragma unroll
           for (int c = 0; c < 4; ++c) z[n][2 * h + (c >> 1)][c & 1] = d[n][c];
       }
-#pragma unroll
-      for (int i = 0; i < 4; ++i) vs[i] = max_nan(vs[i], VS_MIN);
       if (left < STEP || out_now) {
+        if (out_now && lane == 0) fc_flag(FC_ERR_WORD(a.err), FC_EBIT_INVALID);
         // keys past the request's end, or in a page outside the pool: no weight, whatever stands there
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           const int j = 4 * g + i;
           if (j >= left || ((out_now >> (j >> 4)) & 1u)) {
-            vs[i] = VS_MIN;
+            vs[i] = 0.f;
             ks[i] = 1.f;
 #pragma unroll
             for (int n = 0; n < NT; ++n) z[n][i][0] = z[n][i][1] = -INFINITY;
@@ -605,7 +615,7 @@ __global__ void __launch_bounds__(FEW_THREADS, NT == 1 ? 2 : 1) k_kv4_attn_few(F
       }
       const int words = (a.n_pad + 63) / 64;
       uint32_t pb[NT][2];
-      const float one[4] = {1.f, 1.f, VS_MIN, VS_MIN};
+      const float one[4] = {1.f, 1.f, 0.f, 0.f};
       const float by[4] = {a.scale_log2, a.scale_log2, 1.f, 1.f};
 #pragma unroll
       for (int n = 0; n < NT; ++n) {
