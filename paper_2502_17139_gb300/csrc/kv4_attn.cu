@@ -11,85 +11,6 @@ namespace {
 
 constexpr int HD = KV4_D;
 
-struct Kv4Args {
-  const __nv_bfloat16* q;
-  const uint8_t *kc, *vc;
-  const __nv_bfloat16 *ks, *vs;
-  const int32_t* table;
-  const int32_t* kv_len;
-  const __nv_bfloat16 *k_new, *v_new;
-  const uint64_t* mask;
-  const int32_t* n_nodes;
-  __nv_bfloat16* out;
-  int B, n_pad, H, Hkv, G, max_pages, n_pages, shift;
-  float scale_log2;
-  unsigned int* err;
-};
-
-// One warp a query row, one key at a time, four dimensions a lane.
-__global__ void __launch_bounds__(128) k_kv4_attn_row(Kv4Args a) {
-  const int lane = threadIdx.x & 31;
-  const long long row = (long long)blockIdx.x * 4 + (threadIdx.x >> 5);
-  if (row >= (long long)a.B * a.n_pad * a.H) return;
-  const int h = (int)(row % a.H), i = (int)(row / a.H % a.n_pad), b = (int)(row / a.H / a.n_pad), g = h / a.G;
-  const int kvl = a.kv_len[b], nn = a.n_nodes ? a.n_nodes[b] : a.n_pad;
-  const bool bad = nn < 0 || nn > a.n_pad || kvl < 0 || kvl > (long long)a.max_pages << a.shift;
-  if (bad && lane == 0) fc_flag(FC_ERR_WORD(a.err), FC_EBIT_INVALID);
-  auto f4 = [](const __nv_bfloat16* p, float (&v)[4]) {
-    const uint2 u = *reinterpret_cast<const uint2*>(p);
-    v[0] = __uint_as_float(u.x << 16), v[1] = __uint_as_float(u.x & 0xFFFF0000u);
-    v[2] = __uint_as_float(u.y << 16), v[3] = __uint_as_float(u.y & 0xFFFF0000u);
-  };
-  float q[4], o[4] = {0.f, 0.f, 0.f, 0.f};
-  f4(a.q + row * HD + 4 * lane, q);
-  float m = -INFINITY, l = 0.f;
-  auto key = [&](const float (&k)[4], const float (&v)[4]) {
-    float s = q[0] * k[0] + q[1] * k[1] + q[2] * k[2] + q[3] * k[3];
-#pragma unroll
-    for (int x = 16; x > 0; x >>= 1) s += __shfl_xor_sync(0xFFFFFFFFu, s, x);
-    s *= a.scale_log2;
-    const float mn = fmaxf(m, s), al = exp2f(m - mn), p = exp2f(s - mn);
-    l = l * al + p;
-#pragma unroll
-    for (int x = 0; x < 4; ++x) o[x] = o[x] * al + p * v[x];
-    m = mn;
-  };
-  if (!bad && i < nn) {
-    for (int j = 0; j < kvl; ++j) {
-      const int id = a.table[(size_t)b * a.max_pages + (j >> a.shift)];
-      if (id < 0 || id >= a.n_pages) {
-        if (lane == 0) fc_flag(FC_ERR_WORD(a.err), FC_EBIT_INVALID);
-        continue;
-      }
-      const size_t r = (((size_t)id * a.Hkv + g) << a.shift) + (j & ((1 << a.shift) - 1));
-      const float ks = __bfloat162float(a.ks[r]), vs = __bfloat162float(a.vs[r]);
-      const uint32_t kb = *reinterpret_cast<const uint16_t*>(a.kc + r * KV4_ROW + 2 * lane);
-      const uint32_t vb = *reinterpret_cast<const uint16_t*>(a.vc + r * KV4_ROW + 2 * lane);
-      float k[4], v[4];
-#pragma unroll
-      for (int x = 0; x < 4; ++x) {
-        k[x] = (float)((int)((kb >> (4 * x)) & 15u) - 8) * ks;
-        v[x] = (float)((int)((vb >> (4 * x)) & 15u) - 8) * vs;
-      }
-      key(k, v);
-    }
-    const int words = (a.n_pad + 63) / 64;
-    for (int j = 0; a.k_new && j < nn; ++j) {
-      const bool sees = a.mask ? (a.mask[((size_t)b * a.n_pad + i) * words + (j >> 6)] >> (j & 63)) & 1 : j <= i;
-      if (!sees) continue;
-      const size_t r = ((size_t)b * a.Hkv + g) * a.n_pad + j;
-      float k[4], v[4];
-      f4(a.k_new + r * HD + 4 * lane, k);
-      f4(a.v_new + r * HD + 4 * lane, v);
-      key(k, v);
-    }
-  }
-  const float inv = l > 0.f ? 1.f / l : 0.f;
-  *reinterpret_cast<uint2*>(a.out + row * HD + 4 * lane) =
-      make_uint2(pack_bf16x2(o[0] * inv, o[1] * inv), pack_bf16x2(o[2] * inv, o[3] * inv));
-}
-
-
 // ---------------------------------------------------------------------------
 // Few query rows for a kv head (n_pad * H / Hkv <= 16: single tokens, small
 // trees).  The cache's read bounds this, so the work is what it costs to turn
@@ -217,21 +138,6 @@ __device__ __forceinline__ int few_steps(const Kv4Args& a, int b, int& nn, int& 
   return nn == 0 ? 1 : max(1, (kvl + STEP - 1) / STEP + (a.k_new ? 1 : 0));
 }
 
-// A total cost cut into n shares of equal size, the first rem one longer.
-struct FewCut {
-  int n, q, rem;
-  __device__ __forceinline__ FewCut(int total, int grid) {
-    n = max(1, min(grid, total / (UNIT_COST + PART_STEPS)));
-    q = total / n;
-    rem = total - q * n;
-  }
-  __device__ __forceinline__ int start(int c) const { return c * q + min(c, rem); }
-  __device__ __forceinline__ int share_of(int step) const {
-    const int longer = rem * (q + 1);
-    return step < longer ? step / (q + 1) : rem + (step - longer) / q;
-  }
-};
-
 template <int NT>
 __global__ void __launch_bounds__(FEW_THREADS, NT == 1 ? 2 : 1) k_kv4_attn_few(FewArgs f) {
   using L = FewSmem<NT>;
@@ -251,7 +157,7 @@ __global__ void __launch_bounds__(FEW_THREADS, NT == 1 ? 2 : 1) k_kv4_attn_few(F
   int cur, end, b = 0, req_base = 0;  // req_base: first cost of request b
   int parts = 0;                      // even: parts a unit; 0: balanced
   const int units = a.B * a.Hkv;
-  FewCut cut(1, 1);
+  Kv4Cut cut(1, 1, 1);
   if (f.split) {  // every warp for itself
     int nn, kvl;
     bool bad;
@@ -263,7 +169,7 @@ __global__ void __launch_bounds__(FEW_THREADS, NT == 1 ? 2 : 1) k_kv4_attn_few(F
       sum += st;
       longest = max(longest, st);
     }
-    cut = FewCut(__reduce_add_sync(0xFFFFFFFFu, sum) * a.Hkv, gridDim.x);
+    cut = Kv4Cut(__reduce_add_sync(0xFFFFFFFFu, sum) * a.Hkv, gridDim.x, UNIT_COST + PART_STEPS);
     longest = __reduce_max_sync(0xFFFFFFFFu, longest);
     if (units <= (int)gridDim.x) {
       const int k = max(1, min((int)gridDim.x / units, (longest - UNIT_COST) / PART_STEPS));
@@ -820,7 +726,7 @@ bool shape_ok(int n_pad, int H, int Hkv) {
 extern "C" size_t fc_kv4_attn_workspace(int batch, int n_pad, int H, int Hkv) {
   if (batch < 1 || !shape_ok(n_pad, H, Hkv)) return 0;
   const int rows = n_pad * (H / Hkv);
-  if (rows > 16) return 256;
+  if (rows > 16) return kv4_attn_many_workspace(batch, n_pad, H, Hkv);
   return few_cnt_bytes(batch, Hkv) + (size_t)FEW_GRID * 2 * 8 * (HD + 2) * sizeof(float);
 }
 
@@ -862,8 +768,5 @@ extern "C" fc_status fc_kv4_attn(const void* d_q, const fc_kv4_cache* cache, con
   if ((long long)batch * a.Hkv > 0x7FFFFFFFll) return FC_ERR_UNSUPPORTED;
   if (n_pad * a.G <= 8) return launch_few<1>(a, d_ws, ws_bytes, s);
   if (n_pad * a.G <= 16) return launch_few<2>(a, d_ws, ws_bytes, s);
-  const long long rows = (long long)batch * n_pad * H;
-  if ((rows + 3) / 4 > 0x7FFFFFFFll) return FC_ERR_UNSUPPORTED;
-  k_kv4_attn_row<<<(unsigned)((rows + 3) / 4), 128, 0, s>>>(a);
-  return FC_CHECK_LAUNCH();
+  return kv4_attn_many(a, d_ws, ws_bytes, s);
 }

@@ -1,0 +1,803 @@
+// fc_kv4_attn for more than 16 query rows a kv head (draft trees, chunks): the
+// tensor cores' products over the paged 4-bit cache.
+//
+// A unit is up to 256 query rows of one (sequence, kv head) and all its keys,
+// in blocks of 128 keys, the new tokens the last.  Per block
+//   S = Q K^T,  z = S * (key scale),  P = 2^(z - m) * (value scale),  O += P V
+// with K and V the whole numbers -7..7 as bf16: the first product is exact, a
+// key's scale multiplies its column of scores and its column of P.
+//   * Four warps turn 4-bit rows into bf16 tiles in shared memory (128-byte
+//     swizzle), two stages of K and V each, one block ahead in registers.  A
+//     word's 8 numbers come out as the pairs (0,4) (1,5) (2,6) (3,7), so
+//     dimensions are kept in that order within groups of 8: queries and the
+//     new tokens' rows are put in it, the output taken out of it.
+//   * One warp issues every tcgen05.mma (accumulators and P in tensor memory).
+//   * Two softmax warpgroups, a row a thread.  With more than 128 rows each has
+//     its tile and both take every block; with fewer both have the same rows,
+//     one takes the even blocks and one the odd, and their halves are joined
+//     at the end, so that one tile's softmax always has the other's products
+//     beside it.
+//   * Three warps fetch the next unit's queries while this one's end is
+//     written.
+// The CTAs (one an SM) share all units' blocks equally, cut anywhere; a cut
+// unit's pieces go through the workspace to k_kv4_join.
+// Every mbarrier wait is bounded: one that runs out raises FC_ERR_TIMEOUT, the
+// CTA lets its issued products retire, frees its tensor memory and returns.
+#include <algorithm>
+#include <cmath>
+
+#include "fc_common.cuh"
+#include "kv4.cuh"
+
+FC_DEFINE_ERROR_WORD(kv4_tc)
+
+namespace {
+
+constexpr int HD = KV4_D;
+constexpr int THREADS = 512;  // warp 0 products, 1-3 queries, 4-7 / 8-11 softmax, 12-15 numbers to bf16
+constexpr int BM = 128, BN = 128, ROWS = 2 * BM;
+constexpr uint32_t HALF_BYTES = 128 * 128;         // 64 dims of 128 rows
+constexpr uint32_t TILE_BYTES = 2 * HALF_BYTES;
+constexpr uint32_t OFF_Q = 0;                      // two tiles
+constexpr uint32_t OFF_K = OFF_Q + 2 * TILE_BYTES; // two stages
+constexpr uint32_t OFF_V = OFF_K + 2 * TILE_BYTES;
+constexpr int SC_SLOTS = 4;
+constexpr uint32_t OFF_KS = OFF_V + 2 * TILE_BYTES;             // [slot][128] key scales (times the softmax's)
+constexpr uint32_t OFF_VS = OFF_KS + SC_SLOTS * BN * 4;         // [slot][128] value scales
+constexpr uint32_t OFF_KEEP = OFF_VS + SC_SLOTS * BN * 4;       // [slot][4] bits of the keys that count
+constexpr uint32_t OFF_ML = OFF_KEEP + SC_SLOTS * 16;           // [2 turns][2][128] (m, l) exchanged at a unit's end
+constexpr uint32_t OFF_BAR = OFF_ML + 4 * BM * 8;
+constexpr uint32_t SMEM_BYTES = OFF_BAR + 256 + 1024;           // + alignment slack
+constexpr uint32_t TMEM_COLS = 512;                             // S_0, S_1, O_0, O_1
+constexpr uint64_t WAIT_CYCLES = 4000000000ull;                 // ~2 s
+constexpr uint64_t DRAIN_CYCLES = 400000000ull;
+constexpr float RESCALE_THRESHOLD = 8.f;  // O is rescaled when a row's maximum (base 2) grows by more
+// A unit's start and end in blocks of one tile, and the least share worth a CTA.
+constexpr int UNIT_COST = 8, LEAST = 12;
+
+enum {
+  B_KFULL = 0,   // [2] 128 arrivals
+  B_VFULL = 2,   // [2] 128
+  B_KEMPTY = 4,  // [2]
+  B_VEMPTY = 6,  // [2]
+  B_SFULL = 8,   // [2 tiles]
+  B_PFULL = 10,  // [2 tiles] 128
+  B_SCALES = 12, // [4 slots] 128
+  B_QFULL = 16,  // 96
+  B_QFREE = 17,
+  B_OFIN = 18,
+  B_OFREE = 19,  // 256
+  B_ML = 20,     // 256: a row's halves exchanged
+  B_DRAIN = 21,
+  N_BARS = 22
+};
+
+struct ManyArgs {
+  Kv4Args a;
+  int chunks;      // most units a (sequence, kv head)
+  int split;       // 0: whole units, CTA by CTA
+  int rows_cap;    // rows a piece's slot has room for
+  int* list;       // [grid][8] cut units for k_kv4_join
+  float* part_o;   // [grid][2][rows_cap][HD]
+  float2* part_ml; // [grid][2][rows_cap]
+};
+
+__device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, volatile int* abort) {
+  return __all_sync(0xFFFFFFFFu, mbar_wait_bounded(bar, parity, abort, WAIT_CYCLES));
+}
+__device__ __forceinline__ float exp2_fast(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+__device__ __forceinline__ uint64_t f2_pack(float a, float b) {
+  uint64_t r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
+  return r;
+}
+__device__ __forceinline__ void f2_unpack(uint64_t v, float& a, float& b) {
+  asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(v));
+}
+__device__ __forceinline__ uint64_t f2_fma(uint64_t a, uint64_t b, uint64_t c) {
+  uint64_t d;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
+  return d;
+}
+__device__ __forceinline__ uint64_t f2_mul(uint64_t a, uint64_t b) {
+  uint64_t d;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+  return d;
+}
+__device__ __forceinline__ uint64_t f2_add(uint64_t a, uint64_t b) {
+  uint64_t d;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+  return d;
+}
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float d;
+  asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+  return d;
+}
+// 16 bytes of bf16 in dimension order to the tiles' order
+__device__ __forceinline__ uint4 permute8(const uint4& v) {
+  return make_uint4(__byte_perm(v.x, v.z, 0x5410), __byte_perm(v.x, v.z, 0x7632), __byte_perm(v.y, v.w, 0x5410),
+                    __byte_perm(v.y, v.w, 0x7632));
+}
+// 8 numbers (one word) to 8 bf16 values in the tiles' order: 0x4300 | c is 128 + c
+__device__ __forceinline__ uint4 to_bf16(uint32_t w) {
+  auto two = [](uint32_t v) {
+    uint32_t r;
+    asm("sub.rn.bf16x2 %0, %1, %2;" : "=r"(r) : "r"((v & 0x000F000Fu) | 0x43004300u), "r"(0x43084308u));
+    return r;
+  };
+  return make_uint4(two(w), two(w >> 4), two(w >> 8), two(w >> 12));
+}
+
+// The units' blocks dealt out, walked alike by every role of a CTA.
+struct Walk {
+  const ManyArgs& f;
+  Kv4Cut cut;
+  int cur, end, b, base;  // balanced: position, end, request, its first cost; whole units: unit, units
+  // the piece: blocks [s0, s1) of the unit's `blocks`
+  int gh, chunk, nn, kvl, R, row0, rows, cached, blocks, s0, s1, unit_base, cost;
+  bool bad, two;  // two: both softmax warpgroups' rows differ
+
+  struct Req {
+    int nn, kvl, R, n_chunks, rows_each, cached, blocks, w;
+    bool bad;
+  };
+  // chunk sizes are equal, so that a request's units cost the same
+  __device__ __forceinline__ Req req(int i) const {
+    const Kv4Args& a = f.a;
+    Req r;
+    r.kvl = a.kv_len[i];
+    r.nn = a.n_nodes ? a.n_nodes[i] : a.n_pad;
+    r.bad = r.nn < 0 || r.nn > a.n_pad || r.kvl < 0 || r.kvl > (long long)a.max_pages << a.shift;
+    if (r.bad) r.nn = r.kvl = 0;
+    r.R = r.nn * a.G;
+    r.n_chunks = max(1, (r.R + ROWS - 1) / ROWS);
+    r.rows_each = (r.R + r.n_chunks - 1) / r.n_chunks;
+    r.cached = r.R ? (r.kvl + BN - 1) / BN : 0;
+    r.blocks = max(1, r.cached + (a.k_new && r.R ? 1 : 0));
+    r.w = r.rows_each > BM ? 2 : 1;
+    return r;
+  }
+  __device__ __forceinline__ int unit_cost(const Req& r) const { return UNIT_COST + r.blocks * r.w; }
+
+  // every lane of a warp calls this
+  __device__ __noinline__ Walk(const ManyArgs& args) : f(args), cut(1, 1, 1) {
+    const Kv4Args& a = f.a;
+    const int lane = threadIdx.x & 31;
+    b = 0;
+    base = 0;
+    if (!f.split) {
+      cur = blockIdx.x;
+      end = a.B * a.Hkv * f.chunks;
+      return;
+    }
+    int sum = 0;
+#pragma unroll 1
+    for (int i = lane; i < a.B; i += 32) {
+      const Req r = req(i);
+      sum += unit_cost(r) * r.n_chunks;
+    }
+    cut = Kv4Cut(__reduce_add_sync(0xFFFFFFFFu, sum) * a.Hkv, gridDim.x, LEAST);
+    cur = (int)blockIdx.x < cut.n ? cut.start(blockIdx.x) : 0;
+    end = (int)blockIdx.x < cut.n ? cut.start(blockIdx.x + 1) : 0;
+#pragma unroll 1
+    for (int b0 = 0; b0 < a.B; b0 += 32) {
+      int mine = 0;
+      if (b0 + lane < a.B) {
+        const Req r = req(b0 + lane);
+        mine = unit_cost(r) * r.n_chunks * a.Hkv;
+      }
+      int inc = mine;
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const int v = __shfl_up_sync(0xFFFFFFFFu, inc, o);
+        if (lane >= o) inc += v;
+      }
+      const uint32_t hit = __ballot_sync(0xFFFFFFFFu, base + inc > cur);
+      if (hit) {
+        const int w = __ffs(hit) - 1;
+        b = b0 + w;
+        base += __shfl_sync(0xFFFFFFFFu, inc - mine, w);
+        break;
+      }
+      base += __shfl_sync(0xFFFFFFFFu, inc, 31);
+    }
+  }
+
+  // the next piece of this CTA; false when there is none
+  __device__ __noinline__ bool next() {
+    const Kv4Args& a = f.a;
+    for (;;) {
+      if (cur >= end) return false;
+      Req r;
+      if (f.split) {
+        r = req(b);
+        while (cur - base >= unit_cost(r) * r.n_chunks * a.Hkv) {
+          base += unit_cost(r) * r.n_chunks * a.Hkv;
+          ++b;
+          r = req(b);
+        }
+        cost = unit_cost(r);
+        const int u = (cur - base) / cost;
+        gh = u / r.n_chunks;
+        chunk = u - gh * r.n_chunks;
+        unit_base = base + u * cost;
+        // a block belongs to the share that holds its first cost
+        const int from = max(0, cur - unit_base - UNIT_COST), to = min(cost, end - unit_base) - UNIT_COST;
+        s0 = (from + r.w - 1) / r.w;
+        s1 = to <= 0 ? 0 : (to + r.w - 1) / r.w;
+        cur = min(unit_base + cost, end);
+      } else {
+        const int u = cur;
+        cur += gridDim.x;
+        b = u / (a.Hkv * f.chunks);
+        gh = u / f.chunks - b * a.Hkv;
+        chunk = u % f.chunks;
+        r = req(b);
+        if (chunk >= r.n_chunks) continue;
+        unit_base = cost = 0;
+        s0 = 0;
+        s1 = r.blocks;
+      }
+      if (s1 <= s0) continue;
+      nn = r.nn, kvl = r.kvl, R = r.R, bad = r.bad, cached = r.cached, blocks = r.blocks;
+      row0 = chunk * r.rows_each;
+      rows = max(0, min(r.rows_each, r.R - row0));
+      two = r.rows_each > BM;
+      return true;
+    }
+  }
+  __device__ __forceinline__ bool whole() const { return s0 == 0 && s1 == blocks; }
+  __device__ __forceinline__ int first_cta() const { return cut.share_of(unit_base + UNIT_COST); }
+  __device__ __forceinline__ int last_cta() const {
+    return cut.share_of(unit_base + UNIT_COST + (blocks - 1) * (two ? 2 : 1));
+  }
+  __device__ __forceinline__ int slot(int c) const { return 2 * c + (cut.start(c) < unit_base ? 1 : 0); }
+};
+
+__global__ void __launch_bounds__(THREADS, 1) k_kv4_attn_many(ManyArgs f) {
+  extern __shared__ __align__(1024) unsigned char smem_raw[];
+  __shared__ uint32_t s_tmem;
+  __shared__ volatile int s_abort;
+  const Kv4Args& a = f.a;
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  unsigned char* smem =
+      reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
+  const uint32_t sbase = smem_u32(smem);
+  const uint32_t sQ = sbase + OFF_Q, sK = sbase + OFF_K, sV = sbase + OFF_V;
+  auto bar = [&](int i) { return sbase + OFF_BAR + 8u * (uint32_t)i; };
+  if (tid == 0) {
+    s_abort = 0;
+    for (int i = 0; i < N_BARS; ++i) {
+      uint32_t n = 1;
+      if (i < B_KEMPTY || i == B_PFULL || i == B_PFULL + 1 || (i >= B_SCALES && i < B_SCALES + SC_SLOTS)) n = 128;
+      if (i == B_QFULL) n = 96;
+      if (i == B_OFREE || i == B_ML) n = 256;
+      mbar_init(bar(i), n);
+    }
+    fence_mbar_init();
+  }
+  if (warp == 0) {
+    tmem_alloc(smem_u32(&s_tmem), TMEM_COLS);
+    tmem_relinquish();
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = s_tmem;
+  Walk wk(f);
+
+  if (warp == 0) {
+    // ---------------- products ----------------
+    constexpr uint32_t IDESC_QK = idesc_bf16_f32(BM, BN, 0), IDESC_PV = idesc_bf16_f32(BM, HD, 1);
+    uint32_t nb = 0, np = 0, t_of[2] = {0, 0};  // blocks, pieces, steps of each tile so far
+    bool ok = true;
+    auto qk = [&](uint32_t blk, int x, int qx) {  // S_x <- Q_qx . K(blk)^T
+      const uint32_t kb = sK + (blk & 1) * TILE_BYTES, qb = sQ + qx * TILE_BYTES;
+#pragma unroll
+      for (int kk = 0; kk < HD / 16; ++kk) {
+        const uint32_t off = (kk >> 2) * HALF_BYTES + (kk & 3) * 32;
+        tc_mma_f16(tmem + x * 128, smem_desc_sw128(qb + off, 16, 1024), smem_desc_sw128(kb + off, 16, 1024), IDESC_QK,
+                   kk > 0);
+      }
+      tc_commit(bar(B_SFULL + x));
+    };
+    auto pv = [&](uint32_t blk, int x, bool add) {  // O_x (+)= P_x . V(blk)
+      const uint32_t vb = sV + (blk & 1) * TILE_BYTES;
+#pragma unroll
+      for (int kk = 0; kk < BN / 16; ++kk)
+        tc_mma_f16_tmem_a(tmem + 256 + x * 128, tmem + x * 128 + kk * 8, smem_desc_sw128(vb + kk * 2048, HALF_BYTES, 1024),
+                          IDESC_PV, add || kk > 0);
+    };
+    auto wait = [&](int which, uint32_t parity) {
+      ok = ok && warp_wait(bar(which), parity & 1, &s_abort);
+      tc_fence_after();
+      return ok;
+    };
+    while (ok && wk.next()) {
+      const int n = wk.s1 - wk.s0;
+      const uint32_t b0 = nb;
+      if (!wait(B_QFULL, np)) break;
+      if (wk.two) {
+        if (!wait(B_KFULL + (b0 & 1), b0 >> 1)) break;
+        qk(b0, 0, 0);
+        qk(b0, 1, 1);
+        tc_commit(bar(B_KEMPTY + (b0 & 1)));
+        if (n == 1) tc_commit(bar(B_QFREE));
+        for (int i = 1; ok && i <= n; ++i) {
+          const uint32_t p = b0 + i - 1, c = b0 + i;
+          if (!wait(B_VFULL + (p & 1), p >> 1)) break;
+          for (int x = 0; ok && x < 2; ++x) {
+            if (!wait(B_PFULL + x, t_of[x])) break;
+            ++t_of[x];
+            if (i == 1 && x == 0 && np > 0 && !wait(B_OFREE, np - 1)) break;
+            pv(p, x, i > 1);
+            if (i < n) {
+              if (x == 0 && !wait(B_KFULL + (c & 1), c >> 1)) break;
+              qk(c, x, x);
+            }
+          }
+          if (!ok) break;
+          if (i < n) tc_commit(bar(B_KEMPTY + (c & 1)));
+          if (i == n - 1) tc_commit(bar(B_QFREE));
+          tc_commit(bar(B_VEMPTY + (p & 1)));
+        }
+      } else {
+        for (int i = 0; ok && i < min(2, n); ++i) {
+          const uint32_t c = b0 + i;
+          if (!wait(B_KFULL + (c & 1), c >> 1)) break;
+          qk(c, i, 0);
+          tc_commit(bar(B_KEMPTY + (c & 1)));
+          if (i == n - 1) tc_commit(bar(B_QFREE));
+        }
+        for (int i = 0; ok && i < n; ++i) {
+          const uint32_t p = b0 + i, c = p + 2;
+          const int x = i & 1;
+          if (!wait(B_VFULL + (p & 1), p >> 1)) break;
+          if (!wait(B_PFULL + x, t_of[x])) break;
+          ++t_of[x];
+          if (i == 0 && np > 0 && !wait(B_OFREE, np - 1)) break;
+          pv(p, x, i > 1);
+          tc_commit(bar(B_VEMPTY + (p & 1)));
+          if (i + 2 < n) {
+            if (!wait(B_KFULL + (c & 1), c >> 1)) break;
+            qk(c, x, 0);
+            tc_commit(bar(B_KEMPTY + (c & 1)));
+            if (i + 2 == n - 1) tc_commit(bar(B_QFREE));
+          }
+        }
+      }
+      if (!ok) break;
+      tc_commit(bar(B_OFIN));
+      nb += n;
+      ++np;
+    }
+    if (__any_sync(0xFFFFFFFFu, s_abort)) {  // let issued products retire before the tensor memory is freed
+      tc_commit(bar(B_DRAIN));
+      volatile int dummy = 0;
+      mbar_wait_bounded(bar(B_DRAIN), 0, &dummy, DRAIN_CYCLES);
+    }
+  } else if (warp < 4) {
+    // ---------------- queries, padding rows, the list of cut units ----------------
+    const int qt = tid - 32;  // 0..95
+    uint32_t np = 0;
+    if (f.split && qt == 0) f.list[8 * blockIdx.x] = -1;
+    while (wk.next()) {
+      if (np > 0 && !warp_wait(bar(B_QFREE), (np - 1) & 1, &s_abort)) break;
+      const int lim = wk.two ? 2 * BM * 16 : BM * 16;
+#pragma unroll 4
+      for (int e = qt; e < lim; e += 96) {
+        const int r = e >> 4, ch = e & 15;
+        // rows [0, 128) are tile 0, the others tile 1
+        uint4 v = make_uint4(0, 0, 0, 0);
+        if (r < wk.rows) {
+          const int rr = wk.row0 + r, i = rr / a.G, hh = rr - i * a.G;
+          v = permute8(reinterpret_cast<const uint4*>(
+              a.q + (((size_t)wk.b * a.n_pad + i) * a.H + wk.gh * a.G + hh) * HD)[ch]);
+        }
+        *reinterpret_cast<uint4*>(smem + OFF_Q + (r >> 7) * TILE_BYTES + (ch >> 3) * HALF_BYTES + (r & 127) * 128 +
+                                  (((ch & 7) ^ (r & 7)) << 4)) = v;
+      }
+      fence_proxy_async_smem();
+      mbar_arrive(bar(B_QFULL));
+      if (wk.s0 == 0 && wk.chunk == 0) {
+        if (wk.bad && wk.gh == 0 && qt == 0) fc_flag(FC_ERR_WORD(a.err), FC_EBIT_INVALID);
+        const int pad = (a.n_pad - wk.nn) * a.G;
+        for (int e = qt; e < pad * (HD / 8); e += 96) {
+          const int r = e / (HD / 8), ch = e % (HD / 8), i = wk.nn + r / a.G, hh = r % a.G;
+          reinterpret_cast<uint4*>(a.out + (((size_t)wk.b * a.n_pad + i) * a.H + wk.gh * a.G + hh) * HD)[ch] =
+              make_uint4(0, 0, 0, 0);
+        }
+      }
+      if (f.split && wk.s0 > 0 && qt == 0 && wk.first_cta() + 1 == (int)blockIdx.x) {  // one entry a cut unit
+        const int c0 = blockIdx.x - 1;
+        int* e = f.list + 8 * blockIdx.x;
+        e[1] = wk.gh, e[2] = wk.row0, e[3] = wk.rows, e[4] = c0, e[5] = wk.last_cta() - c0 + 1, e[6] = wk.slot(c0);
+        e[0] = wk.b;
+      }
+      ++np;
+    }
+  } else if (warp >= 12) {
+    // ---------------- numbers to bf16 tiles ----------------
+    const int r = tid - 384, w = warp - 12, c = lane & 3, rho = lane >> 2;
+    // 32-row pass p: row 32p + 8w + rho, 16 bytes c of its 64; the lanes of the
+    // two 64-dim halves take their words two apart, so that eight lanes' stores
+    // fall in different banks
+    const int swap = c >> 1;
+    uint32_t dst[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      dst[i] = swap * HALF_BYTES + (8 * w + rho) * 128 + ((((c & 1) * 4 + (i ^ (2 * swap))) ^ rho) << 4);
+    uint4 kr[4], vr[4];
+    uint32_t rowi[4];  // the block's run of 8 rows of each pass, in units of 8 rows
+    float ksc = 0.f, vsc = 0.f;
+    bool live = false;
+    uint32_t nb = 0;
+    bool ok = true;
+    const uint32_t per_page = (uint32_t)a.Hkv << (a.shift - 3);
+    auto find = [&](int blk) {  // page ids and scales of cached block blk
+      const int32_t* tab = a.table + (size_t)wk.b * a.max_pages;
+      const uint32_t head = (uint32_t)wk.gh << (a.shift - 3), in_page = (1u << (a.shift - 3)) - 1u;
+#pragma unroll
+      for (int p = 0; p < 4; ++p) {
+        const long long key = (long long)blk * BN + 32 * p + 8 * w;
+        int id = key < wk.kvl ? tab[key >> a.shift] : -1;
+        rowi[p] = (unsigned)id < (unsigned)a.n_pages
+                      ? id * per_page + head + ((uint32_t)(key >> 3) & in_page)
+                      : 0xFFFFFFFFu;
+      }
+      const long long key = (long long)blk * BN + r;
+      live = false;
+      ksc = vsc = 0.f;
+      if (key < wk.kvl) {
+        const int id = tab[key >> a.shift];
+        live = (unsigned)id < (unsigned)a.n_pages;
+        if (live) {
+          const size_t at = (((size_t)id * a.Hkv + wk.gh) << a.shift) + (key & ((1 << a.shift) - 1));
+          ksc = __bfloat162float(a.ks[at]) * a.scale_log2;
+          vsc = __bfloat162float(a.vs[at]);
+        } else {
+          fc_flag(FC_ERR_WORD(a.err), FC_EBIT_INVALID);
+        }
+      }
+    };
+    auto load = [&](const uint8_t* codes, uint4 (&x)[4]) {
+#pragma unroll
+      for (int p = 0; p < 4; ++p)
+        x[p] = rowi[p] != 0xFFFFFFFFu
+                   ? *reinterpret_cast<const uint4*>(codes + (uint64_t)rowi[p] * 512u + lane * 16)
+                   : make_uint4(0x88888888u, 0x88888888u, 0x88888888u, 0x88888888u);
+    };
+    auto store = [&](uint32_t tile, const uint4 (&x)[4]) {
+#pragma unroll
+      for (int p = 0; p < 4; ++p) {
+        const uint32_t w0 = swap ? x[p].z : x[p].x, w1 = swap ? x[p].w : x[p].y;
+        const uint32_t w2 = swap ? x[p].x : x[p].z, w3 = swap ? x[p].y : x[p].w;
+        unsigned char* t = smem + tile + p * 4096;
+        *reinterpret_cast<uint4*>(t + dst[0]) = to_bf16(w0);
+        *reinterpret_cast<uint4*>(t + dst[1]) = to_bf16(w1);
+        *reinterpret_cast<uint4*>(t + dst[2]) = to_bf16(w2);
+        *reinterpret_cast<uint4*>(t + dst[3]) = to_bf16(w3);
+      }
+    };
+    auto store_new = [&](uint32_t tile, const __nv_bfloat16* src) {  // the new tokens' rows, zeros past them
+      const size_t row = ((size_t)wk.b * a.Hkv + wk.gh) * a.n_pad;
+#pragma unroll 1
+      for (int e = r; e < BN * 16; e += 128) {
+        const int j = e >> 4, ch = e & 15;
+        uint4 v = make_uint4(0, 0, 0, 0);
+        if (src && j < wk.nn) v = permute8(reinterpret_cast<const uint4*>(src + (row + j) * HD)[ch]);
+        *reinterpret_cast<uint4*>(smem + tile + (ch >> 3) * HALF_BYTES + j * 128 + (((ch & 7) ^ (j & 7)) << 4)) = v;
+      }
+    };
+    while (ok && wk.next()) {
+      if (wk.s0 < wk.cached) {
+        find(wk.s0);
+        load(a.kc, kr);
+        load(a.vc, vr);
+      }
+      for (int blk = wk.s0; blk < wk.s1; ++blk, ++nb) {
+        const int st = nb & 1, slot = nb & (SC_SLOTS - 1);
+        const bool fresh = blk >= wk.cached, more = blk + 1 < wk.s1 && blk + 1 < wk.cached;
+        // scales: the slot's last readers are done (the V stage of three blocks ago was waited for)
+        if (fresh) {
+          live = a.k_new && r < wk.nn;
+          ksc = a.scale_log2;
+          vsc = 1.f;
+        }
+        reinterpret_cast<float*>(smem + OFF_KS)[slot * BN + r] = live ? ksc : 0.f;
+        reinterpret_cast<float*>(smem + OFF_VS)[slot * BN + r] = live ? vsc : 0.f;
+        const uint32_t keep = __ballot_sync(0xFFFFFFFFu, live);
+        if (lane == 0) reinterpret_cast<uint32_t*>(smem + OFF_KEEP)[slot * 4 + w] = keep;
+        __syncwarp();
+        mbar_arrive(bar(B_SCALES + slot));
+        if (nb >= 2 && !(ok = warp_wait(bar(B_KEMPTY + st), ((nb >> 1) - 1) & 1, &s_abort))) break;
+        if (!fresh) store(OFF_K + st * TILE_BYTES, kr);
+        else store_new(OFF_K + st * TILE_BYTES, a.k_new);
+        fence_proxy_async_smem();
+        mbar_arrive(bar(B_KFULL + st));
+        if (more) {
+          find(blk + 1);
+          load(a.kc, kr);
+        }
+        if (nb >= 2 && !(ok = warp_wait(bar(B_VEMPTY + st), ((nb >> 1) - 1) & 1, &s_abort))) break;
+        if (!fresh) store(OFF_V + st * TILE_BYTES, vr);
+        else store_new(OFF_V + st * TILE_BYTES, a.v_new);
+        fence_proxy_async_smem();
+        mbar_arrive(bar(B_VFULL + st));
+        if (more) load(a.vc, vr);
+      }
+    }
+  } else {
+    // ---------------- softmax: warpgroup x, a row a thread ----------------
+    const int x = (warp - 4) >> 2, q4 = warp & 3, r = q4 * 32 + lane;
+    const uint32_t lane_off = (uint32_t)(q4 * 32) << 16;
+    const uint32_t tS = tmem + x * 128 + lane_off;
+    uint32_t nb = 0, np = 0, nx = 0, t = 0;
+    bool ok = true;
+    while (ok && wk.next()) {
+      const int n = wk.s1 - wk.s0;
+      const int lr = wk.two ? x * BM + r : r;  // row of the piece
+      const bool row_ok = lr < wk.rows;
+      const int rr = wk.row0 + lr, i = row_ok ? rr / a.G : 0, hh = row_ok ? rr - i * a.G : 0;
+      // the new tokens that this row sees
+      uint64_t m0 = 0, m1 = 0;
+      if (wk.s1 > wk.cached && row_ok) {
+        if (a.mask) {
+          const int words = (a.n_pad + 63) / 64;
+          const uint64_t* mr = a.mask + ((size_t)wk.b * a.n_pad + i) * words;
+          m0 = mr[0];
+          m1 = words > 1 ? mr[1] : 0ull;
+        } else {
+          m0 = i >= 63 ? ~0ull : (1ull << (i + 1)) - 1ull;
+          m1 = i < 64 ? 0ull : (i >= 127 ? ~0ull : (1ull << (i - 63)) - 1ull);
+        }
+      }
+      float m = -INFINITY, l = 0.f;
+      bool any = false;  // O_x holds a product
+      const uint32_t tO = tmem + 256 + x * 128 + lane_off;
+      for (int j = wk.two ? 0 : x; j < n; j += wk.two ? 1 : 2, ++t) {
+        const int slot = (nb + j) & (SC_SLOTS - 1);
+        if (!(ok = warp_wait(bar(B_SCALES + slot), ((nb + j) / SC_SLOTS) & 1, &s_abort))) break;
+        if (!(ok = warp_wait(bar(B_SFULL + x), t & 1, &s_abort))) break;
+        tc_fence_after();
+        const float4* ks4 = reinterpret_cast<const float4*>(smem + OFF_KS) + slot * (BN / 4);
+        const float4* vs4 = reinterpret_cast<const float4*>(smem + OFF_VS) + slot * (BN / 4);
+        const uint4 kp = *reinterpret_cast<const uint4*>(smem + OFF_KEEP + slot * 16);
+        const bool fresh = wk.s0 + j >= wk.cached;
+        const bool masked = fresh || (kp.x & kp.y & kp.z & kp.w) != 0xFFFFFFFFu;  // alike in the warpgroup
+        auto keep_bits = [&](int c4) {
+          const uint32_t k = reinterpret_cast<const uint32_t*>(smem + OFF_KEEP)[slot * 4 + c4];
+          return fresh ? k & (uint32_t)((c4 < 2 ? m0 : m1) >> (32 * (c4 & 1))) : k;
+        };
+        auto scores = [&](int c4, float (&z)[32]) {  // 32 columns of this row, scaled; masked ones -inf
+          uint32_t s[32];
+          tmem_ld32(tS + c4 * 32, s);
+          tc_wait_ld();
+#pragma unroll
+          for (int u = 0; u < 8; ++u) {
+            const float4 k = ks4[c4 * 8 + u];
+            f2_unpack(f2_mul(f2_pack(__uint_as_float(s[4 * u]), __uint_as_float(s[4 * u + 1])), f2_pack(k.x, k.y)),
+                      z[4 * u], z[4 * u + 1]);
+            f2_unpack(f2_mul(f2_pack(__uint_as_float(s[4 * u + 2]), __uint_as_float(s[4 * u + 3])), f2_pack(k.z, k.w)),
+                      z[4 * u + 2], z[4 * u + 3]);
+          }
+          if (masked) {
+            const uint32_t keep = keep_bits(c4);
+#pragma unroll
+            for (int u = 0; u < 32; ++u)
+              if (!((keep >> u) & 1u)) z[u] = -INFINITY;
+          }
+        };
+        float top = -INFINITY;
+#pragma unroll 1
+        for (int c4 = 0; c4 < 4; ++c4) {
+          float z[32];
+          scores(c4, z);
+#pragma unroll
+          for (int u = 0; u < 32; u += 2) top = max3(top, z[u], z[u + 1]);
+        }
+        const float m_new = top > m + RESCALE_THRESHOLD ? top : m;
+        const float m_use = m_new == -INFINITY ? 0.f : m_new;
+        const float alpha = exp2_fast(m - m_use);
+        // S_x is the newest product of this tile, so O_x is complete
+        if (any && __any_sync(0xFFFFFFFFu, alpha != 1.f)) {
+#pragma unroll 1
+          for (int cc = 0; cc < HD / 32; ++cc) {
+            uint32_t o[32];
+            tmem_ld32(tO + cc * 32, o);
+            tc_wait_ld();
+#pragma unroll
+            for (int u = 0; u < 32; ++u) o[u] = __float_as_uint(__uint_as_float(o[u]) * alpha);
+            tmem_st32(tO + cc * 32, o);
+          }
+        }
+        uint64_t sum[2] = {0ull, 0ull};
+        const uint64_t neg = f2_pack(-m_use, -m_use);
+#pragma unroll 1
+        for (int c4 = 0; c4 < 4; ++c4) {
+          float z[32];
+          scores(c4, z);
+          uint32_t pk[16];
+#pragma unroll
+          for (int u = 0; u < 8; ++u) {
+            const float4 v = vs4[c4 * 8 + u];
+            float p0, p1, p2, p3;
+            f2_unpack(f2_add(f2_pack(z[4 * u], z[4 * u + 1]), neg), p0, p1);
+            f2_unpack(f2_add(f2_pack(z[4 * u + 2], z[4 * u + 3]), neg), p2, p3);
+            p0 = exp2_fast(p0), p1 = exp2_fast(p1), p2 = exp2_fast(p2), p3 = exp2_fast(p3);
+            const uint64_t a0 = f2_pack(p0, p1), a1 = f2_pack(p2, p3);
+            sum[0] = f2_add(sum[0], a0);
+            sum[1] = f2_add(sum[1], a1);
+            f2_unpack(f2_mul(a0, f2_pack(v.x, v.y)), p0, p1);
+            f2_unpack(f2_mul(a1, f2_pack(v.z, v.w)), p2, p3);
+            pk[2 * u] = pack_bf16x2(p0, p1);
+            pk[2 * u + 1] = pack_bf16x2(p2, p3);
+          }
+          tmem_st16(tS + c4 * 16, pk);  // over columns already read
+        }
+        tc_wait_st();
+        float s0, s1, s2, s3;
+        f2_unpack(sum[0], s0, s1);
+        f2_unpack(sum[1], s2, s3);
+        l = l * alpha + ((s0 + s1) + (s2 + s3));
+        m = m_new;
+        any = true;
+        tc_fence_before();
+        mbar_arrive(bar(B_PFULL + x));
+      }
+      if (!ok || !(ok = warp_wait(bar(B_OFIN), np & 1, &s_abort))) break;
+      tc_fence_after();
+      // ---- the piece's rows: this tile's, or half the dimensions of both halves' sum
+      const bool whole = wk.whole() || !f.split;
+      const size_t slot = whole ? 0 : (size_t)wk.slot(blockIdx.x) * f.rows_cap;
+      __nv_bfloat16* dst = a.out + (((size_t)wk.b * a.n_pad + i) * a.H + wk.gh * a.G + hh) * HD;
+      float m_all = m, k0 = 1.f, k1 = 0.f;
+      bool have0 = any, have1 = false;
+      uint32_t tO0 = tO, tO1 = tO;
+      int cc0 = 0, cc1 = HD / 32;
+      if (!wk.two) {
+        // two turns' room: a turn is written again only after both have read it
+        float2* ml = reinterpret_cast<float2*>(smem + OFF_ML) + (nx & 1) * 2 * BM;
+        ml[x * BM + r] = make_float2(m, l);
+        mbar_arrive(bar(B_ML));
+        if (!(ok = warp_wait(bar(B_ML), nx & 1, &s_abort))) break;
+        ++nx;
+        const float2 other = ml[(1 - x) * BM + r];
+        m_all = fmaxf(m, other.x);
+        const float mu = m_all == -INFINITY ? 0.f : m_all;
+        const float mine = exp2_fast(m - mu), theirs = exp2_fast(other.x - mu);
+        l = l * mine + other.y * theirs;
+        k0 = x == 0 ? mine : theirs;
+        k1 = x == 0 ? theirs : mine;
+        have0 = n > 0;
+        have1 = n > 1;
+        tO0 = tmem + 256 + lane_off;
+        tO1 = tO0 + 128;
+        cc0 = 2 * x;
+        cc1 = cc0 + 2;
+      }
+      const float inv = !whole ? 1.f : (l == 0.f ? 0.f : 1.f / l);
+#pragma unroll 1
+      for (int cc = cc0; cc < cc1; ++cc) {
+        uint32_t o[32], o1[32];
+        float v[32];
+        if (have0) tmem_ld32(tO0 + cc * 32, o);
+        if (have1) tmem_ld32(tO1 + cc * 32, o1);
+        tc_wait_ld();
+#pragma unroll
+        for (int u = 0; u < 32; ++u) {
+          float y = have0 ? __uint_as_float(o[u]) * k0 : 0.f;
+          if (have1) y += __uint_as_float(o1[u]) * k1;
+          v[u] = y * inv;
+        }
+        if (row_ok) {
+#pragma unroll
+          for (int u = 0; u < 32; u += 8) {  // out of the tiles' order: 0 4 1 5 2 6 3 7
+            if (whole) {
+              *reinterpret_cast<uint4*>(dst + cc * 32 + u) =
+                  make_uint4(pack_bf16x2(v[u], v[u + 2]), pack_bf16x2(v[u + 4], v[u + 6]),
+                             pack_bf16x2(v[u + 1], v[u + 3]), pack_bf16x2(v[u + 5], v[u + 7]));
+            } else {
+              float4* po = reinterpret_cast<float4*>(f.part_o + (slot + lr) * HD + cc * 32 + u);
+              po[0] = make_float4(v[u], v[u + 2], v[u + 4], v[u + 6]);
+              po[1] = make_float4(v[u + 1], v[u + 3], v[u + 5], v[u + 7]);
+            }
+          }
+        }
+      }
+      if (!whole && row_ok && (wk.two || x == 0)) f.part_ml[slot + lr] = make_float2(m_all, l);
+      tc_fence_before();
+      mbar_arrive(bar(B_OFREE));
+      nb += n;
+      ++np;
+    }
+  }
+  tc_fence_before();
+  __syncthreads();
+  if (tid == 0 && s_abort) fc_flag(FC_ERR_WORD(a.err), FC_EBIT_TIMEOUT);
+  if (warp == 0) {
+    tc_fence_after();
+    tmem_dealloc(tmem, TMEM_COLS);
+  }
+}
+
+// The pieces of cut units, added up in CTA order.  CTA (c, y): the unit whose
+// second piece CTA c of k_kv4_attn_many began with, 8 of its rows, a warp each.
+__global__ void __launch_bounds__(256) k_kv4_join(ManyArgs f) {
+  const Kv4Args& a = f.a;
+  const int* e = f.list + 8 * blockIdx.x;
+  const int b = e[0];
+  if (b < 0) return;
+  const int gh = e[1], row0 = e[2], rows = e[3], c0 = e[4], nc = e[5], slot0 = e[6];
+  const int lane = threadIdx.x & 31, r = blockIdx.y * 8 + (threadIdx.x >> 5);
+  if (r >= rows) return;
+  auto slot = [&](int c) { return (size_t)(c == 0 ? slot0 : 2 * (c0 + c)) * f.rows_cap + r; };
+  float m = -INFINITY;
+  for (int c = lane; c < nc; c += 32) m = fmaxf(m, f.part_ml[slot(c)].x);
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xFFFFFFFFu, m, o));
+  if (m == -INFINITY) m = 0.f;
+  float l = 0.f;
+  float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 4
+  for (int c = 0; c < nc; ++c) {
+    const float2 ml = f.part_ml[slot(c)];
+    const float4 v = reinterpret_cast<const float4*>(f.part_o + slot(c) * HD)[lane];
+    const float k = exp2_fast(ml.x - m);
+    l += ml.y * k;
+    acc.x += v.x * k, acc.y += v.y * k, acc.z += v.z * k, acc.w += v.w * k;
+  }
+  const float inv = l == 0.f ? 0.f : 1.f / l;
+  const int i = (row0 + r) / a.G, hh = (row0 + r) - i * a.G;
+  __nv_bfloat16* dst = a.out + (((size_t)b * a.n_pad + i) * a.H + gh * a.G + hh) * HD + 4 * lane;
+  *reinterpret_cast<uint2*>(dst) =
+      make_uint2(pack_bf16x2(acc.x * inv, acc.y * inv), pack_bf16x2(acc.z * inv, acc.w * inv));
+}
+
+int rows_of_chunk(int n_pad, int G) { return std::min(ROWS, n_pad * G); }
+
+size_t list_bytes(int grid) { return ((size_t)grid * 32 + 255) / 256 * 256; }
+size_t slot_bytes(int rows) { return (size_t)rows * (HD * sizeof(float) + sizeof(float2)); }
+
+constexpr int FULL_GRID = 152;
+
+}  // namespace
+
+size_t kv4_attn_many_workspace(int batch, int n_pad, int H, int Hkv) {
+  (void)batch;
+  return list_bytes(FULL_GRID) + (size_t)FULL_GRID * 2 * slot_bytes(rows_of_chunk(n_pad, H / Hkv));
+}
+
+fc_status kv4_attn_many(const Kv4Args& a, void* ws, size_t ws_bytes, cudaStream_t s) {
+  static std::atomic<unsigned long long> done{0};
+  const fc_status st = fc_once_per_device(done, [](int) {
+    return fc_cuda_status(cudaFuncSetAttribute(k_kv4_attn_many, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM_BYTES));
+  });
+  if (st != FC_OK) return st;
+  ManyArgs f{a, 0, 1, rows_of_chunk(a.n_pad, a.G), nullptr, nullptr, nullptr};
+  f.chunks = (a.n_pad * a.G + ROWS - 1) / ROWS;
+  const long long units = (long long)a.B * a.Hkv * f.chunks;
+  if (units > 0x7FFFFFFFll) return FC_ERR_UNSUPPORTED;
+  const long long longest = (((long long)a.max_pages << a.shift) + BN - 1) / BN + 1;
+  const bool fits = units * (UNIT_COST + 2 * longest) <= 0x7FFFFFFFll;
+  int grid = (int)std::min<long long>(FULL_GRID, units * ((UNIT_COST + 2 * longest) / LEAST));
+  while (grid > 1 && ws && list_bytes(grid) + (size_t)grid * 2 * slot_bytes(f.rows_cap) > ws_bytes) --grid;
+  if (!ws || !fits || list_bytes(grid) + (size_t)grid * 2 * slot_bytes(f.rows_cap) > ws_bytes ||
+      (grid < FULL_GRID && units >= FULL_GRID)) {
+    f.split = 0;
+    grid = (int)std::min<long long>(units, FULL_GRID);
+  } else {
+    unsigned char* p = static_cast<unsigned char*>(ws);
+    f.list = reinterpret_cast<int*>(p);
+    f.part_o = reinterpret_cast<float*>(p + list_bytes(grid));
+    f.part_ml = reinterpret_cast<float2*>(f.part_o + (size_t)grid * 2 * f.rows_cap * HD);
+  }
+  k_kv4_attn_many<<<grid, THREADS, SMEM_BYTES, s>>>(f);
+  if (f.split && grid > 1) k_kv4_join<<<dim3(grid, (f.rows_cap + 7) / 8), 256, 0, s>>>(f);
+  return FC_CHECK_LAUNCH();
+}
