@@ -3,14 +3,24 @@
 //
 // A unit is up to 256 query rows of one (sequence, kv head) and all its keys,
 // in blocks of 128 keys, the new tokens the last.  Per block
-//   S = Q K^T,  z = S * (key scale),  P = 2^(z - m) * (value scale),  O += P V
-// with K and V the whole numbers -7..7 as bf16: the first product is exact, a
-// key's scale multiplies its column of scores and its column of P.
-//   * Four warps turn 4-bit rows into bf16 tiles in shared memory (128-byte
+//   S = Q K^T,  P = 2^(c S - m) * (value scale),  O += P V.
+// The first product is in fp16: a cached key's values c * s have at most 3 + 8
+// significant bits, so they are exact, and powers of two (one per query row,
+// one per block of K) keep them in range.  The second is in bf16, P needing
+// its range: V the whole numbers -7..7, their scales multiplied into P.
+// (Folding these into V as well would round them; applying K's scales to S
+// would have every row read them from shared memory, as it does V's: 256
+// bytes a row and block as bf16, a third of the products' own operands.)
+//   * Four warps turn 4-bit rows into 16-bit tiles in shared memory (128-byte
 //     swizzle), two stages of K and V each, one block ahead in registers.  A
-//     word's 8 numbers come out as the pairs (0,4) (1,5) (2,6) (3,7), so
-//     dimensions are kept in that order within groups of 8: queries and the
-//     new tokens' rows are put in it, the output taken out of it.
+//     number c + 8 placed in bits 6..9 of a half is 16 + (c + 8) in fp16; one
+//     packed fma with (s, -24 s), exact, makes it c s.  In bits 0..3 it is 128
+//     + (c + 8) in bf16, and one subtraction makes it c.  A word's 8 numbers come out
+//     as the pairs (0,4) (1,5) (2,6) (3,7), so dimensions are kept in that
+//     order within groups of 8: queries and the new tokens' rows are put in
+//     it, the output taken out of it.  (Scales applied to S and P instead
+//     would be read from shared memory by every row: 1 KB a row and block,
+//     more than the products' own operands.)
 //   * One warp issues every tcgen05.mma (accumulators and P in tensor memory).
 //   * Two softmax warpgroups, a row a thread.  With more than 128 rows each has
 //     its tile and both take every block; with fewer both have the same rows,
@@ -34,26 +44,41 @@ FC_DEFINE_ERROR_WORD(kv4_tc)
 namespace {
 
 constexpr int HD = KV4_D;
-constexpr int THREADS = 512;  // warp 0 products, 1-3 queries, 4-7 / 8-11 softmax, 12-15 numbers to bf16
+constexpr int THREADS = 512;  // warp 0 products, 1-3 queries, 4-7 / 8-11 softmax, 12-15 numbers to tiles
 constexpr int BM = 128, BN = 128, ROWS = 2 * BM;
 constexpr uint32_t HALF_BYTES = 128 * 128;         // 64 dims of 128 rows
 constexpr uint32_t TILE_BYTES = 2 * HALF_BYTES;
 constexpr uint32_t OFF_Q = 0;                      // two tiles
 constexpr uint32_t OFF_K = OFF_Q + 2 * TILE_BYTES; // two stages
 constexpr uint32_t OFF_V = OFF_K + 2 * TILE_BYTES;
-constexpr int SC_SLOTS = 4;
-constexpr uint32_t OFF_KS = OFF_V + 2 * TILE_BYTES;             // [slot][128] key scales (times the softmax's)
-constexpr uint32_t OFF_VS = OFF_KS + SC_SLOTS * BN * 4;         // [slot][128] value scales
-constexpr uint32_t OFF_KEEP = OFF_VS + SC_SLOTS * BN * 4;       // [slot][4] bits of the keys that count
-constexpr uint32_t OFF_ML = OFF_KEEP + SC_SLOTS * 16;           // [2 turns][2][128] (m, l) exchanged at a unit's end
-constexpr uint32_t OFF_BAR = OFF_ML + 4 * BM * 8;
+constexpr int SLOTS = 4;                                        // blocks whose exponents and keep bits are kept
+constexpr uint32_t OFF_KEEP = OFF_V + 2 * TILE_BYTES;           // [slot][4] bits of the keys that count
+constexpr uint32_t OFF_VS = OFF_KEEP + SLOTS * 16;              // [slot][128] value scales, bf16
+constexpr uint32_t OFF_EXP = OFF_VS + SLOTS * BN * 2;           // [slot] exponent of K
+constexpr uint32_t OFF_TOP = OFF_EXP + SLOTS * 4;               // [2][4 warps] largest key scales of a block
+constexpr uint32_t OFF_QE = OFF_TOP + 2 * 16;                   // [2 pieces][256] exponents of the query rows
+constexpr uint32_t OFF_ML = OFF_QE + 2 * ROWS * 4;              // [2 turns][2][128] (m, l) exchanged at a unit's end
+constexpr int PIECES = 4;                                       // piece descriptions kept
+constexpr uint32_t OFF_PIECE = OFF_ML + 4 * BM * 8;             // [PIECES]
+constexpr uint32_t OFF_BAR = OFF_PIECE + PIECES * 64;
 constexpr uint32_t SMEM_BYTES = OFF_BAR + 256 + 1024;           // + alignment slack
 constexpr uint32_t TMEM_COLS = 512;                             // S_0, S_1, O_0, O_1
 constexpr uint64_t WAIT_CYCLES = 4000000000ull;                 // ~2 s
 constexpr uint64_t DRAIN_CYCLES = 400000000ull;
 constexpr float RESCALE_THRESHOLD = 8.f;  // O is rescaled when a row's maximum (base 2) grows by more
+constexpr int E_TOP = 9;  // a query row's largest value, a K block's largest scale (or new value), is put at 2^9..2^10
+constexpr float M_START = -1e30f;  // a reference before any key
+// Exponents below count as this, so that the product of two is no fp32
+// underflow; such scores are 0 to fp32 all the same.
+constexpr int E_MIN = -50;
 // A unit's start and end in blocks of one tile, and the least share worth a CTA.
 constexpr int UNIT_COST = 8, LEAST = 12;
+
+// Registers a thread by warpgroup (setmaxnreg), of the launch's 128: a softmax
+// thread holds a row's 128 scores.  The shares must add up to the launch's
+// allocation, or the increase never returns; the host checks the compiled count.
+constexpr int REGS_LAUNCH = 128, REGS_ISSUE = 56, REGS_NUMBERS = 88, REGS_SOFTMAX = 184;
+static_assert(REGS_ISSUE + REGS_NUMBERS + 2 * REGS_SOFTMAX <= 4 * REGS_LAUNCH, "register split");
 
 enum {
   B_KFULL = 0,   // [2] 128 arrivals
@@ -62,14 +87,17 @@ enum {
   B_VEMPTY = 6,  // [2]
   B_SFULL = 8,   // [2 tiles]
   B_PFULL = 10,  // [2 tiles] 128
-  B_SCALES = 12, // [4 slots] 128
-  B_QFULL = 16,  // 96
+  B_INFO = 12,   // [4 slots] 4: a block's exponents and keep bits
+  B_QFULL = 16,  // 65
   B_QFREE = 17,
   B_OFIN = 18,
   B_OFREE = 19,  // 256
   B_ML = 20,     // 256: a row's halves exchanged
-  B_DRAIN = 21,
-  N_BARS = 22
+  B_PIECE = 21,  // [PIECES] a description is written
+  B_TOP = 25,    // [2] 4: largest scales of a block to come
+  B_QE = 27,     // [2] 64: the query rows' exponents
+  B_DRAIN = 29,
+  N_BARS = 30
 };
 
 struct ManyArgs {
@@ -118,13 +146,59 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
   asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
   return d;
 }
+__device__ __forceinline__ void tmem_ld16(uint32_t taddr, uint32_t (&r)[16]) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
+        "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+      : "r"(taddr));
+}
+template <int N>
+__device__ __forceinline__ void regs_dec() {
+  asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N));
+}
+template <int N>
+__device__ __forceinline__ void regs_inc() {
+  asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N));
+}
 // 16 bytes of bf16 in dimension order to the tiles' order
 __device__ __forceinline__ uint4 permute8(const uint4& v) {
   return make_uint4(__byte_perm(v.x, v.z, 0x5410), __byte_perm(v.x, v.z, 0x7632), __byte_perm(v.y, v.w, 0x5410),
                     __byte_perm(v.y, v.w, 0x7632));
 }
-// 8 numbers (one word) to 8 bf16 values in the tiles' order: 0x4300 | c is 128 + c
-__device__ __forceinline__ uint4 to_bf16(uint32_t w) {
+__device__ __forceinline__ float pow2i(int e) { return __uint_as_float((uint32_t)(e + 127) << 23); }  // -126 <= e <= 127
+__device__ __forceinline__ float lo_f(uint32_t w) { return __uint_as_float(w << 16); }
+__device__ __forceinline__ float hi_f(uint32_t w) { return __uint_as_float(w & 0xFFFF0000u); }
+__device__ __forceinline__ uint32_t pack_f16x2(float lo, float hi) {
+  uint32_t r;
+  asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+  return r;
+}
+// Largest finite magnitude of a word's two bf16 values, packed like them.
+__device__ __forceinline__ uint32_t top2(uint32_t top, uint32_t w) {
+  const uint32_t mag = w & 0x7FFF7FFFu;
+  return __vmaxu2(top, mag & ~__vcmpgeu2(mag, 0x7F807F80u));
+}
+// Exponent of a magnitude given as bf16 bits, in E_MIN..100.
+__device__ __forceinline__ int expo_of(uint32_t bits) { return min(max((int)(bits >> 7) - 127, E_MIN), 100); }
+// 16 bytes of bf16 in the tiles' order times a power of two, as fp16
+__device__ __forceinline__ uint4 to_f16(const uint4& v, float by) {
+  auto two = [&](uint32_t w) { return pack_f16x2(lo_f(w) * by, hi_f(w) * by); };
+  return make_uint4(two(v.x), two(v.y), two(v.z), two(v.w));
+}
+// 8 numbers (one word) times a scale, as fp16 in the tiles' order: 0x4C00 |
+// (c << 6) is 16 + c; less24 is -24 times the scale
+__device__ __forceinline__ uint4 scaled(uint32_t w, uint32_t s2, uint32_t less24) {
+  auto two = [&](uint32_t v) {
+    uint32_t r;
+    asm("fma.rn.f16x2 %0, %1, %2, %3;" : "=r"(r) : "r"((v & 0x03C003C0u) | 0x4C004C00u), "r"(s2), "r"(less24));
+    return r;
+  };
+  return make_uint4(two(w << 6), two(w << 2), two(w >> 2), two(w >> 6));
+}
+
+// 8 numbers as bf16 in the tiles' order: 0x4300 | c is 128 + c
+__device__ __forceinline__ uint4 numbers(uint32_t w) {
   auto two = [](uint32_t v) {
     uint32_t r;
     asm("sub.rn.bf16x2 %0, %1, %2;" : "=r"(r) : "r"((v & 0x000F000Fu) | 0x43004300u), "r"(0x43084308u));
@@ -133,7 +207,17 @@ __device__ __forceinline__ uint4 to_bf16(uint32_t w) {
   return make_uint4(two(w), two(w >> 4), two(w >> 8), two(w >> 12));
 }
 
-// The units' blocks dealt out, walked alike by every role of a CTA.
+// A CTA's part of a unit: n blocks from s0 on (n = 0: there is no more).
+struct Piece {
+  int b, gh, row0, rows, nn, kvl, cached, s0, n;
+  int two;    // the softmax warpgroups have different rows
+  int whole;  // all of the unit's blocks
+  int slot;   // else where its sums go
+};
+static_assert(sizeof(Piece) <= 64, "piece description");
+
+// The units' blocks dealt out.  One warp of a CTA walks them and leaves each
+// piece's description in shared memory for the other roles.
 struct Walk {
   const ManyArgs& f;
   Kv4Cut cut;
@@ -165,7 +249,7 @@ struct Walk {
   __device__ __forceinline__ int unit_cost(const Req& r) const { return UNIT_COST + r.blocks * r.w; }
 
   // every lane of a warp calls this
-  __device__ __noinline__ Walk(const ManyArgs& args) : f(args), cut(1, 1, 1) {
+  __device__ __forceinline__ Walk(const ManyArgs& args) : f(args), cut(1, 1, 1) {
     const Kv4Args& a = f.a;
     const int lane = threadIdx.x & 31;
     b = 0;
@@ -209,7 +293,7 @@ struct Walk {
   }
 
   // the next piece of this CTA; false when there is none
-  __device__ __noinline__ bool next() {
+  __device__ __forceinline__ bool next() {
     const Kv4Args& a = f.a;
     for (;;) {
       if (cur >= end) return false;
@@ -274,8 +358,10 @@ __global__ void __launch_bounds__(THREADS, 1) k_kv4_attn_many(ManyArgs f) {
     s_abort = 0;
     for (int i = 0; i < N_BARS; ++i) {
       uint32_t n = 1;
-      if (i < B_KEMPTY || i == B_PFULL || i == B_PFULL + 1 || (i >= B_SCALES && i < B_SCALES + SC_SLOTS)) n = 128;
-      if (i == B_QFULL) n = 96;
+      if (i < B_KEMPTY || i == B_PFULL || i == B_PFULL + 1) n = 128;
+      if ((i >= B_INFO && i < B_INFO + SLOTS) || i == B_TOP || i == B_TOP + 1) n = 4;
+      if (i == B_QE || i == B_QE + 1) n = 64;
+      if (i == B_QFULL) n = 65;
       if (i == B_OFREE || i == B_ML) n = 256;
       mbar_init(bar(i), n);
     }
@@ -289,11 +375,16 @@ __global__ void __launch_bounds__(THREADS, 1) k_kv4_attn_many(ManyArgs f) {
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = s_tmem;
-  Walk wk(f);
+  if (warp < 4) regs_dec<REGS_ISSUE>();
+  else if (warp >= 12) regs_dec<REGS_NUMBERS>();
+  else regs_inc<REGS_SOFTMAX>();
+  auto piece = [&](uint32_t i) { return reinterpret_cast<const Piece*>(smem + OFF_PIECE) + i % PIECES; };
 
   if (warp == 0) {
     // ---------------- products ----------------
-    constexpr uint32_t IDESC_QK = idesc_bf16_f32(BM, BN, 0), IDESC_PV = idesc_bf16_f32(BM, HD, 1);
+    // fp16 operands: format 0 where bf16 is 1 (bits 7..9, 10..12)
+    constexpr uint32_t BF16 = (1u << 7) | (1u << 10);
+    constexpr uint32_t IDESC_QK = idesc_bf16_f32(BM, BN, 0) & ~BF16, IDESC_PV = idesc_bf16_f32(BM, HD, 1);
     uint32_t nb = 0, np = 0, t_of[2] = {0, 0};  // blocks, pieces, steps of each tile so far
     bool ok = true;
     auto qk = [&](uint32_t blk, int x, int qx) {  // S_x <- Q_qx . K(blk)^T
@@ -318,11 +409,14 @@ __global__ void __launch_bounds__(THREADS, 1) k_kv4_attn_many(ManyArgs f) {
       tc_fence_after();
       return ok;
     };
-    while (ok && wk.next()) {
-      const int n = wk.s1 - wk.s0;
+    for (;;) {
+      if (!wait(B_PIECE + np % PIECES, np / PIECES)) break;
+      const Piece* pc = piece(np);
+      const int n = pc->n;
+      if (n == 0) break;
       const uint32_t b0 = nb;
       if (!wait(B_QFULL, np)) break;
-      if (wk.two) {
+      if (pc->two) {
         if (!wait(B_KFULL + (b0 & 1), b0 >> 1)) break;
         qk(b0, 0, 0);
         qk(b0, 1, 1);
@@ -385,151 +479,248 @@ __global__ void __launch_bounds__(THREADS, 1) k_kv4_attn_many(ManyArgs f) {
     // ---------------- queries, padding rows, the list of cut units ----------------
     const int qt = tid - 32;  // 0..95
     uint32_t np = 0;
-    if (f.split && qt == 0) f.list[8 * blockIdx.x] = -1;
-    while (wk.next()) {
-      if (np > 0 && !warp_wait(bar(B_QFREE), (np - 1) & 1, &s_abort)) break;
-      const int lim = wk.two ? 2 * BM * 16 : BM * 16;
-#pragma unroll 4
-      for (int e = qt; e < lim; e += 96) {
-        const int r = e >> 4, ch = e & 15;
-        // rows [0, 128) are tile 0, the others tile 1
-        uint4 v = make_uint4(0, 0, 0, 0);
-        if (r < wk.rows) {
-          const int rr = wk.row0 + r, i = rr / a.G, hh = rr - i * a.G;
-          v = permute8(reinterpret_cast<const uint4*>(
-              a.q + (((size_t)wk.b * a.n_pad + i) * a.H + wk.gh * a.G + hh) * HD)[ch]);
+    if (warp == 1) {
+      Walk wk(f);
+      if (f.split && lane == 0) f.list[8 * blockIdx.x] = -1;
+      // Description i is written once the queries of piece i - 2 have been
+      // used: by then every role is done with piece i - 4, whose place it
+      // takes.  Piece i - 1 starts only after this warp has seen that.
+      for (;; ++np) {
+        if (np >= 2 && !warp_wait(bar(B_QFREE), (np - 2) & 1, &s_abort)) break;
+        if (np >= 1 && lane == 0) mbar_arrive(bar(B_QFULL));
+        const bool any = wk.next();
+        if (lane == 0) {
+          Piece* p = reinterpret_cast<Piece*>(smem + OFF_PIECE) + np % PIECES;
+          p->n = 0;
+          if (any) {
+            p->b = wk.b, p->gh = wk.gh, p->row0 = wk.row0, p->rows = wk.rows, p->nn = wk.nn, p->kvl = wk.kvl;
+            p->cached = wk.cached, p->s0 = wk.s0, p->n = wk.s1 - wk.s0, p->two = wk.two;
+            p->whole = !f.split || wk.whole();
+            p->slot = p->whole ? 0 : wk.slot(blockIdx.x);
+            if (wk.bad && wk.gh == 0 && wk.s0 == 0 && wk.chunk == 0) fc_flag(FC_ERR_WORD(a.err), FC_EBIT_INVALID);
+            if (f.split && wk.s0 > 0 && wk.first_cta() + 1 == (int)blockIdx.x) {  // one entry a cut unit
+              const int c0 = blockIdx.x - 1;
+              int* e = f.list + 8 * blockIdx.x;
+              e[1] = wk.gh, e[2] = wk.row0, e[3] = wk.rows, e[4] = c0, e[5] = wk.last_cta() - c0 + 1;
+              e[6] = wk.slot(c0);
+              e[0] = wk.b;
+            }
+          }
+          mbar_arrive(bar(B_PIECE + np % PIECES));
         }
-        *reinterpret_cast<uint4*>(smem + OFF_Q + (r >> 7) * TILE_BYTES + (ch >> 3) * HALF_BYTES + (r & 127) * 128 +
-                                  (((ch & 7) ^ (r & 7)) << 4)) = v;
+        if (!any) break;
       }
-      fence_proxy_async_smem();
-      mbar_arrive(bar(B_QFULL));
-      if (wk.s0 == 0 && wk.chunk == 0) {
-        if (wk.bad && wk.gh == 0 && qt == 0) fc_flag(FC_ERR_WORD(a.err), FC_EBIT_INVALID);
-        const int pad = (a.n_pad - wk.nn) * a.G;
-        for (int e = qt; e < pad * (HD / 8); e += 96) {
-          const int r = e / (HD / 8), ch = e % (HD / 8), i = wk.nn + r / a.G, hh = r % a.G;
-          reinterpret_cast<uint4*>(a.out + (((size_t)wk.b * a.n_pad + i) * a.H + wk.gh * a.G + hh) * HD)[ch] =
-              make_uint4(0, 0, 0, 0);
+    } else {
+      const int st = qt - 32;  // 0..63
+      for (;; ++np) {
+        if (!warp_wait(bar(B_PIECE + np % PIECES), (np / PIECES) & 1, &s_abort)) break;
+        const Piece pc = *piece(np);
+        if (pc.n == 0) break;
+        if (np > 0 && !warp_wait(bar(B_QFREE), (np - 1) & 1, &s_abort)) break;
+        const int lim = (pc.two ? 2 : 1) * BM * 16;
+        int* qe = reinterpret_cast<int*>(smem + OFF_QE) + (np & 1) * ROWS;
+#pragma unroll 1
+        for (int e0 = st; e0 < lim; e0 += 64 * 8) {  // 16 lanes a row
+          uint4 v[8];
+#pragma unroll
+          for (int k = 0; k < 8; ++k) {
+            const int e = e0 + 64 * k, r = e >> 4, ch = e & 15;  // rows [0, 128) are tile 0, the others tile 1
+            v[k] = make_uint4(0, 0, 0, 0);
+            if (r < pc.rows) {
+              const int rr = pc.row0 + r, i = rr / a.G, hh = rr - i * a.G;
+              v[k] = reinterpret_cast<const uint4*>(a.q + (((size_t)pc.b * a.n_pad + i) * a.H + pc.gh * a.G + hh) * HD)[ch];
+            }
+          }
+#pragma unroll
+          for (int k = 0; k < 8; ++k) {
+            const int e = e0 + 64 * k, r = e >> 4, ch = e & 15;
+            uint32_t top = top2(top2(top2(top2(0u, v[k].x), v[k].y), v[k].z), v[k].w);
+#pragma unroll
+            for (int o = 1; o < 16; o <<= 1) top = __vmaxu2(top, __shfl_xor_sync(0xFFFFFFFFu, top, o));
+            const int ex = expo_of(max(top & 0xFFFFu, top >> 16));
+            if (ch == 0) qe[r] = ex;
+            *reinterpret_cast<uint4*>(smem + OFF_Q + (r >> 7) * TILE_BYTES + (ch >> 3) * HALF_BYTES + (r & 127) * 128 +
+                                      (((ch & 7) ^ (r & 7)) << 4)) = to_f16(permute8(v[k]), pow2i(E_TOP - ex));
+          }
+        }
+        mbar_arrive(bar(B_QE + (np & 1)));
+        fence_proxy_async_smem();
+        mbar_arrive(bar(B_QFULL));
+        if (pc.s0 == 0 && pc.row0 == 0) {  // the rows past the nodes
+          const int pad = (a.n_pad - pc.nn) * a.G;
+#pragma unroll 1
+          for (int e = st; e < pad * (HD / 8); e += 64) {
+            const int r = e / (HD / 8), ch = e % (HD / 8), i = pc.nn + r / a.G, hh = r % a.G;
+            reinterpret_cast<uint4*>(a.out + (((size_t)pc.b * a.n_pad + i) * a.H + pc.gh * a.G + hh) * HD)[ch] =
+                make_uint4(0, 0, 0, 0);
+          }
         }
       }
-      if (f.split && wk.s0 > 0 && qt == 0 && wk.first_cta() + 1 == (int)blockIdx.x) {  // one entry a cut unit
-        const int c0 = blockIdx.x - 1;
-        int* e = f.list + 8 * blockIdx.x;
-        e[1] = wk.gh, e[2] = wk.row0, e[3] = wk.rows, e[4] = c0, e[5] = wk.last_cta() - c0 + 1, e[6] = wk.slot(c0);
-        e[0] = wk.b;
-      }
-      ++np;
     }
   } else if (warp >= 12) {
-    // ---------------- numbers to bf16 tiles ----------------
+    // ---------------- numbers to tiles ----------------
     const int r = tid - 384, w = warp - 12, c = lane & 3, rho = lane >> 2;
     // 32-row pass p: row 32p + 8w + rho, 16 bytes c of its 64; the lanes of the
     // two 64-dim halves take their words two apart, so that eight lanes' stores
     // fall in different banks
     const int swap = c >> 1;
+    Piece pc;
     uint32_t dst[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i)
       dst[i] = swap * HALF_BYTES + (8 * w + rho) * 128 + ((((c & 1) * 4 + (i ^ (2 * swap))) ^ rho) << 4);
     uint4 kr[4], vr[4];
-    uint32_t rowi[4];  // the block's run of 8 rows of each pass, in units of 8 rows
-    float ksc = 0.f, vsc = 0.f;
-    bool live = false;
+    int ids[4];            // pages of the passes' rows in the next block to fetch (-1: none)
+    uint32_t runs[4];      // 8-row runs of the block being fetched
+    uint32_t sc[4];        // its scales: K in the low half, V in the high
+    uint32_t live = 0;     // bit p: the pass's rows are in the pool
     uint32_t nb = 0;
     bool ok = true;
-    const uint32_t per_page = (uint32_t)a.Hkv << (a.shift - 3);
-    auto find = [&](int blk) {  // page ids and scales of cached block blk
-      const int32_t* tab = a.table + (size_t)wk.b * a.max_pages;
-      const uint32_t head = (uint32_t)wk.gh << (a.shift - 3), in_page = (1u << (a.shift - 3)) - 1u;
+    const uint32_t per_page = (uint32_t)a.Hkv << (a.shift - 3), in_page = (1u << (a.shift - 3)) - 1u;
+    auto look_up = [&](int blk) {
+      const int32_t* tab = a.table + (size_t)pc.b * a.max_pages;
 #pragma unroll
       for (int p = 0; p < 4; ++p) {
         const long long key = (long long)blk * BN + 32 * p + 8 * w;
-        int id = key < wk.kvl ? tab[key >> a.shift] : -1;
-        rowi[p] = (unsigned)id < (unsigned)a.n_pages
-                      ? id * per_page + head + ((uint32_t)(key >> 3) & in_page)
-                      : 0xFFFFFFFFu;
-      }
-      const long long key = (long long)blk * BN + r;
-      live = false;
-      ksc = vsc = 0.f;
-      if (key < wk.kvl) {
-        const int id = tab[key >> a.shift];
-        live = (unsigned)id < (unsigned)a.n_pages;
-        if (live) {
-          const size_t at = (((size_t)id * a.Hkv + wk.gh) << a.shift) + (key & ((1 << a.shift) - 1));
-          ksc = __bfloat162float(a.ks[at]) * a.scale_log2;
-          vsc = __bfloat162float(a.vs[at]);
-        } else {
-          fc_flag(FC_ERR_WORD(a.err), FC_EBIT_INVALID);
-        }
+        ids[p] = key < pc.kvl ? tab[key >> a.shift] : -1;
       }
     };
-    auto load = [&](const uint8_t* codes, uint4 (&x)[4]) {
+    auto fetch_k = [&](int blk) {  // K rows and both scales, of the pages looked up before
+      live = 0;
+#pragma unroll
+      for (int p = 0; p < 4; ++p) {
+        const uint32_t key8 = (uint32_t)blk * (BN / 8) + 4 * p + w;
+        const bool in = (unsigned)ids[p] < (unsigned)a.n_pages;
+        if (!in && (long long)key8 * 8 < pc.kvl && lane == 0) fc_flag(FC_ERR_WORD(a.err), FC_EBIT_INVALID);
+        live |= (in ? 1u : 0u) << p;
+        runs[p] = in ? ids[p] * per_page + ((uint32_t)pc.gh << (a.shift - 3)) + (key8 & in_page) : 0u;
+        kr[p] = *reinterpret_cast<const uint4*>(a.kc + (uint64_t)runs[p] * 512u + lane * 16);
+        const uint64_t row = (uint64_t)runs[p] * 8u + rho;
+        sc[p] = reinterpret_cast<const uint16_t*>(a.ks)[row] |
+                ((uint32_t)reinterpret_cast<const uint16_t*>(a.vs)[row] << 16);
+      }
+    };
+    auto fetch_v = [&]() {
 #pragma unroll
       for (int p = 0; p < 4; ++p)
-        x[p] = rowi[p] != 0xFFFFFFFFu
-                   ? *reinterpret_cast<const uint4*>(codes + (uint64_t)rowi[p] * 512u + lane * 16)
-                   : make_uint4(0x88888888u, 0x88888888u, 0x88888888u, 0x88888888u);
+        vr[p] = *reinterpret_cast<const uint4*>(a.vc + (uint64_t)runs[p] * 512u + lane * 16);
     };
-    auto store = [&](uint32_t tile, const uint4 (&x)[4]) {
+    const size_t no_row = ~(size_t)0;
+    auto new_row = [&](int j) {
+      return a.k_new && j < pc.nn ? (((size_t)pc.b * a.Hkv + pc.gh) * a.n_pad + j) * HD : no_row;
+    };
+    // The largest key scale (magnitude, for the new tokens) of this warp's rows of block blk.
+    auto announce = [&](int blk) {
+      uint32_t top = 0;
+      if (blk < pc.cached) {
+#pragma unroll
+        for (int p = 0; p < 4; ++p) {
+          const long long key = (long long)blk * BN + 32 * p + 8 * w + rho;
+          if (!((live >> p) & 1u) || key >= pc.kvl) sc[p] = 0;  // a key that does not count: whatever stands there
+          top = top2(top, sc[p] & 0xFFFFu);
+        }
+      } else {
+        uint32_t tk = 0;
+#pragma unroll 4
+        for (int e = r; e < BN * 16; e += 128) {
+          const size_t row = new_row(e >> 4);
+          if (row == no_row) break;
+          const uint4 k = reinterpret_cast<const uint4*>(a.k_new + row)[e & 15];
+          tk = top2(top2(top2(top2(tk, k.x), k.y), k.z), k.w);
+        }
+        top = max(tk & 0xFFFFu, tk >> 16);
+      }
+      return __reduce_max_sync(0xFFFFFFFFu, top);
+    };
+    auto store = [&](uint32_t tile, const uint4 (&x)[4], auto&& convert) {
 #pragma unroll
       for (int p = 0; p < 4; ++p) {
         const uint32_t w0 = swap ? x[p].z : x[p].x, w1 = swap ? x[p].w : x[p].y;
         const uint32_t w2 = swap ? x[p].x : x[p].z, w3 = swap ? x[p].y : x[p].w;
         unsigned char* t = smem + tile + p * 4096;
-        *reinterpret_cast<uint4*>(t + dst[0]) = to_bf16(w0);
-        *reinterpret_cast<uint4*>(t + dst[1]) = to_bf16(w1);
-        *reinterpret_cast<uint4*>(t + dst[2]) = to_bf16(w2);
-        *reinterpret_cast<uint4*>(t + dst[3]) = to_bf16(w3);
+        *reinterpret_cast<uint4*>(t + dst[0]) = convert(p, w0);
+        *reinterpret_cast<uint4*>(t + dst[1]) = convert(p, w1);
+        *reinterpret_cast<uint4*>(t + dst[2]) = convert(p, w2);
+        *reinterpret_cast<uint4*>(t + dst[3]) = convert(p, w3);
       }
     };
-    auto store_new = [&](uint32_t tile, const __nv_bfloat16* src) {  // the new tokens' rows, zeros past them
-      const size_t row = ((size_t)wk.b * a.Hkv + wk.gh) * a.n_pad;
-#pragma unroll 1
+    auto store_new = [&](uint32_t tile, const __nv_bfloat16* src, auto&& convert) {  // the new rows, zeros past them
+#pragma unroll 4
       for (int e = r; e < BN * 16; e += 128) {
         const int j = e >> 4, ch = e & 15;
+        const size_t row = new_row(j);
         uint4 v = make_uint4(0, 0, 0, 0);
-        if (src && j < wk.nn) v = permute8(reinterpret_cast<const uint4*>(src + (row + j) * HD)[ch]);
+        if (row != no_row) v = convert(permute8(reinterpret_cast<const uint4*>(src + row)[ch]));
         *reinterpret_cast<uint4*>(smem + tile + (ch >> 3) * HALF_BYTES + j * 128 + (((ch & 7) ^ (j & 7)) << 4)) = v;
       }
     };
-    while (ok && wk.next()) {
-      if (wk.s0 < wk.cached) {
-        find(wk.s0);
-        load(a.kc, kr);
-        load(a.vc, vr);
+    for (uint32_t np = 0; ok; ++np) {
+      if (!warp_wait(bar(B_PIECE + np % PIECES), (np / PIECES) & 1, &s_abort)) break;
+      pc = *piece(np);
+      if (pc.n == 0) break;
+      const int s1 = pc.s0 + pc.n;
+      if (pc.s0 < pc.cached) {
+        look_up(pc.s0);
+        fetch_k(pc.s0);
+        fetch_v();
+        look_up(pc.s0 + 1);
       }
-      for (int blk = wk.s0; blk < wk.s1; ++blk, ++nb) {
-        const int st = nb & 1, slot = nb & (SC_SLOTS - 1);
-        const bool fresh = blk >= wk.cached, more = blk + 1 < wk.s1 && blk + 1 < wk.cached;
-        // scales: the slot's last readers are done (the V stage of three blocks ago was waited for)
-        if (fresh) {
-          live = a.k_new && r < wk.nn;
-          ksc = a.scale_log2;
-          vsc = 1.f;
+      for (int blk = pc.s0; blk < s1; ++blk, ++nb) {
+        const int st = nb & 1, slot = nb % SLOTS;
+        const bool fresh = blk >= pc.cached;
+        {
+          const uint32_t top = announce(blk);
+          if (lane == 0) {
+            reinterpret_cast<uint32_t*>(smem + OFF_TOP)[st * 4 + w] = top;
+            mbar_arrive(bar(B_TOP + st));
+          }
         }
-        reinterpret_cast<float*>(smem + OFF_KS)[slot * BN + r] = live ? ksc : 0.f;
-        reinterpret_cast<float*>(smem + OFF_VS)[slot * BN + r] = live ? vsc : 0.f;
-        const uint32_t keep = __ballot_sync(0xFFFFFFFFu, live);
-        if (lane == 0) reinterpret_cast<uint32_t*>(smem + OFF_KEEP)[slot * 4 + w] = keep;
+        if (!(ok = warp_wait(bar(B_TOP + st), (nb >> 1) & 1, &s_abort))) break;
+        const uint4 t4 = *reinterpret_cast<const uint4*>(smem + OFF_TOP + st * 16);
+        const int ek = expo_of(max(max(t4.x, t4.y), max(t4.z, t4.w)));
+        // the slot's last readers are done (the V stage of three blocks ago was waited for)
+        if (lane < 4) {  // word p = lane: this warp's 8 keys of it
+          const int left = fresh ? (a.k_new ? pc.nn : 0) - (32 * lane + 8 * w)
+                                 : (int)min((long long)BN, pc.kvl - (long long)blk * BN) - (32 * lane + 8 * w);
+          const uint32_t k8 = left >= 8 ? 0xFFu : (left <= 0 ? 0u : (1u << left) - 1u);
+          smem[OFF_KEEP + slot * 16 + lane * 4 + w] = (unsigned char)(fresh || ((live >> lane) & 1u) ? k8 : 0u);
+        }
+        if (w == 0 && lane == 0) reinterpret_cast<int*>(smem + OFF_EXP)[slot] = ek;
+        uint16_t* vs = reinterpret_cast<uint16_t*>(smem + OFF_VS) + slot * BN;
+        if (fresh) {
+          vs[32 * w + lane] = 0x3F80;
+        } else if (c == 0) {
+#pragma unroll
+          for (int p = 0; p < 4; ++p) vs[32 * p + 8 * w + rho] = (uint16_t)(sc[p] >> 16);
+        }
         __syncwarp();
-        mbar_arrive(bar(B_SCALES + slot));
+        if (lane == 0) mbar_arrive(bar(B_INFO + slot));
         if (nb >= 2 && !(ok = warp_wait(bar(B_KEMPTY + st), ((nb >> 1) - 1) & 1, &s_abort))) break;
-        if (!fresh) store(OFF_K + st * TILE_BYTES, kr);
-        else store_new(OFF_K + st * TILE_BYTES, a.k_new);
+        const float by = pow2i(E_TOP - ek);
+        if (!fresh) {
+          uint32_t s2[4], less24[4];
+#pragma unroll
+          for (int p = 0; p < 4; ++p) {
+            const float s = lo_f(sc[p]) * by;
+            s2[p] = pack_f16x2(s, s);
+            less24[p] = pack_f16x2(-24.f * s, -24.f * s);
+          }
+          store(OFF_K + st * TILE_BYTES, kr, [&](int p, uint32_t v) { return scaled(v, s2[p], less24[p]); });
+        } else {
+          store_new(OFF_K + st * TILE_BYTES, a.k_new, [&](const uint4& v) { return to_f16(v, by); });
+        }
         fence_proxy_async_smem();
         mbar_arrive(bar(B_KFULL + st));
-        if (more) {
-          find(blk + 1);
-          load(a.kc, kr);
-        }
         if (nb >= 2 && !(ok = warp_wait(bar(B_VEMPTY + st), ((nb >> 1) - 1) & 1, &s_abort))) break;
-        if (!fresh) store(OFF_V + st * TILE_BYTES, vr);
-        else store_new(OFF_V + st * TILE_BYTES, a.v_new);
+        if (!fresh) store(OFF_V + st * TILE_BYTES, vr, [](int, uint32_t v) { return numbers(v); });
+        else store_new(OFF_V + st * TILE_BYTES, a.v_new, [](const uint4& v) { return v; });
         fence_proxy_async_smem();
         mbar_arrive(bar(B_VFULL + st));
-        if (more) load(a.vc, vr);
+        if (blk + 1 < s1 && blk + 1 < pc.cached) {
+          fetch_k(blk + 1);
+          fetch_v();
+          look_up(blk + 2);
+        }
       }
     }
   } else {
@@ -539,14 +730,17 @@ __global__ void __launch_bounds__(THREADS, 1) k_kv4_attn_many(ManyArgs f) {
     const uint32_t tS = tmem + x * 128 + lane_off;
     uint32_t nb = 0, np = 0, nx = 0, t = 0;
     bool ok = true;
-    while (ok && wk.next()) {
-      const int n = wk.s1 - wk.s0;
+    for (;;) {
+      if (!(ok = warp_wait(bar(B_PIECE + np % PIECES), (np / PIECES) & 1, &s_abort))) break;
+      const Piece wk = *piece(np);
+      const int n = wk.n;
+      if (n == 0) break;
       const int lr = wk.two ? x * BM + r : r;  // row of the piece
       const bool row_ok = lr < wk.rows;
       const int rr = wk.row0 + lr, i = row_ok ? rr / a.G : 0, hh = row_ok ? rr - i * a.G : 0;
       // the new tokens that this row sees
       uint64_t m0 = 0, m1 = 0;
-      if (wk.s1 > wk.cached && row_ok) {
+      if (wk.s0 + n > wk.cached && row_ok) {
         if (a.mask) {
           const int words = (a.n_pad + 63) / 64;
           const uint64_t* mr = a.mask + ((size_t)wk.b * a.n_pad + i) * words;
@@ -557,94 +751,80 @@ __global__ void __launch_bounds__(THREADS, 1) k_kv4_attn_many(ManyArgs f) {
           m1 = i < 64 ? 0ull : (i >= 127 ? ~0ull : (1ull << (i - 63)) - 1ull);
         }
       }
-      float m = -INFINITY, l = 0.f;
-      bool any = false;  // O_x holds a product
+      float m = M_START, l = 0.f;  // m: the reference
+      bool any = false;            // O_x holds a product
+      if (!(ok = warp_wait(bar(B_QE + (np & 1)), (np >> 1) & 1, &s_abort))) break;
+      // scores: S times 2^(qe - E_TOP) 2^(ek - E_TOP) and the softmax's scale
+      const float c_row = a.scale_log2 * pow2i(reinterpret_cast<const int*>(smem + OFF_QE)[(np & 1) * ROWS + lr] - E_TOP);
       const uint32_t tO = tmem + 256 + x * 128 + lane_off;
       for (int j = wk.two ? 0 : x; j < n; j += wk.two ? 1 : 2, ++t) {
-        const int slot = (nb + j) & (SC_SLOTS - 1);
-        if (!(ok = warp_wait(bar(B_SCALES + slot), ((nb + j) / SC_SLOTS) & 1, &s_abort))) break;
+        const int slot = (nb + j) % SLOTS;
+        if (!(ok = warp_wait(bar(B_INFO + slot), ((nb + j) / SLOTS) & 1, &s_abort))) break;
+        const float cz = c_row * pow2i(reinterpret_cast<const int*>(smem + OFF_EXP)[slot] - E_TOP);
+        const uint4* vs8 = reinterpret_cast<const uint4*>(smem + OFF_VS + slot * BN * 2);
+        const uint4 kp = *reinterpret_cast<const uint4*>(smem + OFF_KEEP + slot * 16);
         if (!(ok = warp_wait(bar(B_SFULL + x), t & 1, &s_abort))) break;
         tc_fence_after();
-        const float4* ks4 = reinterpret_cast<const float4*>(smem + OFF_KS) + slot * (BN / 4);
-        const float4* vs4 = reinterpret_cast<const float4*>(smem + OFF_VS) + slot * (BN / 4);
-        const uint4 kp = *reinterpret_cast<const uint4*>(smem + OFF_KEEP + slot * 16);
+        // the block's 128 scores of this row stay in registers from here on
+        uint32_t sv[BN];
+#pragma unroll
+        for (int c4 = 0; c4 < 4; ++c4) tmem_ld32(tS + c4 * 32, *reinterpret_cast<uint32_t(*)[32]>(&sv[c4 * 32]));
+        tc_wait_ld();
         const bool fresh = wk.s0 + j >= wk.cached;
-        const bool masked = fresh || (kp.x & kp.y & kp.z & kp.w) != 0xFFFFFFFFu;  // alike in the warpgroup
-        auto keep_bits = [&](int c4) {
-          const uint32_t k = reinterpret_cast<const uint32_t*>(smem + OFF_KEEP)[slot * 4 + c4];
-          return fresh ? k & (uint32_t)((c4 < 2 ? m0 : m1) >> (32 * (c4 & 1))) : k;
-        };
-        auto scores = [&](int c4, float (&z)[32]) {  // 32 columns of this row, scaled; masked ones -inf
-          uint32_t s[32];
-          tmem_ld32(tS + c4 * 32, s);
-          tc_wait_ld();
+        if (fresh || (kp.x & kp.y & kp.z & kp.w) != 0xFFFFFFFFu) {  // alike in the warpgroup
+          const uint32_t keep[4] = {fresh ? kp.x & (uint32_t)m0 : kp.x, fresh ? kp.y & (uint32_t)(m0 >> 32) : kp.y,
+                                    fresh ? kp.z & (uint32_t)m1 : kp.z, fresh ? kp.w & (uint32_t)(m1 >> 32) : kp.w};
 #pragma unroll
-          for (int u = 0; u < 8; ++u) {
-            const float4 k = ks4[c4 * 8 + u];
-            f2_unpack(f2_mul(f2_pack(__uint_as_float(s[4 * u]), __uint_as_float(s[4 * u + 1])), f2_pack(k.x, k.y)),
-                      z[4 * u], z[4 * u + 1]);
-            f2_unpack(f2_mul(f2_pack(__uint_as_float(s[4 * u + 2]), __uint_as_float(s[4 * u + 3])), f2_pack(k.z, k.w)),
-                      z[4 * u + 2], z[4 * u + 3]);
-          }
-          if (masked) {
-            const uint32_t keep = keep_bits(c4);
-#pragma unroll
-            for (int u = 0; u < 32; ++u)
-              if (!((keep >> u) & 1u)) z[u] = -INFINITY;
-          }
-        };
-        float top = -INFINITY;
-#pragma unroll 1
-        for (int c4 = 0; c4 < 4; ++c4) {
-          float z[32];
-          scores(c4, z);
-#pragma unroll
-          for (int u = 0; u < 32; u += 2) top = max3(top, z[u], z[u + 1]);
+          for (int u = 0; u < BN; ++u)
+            if (!((keep[u >> 5] >> (u & 31)) & 1u)) sv[u] = __float_as_uint(-INFINITY);
         }
+        float pm[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+        for (int u = 0; u < BN; u += 2)
+          pm[(u >> 1) & 3] = max3(pm[(u >> 1) & 3], __uint_as_float(sv[u]), __uint_as_float(sv[u + 1]));
+        const float top = fmaxf(fmaxf(pm[0], pm[1]), fmaxf(pm[2], pm[3])) * cz;
         const float m_new = top > m + RESCALE_THRESHOLD ? top : m;
-        const float m_use = m_new == -INFINITY ? 0.f : m_new;
-        const float alpha = exp2_fast(m - m_use);
+        const float alpha = exp2_fast(m - m_new);
+        l *= alpha;
         // S_x is the newest product of this tile, so O_x is complete
         if (any && __any_sync(0xFFFFFFFFu, alpha != 1.f)) {
 #pragma unroll 1
-          for (int cc = 0; cc < HD / 32; ++cc) {
-            uint32_t o[32];
-            tmem_ld32(tO + cc * 32, o);
+          for (int cc = 0; cc < HD / 16; ++cc) {
+            uint32_t o[16];
+            tmem_ld16(tO + cc * 16, o);
             tc_wait_ld();
 #pragma unroll
-            for (int u = 0; u < 32; ++u) o[u] = __float_as_uint(__uint_as_float(o[u]) * alpha);
-            tmem_st32(tO + cc * 32, o);
+            for (int u = 0; u < 16; ++u) o[u] = __float_as_uint(__uint_as_float(o[u]) * alpha);
+            tmem_st16(tO + cc * 16, o);
           }
         }
-        uint64_t sum[2] = {0ull, 0ull};
-        const uint64_t neg = f2_pack(-m_use, -m_use);
-#pragma unroll 1
+        uint64_t sum[4] = {0ull, 0ull, 0ull, 0ull};
+        const uint64_t c2 = f2_pack(cz, cz), neg = f2_pack(-m_new, -m_new);
+#pragma unroll
         for (int c4 = 0; c4 < 4; ++c4) {
-          float z[32];
-          scores(c4, z);
           uint32_t pk[16];
 #pragma unroll
-          for (int u = 0; u < 8; ++u) {
-            const float4 v = vs4[c4 * 8 + u];
-            float p0, p1, p2, p3;
-            f2_unpack(f2_add(f2_pack(z[4 * u], z[4 * u + 1]), neg), p0, p1);
-            f2_unpack(f2_add(f2_pack(z[4 * u + 2], z[4 * u + 3]), neg), p2, p3);
-            p0 = exp2_fast(p0), p1 = exp2_fast(p1), p2 = exp2_fast(p2), p3 = exp2_fast(p3);
-            const uint64_t a0 = f2_pack(p0, p1), a1 = f2_pack(p2, p3);
-            sum[0] = f2_add(sum[0], a0);
-            sum[1] = f2_add(sum[1], a1);
-            f2_unpack(f2_mul(a0, f2_pack(v.x, v.y)), p0, p1);
-            f2_unpack(f2_mul(a1, f2_pack(v.z, v.w)), p2, p3);
-            pk[2 * u] = pack_bf16x2(p0, p1);
-            pk[2 * u + 1] = pack_bf16x2(p2, p3);
+          for (int g = 0; g < 4; ++g) {  // 8 keys, their value scales in one load
+            const uint4 v4 = vs8[c4 * 4 + g];
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+              const int k = c4 * 32 + 8 * g + 2 * u;
+              const uint32_t v = (&v4.x)[u];
+              float p0, p1;
+              f2_unpack(f2_fma(f2_pack(__uint_as_float(sv[k]), __uint_as_float(sv[k + 1])), c2, neg), p0, p1);
+              const uint64_t pp = f2_pack(exp2_fast(p0), exp2_fast(p1));
+              sum[u] = f2_add(sum[u], pp);
+              f2_unpack(f2_mul(pp, f2_pack(lo_f(v), hi_f(v))), p0, p1);
+              pk[4 * g + u] = pack_bf16x2(p0, p1);
+            }
           }
-          tmem_st16(tS + c4 * 16, pk);  // over columns already read
+          tmem_st16(tS + c4 * 16, pk);  // over scores already read
         }
         tc_wait_st();
         float s0, s1, s2, s3;
-        f2_unpack(sum[0], s0, s1);
-        f2_unpack(sum[1], s2, s3);
-        l = l * alpha + ((s0 + s1) + (s2 + s3));
+        f2_unpack(f2_add(sum[0], sum[1]), s0, s1);
+        f2_unpack(f2_add(sum[2], sum[3]), s2, s3);
+        l += (s0 + s1) + (s2 + s3);
         m = m_new;
         any = true;
         tc_fence_before();
@@ -653,8 +833,8 @@ __global__ void __launch_bounds__(THREADS, 1) k_kv4_attn_many(ManyArgs f) {
       if (!ok || !(ok = warp_wait(bar(B_OFIN), np & 1, &s_abort))) break;
       tc_fence_after();
       // ---- the piece's rows: this tile's, or half the dimensions of both halves' sum
-      const bool whole = wk.whole() || !f.split;
-      const size_t slot = whole ? 0 : (size_t)wk.slot(blockIdx.x) * f.rows_cap;
+      const bool whole = wk.whole;
+      const size_t slot = (size_t)wk.slot * f.rows_cap;
       __nv_bfloat16* dst = a.out + (((size_t)wk.b * a.n_pad + i) * a.H + wk.gh * a.G + hh) * HD;
       float m_all = m, k0 = 1.f, k1 = 0.f;
       bool have0 = any, have1 = false;
@@ -669,8 +849,7 @@ __global__ void __launch_bounds__(THREADS, 1) k_kv4_attn_many(ManyArgs f) {
         ++nx;
         const float2 other = ml[(1 - x) * BM + r];
         m_all = fmaxf(m, other.x);
-        const float mu = m_all == -INFINITY ? 0.f : m_all;
-        const float mine = exp2_fast(m - mu), theirs = exp2_fast(other.x - mu);
+        const float mine = exp2_fast(m - m_all), theirs = exp2_fast(other.x - m_all);
         l = l * mine + other.y * theirs;
         k0 = x == 0 ? mine : theirs;
         k1 = x == 0 ? theirs : mine;
@@ -683,27 +862,27 @@ __global__ void __launch_bounds__(THREADS, 1) k_kv4_attn_many(ManyArgs f) {
       }
       const float inv = !whole ? 1.f : (l == 0.f ? 0.f : 1.f / l);
 #pragma unroll 1
-      for (int cc = cc0; cc < cc1; ++cc) {
-        uint32_t o[32], o1[32];
-        float v[32];
-        if (have0) tmem_ld32(tO0 + cc * 32, o);
-        if (have1) tmem_ld32(tO1 + cc * 32, o1);
+      for (int cc = 2 * cc0; cc < 2 * cc1; ++cc) {
+        uint32_t o[16], o1[16];
+        float v[16];
+        if (have0) tmem_ld16(tO0 + cc * 16, o);
+        if (have1) tmem_ld16(tO1 + cc * 16, o1);
         tc_wait_ld();
 #pragma unroll
-        for (int u = 0; u < 32; ++u) {
+        for (int u = 0; u < 16; ++u) {
           float y = have0 ? __uint_as_float(o[u]) * k0 : 0.f;
           if (have1) y += __uint_as_float(o1[u]) * k1;
           v[u] = y * inv;
         }
         if (row_ok) {
 #pragma unroll
-          for (int u = 0; u < 32; u += 8) {  // out of the tiles' order: 0 4 1 5 2 6 3 7
+          for (int u = 0; u < 16; u += 8) {  // out of the tiles' order: 0 4 1 5 2 6 3 7
             if (whole) {
-              *reinterpret_cast<uint4*>(dst + cc * 32 + u) =
+              *reinterpret_cast<uint4*>(dst + cc * 16 + u) =
                   make_uint4(pack_bf16x2(v[u], v[u + 2]), pack_bf16x2(v[u + 4], v[u + 6]),
                              pack_bf16x2(v[u + 1], v[u + 3]), pack_bf16x2(v[u + 5], v[u + 7]));
             } else {
-              float4* po = reinterpret_cast<float4*>(f.part_o + (slot + lr) * HD + cc * 32 + u);
+              float4* po = reinterpret_cast<float4*>(f.part_o + (slot + lr) * HD + cc * 16 + u);
               po[0] = make_float4(v[u], v[u + 2], v[u + 4], v[u + 6]);
               po[1] = make_float4(v[u + 1], v[u + 3], v[u + 5], v[u + 7]);
             }
@@ -776,6 +955,9 @@ size_t kv4_attn_many_workspace(int batch, int n_pad, int H, int Hkv) {
 fc_status kv4_attn_many(const Kv4Args& a, void* ws, size_t ws_bytes, cudaStream_t s) {
   static std::atomic<unsigned long long> done{0};
   const fc_status st = fc_once_per_device(done, [](int) {
+    cudaFuncAttributes attr;
+    if (cudaFuncGetAttributes(&attr, k_kv4_attn_many) != cudaSuccess) return FC_ERR_CUDA;
+    if (attr.numRegs != REGS_LAUNCH) return FC_ERR_INTERNAL;  // the register split would not add up
     return fc_cuda_status(cudaFuncSetAttribute(k_kv4_attn_many, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM_BYTES));
   });
   if (st != FC_OK) return st;
