@@ -161,6 +161,61 @@ template <int N>
 __device__ __forceinline__ void regs_inc() {
   asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N));
 }
+// The eight products of a tile and a block (K = 16 each), one lane elected for
+// all of them: descriptors differ in their low words, by constants; their high
+// words are alike (1024 bytes between 8-row groups, version 1, 128-byte
+// swizzle).  One statement, so that the operands move to uniform registers once.
+constexpr uint32_t DESC_HI = (1024u >> 4) | (1u << 14) | (2u << 29);
+// S[tmem d] = A . B^T, both from shared memory, K-major halves of 64 dims
+__device__ __forceinline__ void mma_qk(uint32_t d, uint32_t a_lo, uint32_t b_lo, uint32_t idesc) {
+  asm volatile(
+      "{\n\t.reg .pred z, o, e;\n\t.reg .b64 a, b;\n\t.reg .b32 t, h;\n\tmov.b32 h, %4;\n\t"
+      "setp.ne.b32 z, 0, 0;\n\tsetp.eq.b32 o, 0, 0;\n\telect.sync _|e, 0xffffffff;\n\t"
+      "add.u32 t, %1, 0;\n\tmov.b64 a, {t, h};\n\tadd.u32 t, %2, 0;\n\tmov.b64 b, {t, h};\n\t"
+      "@e tcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %3, z;\n\t"
+      "add.u32 t, %1, 2;\n\tmov.b64 a, {t, h};\n\tadd.u32 t, %2, 2;\n\tmov.b64 b, {t, h};\n\t"
+      "@e tcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %3, o;\n\t"
+      "add.u32 t, %1, 4;\n\tmov.b64 a, {t, h};\n\tadd.u32 t, %2, 4;\n\tmov.b64 b, {t, h};\n\t"
+      "@e tcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %3, o;\n\t"
+      "add.u32 t, %1, 6;\n\tmov.b64 a, {t, h};\n\tadd.u32 t, %2, 6;\n\tmov.b64 b, {t, h};\n\t"
+      "@e tcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %3, o;\n\t"
+      "add.u32 t, %1, 1024;\n\tmov.b64 a, {t, h};\n\tadd.u32 t, %2, 1024;\n\tmov.b64 b, {t, h};\n\t"
+      "@e tcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %3, o;\n\t"
+      "add.u32 t, %1, 1026;\n\tmov.b64 a, {t, h};\n\tadd.u32 t, %2, 1026;\n\tmov.b64 b, {t, h};\n\t"
+      "@e tcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %3, o;\n\t"
+      "add.u32 t, %1, 1028;\n\tmov.b64 a, {t, h};\n\tadd.u32 t, %2, 1028;\n\tmov.b64 b, {t, h};\n\t"
+      "@e tcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %3, o;\n\t"
+      "add.u32 t, %1, 1030;\n\tmov.b64 a, {t, h};\n\tadd.u32 t, %2, 1030;\n\tmov.b64 b, {t, h};\n\t"
+      "@e tcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %3, o;\n\t"
+      "}" ::"r"(d),
+      "r"(a_lo), "r"(b_lo), "r"(idesc), "n"(DESC_HI)
+      : "memory");
+}
+// O[tmem d] (+)= P[tmem a] . V, V's rows (keys) in shared memory
+__device__ __forceinline__ void mma_pv(uint32_t d, uint32_t a_tmem, uint32_t b_lo, uint32_t idesc, uint32_t add) {
+  asm volatile(
+      "{\n\t.reg .pred z, o, e;\n\t.reg .b64 b;\n\t.reg .b32 t, h;\n\tmov.b32 h, %5;\n\t"
+      "setp.ne.b32 z, %4, 0;\n\tsetp.eq.b32 o, 0, 0;\n\telect.sync _|e, 0xffffffff;\n\t"
+      "add.u32 t, %2, 0;\n\tmov.b64 b, {t, h};\n\tadd.u32 t, %1, 0;\n\t"
+      "@e tcgen05.mma.cta_group::1.kind::f16 [%0], [t], b, %3, z;\n\t"
+      "add.u32 t, %2, 128;\n\tmov.b64 b, {t, h};\n\tadd.u32 t, %1, 8;\n\t"
+      "@e tcgen05.mma.cta_group::1.kind::f16 [%0], [t], b, %3, o;\n\t"
+      "add.u32 t, %2, 256;\n\tmov.b64 b, {t, h};\n\tadd.u32 t, %1, 16;\n\t"
+      "@e tcgen05.mma.cta_group::1.kind::f16 [%0], [t], b, %3, o;\n\t"
+      "add.u32 t, %2, 384;\n\tmov.b64 b, {t, h};\n\tadd.u32 t, %1, 24;\n\t"
+      "@e tcgen05.mma.cta_group::1.kind::f16 [%0], [t], b, %3, o;\n\t"
+      "add.u32 t, %2, 512;\n\tmov.b64 b, {t, h};\n\tadd.u32 t, %1, 32;\n\t"
+      "@e tcgen05.mma.cta_group::1.kind::f16 [%0], [t], b, %3, o;\n\t"
+      "add.u32 t, %2, 640;\n\tmov.b64 b, {t, h};\n\tadd.u32 t, %1, 40;\n\t"
+      "@e tcgen05.mma.cta_group::1.kind::f16 [%0], [t], b, %3, o;\n\t"
+      "add.u32 t, %2, 768;\n\tmov.b64 b, {t, h};\n\tadd.u32 t, %1, 48;\n\t"
+      "@e tcgen05.mma.cta_group::1.kind::f16 [%0], [t], b, %3, o;\n\t"
+      "add.u32 t, %2, 896;\n\tmov.b64 b, {t, h};\n\tadd.u32 t, %1, 56;\n\t"
+      "@e tcgen05.mma.cta_group::1.kind::f16 [%0], [t], b, %3, o;\n\t"
+      "}" ::"r"(d),
+      "r"(a_tmem), "r"(b_lo), "r"(idesc), "r"(add), "n"(DESC_HI)
+      : "memory");
+}
 // 16 bytes of bf16 in dimension order to the tiles' order
 __device__ __forceinline__ uint4 permute8(const uint4& v) {
   return make_uint4(__byte_perm(v.x, v.z, 0x5410), __byte_perm(v.x, v.z, 0x7632), __byte_perm(v.y, v.w, 0x5410),
@@ -387,22 +442,15 @@ __global__ void __launch_bounds__(THREADS, 1) k_kv4_attn_many(ManyArgs f) {
     constexpr uint32_t IDESC_QK = idesc_bf16_f32(BM, BN, 0) & ~BF16, IDESC_PV = idesc_bf16_f32(BM, HD, 1);
     uint32_t nb = 0, np = 0, t_of[2] = {0, 0};  // blocks, pieces, steps of each tile so far
     bool ok = true;
+    // descriptors' low words: a byte offset adds to them in units of 16
+    const uint32_t q_lo = (uint32_t)smem_desc_sw128(sQ, 16, 1024), k_lo = (uint32_t)smem_desc_sw128(sK, 16, 1024);
+    const uint32_t v_lo = (uint32_t)smem_desc_sw128(sV, HALF_BYTES, 1024);
     auto qk = [&](uint32_t blk, int x, int qx) {  // S_x <- Q_qx . K(blk)^T
-      const uint32_t kb = sK + (blk & 1) * TILE_BYTES, qb = sQ + qx * TILE_BYTES;
-#pragma unroll
-      for (int kk = 0; kk < HD / 16; ++kk) {
-        const uint32_t off = (kk >> 2) * HALF_BYTES + (kk & 3) * 32;
-        tc_mma_f16(tmem + x * 128, smem_desc_sw128(qb + off, 16, 1024), smem_desc_sw128(kb + off, 16, 1024), IDESC_QK,
-                   kk > 0);
-      }
+      mma_qk(tmem + x * 128, q_lo + qx * (TILE_BYTES >> 4), k_lo + (blk & 1) * (TILE_BYTES >> 4), IDESC_QK);
       tc_commit(bar(B_SFULL + x));
     };
     auto pv = [&](uint32_t blk, int x, bool add) {  // O_x (+)= P_x . V(blk)
-      const uint32_t vb = sV + (blk & 1) * TILE_BYTES;
-#pragma unroll
-      for (int kk = 0; kk < BN / 16; ++kk)
-        tc_mma_f16_tmem_a(tmem + 256 + x * 128, tmem + x * 128 + kk * 8, smem_desc_sw128(vb + kk * 2048, HALF_BYTES, 1024),
-                          IDESC_PV, add || kk > 0);
+      mma_pv(tmem + 256 + x * 128, tmem + x * 128, v_lo + (blk & 1) * (TILE_BYTES >> 4), IDESC_PV, add);
     };
     auto wait = [&](int which, uint32_t parity) {
       ok = ok && warp_wait(bar(which), parity & 1, &s_abort);
@@ -564,7 +612,7 @@ __global__ void __launch_bounds__(THREADS, 1) k_kv4_attn_many(ManyArgs f) {
     // two 64-dim halves take their words two apart, so that eight lanes' stores
     // fall in different banks
     const int swap = c >> 1;
-    Piece pc;
+    Piece pc = {};
     uint32_t dst[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i)
