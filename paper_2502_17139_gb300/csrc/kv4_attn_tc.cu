@@ -11,8 +11,9 @@
 // (Folding these into V as well would round them; applying K's scales to S
 // would have every row read them from shared memory, as it does V's: 256
 // bytes a row and block as bf16, a third of the products' own operands.)
-//   * Four warps turn 4-bit rows into 16-bit tiles in shared memory (128-byte
-//     swizzle), two stages of K and V each, one block ahead in registers.  A
+//   * Eight warps turn 4-bit rows into 16-bit tiles in shared memory (128-byte
+//     swizzle), two stages of K and V each, one block ahead in
+//     registers and more asked into L2.  A
 //     number c + 8 placed in bits 6..9 of a half is 16 + (c + 8) in fp16; one
 //     packed fma with (s, -24 s), exact, makes it c s.  In bits 0..3 it is 128
 //     + (c + 8) in bf16, and one subtraction makes it c.  A word's 8 numbers come out
@@ -44,7 +45,8 @@ FC_DEFINE_ERROR_WORD(kv4_tc)
 namespace {
 
 constexpr int HD = KV4_D;
-constexpr int THREADS = 512;  // warp 0 products, 1-3 queries, 4-7 / 8-11 softmax, 12-15 numbers to tiles
+constexpr int THREADS = 640;  // warp 0 products, 1 pieces, 2-3 queries, 4-7 / 8-11 softmax, 12-19 numbers to tiles
+constexpr int NUM_WARPS = 8;
 constexpr int BM = 128, BN = 128, ROWS = 2 * BM;
 constexpr uint32_t HALF_BYTES = 128 * 128;         // 64 dims of 128 rows
 constexpr uint32_t TILE_BYTES = 2 * HALF_BYTES;
@@ -55,8 +57,8 @@ constexpr int SLOTS = 4;                                        // blocks whose 
 constexpr uint32_t OFF_KEEP = OFF_V + 2 * TILE_BYTES;           // [slot][4] bits of the keys that count
 constexpr uint32_t OFF_VS = OFF_KEEP + SLOTS * 16;              // [slot][128] value scales, bf16
 constexpr uint32_t OFF_EXP = OFF_VS + SLOTS * BN * 2;           // [slot] exponent of K
-constexpr uint32_t OFF_TOP = OFF_EXP + SLOTS * 4;               // [2][4 warps] largest key scales of a block
-constexpr uint32_t OFF_QE = OFF_TOP + 2 * 16;                   // [2 pieces][256] exponents of the query rows
+constexpr uint32_t OFF_TOP = OFF_EXP + SLOTS * 4;               // [2][8 warps] largest key scales of a block
+constexpr uint32_t OFF_QE = OFF_TOP + 2 * 32;                   // [2 pieces][256] exponents of the query rows
 constexpr uint32_t OFF_ML = OFF_QE + 2 * ROWS * 4;              // [2 turns][2][128] (m, l) exchanged at a unit's end
 constexpr int PIECES = 4;                                       // piece descriptions kept
 constexpr uint32_t OFF_PIECE = OFF_ML + 4 * BM * 8;             // [PIECES]
@@ -73,28 +75,28 @@ constexpr float M_START = -1e30f;  // a reference before any key
 constexpr int E_MIN = -50;
 // A unit's start and end in blocks of one tile, and the least share worth a CTA.
 constexpr int UNIT_COST = 8, LEAST = 12;
+constexpr int AHEAD = 4;  // blocks asked into L2 before they are fetched
 
-// Registers a thread by warpgroup (setmaxnreg), of the launch's 128: a softmax
-// thread holds a row's 128 scores.  The shares must add up to the launch's
+// Registers a thread by warpgroup (setmaxnreg), of the launch's 96.  The shares must add up to the launch's
 // allocation, or the increase never returns; the host checks the compiled count.
-constexpr int REGS_LAUNCH = 128, REGS_ISSUE = 56, REGS_NUMBERS = 88, REGS_SOFTMAX = 184;
-static_assert(REGS_ISSUE + REGS_NUMBERS + 2 * REGS_SOFTMAX <= 4 * REGS_LAUNCH, "register split");
+constexpr int REGS_LAUNCH = 96, REGS_ISSUE = 64, REGS_NUMBERS = 80, REGS_SOFTMAX = 128;
+static_assert(REGS_ISSUE + 2 * REGS_NUMBERS + 2 * REGS_SOFTMAX <= 5 * REGS_LAUNCH, "register split");
 
 enum {
-  B_KFULL = 0,   // [2] 128 arrivals
-  B_VFULL = 2,   // [2] 128
+  B_KFULL = 0,   // [2] 8 arrivals
+  B_VFULL = 2,   // [2] 8
   B_KEMPTY = 4,  // [2]
   B_VEMPTY = 6,  // [2]
   B_SFULL = 8,   // [2 tiles]
   B_PFULL = 10,  // [2 tiles] 128
-  B_INFO = 12,   // [4 slots] 4: a block's exponents and keep bits
+  B_INFO = 12,   // [4 slots] 8: a block's exponents and keep bits
   B_QFULL = 16,  // 65
   B_QFREE = 17,
   B_OFIN = 18,
   B_OFREE = 19,  // 256
   B_ML = 20,     // 256: a row's halves exchanged
   B_PIECE = 21,  // [PIECES] a description is written
-  B_TOP = 25,    // [2] 4: largest scales of a block to come
+  B_TOP = 25,    // [2] 8: largest key scales of a block
   B_QE = 27,     // [2] 64: the query rows' exponents
   B_DRAIN = 29,
   N_BARS = 30
@@ -216,6 +218,7 @@ __device__ __forceinline__ void mma_pv(uint32_t d, uint32_t a_tmem, uint32_t b_l
       "r"(a_tmem), "r"(b_lo), "r"(idesc), "r"(add), "n"(DESC_HI)
       : "memory");
 }
+__device__ __forceinline__ void prefetch_l2(const void* p) { asm volatile("prefetch.global.L2 [%0];" ::"l"(p)); }
 // 16 bytes of bf16 in dimension order to the tiles' order
 __device__ __forceinline__ uint4 permute8(const uint4& v) {
   return make_uint4(__byte_perm(v.x, v.z, 0x5410), __byte_perm(v.x, v.z, 0x7632), __byte_perm(v.y, v.w, 0x5410),
@@ -413,8 +416,8 @@ __global__ void __launch_bounds__(THREADS, 1) k_kv4_attn_many(ManyArgs f) {
     s_abort = 0;
     for (int i = 0; i < N_BARS; ++i) {
       uint32_t n = 1;
-      if (i < B_KEMPTY || i == B_PFULL || i == B_PFULL + 1) n = 128;
-      if ((i >= B_INFO && i < B_INFO + SLOTS) || i == B_TOP || i == B_TOP + 1) n = 4;
+      if (i == B_PFULL || i == B_PFULL + 1) n = 128;
+      if (i < B_KEMPTY || (i >= B_INFO && i < B_INFO + SLOTS) || i == B_TOP || i == B_TOP + 1) n = NUM_WARPS;
       if (i == B_QE || i == B_QE + 1) n = 64;
       if (i == B_QFULL) n = 65;
       if (i == B_OFREE || i == B_ML) n = 256;
@@ -607,85 +610,99 @@ __global__ void __launch_bounds__(THREADS, 1) k_kv4_attn_many(ManyArgs f) {
     }
   } else if (warp >= 12) {
     // ---------------- numbers to tiles ----------------
-    const int r = tid - 384, w = warp - 12, c = lane & 3, rho = lane >> 2;
-    // 32-row pass p: row 32p + 8w + rho, 16 bytes c of its 64; the lanes of the
-    // two 64-dim halves take their words two apart, so that eight lanes' stores
-    // fall in different banks
-    const int swap = c >> 1;
-    Piece pc = {};
+    // Warp w has rows 16w .. 16w + 15 of a block, one run of a page: lane (rho,
+    // c) rows rho and rho + 8, 16 bytes c of their 64.  The lanes of the two
+    // 64-dim halves take their words two apart, so that eight lanes' stores
+    // fall in different banks.
+    const int w = warp - 12, c = lane & 3, rho = lane >> 2, swap = c >> 1;
     uint32_t dst[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i)
-      dst[i] = swap * HALF_BYTES + (8 * w + rho) * 128 + ((((c & 1) * 4 + (i ^ (2 * swap))) ^ rho) << 4);
-    uint4 kr[4], vr[4];
-    int ids[4];            // pages of the passes' rows in the next block to fetch (-1: none)
-    uint32_t runs[4];      // 8-row runs of the block being fetched
-    uint32_t sc[4];        // its scales: K in the low half, V in the high
-    uint32_t live = 0;     // bit p: the pass's rows are in the pool
+      dst[i] = swap * HALF_BYTES + (16 * w + rho) * 128 + ((((c & 1) * 4 + (i ^ (2 * swap))) ^ rho) << 4);
+    Piece pc = {};
+    uint4 kr[2], vr[2];
+    uint32_t sc[2] = {0u, 0u};  // scales: K in the low half, V in the high
+    int id = -1, id_next = -1, id_ahead = -1;  // pages: of the block fetched, of the next, of the one to ask for
     uint32_t nb = 0;
     bool ok = true;
-    const uint32_t per_page = (uint32_t)a.Hkv << (a.shift - 3), in_page = (1u << (a.shift - 3)) - 1u;
+    // runs of 16 rows are counted in 32 bits (1024 bytes each: 4 TB)
+    const uint32_t per_page = (uint32_t)a.Hkv << (a.shift - 4), in_page = (1u << (a.shift - 4)) - 1u;
     auto look_up = [&](int blk) {
-      const int32_t* tab = a.table + (size_t)pc.b * a.max_pages;
-#pragma unroll
-      for (int p = 0; p < 4; ++p) {
-        const long long key = (long long)blk * BN + 32 * p + 8 * w;
-        ids[p] = key < pc.kvl ? tab[key >> a.shift] : -1;
-      }
+      const uint32_t run = (uint32_t)blk * (BN / 16) + w;
+      return pc.kvl > 0 && run <= (uint32_t)(pc.kvl - 1) >> 4 ? a.table[(size_t)pc.b * a.max_pages + (run >> (a.shift - 4))] : -1;
     };
-    auto fetch_k = [&](int blk) {  // K rows and both scales, of the pages looked up before
-      live = 0;
-#pragma unroll
-      for (int p = 0; p < 4; ++p) {
-        const uint32_t key8 = (uint32_t)blk * (BN / 8) + 4 * p + w;
-        const bool in = (unsigned)ids[p] < (unsigned)a.n_pages;
-        if (!in && (long long)key8 * 8 < pc.kvl && lane == 0) fc_flag(FC_ERR_WORD(a.err), FC_EBIT_INVALID);
-        live |= (in ? 1u : 0u) << p;
-        runs[p] = in ? ids[p] * per_page + ((uint32_t)pc.gh << (a.shift - 3)) + (key8 & in_page) : 0u;
-        kr[p] = *reinterpret_cast<const uint4*>(a.kc + (uint64_t)runs[p] * 512u + lane * 16);
-        const uint64_t row = (uint64_t)runs[p] * 8u + rho;
-        sc[p] = reinterpret_cast<const uint16_t*>(a.ks)[row] |
-                ((uint32_t)reinterpret_cast<const uint16_t*>(a.vs)[row] << 16);
-      }
+    auto run_of = [&](int page, int blk) {
+      return page * per_page + ((uint32_t)pc.gh << (a.shift - 4)) + (((uint32_t)blk * (BN / 16) + w) & in_page);
     };
-    auto fetch_v = [&]() {
-#pragma unroll
-      for (int p = 0; p < 4; ++p)
-        vr[p] = *reinterpret_cast<const uint4*>(a.vc + (uint64_t)runs[p] * 512u + lane * 16);
+    auto fetch_k = [&](int blk) {  // K rows and both scales, of page id
+      const bool in = (unsigned)id < (unsigned)a.n_pages;
+      const uint32_t run = in ? run_of(id, blk) : 0u;
+      const uint4* src = reinterpret_cast<const uint4*>(a.kc + (uint64_t)run * 1024u) + lane;
+      kr[0] = src[0];
+      kr[1] = src[32];
+      const uint16_t* ks = reinterpret_cast<const uint16_t*>(a.ks) + (uint64_t)run * 16u + rho;
+      const uint16_t* vs = reinterpret_cast<const uint16_t*>(a.vs) + (uint64_t)run * 16u + rho;
+      sc[0] = ks[0] | ((uint32_t)vs[0] << 16);
+      sc[1] = ks[8] | ((uint32_t)vs[8] << 16);
+    };
+    auto fetch_v = [&](int blk) {
+      const uint32_t run = (unsigned)id < (unsigned)a.n_pages ? run_of(id, blk) : 0u;
+      const uint4* src = reinterpret_cast<const uint4*>(a.vc + (uint64_t)run * 1024u) + lane;
+      vr[0] = src[0];
+      vr[1] = src[32];
+    };
+    // Blocks AHEAD of the one being fetched are asked into L2: 8 lines of K, 8
+    // of V, the scales.
+    auto ask = [&](int blk) {
+      if ((unsigned)id_ahead < (unsigned)a.n_pages && lane < 18) {
+        const uint64_t run = run_of(id_ahead, blk);
+        prefetch_l2(lane < 8    ? (const void*)(a.kc + run * 1024u + lane * 128)
+                    : lane < 16 ? (const void*)(a.vc + run * 1024u + (lane - 8) * 128)
+                                : (const void*)((lane == 16 ? a.ks : a.vs) + run * 16u));
+      }
+      id_ahead = look_up(blk + 1);
     };
     const size_t no_row = ~(size_t)0;
     auto new_row = [&](int j) {
       return a.k_new && j < pc.nn ? (((size_t)pc.b * a.Hkv + pc.gh) * a.n_pad + j) * HD : no_row;
     };
-    // The largest key scale (magnitude, for the new tokens) of this warp's rows of block blk.
-    auto announce = [&](int blk) {
+    // keys of this warp's 16 that count in block blk
+    auto keys_of = [&](int blk) {
+      if (blk >= pc.cached) return a.k_new ? pc.nn - 16 * w : 0;
+      return (unsigned)id < (unsigned)a.n_pages ? (int)min(16ll, pc.kvl - (long long)blk * BN - 16 * w) : 0;
+    };
+    // The largest key scale (magnitude, for the new tokens) of this warp's rows
+    // of block blk, to the other warps.
+    auto announce = [&](int blk, int st) {
       uint32_t top = 0;
       if (blk < pc.cached) {
-#pragma unroll
-        for (int p = 0; p < 4; ++p) {
-          const long long key = (long long)blk * BN + 32 * p + 8 * w + rho;
-          if (!((live >> p) & 1u) || key >= pc.kvl) sc[p] = 0;  // a key that does not count: whatever stands there
-          top = top2(top, sc[p] & 0xFFFFu);
-        }
+        const int left = keys_of(blk);  // a key that does not count: whatever stands there
+        if (rho >= left) sc[0] = 0;
+        if (rho + 8 >= left) sc[1] = 0;
+        top = top2(top2(0u, sc[0] & 0xFFFFu), sc[1] & 0xFFFFu);
       } else {
         uint32_t tk = 0;
 #pragma unroll 4
-        for (int e = r; e < BN * 16; e += 128) {
-          const size_t row = new_row(e >> 4);
+        for (int e = lane; e < 256; e += 32) {
+          const size_t row = new_row(16 * w + (e >> 4));
           if (row == no_row) break;
           const uint4 k = reinterpret_cast<const uint4*>(a.k_new + row)[e & 15];
           tk = top2(top2(top2(top2(tk, k.x), k.y), k.z), k.w);
         }
         top = max(tk & 0xFFFFu, tk >> 16);
       }
-      return __reduce_max_sync(0xFFFFFFFFu, top);
+      top = __reduce_max_sync(0xFFFFFFFFu, top);
+      if (lane == 0) {
+        reinterpret_cast<uint32_t*>(smem + OFF_TOP)[st * NUM_WARPS + w] = top;
+        mbar_arrive(bar(B_TOP + st));
+      }
     };
-    auto store = [&](uint32_t tile, const uint4 (&x)[4], auto&& convert) {
+    auto store = [&](uint32_t tile, const uint4 (&x)[2], auto&& convert) {
 #pragma unroll
-      for (int p = 0; p < 4; ++p) {
+      for (int p = 0; p < 2; ++p) {
         const uint32_t w0 = swap ? x[p].z : x[p].x, w1 = swap ? x[p].w : x[p].y;
         const uint32_t w2 = swap ? x[p].x : x[p].z, w3 = swap ? x[p].y : x[p].w;
-        unsigned char* t = smem + tile + p * 4096;
+        unsigned char* t = smem + tile + p * 1024;
         *reinterpret_cast<uint4*>(t + dst[0]) = convert(p, w0);
         *reinterpret_cast<uint4*>(t + dst[1]) = convert(p, w1);
         *reinterpret_cast<uint4*>(t + dst[2]) = convert(p, w2);
@@ -694,13 +711,18 @@ __global__ void __launch_bounds__(THREADS, 1) k_kv4_attn_many(ManyArgs f) {
     };
     auto store_new = [&](uint32_t tile, const __nv_bfloat16* src, auto&& convert) {  // the new rows, zeros past them
 #pragma unroll 4
-      for (int e = r; e < BN * 16; e += 128) {
-        const int j = e >> 4, ch = e & 15;
+      for (int e = lane; e < 256; e += 32) {
+        const int j = 16 * w + (e >> 4), ch = e & 15;
         const size_t row = new_row(j);
         uint4 v = make_uint4(0, 0, 0, 0);
         if (row != no_row) v = convert(permute8(reinterpret_cast<const uint4*>(src + row)[ch]));
         *reinterpret_cast<uint4*>(smem + tile + (ch >> 3) * HALF_BYTES + j * 128 + (((ch & 7) ^ (j & 7)) << 4)) = v;
       }
+    };
+    auto done = [&](int which) {  // this warp's part of a tile is written
+      fence_proxy_async_smem();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(bar(which));
     };
     for (uint32_t np = 0; ok; ++np) {
       if (!warp_wait(bar(B_PIECE + np % PIECES), (np / PIECES) & 1, &s_abort)) break;
@@ -708,47 +730,42 @@ __global__ void __launch_bounds__(THREADS, 1) k_kv4_attn_many(ManyArgs f) {
       if (pc.n == 0) break;
       const int s1 = pc.s0 + pc.n;
       if (pc.s0 < pc.cached) {
-        look_up(pc.s0);
+        id = look_up(pc.s0);
+        id_next = look_up(pc.s0 + 1);
+        id_ahead = look_up(pc.s0 + AHEAD);
         fetch_k(pc.s0);
-        fetch_v();
-        look_up(pc.s0 + 1);
+        fetch_v(pc.s0);
       }
+      announce(pc.s0, nb & 1);
       for (int blk = pc.s0; blk < s1; ++blk, ++nb) {
         const int st = nb & 1, slot = nb % SLOTS;
-        const bool fresh = blk >= pc.cached;
-        {
-          const uint32_t top = announce(blk);
-          if (lane == 0) {
-            reinterpret_cast<uint32_t*>(smem + OFF_TOP)[st * 4 + w] = top;
-            mbar_arrive(bar(B_TOP + st));
-          }
-        }
+        const bool fresh = blk >= pc.cached, more = blk + 1 < s1 && blk + 1 < pc.cached;
         if (!(ok = warp_wait(bar(B_TOP + st), (nb >> 1) & 1, &s_abort))) break;
-        const uint4 t4 = *reinterpret_cast<const uint4*>(smem + OFF_TOP + st * 16);
-        const int ek = expo_of(max(max(t4.x, t4.y), max(t4.z, t4.w)));
+        const uint4 t4 = *reinterpret_cast<const uint4*>(smem + OFF_TOP + st * 32);
+        const uint4 t8 = *reinterpret_cast<const uint4*>(smem + OFF_TOP + st * 32 + 16);
+        const int ek = expo_of(max(max(max(t4.x, t4.y), max(t4.z, t4.w)), max(max(t8.x, t8.y), max(t8.z, t8.w))));
         // the slot's last readers are done (the V stage of three blocks ago was waited for)
-        if (lane < 4) {  // word p = lane: this warp's 8 keys of it
-          const int left = fresh ? (a.k_new ? pc.nn : 0) - (32 * lane + 8 * w)
-                                 : (int)min((long long)BN, pc.kvl - (long long)blk * BN) - (32 * lane + 8 * w);
-          const uint32_t k8 = left >= 8 ? 0xFFu : (left <= 0 ? 0u : (1u << left) - 1u);
-          smem[OFF_KEEP + slot * 16 + lane * 4 + w] = (unsigned char)(fresh || ((live >> lane) & 1u) ? k8 : 0u);
+        if (lane == 0) {
+          const int left = keys_of(blk);
+          reinterpret_cast<uint16_t*>(smem + OFF_KEEP + slot * 16)[w] =
+              (uint16_t)(left >= 16 ? 0xFFFFu : (left <= 0 ? 0u : (1u << left) - 1u));
+          if (w == 0) reinterpret_cast<int*>(smem + OFF_EXP)[slot] = ek;
+          if (!fresh && (unsigned)id >= (unsigned)a.n_pages && (long long)blk * BN + 16 * w < pc.kvl)
+            fc_flag(FC_ERR_WORD(a.err), FC_EBIT_INVALID);
         }
-        if (w == 0 && lane == 0) reinterpret_cast<int*>(smem + OFF_EXP)[slot] = ek;
-        uint16_t* vs = reinterpret_cast<uint16_t*>(smem + OFF_VS) + slot * BN;
-        if (fresh) {
-          vs[32 * w + lane] = 0x3F80;
-        } else if (c == 0) {
-#pragma unroll
-          for (int p = 0; p < 4; ++p) vs[32 * p + 8 * w + rho] = (uint16_t)(sc[p] >> 16);
+        if (c == 0) {
+          uint16_t* vs = reinterpret_cast<uint16_t*>(smem + OFF_VS) + slot * BN + 16 * w + rho;
+          vs[0] = fresh ? 0x3F80 : (uint16_t)(sc[0] >> 16);
+          vs[8] = fresh ? 0x3F80 : (uint16_t)(sc[1] >> 16);
         }
         __syncwarp();
         if (lane == 0) mbar_arrive(bar(B_INFO + slot));
         if (nb >= 2 && !(ok = warp_wait(bar(B_KEMPTY + st), ((nb >> 1) - 1) & 1, &s_abort))) break;
         const float by = pow2i(E_TOP - ek);
         if (!fresh) {
-          uint32_t s2[4], less24[4];
+          uint32_t s2[2], less24[2];
 #pragma unroll
-          for (int p = 0; p < 4; ++p) {
+          for (int p = 0; p < 2; ++p) {
             const float s = lo_f(sc[p]) * by;
             s2[p] = pack_f16x2(s, s);
             less24[p] = pack_f16x2(-24.f * s, -24.f * s);
@@ -757,18 +774,19 @@ __global__ void __launch_bounds__(THREADS, 1) k_kv4_attn_many(ManyArgs f) {
         } else {
           store_new(OFF_K + st * TILE_BYTES, a.k_new, [&](const uint4& v) { return to_f16(v, by); });
         }
-        fence_proxy_async_smem();
-        mbar_arrive(bar(B_KFULL + st));
+        done(B_KFULL + st);
+        if (more) {
+          id = id_next;
+          fetch_k(blk + 1);
+          id_next = look_up(blk + 2);
+          ask(blk + AHEAD);
+        }
         if (nb >= 2 && !(ok = warp_wait(bar(B_VEMPTY + st), ((nb >> 1) - 1) & 1, &s_abort))) break;
         if (!fresh) store(OFF_V + st * TILE_BYTES, vr, [](int, uint32_t v) { return numbers(v); });
         else store_new(OFF_V + st * TILE_BYTES, a.v_new, [](const uint4& v) { return v; });
-        fence_proxy_async_smem();
-        mbar_arrive(bar(B_VFULL + st));
-        if (blk + 1 < s1 && blk + 1 < pc.cached) {
-          fetch_k(blk + 1);
-          fetch_v();
-          look_up(blk + 2);
-        }
+        done(B_VFULL + st);
+        if (more) fetch_v(blk + 1);
+        if (blk + 1 < s1) announce(blk + 1, st ^ 1);
       }
     }
   } else {
@@ -813,23 +831,30 @@ __global__ void __launch_bounds__(THREADS, 1) k_kv4_attn_many(ManyArgs f) {
         const uint4 kp = *reinterpret_cast<const uint4*>(smem + OFF_KEEP + slot * 16);
         if (!(ok = warp_wait(bar(B_SFULL + x), t & 1, &s_abort))) break;
         tc_fence_after();
-        // the block's 128 scores of this row stay in registers from here on
-        uint32_t sv[BN];
-#pragma unroll
-        for (int c4 = 0; c4 < 4; ++c4) tmem_ld32(tS + c4 * 32, *reinterpret_cast<uint32_t(*)[32]>(&sv[c4 * 32]));
-        tc_wait_ld();
         const bool fresh = wk.s0 + j >= wk.cached;
-        if (fresh || (kp.x & kp.y & kp.z & kp.w) != 0xFFFFFFFFu) {  // alike in the warpgroup
-          const uint32_t keep[4] = {fresh ? kp.x & (uint32_t)m0 : kp.x, fresh ? kp.y & (uint32_t)(m0 >> 32) : kp.y,
-                                    fresh ? kp.z & (uint32_t)m1 : kp.z, fresh ? kp.w & (uint32_t)(m1 >> 32) : kp.w};
+        const bool masked = fresh || (kp.x & kp.y & kp.z & kp.w) != 0xFFFFFFFFu;  // alike in the warpgroup
+        const uint32_t keep[4] = {fresh ? kp.x & (uint32_t)m0 : kp.x, fresh ? kp.y & (uint32_t)(m0 >> 32) : kp.y,
+                                  fresh ? kp.z & (uint32_t)m1 : kp.z, fresh ? kp.w & (uint32_t)(m1 >> 32) : kp.w};
+        // half of the row's 128 scores (read twice: for the maximum, then for P)
+        auto scores = [&](int h, uint32_t (&sv)[64]) {
+          tmem_ld32(tS + h * 64, *reinterpret_cast<uint32_t(*)[32]>(&sv[0]));
+          tmem_ld32(tS + h * 64 + 32, *reinterpret_cast<uint32_t(*)[32]>(&sv[32]));
+          tc_wait_ld();
+          if (masked) {
 #pragma unroll
-          for (int u = 0; u < BN; ++u)
-            if (!((keep[u >> 5] >> (u & 31)) & 1u)) sv[u] = __float_as_uint(-INFINITY);
-        }
+            for (int u = 0; u < 64; ++u)
+              if (!((keep[2 * h + (u >> 5)] >> (u & 31)) & 1u)) sv[u] = __float_as_uint(-INFINITY);
+          }
+        };
         float pm[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
-        for (int u = 0; u < BN; u += 2)
-          pm[(u >> 1) & 3] = max3(pm[(u >> 1) & 3], __uint_as_float(sv[u]), __uint_as_float(sv[u + 1]));
+        for (int h = 0; h < 2; ++h) {
+          uint32_t sv[64];
+          scores(h, sv);
+#pragma unroll
+          for (int u = 0; u < 64; u += 2)
+            pm[(u >> 1) & 3] = max3(pm[(u >> 1) & 3], __uint_as_float(sv[u]), __uint_as_float(sv[u + 1]));
+        }
         const float top = fmaxf(fmaxf(pm[0], pm[1]), fmaxf(pm[2], pm[3])) * cz;
         const float m_new = top > m + RESCALE_THRESHOLD ? top : m;
         const float alpha = exp2_fast(m - m_new);
@@ -849,24 +874,29 @@ __global__ void __launch_bounds__(THREADS, 1) k_kv4_attn_many(ManyArgs f) {
         uint64_t sum[4] = {0ull, 0ull, 0ull, 0ull};
         const uint64_t c2 = f2_pack(cz, cz), neg = f2_pack(-m_new, -m_new);
 #pragma unroll
-        for (int c4 = 0; c4 < 4; ++c4) {
-          uint32_t pk[16];
+        for (int h = 0; h < 2; ++h) {
+          uint32_t sv[64];
+          scores(h, sv);
 #pragma unroll
-          for (int g = 0; g < 4; ++g) {  // 8 keys, their value scales in one load
-            const uint4 v4 = vs8[c4 * 4 + g];
+          for (int q = 0; q < 2; ++q) {
+            uint32_t pk[16];
 #pragma unroll
-            for (int u = 0; u < 4; ++u) {
-              const int k = c4 * 32 + 8 * g + 2 * u;
-              const uint32_t v = (&v4.x)[u];
-              float p0, p1;
-              f2_unpack(f2_fma(f2_pack(__uint_as_float(sv[k]), __uint_as_float(sv[k + 1])), c2, neg), p0, p1);
-              const uint64_t pp = f2_pack(exp2_fast(p0), exp2_fast(p1));
-              sum[u] = f2_add(sum[u], pp);
-              f2_unpack(f2_mul(pp, f2_pack(lo_f(v), hi_f(v))), p0, p1);
-              pk[4 * g + u] = pack_bf16x2(p0, p1);
+            for (int g = 0; g < 4; ++g) {  // 8 keys, their value scales in one load
+              const uint4 v4 = vs8[h * 8 + q * 4 + g];
+#pragma unroll
+              for (int u = 0; u < 4; ++u) {
+                const int k = q * 32 + 8 * g + 2 * u;
+                const uint32_t v = (&v4.x)[u];
+                float p0, p1;
+                f2_unpack(f2_fma(f2_pack(__uint_as_float(sv[k]), __uint_as_float(sv[k + 1])), c2, neg), p0, p1);
+                const uint64_t pp = f2_pack(exp2_fast(p0), exp2_fast(p1));
+                sum[u] = f2_add(sum[u], pp);
+                f2_unpack(f2_mul(pp, f2_pack(lo_f(v), hi_f(v))), p0, p1);
+                pk[4 * g + u] = pack_bf16x2(p0, p1);
+              }
             }
+            tmem_st16(tS + h * 32 + q * 16, pk);  // over scores already read
           }
-          tmem_st16(tS + c4 * 16, pk);  // over scores already read
         }
         tc_wait_st();
         float s0, s1, s2, s3;
