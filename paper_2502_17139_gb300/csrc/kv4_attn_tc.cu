@@ -79,7 +79,7 @@ constexpr int AHEAD = 4;  // blocks asked into L2 before they are fetched
 
 // Registers a thread by warpgroup (setmaxnreg), of the launch's 96.  The shares must add up to the launch's
 // allocation, or the increase never returns; the host checks the compiled count.
-constexpr int REGS_LAUNCH = 96, REGS_ISSUE = 64, REGS_NUMBERS = 80, REGS_SOFTMAX = 128;
+constexpr int REGS_LAUNCH = 96, REGS_ISSUE = 80, REGS_NUMBERS = 80, REGS_SOFTMAX = 120;
 static_assert(REGS_ISSUE + 2 * REGS_NUMBERS + 2 * REGS_SOFTMAX <= 5 * REGS_LAUNCH, "register split");
 
 enum {
@@ -448,13 +448,6 @@ __global__ void __launch_bounds__(THREADS, 1) k_kv4_attn_many(ManyArgs f) {
     // descriptors' low words: a byte offset adds to them in units of 16
     const uint32_t q_lo = (uint32_t)smem_desc_sw128(sQ, 16, 1024), k_lo = (uint32_t)smem_desc_sw128(sK, 16, 1024);
     const uint32_t v_lo = (uint32_t)smem_desc_sw128(sV, HALF_BYTES, 1024);
-    auto qk = [&](uint32_t blk, int x, int qx) {  // S_x <- Q_qx . K(blk)^T
-      mma_qk(tmem + x * 128, q_lo + qx * (TILE_BYTES >> 4), k_lo + (blk & 1) * (TILE_BYTES >> 4), IDESC_QK);
-      tc_commit(bar(B_SFULL + x));
-    };
-    auto pv = [&](uint32_t blk, int x, bool add) {  // O_x (+)= P_x . V(blk)
-      mma_pv(tmem + 256 + x * 128, tmem + x * 128, v_lo + (blk & 1) * (TILE_BYTES >> 4), IDESC_PV, add);
-    };
     auto wait = [&](int which, uint32_t parity) {
       ok = ok && warp_wait(bar(which), parity & 1, &s_abort);
       tc_fence_after();
@@ -465,55 +458,29 @@ __global__ void __launch_bounds__(THREADS, 1) k_kv4_attn_many(ManyArgs f) {
       const Piece* pc = piece(np);
       const int n = pc->n;
       if (n == 0) break;
-      const uint32_t b0 = nb;
       if (!wait(B_QFULL, np)) break;
-      if (pc->two) {
-        if (!wait(B_KFULL + (b0 & 1), b0 >> 1)) break;
-        qk(b0, 0, 0);
-        qk(b0, 1, 1);
-        tc_commit(bar(B_KEMPTY + (b0 & 1)));
-        if (n == 1) tc_commit(bar(B_QFREE));
-        for (int i = 1; ok && i <= n; ++i) {
-          const uint32_t p = b0 + i - 1, c = b0 + i;
-          if (!wait(B_VFULL + (p & 1), p >> 1)) break;
-          for (int x = 0; ok && x < 2; ++x) {
-            if (!wait(B_PFULL + x, t_of[x])) break;
-            ++t_of[x];
-            if (i == 1 && x == 0 && np > 0 && !wait(B_OFREE, np - 1)) break;
-            pv(p, x, i > 1);
-            if (i < n) {
-              if (x == 0 && !wait(B_KFULL + (c & 1), c >> 1)) break;
-              qk(c, x, x);
-            }
-          }
-          if (!ok) break;
-          if (i < n) tc_commit(bar(B_KEMPTY + (c & 1)));
-          if (i == n - 1) tc_commit(bar(B_QFREE));
-          tc_commit(bar(B_VEMPTY + (p & 1)));
-        }
-      } else {
-        for (int i = 0; ok && i < min(2, n); ++i) {
-          const uint32_t c = b0 + i;
-          if (!wait(B_KFULL + (c & 1), c >> 1)) break;
-          qk(c, i, 0);
-          tc_commit(bar(B_KEMPTY + (c & 1)));
-          if (i == n - 1) tc_commit(bar(B_QFREE));
-        }
-        for (int i = 0; ok && i < n; ++i) {
-          const uint32_t p = b0 + i, c = p + 2;
-          const int x = i & 1;
-          if (!wait(B_VFULL + (p & 1), p >> 1)) break;
-          if (!wait(B_PFULL + x, t_of[x])) break;
+      // Steps in order: with two tiles, tile 0 then tile 1 of each block, else
+      // the blocks, tile by tile in turn.  Step k's second product comes before
+      // step k + 2's first, which writes the scores that P took the place of.
+      const int two = pc->two ? 1 : 0, steps = n << two;
+#pragma unroll 1
+      for (int k = -2; k < steps; ++k) {
+        const uint32_t x = k & 1;
+        if (k >= 0) {  // O_x (+)= P_x V
+          const uint32_t blk = nb + (k >> two), st = blk & 1;
+          if (!wait(B_VFULL + st, blk >> 1) || !wait(B_PFULL + x, t_of[x])) break;
           ++t_of[x];
-          if (i == 0 && np > 0 && !wait(B_OFREE, np - 1)) break;
-          pv(p, x, i > 1);
-          tc_commit(bar(B_VEMPTY + (p & 1)));
-          if (i + 2 < n) {
-            if (!wait(B_KFULL + (c & 1), c >> 1)) break;
-            qk(c, x, 0);
-            tc_commit(bar(B_KEMPTY + (c & 1)));
-            if (i + 2 == n - 1) tc_commit(bar(B_QFREE));
-          }
+          if (k == 0 && np > 0 && !wait(B_OFREE, np - 1)) break;
+          mma_pv(tmem + 256 + x * 128, tmem + x * 128, v_lo + st * (TILE_BYTES >> 4), IDESC_PV, k >= 2);
+          if (!two || x) tc_commit(bar(B_VEMPTY + st));
+        }
+        if (k + 2 < steps) {  // S_x <- Q K^T
+          const uint32_t blk = nb + ((k + 2) >> two), st = blk & 1;
+          if (!wait(B_KFULL + st, blk >> 1)) break;
+          mma_qk(tmem + x * 128, q_lo + (two ? x : 0u) * (TILE_BYTES >> 4), k_lo + st * (TILE_BYTES >> 4), IDESC_QK);
+          tc_commit(bar(B_SFULL + x));
+          if (!two || x) tc_commit(bar(B_KEMPTY + st));
+          if (k + 3 == steps) tc_commit(bar(B_QFREE));
         }
       }
       if (!ok) break;
@@ -791,134 +758,149 @@ __global__ void __launch_bounds__(THREADS, 1) k_kv4_attn_many(ManyArgs f) {
     }
   } else {
     // ---------------- softmax: warpgroup x, a row a thread ----------------
-    const int x = (warp - 4) >> 2, q4 = warp & 3, r = q4 * 32 + lane;
-    const uint32_t lane_off = (uint32_t)(q4 * 32) << 16;
-    const uint32_t tS = tmem + x * 128 + lane_off;
+    // (A piece's description is read again where it is needed, not kept: the
+    // loop wants its registers for the scores.)
+    const int x = (warp - 4) >> 2, r = (warp & 3) * 32 + lane;
+    const uint32_t tS = tmem + x * 128 + ((uint32_t)((warp & 3) * 32) << 16), tO = tS + 256;
     uint32_t nb = 0, np = 0, nx = 0, t = 0;
     bool ok = true;
+    auto row_of = [&](const Piece* pc) { return pc->two ? x * BM + r : r; };  // row of the piece
     for (;;) {
       if (!(ok = warp_wait(bar(B_PIECE + np % PIECES), (np / PIECES) & 1, &s_abort))) break;
-      const Piece wk = *piece(np);
-      const int n = wk.n;
+      const Piece* pc = piece(np);
+      const int n = pc->n;
       if (n == 0) break;
-      const int lr = wk.two ? x * BM + r : r;  // row of the piece
-      const bool row_ok = lr < wk.rows;
-      const int rr = wk.row0 + lr, i = row_ok ? rr / a.G : 0, hh = row_ok ? rr - i * a.G : 0;
-      // the new tokens that this row sees
-      uint64_t m0 = 0, m1 = 0;
-      if (wk.s0 + n > wk.cached && row_ok) {
-        if (a.mask) {
-          const int words = (a.n_pad + 63) / 64;
-          const uint64_t* mr = a.mask + ((size_t)wk.b * a.n_pad + i) * words;
-          m0 = mr[0];
-          m1 = words > 1 ? mr[1] : 0ull;
-        } else {
-          m0 = i >= 63 ? ~0ull : (1ull << (i + 1)) - 1ull;
-          m1 = i < 64 ? 0ull : (i >= 127 ? ~0ull : (1ull << (i - 63)) - 1ull);
-        }
-      }
       float m = M_START, l = 0.f;  // m: the reference
-      bool any = false;            // O_x holds a product
       if (!(ok = warp_wait(bar(B_QE + (np & 1)), (np >> 1) & 1, &s_abort))) break;
       // scores: S times 2^(qe - E_TOP) 2^(ek - E_TOP) and the softmax's scale
-      const float c_row = a.scale_log2 * pow2i(reinterpret_cast<const int*>(smem + OFF_QE)[(np & 1) * ROWS + lr] - E_TOP);
-      const uint32_t tO = tmem + 256 + x * 128 + lane_off;
-      for (int j = wk.two ? 0 : x; j < n; j += wk.two ? 1 : 2, ++t) {
+      const float c_row =
+          a.scale_log2 * pow2i(reinterpret_cast<const int*>(smem + OFF_QE)[(np & 1) * ROWS + row_of(pc)] - E_TOP);
+      const int every = pc->two ? 1 : 2, first = pc->two ? 0 : x, n_cached = pc->cached - pc->s0;
+#pragma unroll 1
+      for (int j = first; j < n; j += every, ++t) {
         const int slot = (nb + j) % SLOTS;
         if (!(ok = warp_wait(bar(B_INFO + slot), ((nb + j) / SLOTS) & 1, &s_abort))) break;
         const float cz = c_row * pow2i(reinterpret_cast<const int*>(smem + OFF_EXP)[slot] - E_TOP);
-        const uint4* vs8 = reinterpret_cast<const uint4*>(smem + OFF_VS + slot * BN * 2);
-        const uint4 kp = *reinterpret_cast<const uint4*>(smem + OFF_KEEP + slot * 16);
+        const uint32_t* keep = reinterpret_cast<const uint32_t*>(smem + OFF_KEEP) + slot * 4;
+        const bool masked = j >= n_cached || (keep[0] & keep[1] & keep[2] & keep[3]) != 0xFFFFFFFFu;  // in all rows alike
         if (!(ok = warp_wait(bar(B_SFULL + x), t & 1, &s_abort))) break;
         tc_fence_after();
-        const bool fresh = wk.s0 + j >= wk.cached;
-        const bool masked = fresh || (kp.x & kp.y & kp.z & kp.w) != 0xFFFFFFFFu;  // alike in the warpgroup
-        const uint32_t keep[4] = {fresh ? kp.x & (uint32_t)m0 : kp.x, fresh ? kp.y & (uint32_t)(m0 >> 32) : kp.y,
-                                  fresh ? kp.z & (uint32_t)m1 : kp.z, fresh ? kp.w & (uint32_t)(m1 >> 32) : kp.w};
-        // half of the row's 128 scores (read twice: for the maximum, then for P)
-        auto scores = [&](int h, uint32_t (&sv)[64]) {
-          tmem_ld32(tS + h * 64, *reinterpret_cast<uint32_t(*)[32]>(&sv[0]));
-          tmem_ld32(tS + h * 64 + 32, *reinterpret_cast<uint32_t(*)[32]>(&sv[32]));
-          tc_wait_ld();
-          if (masked) {
-#pragma unroll
-            for (int u = 0; u < 64; ++u)
-              if (!((keep[2 * h + (u >> 5)] >> (u & 31)) & 1u)) sv[u] = __float_as_uint(-INFINITY);
+        if (masked) {  // masked scores are overwritten by -inf
+          uint64_t sees[2] = {~0ull, ~0ull};
+          if (j >= n_cached) {  // the new tokens that this row sees
+            const int lr = row_of(pc), i = (pc->row0 + lr) / a.G;
+            if (lr >= pc->rows) {
+              sees[0] = sees[1] = 0;
+            } else if (a.mask) {
+              const int words = (a.n_pad + 63) / 64;
+              const uint64_t* mr = a.mask + ((size_t)pc->b * a.n_pad + i) * words;
+              sees[0] = mr[0];
+              sees[1] = words > 1 ? mr[1] : 0ull;
+            } else {
+              sees[0] = i >= 63 ? ~0ull : (1ull << (i + 1)) - 1ull;
+              sees[1] = i < 64 ? 0ull : (i >= 127 ? ~0ull : (1ull << (i - 63)) - 1ull);
+            }
           }
-        };
-        float pm[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          uint32_t sv[64];
-          scores(h, sv);
-#pragma unroll
-          for (int u = 0; u < 64; u += 2)
-            pm[(u >> 1) & 3] = max3(pm[(u >> 1) & 3], __uint_as_float(sv[u]), __uint_as_float(sv[u + 1]));
-        }
-        const float top = fmaxf(fmaxf(pm[0], pm[1]), fmaxf(pm[2], pm[3])) * cz;
-        const float m_new = top > m + RESCALE_THRESHOLD ? top : m;
-        const float alpha = exp2_fast(m - m_new);
-        l *= alpha;
-        // S_x is the newest product of this tile, so O_x is complete
-        if (any && __any_sync(0xFFFFFFFFu, alpha != 1.f)) {
 #pragma unroll 1
-          for (int cc = 0; cc < HD / 16; ++cc) {
-            uint32_t o[16];
-            tmem_ld16(tO + cc * 16, o);
+          for (int q = 0; q < 4; ++q) {
+            const uint32_t k = keep[q] & (uint32_t)(sees[q >> 1] >> (32 * (q & 1)));
+            uint32_t sv[32];
+            tmem_ld32(tS + q * 32, sv);
             tc_wait_ld();
 #pragma unroll
-            for (int u = 0; u < 16; ++u) o[u] = __float_as_uint(__uint_as_float(o[u]) * alpha);
-            tmem_st16(tO + cc * 16, o);
+            for (int u = 0; u < 32; ++u)
+              if (!((k >> u) & 1u)) sv[u] = __float_as_uint(-INFINITY);
+            tmem_st32(tS + q * 32, sv);
           }
+          tc_wait_st();
         }
-        uint64_t sum[4] = {0ull, 0ull, 0ull, 0ull};
-        const uint64_t c2 = f2_pack(cz, cz), neg = f2_pack(-m_new, -m_new);
+        // The row's scores come 32 at a time, the next in flight meanwhile; once
+        // for the maximum, once for P.
+        uint32_t sa[32], sb[32];
+        float pm[2] = {-INFINITY, -INFINITY};
+        auto largest = [&](const uint32_t (&sv)[32]) {
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          uint32_t sv[64];
-          scores(h, sv);
+          for (int u = 0; u < 32; u += 2)
+            pm[(u >> 1) & 1] = max3(pm[(u >> 1) & 1], __uint_as_float(sv[u]), __uint_as_float(sv[u + 1]));
+        };
+        tmem_ld32(tS, sa);
+        tc_wait_ld();
+#pragma unroll 1
+        for (int q = 0; q < 4; q += 2) {
+          tmem_ld32(tS + (q + 1) * 32, sb);
+          largest(sa);
+          tc_wait_ld();
+          tmem_ld32(tS + ((q + 2) & 3) * 32, sa);  // the last one: P's first
+          largest(sb);
+          tc_wait_ld();
+        }
+        {
+          const float top = fmaxf(pm[0], pm[1]) * cz;
+          if (__any_sync(0xFFFFFFFFu, top > m + RESCALE_THRESHOLD)) {
+            const float m_new = top > m + RESCALE_THRESHOLD ? top : m, alpha = exp2_fast(m - m_new);
+            l *= alpha;
+            m = m_new;
+            if (j > first) {  // S_x is the newest product of this tile, so O_x is complete
+#pragma unroll 1
+              for (int cc = 0; cc < HD / 32; ++cc) {
+                tmem_ld32(tO + cc * 32, sb);
+                tc_wait_ld();
 #pragma unroll
-          for (int q = 0; q < 2; ++q) {
-            uint32_t pk[16];
-#pragma unroll
-            for (int g = 0; g < 4; ++g) {  // 8 keys, their value scales in one load
-              const uint4 v4 = vs8[h * 8 + q * 4 + g];
-#pragma unroll
-              for (int u = 0; u < 4; ++u) {
-                const int k = q * 32 + 8 * g + 2 * u;
-                const uint32_t v = (&v4.x)[u];
-                float p0, p1;
-                f2_unpack(f2_fma(f2_pack(__uint_as_float(sv[k]), __uint_as_float(sv[k + 1])), c2, neg), p0, p1);
-                const uint64_t pp = f2_pack(exp2_fast(p0), exp2_fast(p1));
-                sum[u] = f2_add(sum[u], pp);
-                f2_unpack(f2_mul(pp, f2_pack(lo_f(v), hi_f(v))), p0, p1);
-                pk[4 * g + u] = pack_bf16x2(p0, p1);
+                for (int u = 0; u < 32; ++u) sb[u] = __float_as_uint(__uint_as_float(sb[u]) * alpha);
+                tmem_st32(tO + cc * 32, sb);
               }
             }
-            tmem_st16(tS + h * 32 + q * 16, pk);  // over scores already read
           }
         }
+        uint64_t sum[2] = {0ull, 0ull};
+        const uint64_t c2 = f2_pack(cz, cz), neg = f2_pack(-m, -m);
+        const uint4* vs8 = reinterpret_cast<const uint4*>(smem + OFF_VS + slot * BN * 2);
+        auto weigh = [&](int q, const uint32_t (&sv)[32]) {  // over scores already read
+          uint32_t pk[16];
+#pragma unroll
+          for (int g = 0; g < 4; ++g) {  // 8 keys, their value scales in one load
+            const uint4 v4 = vs8[q * 4 + g];
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+              const int k = 8 * g + 2 * u;
+              const uint32_t v = (&v4.x)[u];
+              float p0, p1;
+              f2_unpack(f2_fma(f2_pack(__uint_as_float(sv[k]), __uint_as_float(sv[k + 1])), c2, neg), p0, p1);
+              const uint64_t pp = f2_pack(exp2_fast(p0), exp2_fast(p1));
+              sum[u & 1] = f2_add(sum[u & 1], pp);
+              f2_unpack(f2_mul(pp, f2_pack(lo_f(v), hi_f(v))), p0, p1);
+              pk[4 * g + u] = pack_bf16x2(p0, p1);
+            }
+          }
+          tmem_st16(tS + q * 16, pk);
+        };
+#pragma unroll 1
+        for (int q = 0; q < 4; q += 2) {
+          tmem_ld32(tS + (q + 1) * 32, sb);
+          weigh(q, sa);
+          tc_wait_ld();
+          if (q == 0) tmem_ld32(tS + 64, sa);
+          weigh(q + 1, sb);
+          tc_wait_ld();
+        }
         tc_wait_st();
-        float s0, s1, s2, s3;
+        float s0, s1;
         f2_unpack(f2_add(sum[0], sum[1]), s0, s1);
-        f2_unpack(f2_add(sum[2], sum[3]), s2, s3);
-        l += (s0 + s1) + (s2 + s3);
-        m = m_new;
-        any = true;
+        l += s0 + s1;
         tc_fence_before();
         mbar_arrive(bar(B_PFULL + x));
       }
       if (!ok || !(ok = warp_wait(bar(B_OFIN), np & 1, &s_abort))) break;
       tc_fence_after();
       // ---- the piece's rows: this tile's, or half the dimensions of both halves' sum
-      const bool whole = wk.whole;
-      const size_t slot = (size_t)wk.slot * f.rows_cap;
-      __nv_bfloat16* dst = a.out + (((size_t)wk.b * a.n_pad + i) * a.H + wk.gh * a.G + hh) * HD;
+      const bool two = pc->two, whole = pc->whole;
+      const int lr = row_of(pc), rr = pc->row0 + lr, i = rr / a.G, hh = rr - i * a.G;
+      const bool row_ok = lr < pc->rows;
+      __nv_bfloat16* dst = a.out + (((size_t)pc->b * a.n_pad + (row_ok ? i : 0)) * a.H + pc->gh * a.G + hh) * HD;
+      const size_t slot = (size_t)pc->slot * f.rows_cap + lr;
       float m_all = m, k0 = 1.f, k1 = 0.f;
-      bool have0 = any, have1 = false;
-      uint32_t tO0 = tO, tO1 = tO;
-      int cc0 = 0, cc1 = HD / 32;
-      if (!wk.two) {
+      uint32_t tO0 = tO;
+      if (!two) {
         // two turns' room: a turn is written again only after both have read it
         float2* ml = reinterpret_cast<float2*>(smem + OFF_ML) + (nx & 1) * 2 * BM;
         ml[x * BM + r] = make_float2(m, l);
@@ -931,26 +913,25 @@ __global__ void __launch_bounds__(THREADS, 1) k_kv4_attn_many(ManyArgs f) {
         l = l * mine + other.y * theirs;
         k0 = x == 0 ? mine : theirs;
         k1 = x == 0 ? theirs : mine;
-        have0 = n > 0;
-        have1 = n > 1;
-        tO0 = tmem + 256 + lane_off;
-        tO1 = tO0 + 128;
-        cc0 = 2 * x;
-        cc1 = cc0 + 2;
+        tO0 -= x * 128;
       }
       const float inv = !whole ? 1.f : (l == 0.f ? 0.f : 1.f / l);
+      k0 *= inv;
+      k1 *= inv;
+      const bool both = !two && n > 1;
 #pragma unroll 1
-      for (int cc = 2 * cc0; cc < 2 * cc1; ++cc) {
-        uint32_t o[16], o1[16];
+      for (int cc = two ? 0 : 4 * x; cc < (two ? 8 : 4 * x + 4); ++cc) {
+        uint32_t o[16];
         float v[16];
-        if (have0) tmem_ld16(tO0 + cc * 16, o);
-        if (have1) tmem_ld16(tO1 + cc * 16, o1);
+        tmem_ld16(tO0 + cc * 16, o);
         tc_wait_ld();
 #pragma unroll
-        for (int u = 0; u < 16; ++u) {
-          float y = have0 ? __uint_as_float(o[u]) * k0 : 0.f;
-          if (have1) y += __uint_as_float(o1[u]) * k1;
-          v[u] = y * inv;
+        for (int u = 0; u < 16; ++u) v[u] = __uint_as_float(o[u]) * k0;
+        if (both) {
+          tmem_ld16(tO0 + 128 + cc * 16, o);
+          tc_wait_ld();
+#pragma unroll
+          for (int u = 0; u < 16; ++u) v[u] = fmaf(__uint_as_float(o[u]), k1, v[u]);
         }
         if (row_ok) {
 #pragma unroll
@@ -960,14 +941,14 @@ __global__ void __launch_bounds__(THREADS, 1) k_kv4_attn_many(ManyArgs f) {
                   make_uint4(pack_bf16x2(v[u], v[u + 2]), pack_bf16x2(v[u + 4], v[u + 6]),
                              pack_bf16x2(v[u + 1], v[u + 3]), pack_bf16x2(v[u + 5], v[u + 7]));
             } else {
-              float4* po = reinterpret_cast<float4*>(f.part_o + (slot + lr) * HD + cc * 16 + u);
+              float4* po = reinterpret_cast<float4*>(f.part_o + slot * HD + cc * 16 + u);
               po[0] = make_float4(v[u], v[u + 2], v[u + 4], v[u + 6]);
               po[1] = make_float4(v[u + 1], v[u + 3], v[u + 5], v[u + 7]);
             }
           }
         }
       }
-      if (!whole && row_ok && (wk.two || x == 0)) f.part_ml[slot + lr] = make_float2(m_all, l);
+      if (!whole && row_ok && (two || x == 0)) f.part_ml[slot] = make_float2(m_all, l);
       tc_fence_before();
       mbar_arrive(bar(B_OFREE));
       nb += n;
