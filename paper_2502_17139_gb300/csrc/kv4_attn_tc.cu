@@ -6,7 +6,7 @@
 //   S = Q K^T,  P = 2^(c S - m) * (value scale),  O += P V.
 // The first product is in fp16: a cached key's values c * s have at most 3 + 8
 // significant bits, so they are exact, and powers of two (one per query row,
-// one per block of K) keep them in range.  The second is in bf16, P needing
+// one per 16 keys) keep them in range.  The second is in bf16, P needing
 // its range: V the whole numbers -7..7, their scales multiplied into P.
 // (Folding these into V as well would round them; applying K's scales to S
 // would have every row read them from shared memory, as it does V's: 256
@@ -28,7 +28,7 @@
 //     one takes the even blocks and one the odd, and their halves are joined
 //     at the end, so that one tile's softmax always has the other's products
 //     beside it.
-//   * Three warps fetch the next unit's queries while this one's end is
+//   * The eight warps also fetch a unit's queries, while the last one's end is
 //     written.
 // The CTAs (one an SM) share all units' blocks equally, cut anywhere; a cut
 // unit's pieces go through the workspace to k_kv4_join.
@@ -45,7 +45,7 @@ FC_DEFINE_ERROR_WORD(kv4_tc)
 namespace {
 
 constexpr int HD = KV4_D;
-constexpr int THREADS = 640;  // warp 0 products, 1 pieces, 2-3 queries, 4-7 / 8-11 softmax, 12-19 numbers to tiles
+constexpr int THREADS = 640;  // warp 0 products, 1 pieces, 2-3 padding rows, 4-7 / 8-11 softmax, 12-19 queries and numbers to tiles
 constexpr int NUM_WARPS = 8;
 constexpr int BM = 128, BN = 128, ROWS = 2 * BM;
 constexpr uint32_t HALF_BYTES = 128 * 128;         // 64 dims of 128 rows
@@ -53,12 +53,11 @@ constexpr uint32_t TILE_BYTES = 2 * HALF_BYTES;
 constexpr uint32_t OFF_Q = 0;                      // two tiles
 constexpr uint32_t OFF_K = OFF_Q + 2 * TILE_BYTES; // two stages
 constexpr uint32_t OFF_V = OFF_K + 2 * TILE_BYTES;
-constexpr int SLOTS = 4;                                        // blocks whose exponents and keep bits are kept
+constexpr int SLOTS = 4;                                        // blocks whose scales and keep bits are kept
 constexpr uint32_t OFF_KEEP = OFF_V + 2 * TILE_BYTES;           // [slot][4] bits of the keys that count
 constexpr uint32_t OFF_VS = OFF_KEEP + SLOTS * 16;              // [slot][128] value scales, bf16
-constexpr uint32_t OFF_EXP = OFF_VS + SLOTS * BN * 2;           // [slot] exponent of K
-constexpr uint32_t OFF_TOP = OFF_EXP + SLOTS * 4;               // [2][8 warps] largest key scales of a block
-constexpr uint32_t OFF_QE = OFF_TOP + 2 * 32;                   // [2 pieces][256] exponents of the query rows
+constexpr uint32_t OFF_BACK = OFF_VS + SLOTS * BN * 2;          // [slot][8] what 16 keys' scores are to be multiplied by
+constexpr uint32_t OFF_QE = OFF_BACK + SLOTS * 32;              // [2 pieces][256] the same for the query rows
 constexpr uint32_t OFF_ML = OFF_QE + 2 * ROWS * 4;              // [2 turns][2][128] (m, l) exchanged at a unit's end
 constexpr int PIECES = 4;                                       // piece descriptions kept
 constexpr uint32_t OFF_PIECE = OFF_ML + 4 * BM * 8;             // [PIECES]
@@ -68,7 +67,7 @@ constexpr uint32_t TMEM_COLS = 512;                             // S_0, S_1, O_0
 constexpr uint64_t WAIT_CYCLES = 4000000000ull;                 // ~2 s
 constexpr uint64_t DRAIN_CYCLES = 400000000ull;
 constexpr float RESCALE_THRESHOLD = 8.f;  // O is rescaled when a row's maximum (base 2) grows by more
-constexpr int E_TOP = 9;  // a query row's largest value, a K block's largest scale (or new value), is put at 2^9..2^10
+constexpr int E_TOP = 9;  // a query row's largest value, 16 keys' largest scale (or new value), is put at 2^9..2^10
 constexpr float M_START = -1e30f;  // a reference before any key
 // Exponents below count as this, so that the product of two is no fp32
 // underflow; such scores are 0 to fp32 all the same.
@@ -89,17 +88,16 @@ enum {
   B_VEMPTY = 6,  // [2]
   B_SFULL = 8,   // [2 tiles]
   B_PFULL = 10,  // [2 tiles] 128
-  B_INFO = 12,   // [4 slots] 8: a block's exponents and keep bits
-  B_QFULL = 16,  // 65
+  B_INFO = 12,   // [4 slots] 8: a block's scales and keep bits
+  B_QFULL = 16,  // 9
   B_QFREE = 17,
   B_OFIN = 18,
   B_OFREE = 19,  // 256
   B_ML = 20,     // 256: a row's halves exchanged
   B_PIECE = 21,  // [PIECES] a description is written
-  B_TOP = 25,    // [2] 8: largest key scales of a block
-  B_QE = 27,     // [2] 64: the query rows' exponents
-  B_DRAIN = 29,
-  N_BARS = 30
+  B_QE = 25,     // [2] 8: the query rows' factors
+  B_DRAIN = 27,
+  N_BARS = 28
 };
 
 struct ManyArgs {
@@ -317,22 +315,20 @@ struct Walk {
       end = a.B * a.Hkv * f.chunks;
       return;
     }
-    int sum = 0;
-#pragma unroll 1
-    for (int i = lane; i < a.B; i += 32) {
+    auto cost_of = [&](int i) {
       const Req r = req(i);
-      sum += unit_cost(r) * r.n_chunks;
-    }
-    cut = Kv4Cut(__reduce_add_sync(0xFFFFFFFFu, sum) * a.Hkv, gridDim.x, LEAST);
+      return unit_cost(r) * r.n_chunks * a.Hkv;
+    };
+    const int first = lane < a.B ? cost_of(lane) : 0;
+    int sum = first;
+#pragma unroll 1
+    for (int i = lane + 32; i < a.B; i += 32) sum += cost_of(i);
+    cut = Kv4Cut(__reduce_add_sync(0xFFFFFFFFu, sum), gridDim.x, LEAST);
     cur = (int)blockIdx.x < cut.n ? cut.start(blockIdx.x) : 0;
     end = (int)blockIdx.x < cut.n ? cut.start(blockIdx.x + 1) : 0;
 #pragma unroll 1
     for (int b0 = 0; b0 < a.B; b0 += 32) {
-      int mine = 0;
-      if (b0 + lane < a.B) {
-        const Req r = req(b0 + lane);
-        mine = unit_cost(r) * r.n_chunks * a.Hkv;
-      }
+      const int mine = b0 == 0 ? first : (b0 + lane < a.B ? cost_of(b0 + lane) : 0);
       int inc = mine;
 #pragma unroll
       for (int o = 1; o < 32; o <<= 1) {
@@ -417,9 +413,8 @@ __global__ void __launch_bounds__(THREADS, 1) k_kv4_attn_many(ManyArgs f) {
     for (int i = 0; i < N_BARS; ++i) {
       uint32_t n = 1;
       if (i == B_PFULL || i == B_PFULL + 1) n = 128;
-      if (i < B_KEMPTY || (i >= B_INFO && i < B_INFO + SLOTS) || i == B_TOP || i == B_TOP + 1) n = NUM_WARPS;
-      if (i == B_QE || i == B_QE + 1) n = 64;
-      if (i == B_QFULL) n = 65;
+      if (i < B_KEMPTY || (i >= B_INFO && i < B_INFO + SLOTS) || i == B_QE || i == B_QE + 1) n = NUM_WARPS;
+      if (i == B_QFULL) n = NUM_WARPS + 1;
       if (i == B_OFREE || i == B_ML) n = 256;
       mbar_init(bar(i), n);
     }
@@ -494,8 +489,7 @@ __global__ void __launch_bounds__(THREADS, 1) k_kv4_attn_many(ManyArgs f) {
       mbar_wait_bounded(bar(B_DRAIN), 0, &dummy, DRAIN_CYCLES);
     }
   } else if (warp < 4) {
-    // ---------------- queries, padding rows, the list of cut units ----------------
-    const int qt = tid - 32;  // 0..95
+    // ---------------- pieces, the list of cut units, padding rows ----------------
     uint32_t np = 0;
     if (warp == 1) {
       Walk wk(f);
@@ -529,49 +523,17 @@ __global__ void __launch_bounds__(THREADS, 1) k_kv4_attn_many(ManyArgs f) {
         if (!any) break;
       }
     } else {
-      const int st = qt - 32;  // 0..63
-      for (;; ++np) {
+      for (;; ++np) {  // the rows past the nodes
         if (!warp_wait(bar(B_PIECE + np % PIECES), (np / PIECES) & 1, &s_abort)) break;
-        const Piece pc = *piece(np);
-        if (pc.n == 0) break;
-        if (np > 0 && !warp_wait(bar(B_QFREE), (np - 1) & 1, &s_abort)) break;
-        const int lim = (pc.two ? 2 : 1) * BM * 16;
-        int* qe = reinterpret_cast<int*>(smem + OFF_QE) + (np & 1) * ROWS;
+        const Piece* pc = piece(np);
+        if (pc->n == 0) break;
+        if (pc->s0 != 0 || pc->row0 != 0) continue;
+        const int nn = pc->nn, pad = (a.n_pad - nn) * a.G, bb = pc->b, gh = pc->gh;
 #pragma unroll 1
-        for (int e0 = st; e0 < lim; e0 += 64 * 8) {  // 16 lanes a row
-          uint4 v[8];
-#pragma unroll
-          for (int k = 0; k < 8; ++k) {
-            const int e = e0 + 64 * k, r = e >> 4, ch = e & 15;  // rows [0, 128) are tile 0, the others tile 1
-            v[k] = make_uint4(0, 0, 0, 0);
-            if (r < pc.rows) {
-              const int rr = pc.row0 + r, i = rr / a.G, hh = rr - i * a.G;
-              v[k] = reinterpret_cast<const uint4*>(a.q + (((size_t)pc.b * a.n_pad + i) * a.H + pc.gh * a.G + hh) * HD)[ch];
-            }
-          }
-#pragma unroll
-          for (int k = 0; k < 8; ++k) {
-            const int e = e0 + 64 * k, r = e >> 4, ch = e & 15;
-            uint32_t top = top2(top2(top2(top2(0u, v[k].x), v[k].y), v[k].z), v[k].w);
-#pragma unroll
-            for (int o = 1; o < 16; o <<= 1) top = __vmaxu2(top, __shfl_xor_sync(0xFFFFFFFFu, top, o));
-            const int ex = expo_of(max(top & 0xFFFFu, top >> 16));
-            if (ch == 0) qe[r] = ex;
-            *reinterpret_cast<uint4*>(smem + OFF_Q + (r >> 7) * TILE_BYTES + (ch >> 3) * HALF_BYTES + (r & 127) * 128 +
-                                      (((ch & 7) ^ (r & 7)) << 4)) = to_f16(permute8(v[k]), pow2i(E_TOP - ex));
-          }
-        }
-        mbar_arrive(bar(B_QE + (np & 1)));
-        fence_proxy_async_smem();
-        mbar_arrive(bar(B_QFULL));
-        if (pc.s0 == 0 && pc.row0 == 0) {  // the rows past the nodes
-          const int pad = (a.n_pad - pc.nn) * a.G;
-#pragma unroll 1
-          for (int e = st; e < pad * (HD / 8); e += 64) {
-            const int r = e / (HD / 8), ch = e % (HD / 8), i = pc.nn + r / a.G, hh = r % a.G;
-            reinterpret_cast<uint4*>(a.out + (((size_t)pc.b * a.n_pad + i) * a.H + pc.gh * a.G + hh) * HD)[ch] =
-                make_uint4(0, 0, 0, 0);
-          }
+        for (int e = tid - 64; e < pad * (HD / 8); e += 64) {
+          const int r = e / (HD / 8), ch = e % (HD / 8), i = nn + r / a.G, hh = r % a.G;
+          reinterpret_cast<uint4*>(a.out + (((size_t)bb * a.n_pad + i) * a.H + gh * a.G + hh) * HD)[ch] =
+              make_uint4(0, 0, 0, 0);
         }
       }
     }
@@ -633,23 +595,51 @@ __global__ void __launch_bounds__(THREADS, 1) k_kv4_attn_many(ManyArgs f) {
     auto new_row = [&](int j) {
       return a.k_new && j < pc.nn ? (((size_t)pc.b * a.Hkv + pc.gh) * a.n_pad + j) * HD : no_row;
     };
+    // The piece's queries: a row 16 lanes, 16 rows at a time, times a power of two.
+    auto stage_q = [&](uint32_t np) {
+      float* back = reinterpret_cast<float*>(smem + OFF_QE) + (np & 1) * ROWS;
+      const int ch = lane & 15, passes = (pc.two ? 2 : 1) * BM / 16;
+#pragma unroll 1
+      for (int p0 = 0; p0 < passes; p0 += 4) {
+        uint4 v[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          const int r = 16 * (p0 + k) + 2 * w + (lane >> 4);
+          v[k] = make_uint4(0, 0, 0, 0);
+          if (r < pc.rows) {
+            const int rr = pc.row0 + r, i = rr / a.G, hh = rr - i * a.G;
+            v[k] = reinterpret_cast<const uint4*>(a.q + (((size_t)pc.b * a.n_pad + i) * a.H + pc.gh * a.G + hh) * HD)[ch];
+          }
+        }
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          const int r = 16 * (p0 + k) + 2 * w + (lane >> 4);
+          const uint32_t sign = 0x7FFF7FFFu;
+          uint32_t top = __vmaxu2(__vmaxu2(v[k].x & sign, v[k].y & sign), __vmaxu2(v[k].z & sign, v[k].w & sign));
+#pragma unroll
+          for (int o = 1; o < 16; o <<= 1) top = __vmaxu2(top, __shfl_xor_sync(0xFFFFFFFFu, top, o));
+          const int ex = expo_of(max(top & 0xFFFFu, top >> 16));
+          if (ch == 0) back[r] = pow2i(ex - E_TOP);
+          *reinterpret_cast<uint4*>(smem + OFF_Q + (r >> 7) * TILE_BYTES + (ch >> 3) * HALF_BYTES + (r & 127) * 128 +
+                                    (((ch & 7) ^ (r & 7)) << 4)) = to_f16(permute8(v[k]), pow2i(E_TOP - ex));
+        }
+      }
+    };
     // keys of this warp's 16 that count in block blk
     auto keys_of = [&](int blk) {
       if (blk >= pc.cached) return a.k_new ? pc.nn - 16 * w : 0;
       return (unsigned)id < (unsigned)a.n_pages ? (int)min(16ll, pc.kvl - (long long)blk * BN - 16 * w) : 0;
     };
-    // The largest key scale (magnitude, for the new tokens) of this warp's rows
-    // of block blk, to the other warps.
-    auto announce = [&](int blk, int st) {
+    // The largest key scale (magnitude, for the new tokens) of this warp's keys.
+    auto largest = [&](bool fresh, int left) {
       uint32_t top = 0;
-      if (blk < pc.cached) {
-        const int left = keys_of(blk);  // a key that does not count: whatever stands there
+      if (!fresh) {  // a key that does not count: whatever stands there
         if (rho >= left) sc[0] = 0;
         if (rho + 8 >= left) sc[1] = 0;
         top = top2(top2(0u, sc[0] & 0xFFFFu), sc[1] & 0xFFFFu);
       } else {
         uint32_t tk = 0;
-#pragma unroll 4
+#pragma unroll 1
         for (int e = lane; e < 256; e += 32) {
           const size_t row = new_row(16 * w + (e >> 4));
           if (row == no_row) break;
@@ -658,11 +648,7 @@ __global__ void __launch_bounds__(THREADS, 1) k_kv4_attn_many(ManyArgs f) {
         }
         top = max(tk & 0xFFFFu, tk >> 16);
       }
-      top = __reduce_max_sync(0xFFFFFFFFu, top);
-      if (lane == 0) {
-        reinterpret_cast<uint32_t*>(smem + OFF_TOP)[st * NUM_WARPS + w] = top;
-        mbar_arrive(bar(B_TOP + st));
-      }
+      return __reduce_max_sync(0xFFFFFFFFu, top);
     };
     auto store = [&](uint32_t tile, const uint4 (&x)[2], auto&& convert) {
 #pragma unroll
@@ -677,7 +663,7 @@ __global__ void __launch_bounds__(THREADS, 1) k_kv4_attn_many(ManyArgs f) {
       }
     };
     auto store_new = [&](uint32_t tile, const __nv_bfloat16* src, auto&& convert) {  // the new rows, zeros past them
-#pragma unroll 4
+#pragma unroll 2
       for (int e = lane; e < 256; e += 32) {
         const int j = 16 * w + (e >> 4), ch = e & 15;
         const size_t row = new_row(j);
@@ -703,20 +689,23 @@ __global__ void __launch_bounds__(THREADS, 1) k_kv4_attn_many(ManyArgs f) {
         fetch_k(pc.s0);
         fetch_v(pc.s0);
       }
-      announce(pc.s0, nb & 1);
+      if (np > 0 && !(ok = warp_wait(bar(B_QFREE), (np - 1) & 1, &s_abort))) break;
+      stage_q(np);
+      fence_proxy_async_smem();
+      __syncwarp();
+      if (lane == 0) {
+        mbar_arrive(bar(B_QE + (np & 1)));
+        mbar_arrive(bar(B_QFULL));
+      }
       for (int blk = pc.s0; blk < s1; ++blk, ++nb) {
         const int st = nb & 1, slot = nb % SLOTS;
         const bool fresh = blk >= pc.cached, more = blk + 1 < s1 && blk + 1 < pc.cached;
-        if (!(ok = warp_wait(bar(B_TOP + st), (nb >> 1) & 1, &s_abort))) break;
-        const uint4 t4 = *reinterpret_cast<const uint4*>(smem + OFF_TOP + st * 32);
-        const uint4 t8 = *reinterpret_cast<const uint4*>(smem + OFF_TOP + st * 32 + 16);
-        const int ek = expo_of(max(max(max(t4.x, t4.y), max(t4.z, t4.w)), max(max(t8.x, t8.y), max(t8.z, t8.w))));
+        const int left = keys_of(blk), ek = expo_of(largest(fresh, left));
         // the slot's last readers are done (the V stage of three blocks ago was waited for)
         if (lane == 0) {
-          const int left = keys_of(blk);
           reinterpret_cast<uint16_t*>(smem + OFF_KEEP + slot * 16)[w] =
               (uint16_t)(left >= 16 ? 0xFFFFu : (left <= 0 ? 0u : (1u << left) - 1u));
-          if (w == 0) reinterpret_cast<int*>(smem + OFF_EXP)[slot] = ek;
+          reinterpret_cast<float*>(smem + OFF_BACK)[slot * NUM_WARPS + w] = pow2i(ek - E_TOP);
           if (!fresh && (unsigned)id >= (unsigned)a.n_pages && (long long)blk * BN + 16 * w < pc.kvl)
             fc_flag(FC_ERR_WORD(a.err), FC_EBIT_INVALID);
         }
@@ -753,7 +742,6 @@ __global__ void __launch_bounds__(THREADS, 1) k_kv4_attn_many(ManyArgs f) {
         else store_new(OFF_V + st * TILE_BYTES, a.v_new, [](const uint4& v) { return v; });
         done(B_VFULL + st);
         if (more) fetch_v(blk + 1);
-        if (blk + 1 < s1) announce(blk + 1, st ^ 1);
       }
     }
   } else {
@@ -772,15 +760,13 @@ __global__ void __launch_bounds__(THREADS, 1) k_kv4_attn_many(ManyArgs f) {
       if (n == 0) break;
       float m = M_START, l = 0.f;  // m: the reference
       if (!(ok = warp_wait(bar(B_QE + (np & 1)), (np >> 1) & 1, &s_abort))) break;
-      // scores: S times 2^(qe - E_TOP) 2^(ek - E_TOP) and the softmax's scale
-      const float c_row =
-          a.scale_log2 * pow2i(reinterpret_cast<const int*>(smem + OFF_QE)[(np & 1) * ROWS + row_of(pc)] - E_TOP);
+      const float c_row = a.scale_log2 * reinterpret_cast<const float*>(smem + OFF_QE)[(np & 1) * ROWS + row_of(pc)];
       const int every = pc->two ? 1 : 2, first = pc->two ? 0 : x, n_cached = pc->cached - pc->s0;
 #pragma unroll 1
       for (int j = first; j < n; j += every, ++t) {
         const int slot = (nb + j) % SLOTS;
         if (!(ok = warp_wait(bar(B_INFO + slot), ((nb + j) / SLOTS) & 1, &s_abort))) break;
-        const float cz = c_row * pow2i(reinterpret_cast<const int*>(smem + OFF_EXP)[slot] - E_TOP);
+        const float2* back = reinterpret_cast<const float2*>(smem + OFF_BACK) + slot * (NUM_WARPS / 2);
         const uint32_t* keep = reinterpret_cast<const uint32_t*>(smem + OFF_KEEP) + slot * 4;
         const bool masked = j >= n_cached || (keep[0] & keep[1] & keep[2] & keep[3]) != 0xFFFFFFFFu;  // in all rows alike
         if (!(ok = warp_wait(bar(B_SFULL + x), t & 1, &s_abort))) break;
@@ -817,25 +803,30 @@ __global__ void __launch_bounds__(THREADS, 1) k_kv4_attn_many(ManyArgs f) {
         // The row's scores come 32 at a time, the next in flight meanwhile; once
         // for the maximum, once for P.
         uint32_t sa[32], sb[32];
-        float pm[2] = {-INFINITY, -INFINITY};
-        auto largest = [&](const uint32_t (&sv)[32]) {
+        float top = -INFINITY;
+        auto largest = [&](int q, const uint32_t (&sv)[32]) {
+          const float2 bk = back[q];  // of its two runs of 16 keys
+          float p0 = -INFINITY, p1 = -INFINITY;
 #pragma unroll
-          for (int u = 0; u < 32; u += 2)
-            pm[(u >> 1) & 1] = max3(pm[(u >> 1) & 1], __uint_as_float(sv[u]), __uint_as_float(sv[u + 1]));
+          for (int u = 0; u < 16; u += 2) {
+            p0 = max3(p0, __uint_as_float(sv[u]), __uint_as_float(sv[u + 1]));
+            p1 = max3(p1, __uint_as_float(sv[16 + u]), __uint_as_float(sv[17 + u]));
+          }
+          top = max3(top, p0 * bk.x, p1 * bk.y);
         };
         tmem_ld32(tS, sa);
         tc_wait_ld();
 #pragma unroll 1
         for (int q = 0; q < 4; q += 2) {
           tmem_ld32(tS + (q + 1) * 32, sb);
-          largest(sa);
+          largest(q, sa);
           tc_wait_ld();
           tmem_ld32(tS + ((q + 2) & 3) * 32, sa);  // the last one: P's first
-          largest(sb);
+          largest(q + 1, sb);
           tc_wait_ld();
         }
         {
-          const float top = fmaxf(pm[0], pm[1]) * cz;
+          top *= c_row;
           if (__any_sync(0xFFFFFFFFu, top > m + RESCALE_THRESHOLD)) {
             const float m_new = top > m + RESCALE_THRESHOLD ? top : m, alpha = exp2_fast(m - m_new);
             l *= alpha;
@@ -853,13 +844,16 @@ __global__ void __launch_bounds__(THREADS, 1) k_kv4_attn_many(ManyArgs f) {
           }
         }
         uint64_t sum[2] = {0ull, 0ull};
-        const uint64_t c2 = f2_pack(cz, cz), neg = f2_pack(-m, -m);
+        const uint64_t neg = f2_pack(-m, -m);
         const uint4* vs8 = reinterpret_cast<const uint4*>(smem + OFF_VS + slot * BN * 2);
         auto weigh = [&](int q, const uint32_t (&sv)[32]) {  // over scores already read
           uint32_t pk[16];
+          const float2 bk = back[q];
 #pragma unroll
           for (int g = 0; g < 4; ++g) {  // 8 keys, their value scales in one load
             const uint4 v4 = vs8[q * 4 + g];
+            const float cz = c_row * (g < 2 ? bk.x : bk.y);
+            const uint64_t c2 = f2_pack(cz, cz);
 #pragma unroll
             for (int u = 0; u < 4; ++u) {
               const int k = 8 * g + 2 * u;
