@@ -550,7 +550,7 @@ __global__ void __launch_bounds__(THREADS, 1) k_kv4_attn_many(ManyArgs f) {
       dst[i] = swap * HALF_BYTES + (16 * w + rho) * 128 + ((((c & 1) * 4 + (i ^ (2 * swap))) ^ rho) << 4);
     Piece pc = {};
     uint4 kr[2], vr[2];
-    uint32_t sc[2] = {0u, 0u};  // scales: K in the low half, V in the high
+    uint32_t ksc[2] = {0u, 0u}, vsc[2] = {0u, 0u};  // scales, bf16 bits (apart, so that nothing waits for their loads)
     int id = -1, id_next = -1, id_ahead = -1;  // pages: of the block fetched, of the next, of the one to ask for
     uint32_t nb = 0;
     bool ok = true;
@@ -571,8 +571,10 @@ __global__ void __launch_bounds__(THREADS, 1) k_kv4_attn_many(ManyArgs f) {
       kr[1] = src[32];
       const uint16_t* ks = reinterpret_cast<const uint16_t*>(a.ks) + (uint64_t)run * 16u + rho;
       const uint16_t* vs = reinterpret_cast<const uint16_t*>(a.vs) + (uint64_t)run * 16u + rho;
-      sc[0] = ks[0] | ((uint32_t)vs[0] << 16);
-      sc[1] = ks[8] | ((uint32_t)vs[8] << 16);
+      ksc[0] = ks[0];
+      ksc[1] = ks[8];
+      vsc[0] = vs[0];
+      vsc[1] = vs[8];
     };
     auto fetch_v = [&](int blk) {
       const uint32_t run = (unsigned)id < (unsigned)a.n_pages ? run_of(id, blk) : 0u;
@@ -634,9 +636,10 @@ __global__ void __launch_bounds__(THREADS, 1) k_kv4_attn_many(ManyArgs f) {
     auto largest = [&](bool fresh, int left) {
       uint32_t top = 0;
       if (!fresh) {  // a key that does not count: whatever stands there
-        if (rho >= left) sc[0] = 0;
-        if (rho + 8 >= left) sc[1] = 0;
-        top = top2(top2(0u, sc[0] & 0xFFFFu), sc[1] & 0xFFFFu);
+        if (rho >= left) ksc[0] = vsc[0] = 0;
+        if (rho + 8 >= left) ksc[1] = vsc[1] = 0;
+        top = top2(0u, ksc[0] | (ksc[1] << 16));
+        top = max(top & 0xFFFFu, top >> 16);
       } else {
         uint32_t tk = 0;
 #pragma unroll 1
@@ -711,8 +714,8 @@ __global__ void __launch_bounds__(THREADS, 1) k_kv4_attn_many(ManyArgs f) {
         }
         if (c == 0) {
           uint16_t* vs = reinterpret_cast<uint16_t*>(smem + OFF_VS) + slot * BN + 16 * w + rho;
-          vs[0] = fresh ? 0x3F80 : (uint16_t)(sc[0] >> 16);
-          vs[8] = fresh ? 0x3F80 : (uint16_t)(sc[1] >> 16);
+          vs[0] = fresh ? 0x3F80 : (uint16_t)vsc[0];
+          vs[8] = fresh ? 0x3F80 : (uint16_t)vsc[1];
         }
         __syncwarp();
         if (lane == 0) mbar_arrive(bar(B_INFO + slot));
@@ -722,7 +725,7 @@ __global__ void __launch_bounds__(THREADS, 1) k_kv4_attn_many(ManyArgs f) {
           uint32_t s2[2], less24[2];
 #pragma unroll
           for (int p = 0; p < 2; ++p) {
-            const float s = lo_f(sc[p]) * by;
+            const float s = lo_f(ksc[p]) * by;
             s2[p] = pack_f16x2(s, s);
             less24[p] = pack_f16x2(-24.f * s, -24.f * s);
           }
