@@ -12,6 +12,7 @@
 // lane's part of x is 8 values in a row, one 16-byte load for two k-steps, and
 // no k-step crosses a group of 32.  Tiles run over k first.
 #include <algorithm>
+#include <atomic>
 
 #include "fc_common.cuh"
 
@@ -20,7 +21,8 @@ namespace {
 constexpr int TK = 64;           // k a tile
 constexpr int TN = 16;           // columns a tile
 constexpr int TILE_BYTES = 512;
-constexpr int MV_WARPS = 8;
+constexpr int MAX_WARPS = 8;     // a CTA
+constexpr int FILL = 152 * 8;    // warps that keep HBM busy
 
 // (k in the tile, column in the tile) of element e (0 or 1) of register i of
 // k-step w in lane (g, t)
@@ -96,16 +98,94 @@ __device__ __forceinline__ uint32_t two(uint32_t w, int i) { return ((w >> (4 * 
 
 constexpr uint32_t MINUS_136 = 0xC308C308u;  // two bf16 values
 
-// A CTA takes MT tiles of columns, its warps every MV_WARPS-th tile of k; the
-// warps' sums meet in shared memory.  NT: 8-row tiles of x.  STEPS: k-steps
-// that share a scale (the group, or the whole tile).
+__device__ __forceinline__ void cp_async16(uint32_t dst, const void* src) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;\n" ::"r"(dst), "l"(src) : "memory");
+}
+__device__ __forceinline__ void cp_async4(uint32_t dst, const void* src) {
+  asm volatile("cp.async.ca.shared.global [%0], [%1], 4;\n" ::"r"(dst), "l"(src) : "memory");
+}
+__device__ __forceinline__ void cp_async_commit() { asm volatile("cp.async.commit_group;\n" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void cp_async_wait() {
+  asm volatile("cp.async.wait_group %0;\n" ::"n"(N) : "memory");
+}
+// The weights' read bounds this: 4.1 to 4.5 bits a weight, each used once;
+// next to it the integer pipe, which turns a word's 8 numbers into operands in
+// 7 instructions and can spare few others (half of one per weight byte read at
+// full bandwidth), so the loop's addresses are pointers that advance, its
+// stages unrolled, and rows and tiles past the end are read from valid places
+// instead of being tested for.
+// A warp takes MT tiles of columns (which share the rows of x that it loads)
+// and every ks-th tile of k, seven tiles in flight by asynchronous copies, x
+// AHEAD tiles ahead in registers; with ks = 1 a sum never leaves its warp, else
+// the ks warps' sums meet in shared memory.  NT: 8-row tiles of x.  STEPS:
+// k-steps that share a scale (the group, or the whole tile).
+constexpr int STAGES = 8;
+// codes of MT tiles, then the scales [group][MT * TN]
+__host__ __device__ constexpr int stage_bytes(int MT, int STEPS) { return MT * TILE_BYTES + MT * TN * 2 * (4 / STEPS); }
+
 template <int MT, int NT, int STEPS>
-__global__ void __launch_bounds__(MV_WARPS * 32) k_w4_matvec(const uint4* __restrict__ x, const uint4* __restrict__ codes,
-                                                             const __nv_bfloat16* __restrict__ scale, int M, int K,
-                                                             int N, int gshift, __nv_bfloat16* __restrict__ y) {
-  __shared__ float s_sum[MV_WARPS][MT * TN][NT * 8 + 1];
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
-  const int kt = K / TK, n0 = blockIdx.x * (MT * TN), n_tiles = (N + TN - 1) / TN;
+__global__ void __launch_bounds__(MAX_WARPS * 32) k_w4_matvec(const uint4* __restrict__ x, const uint4* __restrict__ codes,
+                                                              const uint16_t* __restrict__ scale, int M, int K, int N,
+                                                              int gshift, int ks, __nv_bfloat16* __restrict__ y) {
+  extern __shared__ __align__(16) unsigned char smem[];  // rings; then the sums
+  constexpr int GROUPS = 4 / STEPS, OFF_SC = MT * TILE_BYTES, STAGE_BYTES = stage_bytes(MT, STEPS);
+  constexpr int AHEAD = 4;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3, warps = blockDim.x >> 5;
+  const int kt = K / TK, part = warp % ks, tile0 = (blockIdx.x * (warps / ks) + warp / ks) * MT;
+  const int n_tiles = (N + TN - 1) / TN;
+  const uint32_t ring = smem_u32(smem) + warp * (STAGES * STAGE_BYTES);
+  const unsigned char* ring_p = smem + warp * (STAGES * STAGE_BYTES);
+  const int n_it = tile0 < n_tiles && part < kt ? (kt - part + ks - 1) / ks : 0;
+  // ---- what a step fetches: this lane's part of MT tiles and of their scales
+  const uint4* src[MT];
+#pragma unroll
+  for (int m = 0; m < MT; ++m) src[m] = codes + ((size_t)min(tile0 + m, n_tiles - 1) * kt + part) * 32 + lane;
+  const int sq = lane / (8 * MT), sc_c = 2 * (lane % (8 * MT)), sc_col = tile0 * TN + sc_c;  // two columns of group sq
+  const bool sc_lane = lane < 8 * MT * GROUPS && sc_col < N;
+  const uint32_t sc_dst = ring + OFF_SC + (sq * MT * TN + sc_c) * 2;
+  const uint16_t* sc_src = scale + sc_col;
+  uint32_t sc_k = part * TK + sq * STEPS * 16;
+  int to_fetch = n_it;
+  auto issue = [&](int stage) {
+    if (to_fetch > 0) {
+#pragma unroll
+      for (int m = 0; m < MT; ++m) {
+        cp_async16(ring + stage * STAGE_BYTES + m * TILE_BYTES + lane * 16, src[m]);
+        src[m] += ks * 32;
+      }
+      if (sc_lane) {
+        const uint16_t* sp = sc_src + (uint64_t)(sc_k >> gshift) * (uint32_t)N;
+        if (N & 1) {  // rows of odd length: two columns are not one aligned word
+          const uint32_t lo = sp[0], hi = sc_col + 1 < N ? sp[1] : 0u;
+          asm volatile("st.shared.b32 [%0], %1;" ::"r"(sc_dst + stage * STAGE_BYTES), "r"(lo | (hi << 16)) : "memory");
+        } else {
+          cp_async4(sc_dst + stage * STAGE_BYTES, sp);
+        }
+      }
+      sc_k += ks * TK;
+      --to_fetch;
+    }
+    cp_async_commit();
+  };
+#pragma unroll
+  for (int i = 0; i < STAGES - 1; ++i) issue(i);
+  // ---- x: rows past M repeat row 0 (their sums are not stored); past the end the last tile is read again
+  const uint4* xp[NT];
+#pragma unroll
+  for (int n = 0; n < NT; ++n) xp[n] = x + ((size_t)(n * 8 + g < M ? n * 8 + g : 0) * K + part * TK) / 8 + t;
+  int x_left = n_it;
+  uint4 xv[AHEAD][NT][2];
+  auto load_x = [&](uint4 (&v)[NT][2]) {
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+      v[n][0] = xp[n][0];
+      v[n][1] = xp[n][4];
+    }
+    const int step = --x_left > 0 ? ks * (TK / 8) : 0;
+#pragma unroll
+    for (int n = 0; n < NT; ++n) xp[n] += step;
+  };
   float acc[MT][NT][4];
 #pragma unroll
   for (int m = 0; m < MT; ++m)
@@ -113,71 +193,94 @@ __global__ void __launch_bounds__(MV_WARPS * 32) k_w4_matvec(const uint4* __rest
     for (int n = 0; n < NT; ++n)
 #pragma unroll
       for (int i = 0; i < 4; ++i) acc[m][n][i] = 0.f;
-#pragma unroll 2
-  for (int j = warp; j < kt; j += MV_WARPS) {
-    uint4 cw[MT];
+  if (n_it > 0) {
 #pragma unroll
-    for (int m = 0; m < MT; ++m) {
-      const int tile = blockIdx.x * MT + m;
-      cw[m] = tile < n_tiles ? codes[((size_t)tile * kt + j) * 32 + lane] : make_uint4(0, 0, 0, 0);
-    }
-    uint4 xv[NT][2];
+    for (int i = 0; i < AHEAD; ++i) load_x(xv[i]);
+  }
+  auto step = [&](int stage, uint4 (&xr)[NT][2]) {
+    uint4 cw[MT];
+    cp_async_wait<STAGES - 2>();
+    __syncwarp();
+    const unsigned char* st = ring_p + stage * STAGE_BYTES;
+#pragma unroll
+    for (int m = 0; m < MT; ++m) cw[m] = *reinterpret_cast<const uint4*>(st + m * TILE_BYTES + lane * 16);
+    uint32_t sc[MT][GROUPS][2];
+    const uint16_t* sp = reinterpret_cast<const uint16_t*>(st + OFF_SC) + g;
+#pragma unroll
+    for (int m = 0; m < MT; ++m)
+#pragma unroll
+      for (int q = 0; q < GROUPS; ++q)
+#pragma unroll
+        for (int i = 0; i < 2; ++i) sc[m][q][i] = sp[q * MT * TN + m * TN + 8 * i];
+    issue((stage + STAGES - 1) % STAGES);
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
-      const int row = n * 8 + g;
 #pragma unroll
-      for (int p = 0; p < 2; ++p)
-        xv[n][p] = row < M ? x[((size_t)row * K + j * TK + 32 * p) / 8 + t] : make_uint4(0, 0, 0, 0);
-    }
+      for (int q = 0; q < GROUPS; ++q) {
+        float off[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int w0 = 0; w0 < 4; w0 += STEPS) {
-      float sc[MT][2];
-      const size_t grp = (size_t)((j * TK + w0 * 16) >> gshift) * N;
-#pragma unroll
-      for (int m = 0; m < MT; ++m)
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-          const int n = n0 + m * TN + g + 8 * i;
-          sc[m][i] = n < N ? __bfloat162float(scale[grp + n]) : 0.f;
-        }
-#pragma unroll
-      for (int n = 0; n < NT; ++n) {
-        const float zero[4] = {0.f, 0.f, 0.f, 0.f};
-        float off[4];
-#pragma unroll
-        for (int w = w0; w < w0 + STEPS; ++w) {
-          const uint32_t* xw = &xv[n][w >> 1].x;
-          if (w == w0) mma_bf16(off, MINUS_136, MINUS_136, MINUS_136, MINUS_136, xw[2 * (w & 1)], xw[2 * (w & 1) + 1], zero);
-          else mma_bf16(off, MINUS_136, MINUS_136, MINUS_136, MINUS_136, xw[2 * (w & 1)], xw[2 * (w & 1) + 1], off);
+        for (int w = q * STEPS; w < (q + 1) * STEPS; ++w) {
+          const uint32_t* xw = &xr[n][w >> 1].x;
+          mma_bf16(off, MINUS_136, MINUS_136, MINUS_136, MINUS_136, xw[2 * (w & 1)], xw[2 * (w & 1) + 1], off);
         }
 #pragma unroll
         for (int m = 0; m < MT; ++m) {
           float d[4] = {off[0], off[1], off[2], off[3]};
           const uint32_t* c = &cw[m].x;
 #pragma unroll
-          for (int w = w0; w < w0 + STEPS; ++w) {
-            const uint32_t* xw = &xv[n][w >> 1].x;
-            mma_bf16(d, two(c[w], 0), two(c[w], 1), two(c[w], 2), two(c[w], 3), xw[2 * (w & 1)], xw[2 * (w & 1) + 1], d);
+          for (int w = q * STEPS; w < (q + 1) * STEPS; ++w) {
+            const uint32_t* xw = &xr[n][w >> 1].x;
+            mma_bf16(d, two(c[w], 0), two(c[w], 1), two(c[w], 2), two(c[w], 3), xw[2 * (w & 1)], xw[2 * (w & 1) + 1],
+                     w == q * STEPS ? off : d);
           }
 #pragma unroll
-          for (int i = 0; i < 4; ++i) acc[m][n][i] = fmaf(sc[m][i >> 1], d[i], acc[m][n][i]);
+          for (int i = 0; i < 4; ++i)
+            acc[m][n][i] = fmaf(__uint_as_float(sc[m][q][i >> 1] << 16), d[i], acc[m][n][i]);
         }
       }
     }
+    load_x(xr);
+  };
+#pragma unroll 1
+  for (int it = 0; it < n_it; it += STAGES) {
+#pragma unroll
+    for (int i = 0; i < STAGES; ++i) {
+      if (it + i >= n_it) break;
+      step(i, xv[i % AHEAD]);
+    }
   }
+  cp_async_wait<0>();
+  if (ks == 1) {
+#pragma unroll
+    for (int m = 0; m < MT; ++m)
+#pragma unroll
+      for (int n = 0; n < NT; ++n)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int row = n * 8 + 2 * t + (i & 1), col = (tile0 + m) * TN + g + 8 * (i >> 1);
+          if (row < M && col < N) y[(size_t)row * N + col] = __float2bfloat16_rn(acc[m][n][i]);
+        }
+    return;
+  }
+  __syncthreads();  // every warp is done with its ring
+  constexpr int PITCH = NT * 8 + 1;
+  float* sums = reinterpret_cast<float*>(smem);  // [warps][MT * TN][PITCH]
 #pragma unroll
   for (int m = 0; m < MT; ++m)
 #pragma unroll
     for (int n = 0; n < NT; ++n)
 #pragma unroll
-      for (int i = 0; i < 4; ++i) s_sum[warp][m * TN + g + 8 * (i >> 1)][n * 8 + 2 * t + (i & 1)] = acc[m][n][i];
+      for (int i = 0; i < 4; ++i)
+        sums[(warp * (MT * TN) + m * TN + g + 8 * (i >> 1)) * PITCH + n * 8 + 2 * t + (i & 1)] = acc[m][n][i];
   __syncthreads();
-  for (int e = threadIdx.x; e < MT * TN * M; e += MV_WARPS * 32) {
-    const int row = e / (MT * TN), c = e - row * (MT * TN);
+  const int cols = (warps / ks) * MT * TN, n0 = blockIdx.x * cols;
+#pragma unroll 1
+  for (int e = threadIdx.x; e < cols * M; e += blockDim.x) {
+    const int row = e / cols, c = e - row * cols;
     if (n0 + c >= N) continue;
+    const int w0 = c / (MT * TN) * ks, cc = c % (MT * TN);
     float sum = 0.f;
-#pragma unroll
-    for (int w = 0; w < MV_WARPS; ++w) sum += s_sum[w][c][row];
+    for (int w = 0; w < ks; ++w) sum += sums[((w0 + w) * (MT * TN) + cc) * PITCH + row];
     y[(size_t)row * N + n0 + c] = __float2bfloat16_rn(sum);
   }
 }
@@ -188,22 +291,39 @@ bool shape_ok(int K, int N, int group) {
   return K >= TK && K % TK == 0 && N >= 1 && (group == 32 || group == 64 || group == 128) && K % group == 0;
 }
 
+template <int MT, int NT, int STEPS>
+fc_status launch(const void* x, const void* codes, const void* scale, int M, int K, int N, int gshift, void* y,
+                 cudaStream_t s) {
+  constexpr size_t RING = (size_t)STAGES * stage_bytes(MT, STEPS);           // a warp
+  constexpr size_t SUMS = (size_t)MT * TN * (NT * 8 + 1) * sizeof(float);
+  constexpr size_t SMEM = RING > SUMS ? RING : SUMS;
+  static std::atomic<unsigned long long> done{0};
+  const fc_status st = fc_once_per_device(done, [](int) {
+    return fc_cuda_status(cudaFuncSetAttribute(k_w4_matvec<MT, NT, STEPS>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                               (int)(MAX_WARPS * SMEM)));
+  });
+  if (st != FC_OK) return st;
+  // Warps enough for the GPU (FILL): split k while column tiles alone are too
+  // few and every part keeps two tiles.
+  const int tasks = (int)(((long long)N + MT * TN - 1) / (MT * TN)), kt = K / TK;
+  int ks = 1;
+  while (ks < MAX_WARPS && (long long)tasks * ks < FILL && kt >= 4 * ks) ks *= 2;
+  const int warps = std::max(ks, 4), per = warps / ks;  // small CTAs: they spread over the SMs evenly
+  k_w4_matvec<MT, NT, STEPS><<<(unsigned)((tasks + per - 1) / per), warps * 32, warps * SMEM, s>>>(
+      static_cast<const uint4*>(x), static_cast<const uint4*>(codes), static_cast<const uint16_t*>(scale), M, K, N,
+      gshift, ks, static_cast<__nv_bfloat16*>(y));
+  return FC_CHECK_LAUNCH();
+}
+
 template <int MT>
-void launch(const void* x, const void* codes, const void* scale, int M, int K, int N, int group, void* y,
-            cudaStream_t s) {
-  const unsigned grid = (unsigned)(((long long)N + MT * TN - 1) / (MT * TN));
-  auto go = [&](auto kernel) {
-    kernel<<<grid, MV_WARPS * 32, 0, s>>>(static_cast<const uint4*>(x), static_cast<const uint4*>(codes),
-                                          static_cast<const __nv_bfloat16*>(scale), M, K, N,
-                                          group == 32 ? 5 : (group == 64 ? 6 : 7), static_cast<__nv_bfloat16*>(y));
-  };
-  if (M <= 8) {
-    if (group == 32) go(k_w4_matvec<MT, 1, 2>);
-    else go(k_w4_matvec<MT, 1, 4>);
-  } else {
-    if (group == 32) go(k_w4_matvec<MT, 2, 2>);
-    else go(k_w4_matvec<MT, 2, 4>);
-  }
+fc_status launch_rows(const void* x, const void* codes, const void* scale, int M, int K, int N, int group, void* y,
+                      cudaStream_t s) {
+  const int gshift = group == 32 ? 5 : (group == 64 ? 6 : 7);
+  if (M <= 8)
+    return group == 32 ? launch<MT, 1, 2>(x, codes, scale, M, K, N, gshift, y, s)
+                       : launch<MT, 1, 4>(x, codes, scale, M, K, N, gshift, y, s);
+  return group == 32 ? launch<MT, 2, 2>(x, codes, scale, M, K, N, gshift, y, s)
+                     : launch<MT, 2, 4>(x, codes, scale, M, K, N, gshift, y, s);
 }
 
 }  // namespace
@@ -241,7 +361,8 @@ extern "C" fc_status fc_w4_matvec(const void* d_x, const void* d_codes, const vo
       !aligned(d_y, 2))
     return FC_ERR_INVALID_ARG;
   cudaStream_t s = static_cast<cudaStream_t>(stream);
-  if (N <= 152 * TN) launch<1>(d_x, d_codes, d_scale, M, K, N, group, d_y, s);
-  else launch<2>(d_x, d_codes, d_scale, M, K, N, group, d_y, s);
-  return FC_CHECK_LAUNCH();
+  // Two column tiles a warp halve what it loads of x; they take a wide output
+  // (else a warp's tiles alone leave the GPU short of warps).
+  if (N <= 152 * TN * 8) return launch_rows<1>(d_x, d_codes, d_scale, M, K, N, group, d_y, s);
+  return launch_rows<2>(d_x, d_codes, d_scale, M, K, N, group, d_y, s);
 }

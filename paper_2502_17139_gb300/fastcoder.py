@@ -192,8 +192,14 @@ def _load():
 LIB = _load()
 
 
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)  # torch.cuda.current_stream() takes 3 us
+_device = getattr(torch._C, "_cuda_getDevice", None)
+
+
 def _stream():
-    return C.c_void_p(torch.cuda.current_stream().cuda_stream)
+    if _raw_stream is None or _device is None:
+        return C.c_void_p(torch.cuda.current_stream().cuda_stream)
+    return C.c_void_p(_raw_stream(_device()))
 
 
 def _ptr(t):
