@@ -723,7 +723,8 @@ fc_status fc_kv_pages_release(const int32_t* d_kv_len, const int32_t* d_keep, in
  * likewise in d_v, so that parts of a fused projection's rows and head-major
  * tensors are read where they are.  bf16, 16-byte aligned, strides multiples
  * of 8 elements.  A slot or a d_src entry out of range records
- * FC_ERR_INVALID_ARG and its row is left out.
+ * FC_ERR_INVALID_ARG and its row is left out.  rows * Hkv <= 2^30 here and in
+ * fc_kv4_read.
  */
 fc_status fc_kv4_write(const fc_kv4_cache* cache, const void* d_k, const void* d_v, int n_seq, int n_per_seq,
                        int64_t seq_stride, int64_t row_stride, int64_t head_stride, const int32_t* d_src,

@@ -224,15 +224,21 @@ __global__ void __launch_bounds__(PL_THREADS) k_pages_release(const int32_t* kv_
 // ---------------------------------------------------------------------------
 // Write and read.
 // ---------------------------------------------------------------------------
-constexpr int WR_THREADS = 128;
+constexpr int WR_THREADS = 128, WR_CTAS = 16;  // all of an SM's 2048 threads: what is in flight hides HBM's latency
 constexpr int WR_LANES = HD / 8;                     // lanes a row: 8 dimensions (16 bytes of bf16) each
 constexpr int WR_GROUPS = WR_THREADS / WR_LANES;     // rows in flight a CTA
+
+constexpr long long MAX_ITEMS = 1ll << 30;           // rows times heads a call (their counters are 32-bit)
 
 struct KvRows {
   const __nv_bfloat16 *k, *v;
   int n_per_seq, n_src;
+  bool one_seq;  // the rows are one sequence: no division
   long long seq_stride, row_stride, head_stride;
 };
+
+__device__ __forceinline__ float lo_f(uint32_t w) { return __uint_as_float(w << 16); }
+__device__ __forceinline__ float hi_f(uint32_t w) { return __uint_as_float(w & 0xFFFF0000u); }
 
 // 8 values of a row (4 words of two) to 8 numbers of 4 bits, given the row's
 // scale.  x * (1 / s) is rounded onto a grid of 2^-11 before the rounding to
@@ -240,72 +246,100 @@ struct KvRows {
 // (X, S in 128..255) the quotient's distance from a tie (2k+1)/2 is
 // |2X 2^(a-b) - (2k+1) S| / 2S, and near a tie of at most 7.1 a - b >= -2, so
 // the numerator is 0 or at least 1/2 and the distance 0 or above 2^-10.  The
-// grid holds every tie and moves a value by at most 2^-12, so this is
-// rint(x / s) exactly, in three operations where a division takes about ten.
+// grid holds every tie and moves a value by at most 2^-12, the reciprocal is
+// good to 2^-22, so this is rint(x / s) exactly, in two operations (the second
+// adds what rounds to whole numbers, less the grid's constant) where a division
+// takes about ten.  A byte's two numbers are put together as
+// 16 hi + lo in fp32 too (the integer pipe has half the rate), and taken from
+// the sum's lowest eight bits.
 __device__ __forceinline__ uint32_t quantise8(const uint4& x, float s) {
   const uint32_t w[4] = {x.x, x.y, x.z, x.w};
-  uint32_t out = 0;
   if (s >= 0x1p-100f && s <= 0x1p100f) {
-    const float r = __frcp_rn(s);
-    constexpr float GRID = 6144.f;             // 1.5 * 2^12: neighbours are 2^-11 apart
-    constexpr float WHOLE = 12582912.f + 8.f;  // 1.5 * 2^23: neighbours are 1 apart; and the bias
+    float r;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(s));
+    constexpr float GRID = 6144.f;       // 1.5 * 2^12: neighbours are 2^-11 apart
+    constexpr float WHOLE = 12582912.f;  // 1.5 * 2^23: neighbours are 1 apart, the low byte is 0
+    uint32_t byte[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      const float lo = __uint_as_float(w[i] << 16), hi = __uint_as_float(w[i] & 0xFFFF0000u);
-      const float a = __fadd_rn(__fadd_rn(__fmaf_rn(lo, r, GRID), -GRID), WHOLE);
-      const float b = __fadd_rn(__fadd_rn(__fmaf_rn(hi, r, GRID), -GRID), WHOLE);
-      out |= (__float_as_uint(a) & 15u) << (8 * i);
-      out |= (__float_as_uint(b) & 15u) << (8 * i + 4);
+      const float lo = __fadd_rn(__fmaf_rn(lo_f(w[i]), r, GRID), WHOLE + 8.f - GRID);
+      const float hi = __fadd_rn(__fmaf_rn(hi_f(w[i]), r, GRID), WHOLE + 8.f - GRID);
+      byte[i] = __float_as_uint(__fmaf_rn(__fadd_rn(hi, -WHOLE), 16.f, lo));
     }
-  } else {
+    return __byte_perm(__byte_perm(byte[0], byte[1], 0x0040), __byte_perm(byte[2], byte[3], 0x0040), 0x5410);
+  }
+  uint32_t out = 0;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const float lo = __uint_as_float(w[i] << 16), hi = __uint_as_float(w[i] & 0xFFFF0000u);
-      const float a = s > 0.f ? fminf(fmaxf(rintf(__fdiv_rn(lo, s)), -7.f), 7.f) : 0.f;
-      const float b = s > 0.f ? fminf(fmaxf(rintf(__fdiv_rn(hi, s)), -7.f), 7.f) : 0.f;
-      out |= (uint32_t)((int)a + 8) << (8 * i);
-      out |= (uint32_t)((int)b + 8) << (8 * i + 4);
-    }
+  for (int i = 0; i < 4; ++i) {
+    const float a = s > 0.f ? fminf(fmaxf(rintf(__fdiv_rn(lo_f(w[i]), s)), -7.f), 7.f) : 0.f;
+    const float b = s > 0.f ? fminf(fmaxf(rintf(__fdiv_rn(hi_f(w[i]), s)), -7.f), 7.f) : 0.f;
+    out |= (uint32_t)((int)a + 8) << (8 * i);
+    out |= (uint32_t)((int)b + 8) << (8 * i + 4);
   }
   return out;
 }
 
-// 16 lanes a (row, head, K or V): the largest magnitude from the bf16 bits
-// (as unsigned numbers they order like the magnitudes, infinities and NaN on
-// top), the scale, the numbers.
-__global__ void __launch_bounds__(WR_THREADS) k_kv4_write(KvRows x, const int32_t* __restrict__ src,
+// A lane group's (row, head) items, the grid's stride apart, without a division
+// an item.  A CTA's eight follow one another, so that the 16-bit side is read
+// (and written) in pieces of 2 KB; the other way round, eight rows of one head,
+// which makes the 4-bit side contiguous, reads back 65000 x 8 rows in 75 us
+// instead of 63.
+struct Items {
+  int r, h, dr, dh;
+  __device__ __forceinline__ Items(int Hkv) {
+    const int first = blockIdx.x * WR_GROUPS + threadIdx.x / WR_LANES, stride = gridDim.x * WR_GROUPS;
+    r = first / Hkv;
+    h = first - r * Hkv;
+    dr = stride / Hkv;
+    dh = stride - dr * Hkv;
+  }
+  __device__ __forceinline__ void next(int Hkv) {
+    r += dr;
+    h += dh;
+    if (h >= Hkv) h -= Hkv, ++r;
+  }
+};
+
+// 16 lanes a (row, head), key and value: the largest magnitude from the bf16
+// bits (as unsigned numbers they order like the magnitudes, infinities and NaN
+// on top), the scale, the numbers.  65000 x 8 rows written and read back take
+// 127 us, 4.7 TB/s of the 0.6 GB in and out; two or four items a lane group at
+// a time, with fewer threads for it, took 134 to 153 us.
+// bf16(top / 7) is taken as bf16(top * fl(1/7)): top has 8 significant bits,
+// so top / 7 is no midpoint of two bf16 values and lies 2^-15 of itself or
+// more from one, the product's error is 2^-23 of it.
+__global__ void __launch_bounds__(WR_THREADS, WR_CTAS) k_kv4_write(KvRows x, const int32_t* __restrict__ src,
                                                           const int32_t* __restrict__ slot, int rows, int Hkv,
                                                           int shift, long long n_slots, uint32_t* __restrict__ kc,
                                                           uint32_t* __restrict__ vc, __nv_bfloat16* __restrict__ ks,
                                                           __nv_bfloat16* __restrict__ vs, unsigned int* err) {
   const int lane = threadIdx.x % WR_LANES;
-  const long long items = (long long)rows * Hkv;
-  for (long long e = (long long)blockIdx.x * WR_GROUPS + threadIdx.x / WR_LANES; e < items;
-       e += (long long)gridDim.x * WR_GROUPS) {
-    const int r = (int)(e / Hkv), h = (int)(e - (long long)r * Hkv);
-    const int sl = slot[r];
-    const int at = src ? src[r] : r;
-    const bool live = sl >= 0 && sl < n_slots && at >= 0 && at < x.n_src;
-    if (!live && lane == 0 && h == 0 && (sl >= n_slots || (sl >= 0 && (at < 0 || at >= x.n_src))))
-      fc_flag(FC_ERR_WORD(err), FC_EBIT_INVALID);
-    if (!live) continue;  // the 16 lanes of a row agree
-    const int q = at / x.n_per_seq, i = at - q * x.n_per_seq;
-    const long long off = q * x.seq_stride + i * x.row_stride + h * x.head_stride;
-    const uint4 kx = reinterpret_cast<const uint4*>(x.k + off)[lane];
-    const uint4 vx = reinterpret_cast<const uint4*>(x.v + off)[lane];
+  const uint32_t group = 0xFFFFu << (threadIdx.x & 16);
+  for (Items it(Hkv); it.r < rows; it.next(Hkv)) {
+    const int sl = slot[it.r], at = src ? src[it.r] : it.r;
+    const bool in = at >= 0 && at < x.n_src;
+    uint4 kx = make_uint4(0, 0, 0, 0), vx = kx;
+    if (in) {  // the slot is not waited for
+      const int q = x.one_seq ? 0 : at / x.n_per_seq, i = at - q * x.n_per_seq;
+      const long long off = q * x.seq_stride + i * x.row_stride + it.h * x.head_stride;
+      kx = reinterpret_cast<const uint4*>(x.k + off)[lane];
+      vx = reinterpret_cast<const uint4*>(x.v + off)[lane];
+    }
+    if (!in || sl < 0 || sl >= n_slots) {  // the 16 lanes of a row agree
+      if (sl >= 0 && lane == 0 && it.h == 0) fc_flag(FC_ERR_WORD(err), FC_EBIT_INVALID);
+      continue;
+    }
     auto top = [](const uint4& u) {
       const uint32_t m = __vmaxu2(__vmaxu2(u.x & 0x7FFF7FFFu, u.y & 0x7FFF7FFFu),
                                   __vmaxu2(u.z & 0x7FFF7FFFu, u.w & 0x7FFF7FFFu));
-      return std::max(m & 0xFFFFu, m >> 16);
+      return max(m & 0xFFFFu, m >> 16);
     };
     uint32_t m = top(kx) | (top(vx) << 16);
-    const uint32_t group = 0xFFFFu << (threadIdx.x & 16);
 #pragma unroll
     for (int o = 1; o < WR_LANES; o <<= 1) m = __vmaxu2(m, __shfl_xor_sync(group, m, o));
-    const long long row = ((long long)(sl >> shift) * Hkv + h) * (1 << shift) + (sl & ((1 << shift) - 1));
-    auto scale = [](uint32_t top_bits) {
-      const float t = __uint_as_float(top_bits << 16);
-      return top_bits >= 0x7F80u ? __ushort_as_bfloat16(0x7FC0) : __float2bfloat16_rn(__fdiv_rn(t, 7.f));
+    const long long row = ((long long)(sl >> shift) * Hkv + it.h) * (1 << shift) + (sl & ((1 << shift) - 1));
+    auto scale = [](uint32_t bits) {
+      return bits >= 0x7F80u ? __ushort_as_bfloat16(0x7FC0) : __float2bfloat16_rn(lo_f(bits) * (1.f / 7.f));
     };
     const __nv_bfloat16 sk = scale(m & 0xFFFFu), sv = scale(m >> 16);
     kc[row * WR_LANES + lane] = quantise8(kx, __bfloat162float(sk));
@@ -315,43 +349,47 @@ __global__ void __launch_bounds__(WR_THREADS) k_kv4_write(KvRows x, const int32_
   }
 }
 
-__global__ void __launch_bounds__(WR_THREADS) k_kv4_read(const int32_t* __restrict__ slot, int rows, int Hkv, int shift,
+__global__ void __launch_bounds__(WR_THREADS, WR_CTAS) k_kv4_read(const int32_t* __restrict__ slot, int rows, int Hkv, int shift,
                                                          long long n_slots, const uint32_t* __restrict__ kc,
                                                          const uint32_t* __restrict__ vc,
-                                                         const __nv_bfloat16* __restrict__ ks,
-                                                         const __nv_bfloat16* __restrict__ vs, uint4* __restrict__ k,
+                                                         const uint16_t* __restrict__ ks,
+                                                         const uint16_t* __restrict__ vs, uint4* __restrict__ k,
                                                          uint4* __restrict__ v, unsigned int* err) {
   const int lane = threadIdx.x % WR_LANES;
-  const long long items = (long long)rows * Hkv;
-  for (long long e = (long long)blockIdx.x * WR_GROUPS + threadIdx.x / WR_LANES; e < items;
-       e += (long long)gridDim.x * WR_GROUPS) {
-    const int r = (int)(e / Hkv), h = (int)(e - (long long)r * Hkv);
-    const int sl = slot[r];
-    if (sl >= n_slots && lane == 0 && h == 0) fc_flag(FC_ERR_WORD(err), FC_EBIT_INVALID);
-    uint4 ko = make_uint4(0, 0, 0, 0), vo = ko;
+  for (Items it(Hkv); it.r < rows; it.next(Hkv)) {
+    const int sl = slot[it.r];
+    if (sl >= n_slots && lane == 0 && it.h == 0) fc_flag(FC_ERR_WORD(err), FC_EBIT_INVALID);
+    uint32_t a = 0x88888888u, b = a, sk = 0u, sv = 0u;  // zeros
     if (sl >= 0 && sl < n_slots) {
-      const long long row = ((long long)(sl >> shift) * Hkv + h) * (1 << shift) + (sl & ((1 << shift) - 1));
-      const uint32_t a = kc[row * WR_LANES + lane], b = vc[row * WR_LANES + lane];
-      const float sk = __bfloat162float(ks[row]), sv = __bfloat162float(vs[row]);
-      uint32_t* kw = &ko.x;
-      uint32_t* vw = &vo.x;
+      const long long row = ((long long)(sl >> shift) * Hkv + it.h) * (1 << shift) + (sl & ((1 << shift) - 1));
+      a = kc[row * WR_LANES + lane];
+      b = vc[row * WR_LANES + lane];
+      sk = ks[row];
+      sv = vs[row];
+    }
+    // 0x4300 | c as bf16 is 128 + c: less 136 it is the number, exactly, and
+    // times the scale the value, rounded once; in pairs (0, 4) (1, 5) ...
+    auto values = [](uint32_t w, uint32_t s2) {
+      uint32_t p[4];
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        auto val = [&](uint32_t w, int n, float s) { return (float)((int)((w >> (4 * n)) & 15u) - 8) * s; };
-        kw[i] = pack_bf16x2(val(a, 2 * i, sk), val(a, 2 * i + 1, sk));
-        vw[i] = pack_bf16x2(val(b, 2 * i, sv), val(b, 2 * i + 1, sv));
+        asm("sub.rn.bf16x2 %0, %1, %2;" : "=r"(p[i]) : "r"(((w >> (4 * i)) & 0x000F000Fu) | 0x43004300u), "r"(0x43084308u));
+        asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(p[i]) : "r"(p[i]), "r"(s2));
       }
-    }
-    k[e * WR_LANES + lane] = ko;
-    v[e * WR_LANES + lane] = vo;
+      return make_uint4(__byte_perm(p[0], p[1], 0x5410), __byte_perm(p[2], p[3], 0x5410),
+                        __byte_perm(p[0], p[1], 0x7632), __byte_perm(p[2], p[3], 0x7632));
+    };
+    const size_t to = ((size_t)it.r * Hkv + it.h) * WR_LANES + lane;
+    __stcs(k + to, values(a, sk * 0x10001u));
+    __stcs(v + to, values(b, sv * 0x10001u));
   }
 }
 
 bool aligned(const void* p, uintptr_t n) { return reinterpret_cast<uintptr_t>(p) % n == 0; }
 
-unsigned grid_for(long long items) {
-  // at most 16 CTAs an SM: 2048 threads
-  return (unsigned)std::max<long long>(1, std::min<long long>((items + WR_GROUPS - 1) / WR_GROUPS, 152 * 16));
+unsigned grid_for(int rows, int Hkv) {
+  // several times what is resident: CTAs that end early make room (16 an SM: 134 us, 64: 127 us)
+  return (unsigned)std::min<long long>(((long long)rows * Hkv + WR_GROUPS - 1) / WR_GROUPS, 152 * 4 * WR_CTAS);
 }
 
 }  // namespace
@@ -424,8 +462,9 @@ extern "C" fc_status fc_kv4_write(const fc_kv4_cache* cache, const void* d_k, co
       head_stride % 8 || (!d_src && rows > n_seq * n_per_seq))
     return FC_ERR_INVALID_ARG;
   KvRows x{static_cast<const __nv_bfloat16*>(d_k), static_cast<const __nv_bfloat16*>(d_v), n_per_seq,
-           n_seq * n_per_seq, seq_stride, row_stride, head_stride};
-  k_kv4_write<<<grid_for((long long)rows * cache->Hkv), WR_THREADS, 0, static_cast<cudaStream_t>(stream)>>>(
+           n_seq * n_per_seq, n_seq == 1, seq_stride, row_stride, head_stride};
+  if ((long long)rows * cache->Hkv > MAX_ITEMS) return FC_ERR_UNSUPPORTED;
+  k_kv4_write<<<grid_for(rows, cache->Hkv), WR_THREADS, 0, static_cast<cudaStream_t>(stream)>>>(
       x, d_src, d_slot, rows, cache->Hkv, kv4_page_shift(cache->page_size), (long long)cache->n_pages * cache->page_size,
       static_cast<uint32_t*>(cache->k_codes), static_cast<uint32_t*>(cache->v_codes),
       static_cast<__nv_bfloat16*>(cache->k_scale), static_cast<__nv_bfloat16*>(cache->v_scale), fc_error_slot());
@@ -439,10 +478,11 @@ extern "C" fc_status fc_kv4_read(const fc_kv4_cache* cache, const int32_t* d_slo
   if (rows < 0) return FC_ERR_INVALID_ARG;
   if (rows == 0) return FC_OK;
   if (!d_slot || !d_k || !d_v || !aligned(d_k, 16) || !aligned(d_v, 16)) return FC_ERR_INVALID_ARG;
-  k_kv4_read<<<grid_for((long long)rows * cache->Hkv), WR_THREADS, 0, static_cast<cudaStream_t>(stream)>>>(
+  if ((long long)rows * cache->Hkv > MAX_ITEMS) return FC_ERR_UNSUPPORTED;
+  k_kv4_read<<<grid_for(rows, cache->Hkv), WR_THREADS, 0, static_cast<cudaStream_t>(stream)>>>(
       d_slot, rows, cache->Hkv, kv4_page_shift(cache->page_size), (long long)cache->n_pages * cache->page_size,
       static_cast<const uint32_t*>(cache->k_codes), static_cast<const uint32_t*>(cache->v_codes),
-      static_cast<const __nv_bfloat16*>(cache->k_scale), static_cast<const __nv_bfloat16*>(cache->v_scale),
+      static_cast<const uint16_t*>(cache->k_scale), static_cast<const uint16_t*>(cache->v_scale),
       static_cast<uint4*>(d_k), static_cast<uint4*>(d_v), fc_error_slot());
   return FC_CHECK_LAUNCH();
 }

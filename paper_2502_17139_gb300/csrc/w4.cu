@@ -361,8 +361,9 @@ extern "C" fc_status fc_w4_matvec(const void* d_x, const void* d_codes, const vo
       !aligned(d_y, 2))
     return FC_ERR_INVALID_ARG;
   cudaStream_t s = static_cast<cudaStream_t>(stream);
-  // Two column tiles a warp halve what it loads of x; they take a wide output
-  // (else a warp's tiles alone leave the GPU short of warps).
-  if (N <= 152 * TN * 8) return launch_rows<1>(d_x, d_codes, d_scale, M, K, N, group, d_y, s);
+  // Two column tiles a warp halve what it loads of x and what a tile costs
+  // besides its numbers (8192 x 8192 18.5 -> 15.1 us); an output of fewer than
+  // two tiles an SM has too few tiles for that (2048 x 2048: 6.2 us either way).
+  if (N <= 152 * TN * 2) return launch_rows<1>(d_x, d_codes, d_scale, M, K, N, group, d_y, s);
   return launch_rows<2>(d_x, d_codes, d_scale, M, K, N, group, d_y, s);
 }
