@@ -22,9 +22,8 @@ constexpr int HD = KV4_D;
 // ---------------------------------------------------------------------------
 // Pages.
 // ---------------------------------------------------------------------------
-constexpr int PL_THREADS = 512;
-constexpr int PL_CHUNK = PL_THREADS;  // requests scanned at a time, one a thread
-constexpr int PL_MIN_ROWS = 512;      // rows a CTA takes at least
+constexpr int PL_MAX_THREADS = 1024;  // a CTA has a thread for each request of a chunk
+constexpr int PL_ROWS = 2;            // rows a thread takes at least, once there are CTAs for every SM
 
 struct PlanArgs {
   const int32_t *kv_len, *n_new;
@@ -42,47 +41,58 @@ struct PlanArgs {
 // Inclusive sums of two values over the block's threads (64-bit: lengths are
 // the caller's data, and their sum may pass 32 bits before it is refused).
 __device__ __forceinline__ void block_scan2(long long& a, long long& b, long long (*s_part)[2]) {
-  const int lane = threadIdx.x & 31, wp = threadIdx.x >> 5;
+  const int lane = threadIdx.x & 31, wp = threadIdx.x >> 5, warps = blockDim.x >> 5;
 #pragma unroll
   for (int o = 1; o < 32; o <<= 1) {
     const long long x = __shfl_up_sync(0xFFFFFFFFu, a, o), y = __shfl_up_sync(0xFFFFFFFFu, b, o);
     if (lane >= o) a += x, b += y;
   }
+  if (warps == 1) return;
   if (lane == 31) s_part[wp][0] = a, s_part[wp][1] = b;
   __syncthreads();
-  long long pa = 0, pb = 0;
-  for (int w = 0; w < wp; ++w) pa += s_part[w][0], pb += s_part[w][1];
-  a += pa, b += pb;
+  // every warp sums the warps' totals for itself
+  long long ta = lane < wp ? s_part[lane][0] : 0, tb = lane < wp ? s_part[lane][1] : 0;
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) {
+    ta += __shfl_xor_sync(0xFFFFFFFFu, ta, o);
+    tb += __shfl_xor_sync(0xFFFFFFFFu, tb, o);
+  }
+  a += ta, b += tb;
 }
 
-// Every CTA sums over all requests itself, a chunk of PL_CHUNK at a time, and
-// fills its own rows and its own requests' table entries, so one launch does
-// the whole plan with no CTA waiting for another.  The lengths are a few KB
-// that L2 serves; bound by latency at every size that a step has.
-__global__ void __launch_bounds__(PL_THREADS) k_pages_plan(PlanArgs a, int rows_per_cta) {
-  __shared__ long long s_part[PL_THREADS / 32][2];
-  __shared__ int32_t s_cu[PL_CHUNK + 1], s_kv[PL_CHUNK], s_have[PL_CHUNK], s_off[PL_CHUNK], s_more[PL_CHUNK];
-  const int tid = threadIdx.x;
+// Every CTA sums over all requests itself, a chunk (a thread each) at a time,
+// and fills its own rows and its own requests' table entries, so one launch
+// does the whole plan with no CTA waiting for another.  The lengths are a few
+// KB that L2 serves; bound by latency at every size that a step has: 6 us for
+// 32 requests, and for 1000 with 243,000 new tokens.
+__global__ void __launch_bounds__(PL_MAX_THREADS) k_pages_plan(PlanArgs a, int rows_per_cta) {
+  __shared__ long long s_part[PL_MAX_THREADS / 32][2];
+  __shared__ long long s_sum[2];
+  __shared__ int32_t s_cu[PL_MAX_THREADS + 1], s_off[PL_MAX_THREADS], s_more[PL_MAX_THREADS];
+  __shared__ int2 s_kv[PL_MAX_THREADS];  // length, pages held
+  const int tid = threadIdx.x, chunk = blockDim.x;
   const long long page = 1ll << a.shift;
+  const int in_page = (1 << a.shift) - 1;
   int n_free = *a.n_free_in;
+  const int r_lo = (int)min((long long)blockIdx.x * rows_per_cta, (long long)a.rows_cap);
+  const int r_hi = (int)min((long long)r_lo + rows_per_cta, (long long)a.rows_cap);
   if (n_free < 0 || n_free > a.n_pages) {
     if (blockIdx.x == 0 && tid == 0) fc_flag(FC_ERR_WORD(a.err), FC_EBIT_INVALID);
     n_free = 0;
   }
-  const int r_lo = (int)std::min<long long>((long long)blockIdx.x * rows_per_cta, a.rows_cap);
-  const int r_hi = (int)std::min<long long>((long long)r_lo + rows_per_cta, a.rows_cap);
   long long row_base = 0, page_base = 0;
   long long taken = 0;  // pages of the requests served so far (CTA 0)
-  for (int b0 = 0; b0 < a.batch; b0 += PL_CHUNK) {
+  for (int b0 = 0; b0 < a.batch; b0 += chunk) {
     const int b = b0 + tid;
     long long kv = 0, n = 0;
-    bool ok = b < a.batch, bad = false;
+    const bool ok = b < a.batch;
+    bool bad = false;
     if (ok) {
       kv = a.kv_len[b];
       n = a.n_new[b];
       bad = kv < 0 || n < 0;
-      kv = std::max(kv, 0ll);
-      n = std::max(n, 0ll);
+      kv = max(kv, 0ll);
+      n = max(n, 0ll);
     }
     const long long have = (kv + page - 1) >> a.shift, need = (kv + n + page - 1) >> a.shift;
     const bool fits = ok && !bad && need <= a.max_pages && kv + n <= 0x7FFFFFFFll;
@@ -93,64 +103,62 @@ __global__ void __launch_bounds__(PL_THREADS) k_pages_plan(PlanArgs a, int rows_
     page_end += page_base;
     const bool served = fits && rows_end <= a.rows_cap && (more == 0 || page_end <= n_free);
     if (ok) {
-      s_cu[tid + 1] = (int32_t)std::min<long long>(rows_end, a.rows_cap);
-      s_kv[tid] = (int32_t)kv;
-      s_have[tid] = (int32_t)have;
-      s_off[tid] = (int32_t)std::min<long long>(page_end - more, n_free);
+      s_cu[tid + 1] = (int32_t)min(rows_end, (long long)a.rows_cap);
+      s_kv[tid] = make_int2((int32_t)kv, (int32_t)have);
+      s_off[tid] = (int32_t)min(page_end - more, (long long)n_free);
       s_more[tid] = served ? (int32_t)more : -1;
     }
-    if (tid == 0) s_cu[0] = (int32_t)std::min<long long>(row_base, a.rows_cap);
+    if (tid == 0) s_cu[0] = (int32_t)min(row_base, (long long)a.rows_cap);
+    if (tid == chunk - 1) s_sum[0] = rows_end, s_sum[1] = page_end;
     if (blockIdx.x == 0 && ok) {
-      a.cu[b + 1] = (int32_t)std::min<long long>(rows_end, a.rows_cap);
+      a.cu[b + 1] = (int32_t)min(rows_end, (long long)a.rows_cap);
       a.kv_out[b] = (int32_t)(served ? kv + n : kv);
       if (b == 0) a.cu[0] = 0;
       if (!served) fc_flag(FC_ERR_WORD(a.err), bad ? FC_EBIT_INVALID : FC_EBIT_CAPACITY);
+      taken += served ? more : 0;
     }
-    const int in_chunk = min(PL_CHUNK, a.batch - b0);
-    // the last thread holds the chunk's sums
-    __syncthreads();  // s_part is read, the chunk's arrays are written
-    if (tid == PL_THREADS - 1) s_part[0][0] = rows_end, s_part[0][1] = page_end;
-    if (blockIdx.x == 0) taken += served ? more : 0;
-    // table entries of new pages: a warp a request
-    for (int i = (tid >> 5) * gridDim.x + blockIdx.x; i < in_chunk; i += (PL_THREADS / 32) * gridDim.x) {
-      const int m = s_more[i];
-      for (int j = tid & 31; j < m; j += 32)
-        a.table[(size_t)(b0 + i) * a.max_pages + s_have[i] + j] = a.free_list[n_free - 1 - s_off[i] - j];
-    }
+    const int in_chunk = min(chunk, a.batch - b0);
+    __syncthreads();
+    row_base = s_sum[0];
+    page_base = s_sum[1];
     // rows of this chunk's requests in [r_lo, r_hi)
-    const int lo = std::max(r_lo, s_cu[0]), hi = std::min(r_hi, s_cu[in_chunk]);
-    for (int r = lo + tid; r < hi; r += PL_THREADS) {
-      int x = 0, y = in_chunk;  // s_cu[x] <= r < s_cu[y]
-      while (y - x > 1) {
-        const int m = (x + y) >> 1;
-        if (s_cu[m] <= r) x = m;
-        else y = m;
-      }
-      const int q = b0 + x, j = r - s_cu[x], p = (int)((uint32_t)s_kv[x] + (uint32_t)j);
-      int slot = -1;
+    const int lo = max(r_lo, s_cu[0]), hi = min(r_hi, s_cu[in_chunk]);
+#pragma unroll 2
+    for (int r = lo + tid; r < hi; r += chunk) {
+      int x = 0;  // s_cu[x] <= r < s_cu[x + 1]
+#pragma unroll 1
+      for (int step = 512; step > 0; step >>= 1)
+        if (x + step < in_chunk && s_cu[x + step] <= r) x += step;
+      const int q = b0 + x, j = r - s_cu[x];
+      const int2 kh = s_kv[x];
+      const int p = (int)((uint32_t)kh.x + (uint32_t)j);
+      int sl = -1;
       if (s_more[x] >= 0) {
         const int pg = p >> a.shift;
-        const int id = pg < s_have[x] ? a.table[(size_t)q * a.max_pages + pg]
-                                      : a.free_list[n_free - 1 - s_off[x] - (pg - s_have[x])];
-        slot = id < 0 || id >= a.n_pages ? -1 : (id << a.shift) + (p & ((1 << a.shift) - 1));
-        if (id < 0 || id >= a.n_pages) fc_flag(FC_ERR_WORD(a.err), FC_EBIT_INVALID);
+        const int id = pg < kh.y ? a.table[(size_t)q * a.max_pages + pg] : a.free_list[n_free - 1 - s_off[x] - (pg - kh.y)];
+        const bool in = (unsigned)id < (unsigned)a.n_pages;
+        sl = in ? (id << a.shift) + (p & in_page) : -1;
+        if (!in) fc_flag(FC_ERR_WORD(a.err), FC_EBIT_INVALID);
       }
       a.seq[r] = q;
       a.pos[r] = p;
-      a.slot[r] = slot;
+      a.slot[r] = sl;
       if (a.src) {
         const int node = a.path ? (j < a.path_cap ? a.path[(size_t)q * a.path_cap + j] : -1) : j;
         a.src[r] = node < 0 || node >= a.n_per_seq ? -1 : q * a.n_per_seq + node;
       }
     }
-    __syncthreads();
-    row_base = s_part[0][0];
-    page_base = s_part[0][1];
-    __syncthreads();
+    // table entries of new pages: 8 lanes a request
+    for (int i = (tid >> 3) * gridDim.x + blockIdx.x; i < in_chunk; i += (chunk >> 3) * gridDim.x) {
+      const int m = s_more[i];
+      for (int j = tid & 7; j < m; j += 8)
+        a.table[(size_t)(b0 + i) * a.max_pages + s_kv[i].y + j] = a.free_list[n_free - 1 - s_off[i] - j];
+    }
+    __syncthreads();  // the chunk's arrays are read
   }
   // rows past the last request's
-  const int total = (int)std::min<long long>(row_base, a.rows_cap);
-  for (int r = std::max(r_lo, total) + tid; r < r_hi; r += PL_THREADS) {
+  const int total = (int)min(row_base, (long long)a.rows_cap);
+  for (int r = max(r_lo, total) + tid; r < r_hi; r += chunk) {
     a.seq[r] = -1;
     a.pos[r] = -1;
     a.slot[r] = -1;
@@ -159,10 +167,12 @@ __global__ void __launch_bounds__(PL_THREADS) k_pages_plan(PlanArgs a, int rows_
   if (blockIdx.x == 0) {
     long long t2 = 0;
     block_scan2(taken, t2, s_part);
-    if (tid == PL_THREADS - 1) *a.n_free_out = n_free - (int32_t)taken;
+    if (tid == chunk - 1) *a.n_free_out = n_free - (int32_t)taken;
     if (a.batch == 0 && tid == 0) a.cu[0] = 0;
   }
 }
+
+constexpr int PL_THREADS = 512;  // of the release
 
 // One CTA: the pages of request b past ceil(keep / page) go back on the free
 // list in request order.
@@ -425,9 +435,12 @@ extern "C" fc_status fc_kv_pages_plan(const int32_t* d_kv_len, const int32_t* d_
   PlanArgs a{d_kv_len, d_n_new,    batch,    shift,     max_pages, d_table, d_free, n_pages, d_n_free_in,
              d_path,   path_cap,   n_per_seq, rows_cap, d_cu,      d_seq,   d_pos,  d_slot,  d_src,
              d_kv_len_out, d_n_free_out, fc_error_slot()};
-  const int ctas = std::max(1, std::min((rows_cap + PL_MIN_ROWS - 1) / PL_MIN_ROWS, 152 * 4));
-  const int per = std::max(1, (rows_cap + ctas - 1) / ctas);
-  k_pages_plan<<<ctas, PL_THREADS, 0, static_cast<cudaStream_t>(stream)>>>(a, per);
+  int threads = 256;
+  while (threads < PL_MAX_THREADS && threads < batch) threads *= 2;
+  const int ctas = (int)std::max<long long>(
+      1, std::min<long long>(((long long)rows_cap + threads * PL_ROWS - 1) / (threads * PL_ROWS), 152 * (2048 / threads)));
+  const int per = (int)(((long long)rows_cap + ctas - 1) / ctas);
+  k_pages_plan<<<ctas, threads, 0, static_cast<cudaStream_t>(stream)>>>(a, std::max(1, per));
   return FC_CHECK_LAUNCH();
 }
 
