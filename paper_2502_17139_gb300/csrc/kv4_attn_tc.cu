@@ -57,7 +57,9 @@ constexpr int SLOTS = 4;                                        // blocks whose 
 constexpr uint32_t OFF_KEEP = OFF_V + 2 * TILE_BYTES;           // [slot][4] bits of the keys that count
 constexpr uint32_t OFF_VS = OFF_KEEP + SLOTS * 16;              // [slot][128] value scales, bf16
 constexpr uint32_t OFF_BACK = OFF_VS + SLOTS * BN * 2;          // [slot][8] what 16 keys' scores are to be multiplied by
-constexpr uint32_t OFF_QE = OFF_BACK + SLOTS * 32;              // [2 pieces][256] the same for the query rows
+constexpr uint32_t OFF_RUN = OFF_BACK + SLOTS * 32;             // [slot][8] where 16 keys' rows are, in runs of 16 rows
+constexpr uint32_t OFF_KS = OFF_RUN + SLOTS * 32;               // [slot][128] (s, s), (-24 s, -24 s): a key's scale in fp16
+constexpr uint32_t OFF_QE = OFF_KS + SLOTS * BN * 8;              // [2 pieces][256] the same for the query rows
 constexpr uint32_t OFF_ML = OFF_QE + 2 * ROWS * 4;              // [2 turns][2][128] (m, l) exchanged at a unit's end
 constexpr int PIECES = 4;                                       // piece descriptions kept
 constexpr uint32_t OFF_PIECE = OFF_ML + 4 * BM * 8;             // [PIECES]
@@ -74,7 +76,6 @@ constexpr float M_START = -1e30f;  // a reference before any key
 constexpr int E_MIN = -50;
 // A unit's start and end in blocks of one tile, and the least share worth a CTA.
 constexpr int UNIT_COST = 8, LEAST = 12;
-constexpr int AHEAD = 4;  // blocks asked into L2 before they are fetched
 
 // Registers a thread by warpgroup (setmaxnreg), of the launch's 96.  The shares must add up to the launch's
 // allocation, or the increase never returns; the host checks the compiled count.
@@ -88,7 +89,7 @@ enum {
   B_VEMPTY = 6,  // [2]
   B_SFULL = 8,   // [2 tiles]
   B_PFULL = 10,  // [2 tiles] 128
-  B_INFO = 12,   // [4 slots] 8: a block's scales and keep bits
+  B_INFO = 12,   // [4 slots] 2: a block's scales and keep bits
   B_QFULL = 16,  // 9
   B_QFREE = 17,
   B_OFIN = 18,
@@ -97,7 +98,8 @@ enum {
   B_PIECE = 21,  // [PIECES] a description is written
   B_QE = 25,     // [2] 8: the query rows' factors
   B_DRAIN = 27,
-  N_BARS = 28
+  B_SLOT = 28,   // [4 slots] a slot's block is done with
+  N_BARS = 32
 };
 
 struct ManyArgs {
@@ -413,7 +415,8 @@ __global__ void __launch_bounds__(THREADS, 1) k_kv4_attn_many(ManyArgs f) {
     for (int i = 0; i < N_BARS; ++i) {
       uint32_t n = 1;
       if (i == B_PFULL || i == B_PFULL + 1) n = 128;
-      if (i < B_KEMPTY || (i >= B_INFO && i < B_INFO + SLOTS) || i == B_QE || i == B_QE + 1) n = NUM_WARPS;
+      if (i < B_KEMPTY || i == B_QE || i == B_QE + 1) n = NUM_WARPS;
+      if (i >= B_INFO && i < B_INFO + SLOTS) n = 2;
       if (i == B_QFULL) n = NUM_WARPS + 1;
       if (i == B_OFREE || i == B_ML) n = 256;
       mbar_init(bar(i), n);
@@ -467,7 +470,10 @@ __global__ void __launch_bounds__(THREADS, 1) k_kv4_attn_many(ManyArgs f) {
           ++t_of[x];
           if (k == 0 && np > 0 && !wait(B_OFREE, np - 1)) break;
           mma_pv(tmem + 256 + x * 128, tmem + x * 128, v_lo + st * (TILE_BYTES >> 4), IDESC_PV, k >= 2);
-          if (!two || x) tc_commit(bar(B_VEMPTY + st));
+          if (!two || x) {
+            tc_commit(bar(B_VEMPTY + st));
+            tc_commit(bar(B_SLOT + blk % SLOTS));
+          }
         }
         if (k + 2 < steps) {  // S_x <- Q K^T
           const uint32_t blk = nb + ((k + 2) >> two), st = blk & 1;
@@ -521,19 +527,96 @@ __global__ void __launch_bounds__(THREADS, 1) k_kv4_attn_many(ManyArgs f) {
           mbar_arrive(bar(B_PIECE + np % PIECES));
         }
         if (!any) break;
+        if (wk.s0 == 0 && wk.row0 == 0) {  // the rows past the nodes
+          const int pad = (a.n_pad - wk.nn) * a.G;
+#pragma unroll 1
+          for (int e = lane; e < pad * (HD / 8); e += 32) {
+            const int r = e / (HD / 8), ch = e % (HD / 8), i = wk.nn + r / a.G, hh = r % a.G;
+            reinterpret_cast<uint4*>(a.out + (((size_t)wk.b * a.n_pad + i) * a.H + wk.gh * a.G + hh) * HD)[ch] =
+                make_uint4(0, 0, 0, 0);
+          }
+        }
       }
     } else {
-      for (;; ++np) {  // the rows past the nodes
+      // ---------------- keys' scales, ahead of their rows ----------------
+      // Thread i: keys 2i, 2i + 1 of a block, in run i / 8 of its eight.
+      const int i = tid - 64, run_i = i >> 3;
+      const uint32_t per_page = (uint32_t)a.Hkv << (a.shift - 4), in_page = (1u << (a.shift - 4)) - 1u;
+      uint32_t nb = 0;
+      bool ok = true;
+      for (; ok; ++np) {
         if (!warp_wait(bar(B_PIECE + np % PIECES), (np / PIECES) & 1, &s_abort)) break;
-        const Piece* pc = piece(np);
-        if (pc->n == 0) break;
-        if (pc->s0 != 0 || pc->row0 != 0) continue;
-        const int nn = pc->nn, pad = (a.n_pad - nn) * a.G, bb = pc->b, gh = pc->gh;
-#pragma unroll 1
-        for (int e = tid - 64; e < pad * (HD / 8); e += 64) {
-          const int r = e / (HD / 8), ch = e % (HD / 8), i = nn + r / a.G, hh = r % a.G;
-          reinterpret_cast<uint4*>(a.out + (((size_t)bb * a.n_pad + i) * a.H + gh * a.G + hh) * HD)[ch] =
-              make_uint4(0, 0, 0, 0);
+        const Piece pc = *piece(np);
+        if (pc.n == 0) break;
+        const int s1 = pc.s0 + pc.n, to = min(s1, pc.cached);
+        const int32_t* tab = a.table + (size_t)pc.b * a.max_pages;
+        auto look_up = [&](int blk) {
+          const uint32_t run = (uint32_t)blk * (BN / 16) + run_i;
+          return blk < to && run <= (uint32_t)(pc.kvl - 1) >> 4 ? tab[run >> (a.shift - 4)] : -1;
+        };
+        int id = look_up(pc.s0), id_next = look_up(pc.s0 + 1);
+        uint32_t run = 0, kw = 0, vw = 0;
+        bool in = false;
+        auto fetch = [&](int blk) {
+          in = (unsigned)id < (unsigned)a.n_pages;
+          run = in ? id * per_page + ((uint32_t)pc.gh << (a.shift - 4)) + (((uint32_t)blk * (BN / 16) + run_i) & in_page) : 0u;
+          kw = reinterpret_cast<const uint32_t*>(a.ks)[(uint64_t)run * 8u + (i & 7)];
+          vw = reinterpret_cast<const uint32_t*>(a.vs)[(uint64_t)run * 8u + (i & 7)];
+          // the rows of its run: a line of K and one of V, asked into L2
+          prefetch_l2(a.kc + (uint64_t)run * 1024u + (i & 7) * 128);
+          prefetch_l2(a.vc + (uint64_t)run * 1024u + (i & 7) * 128);
+        };
+        if (pc.s0 < to) fetch(pc.s0);
+        for (int blk = pc.s0; blk < s1; ++blk, ++nb) {
+          const int slot = nb % SLOTS;
+          const bool fresh = blk >= pc.cached;
+          const uint32_t run_now = run;
+          int left;  // keys of the run that count
+          uint32_t top, k0 = 0, k1 = 0, v2 = 0x3F803F80u;
+          if (!fresh) {
+            const long long more = pc.kvl - ((long long)blk * BN + 16 * run_i);
+            left = in ? (int)min(16ll, max(0ll, more)) : 0;
+            if (!in && more > 0 && (i & 7) == 0) fc_flag(FC_ERR_WORD(a.err), FC_EBIT_INVALID);
+            // a key that does not count: whatever stands there
+            const uint32_t some = 2 * (i & 7) + 1 < left ? 0xFFFFFFFFu : (2 * (i & 7) < left ? 0xFFFFu : 0u);
+            k0 = kw & some;
+            v2 = vw & some;
+            top = top2(0u, k0);
+            k1 = k0 >> 16;
+            k0 &= 0xFFFFu;
+            if (blk + 1 < to) {
+              id = id_next;
+              fetch(blk + 1);
+              id_next = look_up(blk + 2);
+            }
+          } else {
+            left = a.k_new ? min(16, max(0, pc.nn - 16 * run_i)) : 0;
+            const uint4* src = reinterpret_cast<const uint4*>(a.k_new + (((size_t)pc.b * a.Hkv + pc.gh) * a.n_pad + 16 * run_i) * HD);
+            top = 0;
+#pragma unroll 8
+            for (int e = i & 7; e < left * (HD / 8); e += 8) {
+              const uint4 k = src[e];
+              top = top2(top2(top2(top2(top, k.x), k.y), k.z), k.w);
+            }
+          }
+          top = max(top & 0xFFFFu, top >> 16);
+#pragma unroll
+          for (int o = 1; o < 8; o <<= 1) top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, o));
+          const int ek = expo_of(top);
+          const float by = pow2i(E_TOP - ek);
+          if (nb >= SLOTS && !(ok = warp_wait(bar(B_SLOT + slot), (nb / SLOTS - 1) & 1, &s_abort))) break;
+          if ((i & 7) == 0) {
+            reinterpret_cast<uint16_t*>(smem + OFF_KEEP + slot * 16)[run_i] = (uint16_t)((1u << left) - 1u);
+            reinterpret_cast<float*>(smem + OFF_BACK)[slot * (BN / 16) + run_i] = pow2i(ek - E_TOP);
+            reinterpret_cast<uint32_t*>(smem + OFF_RUN)[slot * (BN / 16) + run_i] = fresh ? __float_as_uint(by) : run_now;
+          }
+          reinterpret_cast<uint32_t*>(smem + OFF_VS)[slot * (BN / 2) + i] = v2;
+          const float f0 = lo_f(k0) * by, f1 = lo_f(k1) * by;
+          reinterpret_cast<uint4*>(smem + OFF_KS)[slot * (BN / 2) + i] =
+              make_uint4(pack_f16x2(f0, f0), pack_f16x2(-24.f * f0, -24.f * f0), pack_f16x2(f1, f1),
+                         pack_f16x2(-24.f * f1, -24.f * f1));
+          __syncwarp();
+          if (lane == 0) mbar_arrive(bar(B_INFO + slot));
         }
       }
     }
@@ -550,48 +633,16 @@ __global__ void __launch_bounds__(THREADS, 1) k_kv4_attn_many(ManyArgs f) {
       dst[i] = swap * HALF_BYTES + (16 * w + rho) * 128 + ((((c & 1) * 4 + (i ^ (2 * swap))) ^ rho) << 4);
     Piece pc = {};
     uint4 kr[2], vr[2];
-    uint32_t ksc[2] = {0u, 0u}, vsc[2] = {0u, 0u};  // scales, bf16 bits (apart, so that nothing waits for their loads)
-    int id = -1, id_next = -1, id_ahead = -1;  // pages: of the block fetched, of the next, of the one to ask for
     uint32_t nb = 0;
     bool ok = true;
-    // runs of 16 rows are counted in 32 bits (1024 bytes each: 4 TB)
-    const uint32_t per_page = (uint32_t)a.Hkv << (a.shift - 4), in_page = (1u << (a.shift - 4)) - 1u;
-    auto look_up = [&](int blk) {
-      const uint32_t run = (uint32_t)blk * (BN / 16) + w;
-      return pc.kvl > 0 && run <= (uint32_t)(pc.kvl - 1) >> 4 ? a.table[(size_t)pc.b * a.max_pages + (run >> (a.shift - 4))] : -1;
+    auto info = [&](uint32_t blk) {
+      return warp_wait(bar(B_INFO + blk % SLOTS), (blk / SLOTS) & 1, &s_abort);
     };
-    auto run_of = [&](int page, int blk) {
-      return page * per_page + ((uint32_t)pc.gh << (a.shift - 4)) + (((uint32_t)blk * (BN / 16) + w) & in_page);
-    };
-    auto fetch_k = [&](int blk) {  // K rows and both scales, of page id
-      const bool in = (unsigned)id < (unsigned)a.n_pages;
-      const uint32_t run = in ? run_of(id, blk) : 0u;
-      const uint4* src = reinterpret_cast<const uint4*>(a.kc + (uint64_t)run * 1024u) + lane;
-      kr[0] = src[0];
-      kr[1] = src[32];
-      const uint16_t* ks = reinterpret_cast<const uint16_t*>(a.ks) + (uint64_t)run * 16u + rho;
-      const uint16_t* vs = reinterpret_cast<const uint16_t*>(a.vs) + (uint64_t)run * 16u + rho;
-      ksc[0] = ks[0];
-      ksc[1] = ks[8];
-      vsc[0] = vs[0];
-      vsc[1] = vs[8];
-    };
-    auto fetch_v = [&](int blk) {
-      const uint32_t run = (unsigned)id < (unsigned)a.n_pages ? run_of(id, blk) : 0u;
-      const uint4* src = reinterpret_cast<const uint4*>(a.vc + (uint64_t)run * 1024u) + lane;
-      vr[0] = src[0];
-      vr[1] = src[32];
-    };
-    // Blocks AHEAD of the one being fetched are asked into L2: 8 lines of K, 8
-    // of V, the scales.
-    auto ask = [&](int blk) {
-      if ((unsigned)id_ahead < (unsigned)a.n_pages && lane < 18) {
-        const uint64_t run = run_of(id_ahead, blk);
-        prefetch_l2(lane < 8    ? (const void*)(a.kc + run * 1024u + lane * 128)
-                    : lane < 16 ? (const void*)(a.vc + run * 1024u + (lane - 8) * 128)
-                                : (const void*)((lane == 16 ? a.ks : a.vs) + run * 16u));
-      }
-      id_ahead = look_up(blk + 1);
+    const uint32_t* runs = reinterpret_cast<const uint32_t*>(smem + OFF_RUN) + w;
+    auto fetch = [&](const uint8_t* codes, uint32_t run, uint4 (&x)[2]) {
+      const uint4* src = reinterpret_cast<const uint4*>(codes + (uint64_t)run * 1024u) + lane;
+      x[0] = src[0];
+      x[1] = src[32];
     };
     const size_t no_row = ~(size_t)0;
     auto new_row = [&](int j) {
@@ -627,32 +678,6 @@ __global__ void __launch_bounds__(THREADS, 1) k_kv4_attn_many(ManyArgs f) {
         }
       }
     };
-    // keys of this warp's 16 that count in block blk
-    auto keys_of = [&](int blk) {
-      if (blk >= pc.cached) return a.k_new ? pc.nn - 16 * w : 0;
-      return (unsigned)id < (unsigned)a.n_pages ? (int)min(16ll, pc.kvl - (long long)blk * BN - 16 * w) : 0;
-    };
-    // The largest key scale (magnitude, for the new tokens) of this warp's keys.
-    auto largest = [&](bool fresh, int left) {
-      uint32_t top = 0;
-      if (!fresh) {  // a key that does not count: whatever stands there
-        if (rho >= left) ksc[0] = vsc[0] = 0;
-        if (rho + 8 >= left) ksc[1] = vsc[1] = 0;
-        top = top2(0u, ksc[0] | (ksc[1] << 16));
-        top = max(top & 0xFFFFu, top >> 16);
-      } else {
-        uint32_t tk = 0;
-#pragma unroll 1
-        for (int e = lane; e < 256; e += 32) {
-          const size_t row = new_row(16 * w + (e >> 4));
-          if (row == no_row) break;
-          const uint4 k = reinterpret_cast<const uint4*>(a.k_new + row)[e & 15];
-          tk = top2(top2(top2(top2(tk, k.x), k.y), k.z), k.w);
-        }
-        top = max(tk & 0xFFFFu, tk >> 16);
-      }
-      return __reduce_max_sync(0xFFFFFFFFu, top);
-    };
     auto store = [&](uint32_t tile, const uint4 (&x)[2], auto&& convert) {
 #pragma unroll
       for (int p = 0; p < 2; ++p) {
@@ -685,12 +710,12 @@ __global__ void __launch_bounds__(THREADS, 1) k_kv4_attn_many(ManyArgs f) {
       pc = *piece(np);
       if (pc.n == 0) break;
       const int s1 = pc.s0 + pc.n;
+      uint32_t run = 0;
       if (pc.s0 < pc.cached) {
-        id = look_up(pc.s0);
-        id_next = look_up(pc.s0 + 1);
-        id_ahead = look_up(pc.s0 + AHEAD);
-        fetch_k(pc.s0);
-        fetch_v(pc.s0);
+        if (!(ok = info(nb))) break;
+        run = runs[nb % SLOTS * (BN / 16)];
+        fetch(a.kc, run, kr);
+        fetch(a.vc, run, vr);
       }
       if (np > 0 && !(ok = warp_wait(bar(B_QFREE), (np - 1) & 1, &s_abort))) break;
       stage_q(np);
@@ -703,48 +728,27 @@ __global__ void __launch_bounds__(THREADS, 1) k_kv4_attn_many(ManyArgs f) {
       for (int blk = pc.s0; blk < s1; ++blk, ++nb) {
         const int st = nb & 1, slot = nb % SLOTS;
         const bool fresh = blk >= pc.cached, more = blk + 1 < s1 && blk + 1 < pc.cached;
-        const int left = keys_of(blk), ek = expo_of(largest(fresh, left));
-        // the slot's last readers are done (the V stage of three blocks ago was waited for)
-        if (lane == 0) {
-          reinterpret_cast<uint16_t*>(smem + OFF_KEEP + slot * 16)[w] =
-              (uint16_t)(left >= 16 ? 0xFFFFu : (left <= 0 ? 0u : (1u << left) - 1u));
-          reinterpret_cast<float*>(smem + OFF_BACK)[slot * NUM_WARPS + w] = pow2i(ek - E_TOP);
-          if (!fresh && (unsigned)id >= (unsigned)a.n_pages && (long long)blk * BN + 16 * w < pc.kvl)
-            fc_flag(FC_ERR_WORD(a.err), FC_EBIT_INVALID);
-        }
-        if (c == 0) {
-          uint16_t* vs = reinterpret_cast<uint16_t*>(smem + OFF_VS) + slot * BN + 16 * w + rho;
-          vs[0] = fresh ? 0x3F80 : (uint16_t)vsc[0];
-          vs[8] = fresh ? 0x3F80 : (uint16_t)vsc[1];
-        }
-        __syncwarp();
-        if (lane == 0) mbar_arrive(bar(B_INFO + slot));
+        if (fresh && !(ok = info(nb))) break;
         if (nb >= 2 && !(ok = warp_wait(bar(B_KEMPTY + st), ((nb >> 1) - 1) & 1, &s_abort))) break;
-        const float by = pow2i(E_TOP - ek);
         if (!fresh) {
-          uint32_t s2[2], less24[2];
-#pragma unroll
-          for (int p = 0; p < 2; ++p) {
-            const float s = lo_f(ksc[p]) * by;
-            s2[p] = pack_f16x2(s, s);
-            less24[p] = pack_f16x2(-24.f * s, -24.f * s);
-          }
-          store(OFF_K + st * TILE_BYTES, kr, [&](int p, uint32_t v) { return scaled(v, s2[p], less24[p]); });
+          const uint2* ks = reinterpret_cast<const uint2*>(smem + OFF_KS) + slot * BN + 16 * w + rho;
+          const uint2 s[2] = {ks[0], ks[8]};
+          store(OFF_K + st * TILE_BYTES, kr, [&](int p, uint32_t v) { return scaled(v, s[p].x, s[p].y); });
         } else {
+          const float by = __uint_as_float(runs[slot * (BN / 16)]);
           store_new(OFF_K + st * TILE_BYTES, a.k_new, [&](const uint4& v) { return to_f16(v, by); });
         }
         done(B_KFULL + st);
         if (more) {
-          id = id_next;
-          fetch_k(blk + 1);
-          id_next = look_up(blk + 2);
-          ask(blk + AHEAD);
+          if (!(ok = info(nb + 1))) break;
+          run = runs[(nb + 1) % SLOTS * (BN / 16)];
+          fetch(a.kc, run, kr);
         }
         if (nb >= 2 && !(ok = warp_wait(bar(B_VEMPTY + st), ((nb >> 1) - 1) & 1, &s_abort))) break;
         if (!fresh) store(OFF_V + st * TILE_BYTES, vr, [](int, uint32_t v) { return numbers(v); });
         else store_new(OFF_V + st * TILE_BYTES, a.v_new, [](const uint4& v) { return v; });
         done(B_VFULL + st);
-        if (more) fetch_v(blk + 1);
+        if (more) fetch(a.vc, run, vr);
       }
     }
   } else {
