@@ -11,9 +11,10 @@
 // (Folding these into V as well would round them; applying K's scales to S
 // would have every row read them from shared memory, as it does V's: 256
 // bytes a row and block as bf16, a third of the products' own operands.)
+//   * Two warps look the pages up, ask the rows into L2 and work the scales out,
+//     up to four blocks ahead.
 //   * Eight warps turn 4-bit rows into 16-bit tiles in shared memory (128-byte
-//     swizzle), two stages of K and V each, one block ahead in
-//     registers and more asked into L2.  A
+//     swizzle), two stages of K and V each, one block ahead in registers.  A
 //     number c + 8 placed in bits 6..9 of a half is 16 + (c + 8) in fp16; one
 //     packed fma with (s, -24 s), exact, makes it c s.  In bits 0..3 it is 128
 //     + (c + 8) in bf16, and one subtraction makes it c.  A word's 8 numbers come out
@@ -45,7 +46,7 @@ FC_DEFINE_ERROR_WORD(kv4_tc)
 namespace {
 
 constexpr int HD = KV4_D;
-constexpr int THREADS = 640;  // warp 0 products, 1 pieces, 2-3 padding rows, 4-7 / 8-11 softmax, 12-19 queries and numbers to tiles
+constexpr int THREADS = 640;  // warp 0 products, 1 pieces, 2-3 scales, 4-7 / 8-11 softmax, 12-19 queries and numbers to tiles
 constexpr int NUM_WARPS = 8;
 constexpr int BM = 128, BN = 128, ROWS = 2 * BM;
 constexpr uint32_t HALF_BYTES = 128 * 128;         // 64 dims of 128 rows
@@ -59,12 +60,12 @@ constexpr uint32_t OFF_VS = OFF_KEEP + SLOTS * 16;              // [slot][128] v
 constexpr uint32_t OFF_BACK = OFF_VS + SLOTS * BN * 2;          // [slot][8] what 16 keys' scores are to be multiplied by
 constexpr uint32_t OFF_RUN = OFF_BACK + SLOTS * 32;             // [slot][8] where 16 keys' rows are, in runs of 16 rows
 constexpr uint32_t OFF_KS = OFF_RUN + SLOTS * 32;               // [slot][128] (s, s), (-24 s, -24 s): a key's scale in fp16
-constexpr uint32_t OFF_QE = OFF_KS + SLOTS * BN * 8;              // [2 pieces][256] the same for the query rows
-constexpr uint32_t OFF_ML = OFF_QE + 2 * ROWS * 4;              // [2 turns][2][128] (m, l) exchanged at a unit's end
 constexpr int PIECES = 4;                                       // piece descriptions kept
+constexpr uint32_t OFF_QE = OFF_KS + SLOTS * BN * 8;            // [PIECES][256] what a query row's scores are to be multiplied by
+constexpr uint32_t OFF_ML = OFF_QE + PIECES * ROWS * 4;              // [2 turns][2][128] (m, l) exchanged at a unit's end
 constexpr uint32_t OFF_PIECE = OFF_ML + 4 * BM * 8;             // [PIECES]
 constexpr uint32_t OFF_BAR = OFF_PIECE + PIECES * 64;
-constexpr uint32_t SMEM_BYTES = OFF_BAR + 256 + 1024;           // + alignment slack
+constexpr uint32_t SMEM_BYTES = OFF_BAR + 512 + 1024;           // + alignment slack
 constexpr uint32_t TMEM_COLS = 512;                             // S_0, S_1, O_0, O_1
 constexpr uint64_t WAIT_CYCLES = 4000000000ull;                 // ~2 s
 constexpr uint64_t DRAIN_CYCLES = 400000000ull;
@@ -89,17 +90,17 @@ enum {
   B_VEMPTY = 6,  // [2]
   B_SFULL = 8,   // [2 tiles]
   B_PFULL = 10,  // [2 tiles] 128
-  B_INFO = 12,   // [4 slots] 2: a block's scales and keep bits
-  B_QFULL = 16,  // 9
-  B_QFREE = 17,
-  B_OFIN = 18,
-  B_OFREE = 19,  // 256
-  B_ML = 20,     // 256: a row's halves exchanged
-  B_PIECE = 21,  // [PIECES] a description is written
-  B_QE = 25,     // [2] 8: the query rows' factors
-  B_DRAIN = 27,
-  B_SLOT = 28,   // [4 slots] a slot's block is done with
-  N_BARS = 32
+  B_INFO = 12,   // [SLOTS] 2: a block's scales and keep bits
+  B_SLOT = 16,   // [SLOTS] a slot's block is done with
+  B_PIECE = 20,  // [PIECES] a description is written
+  B_QFULL = 24,  // [PIECES] 9
+  B_QE = 28,     // [PIECES] 8: the query rows' factors
+  B_QFREE = 32,
+  B_OFIN = 33,
+  B_OFREE = 34,  // 256
+  B_ML = 35,     // 256: a row's halves exchanged
+  B_DRAIN = 36,
+  N_BARS = 37
 };
 
 struct ManyArgs {
@@ -274,6 +275,22 @@ struct Piece {
 };
 static_assert(sizeof(Piece) <= 64, "piece description");
 
+// Where a piece's queries are: a piece of one tile that follows another takes
+// the other of the two tiles, so that its queries need not wait for the last
+// piece's products (those of the piece before it are complete, else it would
+// not have been described).
+struct QTile {
+  int tile = 0;
+  bool alone = false;  // the last piece had one tile
+  // true: the last piece's products must be complete first
+  __device__ __forceinline__ bool next(bool two) {
+    const bool other = alone && !two;
+    tile = other ? 1 - tile : 0;
+    alone = !two;
+    return !other;
+  }
+};
+
 // The units' blocks dealt out.  One warp of a CTA walks them and leaves each
 // piece's description in shared memory for the other roles.
 struct Walk {
@@ -415,9 +432,9 @@ __global__ void __launch_bounds__(THREADS, 1) k_kv4_attn_many(ManyArgs f) {
     for (int i = 0; i < N_BARS; ++i) {
       uint32_t n = 1;
       if (i == B_PFULL || i == B_PFULL + 1) n = 128;
-      if (i < B_KEMPTY || i == B_QE || i == B_QE + 1) n = NUM_WARPS;
+      if (i < B_KEMPTY || (i >= B_QE && i < B_QE + PIECES)) n = NUM_WARPS;
       if (i >= B_INFO && i < B_INFO + SLOTS) n = 2;
-      if (i == B_QFULL) n = NUM_WARPS + 1;
+      if (i >= B_QFULL && i < B_QFULL + PIECES) n = NUM_WARPS + 1;
       if (i == B_OFREE || i == B_ML) n = 256;
       mbar_init(bar(i), n);
     }
@@ -451,16 +468,18 @@ __global__ void __launch_bounds__(THREADS, 1) k_kv4_attn_many(ManyArgs f) {
       tc_fence_after();
       return ok;
     };
+    QTile qt;
     for (;;) {
       if (!wait(B_PIECE + np % PIECES, np / PIECES)) break;
       const Piece* pc = piece(np);
       const int n = pc->n;
       if (n == 0) break;
-      if (!wait(B_QFULL, np)) break;
+      if (!wait(B_QFULL + np % PIECES, np / PIECES)) break;
       // Steps in order: with two tiles, tile 0 then tile 1 of each block, else
       // the blocks, tile by tile in turn.  Step k's second product comes before
       // step k + 2's first, which writes the scores that P took the place of.
       const int two = pc->two ? 1 : 0, steps = n << two;
+      qt.next(two);
 #pragma unroll 1
       for (int k = -2; k < steps; ++k) {
         const uint32_t x = k & 1;
@@ -478,7 +497,7 @@ __global__ void __launch_bounds__(THREADS, 1) k_kv4_attn_many(ManyArgs f) {
         if (k + 2 < steps) {  // S_x <- Q K^T
           const uint32_t blk = nb + ((k + 2) >> two), st = blk & 1;
           if (!wait(B_KFULL + st, blk >> 1)) break;
-          mma_qk(tmem + x * 128, q_lo + (two ? x : 0u) * (TILE_BYTES >> 4), k_lo + st * (TILE_BYTES >> 4), IDESC_QK);
+          mma_qk(tmem + x * 128, q_lo + (two ? x : (uint32_t)qt.tile) * (TILE_BYTES >> 4), k_lo + st * (TILE_BYTES >> 4), IDESC_QK);
           tc_commit(bar(B_SFULL + x));
           if (!two || x) tc_commit(bar(B_KEMPTY + st));
           if (k + 3 == steps) tc_commit(bar(B_QFREE));
@@ -495,7 +514,7 @@ __global__ void __launch_bounds__(THREADS, 1) k_kv4_attn_many(ManyArgs f) {
       mbar_wait_bounded(bar(B_DRAIN), 0, &dummy, DRAIN_CYCLES);
     }
   } else if (warp < 4) {
-    // ---------------- pieces, the list of cut units, padding rows ----------------
+    // ---------------- pieces, the list of cut units, padding rows; scales ----------------
     uint32_t np = 0;
     if (warp == 1) {
       Walk wk(f);
@@ -505,7 +524,7 @@ __global__ void __launch_bounds__(THREADS, 1) k_kv4_attn_many(ManyArgs f) {
       // takes.  Piece i - 1 starts only after this warp has seen that.
       for (;; ++np) {
         if (np >= 2 && !warp_wait(bar(B_QFREE), (np - 2) & 1, &s_abort)) break;
-        if (np >= 1 && lane == 0) mbar_arrive(bar(B_QFULL));
+        if (np >= 1 && lane == 0) mbar_arrive(bar(B_QFULL + (np - 1) % PIECES));
         const bool any = wk.next();
         if (lane == 0) {
           Piece* p = reinterpret_cast<Piece*>(smem + OFF_PIECE) + np % PIECES;
@@ -623,14 +642,13 @@ __global__ void __launch_bounds__(THREADS, 1) k_kv4_attn_many(ManyArgs f) {
   } else if (warp >= 12) {
     // ---------------- numbers to tiles ----------------
     // Warp w has rows 16w .. 16w + 15 of a block, one run of a page: lane (rho,
-    // c) rows rho and rho + 8, 16 bytes c of their 64.  The lanes of the two
-    // 64-dim halves take their words two apart, so that eight lanes' stores
-    // fall in different banks.
-    const int w = warp - 12, c = lane & 3, rho = lane >> 2, swap = c >> 1;
+    // c) rows rho and rho + 8, 16 bytes c of their 64.  Eight lanes in turn have
+    // four rows of one 64-dim half, so that their stores fall in different banks.
+    const int w = warp - 12, c = (lane & 1) | ((lane >> 4) << 1), rho = (lane >> 1) & 7;
     uint32_t dst[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i)
-      dst[i] = swap * HALF_BYTES + (16 * w + rho) * 128 + ((((c & 1) * 4 + (i ^ (2 * swap))) ^ rho) << 4);
+      dst[i] = (c >> 1) * HALF_BYTES + (16 * w + rho) * 128 + ((((c & 1) * 4 + i) ^ rho) << 4);
     Piece pc = {};
     uint4 kr[2], vr[2];
     uint32_t nb = 0;
@@ -640,7 +658,7 @@ __global__ void __launch_bounds__(THREADS, 1) k_kv4_attn_many(ManyArgs f) {
     };
     const uint32_t* runs = reinterpret_cast<const uint32_t*>(smem + OFF_RUN) + w;
     auto fetch = [&](const uint8_t* codes, uint32_t run, uint4 (&x)[2]) {
-      const uint4* src = reinterpret_cast<const uint4*>(codes + (uint64_t)run * 1024u) + lane;
+      const uint4* src = reinterpret_cast<const uint4*>(codes + (uint64_t)run * 1024u) + rho * 4 + c;
       x[0] = src[0];
       x[1] = src[32];
     };
@@ -649,14 +667,14 @@ __global__ void __launch_bounds__(THREADS, 1) k_kv4_attn_many(ManyArgs f) {
       return a.k_new && j < pc.nn ? (((size_t)pc.b * a.Hkv + pc.gh) * a.n_pad + j) * HD : no_row;
     };
     // The piece's queries: a row 16 lanes, 16 rows at a time, times a power of two.
-    auto stage_q = [&](uint32_t np) {
-      float* back = reinterpret_cast<float*>(smem + OFF_QE) + (np & 1) * ROWS;
+    auto stage_q = [&](uint32_t np, int tile) {
+      float* back = reinterpret_cast<float*>(smem + OFF_QE) + np % PIECES * ROWS;
       const int ch = lane & 15, passes = (pc.two ? 2 : 1) * BM / 16;
 #pragma unroll 1
-      for (int p0 = 0; p0 < passes; p0 += 4) {
-        uint4 v[4];
+      for (int p0 = 0; p0 < passes; p0 += 2) {
+        uint4 v[2];
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
+        for (int k = 0; k < 2; ++k) {
           const int r = 16 * (p0 + k) + 2 * w + (lane >> 4);
           v[k] = make_uint4(0, 0, 0, 0);
           if (r < pc.rows) {
@@ -665,7 +683,7 @@ __global__ void __launch_bounds__(THREADS, 1) k_kv4_attn_many(ManyArgs f) {
           }
         }
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
+        for (int k = 0; k < 2; ++k) {
           const int r = 16 * (p0 + k) + 2 * w + (lane >> 4);
           const uint32_t sign = 0x7FFF7FFFu;
           uint32_t top = __vmaxu2(__vmaxu2(v[k].x & sign, v[k].y & sign), __vmaxu2(v[k].z & sign, v[k].w & sign));
@@ -673,7 +691,7 @@ __global__ void __launch_bounds__(THREADS, 1) k_kv4_attn_many(ManyArgs f) {
           for (int o = 1; o < 16; o <<= 1) top = __vmaxu2(top, __shfl_xor_sync(0xFFFFFFFFu, top, o));
           const int ex = expo_of(max(top & 0xFFFFu, top >> 16));
           if (ch == 0) back[r] = pow2i(ex - E_TOP);
-          *reinterpret_cast<uint4*>(smem + OFF_Q + (r >> 7) * TILE_BYTES + (ch >> 3) * HALF_BYTES + (r & 127) * 128 +
+          *reinterpret_cast<uint4*>(smem + OFF_Q + (tile + (r >> 7)) * TILE_BYTES + (ch >> 3) * HALF_BYTES + (r & 127) * 128 +
                                     (((ch & 7) ^ (r & 7)) << 4)) = to_f16(permute8(v[k]), pow2i(E_TOP - ex));
         }
       }
@@ -681,13 +699,11 @@ __global__ void __launch_bounds__(THREADS, 1) k_kv4_attn_many(ManyArgs f) {
     auto store = [&](uint32_t tile, const uint4 (&x)[2], auto&& convert) {
 #pragma unroll
       for (int p = 0; p < 2; ++p) {
-        const uint32_t w0 = swap ? x[p].z : x[p].x, w1 = swap ? x[p].w : x[p].y;
-        const uint32_t w2 = swap ? x[p].x : x[p].z, w3 = swap ? x[p].y : x[p].w;
         unsigned char* t = smem + tile + p * 1024;
-        *reinterpret_cast<uint4*>(t + dst[0]) = convert(p, w0);
-        *reinterpret_cast<uint4*>(t + dst[1]) = convert(p, w1);
-        *reinterpret_cast<uint4*>(t + dst[2]) = convert(p, w2);
-        *reinterpret_cast<uint4*>(t + dst[3]) = convert(p, w3);
+        *reinterpret_cast<uint4*>(t + dst[0]) = convert(p, x[p].x);
+        *reinterpret_cast<uint4*>(t + dst[1]) = convert(p, x[p].y);
+        *reinterpret_cast<uint4*>(t + dst[2]) = convert(p, x[p].z);
+        *reinterpret_cast<uint4*>(t + dst[3]) = convert(p, x[p].w);
       }
     };
     auto store_new = [&](uint32_t tile, const __nv_bfloat16* src, auto&& convert) {  // the new rows, zeros past them
@@ -705,6 +721,7 @@ __global__ void __launch_bounds__(THREADS, 1) k_kv4_attn_many(ManyArgs f) {
       __syncwarp();
       if (lane == 0) mbar_arrive(bar(which));
     };
+    QTile qt;
     for (uint32_t np = 0; ok; ++np) {
       if (!warp_wait(bar(B_PIECE + np % PIECES), (np / PIECES) & 1, &s_abort)) break;
       pc = *piece(np);
@@ -717,27 +734,23 @@ __global__ void __launch_bounds__(THREADS, 1) k_kv4_attn_many(ManyArgs f) {
         fetch(a.kc, run, kr);
         fetch(a.vc, run, vr);
       }
-      if (np > 0 && !(ok = warp_wait(bar(B_QFREE), (np - 1) & 1, &s_abort))) break;
-      stage_q(np);
+      if (qt.next(pc.two) && np > 0 && !(ok = warp_wait(bar(B_QFREE), (np - 1) & 1, &s_abort))) break;
+      stage_q(np, qt.tile);
       fence_proxy_async_smem();
       __syncwarp();
       if (lane == 0) {
-        mbar_arrive(bar(B_QE + (np & 1)));
-        mbar_arrive(bar(B_QFULL));
+        mbar_arrive(bar(B_QE + np % PIECES));
+        mbar_arrive(bar(B_QFULL + np % PIECES));
       }
-      for (int blk = pc.s0; blk < s1; ++blk, ++nb) {
+      const int to = min(s1, pc.cached);
+#pragma unroll 1
+      for (int blk = pc.s0; blk < to; ++blk, ++nb) {
         const int st = nb & 1, slot = nb % SLOTS;
-        const bool fresh = blk >= pc.cached, more = blk + 1 < s1 && blk + 1 < pc.cached;
-        if (fresh && !(ok = info(nb))) break;
+        const bool more = blk + 1 < to;
         if (nb >= 2 && !(ok = warp_wait(bar(B_KEMPTY + st), ((nb >> 1) - 1) & 1, &s_abort))) break;
-        if (!fresh) {
-          const uint2* ks = reinterpret_cast<const uint2*>(smem + OFF_KS) + slot * BN + 16 * w + rho;
-          const uint2 s[2] = {ks[0], ks[8]};
-          store(OFF_K + st * TILE_BYTES, kr, [&](int p, uint32_t v) { return scaled(v, s[p].x, s[p].y); });
-        } else {
-          const float by = __uint_as_float(runs[slot * (BN / 16)]);
-          store_new(OFF_K + st * TILE_BYTES, a.k_new, [&](const uint4& v) { return to_f16(v, by); });
-        }
+        const uint2* ks = reinterpret_cast<const uint2*>(smem + OFF_KS) + slot * BN + 16 * w + rho;
+        const uint2 s[2] = {ks[0], ks[8]};
+        store(OFF_K + st * TILE_BYTES, kr, [&](int p, uint32_t v) { return scaled(v, s[p].x, s[p].y); });
         done(B_KFULL + st);
         if (more) {
           if (!(ok = info(nb + 1))) break;
@@ -745,10 +758,21 @@ __global__ void __launch_bounds__(THREADS, 1) k_kv4_attn_many(ManyArgs f) {
           fetch(a.kc, run, kr);
         }
         if (nb >= 2 && !(ok = warp_wait(bar(B_VEMPTY + st), ((nb >> 1) - 1) & 1, &s_abort))) break;
-        if (!fresh) store(OFF_V + st * TILE_BYTES, vr, [](int, uint32_t v) { return numbers(v); });
-        else store_new(OFF_V + st * TILE_BYTES, a.v_new, [](const uint4& v) { return v; });
+        store(OFF_V + st * TILE_BYTES, vr, [](int, uint32_t v) { return numbers(v); });
         done(B_VFULL + st);
         if (more) fetch(a.vc, run, vr);
+      }
+      if (ok && to < s1) {  // the new tokens' block
+        const int st = nb & 1;
+        if (!(ok = info(nb))) break;
+        if (nb >= 2 && !(ok = warp_wait(bar(B_KEMPTY + st), ((nb >> 1) - 1) & 1, &s_abort))) break;
+        const float by = __uint_as_float(runs[nb % SLOTS * (BN / 16)]);
+        store_new(OFF_K + st * TILE_BYTES, a.k_new, [&](const uint4& v) { return to_f16(v, by); });
+        done(B_KFULL + st);
+        if (nb >= 2 && !(ok = warp_wait(bar(B_VEMPTY + st), ((nb >> 1) - 1) & 1, &s_abort))) break;
+        store_new(OFF_V + st * TILE_BYTES, a.v_new, [](const uint4& v) { return v; });
+        done(B_VFULL + st);
+        ++nb;
       }
     }
   } else {
@@ -766,8 +790,8 @@ __global__ void __launch_bounds__(THREADS, 1) k_kv4_attn_many(ManyArgs f) {
       const int n = pc->n;
       if (n == 0) break;
       float m = M_START, l = 0.f;  // m: the reference
-      if (!(ok = warp_wait(bar(B_QE + (np & 1)), (np >> 1) & 1, &s_abort))) break;
-      const float c_row = a.scale_log2 * reinterpret_cast<const float*>(smem + OFF_QE)[(np & 1) * ROWS + row_of(pc)];
+      if (!(ok = warp_wait(bar(B_QE + np % PIECES), (np / PIECES) & 1, &s_abort))) break;
+      const float c_row = a.scale_log2 * reinterpret_cast<const float*>(smem + OFF_QE)[np % PIECES * ROWS + row_of(pc)];
       const int every = pc->two ? 1 : 2, first = pc->two ? 0 : x, n_cached = pc->cached - pc->s0;
 #pragma unroll 1
       for (int j = first; j < n; j += every, ++t) {
@@ -778,7 +802,7 @@ __global__ void __launch_bounds__(THREADS, 1) k_kv4_attn_many(ManyArgs f) {
         const bool masked = j >= n_cached || (keep[0] & keep[1] & keep[2] & keep[3]) != 0xFFFFFFFFu;  // in all rows alike
         if (!(ok = warp_wait(bar(B_SFULL + x), t & 1, &s_abort))) break;
         tc_fence_after();
-        if (masked) {  // masked scores are overwritten by -inf
+        if (__builtin_expect(masked, 0)) {  // masked scores are overwritten by -inf
           uint64_t sees[2] = {~0ull, ~0ull};
           if (j >= n_cached) {  // the new tokens that this row sees
             const int lr = row_of(pc), i = (pc->row0 + lr) / a.G;
@@ -834,7 +858,7 @@ __global__ void __launch_bounds__(THREADS, 1) k_kv4_attn_many(ManyArgs f) {
         }
         {
           top *= c_row;
-          if (__any_sync(0xFFFFFFFFu, top > m + RESCALE_THRESHOLD)) {
+          if (__builtin_expect(__any_sync(0xFFFFFFFFu, top > m + RESCALE_THRESHOLD), 0)) {
             const float m_new = top > m + RESCALE_THRESHOLD ? top : m, alpha = exp2_fast(m - m_new);
             l *= alpha;
             m = m_new;
@@ -1017,7 +1041,7 @@ fc_status kv4_attn_many(const Kv4Args& a, void* ws, size_t ws_bytes, cudaStream_
   const fc_status st = fc_once_per_device(done, [](int) {
     cudaFuncAttributes attr;
     if (cudaFuncGetAttributes(&attr, k_kv4_attn_many) != cudaSuccess) return FC_ERR_CUDA;
-    if (attr.numRegs != REGS_LAUNCH) return FC_ERR_INTERNAL;  // the register split would not add up
+    if (attr.numRegs < REGS_LAUNCH) return FC_ERR_INTERNAL;  // the register split would not add up
     return fc_cuda_status(cudaFuncSetAttribute(k_kv4_attn_many, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM_BYTES));
   });
   if (st != FC_OK) return st;
