@@ -757,7 +757,11 @@ fc_status fc_kv4_read(const fc_kv4_cache* cache, const int32_t* d_slot, int rows
  * softmax are fp32; probabilities are rounded to bf16 for the second product.
  * A length or node count out of range, or a page id outside the pool, records
  * FC_ERR_INVALID_ARG (that request's rows are zeros; that page's keys are
- * left out).  What a page holds past a request's end is not looked at.
+ * left out).  What a page holds past a request's end is not looked at.  A new
+ * token with a NaN or an infinity, or a cached row that stands for NaN, makes
+ * NaN of the rows that see it, and of no others.  With more than 16 rows a kv
+ * head (n_pad * H / Hkv) keys enter the products in fp16 relative to the
+ * largest of 16 neighbours: one smaller than 2^-20 of that loses bits.
  */
 fc_status fc_kv4_attn(const void* d_q, const fc_kv4_cache* cache, const int32_t* d_table, int max_pages,
                       const int32_t* d_kv_len, const void* d_k_new, const void* d_v_new, const uint64_t* d_mask,

@@ -520,7 +520,7 @@ __global__ void __launch_bounds__(FEW_THREADS, NT == 1 ? 2 : 1) k_kv4_attn_few(F
         }
       }
       const int words = (a.n_pad + 63) / 64;
-      uint32_t pb[NT][2];
+      uint32_t pb[NT][2], seen = 0, bad = 0;  // bits 4n + c: z[n][c]'s key is seen; bits j: values of token j are not finite
       const float one[4] = {1.f, 1.f, 0.f, 0.f};
       const float by[4] = {a.scale_log2, a.scale_log2, 1.f, 1.f};
 #pragma unroll
@@ -531,6 +531,7 @@ __global__ void __launch_bounds__(FEW_THREADS, NT == 1 ? 2 : 1) k_kv4_attn_few(F
           const int r = 8 * n + 2 * t + (c & 1), j = g + 8 * (c >> 1), i = r / a.G;
           bool sees = r < R && j < nn;
           if (sees) sees = a.mask ? (a.mask[((size_t)b * a.n_pad + i) * words] >> j) & 1 : j <= i;
+          seen |= (sees ? 1u : 0u) << (4 * n + c);
           zz[c >> 1][c & 1] = sees ? z[n][c] : -INFINITY;
           zz[2 + (c >> 1)][c & 1] = -INFINITY;
         }
@@ -546,6 +547,15 @@ __global__ void __launch_bounds__(FEW_THREADS, NT == 1 ? 2 : 1) k_kv4_attn_few(F
         for (int k = 0; k < 4; ++k) {
           const int j = 2 * t + (k & 1) + 8 * (k >> 1);
           v[k] = j < nn ? reinterpret_cast<const uint4*>(a.v_new + (nrow + j) * HD)[2 * g + h] : zero;
+          // a value that is not finite becomes 0, as no weight of 0 would take
+          // it out of the rows that do not see its token; those that do are NaN
+          uint32_t* w = &v[k].x;
+#pragma unroll
+          for (int u = 0; u < 4; ++u) {
+            const uint32_t not_finite = __vcmpgeu2(w[u] & 0x7FFF7FFFu, 0x7F807F80u);
+            w[u] &= ~not_finite;
+            if (not_finite) bad |= 1u << j;
+          }
         }
 #pragma unroll
         for (int u = 0; u < 4; ++u) {
@@ -555,6 +565,14 @@ __global__ void __launch_bounds__(FEW_THREADS, NT == 1 ? 2 : 1) k_kv4_attn_few(F
 #pragma unroll
           for (int n = 0; n < NT; ++n) mma_bf16(o[n][4 * h + u], a0, a1, a2, a3, pb[n][0], pb[n][1]);
         }
+      }
+      bad = __reduce_or_sync(0xFFFFFFFFu, bad);
+      if (bad) {
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+          for (int c = 0; c < 4; ++c)
+            if (((seen >> (4 * n + c)) & 1u) && ((bad >> (g + 8 * (c >> 1))) & 1u)) l[n][c & 1] = __uint_as_float(0x7FC00000u);
       }
     }
 
@@ -765,7 +783,7 @@ extern "C" fc_status fc_kv4_attn(const void* d_q, const fc_kv4_cache* cache, con
             scale * 1.4426950408889634f,
             fc_error_slot()};
   cudaStream_t s = static_cast<cudaStream_t>(stream);
-  if ((long long)batch * a.Hkv > 0x7FFFFFFFll) return FC_ERR_UNSUPPORTED;
+  if ((long long)batch * a.Hkv > 1ll << 30) return FC_ERR_UNSUPPORTED;
   if (n_pad * a.G <= 8) return launch_few<1>(a, d_ws, ws_bytes, s);
   if (n_pad * a.G <= 16) return launch_few<2>(a, d_ws, ws_bytes, s);
   return kv4_attn_many(a, d_ws, ws_bytes, s);

@@ -63,7 +63,8 @@ constexpr uint32_t OFF_KS = OFF_RUN + SLOTS * 32;               // [slot][128] (
 constexpr int PIECES = 4;                                       // piece descriptions kept
 constexpr uint32_t OFF_QE = OFF_KS + SLOTS * BN * 8;            // [PIECES][256] what a query row's scores are to be multiplied by
 constexpr uint32_t OFF_ML = OFF_QE + PIECES * ROWS * 4;              // [2 turns][2][128] (m, l) exchanged at a unit's end
-constexpr uint32_t OFF_PIECE = OFF_ML + 4 * BM * 8;             // [PIECES]
+constexpr uint32_t OFF_BAD = OFF_ML + 4 * BM * 8;               // [PIECES][8] bits of the new tokens whose values are not finite
+constexpr uint32_t OFF_PIECE = OFF_BAD + PIECES * 16;           // [PIECES]
 constexpr uint32_t OFF_BAR = OFF_PIECE + PIECES * 64;
 constexpr uint32_t SMEM_BYTES = OFF_BAR + 512 + 1024;           // + alignment slack
 constexpr uint32_t TMEM_COLS = 512;                             // S_0, S_1, O_0, O_1
@@ -712,7 +713,7 @@ __global__ void __launch_bounds__(THREADS, 1) k_kv4_attn_many(ManyArgs f) {
         const int j = 16 * w + (e >> 4), ch = e & 15;
         const size_t row = new_row(j);
         uint4 v = make_uint4(0, 0, 0, 0);
-        if (row != no_row) v = convert(permute8(reinterpret_cast<const uint4*>(src + row)[ch]));
+        if (row != no_row) v = convert(permute8(reinterpret_cast<const uint4*>(src + row)[ch]), e >> 4);
         *reinterpret_cast<uint4*>(smem + tile + (ch >> 3) * HALF_BYTES + j * 128 + (((ch & 7) ^ (j & 7)) << 4)) = v;
       }
     };
@@ -767,10 +768,22 @@ __global__ void __launch_bounds__(THREADS, 1) k_kv4_attn_many(ManyArgs f) {
         if (!(ok = info(nb))) break;
         if (nb >= 2 && !(ok = warp_wait(bar(B_KEMPTY + st), ((nb >> 1) - 1) & 1, &s_abort))) break;
         const float by = __uint_as_float(runs[nb % SLOTS * (BN / 16)]);
-        store_new(OFF_K + st * TILE_BYTES, a.k_new, [&](const uint4& v) { return to_f16(v, by); });
+        store_new(OFF_K + st * TILE_BYTES, a.k_new, [&](const uint4& v, int) { return to_f16(v, by); });
         done(B_KFULL + st);
         if (nb >= 2 && !(ok = warp_wait(bar(B_VEMPTY + st), ((nb >> 1) - 1) & 1, &s_abort))) break;
-        store_new(OFF_V + st * TILE_BYTES, a.v_new, [](const uint4& v) { return v; });
+        // A value that is not finite becomes 0, as no weight of 0 would take it
+        // out of the rows that do not see its token; those that do are NaN.
+        uint32_t bad = 0;
+        store_new(OFF_V + st * TILE_BYTES, a.v_new, [&](const uint4& v, int j) {
+          auto finite = [&](uint32_t x) {
+            const uint32_t not_finite = __vcmpgeu2(x & 0x7FFF7FFFu, 0x7F807F80u);
+            if (not_finite) bad |= 1u << j;
+            return x & ~not_finite;
+          };
+          return make_uint4(finite(v.x), finite(v.y), finite(v.z), finite(v.w));
+        });
+        bad = __reduce_or_sync(0xFFFFFFFFu, bad);
+        if (lane == 0) reinterpret_cast<uint16_t*>(smem + OFF_BAD)[np % PIECES * NUM_WARPS + w] = (uint16_t)bad;
         done(B_VFULL + st);
         ++nb;
       }
@@ -784,6 +797,20 @@ __global__ void __launch_bounds__(THREADS, 1) k_kv4_attn_many(ManyArgs f) {
     uint32_t nb = 0, np = 0, nx = 0, t = 0;
     bool ok = true;
     auto row_of = [&](const Piece* pc) { return pc->two ? x * BM + r : r; };  // row of the piece
+    auto seen = [&](const Piece* pc, uint64_t (&sees)[2]) {  // the new tokens that the row sees
+      const int lr = row_of(pc), i = (pc->row0 + lr) / a.G;
+      if (lr >= pc->rows) {
+        sees[0] = sees[1] = 0;
+      } else if (a.mask) {
+        const int words = (a.n_pad + 63) / 64;
+        const uint64_t* mr = a.mask + ((size_t)pc->b * a.n_pad + i) * words;
+        sees[0] = mr[0];
+        sees[1] = words > 1 ? mr[1] : 0ull;
+      } else {
+        sees[0] = i >= 63 ? ~0ull : (1ull << (i + 1)) - 1ull;
+        sees[1] = i < 64 ? 0ull : (i >= 127 ? ~0ull : (1ull << (i - 63)) - 1ull);
+      }
+    };
     for (;;) {
       if (!(ok = warp_wait(bar(B_PIECE + np % PIECES), (np / PIECES) & 1, &s_abort))) break;
       const Piece* pc = piece(np);
@@ -804,20 +831,7 @@ __global__ void __launch_bounds__(THREADS, 1) k_kv4_attn_many(ManyArgs f) {
         tc_fence_after();
         if (__builtin_expect(masked, 0)) {  // masked scores are overwritten by -inf
           uint64_t sees[2] = {~0ull, ~0ull};
-          if (j >= n_cached) {  // the new tokens that this row sees
-            const int lr = row_of(pc), i = (pc->row0 + lr) / a.G;
-            if (lr >= pc->rows) {
-              sees[0] = sees[1] = 0;
-            } else if (a.mask) {
-              const int words = (a.n_pad + 63) / 64;
-              const uint64_t* mr = a.mask + ((size_t)pc->b * a.n_pad + i) * words;
-              sees[0] = mr[0];
-              sees[1] = words > 1 ? mr[1] : 0ull;
-            } else {
-              sees[0] = i >= 63 ? ~0ull : (1ull << (i + 1)) - 1ull;
-              sees[1] = i < 64 ? 0ull : (i >= 127 ? ~0ull : (1ull << (i - 63)) - 1ull);
-            }
-          }
+          if (j >= n_cached) seen(pc, sees);
 #pragma unroll 1
           for (int q = 0; q < 4; ++q) {
             const uint32_t k = keep[q] & (uint32_t)(sees[q >> 1] >> (32 * (q & 1)));
@@ -923,6 +937,14 @@ __global__ void __launch_bounds__(THREADS, 1) k_kv4_attn_many(ManyArgs f) {
       const bool row_ok = lr < pc->rows;
       __nv_bfloat16* dst = a.out + (((size_t)pc->b * a.n_pad + (row_ok ? i : 0)) * a.H + pc->gh * a.G + hh) * HD;
       const size_t slot = (size_t)pc->slot * f.rows_cap + lr;
+      if (n > n_cached) {  // new tokens: are all values finite?
+        const uint64_t* bad = reinterpret_cast<const uint64_t*>(smem + OFF_BAD) + np % PIECES * 2;
+        if (bad[0] | bad[1]) {
+          uint64_t sees[2];
+          seen(pc, sees);
+          if ((sees[0] & bad[0]) | (sees[1] & bad[1])) l = __uint_as_float(0x7FC00000u);
+        }
+      }
       float m_all = m, k0 = 1.f, k1 = 0.f;
       uint32_t tO0 = tO;
       if (!two) {

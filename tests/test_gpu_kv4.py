@@ -355,6 +355,30 @@ def test_attn_rows_past_the_nodes_and_a_request_without_nodes(fc):
     assert not out[0].any() and not out[2, 3:].any() and out[1].any()
 
 
+@pytest.mark.parametrize("n,H,G", [(3, 4, 2), (7, 4, 2), (40, 4, 2), (70, 4, 2), (128, 4, 2)])
+def test_attn_what_is_not_finite_stays_with_the_rows_that_see_it(fc, n, H, G):
+    """New tokens with a NaN or an infinity among their keys or values: rows
+    that see them are NaN, the others what they are without them."""
+    c = attn_case(n + 9, 2, n, H, G, [300, 9000], 64)
+    c["v_new"][0, 0, n - 1, 5] = float("nan")
+    c["v_new"][1, :, n // 2, 77] = -float("inf")
+    c["k_new"][1, 0, 1, 3] = float("nan")
+    hit = np.zeros((2, n, H), bool)
+    hit[0, :, :H // G] = c["sees"][0, :, n - 1, None]
+    hit[1] = c["sees"][1, :, n // 2, None]
+    hit[1, :, :H // G] |= c["sees"][1, :, 1, None]
+    assert hit.any() and not hit.all()
+    for ws in (True, False):
+        got = num(run_attn(fc, c, ws=ws))
+        assert np.isnan(got[hit]).all() and np.isfinite(got[~hit]).all()
+        d = dict(c, v_new=torch.where(c["v_new"].isfinite(), c["v_new"], 0), k_new=torch.where(c["k_new"].isfinite(), c["k_new"], 0))
+        ref, size = o4.attn(num(d["q"]), *(o4.pack(x) for x in d["codes"]), *d["scales"], d["table"], d["lens"],
+                            num(d["k_new"]), num(d["v_new"]), d["sees"], d["nodes"], d["scale"])
+        bad = np.abs(got - ref) - 2.0 ** -8 * np.abs(ref) - size * (2.0 ** -8 + 2.0 ** -10)
+        assert bad[~hit].max() <= 0
+    assert fc.fc_get_error() == "FC_OK"
+
+
 @pytest.mark.parametrize("n,L", [(1, 40000), (4, 20000), (70, 6000)])
 def test_attn_long_and_split(fc, n, L):
     """Few requests with many keys: the keys are split and the parts joined,
