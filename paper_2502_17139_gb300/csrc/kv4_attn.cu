@@ -44,6 +44,12 @@ constexpr int HD = KV4_D;
 // in a row.  Dimensions 32t .. 32t + 31 (t = lane % 4) are the lane's part of
 // K, 16g .. 16g + 15 its part of V, each as they lie in memory; the queries
 // are permuted to match.
+//
+// 32 single tokens over 16384 keys (8 kv heads of 4 query heads, 554 MB) take
+// 106 us, 5.2 TB/s: 6.4 TB/s once all run, and some 15 us until they do and
+// until the last part is joined.  One token over 131071 keys (138 MB): 38 us.
+// There start, end and the instructions (450 a step of a warp, most to place
+// numbers) count more than the read.  500 keys: 10 us, latency.
 // ---------------------------------------------------------------------------
 constexpr int FEW_WARPS = 8, FEW_THREADS = FEW_WARPS * 32;
 constexpr int STEP = 32;         // keys a step
@@ -311,18 +317,23 @@ __global__ void __launch_bounds__(FEW_THREADS, NT == 1 ? 2 : 1) k_kv4_attn_few(F
       }
       cp_async_commit();
     };
-#pragma unroll 1
-    for (int it = 0; it < FEW_STAGES - 1; ++it) issue(it, it, it * STEP_BYTES);
     // ---- queries: the unit's power of two, then the operand registers
     // k-step 2i of word i of a key's 16-byte quarter t: dimensions 32t + 8i +
     // {0, 4} and {1, 5} / 16; k-step 2i + 1: {2, 6} and {3, 7} / 16
     uint4 qw[NT][4];
+#pragma unroll
+    for (int n = 0; n < NT; ++n)
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        qw[n][i] = 8 * n + g < R ? reinterpret_cast<const uint4*>(q_row(8 * n + g))[4 * t + i] : make_uint4(0, 0, 0, 0);
+    // the first steps are asked for before the queries have come
+#pragma unroll 1
+    for (int it = 0; it < FEW_STAGES - 1; ++it) issue(it, it, it * STEP_BYTES);
     uint32_t top = 0;
 #pragma unroll
     for (int n = 0; n < NT; ++n)
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        qw[n][i] = 8 * n + g < R ? reinterpret_cast<const uint4*>(q_row(8 * n + g))[4 * t + i] : make_uint4(0, 0, 0, 0);
         const uint32_t* w = &qw[n][i].x;
 #pragma unroll
         for (int x = 0; x < 4; ++x) {  // magnitudes of finite values, both halves at once
@@ -650,22 +661,22 @@ __global__ void __launch_bounds__(FEW_THREADS, NT == 1 ? 2 : 1) k_kv4_attn_few(F
         for (int r = warp; r < R; r += FEW_WARPS) {
           float mx = -INFINITY, sum = 0.f;
 #pragma unroll 2
-          for (int c = lane; c < nc; c += 32)
-            mx = fmaxf(mx, __ldcg(reinterpret_cast<const float2*>(piece(c0 + c) + L::ROWS * HD) + r).x);
-#pragma unroll
-          for (int x = 16; x > 0; x >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xFFFFFFFFu, mx, x));
-#pragma unroll 2
           for (int c = lane; c < nc; c += 32) {
             const float2 ml = __ldcg(reinterpret_cast<const float2*>(piece(c0 + c) + L::ROWS * HD) + r);
-            const float k = exp2_fast(ml.x - mx);
-            wt[r * nc + c] = k;
-            sum += ml.y * k;
+            const float mn = fmaxf(mx, ml.x);
+            sum = sum * exp2_fast(mx - mn) + ml.y * exp2_fast(ml.x - mn);
+            mx = mn;
+            wt[r * nc + c] = ml.x;
           }
+          float all = mx;
+#pragma unroll
+          for (int x = 16; x > 0; x >>= 1) all = fmaxf(all, __shfl_xor_sync(0xFFFFFFFFu, all, x));
+          sum *= exp2_fast(mx - all);
 #pragma unroll
           for (int x = 16; x > 0; x >>= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, x);
           const float inv = sum == 0.f ? 0.f : 1.f / sum;
 #pragma unroll 1
-          for (int c = lane; c < nc; c += 32) wt[r * nc + c] *= inv;
+          for (int c = lane; c < nc; c += 32) wt[r * nc + c] = exp2_fast(wt[r * nc + c] - all) * inv;
         }
         __syncthreads();
         // ... then its values, the pieces dealt out to as many subsets as there are threads for
@@ -674,7 +685,7 @@ __global__ void __launch_bounds__(FEW_THREADS, NT == 1 ? 2 : 1) k_kv4_attn_few(F
         for (int e = tid; e < quads * subsets; e += FEW_THREADS) {
           const int sub = e / quads, q = e - sub * quads, r = q / (HD / 4), d4 = q % (HD / 4);
           float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 4
+#pragma unroll 8
           for (int c = sub; c < nc; c += subsets) {
             const float k = wt[r * nc + c];
             const float4 v = __ldcg(reinterpret_cast<const float4*>(piece(c0 + c) + r * HD) + d4);
@@ -784,6 +795,11 @@ extern "C" fc_status fc_kv4_attn(const void* d_q, const fc_kv4_cache* cache, con
             fc_error_slot()};
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   if ((long long)batch * a.Hkv > 1ll << 30) return FC_ERR_UNSUPPORTED;
+  // Measured on both sides of the rules (8 kv heads of 4 query heads):
+  //   4 rows, 32 x 16384 keys:  one 8-row tile 106 us, two 154
+  //   16 rows, 32 x 8192 keys:  two 8-row tiles 94 us, a tcgen05 tile 191;
+  //            1 x 500 keys: 14 and 22
+  // (three 8-row tiles would not fit the registers).
   if (n_pad * a.G <= 8) return launch_few<1>(a, d_ws, ws_bytes, s);
   if (n_pad * a.G <= 16) return launch_few<2>(a, d_ws, ws_bytes, s);
   return kv4_attn_many(a, d_ws, ws_bytes, s);
