@@ -120,6 +120,10 @@ __device__ __forceinline__ void cp_async_wait() {
 // AHEAD tiles ahead in registers; with ks = 1 a sum never leaves its warp, else
 // the ks warps' sums meet in shared memory.  NT: 8-row tiles of x.  STEPS:
 // k-steps that share a scale (the group, or the whole tile).
+// x goes two tiles ahead: four took 64 registers of 16 rows' form, and 12 x
+// 8192 x 8192 22.6 us instead of 18.5; one row is the same either way.
+// Measured: 16 x 8192 x 28672 47 us (126 MB), a row of it 39 us (3.1 TB/s), of
+// 2048 x 32256 14 us, of 2048 x 2048 6 us (latency).
 constexpr int STAGES = 8;
 // codes of MT tiles, then the scales [group][MT * TN]
 __host__ __device__ constexpr int stage_bytes(int MT, int STEPS) { return MT * TILE_BYTES + MT * TN * 2 * (4 / STEPS); }
@@ -130,7 +134,7 @@ __global__ void __launch_bounds__(MAX_WARPS * 32) k_w4_matvec(const uint4* __res
                                                               int gshift, int ks, __nv_bfloat16* __restrict__ y) {
   extern __shared__ __align__(16) unsigned char smem[];  // rings; then the sums
   constexpr int GROUPS = 4 / STEPS, OFF_SC = MT * TILE_BYTES, STAGE_BYTES = stage_bytes(MT, STEPS);
-  constexpr int AHEAD = 4;
+  constexpr int AHEAD = 2;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3, warps = blockDim.x >> 5;
   const int kt = K / TK, part = warp % ks, tile0 = (blockIdx.x * (warps / ks) + warp / ks) * MT;
   const int n_tiles = (N + TN - 1) / TN;
