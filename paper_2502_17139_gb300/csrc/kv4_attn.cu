@@ -769,7 +769,7 @@ extern "C" fc_status fc_kv4_attn(const void* d_q, const fc_kv4_cache* cache, con
   if (!shape_ok(n_pad, H, cache->Hkv)) return FC_ERR_UNSUPPORTED;
   if (batch == 0) return FC_OK;
   if (!d_q || !d_table || !d_kv_len || !d_out || !aligned(d_q, 16) || !aligned(d_out, 16) || !d_k_new != !d_v_new ||
-      !aligned(d_k_new, 16) || !aligned(d_v_new, 16) || (d_ws && !aligned(d_ws, 256)))
+      !aligned(d_k_new, 16) || !aligned(d_v_new, 16) || !aligned(d_mask, 8) || (d_ws && !aligned(d_ws, 256)))
     return FC_ERR_INVALID_ARG;
   Kv4Args a{static_cast<const __nv_bfloat16*>(d_q),
             static_cast<const uint8_t*>(cache->k_codes),

@@ -361,7 +361,7 @@ extern "C" fc_status fc_w4_matvec(const void* d_x, const void* d_codes, const vo
   if (M < 0 || K < 1 || N < 1) return FC_ERR_INVALID_ARG;
   if (M > 16 || !shape_ok(K, N, group)) return FC_ERR_UNSUPPORTED;
   if (M == 0) return FC_OK;
-  if (!d_x || !d_codes || !d_scale || !d_y || !aligned(d_x, 16) || !aligned(d_codes, 16) || !aligned(d_scale, 2) ||
+  if (!d_x || !d_codes || !d_scale || !d_y || !aligned(d_x, 16) || !aligned(d_codes, 16) || !aligned(d_scale, 16) ||
       !aligned(d_y, 2))
     return FC_ERR_INVALID_ARG;
   cudaStream_t s = static_cast<cudaStream_t>(stream);

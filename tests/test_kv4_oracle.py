@@ -107,6 +107,16 @@ def test_host_refusals(fc):
     assert L.fc_w4_matvec(nul, nul, nul, 0, 128, 64, 64, nul, nul) == 0
 
 
+def test_host_refuses_pointers_that_a_wide_load_would_fault_on(fc):
+    L, nul = fc.LIB, None
+    ref = C.byref(fc.fc_kv4_cache(256, 256, 256, 256, 10, 64, 8, 128))
+    for mask in (12, 20):  # masks are read as 64-bit words
+        assert L.fc_kv4_attn(16, ref, 16, 4, 16, 16, 16, mask, nul, 1, 1, 8, C.c_float(0.1), 16, nul, 0, nul) == 1
+    for scale in (18, 20, 24):  # scales are fetched two and more at a time
+        assert L.fc_w4_matvec(16, 16, scale, 4, 128, 64, 64, 16, nul) == 1
+    assert L.fc_w4_matvec(16, 16, 16, 4, 128, 64, 64, 17, nul) == 1
+
+
 def test_binding_refusals(fc):
     t = lambda *s, dt=torch.int32: torch.zeros(s, dtype=dt)
     with pytest.raises((TypeError, ValueError)):
