@@ -9,8 +9,7 @@
 // one per 16 keys) keep them in range.  The second is in bf16, P needing
 // its range: V the whole numbers -7..7, their scales multiplied into P.
 // (Folding these into V as well would round them; applying K's scales to S
-// would have every row read them from shared memory, as it does V's: 256
-// bytes a row and block as bf16, a third of the products' own operands.)
+// would have every row read them from shared memory, as it does V's.)
 //   * Two warps look the pages up, ask the rows into L2 and work the scales out,
 //     up to four blocks ahead.
 //   * Eight warps turn 4-bit rows into 16-bit tiles in shared memory (128-byte
@@ -57,7 +56,7 @@ constexpr uint32_t OFF_V = OFF_K + 2 * TILE_BYTES;
 constexpr int SLOTS = 4;                                        // blocks whose scales and keep bits are kept
 constexpr uint32_t OFF_KEEP = OFF_V + 2 * TILE_BYTES;           // [slot][4] bits of the keys that count
 constexpr uint32_t OFF_VS = OFF_KEEP + SLOTS * 16;              // [slot][128] value scales, bf16
-constexpr uint32_t OFF_BACK = OFF_VS + SLOTS * BN * 2;          // [slot][8] what 16 keys' scores are to be multiplied by
+constexpr uint32_t OFF_BACK = OFF_VS + SLOTS * BN * 4;          // [slot][8] what 16 keys' scores are to be multiplied by
 constexpr uint32_t OFF_RUN = OFF_BACK + SLOTS * 32;             // [slot][8] where 16 keys' rows are, in runs of 16 rows
 constexpr uint32_t OFF_KS = OFF_RUN + SLOTS * 32;               // [slot][128] (s, s), (-24 s, -24 s): a key's scale in fp16
 constexpr int PIECES = 4;                                       // piece descriptions kept
@@ -90,7 +89,7 @@ enum {
   B_KEMPTY = 4,  // [2]
   B_VEMPTY = 6,  // [2]
   B_SFULL = 8,   // [2 tiles]
-  B_PFULL = 10,  // [2 tiles] 128
+  B_PFULL = 10,  // [2 tiles] 4
   B_INFO = 12,   // [SLOTS] 2: a block's scales and keep bits
   B_SLOT = 16,   // [SLOTS] a slot's block is done with
   B_PIECE = 20,  // [PIECES] a description is written
@@ -432,7 +431,7 @@ __global__ void __launch_bounds__(THREADS, 1) k_kv4_attn_many(ManyArgs f) {
     s_abort = 0;
     for (int i = 0; i < N_BARS; ++i) {
       uint32_t n = 1;
-      if (i == B_PFULL || i == B_PFULL + 1) n = 128;
+      if (i == B_PFULL || i == B_PFULL + 1) n = 4;
       if (i < B_KEMPTY || (i >= B_QE && i < B_QE + PIECES)) n = NUM_WARPS;
       if (i >= B_INFO && i < B_INFO + SLOTS) n = 2;
       if (i >= B_QFULL && i < B_QFULL + PIECES) n = NUM_WARPS + 1;
@@ -630,7 +629,7 @@ __global__ void __launch_bounds__(THREADS, 1) k_kv4_attn_many(ManyArgs f) {
             reinterpret_cast<float*>(smem + OFF_BACK)[slot * (BN / 16) + run_i] = pow2i(ek - E_TOP);
             reinterpret_cast<uint32_t*>(smem + OFF_RUN)[slot * (BN / 16) + run_i] = fresh ? __float_as_uint(by) : run_now;
           }
-          reinterpret_cast<uint32_t*>(smem + OFF_VS)[slot * (BN / 2) + i] = v2;
+          reinterpret_cast<float2*>(smem + OFF_VS)[slot * (BN / 2) + i] = make_float2(lo_f(v2), hi_f(v2));
           const float f0 = lo_f(k0) * by, f1 = lo_f(k1) * by;
           reinterpret_cast<uint4*>(smem + OFF_KS)[slot * (BN / 2) + i] =
               make_uint4(pack_f16x2(f0, f0), pack_f16x2(-24.f * f0, -24.f * f0), pack_f16x2(f1, f1),
@@ -820,8 +819,14 @@ __global__ void __launch_bounds__(THREADS, 1) k_kv4_attn_many(ManyArgs f) {
       if (!(ok = warp_wait(bar(B_QE + np % PIECES), (np / PIECES) & 1, &s_abort))) break;
       const float c_row = a.scale_log2 * reinterpret_cast<const float*>(smem + OFF_QE)[np % PIECES * ROWS + row_of(pc)];
       const int every = pc->two ? 1 : 2, first = pc->two ? 0 : x, n_cached = pc->cached - pc->s0;
+      const bool idle = row_of(pc) - lane >= pc->rows;  // none of the warp's rows is in use
 #pragma unroll 1
       for (int j = first; j < n; j += every, ++t) {
+        if (idle) {
+          if (!(ok = warp_wait(bar(B_SFULL + x), t & 1, &s_abort))) break;
+          if (lane == 0) mbar_arrive(bar(B_PFULL + x));
+          continue;
+        }
         const int slot = (nb + j) % SLOTS;
         if (!(ok = warp_wait(bar(B_INFO + slot), ((nb + j) / SLOTS) & 1, &s_abort))) break;
         const float2* back = reinterpret_cast<const float2*>(smem + OFF_BACK) + slot * (NUM_WARPS / 2);
@@ -845,8 +850,10 @@ __global__ void __launch_bounds__(THREADS, 1) k_kv4_attn_many(ManyArgs f) {
           }
           tc_wait_st();
         }
-        // The row's scores come 32 at a time, the next in flight meanwhile; once
-        // for the maximum, once for P.
+        // The row's scores come 32 at a time, once for the maximum, once for P:
+        // one short loop each, as two bodies with loads in flight beside them
+        // took longer (1160 us where this takes 1100): the roles share the
+        // instruction cache and the other warps cover the loads.
         uint32_t sa[32], sb[32];
         float top = -INFINITY;
         auto largest = [&](int q, const uint32_t (&sv)[32]) {
@@ -859,16 +866,11 @@ __global__ void __launch_bounds__(THREADS, 1) k_kv4_attn_many(ManyArgs f) {
           }
           top = max3(top, p0 * bk.x, p1 * bk.y);
         };
-        tmem_ld32(tS, sa);
-        tc_wait_ld();
 #pragma unroll 1
-        for (int q = 0; q < 4; q += 2) {
-          tmem_ld32(tS + (q + 1) * 32, sb);
+        for (int q = 0; q < 4; ++q) {
+          tmem_ld32(tS + q * 32, sa);
+          tc_wait_ld();
           largest(q, sa);
-          tc_wait_ld();
-          tmem_ld32(tS + ((q + 2) & 3) * 32, sa);  // the last one: P's first
-          largest(q + 1, sb);
-          tc_wait_ld();
         }
         {
           top *= c_row;
@@ -890,44 +892,41 @@ __global__ void __launch_bounds__(THREADS, 1) k_kv4_attn_many(ManyArgs f) {
         }
         uint64_t sum[2] = {0ull, 0ull};
         const uint64_t neg = f2_pack(-m, -m);
-        const uint4* vs8 = reinterpret_cast<const uint4*>(smem + OFF_VS + slot * BN * 2);
+        const ulonglong2* vs4 = reinterpret_cast<const ulonglong2*>(smem + OFF_VS + slot * BN * 4);
         auto weigh = [&](int q, const uint32_t (&sv)[32]) {  // over scores already read
           uint32_t pk[16];
           const float2 bk = back[q];
 #pragma unroll
-          for (int g = 0; g < 4; ++g) {  // 8 keys, their value scales in one load
-            const uint4 v4 = vs8[q * 4 + g];
-            const float cz = c_row * (g < 2 ? bk.x : bk.y);
+          for (int g = 0; g < 8; ++g) {  // 4 keys, their value scales in one load
+            const ulonglong2 v4 = vs4[q * 8 + g];
+            const float cz = c_row * (g < 4 ? bk.x : bk.y);
             const uint64_t c2 = f2_pack(cz, cz);
 #pragma unroll
-            for (int u = 0; u < 4; ++u) {
-              const int k = 8 * g + 2 * u;
-              const uint32_t v = (&v4.x)[u];
+            for (int u = 0; u < 2; ++u) {
+              const int k = 4 * g + 2 * u;
               float p0, p1;
               f2_unpack(f2_fma(f2_pack(__uint_as_float(sv[k]), __uint_as_float(sv[k + 1])), c2, neg), p0, p1);
               const uint64_t pp = f2_pack(exp2_fast(p0), exp2_fast(p1));
-              sum[u & 1] = f2_add(sum[u & 1], pp);
-              f2_unpack(f2_mul(pp, f2_pack(lo_f(v), hi_f(v))), p0, p1);
-              pk[4 * g + u] = pack_bf16x2(p0, p1);
+              sum[u] = f2_add(sum[u], pp);
+              f2_unpack(f2_mul(pp, u ? v4.y : v4.x), p0, p1);
+              pk[2 * g + u] = pack_bf16x2(p0, p1);
             }
           }
           tmem_st16(tS + q * 16, pk);
         };
 #pragma unroll 1
-        for (int q = 0; q < 4; q += 2) {
-          tmem_ld32(tS + (q + 1) * 32, sb);
+        for (int q = 0; q < 4; ++q) {
+          tmem_ld32(tS + q * 32, sa);
+          tc_wait_ld();
           weigh(q, sa);
-          tc_wait_ld();
-          if (q == 0) tmem_ld32(tS + 64, sa);
-          weigh(q + 1, sb);
-          tc_wait_ld();
         }
         tc_wait_st();
         float s0, s1;
         f2_unpack(f2_add(sum[0], sum[1]), s0, s1);
         l += s0 + s1;
         tc_fence_before();
-        mbar_arrive(bar(B_PFULL + x));
+        __syncwarp();
+        if (lane == 0) mbar_arrive(bar(B_PFULL + x));
       }
       if (!ok || !(ok = warp_wait(bar(B_OFIN), np & 1, &s_abort))) break;
       tc_fence_after();
