@@ -465,7 +465,6 @@ __global__ void __launch_bounds__(THREADS, 1) k_kv4_attn_many(ManyArgs f) {
     const uint32_t v_lo = (uint32_t)smem_desc_sw128(sV, HALF_BYTES, 1024);
     auto wait = [&](int which, uint32_t parity) {
       ok = ok && warp_wait(bar(which), parity & 1, &s_abort);
-      tc_fence_after();
       return ok;
     };
     QTile qt;
@@ -483,11 +482,15 @@ __global__ void __launch_bounds__(THREADS, 1) k_kv4_attn_many(ManyArgs f) {
 #pragma unroll 1
       for (int k = -2; k < steps; ++k) {
         const uint32_t x = k & 1;
+        const uint32_t blk2 = nb + ((k + 2) >> two);
+        if (two && !x && k + 2 < steps && !wait(B_KFULL + (blk2 & 1), blk2 >> 1)) break;
         if (k >= 0) {  // O_x (+)= P_x V
           const uint32_t blk = nb + (k >> two), st = blk & 1;
-          if (!wait(B_VFULL + st, blk >> 1) || !wait(B_PFULL + x, t_of[x])) break;
+          if (!(two & x) && !wait(B_VFULL + st, blk >> 1)) break;  // tile 1: waited for by tile 0
+          if (!wait(B_PFULL + x, t_of[x])) break;
           ++t_of[x];
           if (k == 0 && np > 0 && !wait(B_OFREE, np - 1)) break;
+          tc_fence_after();
           mma_pv(tmem + 256 + x * 128, tmem + x * 128, v_lo + st * (TILE_BYTES >> 4), IDESC_PV, k >= 2);
           if (!two || x) {
             tc_commit(bar(B_VEMPTY + st));
@@ -496,7 +499,8 @@ __global__ void __launch_bounds__(THREADS, 1) k_kv4_attn_many(ManyArgs f) {
         }
         if (k + 2 < steps) {  // S_x <- Q K^T
           const uint32_t blk = nb + ((k + 2) >> two), st = blk & 1;
-          if (!wait(B_KFULL + st, blk >> 1)) break;
+          if (!two && !wait(B_KFULL + st, blk >> 1)) break;
+          tc_fence_after();
           mma_qk(tmem + x * 128, q_lo + (two ? x : (uint32_t)qt.tile) * (TILE_BYTES >> 4), k_lo + st * (TILE_BYTES >> 4), IDESC_QK);
           tc_commit(bar(B_SFULL + x));
           if (!two || x) tc_commit(bar(B_KEMPTY + st));
