@@ -212,6 +212,9 @@ def _check(fn, code):
 
 
 def _need(t, dtype, name, shape=None):
+    if type(t) is torch.Tensor and t.dtype is dtype and t.is_cuda and t.is_contiguous() and (
+            shape is None or t.shape == shape):  # the usual case, for calls of a few microseconds
+        return t
     if not isinstance(t, torch.Tensor):
         raise TypeError(f"{name} must be a tensor")
     if t.dtype != dtype:
