@@ -116,15 +116,16 @@ __device__ __forceinline__ void cp_async_wait() {
 // stages unrolled, and rows and tiles past the end are read from valid places
 // instead of being tested for.
 // A warp takes MT tiles of columns (which share the rows of x that it loads)
-// and every ks-th tile of k, seven tiles in flight by asynchronous copies, x
+// and every ks-th tile of k, three in flight by asynchronous copies, x
 // AHEAD tiles ahead in registers; with ks = 1 a sum never leaves its warp, else
 // the ks warps' sums meet in shared memory.  NT: 8-row tiles of x.  STEPS:
 // k-steps that share a scale (the group, or the whole tile).
 // x goes two tiles ahead: four took 64 registers of 16 rows' form, and 12 x
-// 8192 x 8192 22.6 us instead of 18.5; one row is the same either way.
-// Measured: 16 x 8192 x 28672 47 us (126 MB), a row of it 39 us (3.1 TB/s), of
-// 2048 x 32256 14 us, of 2048 x 2048 6 us (latency).
-constexpr int STAGES = 8;
+// 8192 x 8192 22.6 us instead of 18.5.  Seven tiles in flight instead of three
+// took as long for large weights and a microsecond more for small ones.
+// Measured: 16 x 8192 x 28672 47 us (126 MB), a row of it 35 us (3.5 TB/s), of
+// 2048 x 32256 14 us, of 2048 x 2048 5 us (latency).
+constexpr int STAGES = 4;
 // codes of MT tiles, then the scales [group][MT * TN]
 __host__ __device__ constexpr int stage_bytes(int MT, int STEPS) { return MT * TILE_BYTES + MT * TN * 2 * (4 / STEPS); }
 
@@ -145,8 +146,10 @@ __global__ void __launch_bounds__(MAX_WARPS * 32) k_w4_matvec(const uint4* __res
   const uint4* src[MT];
 #pragma unroll
   for (int m = 0; m < MT; ++m) src[m] = codes + ((size_t)min(tile0 + m, n_tiles - 1) * kt + part) * 32 + lane;
-  const int sq = lane / (8 * MT), sc_c = 2 * (lane % (8 * MT)), sc_col = tile0 * TN + sc_c;  // two columns of group sq
-  const bool sc_lane = lane < 8 * MT * GROUPS && sc_col < N;
+  // two columns' scales of group sq; with MT = 4 a lane has the same of every group
+  constexpr int SC_LANES = 8 * MT, SC_EACH = SC_LANES * GROUPS > 32 ? GROUPS : 1;
+  const int sq = lane / SC_LANES, sc_c = 2 * (lane % SC_LANES), sc_col = tile0 * TN + sc_c;
+  const bool sc_lane = lane < SC_LANES * GROUPS && sc_col < N;
   const uint32_t sc_dst = ring + OFF_SC + (sq * MT * TN + sc_c) * 2;
   const uint16_t* sc_src = scale + sc_col;
   uint32_t sc_k = part * TK + sq * STEPS * 16;
@@ -159,12 +162,16 @@ __global__ void __launch_bounds__(MAX_WARPS * 32) k_w4_matvec(const uint4* __res
         src[m] += ks * 32;
       }
       if (sc_lane) {
-        const uint16_t* sp = sc_src + (uint64_t)(sc_k >> gshift) * (uint32_t)N;
-        if (N & 1) {  // rows of odd length: two columns are not one aligned word
-          const uint32_t lo = sp[0], hi = sc_col + 1 < N ? sp[1] : 0u;
-          asm volatile("st.shared.b32 [%0], %1;" ::"r"(sc_dst + stage * STAGE_BYTES), "r"(lo | (hi << 16)) : "memory");
-        } else {
-          cp_async4(sc_dst + stage * STAGE_BYTES, sp);
+#pragma unroll
+        for (int e = 0; e < SC_EACH; ++e) {
+          const uint16_t* sp = sc_src + (uint64_t)((sc_k + e * STEPS * 16) >> gshift) * (uint32_t)N;
+          const uint32_t dst = sc_dst + stage * STAGE_BYTES + e * MT * TN * 2;
+          if (N & 1) {  // rows of odd length: two columns are not one aligned word
+            const uint32_t lo = sp[0], hi = sc_col + 1 < N ? sp[1] : 0u;
+            asm volatile("st.shared.b32 [%0], %1;" ::"r"(dst), "r"(lo | (hi << 16)) : "memory");
+          } else {
+            cp_async4(dst, sp);
+          }
         }
       }
       sc_k += ks * TK;
@@ -320,12 +327,18 @@ fc_status launch(const void* x, const void* codes, const void* scale, int M, int
 }
 
 template <int MT>
+fc_status launch_eight(const void* x, const void* codes, const void* scale, int M, int K, int N, int group, void* y,
+                       cudaStream_t s) {
+  const int gshift = group == 32 ? 5 : (group == 64 ? 6 : 7);
+  return group == 32 ? launch<MT, 1, 2>(x, codes, scale, M, K, N, gshift, y, s)
+                     : launch<MT, 1, 4>(x, codes, scale, M, K, N, gshift, y, s);
+}
+
+template <int MT>
 fc_status launch_rows(const void* x, const void* codes, const void* scale, int M, int K, int N, int group, void* y,
                       cudaStream_t s) {
   const int gshift = group == 32 ? 5 : (group == 64 ? 6 : 7);
-  if (M <= 8)
-    return group == 32 ? launch<MT, 1, 2>(x, codes, scale, M, K, N, gshift, y, s)
-                       : launch<MT, 1, 4>(x, codes, scale, M, K, N, gshift, y, s);
+  if (M <= 8) return launch_eight<MT>(x, codes, scale, M, K, N, group, y, s);
   return group == 32 ? launch<MT, 2, 2>(x, codes, scale, M, K, N, gshift, y, s)
                      : launch<MT, 2, 4>(x, codes, scale, M, K, N, gshift, y, s);
 }
@@ -365,9 +378,13 @@ extern "C" fc_status fc_w4_matvec(const void* d_x, const void* d_codes, const vo
       !aligned(d_y, 2))
     return FC_ERR_INVALID_ARG;
   cudaStream_t s = static_cast<cudaStream_t>(stream);
-  // Two column tiles a warp halve what it loads of x and what a tile costs
-  // besides its numbers (8192 x 8192 18.5 -> 15.1 us); an output of fewer than
-  // two tiles an SM has too few tiles for that (2048 x 2048: 6.2 us either way).
+  // More column tiles a warp share what it loads of x and what a step costs
+  // besides its numbers, fewer fill the GPU sooner.  Two against one: 8192 x 8192
+  // 15.1 us instead of 18.5, 2048 x 2048 6.2 either way.  Four against two, up to
+  // 8 rows: 1 x 8192 x 28672 34.9 us instead of 38.9, 8 x 4096 x 20001 21.9
+  // instead of 25.4, but 8 x 4096 x 11008 14.4 instead of 12.4; 16 rows' sums take
+  // too many registers (16 x 8192 x 28672 56 us instead of 47).
   if (N <= 152 * TN * 2) return launch_rows<1>(d_x, d_codes, d_scale, M, K, N, group, d_y, s);
+  if (M <= 8 && N > 152 * TN * 8) return launch_eight<4>(d_x, d_codes, d_scale, M, K, N, group, d_y, s);
   return launch_rows<2>(d_x, d_codes, d_scale, M, K, N, group, d_y, s);
 }

@@ -467,6 +467,15 @@ def test_matvec(fc, M, K, N, group):
     assert np.all((o4.bf16_round(y - e) <= got) & (got <= o4.bf16_round(y + e)))
 
 
+@pytest.mark.parametrize("M", [1, 8, 9, 16])
+@pytest.mark.parametrize("K,N,group", [(64, 4865, 32), (320, 4900, 64), (256, 9728, 128), (192, 19457, 32), (576, 19500, 64),
+                                       (128, 20001, 128), (128, 32256, 32)])
+def test_matvec_of_wide_weights(fc, M, K, N, group):
+    """Widths on either side of where a warp takes two and four column tiles,
+    odd ones and such that end inside a tile."""
+    test_matvec(fc, M, K, N, group)
+
+
 def test_matvec_of_unit_rows_reads_the_weights_back(fc):
     """x = a unit row: the product is one row of the weights, so every number
     of the packed layout is checked by itself."""
