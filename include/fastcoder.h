@@ -750,7 +750,8 @@ fc_status fc_kv4_read(const fc_kv4_cache* cache, const int32_t* d_slot, int rows
  *               see no key at all, are zeros
  *   d_ws        workspace of fc_kv4_attn_workspace() bytes, 256-byte aligned,
  *               ZEROED before its first use; every call leaves it fit for the
- *               next.  Less, or none (NULL), splits the keys less, or not.
+ *               next, whatever its shape.  Less, or none (NULL), splits the
+ *               keys less, or not.
  *               Calls that may overlap need one each.
  * D = 128, 1 <= n_pad <= 128, H a multiple of Hkv, H / Hkv <= 16.  The tensor
  * cores' products of numbers and bf16 queries are exact, sums, scales and the

@@ -16,6 +16,11 @@ static inline int kv4_page_shift(int page_size) {
 // The status of a cache description (kv4.cu).
 fc_status fc_kv4_check(const fc_kv4_cache* c);
 
+// An attention workspace begins with counters that are zero between calls; what
+// is written past them needs no such care, so that one workspace serves every
+// shape.
+constexpr size_t KV4_WS_COUNTERS = 1280;
+
 // What an attention launch passes to its kernels.
 struct Kv4Args {
   const __nv_bfloat16* q;

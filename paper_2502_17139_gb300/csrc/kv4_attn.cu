@@ -77,7 +77,7 @@ struct FewSmem {
 struct FewArgs {
   Kv4Args a;
   int split;         // 1: units are cut anywhere, by steps; 0: a CTA takes whole units
-  int* cnt;          // [units] arrivals at a cut unit, zero between calls
+  int* cnt;          // [grid] arrivals at the cut unit that begins in a CTA (at most one does), zero between calls
   float* part;       // [grid][2][ROWS][HD + 2]: O unnormalised, m, l of a CTA's first and last piece
 };
 
@@ -648,12 +648,11 @@ __global__ void __launch_bounds__(FEW_THREADS, NT == 1 ? 2 : 1) k_kv4_attn_few(F
       // The last CTA to arrive adds up the pieces, in CTA order whichever it is.
       __threadfence();
       __syncthreads();
-      const int unit = b * a.Hkv + gh;
-      if (tid == 0) s_last = atomicAdd(f.cnt + unit, 1) == nc - 1;
+      if (tid == 0) s_last = atomicAdd(f.cnt + c0, 1) == nc - 1;
       __syncthreads();
       if (s_last) {
         __threadfence();
-        if (tid == 0) f.cnt[unit] = 0;  // fit for the next call
+        if (tid == 0) f.cnt[c0] = 0;  // fit for the next call
         // each piece's weight in a row, a warp a row ...
         float* wt = reinterpret_cast<float*>(smem);  // [R][nc]
         float* red = wt + ((R * nc + 3) & ~3);       // [subsets][R][HD]
@@ -715,7 +714,7 @@ __global__ void __launch_bounds__(FEW_THREADS, NT == 1 ? 2 : 1) k_kv4_attn_few(F
 
 constexpr int FEW_GRID = 152 * 2;
 
-size_t few_cnt_bytes(int batch, int Hkv) { return ((size_t)batch * Hkv * sizeof(int) + 255) / 256 * 256; }
+static_assert(FEW_GRID * sizeof(int) <= KV4_WS_COUNTERS, "room for the counters");
 
 template <int NT>
 fc_status launch_few(const Kv4Args& a, void* ws, size_t ws_bytes, cudaStream_t s) {
@@ -726,7 +725,7 @@ fc_status launch_few(const Kv4Args& a, void* ws, size_t ws_bytes, cudaStream_t s
   });
   if (st != FC_OK) return st;
   const int full = NT == 1 ? FEW_GRID : FEW_GRID / 2;
-  const size_t cnt = few_cnt_bytes(a.B, a.Hkv), one = (size_t)2 * FewSmem<NT>::ROWS * (HD + 2) * sizeof(float);
+  const size_t cnt = KV4_WS_COUNTERS, one = (size_t)2 * FewSmem<NT>::ROWS * (HD + 2) * sizeof(float);
   const long long units = (long long)a.B * a.Hkv;
   // at most what the tables could hold, in steps (past 32 bits there are units enough without cutting them)
   const long long longest = (((long long)a.max_pages << a.shift) + STEP - 1) / STEP + 1, most = units * (longest + UNIT_COST);
@@ -756,7 +755,7 @@ extern "C" size_t fc_kv4_attn_workspace(int batch, int n_pad, int H, int Hkv) {
   if (batch < 1 || !shape_ok(n_pad, H, Hkv)) return 0;
   const int rows = n_pad * (H / Hkv);
   if (rows > 16) return kv4_attn_many_workspace(batch, n_pad, H, Hkv);
-  return few_cnt_bytes(batch, Hkv) + (size_t)FEW_GRID * 2 * 8 * (HD + 2) * sizeof(float);
+  return KV4_WS_COUNTERS + (size_t)FEW_GRID * 2 * 8 * (HD + 2) * sizeof(float);
 }
 
 extern "C" fc_status fc_kv4_attn(const void* d_q, const fc_kv4_cache* cache, const int32_t* d_table, int max_pages,

@@ -1066,7 +1066,7 @@ constexpr int FULL_GRID = 152;
 
 size_t kv4_attn_many_workspace(int batch, int n_pad, int H, int Hkv) {
   (void)batch;
-  return list_bytes(FULL_GRID) + (size_t)FULL_GRID * 2 * slot_bytes(rows_of_chunk(n_pad, H / Hkv));
+  return KV4_WS_COUNTERS + list_bytes(FULL_GRID) + (size_t)FULL_GRID * 2 * slot_bytes(rows_of_chunk(n_pad, H / Hkv));
 }
 
 fc_status kv4_attn_many(const Kv4Args& a, void* ws, size_t ws_bytes, cudaStream_t s) {
@@ -1085,13 +1085,14 @@ fc_status kv4_attn_many(const Kv4Args& a, void* ws, size_t ws_bytes, cudaStream_
   const long long longest = (((long long)a.max_pages << a.shift) + BN - 1) / BN + 1;
   const bool fits = units * (UNIT_COST + 2 * longest) <= 0x7FFFFFFFll;
   int grid = (int)std::min<long long>(FULL_GRID, units * ((UNIT_COST + 2 * longest) / LEAST));
-  while (grid > 1 && ws && list_bytes(grid) + (size_t)grid * 2 * slot_bytes(f.rows_cap) > ws_bytes) --grid;
-  if (!ws || !fits || list_bytes(grid) + (size_t)grid * 2 * slot_bytes(f.rows_cap) > ws_bytes ||
+  auto need = [&] { return KV4_WS_COUNTERS + list_bytes(grid) + (size_t)grid * 2 * slot_bytes(f.rows_cap); };
+  while (grid > 1 && ws && need() > ws_bytes) --grid;
+  if (!ws || !fits || need() > ws_bytes ||
       (grid < FULL_GRID && units >= FULL_GRID)) {
     f.split = 0;
     grid = (int)std::min<long long>(units, FULL_GRID);
   } else {
-    unsigned char* p = static_cast<unsigned char*>(ws);
+    unsigned char* p = static_cast<unsigned char*>(ws) + KV4_WS_COUNTERS;
     f.list = reinterpret_cast<int*>(p);
     f.part_o = reinterpret_cast<float*>(p + list_bytes(grid));
     f.part_ml = reinterpret_cast<float2*>(f.part_o + (size_t)grid * 2 * f.rows_cap * HD);

@@ -936,8 +936,8 @@ def fc_kv4_read(cache: Kv4Cache, slot, out=None):
 
 
 def kv4_attn_workspace(B, n_pad, H, Hkv, device):
-    """A zeroed workspace for fc_kv4_attn at this shape.  Calls that may overlap
-    on different streams need one each."""
+    """A zeroed workspace for fc_kv4_attn at this shape (and at any that needs no
+    more).  Calls that may overlap on different streams need one each."""
     n = int(LIB.fc_kv4_attn_workspace(B, n_pad, H, Hkv))
     return torch.zeros(max(n, 256), dtype=torch.uint8, device=device)
 

@@ -407,6 +407,23 @@ def test_attn_sharp_and_shifted_scores(fc, n):
     assert np.all(np.abs(num(out) - ref) <= 2.0 ** -8 * np.abs(ref) + size * (2.0 ** -8 + 2.0 ** -7))
 
 
+def test_attn_one_workspace_for_every_shape(fc):
+    """A workspace as large as any of them needs, zeroed once, for calls of
+    different batches, heads and nodes in turn."""
+    cases = [attn_case(300 + i, B, n, H, G, lens, 64) for i, (B, n, H, G, lens) in enumerate([
+        (2, 40, 8, 2, [3000, 9000]), (1, 1, 8, 2, [20000]), (8, 1, 32, 8, [5000, 1, 0, 7000, 12000, 64, 300, 9000]),
+        (1, 128, 8, 8, [4000]), (3, 5, 8, 2, [9000, 100, 4000]), (1, 1, 8, 8, [30000])])]
+    shapes = [tuple(c["q"].shape[:3]) + (c["codes"][0].shape[1],) for c in cases]
+    ws = torch.zeros(max(int(fc.LIB.fc_kv4_attn_workspace(*s)) for s in shapes), dtype=torch.uint8, device="cuda")
+    want = [check_attn(fc, c) for c in cases]
+    for i in [0, 1, 2, 3, 4, 5, 2, 0, 5, 4, 3, 2, 1]:
+        c = cases[i]
+        got = fc.fc_kv4_attn(c["q"].cuda(), gpu_cache(fc, c), dev(c["table"]), dev(c["lens"]), c["k_new"].cuda(),
+                             c["v_new"].cuda(), dev(mask_words(c["sees"])), dev(c["nodes"]), scale=c["scale"], workspace=ws)
+        assert torch.equal(got, want[i]), i
+    assert fc.fc_get_error() == "FC_OK"
+
+
 @pytest.mark.parametrize("n", [1, 8, 90])
 def test_attn_refuses_bad_lengths_and_pages(fc, n):
     c = attn_case(81, 3, n, 4, 2, [64, 64, 64], 16, spare=0)
