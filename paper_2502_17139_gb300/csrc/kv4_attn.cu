@@ -47,7 +47,7 @@ constexpr int HD = KV4_D;
 //
 // 32 single tokens over 16384 keys (8 kv heads of 4 query heads, 554 MB) take
 // 106 us, 5.2 TB/s: 6.4 TB/s once all run, and some 15 us until they do and
-// until the last part is joined.  One token over 131071 keys (138 MB): 38 us.
+// until the last part is joined.  One token over 131071 keys (138 MB): 37 us.
 // There start, end and the instructions (450 a step of a warp, most to place
 // numbers) count more than the read.  500 keys: 10 us, latency.
 // ---------------------------------------------------------------------------
@@ -71,18 +71,26 @@ struct FewSmem {
   static constexpr int OUT_PITCH = HD + 4;  // floats a row of a warp's partial
   static constexpr int MERGE = FEW_WARPS * ROWS * (OUT_PITCH + 2) * 4;
   static constexpr int JOIN = (ROWS * 152 * 2 + FEW_THREADS * 4) * 4;  // pieces' weights, subsets' sums
-  static constexpr int BYTES = RING > MERGE ? (RING > JOIN ? RING : JOIN) : (MERGE > JOIN ? MERGE : JOIN);
+  // the new tokens' keys, values and masks (a row of 256 bytes at 272, so that
+  // eight rows' reads fall in different banks)
+  static constexpr int NEW_PITCH = HD * 2 + 16, NEW = 2 * 16 * NEW_PITCH + 16 * 8;
+  static constexpr int OFF_NEW = RING > MERGE ? (RING > JOIN ? RING : JOIN) : (MERGE > JOIN ? MERGE : JOIN);
+  static constexpr int BYTES = OFF_NEW + NEW;
 };
 
 struct FewArgs {
   Kv4Args a;
   int split;         // 1: units are cut anywhere, by steps; 0: a CTA takes whole units
+  uint32_t by_G;     // r / G is r * by_G >> 16 for r < 16
   int* cnt;          // [grid] arrivals at the cut unit that begins in a CTA (at most one does), zero between calls
   float* part;       // [grid][2][ROWS][HD + 2]: O unnormalised, m, l of a CTA's first and last piece
 };
 
 __device__ __forceinline__ void cp_async16(uint32_t dst, const void* src) {
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16;\n" ::"r"(dst), "l"(src) : "memory");
+}
+__device__ __forceinline__ void cp_async8(uint32_t dst, const void* src) {
+  asm volatile("cp.async.ca.shared.global [%0], [%1], 8;\n" ::"r"(dst), "l"(src) : "memory");
 }
 __device__ __forceinline__ void cp_async_commit() { asm volatile("cp.async.commit_group;\n" ::: "memory"); }
 template <int N>
@@ -256,7 +264,11 @@ __global__ void __launch_bounds__(FEW_THREADS, NT == 1 ? 2 : 1) k_kv4_attn_few(F
     if (bad && gh == 0 && s0 == 0 && tid == 0) fc_flag(FC_ERR_WORD(a.err), FC_EBIT_INVALID);
     const int c_steps = nn == 0 ? 0 : (kvl + STEP - 1) / STEP;
     const int R = nn * a.G;  // rows in use: node-major, r = node * G + head in group
-    auto q_row = [&](int r) { return a.q + (((size_t)b * a.n_pad + r / a.G) * a.H + gh * a.G + r % a.G) * HD; };
+    auto node_of = [&](int r) { return (int)((uint32_t)r * f.by_G >> 16); };
+    auto q_row = [&](int r) {
+      const int i = node_of(r);
+      return a.q + (((size_t)b * a.n_pad + i) * a.H + gh * a.G + (r - i * a.G)) * HD;
+    };
 
     const uint8_t *k_lane = a.kc + lane * 16, *v_lane = a.vc + lane * 16;
     const __nv_bfloat16* sc0 = (lane & 4) ? a.vs : a.ks;
@@ -326,6 +338,18 @@ __global__ void __launch_bounds__(FEW_THREADS, NT == 1 ? 2 : 1) k_kv4_attn_few(F
 #pragma unroll
       for (int i = 0; i < 4; ++i)
         qw[n][i] = 8 * n + g < R ? reinterpret_cast<const uint4*>(q_row(8 * n + g))[4 * t + i] : make_uint4(0, 0, 0, 0);
+    // the new tokens' rows and masks, by the warp that will use them
+    auto new_here = [&] { return a.k_new && nn > 0 && s1 == steps && warp == (steps - 1 - s0) % FEW_WARPS; };
+    if (new_here()) {
+      const uint32_t to = smem_u32(smem) + L::OFF_NEW;
+      const size_t from = ((size_t)b * a.Hkv + gh) * a.n_pad * HD + (lane & 15) * 8;
+#pragma unroll 1
+      for (int j = lane >> 4; j < nn; j += 2) {
+        cp_async16(to + j * L::NEW_PITCH + (lane & 15) * 16, a.k_new + from + (size_t)j * HD);
+        cp_async16(to + (16 + j) * L::NEW_PITCH + (lane & 15) * 16, a.v_new + from + (size_t)j * HD);
+      }
+      if (a.mask && lane < nn) cp_async8(to + 32 * L::NEW_PITCH + lane * 8, a.mask + (size_t)b * a.n_pad + lane);
+    }
     // the first steps are asked for before the queries have come
 #pragma unroll 1
     for (int it = 0; it < FEW_STAGES - 1; ++it) issue(it, it, it * STEP_BYTES);
@@ -513,16 +537,18 @@ __global__ void __launch_bounds__(FEW_THREADS, NT == 1 ? 2 : 1) k_kv4_attn_few(F
     cp_async_wait<0>();
 
     // ---- the new tokens' step, in bf16: the warp whose turn it would be
-    if (a.k_new && nn > 0 && s1 == steps && warp == (steps - 1 - s0) % FEW_WARPS) {
-      const size_t nrow = ((size_t)b * a.Hkv + gh) * a.n_pad;
+    if (new_here()) {
+      __syncwarp();
+      const unsigned char* rows = smem + L::OFF_NEW;
+      const uint64_t* masks = reinterpret_cast<const uint64_t*>(rows + 32 * L::NEW_PITCH);
       const uint4 zero = make_uint4(0, 0, 0, 0);
       float z[NT][4];
 #pragma unroll
       for (int n = 0; n < NT; ++n) z[n][0] = z[n][1] = z[n][2] = z[n][3] = 0.f;
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        const uint4 x = g < nn ? reinterpret_cast<const uint4*>(a.k_new + (nrow + g) * HD)[4 * t + i] : zero;
-        const uint4 y = g + 8 < nn ? reinterpret_cast<const uint4*>(a.k_new + (nrow + g + 8) * HD)[4 * t + i] : zero;
+        const uint4 x = g < nn ? reinterpret_cast<const uint4*>(rows + g * L::NEW_PITCH)[4 * t + i] : zero;
+        const uint4 y = g + 8 < nn ? reinterpret_cast<const uint4*>(rows + (g + 8) * L::NEW_PITCH)[4 * t + i] : zero;
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
           const uint4 w = 8 * n + g < R ? reinterpret_cast<const uint4*>(q_row(8 * n + g))[4 * t + i] : zero;
@@ -530,7 +556,6 @@ __global__ void __launch_bounds__(FEW_THREADS, NT == 1 ? 2 : 1) k_kv4_attn_few(F
           mma_bf16(z[n], x.z, y.z, x.w, y.w, w.z, w.w);
         }
       }
-      const int words = (a.n_pad + 63) / 64;
       uint32_t pb[NT][2], seen = 0, bad = 0;  // bits 4n + c: z[n][c]'s key is seen; bits j: values of token j are not finite
       const float one[4] = {1.f, 1.f, 0.f, 0.f};
       const float by[4] = {a.scale_log2, a.scale_log2, 1.f, 1.f};
@@ -539,9 +564,9 @@ __global__ void __launch_bounds__(FEW_THREADS, NT == 1 ? 2 : 1) k_kv4_attn_few(F
         float zz[4][2], w[4][2];
 #pragma unroll
         for (int c = 0; c < 4; ++c) {
-          const int r = 8 * n + 2 * t + (c & 1), j = g + 8 * (c >> 1), i = r / a.G;
+          const int r = 8 * n + 2 * t + (c & 1), j = g + 8 * (c >> 1), i = node_of(r);
           bool sees = r < R && j < nn;
-          if (sees) sees = a.mask ? (a.mask[((size_t)b * a.n_pad + i) * words] >> j) & 1 : j <= i;
+          if (sees) sees = a.mask ? (masks[i] >> j) & 1 : j <= i;
           seen |= (sees ? 1u : 0u) << (4 * n + c);
           zz[c >> 1][c & 1] = sees ? z[n][c] : -INFINITY;
           zz[2 + (c >> 1)][c & 1] = -INFINITY;
@@ -557,7 +582,7 @@ __global__ void __launch_bounds__(FEW_THREADS, NT == 1 ? 2 : 1) k_kv4_attn_few(F
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
           const int j = 2 * t + (k & 1) + 8 * (k >> 1);
-          v[k] = j < nn ? reinterpret_cast<const uint4*>(a.v_new + (nrow + j) * HD)[2 * g + h] : zero;
+          v[k] = j < nn ? reinterpret_cast<const uint4*>(rows + (16 + j) * L::NEW_PITCH)[2 * g + h] : zero;
           // a value that is not finite becomes 0, as no weight of 0 would take
           // it out of the rows that do not see its token; those that do are NaN
           uint32_t* w = &v[k].x;
@@ -612,7 +637,7 @@ __global__ void __launch_bounds__(FEW_THREADS, NT == 1 ? 2 : 1) k_kv4_attn_few(F
     const int rows_all = a.n_pad * a.G;  // rows past the nodes are written as zeros
     float* slot = piece(blockIdx.x);
     auto put = [&](int r, int d4, const float4& v) {
-      const int i = r / a.G;
+      const int i = node_of(r);
       __nv_bfloat16* dst = a.out + (((size_t)b * a.n_pad + i) * a.H + gh * a.G + (r - i * a.G)) * HD + 4 * d4;
       *reinterpret_cast<uint2*>(dst) = make_uint2(pack_bf16x2(v.x, v.y), pack_bf16x2(v.z, v.w));
     };
@@ -730,7 +755,7 @@ fc_status launch_few(const Kv4Args& a, void* ws, size_t ws_bytes, cudaStream_t s
   // at most what the tables could hold, in steps (past 32 bits there are units enough without cutting them)
   const long long longest = (((long long)a.max_pages << a.shift) + STEP - 1) / STEP + 1, most = units * (longest + UNIT_COST);
   int grid = (int)std::min<long long>(full, units * std::max<long long>(1, longest / PART_STEPS));
-  FewArgs f{a, 1, nullptr, nullptr};
+  FewArgs f{a, 1, 65536u / a.G + 1, nullptr, nullptr};
   if (ws && ws_bytes > cnt) grid = (int)std::min<size_t>(grid, (ws_bytes - cnt) / one);
   if (!ws || ws_bytes <= cnt || grid < 1 || most > 0x7FFFFFFFll) {
     f.split = 0;
@@ -796,8 +821,8 @@ extern "C" fc_status fc_kv4_attn(const void* d_q, const fc_kv4_cache* cache, con
   if ((long long)batch * a.Hkv > 1ll << 30) return FC_ERR_UNSUPPORTED;
   // Measured on both sides of the rules (8 kv heads of 4 query heads):
   //   4 rows, 32 x 16384 keys:  one 8-row tile 106 us, two 154
-  //   16 rows, 32 x 8192 keys:  two 8-row tiles 94 us, a tcgen05 tile 191;
-  //            1 x 500 keys: 14 and 22
+  //   16 rows, 32 x 8192 keys:  two 8-row tiles 91 us, a tcgen05 tile 174;
+  //            1 x 500 keys: 12 and 22
   // (three 8-row tiles would not fit the registers).
   if (n_pad * a.G <= 8) return launch_few<1>(a, d_ws, ws_bytes, s);
   if (n_pad * a.G <= 16) return launch_few<2>(a, d_ws, ws_bytes, s);
