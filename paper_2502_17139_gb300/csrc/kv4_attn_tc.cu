@@ -43,7 +43,7 @@
 // Every mbarrier wait is bounded: one that runs out raises FC_ERR_TIMEOUT, the
 // CTA lets its issued products retire, frees its tensor memory and returns.
 #include <algorithm>
-#include <cmath>
+#include <atomic>
 
 #include "fc_common.cuh"
 #include "kv4.cuh"
@@ -83,8 +83,12 @@ constexpr float M_START = -1e30f;  // a reference before any key
 // Exponents below count as this, so that the product of two is no fp32
 // underflow; such scores are 0 to fp32 all the same.
 constexpr int E_MIN = -50;
-// A unit's start and end in blocks of one tile, and the least share worth a CTA.
-constexpr int UNIT_COST = 8, LEAST = 12;
+// A unit's start and end in blocks of one tile (4 takes 183 us where 8 takes 161,
+// 16 ragged trees of 64 nodes), and the least share worth a CTA: with 12 instead
+// of 6 a tree of 32 nodes over 2000 keys takes 37 us instead of 31, one of 64 over
+// 8192 43 instead of 41; with 4 they take 27 and 41, but 4 trees of 64 nodes over
+// 300 keys 35 instead of 31.
+constexpr int UNIT_COST = 8, LEAST = 6;
 
 // Registers a thread by warpgroup (setmaxnreg), of the launch's 96.  The shares must add up to the launch's
 // allocation, or the increase never returns; the host checks the compiled count.
