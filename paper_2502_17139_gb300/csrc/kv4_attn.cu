@@ -57,8 +57,11 @@ constexpr int FEW_STAGES = 3;    // steps in flight a warp
 constexpr int OFF_VROWS = STEP * KV4_ROW, OFF_KSC = 2 * STEP * KV4_ROW, OFF_VSC = OFF_KSC + STEP * 2;
 constexpr int STEP_BYTES = OFF_VSC + STEP * 2;
 // A unit's start and end take a CTA about 6 us, 0.2 us a step at full
-// bandwidth; joining two parts of a unit about 4 us.
-constexpr int UNIT_COST = 30, PART_STEPS = 16;
+// bandwidth; joining two parts of a unit about 4 us.  Parts of 8 steps: 1 x 2000
+// and 2 x 1000 keys take 10.3 us where parts of 16 take 12.3, 4 x 4000 14.5 for
+// 16.4; a unit of fewer than CUT_STEPS stays whole (16 x 500 keys 10.3 us, in two
+// parts 12.4).
+constexpr int UNIT_COST = 30, PART_STEPS = 8, CUT_STEPS = 24;
 constexpr float W_MAX = 32768.f;
 constexpr int VS_MIN_EXP = -80;
 constexpr float VS_MIN = 0x1p-80f;
@@ -152,6 +155,9 @@ __device__ __forceinline__ int few_steps(const Kv4Args& a, int b, int& nn, int& 
   return nn == 0 ? 1 : max(1, (kvl + STEP - 1) / STEP + (a.k_new ? 1 : 0));
 }
 
+// parts that a unit of so many steps is worth (0: like 1)
+__device__ __forceinline__ int parts_of(int steps) { return steps < CUT_STEPS ? 0 : steps / PART_STEPS; }
+
 template <int NT>
 __global__ void __launch_bounds__(FEW_THREADS, NT == 1 ? 2 : 1) k_kv4_attn_few(FewArgs f) {
   using L = FewSmem<NT>;
@@ -186,7 +192,7 @@ __global__ void __launch_bounds__(FEW_THREADS, NT == 1 ? 2 : 1) k_kv4_attn_few(F
     cut = Kv4Cut(__reduce_add_sync(0xFFFFFFFFu, sum) * a.Hkv, gridDim.x, UNIT_COST + PART_STEPS);
     longest = __reduce_max_sync(0xFFFFFFFFu, longest);
     if (units <= (int)gridDim.x) {
-      const int k = max(1, min((int)gridDim.x / units, (longest - UNIT_COST) / PART_STEPS));
+      const int k = max(1, min((int)gridDim.x / units, parts_of(longest - UNIT_COST)));
       if ((longest - UNIT_COST) / k <= cut.q) parts = k;
     }
     if (parts) {
@@ -250,7 +256,7 @@ __global__ void __launch_bounds__(FEW_THREADS, NT == 1 ? 2 : 1) k_kv4_attn_few(F
       cur += gridDim.x;
       if (f.split) {
         c0 = unit * parts;
-        nc = max(1, min(parts, steps / PART_STEPS));  // a short unit in fewer parts
+        nc = max(1, min(parts, parts_of(steps)));  // a short unit in fewer parts
         const int part = (int)blockIdx.x - c0, q = steps / nc, rem = steps - q * nc;
         if (part >= nc) break;
         s0 = part * q + min(part, rem);
