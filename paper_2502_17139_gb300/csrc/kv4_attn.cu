@@ -34,7 +34,9 @@ constexpr int HD = KV4_D;
 //     z + log2(value scale), moved lazily.  (High in fp16's range, so that a
 //     weight of 2^-25 of the largest keeps 11 bits.)  For the
 //     reference a value scale counts as at least 2^-80, so that 2^(z - m), and
-//     the row sum, stay in fp32's range where a row of V is all zeros.
+//     the row sum, stay in fp32's range where a row of V is all zeros.  The
+//     test for the move is that w is NOT below 2^15: far above the reference
+//     2^(z - m) is infinite and its product with a scale of 0 NaN.
 // A warp takes every FEW_WARPS-th step of 32 keys (4224 bytes, two runs of 16
 // rows in a page), three steps in flight by 16-byte asynchronous copies.  S^T
 // becomes P^T's operand by 8x8 transposes in registers.
@@ -65,7 +67,9 @@ constexpr int UNIT_COST = 30, PART_STEPS = 8, CUT_STEPS = 24;
 constexpr float W_MAX = 32768.f;
 constexpr int VS_MIN_EXP = -80;
 constexpr float VS_MIN = 0x1p-80f;
-constexpr float M_START = -1e30f;  // a reference before any key: 2^(z + 1e30) passes W_MAX, 2^(-1e30 - m) is 0
+// A reference before any key: 2^(z + 1e30) is infinite and not below W_MAX
+// whatever it is multiplied by, 2^(-1e30 - m) is 0.
+constexpr float M_START = -1e30f;
 
 template <int NT>
 struct FewSmem {
@@ -412,7 +416,8 @@ __global__ void __launch_bounds__(FEW_THREADS, NT == 1 ? 2 : 1) k_kv4_attn_few(F
 
     // Scores d * ks (base 2; masked keys: d -inf, ks 1; d[i][r] of the lane's
     // key i, row 2t + r) and value scales to w = 2^(d ks - m) vs; adds the
-    // powers to the row sums; moves the references when a w is too large.
+    // powers to the row sums; moves the references when a w is too large.  A
+    // NaN of one row's moves the other's for nothing, which harms no result.
     auto weigh = [&](int n, const float (&d)[4][2], const float (&ks)[4], const float (&vs)[4], float (&w)[4][2]) {
       float p[4][2];
 #pragma unroll
@@ -424,7 +429,7 @@ __global__ void __launch_bounds__(FEW_THREADS, NT == 1 ? 2 : 1) k_kv4_attn_few(F
         }
       float ps[2] = {(p[0][0] + p[1][0]) + (p[2][0] + p[3][0]), (p[0][1] + p[1][1]) + (p[2][1] + p[3][1])};
       const float sum = ((w[0][0] + w[0][1]) + (w[1][0] + w[1][1])) + ((w[2][0] + w[2][1]) + (w[3][0] + w[3][1]));
-      if (__any_sync(0xFFFFFFFFu, fmaf(ps[0] + ps[1], VS_MIN, sum) > W_MAX)) {
+      if (__any_sync(0xFFFFFFFFu, !(fmaf(ps[0] + ps[1], VS_MIN, sum) <= W_MAX))) {
 #pragma unroll
         for (int r = 0; r < 2; ++r) {
           float top = M_START;

@@ -466,6 +466,51 @@ def test_attn_on_another_stream_and_in_a_graph(fc):
         assert torch.equal(kw["out"], want)
 
 
+def zero_values(c, which):
+    """Value rows of zeros as a write leaves them: numbers 0, scale 0."""
+    page = c["codes"][1].shape[2]
+    for b, L in enumerate(c["lens"]):
+        at = {"all": np.arange(L), "first": np.arange(1), "first 32": np.arange(min(L, 32)), "every fourth": np.arange(0, L, 4),
+              "last": np.arange(L - 1, L)}[which]
+        c["codes"][1][c["table"][b, at // page], :, at % page] = 0
+        c["scales"][1][c["table"][b, at // page], :, at % page] = 0
+
+
+@pytest.mark.parametrize("which", ["all", "first", "first 32", "every fourth", "last"])
+@pytest.mark.parametrize("n,H,G", [(1, 8, 2), (3, 8, 2), (20, 4, 2)])
+def test_attn_value_rows_of_zeros(fc, which, n, H, G):
+    """Scale 0 is how a row of zeros is held: such keys count in the row sum
+    and add nothing.  33 keys end in a step of one key, 1000 are cut in parts."""
+    c = attn_case(n + len(which), 4, n, H, G, [1, 33, 300, 1000], 16)
+    zero_values(c, which)
+    for ws in (True, False):
+        check_attn(fc, c, ws=ws)
+    out = check_attn(fc, c, new=False)
+    assert bool(out.any()) == (which != "all")
+
+
+@pytest.mark.parametrize("n,H,G", [(1, 2, 1), (1, 16, 2), (2, 16, 2), (20, 4, 2)])
+def test_attn_a_query_with_a_nan_is_alone_with_it(fc, n, H, G):
+    """Rows share lanes and steps with a row of NaN while their own scores grow
+    tenfold after 256 keys, so that their references have to move.  Scores'
+    fp32 errors, 2^-22 * 136 * sum|q| * 2 * scale < 2^-10, are relative errors of
+    p, and of the row sum once more."""
+    c = attn_case(5 * n + H, 2, n, H, G, [2000, 700], 64)
+    c["scales"][0][...] = 0.2
+    for b in range(2):
+        c["scales"][0][c["table"][b, 4:-(-c["lens"][b] // 64)]] = 2.0
+    hit = np.zeros(c["q"].shape[:3], bool)
+    hit[:, 0, ::H // G] = True
+    ref, size = o4.attn(num(c["q"]), *(o4.pack(x) for x in c["codes"]), *c["scales"], c["table"], c["lens"], num(c["k_new"]),
+                        num(c["v_new"]), c["sees"], c["nodes"], c["scale"])
+    c["q"][torch.from_numpy(hit)] = float("nan")
+    for ws in (True, False):
+        got = num(run_attn(fc, c, ws=ws))
+        assert np.isnan(got[hit]).all() and np.isfinite(got[~hit]).all()
+        assert np.all((np.abs(got - ref) <= 2.0 ** -8 * np.abs(ref) + size * (2.0 ** -8 + 2.0 ** -9))[~hit])
+    assert fc.fc_get_error() == "FC_OK"
+
+
 # ------------------------------------------------------------------ product
 @pytest.mark.parametrize("M", [1, 2, 7, 8, 9, 16])
 @pytest.mark.parametrize("K,N,group", [(64, 1, 32), (64, 16, 64), (128, 33, 128), (320, 100, 64), (2048, 50, 32),
