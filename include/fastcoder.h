@@ -753,16 +753,22 @@ fc_status fc_kv4_read(const fc_kv4_cache* cache, const int32_t* d_slot, int rows
  *               next, whatever its shape.  Less, or none (NULL), splits the
  *               keys less, or not.
  *               Calls that may overlap need one each.
- * D = 128, 1 <= n_pad <= 128, H a multiple of Hkv, H / Hkv <= 16.  The tensor
- * cores' products of numbers and bf16 queries are exact, sums, scales and the
- * softmax are fp32; probabilities are rounded to bf16 for the second product.
+ * D = 128, 1 <= n_pad <= 128, H a multiple of Hkv, H / Hkv <= 16.  Sums, scales
+ * and the softmax are fp32.  What the tensor cores multiply is rounded so:
+ *   up to 16 rows a kv head (n_pad * H / Hkv): numbers exact; queries fp16
+ *     relative to the largest of the request's rows of that kv head, exact down
+ *     to 2^-27 of it; probabilities times value scales fp16 relative to the
+ *     row's largest, 11 bits down to 2^-25 of it;
+ *   more: cached and new keys fp16 relative to the largest of 16 neighbours,
+ *     exact down to 2^-20 of it; queries fp16 relative to the row's largest,
+ *     exact down to 2^-26 of it; probabilities times value scales bf16.
+ * Scales and new values may lie anywhere between 2^-80 and 2^100 (or be 0), side
+ * by side; scores, scale * q k, of up to 2^24 in magnitude.
  * A length or node count out of range, or a page id outside the pool, records
  * FC_ERR_INVALID_ARG (that request's rows are zeros; that page's keys are
  * left out).  What a page holds past a request's end is not looked at.  A new
  * token with a NaN or an infinity, or a cached row that stands for NaN, makes
- * NaN of the rows that see it, and of no others.  With more than 16 rows a kv
- * head (n_pad * H / Hkv) keys enter the products in fp16 relative to the
- * largest of 16 neighbours: one smaller than 2^-20 of that loses bits.
+ * NaN of the rows that see it, and of no others.
  */
 fc_status fc_kv4_attn(const void* d_q, const fc_kv4_cache* cache, const int32_t* d_table, int max_pages,
                       const int32_t* d_kv_len, const void* d_k_new, const void* d_v_new, const uint64_t* d_mask,

@@ -511,6 +511,61 @@ def test_attn_a_query_with_a_nan_is_alone_with_it(fc, n, H, G):
     assert fc.fc_get_error() == "FC_OK"
 
 
+@pytest.mark.parametrize("n,H,G", [(1, 8, 2), (4, 16, 4), (20, 4, 2), (128, 4, 2)])
+def test_attn_scales_far_apart(fc, n, H, G):
+    """Value scales of 2^-60 to 2^20 and key scales of 2^-60 to 2^-1 side by
+    side, some of them 0.  Beside the usual tolerance: weights are held
+    relative to the largest, in fp16 at 2^11 or more, so that those below
+    fp16's normal range are off by up to 2^-25: 2^-36 of that key's |c| s (at
+    most 7 times its largest weight's) for each key.  Keys lose 2^-34 of their 16
+    neighbours' largest (2^-1), less than what a score is off by anyway."""
+    rng = np.random.default_rng(n)
+    c = attn_case(n + 7, 3, n, H, G, [300, 37, 1000], 32, stale=False)
+    for i, hi in ((0, -1), (1, 20)):
+        s = o4.bf16_round(2.0 ** rng.uniform(-60, hi, c["scales"][i].shape))
+        s[rng.random(s.shape) < 0.05] = 0
+        c["scales"][i][...] = s
+    for ws in (True, False):
+        for new in (True, False):
+            got = num(run_attn(fc, c, ws=ws, new=new))
+            kn, vn = (num(c["k_new"]), num(c["v_new"])) if new else (None, None)
+            ref, size = o4.attn(num(c["q"]), *(o4.pack(x) for x in c["codes"]), *c["scales"], c["table"], c["lens"], kn, vn,
+                                c["sees"], c["nodes"], c["scale"])
+            floor = (c["lens"].max() + n) * 2.0 ** -33 * size.max(-1, keepdims=True)
+            assert np.all(np.abs(got - ref) <= 2.0 ** -8 * np.abs(ref) + size * (2.0 ** -8 + 2.0 ** -10) + floor)
+    assert fc.fc_get_error() == "FC_OK"
+
+
+@pytest.mark.parametrize("n,H,G", [(1, 8, 2), (4, 16, 4), (20, 4, 2)])
+def test_attn_key_rows_of_zeros_and_a_cache_never_written(fc, n, H, G):
+    c = attn_case(n + 8, 2, n, H, G, [70, 333], 16, stale=False)
+    c["codes"][0][...] = 0
+    c["scales"][0][...] = 0
+    check_attn(fc, c)  # every cached key scores 0: the mean of the values
+    check_attn(fc, c, new=False)
+    n_pages = c["codes"][0].shape[0]
+    cache = fc.Kv4Cache.empty(n_pages, G, 16)
+    assert not run_attn(fc, c, new=False, cache=cache).any()
+    c["codes"][1][...] = 0
+    c["scales"][1][...] = 0
+    check_attn(fc, c, cache=cache)  # zeros weigh as much as the new tokens' scores leave them
+
+
+@pytest.mark.parametrize("n,H,G", [(4, 8, 4), (4, 16, 4), (20, 4, 2)])
+def test_attn_queries_of_other_sizes_beside_each_other(fc, n, H, G):
+    """A head's queries 2^20 times the others': it keeps to its own rows."""
+    c = attn_case(n + 11, 2, n, H, G, [200, 33], 16)
+    big = np.zeros(c["q"].shape[:3], bool)
+    big[:, 0] = True
+    ref, size = o4.attn(num(c["q"]), *(o4.pack(x) for x in c["codes"]), *c["scales"], c["table"], c["lens"], num(c["k_new"]),
+                        num(c["v_new"]), c["sees"], c["nodes"], c["scale"])
+    c["q"][:, 0] *= 2.0 ** 20
+    got = num(run_attn(fc, c))
+    assert np.isfinite(got).all()
+    assert np.all((np.abs(got - ref) <= 2.0 ** -8 * np.abs(ref) + size * (2.0 ** -8 + 2.0 ** -10))[~big])
+    assert fc.fc_get_error() == "FC_OK"
+
+
 # ------------------------------------------------------------------ product
 @pytest.mark.parametrize("M", [1, 2, 7, 8, 9, 16])
 @pytest.mark.parametrize("K,N,group", [(64, 1, 32), (64, 16, 64), (128, 33, 128), (320, 100, 64), (2048, 50, 32),
