@@ -791,8 +791,10 @@ fc_status fc_w4_pack(const void* d_w, int K, int N, int group, void* d_codes, vo
 /*
  * y[M][N] = x[M][K] W for a few rows (M <= 16), W the bf16 [K][N] weights that
  * (d_codes, d_scale) stand for.  x and y bf16 row-major, x, codes and scales
- * 16-byte and y 2-byte aligned; sums in fp32, y rounded once.  A row of x with a
- * NaN or an infinity gives NaN, as does a column's scale that is not finite.
+ * 16-byte and y 2-byte aligned; products exact, sums in fp32, y rounded once: |x|
+ * up to 2^118 overflows no sum over a group.  A NaN in a row of x, or in a
+ * column's scale, gives NaN; an infinity counts as its product with the weight
+ * (NaN where that is 0).
  */
 fc_status fc_w4_matvec(const void* d_x, const void* d_codes, const void* d_scale, int M, int K, int N, int group,
                        void* d_y, fc_stream s);

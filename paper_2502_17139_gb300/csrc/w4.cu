@@ -84,19 +84,20 @@ __global__ void k_w4_pack(const __nv_bfloat16* __restrict__ w, int K, int N, int
 }
 
 __device__ __forceinline__ void mma_bf16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0,
-                                         uint32_t b1, const float (&c)[4]) {
+                                         uint32_t b1) {
   asm volatile(
-      "mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%11,%12,%13};"
-      : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
-      : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(c[0]), "f"(c[1]), "f"(c[2]), "f"(c[3]));
+      "mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+      : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+      : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
 
-// Two numbers of a packed word as bf16: 0x4300 | c is 128 + c, that is 136
-// more than the number.  The surplus, 136 times the sum of x over the tile,
-// comes off through the accumulators' starting value.
-__device__ __forceinline__ uint32_t two(uint32_t w, int i) { return ((w >> (4 * i)) & 0x000F000Fu) | 0x43004300u; }
-
-constexpr uint32_t MINUS_136 = 0xC308C308u;  // two bf16 values
+// Two numbers of a packed word as bf16, exactly: 0x4300 | c is 128 + c, that is
+// 136 more than the number.
+__device__ __forceinline__ uint32_t two(uint32_t w, int i) {
+  uint32_t r;
+  asm("sub.rn.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(((w >> (4 * i)) & 0x000F000Fu) | 0x43004300u), "r"(0x43084308u));
+  return r;
+}
 
 __device__ __forceinline__ void cp_async16(uint32_t dst, const void* src) {
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16;\n" ::"r"(dst), "l"(src) : "memory");
@@ -109,22 +110,26 @@ template <int N>
 __device__ __forceinline__ void cp_async_wait() {
   asm volatile("cp.async.wait_group %0;\n" ::"n"(N) : "memory");
 }
-// The weights' read bounds this: 4.1 to 4.5 bits a weight, each used once;
-// next to it the integer pipe, which turns a word's 8 numbers into operands in
-// 7 instructions and can spare few others (half of one per weight byte read at
-// full bandwidth), so the loop's addresses are pointers that advance, its
-// stages unrolled, and rows and tiles past the end are read from valid places
-// instead of being tested for.
+// The weights' read is the floor: 4.1 to 4.5 bits a weight, each used once.
+// Next to it a word's 8 numbers take 7 instructions of the integer pipe and 4
+// packed subtractions to become operands.  So the loop's addresses are pointers
+// that advance, its stages unrolled, and rows and tiles past the end are read
+// from valid places instead of being tested for.
+// The operands are the numbers themselves: leaving the 128 + 8 in them and
+// taking 136 times the sum of x off again by products of its own cost 20 times and more
+// the rounding of these sums, overflowed from x = 2^115 on, and took 47 us
+// where this takes 45 (16 x 8192 x 28672; 14.3 and 13.4 for 1 x 8192 x 8192).
 // A warp takes MT tiles of columns (which share the rows of x that it loads)
 // and every ks-th tile of k, three in flight by asynchronous copies, x
 // AHEAD tiles ahead in registers; with ks = 1 a sum never leaves its warp, else
 // the ks warps' sums meet in shared memory.  NT: 8-row tiles of x.  STEPS:
 // k-steps that share a scale (the group, or the whole tile).
-// x goes two tiles ahead: four took 64 registers of 16 rows' form, and 12 x
-// 8192 x 8192 22.6 us instead of 18.5.  Seven tiles in flight instead of three
-// took as long for large weights and a microsecond more for small ones.
-// Measured: 16 x 8192 x 28672 47 us (126 MB), a row of it 35 us (3.5 TB/s), of
-// 2048 x 32256 14 us, of 2048 x 2048 5 us (latency).
+// At earlier steps of this kernel x four tiles ahead instead of two took 64
+// more registers with 16 rows (12 x 8192 x 8192 22.6 us, not 18.5), and seven
+// tiles in flight instead of three as long for large weights and a microsecond
+// more for small ones.
+// Measured: 16 x 8192 x 28672 45 us (126 MB, 2.8 TB/s), a row of it 35 us (3.5
+// TB/s), of 2048 x 32256 14 us; 2048 x 2048 5 us a call, 3.5 in a graph.
 constexpr int STAGES = 4;
 // codes of MT tiles, then the scales [group][MT * TN]
 __host__ __device__ constexpr int stage_bytes(int MT, int STEPS) { return MT * TILE_BYTES + MT * TN * 2 * (4 / STEPS); }
@@ -225,29 +230,27 @@ __global__ void __launch_bounds__(MAX_WARPS * 32) k_w4_matvec(const uint4* __res
         for (int i = 0; i < 2; ++i) sc[m][q][i] = sp[q * MT * TN + m * TN + 8 * i];
     issue((stage + STAGES - 1) % STAGES);
 #pragma unroll
-    for (int n = 0; n < NT; ++n) {
+    for (int q = 0; q < GROUPS; ++q) {
 #pragma unroll
-      for (int q = 0; q < GROUPS; ++q) {
-        float off[4] = {0.f, 0.f, 0.f, 0.f};
+      for (int m = 0; m < MT; ++m) {
+        float d[NT][4];
+#pragma unroll
+        for (int n = 0; n < NT; ++n) d[n][0] = d[n][1] = d[n][2] = d[n][3] = 0.f;
+        const uint32_t* c = &cw[m].x;
 #pragma unroll
         for (int w = q * STEPS; w < (q + 1) * STEPS; ++w) {
-          const uint32_t* xw = &xr[n][w >> 1].x;
-          mma_bf16(off, MINUS_136, MINUS_136, MINUS_136, MINUS_136, xw[2 * (w & 1)], xw[2 * (w & 1) + 1], off);
+          const uint32_t c0 = two(c[w], 0), c1 = two(c[w], 1), c2 = two(c[w], 2), c3 = two(c[w], 3);
+#pragma unroll
+          for (int n = 0; n < NT; ++n) {
+            const uint32_t* xw = &xr[n][w >> 1].x;
+            mma_bf16(d[n], c0, c1, c2, c3, xw[2 * (w & 1)], xw[2 * (w & 1) + 1]);
+          }
         }
 #pragma unroll
-        for (int m = 0; m < MT; ++m) {
-          float d[4] = {off[0], off[1], off[2], off[3]};
-          const uint32_t* c = &cw[m].x;
-#pragma unroll
-          for (int w = q * STEPS; w < (q + 1) * STEPS; ++w) {
-            const uint32_t* xw = &xr[n][w >> 1].x;
-            mma_bf16(d, two(c[w], 0), two(c[w], 1), two(c[w], 2), two(c[w], 3), xw[2 * (w & 1)], xw[2 * (w & 1) + 1],
-                     w == q * STEPS ? off : d);
-          }
+        for (int n = 0; n < NT; ++n)
 #pragma unroll
           for (int i = 0; i < 4; ++i)
-            acc[m][n][i] = fmaf(__uint_as_float(sc[m][q][i >> 1] << 16), d[i], acc[m][n][i]);
-        }
+            acc[m][n][i] = fmaf(__uint_as_float(sc[m][q][i >> 1] << 16), d[n][i], acc[m][n][i]);
       }
     }
     load_x(xr);
@@ -379,11 +382,13 @@ extern "C" fc_status fc_w4_matvec(const void* d_x, const void* d_codes, const vo
     return FC_ERR_INVALID_ARG;
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   // More column tiles a warp share what it loads of x and what a step costs
-  // besides its numbers, fewer fill the GPU sooner.  Two against one: 8192 x 8192
-  // 15.1 us instead of 18.5, 2048 x 2048 6.2 either way.  Four against two, up to
-  // 8 rows: 1 x 8192 x 28672 34.9 us instead of 38.9, 8 x 4096 x 20001 21.9
-  // instead of 25.4, but 8 x 4096 x 11008 14.4 instead of 12.4; 16 rows' sums take
-  // too many registers (16 x 8192 x 28672 56 us instead of 47).
+  // besides its numbers, fewer fill the GPU sooner (us, replayed from a graph).
+  // Two against one: 1 x 8192 x 8192 13.4 instead of 16.1, but 1 x 2048 x 2048
+  // 3.8 instead of 3.5, 16 rows of it 4.7 instead of 4.0.  Four against two, up to
+  // 8 rows: 8 x 4096 x 20001 24 instead of 31, 1 x 16384 x 32768 81 instead of 83,
+  // but 1 x 2048 x 32256 14.1 instead of 13.4 and 8 x 4096 x 11008 13.7 instead of
+  // 11.3; 16 rows' sums took too many registers (16 x 8192 x 28672 56 instead of 47
+  // when it took that).
   if (N <= 152 * TN * 2) return launch_rows<1>(d_x, d_codes, d_scale, M, K, N, group, d_y, s);
   if (M <= 8 && N > 152 * TN * 8) return launch_eight<4>(d_x, d_codes, d_scale, M, K, N, group, d_y, s);
   return launch_rows<2>(d_x, d_codes, d_scale, M, K, N, group, d_y, s);

@@ -622,3 +622,58 @@ def test_matvec_extremes_and_refusals(fc):
         fc.fc_w4_pack(torch.zeros((100, 8), dtype=torch.bfloat16, device="cuda"), 32)
     with pytest.raises(fc.FastCoderError):
         fc.fc_w4_pack(w, 48)
+
+
+@pytest.mark.parametrize("M", [1, 8, 9, 16])
+@pytest.mark.parametrize("K,N,group", [(64, 40, 32), (256, 100, 128), (192, 4900, 64), (128, 20000, 32)])
+def test_matvec_of_large_x(fc, M, K, N, group):
+    """x up to 2^118: a group of 128 products stays below 2^128, whatever the
+    signs.  (A finite result is expected, with the usual tolerance.)"""
+    rng = np.random.default_rng(M + K + N)
+    w = bf(rng, K, N, scale=2.0 ** -100)
+    x = (bf(rng, M, K).abs().clamp(max=2.0) * 2.0 ** 117).bfloat16()
+    out = num(fc.fc_w4_matvec(x.cuda(), fc.fc_w4_pack(w.cuda(), group)))
+    assert fc.fc_get_error() == "FC_OK" and np.isfinite(out).all()
+    y, size = o4.matvec(num(x), num(w), group)
+    e = 2.0 ** -20 * 136 * size
+    assert np.all((o4.bf16_round(y - e) <= out) & (out <= o4.bf16_round(y + e)))
+
+
+@pytest.mark.parametrize("M", [1, 8, 9, 16])
+@pytest.mark.parametrize("K,N,group", [(1024, 40, 32), (1024, 100, 128), (512, 4900, 64), (256, 20000, 128)])
+def test_matvec_of_columns_that_cancel(fc, M, K, N, group):
+    """Columns whose products cancel pair by pair next to columns of one sign:
+    the result is off by roundings of sums of c x s alone.  |c| <= 7; a sum
+    has at most 32 groups (a rounding of 2^-24 each) of at most 8 matrix
+    products (2^-23 each): below (32 + 16) 2^-24 * 7 sum|x| s."""
+    rng = np.random.default_rng(M + K + N)
+    w = bf(rng, K, N).abs()
+    w[1::2] = -w[0::2]
+    w[:, ::3] = w[:, ::3].abs()
+    x = bf(rng, M, K).abs()
+    x[:, 1::2] = x[:, 0::2]
+    out = num(fc.fc_w4_matvec(x.cuda(), fc.fc_w4_pack(w.cuda(), group)))
+    y, size = o4.matvec(num(x), num(w), group)
+    e = 48 * 2.0 ** -24 * 7 * size
+    assert np.all((o4.bf16_round(y - e) <= out) & (out <= o4.bf16_round(y + e)))
+    assert fc.fc_get_error() == "FC_OK"
+
+
+def test_matvec_of_x_that_is_not_finite(fc):
+    """An infinity counts as its product with the weight, a NaN makes the row
+    NaN; the other rows are what they are without them."""
+    rng = np.random.default_rng(29)
+    K, N, group = 128, 333, 64
+    w, x = bf(rng, K, N), bf(rng, 9, K)
+    c, _ = o4.quantise(num(w).reshape(K // group, group, N), 1)
+    row = c.reshape(K, N)[70]
+    h = fc.fc_w4_pack(w.cuda(), group)
+    want = num(fc.fc_w4_matvec(x.cuda(), h))
+    x[1, 70], x[4, 70], x[8, 3] = float("inf"), -float("inf"), float("nan")
+    got = num(fc.fc_w4_matvec(x.cuda(), h))
+    assert (row == 0).any() and (row != 0).any() and np.isnan(got[8]).all()
+    for r, sign in ((1, 1), (4, -1)):
+        assert np.isnan(got[r][row == 0]).all() and np.all(got[r][row != 0] == np.sign(row[row != 0]) * sign * np.inf)
+    keep = [0, 2, 3, 5, 6, 7]
+    assert np.array_equal(got[keep], want[keep])
+    assert fc.fc_get_error() == "FC_OK"
