@@ -767,8 +767,11 @@ fc_status fc_kv4_read(const fc_kv4_cache* cache, const int32_t* d_slot, int rows
  * A length or node count out of range, or a page id outside the pool, records
  * FC_ERR_INVALID_ARG (that request's rows are zeros; that page's keys are
  * left out).  What a page holds past a request's end is not looked at.  A new
- * token with a NaN or an infinity, or a cached row that stands for NaN, makes
- * NaN of the rows that see it, and of no others.
+ * token with a NaN in its key, or a NaN or an infinity in its value, or a cached
+ * row that stands for NaN, makes NaN of the rows that see it, and of no others;
+ * so does an infinity in a new key where its product with the query is +inf or
+ * NaN, and where it is -inf the token has no weight.  A query with a NaN makes
+ * its own row NaN.
  */
 fc_status fc_kv4_attn(const void* d_q, const fc_kv4_cache* cache, const int32_t* d_table, int max_pages,
                       const int32_t* d_kv_len, const void* d_k_new, const void* d_v_new, const uint64_t* d_mask,

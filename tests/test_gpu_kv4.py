@@ -566,6 +566,27 @@ def test_attn_queries_of_other_sizes_beside_each_other(fc, n, H, G):
     assert fc.fc_get_error() == "FC_OK"
 
 
+@pytest.mark.parametrize("sign", [1, -1])
+@pytest.mark.parametrize("n,H,G", [(3, 4, 2), (7, 4, 2), (40, 4, 2), (128, 4, 2)])
+def test_attn_an_infinite_key_counts_as_its_product(fc, n, H, G, sign):
+    """Where the product with the query is +inf the row is NaN, where it is
+    -inf the key has no weight; rows that do not see it are untouched."""
+    c = attn_case(n + 13, 2, n, H, G, [300, 0], 64)
+    c["k_new"][:, :, 1, 3] = sign * float("inf")
+    up = num(c["q"])[..., 3] * sign > 0
+    sees = np.broadcast_to(c["sees"][:, :, 1, None], up.shape)
+    assert (up & sees).any() and (~up & sees).any() and (~sees).any()
+    with np.errstate(invalid="ignore"):
+        ref, size = o4.attn(num(c["q"]), *(o4.pack(x) for x in c["codes"]), *c["scales"], c["table"], c["lens"],
+                            num(c["k_new"]), num(c["v_new"]), c["sees"], c["nodes"], c["scale"])
+    hit = up & sees
+    for ws in (True, False):
+        got = num(run_attn(fc, c, ws=ws))
+        assert np.isnan(got[hit]).all() and np.isfinite(got[~hit]).all()
+        assert np.all(np.abs(got - ref)[~hit] <= (2.0 ** -8 * np.abs(ref) + size * (2.0 ** -8 + 2.0 ** -10))[~hit])
+    assert fc.fc_get_error() == "FC_OK"
+
+
 # ------------------------------------------------------------------ product
 @pytest.mark.parametrize("M", [1, 2, 7, 8, 9, 16])
 @pytest.mark.parametrize("K,N,group", [(64, 1, 32), (64, 16, 64), (128, 33, 128), (320, 100, 64), (2048, 50, 32),
