@@ -695,7 +695,8 @@ typedef struct {
  * records FC_ERR_CAPACITY, one with a negative length FC_ERR_INVALID_ARG (as
  * does a free count outside 0..n_pages, read as 0, or a page id outside the
  * pool).  The same inputs give the same outputs, so a call can be repeated.
- * One launch.
+ * One launch; with batch 0 and rows_cap 0 none, and no output is written: the
+ * free count is what it was.
  */
 fc_status fc_kv_pages_plan(const int32_t* d_kv_len, const int32_t* d_n_new, int batch, int page_size,
                            int32_t* d_table, int max_pages, const int32_t* d_free, int n_pages,
@@ -708,7 +709,7 @@ fc_status fc_kv_pages_plan(const int32_t* d_kv_len, const int32_t* d_n_new, int 
  * (0: it is finished); the pages past them go on the end of the free list
  * [n_pages], in request order.  d_kv_len_out, d_n_free_out as above.  More
  * pages than the pool holds, or a negative length, record FC_ERR_INVALID_ARG
- * (what does not fit is not given back).
+ * (what does not fit is not given back).  With batch 0 no output is written.
  */
 fc_status fc_kv_pages_release(const int32_t* d_kv_len, const int32_t* d_keep, int batch, int page_size,
                               const int32_t* d_table, int max_pages, int32_t* d_free, int n_pages,

@@ -847,6 +847,9 @@ def fc_kv_pages_plan(pages: KvPages, kv_len, n_new, n_free, rows_cap=None, path=
     src = out.get("src") if n_per_seq else None
     if n_per_seq and src is None:
         raise ValueError("out has no src")
+    if B == 0 and out["seq"].numel() == 0:  # the call writes nothing then
+        out["cu"].zero_()
+        out["n_free"].copy_(n_free)
     _check("fc_kv_pages_plan", LIB.fc_kv_pages_plan(
         kv_len.data_ptr(), n_new.data_ptr(), B, pages.page_size, pages.table.data_ptr(), pages.max_pages,
         pages.free.data_ptr(), pages.n_pages, n_free.data_ptr(), None if path is None else path.data_ptr(),
@@ -864,6 +867,8 @@ def fc_kv_pages_release(pages: KvPages, kv_len, keep, n_free, out=None):
     _need(keep, torch.int32, "keep", (B,))
     _need(n_free, torch.int32, "n_free", (1,))
     kv_out, free_out = out if out is not None else (torch.empty_like(kv_len), torch.empty_like(n_free))
+    if B == 0:  # the call writes nothing then
+        free_out.copy_(n_free)
     _check("fc_kv_pages_release", LIB.fc_kv_pages_release(
         kv_len.data_ptr(), keep.data_ptr(), B, pages.page_size, pages.table.data_ptr(), pages.max_pages,
         pages.free.data_ptr(), pages.n_pages, n_free.data_ptr(), kv_out.data_ptr(), free_out.data_ptr(), _stream()))

@@ -140,6 +140,25 @@ def test_release_gives_the_pages_back_in_order(fc):
     assert fc.fc_get_error() == "FC_ERR_INVALID_ARG" and len(free) - 4 <= free_out.item() <= len(free)
 
 
+@pytest.mark.parametrize("rows_cap", [0, 3])
+def test_an_empty_plan_and_an_empty_release_carry_the_free_count_over(fc, rows_cap):
+    """No requests: the outputs say so, whatever they held."""
+    i32 = dict(dtype=torch.int32, device="cuda")
+    none, n_free = torch.empty(0, **i32), torch.full((1,), 7, **i32)
+    pages = fc.KvPages(16, torch.empty((0, 4), **i32), torch.arange(9, **i32))
+    out = fc.kv_pages_outputs(0, rows_cap, "cuda", src=True)
+    for t in out.values():
+        t.fill_(99)
+    fc.fc_kv_pages_plan(pages, none, none, n_free, n_per_seq=4, out=out)
+    assert out["n_free"].tolist() == [7] and out["cu"].tolist() == [0]
+    for k in ("seq", "pos", "slot", "src"):
+        assert out[k].tolist() == [-1] * rows_cap
+    kept = (torch.empty(0, **i32), torch.full((1,), 99, **i32))
+    kv, free = fc.fc_kv_pages_release(pages, none, none, n_free, out=kept)
+    assert kv.numel() == 0 and free.tolist() == [7] and n_free.tolist() == [7]
+    assert fc.fc_get_error() == "FC_OK"
+
+
 # ------------------------------------------------------------- write, read
 def rows_of(rng, kind, R, H):
     """(k, v) tensors of three layouts that hold the same kind of rows."""
