@@ -817,6 +817,14 @@ class KvPages:
         self.n_pages = free.numel()
 
 
+def _need_ints(named):
+    """Each (name, tensor, n): n int32 values, dense, on the GPU."""
+    for name, t, n in named:
+        if not (t.dtype is torch.int32 and t.is_cuda and t.is_contiguous() and t.numel() == n):
+            _need(t, torch.int32, name)
+            raise ValueError(f"{name} must have {n} elements, got {t.numel()}")
+
+
 def kv_pages_outputs(batch, rows_cap, device, src=False):
     """Output tensors of fc_kv_pages_plan (``src`` too when wanted)."""
     e = lambda n: torch.empty(n, dtype=torch.int32, device=device)
@@ -838,7 +846,7 @@ def fc_kv_pages_plan(pages: KvPages, kv_len, n_new, n_free, rows_cap=None, path=
     _need(n_free, torch.int32, "n_free", (1,))
     if path is not None:
         _need(path, torch.int32, "path")
-        if path.dim() != 2 or path.shape[0] != B or not n_per_seq:
+        if path.dim() != 2 or path.shape[0] != B or path.shape[1] < 1 or not n_per_seq:
             raise ValueError("path must be [B, path_cap], with n_per_seq")
     if out is None:
         if rows_cap is None:
@@ -847,15 +855,26 @@ def fc_kv_pages_plan(pages: KvPages, kv_len, n_new, n_free, rows_cap=None, path=
     src = out.get("src") if n_per_seq else None
     if n_per_seq and src is None:
         raise ValueError("out has no src")
-    if B == 0 and out["seq"].numel() == 0:  # the call writes nothing then
-        out["cu"].zero_()
-        out["n_free"].copy_(n_free)
+    i32, cu, seq, pos, slot, kv, nf = (torch.int32, out["cu"], out["seq"], out["pos"], out["slot"], out["kv_len"],
+                                       out["n_free"])
+    rows = seq.numel()
+    if not (cu.dtype is i32 and seq.dtype is i32 and pos.dtype is i32 and slot.dtype is i32 and kv.dtype is i32 and
+            nf.dtype is i32 and pos.numel() == rows and slot.numel() == rows and cu.numel() == B + 1 and
+            kv.numel() == B and nf.numel() == 1 and cu.is_cuda and seq.is_cuda and pos.is_cuda and slot.is_cuda and
+            kv.is_cuda and nf.is_cuda and cu.is_contiguous() and seq.is_contiguous() and pos.is_contiguous() and
+            slot.is_contiguous() and kv.is_contiguous() and nf.is_contiguous()):  # one test for the usual case
+        _need_ints((("seq", seq, rows), ("pos", pos, rows), ("slot", slot, rows), ("cu", cu, B + 1),
+                    ("kv_len of out", kv, B), ("n_free of out", nf, 1)))
+    if src is not None:
+        _need_ints((("src", src, rows),))
+    if B == 0 and rows == 0:  # the call writes nothing then
+        cu.zero_()
+        nf.copy_(n_free)
     _check("fc_kv_pages_plan", LIB.fc_kv_pages_plan(
         kv_len.data_ptr(), n_new.data_ptr(), B, pages.page_size, pages.table.data_ptr(), pages.max_pages,
         pages.free.data_ptr(), pages.n_pages, n_free.data_ptr(), None if path is None else path.data_ptr(),
-        0 if path is None else path.shape[1], n_per_seq, out["seq"].numel(), out["cu"].data_ptr(),
-        out["seq"].data_ptr(), out["pos"].data_ptr(), out["slot"].data_ptr(), None if src is None else src.data_ptr(),
-        out["kv_len"].data_ptr(), out["n_free"].data_ptr(), _stream()))
+        0 if path is None else path.shape[1], n_per_seq, rows, cu.data_ptr(), seq.data_ptr(), pos.data_ptr(),
+        slot.data_ptr(), None if src is None else src.data_ptr(), kv.data_ptr(), nf.data_ptr(), _stream()))
     return out
 
 
@@ -867,6 +886,7 @@ def fc_kv_pages_release(pages: KvPages, kv_len, keep, n_free, out=None):
     _need(keep, torch.int32, "keep", (B,))
     _need(n_free, torch.int32, "n_free", (1,))
     kv_out, free_out = out if out is not None else (torch.empty_like(kv_len), torch.empty_like(n_free))
+    _need_ints((("kv_len of out", kv_out, B), ("n_free of out", free_out, 1)))
     if B == 0:  # the call writes nothing then
         free_out.copy_(n_free)
     _check("fc_kv_pages_release", LIB.fc_kv_pages_release(
@@ -980,7 +1000,11 @@ def fc_kv4_attn(q, cache: Kv4Cache, table, kv_len, k_new=None, v_new=None, mask=
         out = torch.empty_like(q)
     else:
         _need(out, torch.bfloat16, "out", q.shape)
-    ws, ws_bytes = (None, 0) if workspace is None else (workspace.data_ptr(), workspace.numel() * workspace.element_size())
+    ws, ws_bytes = None, 0
+    if workspace is not None:
+        if not (workspace.is_cuda and workspace.is_contiguous()):
+            raise ValueError("workspace must be a dense tensor on a CUDA device")
+        ws, ws_bytes = workspace.data_ptr(), workspace.numel() * workspace.element_size()
     _check("fc_kv4_attn", LIB.fc_kv4_attn(q.data_ptr(), cache.ref, table.data_ptr(), table.shape[1], kv_len.data_ptr(), kp,
                                           vp, mp, np_, B, Np, H, D ** -0.5 if scale is None else float(scale),
                                           out.data_ptr(), ws, ws_bytes, _stream()))
@@ -992,12 +1016,18 @@ class W4Weight:
     codes (uint8), scale bf16 [K / group, N]."""
 
     def __init__(self, codes, scale, K, N, group):
+        _need(codes, torch.uint8, "codes", (int(LIB.fc_w4_codes_bytes(K, N)),))
+        if group < 1:
+            raise ValueError("group must be 32, 64 or 128")
+        _need(scale, torch.bfloat16, "scale", (K // group, N))
         self.codes, self.scale, self.K, self.N, self.group = codes, scale, int(K), int(N), int(group)
 
 
 def fc_w4_pack(w, group=128) -> W4Weight:
     """w bf16 [K, N] -> W4Weight, one scale for ``group`` weights of a column."""
     _need(w, torch.bfloat16, "w")
+    if group < 1:
+        raise ValueError("group must be 32, 64 or 128")
     K, N = w.shape
     n = int(LIB.fc_w4_codes_bytes(K, N))
     if n == 0:

@@ -717,3 +717,42 @@ def test_matvec_of_x_that_is_not_finite(fc):
     keep = [0, 2, 3, 5, 6, 7]
     assert np.array_equal(got[keep], want[keep])
     assert fc.fc_get_error() == "FC_OK"
+
+
+def test_binding_refuses_outputs_that_are_too_small(fc):
+    """Nothing is launched: a call would write past their ends, or read what is
+    no device memory."""
+    i32 = dict(dtype=torch.int32, device="cuda")
+    B, rows = 3, 8
+    pages = fc.KvPages(16, torch.zeros((B, 4), **i32), torch.arange(12, **i32))
+    kv, new, n_free = torch.zeros(B, **i32), torch.full((B,), 2, **i32), torch.full((1,), 12, **i32)
+    for k, n in (("pos", rows - 1), ("slot", rows + 1), ("src", rows - 1), ("cu", B), ("kv_len", B - 1), ("n_free", 0)):
+        out = fc.kv_pages_outputs(B, rows, "cuda", src=True)
+        out[k] = torch.empty(n, **i32)
+        with pytest.raises(ValueError):
+            fc.fc_kv_pages_plan(pages, kv, new, n_free, n_per_seq=2, out=out)
+    for k, bad in (("seq", torch.empty(rows, dtype=torch.int64, device="cuda")), ("slot", torch.empty(rows, dtype=torch.int16, device="cuda")),
+                   ("pos", torch.empty(rows, dtype=torch.int32)), ("cu", torch.empty(2 * (B + 1), **i32)[::2])):
+        with pytest.raises((TypeError, ValueError)):
+            fc.fc_kv_pages_plan(pages, kv, new, n_free, out=dict(fc.kv_pages_outputs(B, rows, "cuda"), **{k: bad}))
+    with pytest.raises(ValueError):
+        fc.fc_kv_pages_plan(pages, kv, new, n_free, rows_cap=rows, path=torch.empty((B, 0), **i32), n_per_seq=2)
+    for bad in ((torch.empty(B - 1, **i32), torch.empty(1, **i32)), (torch.empty(B, **i32), torch.empty(0, **i32)),
+                (torch.empty(B, dtype=torch.int64, device="cuda"), torch.empty(1, **i32))):
+        with pytest.raises((TypeError, ValueError)):
+            fc.fc_kv_pages_release(pages, kv, kv, n_free, out=bad)
+    cache = fc.Kv4Cache.empty(12, 2, 16)
+    q = torch.zeros((B, 1, 4, 128), dtype=torch.bfloat16, device="cuda")
+    ws = fc.kv4_attn_workspace(B, 1, 4, 2, "cuda")
+    for bad in (ws.cpu(), ws[::2]):
+        with pytest.raises(ValueError):
+            fc.fc_kv4_attn(q, cache, pages.table, kv, workspace=bad)
+    h = fc.fc_w4_pack(torch.zeros((128, 40), dtype=torch.bfloat16, device="cuda"), 64)
+    fc.W4Weight(h.codes, h.scale, 128, 40, 64)
+    for bad in ((h.codes[:-1], h.scale, 128, 40, 64), (h.codes, h.scale, 128, 56, 64), (h.codes, h.scale, 128, 40, 32),
+                (h.codes.cpu(), h.scale, 128, 40, 64), (h.codes, h.scale.float(), 128, 40, 64), (h.codes, h.scale, 128, 40, 0)):
+        with pytest.raises((TypeError, ValueError)):
+            fc.W4Weight(*bad)
+    with pytest.raises(ValueError):
+        fc.fc_w4_pack(torch.zeros((128, 40), dtype=torch.bfloat16, device="cuda"), 0)
+    assert fc.fc_get_error() == "FC_OK"
