@@ -930,8 +930,12 @@ def fc_kv4_write(cache: Kv4Cache, k, v, slot, src=None):
     st, shape = k.stride(), k.shape
     if not (k.is_cuda and v.is_cuda):
         raise ValueError("k and v must be on a CUDA device")
-    if v.shape != shape or v.stride() != st:
-        raise ValueError("k and v must have the same shape and strides")
+    if v.shape != shape:
+        raise ValueError("k and v must have the same shape")
+    if v.stride() != st or 1 in shape:  # a dimension of 1 has no stride that matters
+        st, sv = ([0 if n == 1 else s for n, s in zip(shape, t.stride())] for t in (k, v))
+        if sv != st:
+            raise ValueError("k and v must have the same strides")
     if len(shape) not in (3, 4) or shape[-2] != cache.Hkv or shape[-1] != cache.D or st[-1] != 1:
         raise ValueError("k and v must be [rows, Hkv, D] or [B, n, Hkv, D] with a dense last dimension")
     _need(slot, torch.int32, "slot")

@@ -264,6 +264,23 @@ def test_write_binding_checks(fc):
         fc.fc_kv4_write(cache, k, k, slot.long())
 
 
+def test_write_looks_at_no_stride_of_a_dimension_of_one(fc):
+    """One row, or one head: whatever stride its dimension has is never used."""
+    rng = np.random.default_rng(23)
+    flat = bf(rng, 40 * 128).cuda()
+    one = lambda at, s: torch.as_strided(flat, (3, 1, 128), (256, s, 1), at)
+    row = lambda at, s: torch.as_strided(flat, (1, 2, 128), (s, 128, 1), at)
+    for k, v, H in ((row(0, 5), row(512, 768), 2), (one(0, 3), one(128, 77), 1), (one(0, 128)[None], one(128, 5)[None], 1)):
+        rows = k.numel() // (128 * H)
+        cache, slot = fc.Kv4Cache.empty(1, H, 16), torch.arange(rows, dtype=torch.int32, device="cuda")
+        fc.fc_kv4_write(cache, k, v, slot)
+        for x, codes, scale in ((k, cache.k_codes, cache.k_scale), (v, cache.v_codes, cache.v_scale)):
+            c, s = o4.quantise(num(x).reshape(rows, H, 128))
+            assert np.array_equal(codes.cpu().numpy()[0, :, :rows].swapaxes(0, 1), o4.pack(c))
+            assert np.array_equal(num(scale)[0, :, :rows].T, s)
+    assert fc.fc_get_error() == "FC_OK"
+
+
 # --------------------------------------------------------------- attention
 def random_cache(rng, n_pages, G, page):
     codes = [np.clip(np.rint(rng.standard_normal((n_pages, G, page, 128)) * 2.6), -7, 7).astype(np.int64) for _ in range(2)]
