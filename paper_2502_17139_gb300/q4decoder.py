@@ -6,7 +6,9 @@ one small draft tree (batch * nodes <= 16).
 A step: forward() runs the rows against the caches, with the new tokens' own
 keys and values in bf16; append() plans where the kept ones go
 (fc_kv_pages_plan, once) and quantises them into every layer's pages
-(fc_kv4_write).  All on the current stream, no host round trip.
+(fc_kv4_write).  All on the current stream, no host round trip.  Both read and
+write the same tensors at every step, so that a step captured in a CUDA graph
+is good for all of them.
 
     python -m paper_2502_17139_gb300.q4decoder [batch] [context]
 
@@ -42,10 +44,13 @@ class Q4Decoder:
         self.pages = fc.KvPages(page_size, torch.zeros((batch, max_pages), **i32),
                                 torch.arange(n_pages - 1, -1, -1, **i32))
         self.caches = [fc.Kv4Cache.empty(n_pages, s.Hkv, page_size, s.D, device) for _ in range(s.layers)]
-        # lengths and the free count alternate between two places, as a plan's in and out
-        self.kv_len = [torch.zeros(batch, **i32), torch.zeros(batch, **i32)]
-        self.n_free = [torch.full((1,), n_pages, **i32), torch.zeros(1, **i32)]
-        self.cur = 0
+        # lengths and the free count: the current ones, and a plan's results, which
+        # are copied back (a plan's outputs are not its inputs)
+        self.state = torch.zeros((2, batch + 1), **i32)
+        self.state[0, batch] = n_pages
+        self.kv_len = [self.state[0, :batch], self.state[1, :batch]]
+        self.n_free = [self.state[0, batch:], self.state[1, batch:]]
+        self.cur = 0  # the place of the current ones
         self.plan = fc.kv_pages_outputs(batch, batch * nodes, device, src=True)
         R = batch * nodes
         bf = lambda *shape_: torch.empty(shape_, dtype=torch.bfloat16, device=device)
@@ -62,7 +67,7 @@ class Q4Decoder:
         """tok [B, n] int32 -> logits [B, n, vocab].  pos [B, n] (None: the
         tokens follow the cache in order), mask [B, n, 1] int64 ancestor bits
         (None: each sees those before it), n_nodes [B]."""
-        s, B, n, kv_len = self.s, self.B, self.n, self.kv_len[self.cur]
+        s, B, n, kv_len = self.s, self.B, self.n, self.kv_len[0]
         if pos is None:
             pos = kv_len[:, None] + self.steps
         fc.fc_embed(tok.reshape(-1), self.embed, self.x)
@@ -90,21 +95,18 @@ class Q4Decoder:
     def append(self, n_keep=None, path=None):
         """Keeps the step's first n_keep[b] tokens of each sequence (None: all),
         or those of an accepted path [B, path_cap], in the caches."""
-        c = self.cur
-        out = dict(self.plan, kv_len=self.kv_len[1 - c], n_free=self.n_free[1 - c])
-        fc.fc_kv_pages_plan(self.pages, self.kv_len[c], self.ones if n_keep is None else n_keep, self.n_free[c], path=path,
+        out = dict(self.plan, kv_len=self.kv_len[1], n_free=self.n_free[1])
+        fc.fc_kv_pages_plan(self.pages, self.kv_len[0], self.ones if n_keep is None else n_keep, self.n_free[0], path=path,
                             n_per_seq=self.n, out=out)
+        self.state[0].copy_(self.state[1])
         for cache, k, v in zip(self.caches, self.k_new, self.v_new):
             fc.fc_kv4_write(cache, k.transpose(1, 2), v.transpose(1, 2), out["slot"], src=out["src"])
-        self.cur = 1 - c
 
     def release(self, keep):
         """Sequence b keeps its first keep[b] tokens (0: it is finished); its
         other pages are free again."""
-        c = self.cur
-        fc.fc_kv_pages_release(self.pages, self.kv_len[c], keep, self.n_free[c],
-                               out=(self.kv_len[1 - c], self.n_free[1 - c]))
-        self.cur = 1 - c
+        fc.fc_kv_pages_release(self.pages, self.kv_len[0], keep, self.n_free[0], out=(self.kv_len[1], self.n_free[1]))
+        self.state[0].copy_(self.state[1])
 
     def generate(self, tok, steps):
         """Greedy decoding of ``steps`` tokens from tok [B] (nodes = 1): [B, steps]."""
@@ -122,23 +124,30 @@ def main(batch=1, context=4096, steps=20):
     from .decoder import DEEPSEEK_CODER_1_3B as shape
     s = shape
     W = synth.decoder_weights(s.hidden, s.layers, s.H, s.Hkv, s.D, s.inter, s.vocab, 7, device="cuda")
-    most = -(-(context + 2 * steps + 2) // 64)
+    held, most = -(-context // 64), -(-(context + 2 * steps + 4) // 64)
     dec = Q4Decoder(s, W, batch, batch * most, most)
-    # a context of random numbers, as if it had been decoded
-    dec.pages.table.copy_(torch.arange(batch * most, dtype=torch.int32).view(batch, most))
+    # a context of random numbers, as if it had been decoded: the pages at the pool's end
+    order = torch.arange(batch * most - 1, -1, -1, dtype=torch.int32, device="cuda")
+    dec.pages.table[:, :held] = order[:batch * held].view(batch, held)
     dec.kv_len[dec.cur].fill_(context)
-    dec.n_free[dec.cur].zero_()
+    dec.n_free[dec.cur].fill_(batch * (most - held))
+    dec.pages.free.copy_(torch.arange(batch * most, dtype=torch.int32))
     for c in dec.caches:
         c.k_codes.random_(0x11, 0xFF)
         c.v_codes.random_(0x11, 0xFF)
         c.k_scale.fill_(0.1)
         c.v_scale.fill_(0.1)
     tok = torch.zeros((batch, 1), dtype=torch.int32, device="cuda")
-    for _ in range(3):
+
+    def step():
         dec.forward(tok)
+        dec.append()
+
+    for _ in range(3):
+        step()
     g = torch.cuda.CUDAGraph()
     with torch.cuda.graph(g):
-        dec.forward(tok)
+        step()
     a, b = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
     torch.cuda.synchronize()
     a.record()
@@ -147,8 +156,9 @@ def main(batch=1, context=4096, steps=20):
     b.record()
     torch.cuda.synchronize()
     assert fc.fc_get_error() == "FC_OK"
+    assert dec.kv_len[dec.cur].tolist() == [context + 3 + steps] * batch
     ms = a.elapsed_time(b) / steps
-    print(f"batch {batch}, context {context}: {ms:.3f} ms a step, {batch / ms * 1e3:.0f} tokens/s (forward, from a graph)")
+    print(f"batch {batch}, context {context}: {ms:.3f} ms a step, {batch / ms * 1e3:.0f} tokens/s (forward and append, from a graph)")
 
 
 if __name__ == "__main__":

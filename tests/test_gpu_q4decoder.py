@@ -161,3 +161,36 @@ def test_greedy_decoding_takes_the_largest_logit(weights):
         b.append()
         assert torch.equal(got[:, t], tok)
     assert a.kv_len[a.cur].tolist() == [20, 20]
+
+
+def test_a_captured_step_is_good_for_every_step(weights):
+    """forward() and append() captured once and replayed follow the same calls
+    made one by one, over page boundaries and a release."""
+    from paper_2502_17139_gb300 import fastcoder as fc
+    from paper_2502_17139_gb300.q4decoder import Q4Decoder
+    shape, W = weights
+    a, b = (Q4Decoder(shape, W, 2, 8, 4, page_size=16) for _ in range(2))
+    tok = torch.zeros((2, 1), dtype=torch.int32, device="cuda")
+    gen = torch.Generator(device="cuda").manual_seed(9)
+    g = None
+    for t in range(40):
+        if t == 25:
+            for d in (a, b):
+                d.release(torch.tensor([3, 19], dtype=torch.int32, device="cuda"))
+        tok.copy_(torch.randint(0, VOCAB, (2, 1), generator=gen, dtype=torch.int32, device="cuda"))
+        want = b.forward(tok).clone()
+        b.append()
+        if t < 2:  # the steps before the capture
+            got = a.forward(tok)
+            a.append()
+        else:
+            if g is None:
+                torch.cuda.synchronize()
+                g = torch.cuda.CUDAGraph()
+                with torch.cuda.graph(g):
+                    got = a.forward(tok)
+                    a.append()
+            g.replay()
+        assert torch.equal(got, want), t
+    assert a.kv_len[a.cur].tolist() == b.kv_len[b.cur].tolist() == [18, 34]
+    assert fc.fc_get_error() == "FC_OK"
