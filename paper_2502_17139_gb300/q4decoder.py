@@ -94,7 +94,9 @@ class Q4Decoder:
 
     def append(self, n_keep=None, path=None):
         """Keeps the step's first n_keep[b] tokens of each sequence (None: all),
-        or those of an accepted path [B, path_cap], in the caches."""
+        or those of an accepted path [B, path_cap], in the caches.  A sequence
+        whose tokens find no free page keeps its length and none of them, and
+        fc_get_error() says FC_ERR_CAPACITY."""
         out = dict(self.plan, kv_len=self.kv_len[1], n_free=self.n_free[1])
         fc.fc_kv_pages_plan(self.pages, self.kv_len[0], self.ones if n_keep is None else n_keep, self.n_free[0], path=path,
                             n_per_seq=self.n, out=out)
@@ -109,13 +111,19 @@ class Q4Decoder:
         self.state[0].copy_(self.state[1])
 
     def generate(self, tok, steps):
-        """Greedy decoding of ``steps`` tokens from tok [B] (nodes = 1): [B, steps]."""
+        """Greedy decoding of ``steps`` tokens from tok [B] (nodes = 1): [B, steps].
+        Waits for them, and raises FastCoderError if an error was recorded: a
+        sequence that found no free page (FC_ERR_CAPACITY) kept its length
+        there, so that its later tokens are not to be used."""
         out, root = [], torch.full((self.B, 1), -1, dtype=torch.int32, device=tok.device)
         for _ in range(steps):
             tok = tok.view(self.B, 1)
             tok = fc.fc_argmax_accept(self.forward(tok), tok, root, self.ones, 2)["bonus"]
             self.append()
             out.append(tok)
+        status = fc.LIB.fc_get_error(fc._stream())
+        if status:
+            raise fc.FastCoderError("Q4Decoder.generate", status)
         return torch.stack(out, 1)
 
 

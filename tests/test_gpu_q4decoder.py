@@ -194,3 +194,19 @@ def test_a_captured_step_is_good_for_every_step(weights):
         assert torch.equal(got, want), t
     assert a.kv_len[a.cur].tolist() == b.kv_len[b.cur].tolist() == [18, 34]
     assert fc.fc_get_error() == "FC_OK"
+
+
+def test_generate_says_when_the_pool_is_empty(weights):
+    """A sequence that finds no page cannot go on: no tokens, but an error."""
+    from paper_2502_17139_gb300 import fastcoder as fc
+    from paper_2502_17139_gb300.q4decoder import Q4Decoder
+    shape, W = weights
+    tok = torch.tensor([5, 7], dtype=torch.int32, device="cuda")
+    dec = Q4Decoder(shape, W, 2, 3, 4, page_size=16)  # pages for 32 and 16 tokens
+    with pytest.raises(fc.FastCoderError) as e:
+        dec.generate(tok, 20)
+    assert e.value.status == "FC_ERR_CAPACITY"
+    assert sorted(dec.kv_len[dec.cur].tolist()) == [16, 20]
+    assert fc.fc_get_error() == "FC_OK"
+    dec.release(torch.zeros(2, dtype=torch.int32, device="cuda"))
+    assert dec.generate(tok, 16).shape == (2, 16)
