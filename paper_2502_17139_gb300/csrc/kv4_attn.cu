@@ -151,12 +151,15 @@ __device__ __forceinline__ float hi_f(uint32_t w) { return __uint_as_float(w & 0
 // two chunks) each fall in different banks.  Every address below is one of
 // three lane constants plus an immediate.
 
+// steps of a length up to 2^31 - 1, whose rounding up passes an int
+__device__ __forceinline__ int steps_of(int kvl) { return (int)(((uint32_t)kvl + STEP - 1) / STEP); }
+
 __device__ __forceinline__ int few_steps(const Kv4Args& a, int b, int& nn, int& kvl, bool& bad) {
   kvl = a.kv_len[b];
   nn = a.n_nodes ? a.n_nodes[b] : a.n_pad;
   bad = nn < 0 || nn > a.n_pad || kvl < 0 || kvl > (long long)a.max_pages << a.shift;
   if (bad) nn = kvl = 0;
-  return nn == 0 ? 1 : max(1, (kvl + STEP - 1) / STEP + (a.k_new ? 1 : 0));
+  return nn == 0 ? 1 : max(1, steps_of(kvl) + (a.k_new ? 1 : 0));
 }
 
 // parts that a unit of so many steps is worth (0: like 1)
@@ -272,7 +275,7 @@ __global__ void __launch_bounds__(FEW_THREADS, NT == 1 ? 2 : 1) k_kv4_attn_few(F
       return f.part + (2 * c + (!parts && cut.start(c) < unit_base ? 1 : 0)) * (L::ROWS * (HD + 2));
     };
     if (bad && gh == 0 && s0 == 0 && tid == 0) fc_flag(FC_ERR_WORD(a.err), FC_EBIT_INVALID);
-    const int c_steps = nn == 0 ? 0 : (kvl + STEP - 1) / STEP;
+    const int c_steps = nn == 0 ? 0 : steps_of(kvl);
     const int R = nn * a.G;  // rows in use: node-major, r = node * G + head in group
     auto node_of = [&](int r) { return (int)((uint32_t)r * f.by_G >> 16); };
     auto q_row = [&](int r) {

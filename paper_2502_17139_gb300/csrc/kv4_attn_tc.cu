@@ -328,7 +328,7 @@ struct Walk {
     r.R = r.nn * a.G;
     r.n_chunks = max(1, (r.R + ROWS - 1) / ROWS);
     r.rows_each = (r.R + r.n_chunks - 1) / r.n_chunks;
-    r.cached = r.R ? (r.kvl + BN - 1) / BN : 0;
+    r.cached = r.R ? (int)(((uint32_t)r.kvl + BN - 1) / BN) : 0;  // lengths up to 2^31 - 1
     r.blocks = max(1, r.cached + (a.k_new && r.R ? 1 : 0));
     r.w = r.rows_each > BM ? 2 : 1;
     return r;

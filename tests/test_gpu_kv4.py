@@ -623,6 +623,29 @@ def test_attn_an_infinite_key_counts_as_its_product(fc, n, H, G, sign):
     assert fc.fc_get_error() == "FC_OK"
 
 
+@pytest.mark.parametrize("L", [2 ** 31 - 1, 2 ** 31 - 200, 2 ** 31 - 40])
+@pytest.mark.parametrize("n,tol", [(1, 2.0 ** -7 + 2.0 ** -7), (20, 2.0 ** -7 + 0.053)])
+def test_attn_of_a_length_just_below_32_bits(fc, L, n, tol):
+    """One page again and again: all keys score alike, so that the result is
+    the page's mean.  Roundings of two bf16 (2^-7), and of the fp32 sums: 56,000
+    (of one token's warps) or 442,000 (of a tile) products one after another, each
+    off by up to 2^-23 of the sum so far."""
+    rng = np.random.default_rng(n)
+    v = rng.integers(1, 8, (256, 128))
+    cache = fc.Kv4Cache.empty(1, 1, 256)
+    cache.k_codes.copy_(dev(o4.pack(np.zeros((1, 1, 256, 128), np.int64))))
+    cache.v_codes.copy_(dev(o4.pack(v)[None, None]))
+    cache.k_scale.fill_(1)
+    cache.v_scale.fill_(1)
+    q = bf(rng, 1, n, 1, 128).cuda()
+    table = torch.zeros((1, 2 ** 23), dtype=torch.int32, device="cuda")
+    out = fc.fc_kv4_attn(q, cache, table, torch.tensor([L], dtype=torch.int32, device="cuda"),
+                         workspace=fc.kv4_attn_workspace(1, n, 1, 1, "cuda"))
+    assert fc.fc_get_error() == "FC_OK"
+    want = v.mean(0)
+    assert np.all(np.abs(num(out) - want) <= tol * want)
+
+
 # ------------------------------------------------------------------ product
 @pytest.mark.parametrize("M", [1, 2, 7, 8, 9, 16])
 @pytest.mark.parametrize("K,N,group", [(64, 1, 32), (64, 16, 64), (128, 33, 128), (320, 100, 64), (2048, 50, 32),
