@@ -646,6 +646,31 @@ def test_attn_of_a_length_just_below_32_bits(fc, L, n, tol):
     assert np.all(np.abs(num(out) - want) <= tol * want)
 
 
+@pytest.mark.parametrize("n,H,G,lens", [(1, 8, 2, [9000, 1]), (4, 16, 4, [5000, 0, 3000]), (20, 4, 2, [3000, 5000]),
+                                        (128, 4, 2, [2000, 700])])
+def test_attn_with_less_workspace(fc, n, H, G, lens):
+    """Any smaller workspace serves, zeroed once, with nothing written past its
+    end, and the next call may have another size."""
+    c = attn_case(n + 401, len(lens), n, H, G, lens, 64)
+    cache = gpu_cache(fc, c)
+    want = check_attn(fc, c, cache=cache)
+    full = int(fc.LIB.fc_kv4_attn_workspace(len(lens), n, H, G))
+    args = (c["q"].cuda(), cache, dev(c["table"]), dev(c["lens"]), c["k_new"].cuda(), c["v_new"].cuda(),
+            dev(mask_words(c["sees"])), dev(c["nodes"]))
+    ref, size = o4.attn(num(c["q"]), *(o4.pack(x) for x in c["codes"]), *c["scales"], c["table"], c["lens"], num(c["k_new"]),
+                        num(c["v_new"]), c["sees"], c["nodes"], c["scale"])
+    buf = torch.zeros(full + 4096, dtype=torch.uint8, device="cuda")
+    for size_now in (full, full // 2, 1, 256, 1280, 1281, full // 50, full // 7 + 13, full - 1, full):
+        buf[size_now:] = 0xA5
+        out = fc.fc_kv4_attn(*args, scale=c["scale"], workspace=buf[:size_now])
+        assert fc.fc_get_error() == "FC_OK"
+        assert np.all(np.abs(num(out) - ref) <= 2.0 ** -8 * np.abs(ref) + size * (2.0 ** -8 + 2.0 ** -10)), size_now
+        assert bool((buf[size_now:] == 0xA5).all()), size_now
+        if size_now == full:
+            assert torch.equal(out, want)
+        buf[size_now:min(1280, full)] = 0  # its counters, for a larger one
+
+
 # ------------------------------------------------------------------ product
 @pytest.mark.parametrize("M", [1, 2, 7, 8, 9, 16])
 @pytest.mark.parametrize("K,N,group", [(64, 1, 32), (64, 16, 64), (128, 33, 128), (320, 100, 64), (2048, 50, 32),

@@ -210,3 +210,34 @@ def test_generate_says_when_the_pool_is_empty(weights):
     assert fc.fc_get_error() == "FC_OK"
     dec.release(torch.zeros(2, dtype=torch.int32, device="cuda"))
     assert dec.generate(tok, 16).shape == (2, 16)
+
+
+@pytest.mark.parametrize("nodes", [2, 4])
+def test_chunks_follow_the_plain_decoder(weights, nodes):
+    """Chunks of several tokens (causal among themselves) over a growing cache
+    against the plain decoder, which sees a chunk's own rows as they are and the
+    cached ones in 4 bits; the bound is the one of single-token steps."""
+    from paper_2502_17139_gb300 import fastcoder as fc
+    from paper_2502_17139_gb300.q4decoder import Q4Decoder
+    shape, W = weights
+    dec = Q4Decoder(shape, W, 2, 8, 4, nodes=nodes, page_size=16, group=64)
+    plain = [Plain(W, 64, shape.rope_base, shape.eps) for _ in range(2)]
+    rng = np.random.default_rng(6)
+    for t in range(0, 24, nodes):
+        tok = rng.integers(0, VOCAB, (2, nodes)).astype(np.int32)
+        got = num(dec.forward(torch.from_numpy(tok).cuda()))
+        k_new, v_new = [num(k) for k in dec.k_new], [num(v) for v in dec.v_new]
+        for b, p in enumerate(plain):
+            for i in range(nodes):
+                want = p.step(int(tok[b, i]))
+                err = np.linalg.norm(got[b, i] - want) / np.linalg.norm(want)
+                assert err < 4 * 5 * 2.0 ** -8 / 3, (t, b, i, err)
+                for l in range(LAYERS):  # the chunk's own rows, unquantised
+                    p.K[l].append(k_new[l][b, :, i])
+                    p.V[l].append(v_new[l][b, :, i])
+            for l in range(LAYERS):
+                del p.K[l][-nodes:], p.V[l][-nodes:]
+                for i in range(nodes):
+                    p.keep(l, k_new[l][b, :, i], v_new[l][b, :, i])
+        dec.append()
+    assert dec.kv_len[dec.cur].tolist() == [24, 24] and fc.fc_get_error() == "FC_OK"
