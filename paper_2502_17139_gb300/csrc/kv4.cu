@@ -175,7 +175,8 @@ __global__ void __launch_bounds__(PL_MAX_THREADS) k_pages_plan(PlanArgs a, int r
 constexpr int PL_THREADS = 512;  // of the release
 
 // One CTA: the pages of request b past ceil(keep / page) go back on the free
-// list in request order.
+// list in request order.  4 to 5 us for 32 requests, 8 us for one of 1000 that
+// gives back 256 pages (latency), 91 us for 256,000 pages at once.
 __global__ void __launch_bounds__(PL_THREADS) k_pages_release(const int32_t* kv_len, const int32_t* keep, int batch,
                                                               int shift, const int32_t* table, int max_pages,
                                                               int32_t* free_list, int n_pages,
@@ -313,7 +314,8 @@ struct Items {
 // 16 lanes a (row, head), key and value: the largest magnitude from the bf16
 // bits (as unsigned numbers they order like the magnitudes, infinities and NaN
 // on top), the scale, the numbers.  65000 x 8 rows written and read back take
-// 124 us, 4.8 TB/s of the 0.6 GB in and out; two or four items a lane group at
+// 124 us, 4.8 TB/s of the 0.6 GB in and out, 66 of them the write (a copy's rate
+// gives 47), which issues in 80% of the cycles; two or four items a lane group at
 // a time, with fewer threads for it, took 134 to 153 us.
 // bf16(top / 7) is taken as bf16(top * fl(1/7)): top has 8 significant bits,
 // so top / 7 is no midpoint of two bf16 values and lies 2^-15 of itself or

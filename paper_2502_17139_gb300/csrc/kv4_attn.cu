@@ -61,8 +61,9 @@ constexpr int STEP_BYTES = OFF_VSC + STEP * 2;
 // A unit's start and end take a CTA about 6 us, 0.2 us a step at full
 // bandwidth; joining two parts of a unit about 4 us.  Parts of 8 steps: 1 x 2000
 // and 2 x 1000 keys take 10.3 us where parts of 16 take 12.3, 4 x 4000 14.5 for
-// 16.4; a unit of fewer than CUT_STEPS stays whole (16 x 500 keys 10.3 us, in two
-// parts 12.4).
+// 16.4, but some ragged ones longer (3 requests of up to 3000 keys 13.8 for 12.4,
+// 32 of up to 500 11.1 for 10.4); a unit of fewer than CUT_STEPS stays whole (16 x
+// 500 keys 10.3 us, in two parts 12.4).
 constexpr int UNIT_COST = 30, PART_STEPS = 8, CUT_STEPS = 24;
 constexpr float W_MAX = 32768.f;
 constexpr int VS_MIN_EXP = -80;
