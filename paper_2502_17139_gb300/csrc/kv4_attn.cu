@@ -772,7 +772,9 @@ fc_status launch_few(const Kv4Args& a, void* ws, size_t ws_bytes, cudaStream_t s
   int grid = (int)std::min<long long>(full, units * std::max<long long>(1, longest / PART_STEPS));
   FewArgs f{a, 1, 65536u / a.G + 1, nullptr, nullptr};
   if (ws && ws_bytes > cnt) grid = (int)std::min<size_t>(grid, (ws_bytes - cnt) / one);
-  if (!ws || ws_bytes <= cnt || grid < 1 || most > 0x7FFFFFFFll) {
+  // a workspace for fewer CTAs than whole units would fill: whole units (16 x 8000 keys on two CTAs
+  // 1.09 ms, whole units 0.04)
+  if (!ws || ws_bytes <= cnt || grid < std::min<long long>(full, units) || most > 0x7FFFFFFFll) {
     f.split = 0;
     grid = (int)std::min<long long>(units, 1 << 20);
   } else {

@@ -671,6 +671,34 @@ def test_attn_with_less_workspace(fc, n, H, G, lens):
         buf[size_now:min(1280, full)] = 0  # its counters, for a larger one
 
 
+@pytest.mark.parametrize("n,H,G,L", [(1, 32, 8, 8000), (4, 32, 8, 4000), (32, 32, 8, 2000)])
+def test_attn_a_small_workspace_is_no_slower_than_none(fc, n, H, G, L):
+    """A workspace with room for the parts of two CTAs: whole units then, on
+    all of the GPU (two CTAs for everything would take tens of times as long)."""
+    c = attn_case(n + 77, 1, n, H, G, [L], 64)
+    q, kn, vn = (c[k].cuda().repeat_interleave(16, 0) for k in ("q", "k_new", "v_new"))
+    table, lens = dev(c["table"]).repeat(16, 1), dev(c["lens"]).repeat(16)
+    cache, out = gpu_cache(fc, c), torch.empty_like(q)
+    full = fc.kv4_attn_workspace(16, n, H, G, "cuda")
+    few = 1280 + 2 * 2 * 16 * 130 * 4 if n * H // G <= 16 else 1280 + 256 + 2 * 2 * min(256, n * H // G) * 520
+
+    def ms(ws):
+        call = lambda: fc.fc_kv4_attn(q, cache, table, lens, kn, vn, out=out, workspace=ws)
+        call()
+        a, b = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+        torch.cuda.synchronize()
+        a.record()
+        for _ in range(5):
+            call()
+        b.record()
+        torch.cuda.synchronize()
+        return a.elapsed_time(b) / 5
+
+    none, some = ms(None), ms(full[:few])
+    assert some < 3 * none, (none, some)
+    assert fc.fc_get_error() == "FC_OK"
+
+
 # ------------------------------------------------------------------ product
 @pytest.mark.parametrize("M", [1, 2, 7, 8, 9, 16])
 @pytest.mark.parametrize("K,N,group", [(64, 1, 32), (64, 16, 64), (128, 33, 128), (320, 100, 64), (2048, 50, 32),
