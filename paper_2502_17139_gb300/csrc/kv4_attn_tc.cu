@@ -1091,8 +1091,8 @@ fc_status kv4_attn_many(const Kv4Args& a, void* ws, size_t ws_bytes, cudaStream_
   int grid = (int)std::min<long long>(FULL_GRID, units * ((UNIT_COST + 2 * longest) / LEAST));
   auto need = [&] { return KV4_WS_COUNTERS + list_bytes(grid) + (size_t)grid * 2 * slot_bytes(f.rows_cap); };
   while (grid > 1 && ws && need() > ws_bytes) --grid;
-  // a workspace for fewer CTAs than whole units would fill: whole units (16 trees of 32 nodes over 2000 keys on two CTAs
-  // 1.91 ms, whole units 0.04)
+  // a workspace for fewer CTAs than whole units would fill: whole units (16
+  // trees of 32 nodes over 2000 keys on two CTAs 1.91 ms, whole units 0.04)
   if (!ws || !fits || need() > ws_bytes || grid < std::min<long long>(FULL_GRID, units)) {
     f.split = 0;
     grid = (int)std::min<long long>(units, FULL_GRID);

@@ -116,9 +116,10 @@ __device__ __forceinline__ void cp_async_wait() {
 // that advance, its stages unrolled, and rows and tiles past the end are read
 // from valid places instead of being tested for.
 // The operands are the numbers themselves: leaving the 128 + 8 in them and
-// taking 136 times the sum of x off again by products of its own cost 20 times and more
-// the rounding of these sums, overflowed from x = 2^115 on, and took 47 us
-// where this takes 45 (16 x 8192 x 28672; 14.3 and 13.4 for 1 x 8192 x 8192).
+// taking 136 times the sum of x off again by products of its own cost twenty
+// times and more the rounding of these sums, overflowed from x = 2^115 on, and
+// took 47 us where this takes 45 (16 x 8192 x 28672; 14.3 and 13.4 for 1 x 8192
+// x 8192).
 // A warp takes MT tiles of columns (which share the rows of x that it loads)
 // and every ks-th tile of k, three in flight by asynchronous copies, x
 // AHEAD tiles ahead in registers; with ks = 1 a sum never leaves its warp, else
