@@ -804,6 +804,134 @@ fc_status fc_w4_matvec(const void* d_x, const void* d_codes, const void* d_scale
                        void* d_y, fc_stream s);
 
 /* ------------------------------------------------------------------------
+ * Serving from a cache in eight bits that is kept to a budget (no counterpart
+ * in the paper).  A step of a serving loop: fc_kv_pages_plan (where the new
+ * tokens go) -> per layer fc_qk_norm_rope, fc_kv8_attn, fc_kv8_write -> now and
+ * then per layer fc_kv8_evict, then fc_kv_pages_release.
+ *
+ * Quantisation.  A block is 16 tokens of a page and one kv head.  Its scale is
+ * s = 2^e with the smallest e >= -120 such that max|x| <= 448 s, a number is
+ * e4m3(x / s) (nearest, ties to even) and stands for e4m3 * s.  Tokens added to
+ * a block that holds some already make its scale the larger of its own and
+ * theirs, and the numbers there are rounded to it again (exact, but for those
+ * that become subnormal).  A NaN or an infinity among a block's rows makes its
+ * scale NaN: the block stands for NaN.
+ * ------------------------------------------------------------------------ */
+typedef struct {
+  void* k_codes;     /* device, [n_pages][Hkv][page_size][D] e4m3 bytes, 16-byte aligned */
+  void* v_codes;     /* (0x7F and 0xFF, e4m3's NaN, are not written and not expected) */
+  float* k_scale;    /* device, [n_pages][Hkv][page_size / 16] powers of two, 2^-120 to 2^120, or NaN */
+  float* v_scale;
+  int32_t n_pages;   /* >= 1; n_pages * page_size < 2^31 */
+  int32_t page_size; /* tokens a page: 16, 32, 64, 128 or 256 */
+  int32_t Hkv;
+  int32_t D;         /* 128 */
+} fc_kv8_cache;
+
+/*
+ * RMSNorm of every query and key head and its rotation by position, in one
+ * pass: for a head's row x of D values
+ *   y = x / sqrt(mean(x^2) + eps) * w,   then (y_i, y_{i + D/2}) turned by
+ *   pos * base^(-2i/D)   (fc_rope's pairing; a negative position: not turned),
+ * fp32 inside, rounded once to bf16.
+ *   d_q  row (b, i, h) at element b * q_seq_stride + i * q_row_stride + h *
+ *        q_head_stride, so that parts of a projection's rows are read where
+ *        they are; d_k and d_v likewise with the kv strides.  d_v may be NULL.
+ *   d_wq, d_wk  bf16 [D], one weight vector for all heads
+ *   d_pos       [batch][n] int32; angles are good to 1e-6 below 2^24
+ *   d_q_out     bf16 [batch][n][H][D]; d_k_out and d_v_out (the values as they
+ *               are; NULL with d_v) bf16 [batch][Hkv][n][D].  Not overlapping
+ *               the inputs.
+ * D a multiple of 16 up to 512; pointers 16-byte aligned, strides multiples of
+ * 8 elements.
+ */
+fc_status fc_qk_norm_rope(const void* d_q, int64_t q_seq_stride, int64_t q_row_stride, int64_t q_head_stride,
+                          const void* d_k, const void* d_v, int64_t kv_seq_stride, int64_t kv_row_stride,
+                          int64_t kv_head_stride, const void* d_wq, const void* d_wk, const int32_t* d_pos, int batch,
+                          int n, int H, int Hkv, int D, float base, float eps, void* d_q_out, void* d_k_out,
+                          void* d_v_out, fc_stream s);
+
+/*
+ * Rounds rows of keys and values into the cache: fc_kv4_write's arguments, and
+ * one more rule, as a block's rows share a scale.  The rows of a call that go
+ * to one block of 16 lie within 32 rows of one another (left out rows may stand
+ * between; fc_kv_pages_plan's are neighbours), and what the block holds before
+ * the first of their places is kept, what it holds from there on is not
+ * expected to be.
+ * With d_weight and d_born (both or none, [n_pages][Hkv][page_size]) the rows'
+ * places get weight 0 and position d_pos[r] there, for fc_kv8_attn and
+ * fc_kv8_evict.  rows * Hkv <= 2^30 here and in fc_kv8_read.
+ */
+fc_status fc_kv8_write(const fc_kv8_cache* cache, const void* d_k, const void* d_v, int n_seq, int n_per_seq,
+                       int64_t seq_stride, int64_t row_stride, int64_t head_stride, const int32_t* d_src,
+                       const int32_t* d_slot, int rows, const int32_t* d_pos, float* d_weight, int32_t* d_born,
+                       fc_stream s);
+
+/* The values that cached rows stand for, as bf16 (exact within its range): d_k,
+ * d_v [rows][Hkv][D] from slots d_slot[r] (negative: zeros). */
+fc_status fc_kv8_read(const fc_kv8_cache* cache, const int32_t* d_slot, int rows, void* d_k, void* d_v, fc_stream s);
+
+/*
+ * fc_tree_attn over the paged 8-bit cache, for 1 to 128 new tokens a request:
+ * fc_kv4_attn's arguments and limits (D = 128, H a multiple of Hkv, H / Hkv <=
+ * 16, new tokens in bf16 by mask, rows past n_nodes and rows that see no key
+ * zeros, page ids and lengths checked on the device, a workspace of
+ * fc_kv8_attn_workspace() bytes, 256-byte aligned, ZEROED before its first use
+ * and fit for the next call of any shape after each).
+ *   d_weight  optional [n_pages][Hkv][page_size] fp32: a cached token's becomes
+ *             decay * (what is there) + the sum of its softmax weights over the
+ *             request's query rows of that kv head; decay 0 does not read what
+ *             is there.  For up to 16 rows a kv head (n_pad * H / Hkv, else
+ *             FC_ERR_UNSUPPORTED), batch * Hkv <= 65535, with a workspace made
+ *             for weight_keys = max_pages * page_size (else FC_ERR_WORKSPACE).
+ * Sums and the softmax are fp32, products of cached numbers with queries exact;
+ * probabilities are rounded to 16 bits for the second product.
+ * What a block holds past a request's end, and a scale of a block that begins
+ * there, is not looked at.  A block that stands for NaN makes the rows of its
+ * request and head NaN; new tokens and queries as in fc_kv4_attn.
+ */
+fc_status fc_kv8_attn(const void* d_q, const fc_kv8_cache* cache, const int32_t* d_table, int max_pages,
+                      const int32_t* d_kv_len, const void* d_k_new, const void* d_v_new, const uint64_t* d_mask,
+                      const int32_t* d_n_nodes, int batch, int n_pad, int H, float scale, float* d_weight, float decay,
+                      void* d_out, void* d_ws, size_t ws_bytes, fc_stream s);
+
+/* Workspace bytes for fc_kv8_attn's largest key split at this shape, and for
+ * the weights of up to weight_keys cached tokens a request (0: no weights).  0
+ * for an unsupported shape. */
+size_t fc_kv8_attn_workspace(int batch, int n_pad, int H, int Hkv, int64_t weight_keys);
+
+/*
+ * Cuts requests down to d_keep[b] cached tokens, every kv head choosing its
+ * own: the tokens of the last `recent` positions (of those that it holds,
+ * newest first), then those of the largest weight, ties to the lower index; a
+ * NaN counts as larger than every number.  The tokens that stay at an index >=
+ * keep move, in order, into the places below keep that come free; the others
+ * stay where they are.  A block that takes a token gets the scale for what it
+ * then holds.  Requests with keep[b] >= kv_len[b] keep all.  The caller then
+ * has min(keep, kv_len) tokens a request (fc_kv_pages_release with d_keep gives
+ * the length and the emptied pages).
+ *   d_weight_in, d_born_in   [n_pages][Hkv][page_size]: weights and positions
+ *                as fc_kv8_attn and fc_kv8_write leave them (the positions of a
+ *                head's tokens differ)
+ *   d_weight_out, d_born_out the same of the tokens that are then there; places
+ *                of no such token are left as they were.  Not the arrays they
+ *                come from.
+ *   d_from       [batch][Hkv][cap] int32: the index that place i's token came
+ *                from where it is not i, else -1
+ *   d_ws         workspace of fc_kv8_evict_workspace() bytes (FC_ERR_WORKSPACE)
+ * A request that loses tokens needs keep[b] <= cap: else it records
+ * FC_ERR_CAPACITY, one with a negative length or keep, a length beyond its table
+ * or a page id outside the pool FC_ERR_INVALID_ARG, and is left as it is (its
+ * weights and positions are not carried over).  recent <= 2^22, batch * Hkv <=
+ * 2^24.  Requests share no page that changes.
+ */
+fc_status fc_kv8_evict(const fc_kv8_cache* cache, const int32_t* d_table, int max_pages, const int32_t* d_kv_len,
+                       const int32_t* d_keep, int batch, int recent, const float* d_weight_in, const int32_t* d_born_in,
+                       float* d_weight_out, int32_t* d_born_out, int32_t* d_from, int cap, void* d_ws, size_t ws_bytes,
+                       fc_stream s);
+size_t fc_kv8_evict_workspace(int batch, int Hkv, int cap);
+
+/* ------------------------------------------------------------------------
  * Acceptance (Section IV-D: every correct token from the start is accepted,
  * everything after the first error rejected; Eq. 7 counts tokens per step).
  * ------------------------------------------------------------------------ */

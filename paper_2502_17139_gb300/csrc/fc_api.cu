@@ -12,6 +12,10 @@ extern "C" unsigned int fc_take_error_gemm(cudaStream_t s);
 extern "C" unsigned int fc_take_error_kv4(cudaStream_t s);
 extern "C" unsigned int fc_take_error_kv4_attn(cudaStream_t s);
 extern "C" unsigned int fc_take_error_kv4_tc(cudaStream_t s);
+extern "C" unsigned int fc_take_error_norm(cudaStream_t s);
+extern "C" unsigned int fc_take_error_kv8(cudaStream_t s);
+extern "C" unsigned int fc_take_error_kv8_attn(cudaStream_t s);
+extern "C" unsigned int fc_take_error_kv8_evict(cudaStream_t s);
 
 namespace {
 thread_local unsigned int* t_error_slot = nullptr;
@@ -47,6 +51,7 @@ extern "C" fc_status fc_get_error(fc_stream stream) {
   unsigned int e = fc_take_error_sa(s) | fc_take_error_ret(s) | fc_take_error_tree(s) | fc_take_error_step(s) |
                    fc_take_error_attn(s) | fc_take_error_cache(s) |
                    fc_take_error_dec(s) | fc_take_error_gemm(s) | fc_take_error_kv4(s) |
-                   fc_take_error_kv4_attn(s) | fc_take_error_kv4_tc(s);
+                   fc_take_error_kv4_attn(s) | fc_take_error_kv4_tc(s) | fc_take_error_norm(s) | fc_take_error_kv8(s) |
+                   fc_take_error_kv8_attn(s) | fc_take_error_kv8_evict(s);
   return fc_status_of_bits(e);
 }

@@ -1,0 +1,227 @@
+// Keys and values rounded into the pages of the 8-bit cache and read back
+// (fc_kv8_write, fc_kv8_read).
+#include <algorithm>
+
+#include "kv8.cuh"
+
+FC_DEFINE_ERROR_WORD(kv8)
+
+namespace {
+
+constexpr int HD = KV8_D;
+constexpr int WR_THREADS = 256, WR_WARPS = WR_THREADS / 32;
+constexpr int WINDOW = 32;  // rows of a block lie within so many rows of one another
+constexpr long long MAX_ITEMS = 1ll << 30;
+
+struct Kv8Rows {
+  const __nv_bfloat16 *k, *v;
+  int n_per_seq, n_src;
+  bool one_seq;
+  int64_t seq_stride, row_stride, head_stride;
+};
+
+struct Kv8Write {
+  Kv8Rows x;
+  const int32_t *src, *slot, *pos;
+  int rows, Hkv, shift;
+  long long n_slots;
+  uint8_t *kc, *vc;
+  float *ks, *vs;
+  float* weight;
+  int32_t* born;
+  unsigned int* err;
+};
+
+// A warp takes `per` neighbouring rows of one head.  A row begins a run when
+// none of the WINDOW rows before it goes to its block of 16; the run's rows are
+// those of the next WINDOW that do.  So the warp that meets a run's first row
+// knows the whole block's new tokens, and no two warps write one block.
+// Lanes 0-15 hold the keys, 16-31 the values, 8 dimensions a lane, all rows of
+// the run at once: their largest magnitude (bf16 bits as unsigned numbers order
+// like the magnitudes, infinities and NaN on top) gives the scale.
+__global__ void __launch_bounds__(WR_THREADS) k_kv8_write(Kv8Write a, int per) {
+  const int lane = threadIdx.x & 31, half = lane >> 4, l16 = lane & 15;
+  const uint32_t group = 0xFFFFu << (lane & 16);
+  const long long item = (long long)blockIdx.x * WR_WARPS + (threadIdx.x >> 5);
+  const int h = (int)(item % a.Hkv);
+  const long long r0l = item / a.Hkv * per;
+  if (r0l >= a.rows) return;
+  const int r0 = (int)r0l;
+  // the block that a row goes to and its place there, -1: none
+  auto place = [&](int r) {
+    if (r < 0 || r >= a.rows) return -1;
+    const int sl = a.slot[r];
+    if (sl < 0) return -1;
+    const int at = a.src ? a.src[r] : r;
+    return sl < a.n_slots && at >= 0 && at < a.x.n_src ? sl : -1;
+  };
+  const __nv_bfloat16* x0 = half ? a.x.v : a.x.k;
+  uint8_t* codes = half ? a.vc : a.kc;
+  float* scales = half ? a.vs : a.ks;
+  const int before = place(r0 - WINDOW + lane);
+  int here = place(r0 + lane), next = place(r0 + WINDOW + lane);
+  if (h == 0 && lane < per && r0 + lane < a.rows && a.slot[r0 + lane] >= 0 && here < 0) fc_flag(FC_ERR_WORD(a.err), FC_EBIT_INVALID);
+  for (int i = 0; i < per; ++i) {
+    const int mine = __shfl_sync(0xFFFFFFFFu, here, i);
+    if (mine < 0) continue;
+    const int block = mine >> 4;
+    // rows r0 + i - WINDOW .. - 1, then r0 + i .. + WINDOW - 1
+    const uint32_t same_b = __ballot_sync(0xFFFFFFFFu, before >= 0 && before >> 4 == block);
+    const uint32_t same_h = __ballot_sync(0xFFFFFFFFu, here >= 0 && here >> 4 == block);
+    const uint32_t same_n = __ballot_sync(0xFFFFFFFFu, next >= 0 && next >> 4 == block);
+    if ((same_b >> i) | (same_h & ((1u << i) - 1u))) continue;  // an earlier row's run
+    uint32_t members = (same_h >> i) | (i ? same_n << (32 - i) : 0u);
+    const int page = mine >> a.shift, in_page = (mine & ((1 << a.shift) - 1)) >> 4;
+    const size_t row0 = ((size_t)page * a.Hkv + h) << a.shift;
+    uint4 v[KV8_BLOCK];
+    int off[KV8_BLOCK];  // place in the block, -1: no row
+    uint32_t top = 0;
+    int first = KV8_BLOCK;
+#pragma unroll
+    for (int j = 0; j < KV8_BLOCK; ++j) {
+      off[j] = -1;
+      v[j] = make_uint4(0, 0, 0, 0);
+      if (members) {  // the same for the whole warp
+        const int m = __ffs(members) - 1, rel = i + m;
+        members &= members - 1;
+        const int sh = __shfl_sync(0xFFFFFFFFu, here, rel & 31), sn = __shfl_sync(0xFFFFFFFFu, next, rel & 31);
+        off[j] = (rel < 32 ? sh : sn) & 15;
+        const int r = r0 + rel, at = a.src ? a.src[r] : r;
+        const int q = a.x.one_seq ? 0 : at / a.x.n_per_seq, n = at - q * a.x.n_per_seq;
+        v[j] = reinterpret_cast<const uint4*>(x0 + q * a.x.seq_stride + n * a.x.row_stride + h * a.x.head_stride)[l16];
+        if (a.weight && lane == 0) {
+          a.weight[row0 + in_page * KV8_BLOCK + off[j]] = 0.f;
+          a.born[row0 + in_page * KV8_BLOCK + off[j]] = a.pos[r];
+        }
+        first = min(first, off[j]);
+      }
+    }
+#pragma unroll
+    for (int j = 0; j < KV8_BLOCK; ++j)
+      top = __vmaxu2(top, __vmaxu2(__vmaxu2(v[j].x & 0x7FFF7FFFu, v[j].y & 0x7FFF7FFFu),
+                                   __vmaxu2(v[j].z & 0x7FFF7FFFu, v[j].w & 0x7FFF7FFFu)));
+    top = max(top & 0xFFFFu, top >> 16);
+#pragma unroll
+    for (int o = 1; o < 16; o <<= 1) top = max(top, __shfl_xor_sync(group, top, o));
+    float* scale = scales + (((size_t)page * a.Hkv + h) << (a.shift - 4)) + in_page;
+    uint2* rows = reinterpret_cast<uint2*>(codes + (row0 + in_page * KV8_BLOCK) * HD);
+    const float old = first > 0 ? *scale : 0.f;
+    bool nan = top >= 0x7F80u || (first > 0 && kv8_nan(old));
+    int e = nan ? 0 : max(kv8_exp_for(__uint_as_float(top << 16)), KV8_MIN_EXP);
+    if (first > 0 && !nan) {
+      const int e_old = kv8_exp(old);
+      if (e > e_old) {  // what the block holds, in the new scale
+        for (int j = 0; j < first; ++j) {
+          uint2 w = rows[j * 16 + l16];
+          w.x = kv8_rescale4(w.x, e_old - e);
+          w.y = kv8_rescale4(w.y, e_old - e);
+          rows[j * 16 + l16] = w;
+        }
+      } else {
+        e = e_old;
+      }
+    }
+    __syncwarp(group);  // the scale is read by all before it changes
+    if (l16 == 0) *scale = nan ? __uint_as_float(0x7FC00000u) : kv8_pow2(e);
+    const float by = nan ? 0.f : kv8_pow2(-e);
+#pragma unroll
+    for (int j = 0; j < KV8_BLOCK; ++j) {
+      if (off[j] < 0) continue;
+      uint32_t b[4];
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        const uint32_t w = (&v[j].x)[u];
+        // a block with a NaN or an infinity stands for NaN, whatever its numbers
+        b[u] = nan ? 0u : floats_e4m3x2(__uint_as_float(w << 16) * by, __uint_as_float(w & 0xFFFF0000u) * by);
+      }
+      rows[off[j] * 16 + l16] = make_uint2(b[0] | (b[1] << 16), b[2] | (b[3] << 16));
+    }
+    __syncwarp();
+  }
+}
+
+__global__ void __launch_bounds__(WR_THREADS) k_kv8_read(const int32_t* __restrict__ slot, int rows, int Hkv, int shift, long long n_slots,
+                                                         const uint8_t* __restrict__ kc, const uint8_t* __restrict__ vc,
+                                                         const float* __restrict__ ks, const float* __restrict__ vs, uint4* __restrict__ k,
+                                                         uint4* __restrict__ v, unsigned int* err) {
+  const int lane = threadIdx.x & 15;  // 16 lanes a (row, head)
+  const long long items = (long long)rows * Hkv, stride = (long long)gridDim.x * (WR_THREADS / 16);
+  for (long long it = (long long)blockIdx.x * (WR_THREADS / 16) + threadIdx.x / 16; it < items; it += stride) {
+    const int r = (int)(it / Hkv), h = (int)(it - (long long)r * Hkv);
+    const int sl = slot[r];
+    if (sl >= n_slots && lane == 0 && h == 0) fc_flag(FC_ERR_WORD(err), FC_EBIT_INVALID);
+    uint2 a = make_uint2(0, 0), b = a;
+    float sk = 0.f, sv = 0.f;
+    if (sl >= 0 && sl < n_slots) {
+      const size_t row = ((((size_t)(sl >> shift)) * Hkv + h) << shift) + (sl & ((1 << shift) - 1));
+      a = reinterpret_cast<const uint2*>(kc)[row * 16 + lane];
+      b = reinterpret_cast<const uint2*>(vc)[row * 16 + lane];
+      sk = ks[row >> 4];
+      sv = vs[row >> 4];
+    }
+    auto values = [](const uint2& w, float s) {  // four significant bits times a power of two: exact in bf16's range
+      const float2 p = e4m3x2_floats(w.x & 0xFFFFu), q = e4m3x2_floats(w.x >> 16), t = e4m3x2_floats(w.y & 0xFFFFu), u = e4m3x2_floats(w.y >> 16);
+      return make_uint4(pack_bf16x2(p.x * s, p.y * s), pack_bf16x2(q.x * s, q.y * s), pack_bf16x2(t.x * s, t.y * s), pack_bf16x2(u.x * s, u.y * s));
+    };
+    const size_t to = (size_t)it * 16 + lane;
+    __stcs(k + to, values(a, sk));
+    __stcs(v + to, values(b, sv));
+  }
+}
+
+}  // namespace
+
+fc_status fc_kv8_check(const fc_kv8_cache* c) {
+  if (!c || c->n_pages < 1 || c->Hkv < 1) return FC_ERR_INVALID_ARG;
+  if (c->D != HD || kv8_page_shift(c->page_size) < 0 || (long long)c->n_pages * c->page_size > 0x7FFFFFFFll)
+    return FC_ERR_UNSUPPORTED;
+  if (!c->k_codes || !c->v_codes || !c->k_scale || !c->v_scale || !kv8_aligned(c->k_codes, 16) || !kv8_aligned(c->v_codes, 16) ||
+      !kv8_aligned(c->k_scale, 4) || !kv8_aligned(c->v_scale, 4))
+    return FC_ERR_INVALID_ARG;
+  return FC_OK;
+}
+
+extern "C" fc_status fc_kv8_write(const fc_kv8_cache* cache, const void* d_k, const void* d_v, int n_seq, int n_per_seq,
+                                  int64_t seq_stride, int64_t row_stride, int64_t head_stride, const int32_t* d_src,
+                                  const int32_t* d_slot, int rows, const int32_t* d_pos, float* d_weight, int32_t* d_born,
+                                  fc_stream stream) {
+  FC_NVTX_RANGE();
+  if (const fc_status st = fc_kv8_check(cache)) return st;
+  if (rows < 0 || n_seq < 0 || n_per_seq < 1 || seq_stride < 0 || row_stride < 0 || head_stride < 0 ||
+      (long long)n_seq * n_per_seq > 0x7FFFFFFFll || !d_weight != !d_born || (d_weight && !d_pos && rows))
+    return FC_ERR_INVALID_ARG;
+  if (rows == 0) return FC_OK;
+  if (!d_k || !d_v || !d_slot || !kv8_aligned(d_k, 16) || !kv8_aligned(d_v, 16) || seq_stride % 8 || row_stride % 8 ||
+      head_stride % 8 || (!d_src && rows > n_seq * n_per_seq))
+    return FC_ERR_INVALID_ARG;
+  if ((long long)rows * cache->Hkv > MAX_ITEMS) return FC_ERR_UNSUPPORTED;
+  Kv8Write a{{static_cast<const __nv_bfloat16*>(d_k), static_cast<const __nv_bfloat16*>(d_v), n_per_seq, n_seq * n_per_seq,
+              n_seq == 1, seq_stride, row_stride, head_stride},
+             d_src, d_slot, d_pos, rows, cache->Hkv, kv8_page_shift(cache->page_size),
+             (long long)cache->n_pages * cache->page_size, static_cast<uint8_t*>(cache->k_codes),
+             static_cast<uint8_t*>(cache->v_codes), static_cast<float*>(cache->k_scale), static_cast<float*>(cache->v_scale),
+             d_weight, d_born, fc_error_slot()};
+  // one row a warp while that does not fill the GPU, else a block's worth
+  const int per = (long long)rows * cache->Hkv <= 152 * 64 ? 1 : 16;
+  const long long warps = ((long long)rows + per - 1) / per * cache->Hkv;
+  k_kv8_write<<<(unsigned)((warps + WR_WARPS - 1) / WR_WARPS), WR_THREADS, 0, static_cast<cudaStream_t>(stream)>>>(a, per);
+  return FC_CHECK_LAUNCH();
+}
+
+extern "C" fc_status fc_kv8_read(const fc_kv8_cache* cache, const int32_t* d_slot, int rows, void* d_k, void* d_v,
+                                 fc_stream stream) {
+  FC_NVTX_RANGE();
+  if (const fc_status st = fc_kv8_check(cache)) return st;
+  if (rows < 0) return FC_ERR_INVALID_ARG;
+  if (rows == 0) return FC_OK;
+  if (!d_slot || !d_k || !d_v || !kv8_aligned(d_k, 16) || !kv8_aligned(d_v, 16)) return FC_ERR_INVALID_ARG;
+  const long long items = (long long)rows * cache->Hkv;
+  if (items > MAX_ITEMS) return FC_ERR_UNSUPPORTED;
+  const unsigned grid = (unsigned)std::min<long long>((items + WR_THREADS / 16 - 1) / (WR_THREADS / 16), 152 * 64);
+  k_kv8_read<<<grid, WR_THREADS, 0, static_cast<cudaStream_t>(stream)>>>(
+      d_slot, rows, cache->Hkv, kv8_page_shift(cache->page_size), (long long)cache->n_pages * cache->page_size,
+      static_cast<const uint8_t*>(cache->k_codes), static_cast<const uint8_t*>(cache->v_codes),
+      static_cast<const float*>(cache->k_scale), static_cast<const float*>(cache->v_scale), static_cast<uint4*>(d_k),
+      static_cast<uint4*>(d_v), fc_error_slot());
+  return FC_CHECK_LAUNCH();
+}

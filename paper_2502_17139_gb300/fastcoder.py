@@ -78,6 +78,11 @@ class fc_kv4_cache(C.Structure):
                 ("n_pages", C.c_int32), ("page_size", C.c_int32), ("Hkv", C.c_int32), ("D", C.c_int32)]
 
 
+class fc_kv8_cache(C.Structure):
+    _fields_ = [("k_codes", C.c_void_p), ("v_codes", C.c_void_p), ("k_scale", C.c_void_p), ("v_scale", C.c_void_p),
+                ("n_pages", C.c_int32), ("page_size", C.c_int32), ("Hkv", C.c_int32), ("D", C.c_int32)]
+
+
 EXPORTS = ["fc_status_string", "fc_version", "fc_get_error", "fc_datastore_build_workspace", "fc_datastore_build",
            "fc_datastore_build_noalloc", "fc_datastore_keys", "fc_datastore_save", "fc_datastore_file_info", "fc_datastore_load",
            "fc_retrieve", "fc_retrieve_all", "fc_retrieve_rev", "fc_reverse_tokens", "fc_rcache_bytes", "fc_rcache_init", "fc_rcache_lookup", "fc_rcache_insert", "fc_retrieve_cached",
@@ -87,7 +92,8 @@ EXPORTS = ["fc_status_string", "fc_version", "fc_get_error", "fc_datastore_build
            "fc_pipeline_create", "fc_pipeline_step", "fc_pipeline_step_part", "fc_pipeline_join_part", "fc_pipeline_stream", "fc_pipeline_error", "fc_pipeline_join",
            "fc_pipeline_capture_part", "fc_pipeline_graph_launch", "fc_pipeline_graph_kernels", "fc_pipeline_graph_destroy",
            "fc_pipeline_destroy", "fc_kv_pages_plan", "fc_kv_pages_release", "fc_kv4_write", "fc_kv4_read", "fc_kv4_attn",
-           "fc_kv4_attn_workspace", "fc_w4_codes_bytes", "fc_w4_pack", "fc_w4_matvec"]
+           "fc_kv4_attn_workspace", "fc_w4_codes_bytes", "fc_w4_pack", "fc_w4_matvec", "fc_qk_norm_rope",
+           "fc_kv8_write", "fc_kv8_read", "fc_kv8_attn", "fc_kv8_attn_workspace", "fc_kv8_evict", "fc_kv8_evict_workspace"]
 
 
 def _load():
@@ -96,7 +102,7 @@ def _load():
     if not os.path.exists(path):
         raise ImportError(f"libfastcoder.so is not built ({path}); run __graft_entry__.build()")
     lib = C.CDLL(path)
-    vp, i32, u32, u64, sz = C.c_void_p, C.c_int, C.c_uint32, C.c_uint64, C.c_size_t
+    vp, i32, i64, u32, u64, sz = C.c_void_p, C.c_int, C.c_int64, C.c_uint32, C.c_uint64, C.c_size_t
     sig = {
         "fc_status_string": (C.c_char_p, [C.c_int]),
         "fc_version": (C.c_char_p, []),
@@ -181,6 +187,14 @@ def _load():
         "fc_w4_codes_bytes": (sz, [i32, i32]),
         "fc_w4_pack": (C.c_int, [vp, i32, i32, i32, vp, vp, vp]),
         "fc_w4_matvec": (C.c_int, [vp, vp, vp, i32, i32, i32, i32, vp, vp]),
+        "fc_qk_norm_rope": (C.c_int, [vp, i64, i64, i64, vp, vp, i64, i64, i64, vp, vp, vp, i32, i32, i32, i32, i32, C.c_float,
+                                      C.c_float, vp, vp, vp, vp]),
+        "fc_kv8_write": (C.c_int, [vp, vp, vp, i32, i32, i64, i64, i64, vp, vp, i32, vp, vp, vp, vp]),
+        "fc_kv8_read": (C.c_int, [vp, vp, i32, vp, vp, vp]),
+        "fc_kv8_attn": (C.c_int, [vp, vp, vp, i32, vp, vp, vp, vp, vp, i32, i32, i32, C.c_float, vp, C.c_float, vp, vp, sz, vp]),
+        "fc_kv8_attn_workspace": (sz, [i32, i32, i32, i32, i64]),
+        "fc_kv8_evict": (C.c_int, [vp, vp, i32, vp, vp, i32, i32, vp, vp, vp, vp, vp, i32, vp, sz, vp]),
+        "fc_kv8_evict_workspace": (sz, [i32, i32, i32]),
     }
     for name, (res, args) in sig.items():
         f = getattr(lib, name)
@@ -1054,6 +1068,252 @@ def fc_w4_matvec(x, w: W4Weight, out=None):
         _need(out, torch.bfloat16, "out", (M, w.N))
     _check("fc_w4_matvec", LIB.fc_w4_matvec(x.data_ptr(), w.codes.data_ptr(), w.scale.data_ptr(), M, K, w.N, w.group,
                                             out.data_ptr(), _stream()))
+    return out
+
+
+# ------------------------------- serving from a cache in eight bits, kept to a budget
+def _rows_strides(x):
+    """(b, i, h) strides of x [B, n, heads, D], 0 for a dimension of one."""
+    return [0 if m == 1 else s for m, s in zip(x.shape[:3], x.stride())]
+
+
+def fc_qk_norm_rope(q, k, v, wq, wk, pos, base=10000.0, eps=1e-6, out=None):
+    """RMSNorm of every head of q [B, n, H, D] and k [B, n, Hkv, D] (weights wq,
+    wk [D]) and its rotation by pos [B, n] int32; v [B, n, Hkv, D] or None is
+    laid beside them.  bf16, any strides with a dense last dimension (k and v
+    the same ones): parts of a projection's rows.  Returns q [B, n, H, D], k and
+    v [B, Hkv, n, D] (``out``: these three)."""
+    for t, name in ((q, "q"), (k, "k")) + (((v, "v"),) if v is not None else ()):
+        if not isinstance(t, torch.Tensor) or t.dtype is not torch.bfloat16:
+            raise TypeError(f"{name} must be a torch.bfloat16 tensor")
+        if not t.is_cuda:
+            raise ValueError(f"{name} must be on a CUDA device")
+        if t.dim() != 4 or (t.stride(3) != 1 and t.shape[3] != 1):
+            raise ValueError(f"{name} must be [B, n, heads, D] with a dense last dimension")
+    B, n, H, D = q.shape
+    Hkv = k.shape[2]
+    if k.shape != (B, n, Hkv, D) or (v is not None and v.shape != k.shape):
+        raise ValueError("q, k and v must agree in batch, rows and head dimension")
+    qs, ks = _rows_strides(q), _rows_strides(k)
+    if v is not None and _rows_strides(v) != ks:
+        raise ValueError("k and v must have the same strides")
+    _need(wq, torch.bfloat16, "wq", (D,))
+    _need(wk, torch.bfloat16, "wk", (D,))
+    _need(pos, torch.int32, "pos", (B, n))
+    if out is None:
+        new = lambda *s: torch.empty(s, dtype=torch.bfloat16, device=q.device)
+        out = (new(B, n, H, D), new(B, Hkv, n, D), None if v is None else new(B, Hkv, n, D))
+    qo, ko, vo = out
+    _need(qo, torch.bfloat16, "q of out", (B, n, H, D))
+    _need(ko, torch.bfloat16, "k of out", (B, Hkv, n, D))
+    if (v is None) != (vo is None):
+        raise ValueError("v and v of out go together")
+    if vo is not None:
+        _need(vo, torch.bfloat16, "v of out", (B, Hkv, n, D))
+    _check("fc_qk_norm_rope", LIB.fc_qk_norm_rope(
+        q.data_ptr(), *qs, k.data_ptr(), _ptr(v), *ks, wq.data_ptr(), wk.data_ptr(), pos.data_ptr(), B, n, H, Hkv, D, base, eps,
+        qo.data_ptr(), ko.data_ptr(), _ptr(vo), _stream()))
+    return out
+
+
+class Kv8Cache:
+    """One layer's paged cache in 8 bits: k_codes, v_codes uint8 (e4m3 bytes)
+    [n_pages, Hkv, page_size, D] and k_scale, v_scale fp32 [n_pages, Hkv,
+    page_size / 16] (device tensors owned here)."""
+
+    def __init__(self, k_codes, v_codes, k_scale, v_scale):
+        _need(k_codes, torch.uint8, "k_codes")
+        if k_codes.dim() != 4 or k_codes.shape[2] % 16:
+            raise ValueError("k_codes must be [n_pages, Hkv, page_size, D], pages of a multiple of 16 tokens")
+        _need(v_codes, torch.uint8, "v_codes", k_codes.shape)
+        self.n_pages, self.Hkv, self.page_size, self.D = k_codes.shape
+        blocks = (self.n_pages, self.Hkv, self.page_size // 16)
+        _need(k_scale, torch.float32, "k_scale", blocks)
+        _need(v_scale, torch.float32, "v_scale", blocks)
+        self.k_codes, self.v_codes, self.k_scale, self.v_scale = k_codes, v_codes, k_scale, v_scale
+        self.view = fc_kv8_cache(k_codes.data_ptr(), v_codes.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr(),
+                                 self.n_pages, self.page_size, self.Hkv, self.D)
+        self.ref = C.c_void_p(C.addressof(self.view))
+
+    @classmethod
+    def empty(cls, n_pages, Hkv, page_size=64, D=128, device="cuda"):
+        return cls(*(torch.zeros((n_pages, Hkv, page_size, D), dtype=torch.uint8, device=device) for _ in range(2)),
+                   *(torch.ones((n_pages, Hkv, page_size // 16), dtype=torch.float32, device=device) for _ in range(2)))
+
+
+class Kv8Track:
+    """What eviction goes by, for every place of a layer's cache: weight fp32
+    (fc_kv8_attn) and born int32, its token's position (fc_kv8_write), both
+    [n_pages, Hkv, page_size]."""
+
+    def __init__(self, weight, born):
+        _need(weight, torch.float32, "weight")
+        _need(born, torch.int32, "born", weight.shape)
+        if weight.dim() != 3:
+            raise ValueError("weight and born must be [n_pages, Hkv, page_size]")
+        self.weight, self.born = weight, born
+
+    @classmethod
+    def empty(cls, cache: Kv8Cache):
+        shape, dev = cache.k_codes.shape[:3], cache.k_codes.device
+        return cls(torch.zeros(shape, dtype=torch.float32, device=dev), torch.zeros(shape, dtype=torch.int32, device=dev))
+
+
+def _need_track(track, cache, name):
+    if not isinstance(track, Kv8Track):
+        raise TypeError(f"{name} must be a Kv8Track")
+    if track.weight.shape != cache.k_codes.shape[:3]:
+        raise ValueError(f"{name} must be of the cache's shape")
+
+
+def fc_kv8_write(cache: Kv8Cache, k, v, slot, src=None, track: Kv8Track | None = None, pos=None):
+    """Rounds rows into the cache: k, v bf16 [rows, Hkv, D] or [B, n, Hkv, D] of
+    equal strides (any, the last dimension dense), slot [rows] int32 (negative:
+    left out); src [rows] int32: the row of k, v (of B * n) that goes to a slot.
+    The rows of one block of 16 places lie within 32 rows of one another.  With
+    ``track`` their places get weight 0 and position pos [rows] int32."""
+    if k.dtype is not torch.bfloat16 or v.dtype is not torch.bfloat16:
+        raise TypeError("k and v must be torch.bfloat16")
+    st, shape = k.stride(), k.shape
+    if not (k.is_cuda and v.is_cuda):
+        raise ValueError("k and v must be on a CUDA device")
+    if v.shape != shape:
+        raise ValueError("k and v must have the same shape")
+    if v.stride() != st or 1 in shape:  # a dimension of 1 has no stride that matters
+        st, sv = ([0 if n == 1 else s for n, s in zip(shape, t.stride())] for t in (k, v))
+        if sv != st:
+            raise ValueError("k and v must have the same strides")
+    if len(shape) not in (3, 4) or shape[-2] != cache.Hkv or shape[-1] != cache.D or st[-1] != 1:
+        raise ValueError("k and v must be [rows, Hkv, D] or [B, n, Hkv, D] with a dense last dimension")
+    _need(slot, torch.int32, "slot")
+    rows = slot.numel()
+    if src is not None:
+        _need(src, torch.int32, "src", (rows,))
+    pp = wp = bp = None
+    if track is not None:
+        _need_track(track, cache, "track")
+        if pos is None:
+            raise ValueError("track goes with pos")
+        _need(pos, torch.int32, "pos", (rows,))
+        pp, wp, bp = pos.data_ptr(), track.weight.data_ptr(), track.born.data_ptr()
+    B, n = (1, shape[0]) if len(shape) == 3 else shape[:2]
+    if src is None and rows > B * n:
+        raise ValueError("more slots than rows")
+    _check("fc_kv8_write", LIB.fc_kv8_write(cache.ref, k.data_ptr(), v.data_ptr(), B, max(n, 1),
+                                            0 if len(shape) == 3 else st[0], st[-3], st[-2],
+                                            None if src is None else src.data_ptr(), slot.data_ptr(), rows, pp, wp, bp, _stream()))
+
+
+def fc_kv8_read(cache: Kv8Cache, slot, out=None):
+    """The values that the rows at ``slot`` [rows] stand for, as bf16 (k, v),
+    each [rows, Hkv, D]; negative slots give zeros."""
+    _need(slot, torch.int32, "slot")
+    shape = (slot.numel(), cache.Hkv, cache.D)
+    if out is None:
+        out = tuple(torch.empty(shape, dtype=torch.bfloat16, device=slot.device) for _ in range(2))
+    k, v = out
+    _need(k, torch.bfloat16, "k", shape)
+    _need(v, torch.bfloat16, "v", shape)
+    _check("fc_kv8_read", LIB.fc_kv8_read(cache.ref, slot.data_ptr(), shape[0], k.data_ptr(), v.data_ptr(), _stream()))
+    return out
+
+
+def kv8_attn_workspace(B, n_pad, H, Hkv, device, weight_keys=0):
+    """A zeroed workspace for fc_kv8_attn at this shape (and at any that needs no
+    more), and for the weights of up to weight_keys cached tokens a request
+    (max_pages * page_size; 0: no weights).  Calls that may overlap on different
+    streams need one each."""
+    n = int(LIB.fc_kv8_attn_workspace(B, n_pad, H, Hkv, weight_keys))
+    return torch.zeros(max(n, 256), dtype=torch.uint8, device=device)
+
+
+def fc_kv8_attn(q, cache: Kv8Cache, table, kv_len, k_new=None, v_new=None, mask=None, n_nodes=None, scale=None, out=None,
+                workspace=None, weight=None, decay=1.0):
+    """Attention of q [B, n_pad, H, D] over the cache's tokens [0, kv_len[b]) in
+    pages table [B, max_pages] and the new tokens k_new, v_new [B, Hkv, n_pad,
+    D] (bf16; None: none) by mask [B, n_pad, ceil(n_pad / 64)] (int64 bits;
+    None: causal among the new).  n_nodes [B] (None: all n_pad).  workspace:
+    kv8_attn_workspace(...) or None (no key split).  weight fp32 [n_pages, Hkv,
+    page_size]: becomes decay * weight + the softmax weights that the request's
+    cached tokens received (up to 16 rows a kv head; needs the workspace)."""
+    _need(q, torch.bfloat16, "q")
+    B, Np, H, D = q.shape
+    Hkv = cache.Hkv
+    if D != cache.D:
+        raise ValueError("q and the cache differ in head dimension")
+    _need(table, torch.int32, "table")
+    if table.dim() != 2 or table.shape[0] != B:
+        raise ValueError("table must be [B, max_pages]")
+    _need(kv_len, torch.int32, "kv_len", (B,))
+    kp = vp = mp = np_ = wp = None
+    if k_new is not None:
+        _need(k_new, torch.bfloat16, "k_new", (B, Hkv, Np, D))
+        _need(v_new, torch.bfloat16, "v_new", (B, Hkv, Np, D))
+        kp, vp = k_new.data_ptr(), v_new.data_ptr()
+    elif v_new is not None:
+        raise ValueError("k_new and v_new go together")
+    if mask is not None:
+        _need(mask, torch.int64, "mask", (B, Np, (Np + 63) // 64))
+        mp = mask.data_ptr()
+    if n_nodes is not None:
+        _need(n_nodes, torch.int32, "n_nodes", (B,))
+        np_ = n_nodes.data_ptr()
+    if out is None:
+        out = torch.empty_like(q)
+    else:
+        _need(out, torch.bfloat16, "out", q.shape)
+    if weight is not None:
+        _need(weight, torch.float32, "weight", cache.k_codes.shape[:3])
+        wp = weight.data_ptr()
+    ws, ws_bytes = None, 0
+    if workspace is not None:
+        if not (workspace.is_cuda and workspace.is_contiguous()):
+            raise ValueError("workspace must be a dense tensor on a CUDA device")
+        ws, ws_bytes = workspace.data_ptr(), workspace.numel() * workspace.element_size()
+    _check("fc_kv8_attn", LIB.fc_kv8_attn(q.data_ptr(), cache.ref, table.data_ptr(), table.shape[1], kv_len.data_ptr(), kp,
+                                          vp, mp, np_, B, Np, H, D ** -0.5 if scale is None else float(scale), wp,
+                                          float(decay), out.data_ptr(), ws, ws_bytes, _stream()))
+    return out
+
+
+def kv8_evict_workspace(B, Hkv, cap, device):
+    """A workspace for fc_kv8_evict at this shape (no initial contents needed)."""
+    return torch.empty(max(int(LIB.fc_kv8_evict_workspace(B, Hkv, cap)), 16), dtype=torch.uint8, device=device)
+
+
+def fc_kv8_evict(cache: Kv8Cache, table, kv_len, keep, recent, track: Kv8Track, track_out: Kv8Track, out=None, cap=None,
+                 workspace=None):
+    """Cuts request b down to keep[b] of its kv_len[b] cached tokens, every kv
+    head choosing its own: those of the last ``recent`` positions, then those of
+    the largest weight (track.weight).  Tokens that stay move into the free
+    places below keep[b]; track_out gets weights and positions as they then are.
+    Returns from [B, Hkv, cap] int32: the index that a place's token came from
+    (-1: its own); give ``out`` or ``cap`` (>= every keep[b] below its kv_len[b]).
+    fc_kv_pages_release(pages, kv_len, keep, ...) then gives the lengths and the
+    emptied pages."""
+    _need(table, torch.int32, "table")
+    if table.dim() != 2:
+        raise ValueError("table must be [B, max_pages]")
+    B, H = table.shape[0], cache.Hkv
+    _need(kv_len, torch.int32, "kv_len", (B,))
+    _need(keep, torch.int32, "keep", (B,))
+    _need_track(track, cache, "track")
+    _need_track(track_out, cache, "track_out")
+    if out is None:
+        if cap is None:
+            raise ValueError("give out or cap")
+        out = torch.empty((B, H, cap), dtype=torch.int32, device=table.device)
+    _need(out, torch.int32, "out")
+    if out.dim() != 3 or out.shape[:2] != (B, H) or (cap is not None and cap != out.shape[2]):
+        raise ValueError("out must be [B, Hkv, cap]")
+    if workspace is None:
+        workspace = kv8_evict_workspace(B, H, out.shape[2], table.device)
+    elif not (workspace.is_cuda and workspace.is_contiguous()):
+        raise ValueError("workspace must be a dense tensor on a CUDA device")
+    _check("fc_kv8_evict", LIB.fc_kv8_evict(
+        cache.ref, table.data_ptr(), table.shape[1], kv_len.data_ptr(), keep.data_ptr(), B, int(recent), track.weight.data_ptr(),
+        track.born.data_ptr(), track_out.weight.data_ptr(), track_out.born.data_ptr(), out.data_ptr(), out.shape[2],
+        workspace.data_ptr(), workspace.numel() * workspace.element_size(), _stream()))
     return out
 
 

@@ -1,0 +1,506 @@
+"""Serving from the 8-bit cache on the GPU against the 64-bit oracle (oracle/kv8.py).
+
+Codes, scales, positions and indexes are equal.  bf16 has 8 significant bits,
+so a rounding to it moves a value by at most 2^-8 of itself.  Floating
+tolerances, per element:
+* attention: the output's rounding, 2^-8 |out|; each probability's rounding to
+  16 bits, 2^-8 of A = the mean of |v| under the same probabilities; and a
+  score's error e (oracle.attend), which changes a probability and the row sum
+  by e of themselves: 2 e A.  fp32 sums of up to 2^17 probabilities in pieces:
+  2^-16 A.
+* weights: the scores' error on probability and row sum, 2 e, and fp32's
+  arithmetic (exp2's 2^-22, sums), 2^-18, of each.
+* norm and rotation: y's rounding, 2^-8 |y|; sine and cosine are good to 2^-20
+  and the angle to 1e-6 (absolute), fp32's arithmetic to 2^-20: 2^-18 of |a| + |b|.
+"""
+import numpy as np
+import pytest
+import torch
+
+from oracle import kv8 as o8
+
+pytestmark = pytest.mark.gpu
+D = 128
+
+
+@pytest.fixture(scope="module")
+def fc():
+    import paper_2502_17139_gb300.fastcoder as m
+    assert m.fc_get_error() == "FC_OK"
+    return m
+
+
+def dev(a):
+    return torch.from_numpy(np.ascontiguousarray(a)).cuda()
+
+
+def bf(rng, *shape, scale=1.0):
+    return torch.from_numpy((rng.standard_normal(shape) * scale).astype(np.float32)).bfloat16()
+
+
+def num(t):
+    return t.double().cpu().numpy()
+
+
+def random_cache(rng, n_pages, H, page, stale=False):
+    codes = [o8.encode(np.clip(rng.standard_normal((n_pages, H, page, D)) * 100, -448, 448)) for _ in range(2)]
+    scales = [(2.0 ** rng.integers(-8, -5, (n_pages, H, page // 16))).astype(np.float32) for _ in range(2)]
+    return codes + scales
+
+
+def on_gpu(fc, cache):
+    return fc.Kv8Cache(*(dev(c) for c in cache))
+
+
+def same_cache(got, want):
+    for name, g, w in zip(("k_codes", "v_codes", "k_scale", "v_scale"), (got.k_codes, got.v_codes, got.k_scale, got.v_scale), want):
+        assert np.array_equal(g.cpu().numpy(), w, equal_nan=w.dtype.kind == "f"), name
+
+
+# ------------------------------------------------------------------ norm and rotation
+@pytest.mark.parametrize("B,n,H,Hkv,dim", [(1, 1, 1, 1, 128), (32, 1, 32, 8, 128), (3, 7, 5, 2, 64), (2, 130, 16, 16, 128),
+                                           (1, 3, 6, 3, 16), (2, 5, 4, 1, 80), (1, 9, 8, 2, 256), (1, 2, 2, 2, 512), (700, 3, 40, 8, 128)])
+def test_norm_rope(fc, B, n, H, Hkv, dim):
+    rng = np.random.default_rng(B + n + dim)
+    q, kv = bf(rng, B, n, H + 3, dim, scale=3.0), bf(rng, B, n, 2, Hkv, dim)
+    q[0, 0, 0] = 0
+    wq, wk = (bf(rng, dim) for _ in range(2))
+    pos = rng.integers(0, 1 << 20, (B, n)).astype(np.int32)
+    pos[-1, -1] = -1  # not turned
+    pos[0, 0] = (1 << 24) - 1
+    qg, kvg = q.cuda()[:, :, 1:1 + H], kv.cuda()
+    out = fc.fc_qk_norm_rope(qg, kvg[:, :, 0], kvg[:, :, 1], wq.cuda(), wk.cuda(), dev(pos), 1e6, 1e-5)
+    assert fc.fc_get_error() == "FC_OK"
+    for x, w, got, turn in ((q[:, :, 1:1 + H], wq, out[0], False), (kv[:, :, 0], wk, out[1], True)):
+        ref, mag = o8.norm_rope(num(x), num(w), pos.astype(np.float64), 1e6, 1e-5)
+        if turn:
+            ref, mag = ref.transpose(0, 2, 1, 3), mag.transpose(0, 2, 1, 3)
+        assert np.all(np.abs(num(got) - ref) <= 2.0 ** -8 * np.abs(ref) + 2.0 ** -18 * mag)
+    assert torch.equal(out[2], kvg[:, :, 1].transpose(1, 2))
+    two = fc.fc_qk_norm_rope(qg, kvg[:, :, 0], None, wq.cuda(), wk.cuda(), dev(pos), 1e6, 1e-5)
+    assert two[2] is None and torch.equal(two[0], out[0]) and torch.equal(two[1], out[1])
+
+
+def test_norm_rope_rows_that_are_not_finite_stay_alone(fc):
+    rng = np.random.default_rng(3)
+    q, k = bf(rng, 2, 4, 8, D).cuda(), bf(rng, 2, 4, 2, D).cuda()
+    w, pos = bf(rng, D).cuda(), dev(np.arange(8).reshape(2, 4).astype(np.int32))
+    clean = fc.fc_qk_norm_rope(q, k, k, w, w, pos)
+    q[1, 2, 3, 5], k[0, 1, 1, 70] = float("nan"), float("inf")
+    bad = fc.fc_qk_norm_rope(q, k, k, w, w, pos)
+    assert bad[0][1, 2, 3].isnan().all() and bad[1][0, 1, 1].isnan().any()
+    bad[0][1, 2, 3] = clean[0][1, 2, 3]
+    bad[1][0, 1, 1] = clean[1][0, 1, 1]
+    assert torch.equal(bad[0], clean[0]) and torch.equal(bad[1], clean[1])
+
+
+# ------------------------------------------------------------------ writes
+def plan(rng, kv, new, page, gaps=False):
+    """Slots of new[b] tokens behind kv[b], pages in no order; n_pages, positions, tables."""
+    held = [-(-int(k + n) // page) for k, n in zip(kv, new)]
+    order = rng.permutation(sum(held) + 2).astype(np.int32)
+    slot, pos, at = [], [], 0
+    table = np.zeros((len(kv), max(max(held), 1)), np.int32)
+    for b, h in enumerate(held):
+        table[b, :h] = order[at:at + h]
+        at += h
+        p = np.arange(kv[b], kv[b] + new[b])
+        slot.append(table[b][p // page] * page + p % page)
+        pos.append(p)
+    slot = np.concatenate(slot).astype(np.int32)
+    if gaps:
+        slot[rng.random(len(slot)) < 0.1] = -1
+    return slot, len(order), np.concatenate(pos).astype(np.int32), table
+
+
+@pytest.mark.parametrize("kv,new,H,page,gaps", [([0], [1], 1, 16, False), ([5], [1], 2, 64, False), ([15, 16, 3], [1, 1, 1], 8, 32, False),
+                                                ([7, 0, 100], [40, 16, 333], 3, 128, True), ([0] * 40, [9] * 40, 8, 16, True),
+                                                ([3, 90], [2000, 777], 8, 256, True), ([11] * 5, [0, 1, 2, 3, 70], 32, 64, False)])
+def test_write_and_read(fc, kv, new, H, page, gaps):
+    rng = np.random.default_rng(len(kv) + H + page)
+    slot, n_pages, pos, _ = plan(rng, kv, new, page, gaps)
+    rows = len(slot)
+    cache = random_cache(rng, n_pages, H, page)
+    x = bf(rng, rows, 6 * H * D) * torch.exp(torch.from_numpy(rng.standard_normal((rows, 1)) * 2)).bfloat16()
+    x[rows // 2] = 0
+    xg = x.cuda()
+    got = on_gpu(fc, cache)
+    track = fc.Kv8Track(torch.full((n_pages, H, page), 3.5).cuda(), torch.full((n_pages, H, page), -7, dtype=torch.int32).cuda())
+    rt = [track.weight.cpu().numpy(), track.born.cpu().numpy()]
+    part = lambda t, i: t[:, i * H * D:(i + 1) * H * D].view(rows, H, D)
+    fc.fc_kv8_write(got, part(xg, 4), part(xg, 5), dev(slot), track=track, pos=dev(pos))
+    assert fc.fc_get_error() == "FC_OK"
+    o8.write(cache, num(part(x, 4)), num(part(x, 5)), slot, None, rt, pos)
+    same_cache(got, cache)
+    assert np.array_equal(track.weight.cpu().numpy(), rt[0]) and np.array_equal(track.born.cpu().numpy(), rt[1])
+    k, v = fc.fc_kv8_read(got, dev(slot))
+    for t, i in ((k, 0), (v, 1)):
+        p, o = slot // page, slot % page
+        want = o8.decode(cache[i][p, :, o]) * cache[2 + i][p, :, o // 16].astype(np.float64)[..., None]
+        want[slot < 0] = 0
+        assert np.array_equal(num(t), want)
+    again = on_gpu(fc, cache)  # the same rows once more change nothing
+    fc.fc_kv8_write(again, part(xg, 4), part(xg, 5), dev(slot))
+    same_cache(again, cache)
+
+
+def test_write_one_by_one_and_head_major(fc):
+    """Tokens appended singly, from head-major tensors by src, end as the oracle's do."""
+    rng = np.random.default_rng(5)
+    H, page, n = 4, 32, 45
+    cache = random_cache(rng, 4, H, page)
+    got = on_gpu(fc, cache)
+    x = [bf(rng, 2, H, 8, D, scale=10.0 ** float(e)).cuda() for e in rng.integers(-3, 4, n)]
+    for t in range(n):
+        slot = np.array([2 * page + t if t < 32 else t - 32], np.int32)
+        src = np.array([int(rng.integers(0, 16))], np.int32)
+        rows = x[t].transpose(1, 2)
+        fc.fc_kv8_write(got, rows, rows, dev(slot), src=dev(src))
+        r = num(rows.reshape(16, H, D))
+        o8.write(cache, r, r, slot, src)
+    assert fc.fc_get_error() == "FC_OK"
+    same_cache(got, cache)
+
+
+def test_write_extremes(fc):
+    """The largest and smallest bf16 numbers, zeros, NaN and infinities, and blocks begun anew."""
+    H, page = 1, 16
+    big, tiny = 3.3895313892515355e38, 9.183549615799121e-41
+    x = torch.zeros(5, H, D)
+    x[0, 0, :3] = torch.tensor([big, -1.0, tiny])
+    x[1, 0, :2] = torch.tensor([tiny, -tiny])
+    x[3, 0, 9] = float("nan")
+    x[4, 0, 1] = float("-inf")
+    x = x.bfloat16()
+    slot = np.array([0, 16, 33, 52, 66], np.int32)
+    rng = np.random.default_rng(1)
+    cache = random_cache(rng, 6, H, page)
+    got = on_gpu(fc, cache)
+    fc.fc_kv8_write(got, x.cuda(), x.cuda(), dev(slot))
+    o8.write(cache, num(x), num(x), slot)
+    same_cache(got, cache)
+    one = torch.ones(2, H, D).bfloat16()
+    more = np.array([53, 64], np.int32)  # into a block that stands for NaN; into one from its start
+    fc.fc_kv8_write(got, one.cuda(), one.cuda(), dev(more))
+    o8.write(cache, num(one), num(one), more)
+    same_cache(got, cache)
+    k, _ = fc.fc_kv8_read(got, dev(np.array([52, 53, 64], np.int32)))
+    assert k[:2].isnan().all() and (k[2] == 1).all() and fc.fc_get_error() == "FC_OK"
+
+
+def test_write_leaves_out_what_is_out_of_range(fc):
+    rng = np.random.default_rng(6)
+    cache = random_cache(rng, 3, 2, 16)
+    got = on_gpu(fc, cache)
+    x = bf(rng, 4, 2, D)
+    slot, src = np.array([0, 48, 17, 18], np.int32), np.array([0, 1, 4, 3], np.int32)  # slot 48 and row 4 are none
+    fc.fc_kv8_write(got, x.cuda(), x.cuda(), dev(slot), src=dev(src))
+    assert fc.fc_get_error() == "FC_ERR_INVALID_ARG"
+    o8.write(cache, num(x), num(x), slot, src)
+    same_cache(got, cache)
+    k, v = fc.fc_kv8_read(got, dev(np.array([1 << 30, -1], np.int32)))
+    assert fc.fc_get_error() == "FC_ERR_INVALID_ARG" and (k == 0).all() and (v == 0).all()
+
+
+# ------------------------------------------------------------------ attention
+def trees(rng, nodes, n):
+    words = (n + 63) // 64
+    m = np.zeros((len(nodes), n, words), np.uint64)
+    for b, nn in enumerate(nodes):
+        for i in range(nn):
+            if i:
+                m[b, i] = m[b, rng.integers(max(0, i - 8), i)]
+            m[b, i, i // 64] |= np.uint64(1) << np.uint64(i % 64)
+    return m.view(np.int64)
+
+
+def setup(rng, kv, n, H, Hkv, page, nodes=None, stale=True):
+    B = len(kv)
+    held = [-(-k // page) for k in kv]
+    n_pages = sum(held) + 2
+    order = rng.permutation(n_pages).astype(np.int32)
+    table = np.full((B, max(max(held), 1) + 1), -5, np.int32)
+    at = 0
+    for b, h in enumerate(held):
+        table[b, :h] = order[at:at + h]
+        at += h
+    cache = random_cache(rng, n_pages, Hkv, page)
+    if stale:  # what stands past a request's end is anything
+        for b, k in enumerate(kv):
+            for j in range(k, held[b] * page):
+                for i in range(2):
+                    cache[i][table[b, j // page], :, j % page] = 0x7F
+                    if j % 16 == 0:
+                        cache[2 + i][table[b, j // page], :, j % page // 16] = np.nan
+    return dict(kv=np.array(kv, np.int32), nodes=np.array(nodes if nodes is not None else [n] * B, np.int32), table=table, cache=cache,
+                q=bf(rng, B, n, H, D), k=bf(rng, B, Hkv, n, D), v=bf(rng, B, Hkv, n, D))
+
+
+def reference(s, masks, scale, new=True, causal=False):
+    B, n, H, _ = s["q"].shape
+    Hkv = s["k"].shape[1]
+    G = H // Hkv
+    page = s["cache"][0].shape[2]
+    out, mean, err = (np.zeros((B, n, H, m)) for m in (D, D, 1))
+    weight, werr = np.zeros(s["cache"][0].shape[:3]), np.zeros(s["cache"][0].shape[:3])
+    for b in range(B):
+        L, m = int(s["kv"][b]), int(s["nodes"][b])
+        i = np.arange(L)
+        p, o = s["table"][b][i // page], i % page
+        vis = np.zeros((m, m), bool)
+        for x in range(m):
+            for y in range(m):
+                vis[x, y] = y <= x if causal else bool((int(masks[b, x, y // 64]) >> (y % 64)) & 1)
+        if not new:
+            vis = np.zeros((m, 0), bool)
+        sees = np.concatenate((np.ones((m, L), bool), vis), 1)
+        for g in range(Hkv):
+            K, V = (np.concatenate((o8.cached(s["cache"], w, s["table"][b], L, g), num(s[x][b, g, :m if new else 0])))
+                    for w, x in ((0, "k"), (1, "v")))
+            for h in range(g * G, (g + 1) * G):
+                out[b, :m, h], w, mean[b, :m, h], err[b, :m, h] = o8.attend(num(s["q"][b, :m, h]), K, V, sees, scale)
+                weight[p, g, o] += w[:, :L].sum(0)
+                werr[p, g, o] += ((2 * err[b, :m, h] + 2.0 ** -18) * w[:, :L]).sum(0)
+    return out, (2.0 ** -8 * np.abs(out) + (2.0 ** -8 + 2.0 ** -16 + 2 * err) * mean), weight, werr
+
+
+def call(fc, s, masks=None, new=True, **kw):
+    c = on_gpu(fc, s["cache"])
+    k, v = (s["k"].cuda(), s["v"].cuda()) if new else (None, None)
+    return fc.fc_kv8_attn(s["q"].cuda(), c, dev(s["table"]), dev(s["kv"]), k, v, None if masks is None else dev(masks), dev(s["nodes"]), **kw)
+
+
+SHAPES = [([0], 1, 1, 1, 16), ([1], 1, 8, 8, 16), ([17], 1, 4, 1, 16), ([500], 1, 32, 8, 64), ([31, 32, 33, 0], 1, 16, 2, 32),
+          ([1000, 3, 257], 1, 8, 8, 128), ([700, 64], 2, 16, 8, 256), ([129, 5], 4, 8, 2, 64), ([300], 16, 2, 2, 16),
+          ([2500], 3, 8, 2, 64), ([9000], 1, 2, 1, 64), ([100, 200], 2, 32, 2, 16),
+          ([0, 130], 17, 4, 4, 16), ([127, 128, 129], 20, 8, 8, 32), ([600], 64, 8, 2, 64), ([1], 128, 4, 1, 128),
+          ([700, 0, 31], 40, 16, 1, 16), ([2000], 128, 8, 2, 64), ([383, 900], 100, 3, 3, 256), ([260], 128, 32, 2, 64)]
+
+
+@pytest.mark.parametrize("kv,n,H,Hkv,page", SHAPES)
+@pytest.mark.parametrize("workspace", [True, False])
+def test_attention(fc, kv, n, H, Hkv, page, workspace):
+    rng = np.random.default_rng(sum(kv) + n + H)
+    nodes = [max(1, n - 3 * b) for b in range(len(kv))]
+    s = setup(rng, kv, n, H, Hkv, page, nodes)
+    masks = trees(rng, nodes, n)
+    ws = fc.kv8_attn_workspace(len(kv), n, H, Hkv, "cuda") if workspace else None
+    got = call(fc, s, masks, workspace=ws)
+    assert fc.fc_get_error() == "FC_OK"
+    ref, tol, _, _ = reference(s, masks.view(np.uint64), D ** -0.5)
+    err = np.abs(num(got) - ref)
+    assert np.all(err <= tol), (err - tol).max()
+    for b, m in enumerate(nodes):
+        assert (got[b, m:] == 0).all()
+    if ws is not None:  # the workspace is fit for the next call, and results repeat
+        assert torch.equal(call(fc, s, masks, workspace=ws), got)
+
+
+@pytest.mark.parametrize("n,H,Hkv", [(1, 8, 2), (3, 4, 4), (64, 8, 2)])
+def test_attention_without_new_tokens_and_causal(fc, n, H, Hkv):
+    rng = np.random.default_rng(n)
+    s = setup(rng, [300, 0, 45], n, H, Hkv, 32)
+    got = call(fc, s, new=False, workspace=fc.kv8_attn_workspace(3, n, H, Hkv, "cuda"))
+    ref, tol, _, _ = reference(s, None, D ** -0.5, new=False, causal=True)
+    assert np.all(np.abs(num(got) - ref) <= tol) and (got[1] == 0).all()  # no key at all: zeros
+    got = call(fc, s, scale=0.05)
+    ref, tol, _, _ = reference(s, None, 0.05, causal=True)
+    assert np.all(np.abs(num(got) - ref) <= tol)
+    empty = np.zeros((3, n, (n + 63) // 64), np.int64)
+    assert (call(fc, s, empty)[1] == 0).all()  # masks that leave a row nothing
+    assert fc.fc_get_error() == "FC_OK"
+
+
+@pytest.mark.parametrize("n,H,Hkv", [(1, 8, 2), (4, 16, 4), (16, 1, 1), (2, 8, 8)])
+@pytest.mark.parametrize("decay", [0.0, 1.0, 0.5])
+def test_weights(fc, n, H, Hkv, decay):
+    rng = np.random.default_rng(n + H)
+    kv = [0, 5, 700, 64, 1500]
+    nodes = [n, max(1, n - 1), n, 0, n]
+    s = setup(rng, kv, n, H, Hkv, 64, nodes)
+    masks = trees(rng, nodes, n)
+    P = s["table"].shape[1] * 64
+    ws = fc.kv8_attn_workspace(len(kv), n, H, Hkv, "cuda", P)
+    before = rng.random(s["cache"][0].shape[:3]).astype(np.float32)
+    weight = dev(np.full_like(before, np.nan) if decay == 0 else before)
+    got = call(fc, s, masks, workspace=ws, weight=weight, decay=decay)
+    assert fc.fc_get_error() == "FC_OK"
+    assert torch.equal(got, call(fc, s, masks, workspace=ws))  # the output does not depend on them
+    ref, tol, w, we = reference(s, masks.view(np.uint64), D ** -0.5)
+    assert np.all(np.abs(num(got) - ref) <= tol)
+    have, seen = num(weight), np.zeros(before.shape, bool)
+    for b, k in enumerate(kv):
+        i = np.arange(k)
+        if nodes[b] or decay == 0:
+            seen[s["table"][b][i // 64], :, i % 64] = True
+        else:
+            seen[s["table"][b][i // 64], :, i % 64] = True
+    want = np.where(seen, decay * before.astype(np.float64) + w, before if decay else np.nan)
+    bound = we + 2.0 ** -22 * np.abs(np.nan_to_num(want))
+    assert np.array_equal(np.isnan(have), np.isnan(want))
+    assert np.all(np.abs(np.nan_to_num(have) - np.nan_to_num(want)) <= bound)
+
+
+def test_weights_need_their_workspace_and_few_rows(fc):
+    rng = np.random.default_rng(2)
+    s = setup(rng, [100], 1, 8, 2, 64)
+    w = torch.zeros(s["cache"][0].shape[:3]).cuda()
+    for ws in (None, fc.kv8_attn_workspace(1, 1, 8, 2, "cuda"), fc.kv8_attn_workspace(1, 1, 8, 2, "cuda", 64)):
+        with pytest.raises(fc.FastCoderError) as e:
+            call(fc, s, workspace=ws, weight=w)
+        assert e.value.status == "FC_ERR_WORKSPACE"
+    s = setup(rng, [100], 5, 8, 2, 64)
+    with pytest.raises(fc.FastCoderError) as e:
+        call(fc, s, workspace=torch.zeros(1 << 20, dtype=torch.uint8).cuda(), weight=w)
+    assert e.value.status == "FC_ERR_UNSUPPORTED"
+
+
+@pytest.mark.parametrize("n,H,Hkv", [(1, 8, 2), (2, 16, 2), (40, 4, 2)])
+def test_attention_scales_far_apart(fc, n, H, Hkv):
+    """Blocks of very different size, zeros among them, and a row of large queries."""
+    rng = np.random.default_rng(9)
+    s = setup(rng, [400, 90], n, H, Hkv, 32, stale=False)
+    s["cache"][3][:] = (2.0 ** rng.integers(-60, 60, s["cache"][3].shape)).astype(np.float32)
+    s["cache"][2][:] = (2.0 ** rng.integers(-40, -6, s["cache"][2].shape)).astype(np.float32)
+    s["cache"][1][3], s["cache"][0][4] = 0, 0
+    s["q"][0, 0, 0] *= 64
+    got = call(fc, s, workspace=fc.kv8_attn_workspace(2, n, H, Hkv, "cuda"))
+    ref, tol, _, _ = reference(s, None, D ** -0.5, causal=True)
+    assert np.all(np.abs(num(got) - ref) <= tol)
+
+
+@pytest.mark.parametrize("n,H,Hkv", [(1, 8, 2), (64, 4, 2)])
+def test_attention_many_small_weights_beside_a_large_one(fc, n, H, Hkv):
+    """One key 14 above thousands of others that together outweigh it."""
+    rng = np.random.default_rng(10)
+    L = 6000
+    s = setup(rng, [L], n, H, Hkv, 64, stale=False)
+    s["q"][:] = 0
+    s["q"][..., 0] = 1
+    for i in range(2):
+        s["cache"][2 + i][:] = 1
+    s["cache"][0][:] = 0
+    page, off = s["table"][0][7], 5
+    s["cache"][0][page, :, off, 0] = o8.encode(14.0)
+    s["k"][:] = -30  # new tokens weigh nothing
+    got = call(fc, s, scale=0.6, workspace=fc.kv8_attn_workspace(1, n, H, Hkv, "cuda"))
+    ref, tol, _, _ = reference(s, None, 0.6, causal=True)
+    assert np.all(np.abs(num(got) - ref) <= tol)
+
+
+@pytest.mark.parametrize("n,H,Hkv", [(1, 8, 2), (3, 4, 1), (64, 4, 2)])
+def test_not_finite_values_reach_only_rows_that_see_them(fc, n, H, Hkv):
+    rng = np.random.default_rng(11)
+    s = setup(rng, [200, 70, 90], n, H, Hkv, 32)
+    masks = trees(rng, [n] * 3, n)
+    ws = fc.kv8_attn_workspace(3, n, H, Hkv, "cuda")
+    clean = call(fc, s, masks, workspace=ws)
+    s["cache"][2][s["table"][0][1], 0, 1] = np.nan  # request 0, kv head 0: keys that stand for NaN
+    s["cache"][3][s["table"][1][0], Hkv - 1, 0] = np.nan  # request 1, the last kv head: values
+    s["v"][2, 0, n - 1, 3] = float("inf")  # request 2, head 0: the last new token's value
+    s["k"][2, 0, n - 1, 4] = float("nan")
+    got = call(fc, s, masks, workspace=ws)
+    G = H // Hkv
+    want = torch.zeros(3, n, H, dtype=torch.bool)
+    want[0, :, :G] = True
+    want[1, :, -G:] = True
+    want[2, :, :G] = torch.from_numpy((masks.view(np.uint64)[2, :, (n - 1) // 64] >> np.uint64((n - 1) % 64)) & np.uint64(1) == 1)[:, None]
+    nan = got.isnan().all(-1).cpu()
+    assert torch.equal(nan, want), (nan != want).nonzero()
+    assert torch.equal(got[~want.cuda()], clean[~want.cuda()])
+
+
+def test_bad_pages_and_lengths_are_recorded(fc):
+    rng = np.random.default_rng(12)
+    for n, H, Hkv in ((1, 8, 2), (40, 4, 2)):
+        s = setup(rng, [100, 60, 80], n, H, Hkv, 32)
+        ws = fc.kv8_attn_workspace(3, n, H, Hkv, "cuda")
+        masks = trees(rng, [n] * 3, n)
+        clean = call(fc, s, masks, workspace=ws)
+        s["kv"][1] = 100000
+        s["nodes"][2] = n + 1
+        got = call(fc, s, masks, workspace=ws)
+        assert fc.fc_get_error() == "FC_ERR_INVALID_ARG"
+        assert (got[1:] == 0).all() and torch.equal(got[0], clean[0])
+        s = setup(rng, [100, 60, 80], n, H, Hkv, 32, stale=False)
+        whole = {k: v for k, v in s.items()}
+        s["table"] = s["table"].copy()
+        s["table"][0, 1] = 1 << 20  # its 32 keys are left out
+        got = call(fc, s, masks, workspace=ws)
+        assert fc.fc_get_error() == "FC_ERR_INVALID_ARG"
+        short = dict(whole, table=np.concatenate((whole["table"][:, :1], whole["table"][:, 2:]), 1), kv=np.array([68, 0, 0], np.int32))
+        ref, tol, _, _ = reference(short, masks.view(np.uint64), D ** -0.5)
+        assert np.all(np.abs(num(got)[0] - ref[0]) <= tol[0])
+
+
+# ------------------------------------------------------------------ eviction
+@pytest.mark.parametrize("kv,keep,recent,H,page", [([20], [7], 0, 1, 16), ([64, 30], [40, 40], 8, 2, 32), ([1000, 333, 70], [500, 300, 1], 50, 3, 64),
+                                                   ([100], [99], 100, 2, 16), ([300, 300], [16, 0], 5, 2, 128), ([2100], [2047], 64, 1, 256),
+                                                   ([50, 0, 49], [48, 48, 48], 1000, 2, 16)])
+def test_evict(fc, kv, keep, recent, H, page):
+    rng = np.random.default_rng(sum(kv) + recent)
+    s = setup(rng, kv, 1, H, H, page, stale=False)
+    n_pages = len(s["cache"][0])
+    w = np.where(rng.random((n_pages, H, page)) < 0.3, 0.25, np.exp(rng.standard_normal((n_pages, H, page)))).astype(np.float32)  # many ties
+    w[rng.random(w.shape) < 0.01] = np.nan
+    w[rng.random(w.shape) < 0.01] = np.inf
+    w[rng.random(w.shape) < 0.02] = -0.0
+    born = np.zeros((n_pages, H, page), np.int32)
+    for b, k in enumerate(kv):
+        for h in range(H):
+            i = np.arange(k)
+            born[s["table"][b][i // page], h, i % page] = rng.permutation(k) + 11
+    w0 = np.full(w.shape, -5, np.float32)
+    b0 = np.full(born.shape, -6, np.int32)
+    cap = max([k for k, n in zip(keep, kv) if k < n] + [1]) + 3
+    got = on_gpu(fc, s["cache"])
+    t_in, t_out = fc.Kv8Track(dev(w), dev(born)), fc.Kv8Track(dev(w0), dev(b0))
+    args = (dev(s["table"]), dev(s["kv"]), dev(np.array(keep, np.int32)), recent, t_in, t_out)
+    frm = fc.fc_kv8_evict(got, *args, cap=cap)
+    assert fc.fc_get_error() == "FC_OK"
+    ref = o8.evict(s["cache"], s["table"], s["kv"], keep, recent, [w, born], [w0, b0], cap)
+    assert np.array_equal(frm.cpu().numpy(), ref)
+    same_cache(got, s["cache"])
+    assert np.array_equal(t_out.weight.cpu().numpy(), w0, equal_nan=True) and np.array_equal(t_out.born.cpu().numpy(), b0)
+    assert np.array_equal(t_in.weight.cpu().numpy(), w, equal_nan=True)
+
+
+def test_evict_long_request(fc):
+    """More tokens than the keys' place in shared memory holds."""
+    rng = np.random.default_rng(20)
+    L, K, page = 60000, 41000, 256
+    s = setup(rng, [L], 1, 1, 1, page, stale=False)
+    n_pages = len(s["cache"][0])
+    w = (rng.integers(0, 5000, (n_pages, 1, page)) / 64).astype(np.float32)  # ties
+    born = np.zeros((n_pages, 1, page), np.int32)
+    i = np.arange(L)
+    born[s["table"][0][i // page], 0, i % page] = rng.permutation(L)
+    w0, b0 = np.zeros_like(w), np.zeros_like(born)
+    got = on_gpu(fc, s["cache"])
+    t_out = fc.Kv8Track(dev(w0), dev(b0))
+    frm = fc.fc_kv8_evict(got, dev(s["table"]), dev(s["kv"]), dev(np.array([K], np.int32)), 3000, fc.Kv8Track(dev(w), dev(born)), t_out, cap=K)
+    ref = o8.evict(s["cache"], s["table"], s["kv"], [K], 3000, [w, born], [w0, b0], K)
+    assert np.array_equal(frm.cpu().numpy(), ref)
+    same_cache(got, s["cache"])
+    assert np.array_equal(t_out.weight.cpu().numpy(), w0) and np.array_equal(t_out.born.cpu().numpy(), b0)
+
+
+def test_evict_leaves_what_it_refuses(fc):
+    rng = np.random.default_rng(21)
+    kv = [60, 60, 60, 60]
+    s = setup(rng, kv, 1, 2, 2, 16, stale=False)
+    n_pages = len(s["cache"][0])
+    w, born = rng.random((n_pages, 2, 16)).astype(np.float32), rng.permutation(n_pages * 32).reshape(n_pages, 2, 16).astype(np.int32)
+    good = [s["table"][3].copy(), [c.copy() for c in s["cache"]]]
+    s["kv"][0] = -1
+    s["table"][1, 2] = n_pages  # a page outside the pool
+    keep = np.array([10, 10, 50, 20], np.int32)  # request 2: more than cap
+    got = on_gpu(fc, s["cache"])
+    w0, b0 = np.zeros_like(w), np.zeros_like(born)
+    t_out = fc.Kv8Track(dev(w0), dev(b0))
+    frm = fc.fc_kv8_evict(got, dev(s["table"]), dev(s["kv"]), dev(keep), 4, fc.Kv8Track(dev(w), dev(born)), t_out, cap=30)
+    assert fc.fc_get_error() == "FC_ERR_CAPACITY" and (frm[:3] == -1).all()
+    ref = o8.evict(good[1], good[0][None], [60], [20], 4, [w, born], [w0, b0], 30)
+    assert np.array_equal(frm[3:].cpu().numpy(), ref)
+    same_cache(got, good[1])
+    assert np.array_equal(t_out.weight.cpu().numpy(), w0)
