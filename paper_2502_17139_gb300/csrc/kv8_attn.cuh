@@ -22,3 +22,19 @@ struct Kv8Args {
   long long z_stride;
   unsigned int* err;
 };
+
+// A total cost cut into n shares of equal size (the first rem one longer), of
+// at least `least` each unless there is less.
+struct KvCut {
+  int n, q, rem;
+  __device__ __forceinline__ KvCut(int total, int grid, int least) {
+    n = max(1, min(grid, total / least));
+    q = total / n;
+    rem = total - q * n;
+  }
+  __device__ __forceinline__ int start(int c) const { return c * q + min(c, rem); }
+  __device__ __forceinline__ int share_of(int x) const {
+    const int longer = rem * (q + 1);
+    return x < longer ? x / (q + 1) : rem + (x - longer) / q;
+  }
+};
