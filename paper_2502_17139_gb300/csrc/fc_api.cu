@@ -16,6 +16,7 @@ extern "C" unsigned int fc_take_error_norm(cudaStream_t s);
 extern "C" unsigned int fc_take_error_kv8(cudaStream_t s);
 extern "C" unsigned int fc_take_error_kv8_attn(cudaStream_t s);
 extern "C" unsigned int fc_take_error_kv8_evict(cudaStream_t s);
+extern "C" unsigned int fc_take_error_kv8_tc(cudaStream_t s);
 
 namespace {
 thread_local unsigned int* t_error_slot = nullptr;
@@ -52,6 +53,6 @@ extern "C" fc_status fc_get_error(fc_stream stream) {
                    fc_take_error_attn(s) | fc_take_error_cache(s) |
                    fc_take_error_dec(s) | fc_take_error_gemm(s) | fc_take_error_kv4(s) |
                    fc_take_error_kv4_attn(s) | fc_take_error_kv4_tc(s) | fc_take_error_norm(s) | fc_take_error_kv8(s) |
-                   fc_take_error_kv8_attn(s) | fc_take_error_kv8_evict(s);
+                   fc_take_error_kv8_attn(s) | fc_take_error_kv8_evict(s) | fc_take_error_kv8_tc(s);
   return fc_status_of_bits(e);
 }

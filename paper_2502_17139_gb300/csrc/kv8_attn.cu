@@ -52,10 +52,6 @@ constexpr float VS_MIN = 0x1p-80f;
 // A reference before any key: 2^(z + 1e30) is infinite and not below W_MAX
 // whatever it is multiplied by, 2^(-1e30 - m) is 0.
 constexpr float M_START = -1e30f;
-// A workspace begins with counters that are zero between calls; what is written
-// past them needs no such care, so that one workspace serves every shape.
-constexpr size_t WS_COUNTERS = 4096;
-
 template <int NT>
 struct FewSmem {
   static constexpr int ROWS = 8 * NT;
@@ -744,7 +740,7 @@ __global__ void __launch_bounds__(FEW_THREADS, FEW_CTAS) k_kv8_attn_few(FewArgs 
 
 constexpr int FEW_GRID = 152 * FEW_CTAS;
 
-static_assert(FEW_GRID * sizeof(int) <= WS_COUNTERS, "room for the counters");
+static_assert(FEW_GRID * sizeof(int) <= KV8_WS_COUNTERS, "room for the counters");
 
 template <int NT>
 fc_status launch_few(const Kv8Args& a, void* ws, size_t ws_bytes, cudaStream_t s) {
@@ -755,7 +751,7 @@ fc_status launch_few(const Kv8Args& a, void* ws, size_t ws_bytes, cudaStream_t s
   });
   if (st != FC_OK) return st;
   const int full = FEW_GRID;
-  const size_t cnt = WS_COUNTERS, one = (size_t)2 * FewSmem<NT>::ROWS * (HD + 2) * sizeof(float);
+  const size_t cnt = KV8_WS_COUNTERS, one = (size_t)2 * FewSmem<NT>::ROWS * (HD + 2) * sizeof(float);
   const long long units = (long long)a.B * a.Hkv;
   // at most what the tables could hold, in steps (past 32 bits there are units enough without cutting them)
   const long long longest = (((long long)a.max_pages << a.shift) + STEP - 1) / STEP + 1, most = units * (longest + UNIT_COST);
@@ -773,75 +769,6 @@ fc_status launch_few(const Kv8Args& a, void* ws, size_t ws_bytes, cudaStream_t s
   }
   k_kv8_attn_few<NT><<<grid, FEW_THREADS, FewSmem<NT>::BYTES, s>>>(f);
   return FC_CHECK_LAUNCH();
-}
-
-// A warp a query row (request, node, head), four dimensions a lane, a key at a time.
-__global__ void __launch_bounds__(256) k_kv8_attn_rows(Kv8Args a) {
-  const int lane = threadIdx.x & 31;
-  const long long row = (long long)blockIdx.x * 8 + (threadIdx.x >> 5);
-  if (row >= (long long)a.B * a.n_pad * a.H) return;
-  const int h = (int)(row % a.H), i = (int)(row / a.H % a.n_pad), b = (int)(row / a.H / a.n_pad), gh = h / a.G;
-  int kvl = a.kv_len[b], nn = a.n_nodes ? a.n_nodes[b] : a.n_pad;
-  if (nn < 0 || nn > a.n_pad || kvl < 0 || kvl > (long long)a.max_pages << a.shift) {
-    if (h == 0 && i == 0 && lane == 0) fc_flag(FC_ERR_WORD(a.err), FC_EBIT_INVALID);
-    nn = kvl = 0;
-  }
-  uint2* out = reinterpret_cast<uint2*>(a.out + row * HD) + lane;
-  if (i >= nn) {
-    *out = make_uint2(0, 0);
-    return;
-  }
-  const int r = i * a.G + h - gh * a.G;
-  auto four = [](const uint2& w) {
-    return make_float4(__uint_as_float(w.x << 16), __uint_as_float(w.x & 0xFFFF0000u), __uint_as_float(w.y << 16), __uint_as_float(w.y & 0xFFFF0000u));
-  };
-  const float4 q = four(reinterpret_cast<const uint2*>(a.q + row * HD)[lane]);
-  float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-  float m = -INFINITY, l = 0.f;
-  auto take = [&](const float4& k, const float4& v) {
-    float z = fmaf(q.x, k.x, fmaf(q.y, k.y, fmaf(q.z, k.z, q.w * k.w)));
-#pragma unroll
-    for (int x = 16; x > 0; x >>= 1) z += __shfl_xor_sync(0xFFFFFFFFu, z, x);
-    z *= a.scale_log2;
-    if (!(z <= m)) {
-      const float mn = z, al = exp2_fast(m - mn);
-      m = mn;
-      l *= al;
-      o.x *= al, o.y *= al, o.z *= al, o.w *= al;
-    }
-    const float p = z == -INFINITY ? 0.f : exp2_fast(z - m);
-    l += p;
-    o.x = fmaf(p, v.x, o.x), o.y = fmaf(p, v.y, o.y), o.z = fmaf(p, v.z, o.z), o.w = fmaf(p, v.w, o.w);
-    return z;
-  };
-  const int32_t* tab = a.table + (size_t)b * a.max_pages;
-  float* zs = a.z ? a.z + (((size_t)b * a.Hkv + gh) * a.R + r) * a.z_stride : nullptr;
-  for (int j = 0; j < kvl; ++j) {
-    const int page = tab[j >> a.shift];
-    float z = -INFINITY;
-    if ((unsigned)page >= (unsigned)a.n_pages) {
-      if (lane == 0) fc_flag(FC_ERR_WORD(a.err), FC_EBIT_INVALID);
-    } else {
-      const size_t at = (((size_t)page * a.Hkv + gh) << a.shift) + (j & ((1 << a.shift) - 1));
-      auto cached = [&](const uint8_t* c, const float* s) {
-        const uint32_t w = reinterpret_cast<const uint32_t*>(c + at * HD)[lane];
-        const float2 x = e4m3x2_floats(w & 0xFFFFu), y = e4m3x2_floats(w >> 16);
-        const float by = s[at >> 4];
-        return make_float4(x.x * by, x.y * by, y.x * by, y.y * by);
-      };
-      z = take(cached(a.kc, a.ks), cached(a.vc, a.vs));
-    }
-    if (zs && lane == 0) zs[j] = z;
-  }
-  if (a.k_new)
-    for (int j = 0; j < nn; ++j) {
-      const bool sees = a.mask ? (a.mask[((size_t)b * a.n_pad + i) * ((a.n_pad + 63) / 64) + (j >> 6)] >> (j & 63)) & 1 : j <= i;
-      const size_t at = (((size_t)b * a.Hkv + gh) * a.n_pad + j) * HD;
-      if (sees) take(four(reinterpret_cast<const uint2*>(a.k_new + at)[lane]), four(reinterpret_cast<const uint2*>(a.v_new + at)[lane]));
-    }
-  const float inv = l == 0.f ? 0.f : 1.f / l;
-  *out = make_uint2(pack_bf16x2(o.x * inv, o.y * inv), pack_bf16x2(o.z * inv, o.w * inv));
-  if (a.z && lane == 0) a.lse[((size_t)b * a.Hkv + gh) * a.R + r] = l == 0.f ? INFINITY : m + log2f(l);
 }
 
 // weight = decay * weight + the sum over a kv head's rows of 2^(score - log2 of
@@ -882,7 +809,8 @@ size_t score_bytes(long long batch, int n_pad, int H, long long keys) {
 
 extern "C" size_t fc_kv8_attn_workspace(int batch, int n_pad, int H, int Hkv, int64_t weight_keys) {
   if (batch < 1 || !shape_ok(n_pad, H, Hkv) || weight_keys < 0 || (weight_keys && n_pad * (H / Hkv) > 16)) return 0;
-  return WS_COUNTERS + (size_t)FEW_GRID * 2 * FewSmem<2>::ROWS * (HD + 2) * sizeof(float) +
+  if (n_pad * (H / Hkv) > 16) return kv8_attn_many_workspace(batch, n_pad, H, Hkv);
+  return KV8_WS_COUNTERS + (size_t)FEW_GRID * 2 * FewSmem<2>::ROWS * (HD + 2) * sizeof(float) +
          (weight_keys ? score_bytes(batch, n_pad, H, weight_keys) : 0);
 }
 
@@ -940,7 +868,7 @@ extern "C" fc_status fc_kv8_attn(const void* d_q, const fc_kv8_cache* cache, con
   fc_status st = FC_OK;
   if (a.R <= 8) st = launch_few<1>(a, d_ws, ws_bytes, s);
   else if (a.R <= 16) st = launch_few<2>(a, d_ws, ws_bytes, s);
-  else k_kv8_attn_rows<<<(unsigned)(((long long)batch * n_pad * H + 7) / 8), 256, 0, s>>>(a);
+  else st = kv8_attn_many(a, d_ws, ws_bytes, s);
   if (st != FC_OK) return st;
   if (d_weight) {
     const dim3 grid((unsigned)std::min<long long>((a.z_stride + 1023) / 1024, 1024), (unsigned)(batch * cache->Hkv));

@@ -38,3 +38,11 @@ struct KvCut {
     return x < longer ? x / (q + 1) : rem + (x - longer) / q;
   }
 };
+
+// A workspace begins with counters that are zero between calls; what is written
+// past them needs no such care, so that one workspace serves every shape.
+constexpr size_t KV8_WS_COUNTERS = 4096;
+
+// The kernel for many query rows a kv head (kv8_attn_tc.cu).
+size_t kv8_attn_many_workspace(int batch, int n_pad, int H, int Hkv);
+fc_status kv8_attn_many(const Kv8Args& a, void* ws, size_t ws_bytes, cudaStream_t s);

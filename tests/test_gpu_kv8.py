@@ -369,6 +369,24 @@ def test_attention_scales_far_apart(fc, n, H, Hkv):
     assert np.all(np.abs(num(got) - ref) <= tol)
 
 
+@pytest.mark.parametrize("n,H,Hkv", [(1, 8, 2), (40, 4, 2)])
+def test_attention_subnormal_and_largest_numbers(fc, n, H, Hkv):
+    """Every e4m3 number: keys and values of each byte, e4m3's subnormal ones among them."""
+    rng = np.random.default_rng(8)
+    s = setup(rng, [400, 90], n, H, Hkv, 32, stale=False)
+    for i in range(2):
+        b = rng.integers(0, 254, s["cache"][i].shape).astype(np.uint8)
+        b[b >= 127] += 1  # all but 0x7F and 0xFF
+        b[:, 0] = (b[:, 0] & 0x80) | (b[:, 0] & 7)  # kv head 0: subnormal numbers alone
+        s["cache"][i][:] = b
+        s["cache"][2 + i][:] = 2.0 ** -8
+        s["cache"][2 + i][:, 0] = 2.0 ** 6
+    s["k"][:, 0] *= 0.1
+    got = call(fc, s, workspace=fc.kv8_attn_workspace(2, n, H, Hkv, "cuda"))
+    ref, tol, _, _ = reference(s, None, D ** -0.5, causal=True)
+    assert np.all(np.abs(num(got) - ref) <= tol)
+
+
 @pytest.mark.parametrize("n,H,Hkv", [(1, 8, 2), (64, 4, 2)])
 def test_attention_many_small_weights_beside_a_large_one(fc, n, H, Hkv):
     """One key 14 above thousands of others that together outweigh it."""
