@@ -36,10 +36,12 @@ struct Kv8Write {
 // none of the WINDOW rows before it goes to its block of 16; the run's rows are
 // those of the next WINDOW that do.  So the warp that meets a run's first row
 // knows the whole block's new tokens, and no two warps write one block.
-// Lanes 0-15 hold the keys, 16-31 the values, 8 dimensions a lane, all rows of
-// the run at once: their largest magnitude (bf16 bits as unsigned numbers order
-// like the magnitudes, infinities and NaN on top) gives the scale.
+// Lanes 0-15 hold the keys, 16-31 the values, 8 dimensions a lane, the block's 16
+// places at once: their largest magnitude (bf16 bits as unsigned numbers order
+// like the magnitudes, infinities and NaN on top) gives the scale.  Lane j works
+// out where place j's row is, for all.
 __global__ void __launch_bounds__(WR_THREADS) k_kv8_write(Kv8Write a, int per) {
+  __shared__ int s_row[WR_WARPS][KV8_BLOCK];
   const int lane = threadIdx.x & 31, half = lane >> 4, l16 = lane & 15;
   const uint32_t group = 0xFFFFu << (lane & 16);
   const long long item = (long long)blockIdx.x * WR_WARPS + (threadIdx.x >> 5);
@@ -47,7 +49,7 @@ __global__ void __launch_bounds__(WR_THREADS) k_kv8_write(Kv8Write a, int per) {
   const long long r0l = item / a.Hkv * per;
   if (r0l >= a.rows) return;
   const int r0 = (int)r0l;
-  // the block that a row goes to and its place there, -1: none
+  // the place that a row goes to, -1: none
   auto place = [&](int r) {
     if (r < 0 || r >= a.rows) return -1;
     const int sl = a.slot[r];
@@ -55,78 +57,78 @@ __global__ void __launch_bounds__(WR_THREADS) k_kv8_write(Kv8Write a, int per) {
     const int at = a.src ? a.src[r] : r;
     return sl < a.n_slots && at >= 0 && at < a.x.n_src ? sl : -1;
   };
-  const __nv_bfloat16* x0 = half ? a.x.v : a.x.k;
+  int* row_of = s_row[threadIdx.x >> 5];
+  const __nv_bfloat16* x0 = (half ? a.x.v : a.x.k) + h * a.x.head_stride;
   uint8_t* codes = half ? a.vc : a.kc;
   float* scales = half ? a.vs : a.ks;
-  const int before = place(r0 - WINDOW + lane);
-  int here = place(r0 + lane), next = place(r0 + WINDOW + lane);
-  if (h == 0 && lane < per && r0 + lane < a.rows && a.slot[r0 + lane] >= 0 && here < 0) fc_flag(FC_ERR_WORD(a.err), FC_EBIT_INVALID);
-  for (int i = 0; i < per; ++i) {
-    const int mine = __shfl_sync(0xFFFFFFFFu, here, i);
-    if (mine < 0) continue;
-    const int block = mine >> 4;
+  const int before = place(r0 - WINDOW + lane), here = place(r0 + lane), next = place(r0 + WINDOW + lane);
+  if (h == 0 && lane < per && r0 + lane < a.rows && here < 0 && a.slot[r0 + lane] >= 0) fc_flag(FC_ERR_WORD(a.err), FC_EBIT_INVALID);
+  const int last = __shfl_sync(0xFFFFFFFFu, before, 31), up = __shfl_up_sync(0xFFFFFFFFu, here, 1);
+  // rows whose neighbour above goes elsewhere
+  uint32_t starts = __ballot_sync(0xFFFFFFFFu, lane < per && here >= 0 && here >> 4 != (lane ? up : last) >> 4);
+#pragma unroll 1
+  for (; starts; starts &= starts - 1) {
+    const int i = __ffs(starts) - 1, mine = __shfl_sync(0xFFFFFFFFu, here, i), block = mine >> 4;
     // rows r0 + i - WINDOW .. - 1, then r0 + i .. + WINDOW - 1
-    const uint32_t same_b = __ballot_sync(0xFFFFFFFFu, before >= 0 && before >> 4 == block);
-    const uint32_t same_h = __ballot_sync(0xFFFFFFFFu, here >= 0 && here >> 4 == block);
-    const uint32_t same_n = __ballot_sync(0xFFFFFFFFu, next >= 0 && next >> 4 == block);
+    const uint32_t same_b = __ballot_sync(0xFFFFFFFFu, before >> 4 == block);
+    const uint32_t same_h = __ballot_sync(0xFFFFFFFFu, here >> 4 == block);
     if ((same_b >> i) | (same_h & ((1u << i) - 1u))) continue;  // an earlier row's run
-    uint32_t members = (same_h >> i) | (i ? same_n << (32 - i) : 0u);
+    if (lane < KV8_BLOCK) row_of[lane] = -1;
+    __syncwarp();
+    if (lane >= i && here >> 4 == block) row_of[here & 15] = r0 + lane;
+    if (lane < i && next >> 4 == block) row_of[next & 15] = r0 + WINDOW + lane;
+    __syncwarp();
     const int page = mine >> a.shift, in_page = (mine & ((1 << a.shift) - 1)) >> 4;
-    const size_t row0 = ((size_t)page * a.Hkv + h) << a.shift;
-    uint4 v[KV8_BLOCK];
-    int off[KV8_BLOCK];  // place in the block, -1: no row
-    uint32_t top = 0;
-    int first = KV8_BLOCK;
-#pragma unroll
-    for (int j = 0; j < KV8_BLOCK; ++j) {
-      off[j] = -1;
-      v[j] = make_uint4(0, 0, 0, 0);
-      if (members) {  // the same for the whole warp
-        const int m = __ffs(members) - 1, rel = i + m;
-        members &= members - 1;
-        const int sh = __shfl_sync(0xFFFFFFFFu, here, rel & 31), sn = __shfl_sync(0xFFFFFFFFu, next, rel & 31);
-        off[j] = (rel < 32 ? sh : sn) & 15;
-        const int r = r0 + rel, at = a.src ? a.src[r] : r;
-        const int q = a.x.one_seq ? 0 : at / a.x.n_per_seq, n = at - q * a.x.n_per_seq;
-        v[j] = reinterpret_cast<const uint4*>(x0 + q * a.x.seq_stride + n * a.x.row_stride + h * a.x.head_stride)[l16];
-        if (a.weight && lane == 0) {
-          a.weight[row0 + in_page * KV8_BLOCK + off[j]] = 0.f;
-          a.born[row0 + in_page * KV8_BLOCK + off[j]] = a.pos[r];
-        }
-        first = min(first, off[j]);
+    const size_t row0 = (((size_t)page * a.Hkv + h) << a.shift) + in_page * KV8_BLOCK;
+    const int my_row = row_of[l16];
+    const uint32_t have = __ballot_sync(0xFFFFFFFFu, my_row >= 0) & 0xFFFFu;  // places that get a row
+    const int first = __ffs(have) - 1;
+    long long from = 0;
+    if (my_row >= 0) {
+      const int at = a.src ? a.src[my_row] : my_row, q = a.x.one_seq ? 0 : at / a.x.n_per_seq, n = at - q * a.x.n_per_seq;
+      from = q * a.x.seq_stride + n * a.x.row_stride;
+      if (a.weight && half == 0) {
+        a.weight[row0 + l16] = 0.f;
+        a.born[row0 + l16] = a.pos[my_row];
       }
     }
+    float* scale = scales + (row0 >> 4);
+    uint2* rows = reinterpret_cast<uint2*>(codes + row0 * HD) + l16;
+    uint4 v[KV8_BLOCK];
+#pragma unroll
+    for (int j = 0; j < KV8_BLOCK; ++j) {
+      const long long off = __shfl_sync(0xFFFFFFFFu, from, j);
+      v[j] = make_uint4(0, 0, 0, 0);
+      if ((have >> j) & 1u) v[j] = __ldcs(reinterpret_cast<const uint4*>(x0 + off) + l16);
+    }
+    const float old = first > 0 ? *scale : 0.f;
+    uint32_t top = 0;
 #pragma unroll
     for (int j = 0; j < KV8_BLOCK; ++j)
       top = __vmaxu2(top, __vmaxu2(__vmaxu2(v[j].x & 0x7FFF7FFFu, v[j].y & 0x7FFF7FFFu),
                                    __vmaxu2(v[j].z & 0x7FFF7FFFu, v[j].w & 0x7FFF7FFFu)));
-    top = max(top & 0xFFFFu, top >> 16);
-#pragma unroll
-    for (int o = 1; o < 16; o <<= 1) top = max(top, __shfl_xor_sync(group, top, o));
-    float* scale = scales + (((size_t)page * a.Hkv + h) << (a.shift - 4)) + in_page;
-    uint2* rows = reinterpret_cast<uint2*>(codes + (row0 + in_page * KV8_BLOCK) * HD);
-    const float old = first > 0 ? *scale : 0.f;
-    bool nan = top >= 0x7F80u || (first > 0 && kv8_nan(old));
+    top = __reduce_max_sync(group, max(top & 0xFFFFu, top >> 16));
+    const bool nan = top >= 0x7F80u || kv8_nan(old);
     int e = nan ? 0 : max(kv8_exp_for(__uint_as_float(top << 16)), KV8_MIN_EXP);
     if (first > 0 && !nan) {
       const int e_old = kv8_exp(old);
       if (e > e_old) {  // what the block holds, in the new scale
+#pragma unroll 4
         for (int j = 0; j < first; ++j) {
-          uint2 w = rows[j * 16 + l16];
+          uint2 w = rows[j * 16];
           w.x = kv8_rescale4(w.x, e_old - e);
           w.y = kv8_rescale4(w.y, e_old - e);
-          rows[j * 16 + l16] = w;
+          rows[j * 16] = w;
         }
       } else {
         e = e_old;
       }
     }
-    __syncwarp(group);  // the scale is read by all before it changes
+    __syncwarp();  // all have read the scale
     if (l16 == 0) *scale = nan ? __uint_as_float(0x7FC00000u) : kv8_pow2(e);
-    const float by = nan ? 0.f : kv8_pow2(-e);
+    const float by = kv8_pow2(-e);
 #pragma unroll
     for (int j = 0; j < KV8_BLOCK; ++j) {
-      if (off[j] < 0) continue;
       uint32_t b[4];
 #pragma unroll
       for (int u = 0; u < 4; ++u) {
@@ -134,9 +136,9 @@ __global__ void __launch_bounds__(WR_THREADS) k_kv8_write(Kv8Write a, int per) {
         // a block with a NaN or an infinity stands for NaN, whatever its numbers
         b[u] = nan ? 0u : floats_e4m3x2(__uint_as_float(w << 16) * by, __uint_as_float(w & 0xFFFF0000u) * by);
       }
-      rows[off[j] * 16 + l16] = make_uint2(b[0] | (b[1] << 16), b[2] | (b[3] << 16));
+      if ((have >> j) & 1u) rows[j * 16] = make_uint2(b[0] | (b[1] << 16), b[2] | (b[3] << 16));
     }
-    __syncwarp();
+    __syncwarp();  // the places' rows are read before the next run's
   }
 }
 

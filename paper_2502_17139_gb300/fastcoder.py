@@ -1083,36 +1083,47 @@ def fc_qk_norm_rope(q, k, v, wq, wk, pos, base=10000.0, eps=1e-6, out=None):
     laid beside them.  bf16, any strides with a dense last dimension (k and v
     the same ones): parts of a projection's rows.  Returns q [B, n, H, D], k and
     v [B, Hkv, n, D] (``out``: these three)."""
-    for t, name in ((q, "q"), (k, "k")) + (((v, "v"),) if v is not None else ()):
-        if not isinstance(t, torch.Tensor) or t.dtype is not torch.bfloat16:
-            raise TypeError(f"{name} must be a torch.bfloat16 tensor")
-        if not t.is_cuda:
-            raise ValueError(f"{name} must be on a CUDA device")
-        if t.dim() != 4 or (t.stride(3) != 1 and t.shape[3] != 1):
-            raise ValueError(f"{name} must be [B, n, heads, D] with a dense last dimension")
-    B, n, H, D = q.shape
-    Hkv = k.shape[2]
-    if k.shape != (B, n, Hkv, D) or (v is not None and v.shape != k.shape):
-        raise ValueError("q, k and v must agree in batch, rows and head dimension")
-    qs, ks = _rows_strides(q), _rows_strides(k)
-    if v is not None and _rows_strides(v) != ks:
-        raise ValueError("k and v must have the same strides")
-    _need(wq, torch.bfloat16, "wq", (D,))
-    _need(wk, torch.bfloat16, "wk", (D,))
-    _need(pos, torch.int32, "pos", (B, n))
+    bf = torch.bfloat16
+    B, n, H, D = q.shape if q.dim() == 4 else (0, 0, 0, 0)
+    qs, ks, kshape = q.stride(), k.stride(), k.shape
+    if not (q.dtype is bf and k.dtype is bf and q.is_cuda and k.is_cuda and len(kshape) == 4 and D > 1 and qs[3] == 1 and ks[3] == 1 and
+            kshape[0] == B and kshape[1] == n and kshape[3] == D and
+            (v is None or (v.dtype is bf and v.is_cuda and v.shape == kshape and v.stride() == ks))):  # one test for the usual case
+        for t, name in ((q, "q"), (k, "k")) + (((v, "v"),) if v is not None else ()):
+            if not isinstance(t, torch.Tensor) or t.dtype is not bf:
+                raise TypeError(f"{name} must be a torch.bfloat16 tensor")
+            if not t.is_cuda:
+                raise ValueError(f"{name} must be on a CUDA device")
+            if t.dim() != 4 or t.stride(3) != 1:
+                raise ValueError(f"{name} must be [B, n, heads, D] with a dense last dimension")
+        if (kshape[0], kshape[1], kshape[3]) != (B, n, D) or (v is not None and v.shape != kshape):
+            raise ValueError("q, k and v must agree in batch, rows and head dimension")
+        ks = _rows_strides(k)
+        if v is not None and _rows_strides(v) != ks:
+            raise ValueError("k and v must have the same strides")
+    Hkv = kshape[2]
     if out is None:
-        new = lambda *s: torch.empty(s, dtype=torch.bfloat16, device=q.device)
+        new = lambda *s: torch.empty(s, dtype=bf, device=q.device)
         out = (new(B, n, H, D), new(B, Hkv, n, D), None if v is None else new(B, Hkv, n, D))
     qo, ko, vo = out
-    _need(qo, torch.bfloat16, "q of out", (B, n, H, D))
-    _need(ko, torch.bfloat16, "k of out", (B, Hkv, n, D))
+    heads = (B, Hkv, n, D)
+    if not (qo.dtype is bf and ko.dtype is bf and wq.dtype is bf and wk.dtype is bf and pos.dtype is torch.int32 and qo.is_cuda and
+            ko.is_cuda and wq.is_cuda and wk.is_cuda and pos.is_cuda and qo.is_contiguous() and ko.is_contiguous() and
+            wq.is_contiguous() and wk.is_contiguous() and pos.is_contiguous() and qo.shape == (B, n, H, D) and ko.shape == heads and
+            wq.shape == (D,) and wk.shape == (D,) and pos.shape == (B, n)):
+        _need(wq, bf, "wq", (D,))
+        _need(wk, bf, "wk", (D,))
+        _need(pos, torch.int32, "pos", (B, n))
+        _need(qo, bf, "q of out", (B, n, H, D))
+        _need(ko, bf, "k of out", heads)
     if (v is None) != (vo is None):
         raise ValueError("v and v of out go together")
     if vo is not None:
-        _need(vo, torch.bfloat16, "v of out", (B, Hkv, n, D))
+        _need(vo, bf, "v of out", heads)
     _check("fc_qk_norm_rope", LIB.fc_qk_norm_rope(
-        q.data_ptr(), *qs, k.data_ptr(), _ptr(v), *ks, wq.data_ptr(), wk.data_ptr(), pos.data_ptr(), B, n, H, Hkv, D, base, eps,
-        qo.data_ptr(), ko.data_ptr(), _ptr(vo), _stream()))
+        q.data_ptr(), qs[0], qs[1], qs[2], k.data_ptr(), None if v is None else v.data_ptr(), ks[0], ks[1], ks[2], wq.data_ptr(),
+        wk.data_ptr(), pos.data_ptr(), B, n, H, Hkv, D, base, eps, qo.data_ptr(), ko.data_ptr(), None if vo is None else vo.data_ptr(),
+        _stream()))
     return out
 
 
