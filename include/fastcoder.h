@@ -822,7 +822,7 @@ typedef struct {
   void* v_codes;     /* (0x7F and 0xFF, e4m3's NaN, are not written and not expected) */
   float* k_scale;    /* device, [n_pages][Hkv][page_size / 16] powers of two, 2^-120 to 2^120, or NaN */
   float* v_scale;
-  int32_t n_pages;   /* >= 1; n_pages * page_size < 2^31 */
+  int32_t n_pages;   /* >= 1; n_pages * page_size * Hkv < 2^31 */
   int32_t page_size; /* tokens a page: 16, 32, 64, 128 or 256 */
   int32_t Hkv;
   int32_t D;         /* 128 */
@@ -918,12 +918,13 @@ size_t fc_kv8_attn_workspace(int batch, int n_pad, int H, int Hkv, int64_t weigh
  *                come from.
  *   d_from       [batch][Hkv][cap] int32: the index that place i's token came
  *                from where it is not i, else -1
- *   d_ws         workspace of fc_kv8_evict_workspace() bytes (FC_ERR_WORKSPACE)
+ *   d_ws         workspace of fc_kv8_evict_workspace() bytes, 256-byte aligned
+ *                (FC_ERR_WORKSPACE), no initial contents needed
  * A request that loses tokens needs keep[b] <= cap: else it records
  * FC_ERR_CAPACITY, one with a negative length or keep, a length beyond its table
  * or a page id outside the pool FC_ERR_INVALID_ARG, and is left as it is (its
  * weights and positions are not carried over).  recent <= 2^22, batch * Hkv <=
- * 2^24.  Requests share no page that changes.
+ * 2^24, max_pages * page_size <= 696320.  Requests share no page that changes.
  */
 fc_status fc_kv8_evict(const fc_kv8_cache* cache, const int32_t* d_table, int max_pages, const int32_t* d_kv_len,
                        const int32_t* d_keep, int batch, int recent, const float* d_weight_in, const int32_t* d_born_in,

@@ -32,19 +32,18 @@ struct Kv8Write {
   unsigned int* err;
 };
 
-// A warp takes `per` neighbouring rows of one head.  A row begins a run when
+// A warp takes `per` neighbouring rows of one head, keys or values.  A row begins a run when
 // none of the WINDOW rows before it goes to its block of 16; the run's rows are
 // those of the next WINDOW that do.  So the warp that meets a run's first row
 // knows the whole block's new tokens, and no two warps write one block.
-// Lanes 0-15 hold the keys, 16-31 the values, 8 dimensions a lane, the block's 16
-// places at once: their largest magnitude (bf16 bits as unsigned numbers order
+// Four dimensions a lane, the block's 16 places at once: their largest magnitude (bf16 bits as unsigned numbers order
 // like the magnitudes, infinities and NaN on top) gives the scale.  Lane j works
 // out where place j's row is, for all.
 __global__ void __launch_bounds__(WR_THREADS) k_kv8_write(Kv8Write a, int per) {
   __shared__ int s_row[WR_WARPS][KV8_BLOCK];
-  const int lane = threadIdx.x & 31, half = lane >> 4, l16 = lane & 15;
-  const uint32_t group = 0xFFFFu << (lane & 16);
-  const long long item = (long long)blockIdx.x * WR_WARPS + (threadIdx.x >> 5);
+  const int lane = threadIdx.x & 31;
+  const bool values = threadIdx.x & 32;
+  const long long item = (long long)blockIdx.x * (WR_WARPS / 2) + (threadIdx.x >> 6);
   const int h = (int)(item % a.Hkv);
   const long long r0l = item / a.Hkv * per;
   if (r0l >= a.rows) return;
@@ -58,11 +57,11 @@ __global__ void __launch_bounds__(WR_THREADS) k_kv8_write(Kv8Write a, int per) {
     return sl < a.n_slots && at >= 0 && at < a.x.n_src ? sl : -1;
   };
   int* row_of = s_row[threadIdx.x >> 5];
-  const __nv_bfloat16* x0 = (half ? a.x.v : a.x.k) + h * a.x.head_stride;
-  uint8_t* codes = half ? a.vc : a.kc;
-  float* scales = half ? a.vs : a.ks;
+  const __nv_bfloat16* x0 = (values ? a.x.v : a.x.k) + h * a.x.head_stride;
+  uint8_t* codes = values ? a.vc : a.kc;
+  float* scales = values ? a.vs : a.ks;
   const int before = place(r0 - WINDOW + lane), here = place(r0 + lane), next = place(r0 + WINDOW + lane);
-  if (h == 0 && lane < per && r0 + lane < a.rows && here < 0 && a.slot[r0 + lane] >= 0) fc_flag(FC_ERR_WORD(a.err), FC_EBIT_INVALID);
+  if (h == 0 && !values && lane < per && r0 + lane < a.rows && here < 0 && a.slot[r0 + lane] >= 0) fc_flag(FC_ERR_WORD(a.err), FC_EBIT_INVALID);
   const int last = __shfl_sync(0xFFFFFFFFu, before, 31), up = __shfl_up_sync(0xFFFFFFFFu, here, 1);
   // rows whose neighbour above goes elsewhere
   uint32_t starts = __ballot_sync(0xFFFFFFFFu, lane < per && here >= 0 && here >> 4 != (lane ? up : last) >> 4);
@@ -80,63 +79,51 @@ __global__ void __launch_bounds__(WR_THREADS) k_kv8_write(Kv8Write a, int per) {
     __syncwarp();
     const int page = mine >> a.shift, in_page = (mine & ((1 << a.shift) - 1)) >> 4;
     const size_t row0 = (((size_t)page * a.Hkv + h) << a.shift) + in_page * KV8_BLOCK;
-    const int my_row = row_of[l16];
-    const uint32_t have = __ballot_sync(0xFFFFFFFFu, my_row >= 0) & 0xFFFFu;  // places that get a row
+    const int my_row = lane < KV8_BLOCK ? row_of[lane] : -1;
+    const uint32_t have = __ballot_sync(0xFFFFFFFFu, my_row >= 0);  // places that get a row
     const int first = __ffs(have) - 1;
     long long from = 0;
     if (my_row >= 0) {
       const int at = a.src ? a.src[my_row] : my_row, q = a.x.one_seq ? 0 : at / a.x.n_per_seq, n = at - q * a.x.n_per_seq;
       from = q * a.x.seq_stride + n * a.x.row_stride;
-      if (a.weight && half == 0) {
-        a.weight[row0 + l16] = 0.f;
-        a.born[row0 + l16] = a.pos[my_row];
+      if (a.weight && !values) {
+        a.weight[row0 + lane] = 0.f;
+        a.born[row0 + lane] = a.pos[my_row];
       }
     }
     float* scale = scales + (row0 >> 4);
-    uint2* rows = reinterpret_cast<uint2*>(codes + row0 * HD) + l16;
-    uint4 v[KV8_BLOCK];
+    uint32_t* rows = reinterpret_cast<uint32_t*>(codes + row0 * HD) + lane;
+    uint2 v[KV8_BLOCK];
 #pragma unroll
     for (int j = 0; j < KV8_BLOCK; ++j) {
       const long long off = __shfl_sync(0xFFFFFFFFu, from, j);
-      v[j] = make_uint4(0, 0, 0, 0);
-      if ((have >> j) & 1u) v[j] = __ldcs(reinterpret_cast<const uint4*>(x0 + off) + l16);
+      v[j] = make_uint2(0, 0);
+      if ((have >> j) & 1u) v[j] = __ldcs(reinterpret_cast<const uint2*>(x0 + off) + lane);
     }
     const float old = first > 0 ? *scale : 0.f;
     uint32_t top = 0;
 #pragma unroll
-    for (int j = 0; j < KV8_BLOCK; ++j)
-      top = __vmaxu2(top, __vmaxu2(__vmaxu2(v[j].x & 0x7FFF7FFFu, v[j].y & 0x7FFF7FFFu),
-                                   __vmaxu2(v[j].z & 0x7FFF7FFFu, v[j].w & 0x7FFF7FFFu)));
-    top = __reduce_max_sync(group, max(top & 0xFFFFu, top >> 16));
+    for (int j = 0; j < KV8_BLOCK; ++j) top = __vmaxu2(top, __vmaxu2(v[j].x & 0x7FFF7FFFu, v[j].y & 0x7FFF7FFFu));
+    top = __reduce_max_sync(0xFFFFFFFFu, max(top & 0xFFFFu, top >> 16));
     const bool nan = top >= 0x7F80u || kv8_nan(old);
     int e = nan ? 0 : max(kv8_exp_for(__uint_as_float(top << 16)), KV8_MIN_EXP);
     if (first > 0 && !nan) {
       const int e_old = kv8_exp(old);
       if (e > e_old) {  // what the block holds, in the new scale
 #pragma unroll 4
-        for (int j = 0; j < first; ++j) {
-          uint2 w = rows[j * 16];
-          w.x = kv8_rescale4(w.x, e_old - e);
-          w.y = kv8_rescale4(w.y, e_old - e);
-          rows[j * 16] = w;
-        }
+        for (int j = 0; j < first; ++j) rows[j * 32] = kv8_times4(rows[j * 32], kv8_half_pow2(e_old - e));
       } else {
         e = e_old;
       }
     }
     __syncwarp();  // all have read the scale
-    if (l16 == 0) *scale = nan ? __uint_as_float(0x7FC00000u) : kv8_pow2(e);
+    if (lane == 0) *scale = nan ? __uint_as_float(0x7FC00000u) : kv8_pow2(e);
     const float by = kv8_pow2(-e);
 #pragma unroll
     for (int j = 0; j < KV8_BLOCK; ++j) {
-      uint32_t b[4];
-#pragma unroll
-      for (int u = 0; u < 4; ++u) {
-        const uint32_t w = (&v[j].x)[u];
-        // a block with a NaN or an infinity stands for NaN, whatever its numbers
-        b[u] = nan ? 0u : floats_e4m3x2(__uint_as_float(w << 16) * by, __uint_as_float(w & 0xFFFF0000u) * by);
-      }
-      if ((have >> j) & 1u) rows[j * 16] = make_uint2(b[0] | (b[1] << 16), b[2] | (b[3] << 16));
+      auto two = [&](uint32_t w) { return floats_e4m3x2(__uint_as_float(w << 16) * by, __uint_as_float(w & 0xFFFF0000u) * by); };
+      // a block with a NaN or an infinity stands for NaN, whatever its numbers
+      if ((have >> j) & 1u) rows[j * 32] = nan ? 0u : two(v[j].x) | (two(v[j].y) << 16);
     }
     __syncwarp();  // the places' rows are read before the next run's
   }
@@ -175,7 +162,8 @@ __global__ void __launch_bounds__(WR_THREADS) k_kv8_read(const int32_t* __restri
 
 fc_status fc_kv8_check(const fc_kv8_cache* c) {
   if (!c || c->n_pages < 1 || c->Hkv < 1) return FC_ERR_INVALID_ARG;
-  if (c->D != HD || kv8_page_shift(c->page_size) < 0 || (long long)c->n_pages * c->page_size > 0x7FFFFFFFll)
+  if (c->D != HD || kv8_page_shift(c->page_size) < 0 || (long long)c->n_pages * c->page_size > 0x7FFFFFFFll ||
+      (long long)c->n_pages * c->page_size * c->Hkv > 0x7FFFFFFFll)  // rows are counted in 32 bits (256 GB of codes)
     return FC_ERR_UNSUPPORTED;
   if (!c->k_codes || !c->v_codes || !c->k_scale || !c->v_scale || !kv8_aligned(c->k_codes, 16) || !kv8_aligned(c->v_codes, 16) ||
       !kv8_aligned(c->k_scale, 4) || !kv8_aligned(c->v_scale, 4))
@@ -206,7 +194,7 @@ extern "C" fc_status fc_kv8_write(const fc_kv8_cache* cache, const void* d_k, co
   // one row a warp while that does not fill the GPU, else a block's worth
   const int per = (long long)rows * cache->Hkv <= 152 * 64 ? 1 : 16;
   const long long warps = ((long long)rows + per - 1) / per * cache->Hkv;
-  k_kv8_write<<<(unsigned)((warps + WR_WARPS - 1) / WR_WARPS), WR_THREADS, 0, static_cast<cudaStream_t>(stream)>>>(a, per);
+  k_kv8_write<<<(unsigned)((2 * warps + WR_WARPS - 1) / WR_WARPS), WR_THREADS, 0, static_cast<cudaStream_t>(stream)>>>(a, per);
   return FC_CHECK_LAUNCH();
 }
 

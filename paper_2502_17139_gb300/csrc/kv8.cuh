@@ -50,8 +50,21 @@ __device__ __forceinline__ int kv8_exp_for(float top) {
   return (int)(u >> 23) - 127 - 8 + ((u & 0x7FFFFFu) > 0x600000u ? 1 : 0);
 }
 
-// Four e4m3 numbers times 2^d, rounded again (d clamped: at 31 or more only
-// zeros are left in the range, at -31 or less nothing).
+// Two e4m3 numbers (the low 16 bits) as fp16; exact.
+__device__ __forceinline__ __half2 e4m3x2_halves(uint32_t two) {
+  return __half2(__nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)two, __NV_E4M3));
+}
+// Four e4m3 numbers times f, a power of two from 2^-24 to 2^15 in fp16 or 2^-24
+// for any smaller one, rounded again; products of at most 448.  What fp16 rounds
+// of its subnormal numbers is below 2^-14, nothing to e4m3's 2^-10.
+__device__ __forceinline__ uint32_t kv8_times4(uint32_t w, __half2 f) {
+  auto two = [&](uint32_t x) {
+    return (uint32_t)__nv_cvt_halfraw2_to_fp8x2(static_cast<__half2_raw>(__hmul2(e4m3x2_halves(x), f)), __NV_SATFINITE, __NV_E4M3);
+  };
+  return two(w & 0xFFFFu) | (two(w >> 16) << 16);
+}
+__device__ __forceinline__ __half2 kv8_half_pow2(int d) { return __float2half2_rn(kv8_pow2(min(max(d, -24), 15))); }
+// Four e4m3 numbers times 2^d, any d, rounded again; products of at most 448.
 __device__ __forceinline__ uint32_t kv8_rescale4(uint32_t w, int d) {
   const float f = kv8_pow2(min(max(d, -31), 31));
   const float2 a = e4m3x2_floats(w & 0xFFFFu), b = e4m3x2_floats(w >> 16);

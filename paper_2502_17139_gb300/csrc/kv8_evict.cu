@@ -10,14 +10,15 @@
 //
 //   k_select  a CTA a (request, head): the order of the tokens as 32-bit keys,
 //             the K-th largest by three counts of 11, 11 and 10 bits (keys kept
-//             in shared memory while they fit), then warps that each own a run
-//             of indexes count ties, holes and sources, and write where every
-//             place's token comes from, its weight and its position.
-//   k_move    a warp a block of 16 places: one that takes a token is put
-//             together in registers (8 bytes a lane of each row, lanes 0-15 keys, 16-31
-//             values), gets the scale for what it then holds and is written
-//             whole.  The block that holds both the last places and the first
-//             sources changes its scale too, so it is left for a second launch.
+//             in shared memory while they fit); who stays as a bit a token, whose
+//             sums over groups of 32 rank ties, holes and sources without a walk;
+//             then where every place's token comes from, its weight and position,
+//             and a list of the blocks of 16 places that take a token.
+//   k_move    a warp a block on the list: put together in registers (8 bytes a
+//             lane of each row, lanes 0-15 keys, 16-31 values), it gets the scale
+//             for what it then holds; rows that change are written.  The block
+//             that holds both the last places and the first sources is read from
+//             a copy, as its own warp may have written it.
 #include <algorithm>
 #include <climits>
 
@@ -28,12 +29,15 @@ FC_DEFINE_ERROR_WORD(kv8_evict)
 namespace {
 
 constexpr int HD = KV8_D;
-constexpr int SEL_THREADS = 1024, SEL_WARPS = SEL_THREADS / 32;
+constexpr int SEL_THREADS = 1024;
 constexpr int BINS = 2048;
-constexpr int KEYS_SMEM = 49152;             // keys that fit in shared memory (192 KB)
+constexpr int KEYS_SMEM = 40960;             // keys that fit in shared memory (160 KB)
+constexpr int SEL_SMEM = KEYS_SMEM / 32 * 34 * 4;
+constexpr int MAX_KEYS = SEL_SMEM / 8 * 32;  // 696,320 tokens a request
 constexpr int MAX_RECENT = 1 << 22;
 constexpr uint32_t KEY_RECENT = 0xFF900000u;  // above every weight's key; recent tokens by age from here on
 constexpr int MV_THREADS = 256, MV_WARPS = MV_THREADS / 32;
+constexpr int EDGE_BYTES = 2 * KV8_BLOCK * HD + 16;  // a unit's copy: 16 rows of keys, of values, their scales
 
 struct EvictArgs {
   const int32_t *table, *kv_len, *keep;
@@ -43,7 +47,11 @@ struct EvictArgs {
   float* w_out;
   int32_t* b_out;
   int32_t* from;   // [batch][Hkv][cap]
-  int32_t* list;   // workspace [batch][Hkv][cap]: sources in order
+  // workspace
+  int32_t* count;       // [batch][Hkv] blocks on the list
+  int32_t* todo;        // [batch][Hkv][ceil(cap / 16)] the list
+  int32_t* list;        // [batch][Hkv][cap] sources in order, where they do not fit in shared memory
+  unsigned char* edge;  // [batch][Hkv][EDGE_BYTES]
   uint8_t *kc, *vc;
   float *ks, *vs;
   unsigned int* err;
@@ -56,211 +64,335 @@ __device__ __forceinline__ uint32_t key_of(float w) {
   return (u & 0x80000000u) ? ~u : u | 0x80000000u;
 }
 
-__global__ void __launch_bounds__(SEL_THREADS) k_select(EvictArgs a) {
-  extern __shared__ uint32_t s_keys[];
+// Inclusive sums over the block's threads, by way of one value a warp.
+__device__ __forceinline__ uint32_t block_scan(uint32_t v, uint32_t* s_sum) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const uint32_t x = __shfl_up_sync(0xFFFFFFFFu, v, o);
+    if (lane >= o) v += x;
+  }
+  __syncthreads();
+  if (lane == 31) s_sum[warp] = v;
+  __syncthreads();
+  return v + __reduce_add_sync(0xFFFFFFFFu, lane < warp ? s_sum[lane] : 0u);
+}
+
+__device__ __forceinline__ uint32_t half2_bits(__half2 v) { return *reinterpret_cast<uint32_t*>(&v); }
+__device__ __forceinline__ __half2 bits_half2(uint32_t v) { return *reinterpret_cast<__half2*>(&v); }
+
+// Threads: a power of two, 512 to SEL_THREADS.  Shared memory: held_cap keys (the
+// sources' list takes their place) and two words a group of 32 tokens, or, of a
+// longer request, these words alone.
+__global__ void __launch_bounds__(SEL_THREADS) k_select(EvictArgs a, int held_cap) {
+  extern __shared__ uint32_t s_dyn[];
   __shared__ uint32_t s_hist[BINS];
-  __shared__ int s_warp[SEL_WARPS][3];
-  __shared__ uint32_t s_sum[SEL_WARPS];
-  __shared__ int s_bad, s_newest;
-  __shared__ uint32_t s_digit, s_left;
-  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  __shared__ uint32_t s_sum[32];
+  __shared__ int s_bad, s_newest, s_todo;
+  __shared__ uint32_t s_digit, s_left, s_in_bin;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, threads = blockDim.x, warps = threads >> 5;
   const int unit = blockIdx.x, b = unit / a.Hkv, h = unit - b * a.Hkv;
-  int L = a.kv_len[b], keep = a.keep[b];
+  const int L = a.kv_len[b], keep = a.keep[b];
   const int32_t* tab = a.table + (size_t)b * a.max_pages;
   int32_t* from = a.from + (size_t)unit * a.cap;
-  int32_t* list = a.list + (size_t)unit * a.cap;
-  if (tid == 0) s_bad = 0, s_newest = INT_MIN;
-  __syncthreads();
   const bool wrong = L < 0 || keep < 0 || L > (long long)a.max_pages << a.shift;
-  if (!wrong)
-    for (int i = tid; i < (int)(((long long)L + (1 << a.shift) - 1) >> a.shift); i += SEL_THREADS)
-      if ((unsigned)tab[i] >= (unsigned)a.n_pages) s_bad = 1;
-  __syncthreads();
   const bool full = !wrong && keep < L && keep > a.cap;
-  if (wrong || s_bad || full) {  // left as it is
-    if (tid == 0 && h == 0) fc_flag(FC_ERR_WORD(a.err), full && !s_bad ? FC_EBIT_CAPACITY : FC_EBIT_INVALID);
-    for (int i = tid; i < a.cap; i += SEL_THREADS) from[i] = -1;
-    return;
-  }
-  auto at = [&](int i) { return ((((size_t)tab[i >> a.shift]) * a.Hkv + h) << a.shift) + (i & ((1 << a.shift) - 1)); };
-  if (keep >= L) {
-    for (int i = tid; i < a.cap; i += SEL_THREADS) from[i] = -1;
-    for (int i = tid; i < L; i += SEL_THREADS) {
-      const size_t p = at(i);
-      a.w_out[p] = a.w_in[p];
-      a.b_out[p] = a.b_in[p];
+  const bool held = L <= held_cap;
+  uint32_t* s_keys = s_dyn;
+  uint32_t* bits = held ? s_dyn + held_cap : s_dyn;
+  int32_t* list = held ? reinterpret_cast<int32_t*>(s_keys) : a.list + (size_t)unit * a.cap;
+  if (tid == 0) s_bad = 0, s_newest = INT_MIN, s_todo = 0;
+  for (int i = tid; i < BINS; i += threads) s_hist[i] = 0;
+  __syncthreads();
+  // a token's place; false for a page outside the pool
+  auto at = [&](int i, uint32_t& p) {
+    const uint32_t page = (uint32_t)__ldg(tab + (i >> a.shift));
+    p = ((page * (uint32_t)a.Hkv + (uint32_t)h) << a.shift) | ((uint32_t)i & ((1u << a.shift) - 1u));
+    return page < (uint32_t)a.n_pages;
+  };
+  const bool lose = !wrong && !full && keep < L;
+  // weights and positions of places 0 .. n - 1, from the indexes that `source` gives; four loads ahead of their stores
+  auto copy_tracks = [&](int n, auto&& source) {
+    for (int i0 = tid; i0 < n; i0 += 4 * threads) {
+      uint32_t p[4];
+      float w[4];
+      int born[4];
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        const int i = i0 + u * threads;
+        if (i >= n) continue;
+        uint32_t q;
+        at(i, p[u]);
+        at(source(i), q);
+        w[u] = __ldg(a.w_in + q);
+        born[u] = __ldg(a.b_in + q);
+      }
+#pragma unroll
+      for (int u = 0; u < 4; ++u)
+        if (i0 + u * threads < n) a.w_out[p[u]] = w[u], a.b_out[p[u]] = born[u];
     }
+  };
+  if (!wrong && !full) {
+    int newest = INT_MIN;
+    bool bad = false;
+    const bool read_born = lose && a.recent > 0, read_weight = lose && held;
+#pragma unroll 4
+    for (int i = tid; i < L; i += threads) {
+      uint32_t p;
+      const bool ok = at(i, p);
+      bad |= !ok;
+      const int born = ok && read_born ? __ldg(a.b_in + p) : INT_MIN;
+      const float weight = ok && read_weight ? __ldg(a.w_in + p) : 0.f;
+      newest = max(newest, born);
+      if (read_weight) s_keys[i] = key_of(weight);
+    }
+    if (bad) s_bad = 1;
+    newest = __reduce_max_sync(0xFFFFFFFFu, newest);
+    if (lane == 0 && newest != INT_MIN) atomicMax(&s_newest, newest);
+  }
+  __syncthreads();
+  if (wrong || full || s_bad) {  // left as it is
+    if (tid == 0) {
+      a.count[unit] = 0;
+      if (h == 0) fc_flag(FC_ERR_WORD(a.err), full ? FC_EBIT_CAPACITY : FC_EBIT_INVALID);
+    }
+    for (int i = tid; i < a.cap; i += threads) from[i] = -1;
     return;
   }
-  if (a.recent > 0) {
-    int newest = INT_MIN;
-    for (int i = tid; i < L; i += SEL_THREADS) newest = max(newest, a.b_in[at(i)]);
-    newest = __reduce_max_sync(0xFFFFFFFFu, newest);
-    if (lane == 0) atomicMax(&s_newest, newest);
-    __syncthreads();
+  if (!lose) {
+    if (tid == 0) a.count[unit] = 0;
+    for (int i = tid; i < a.cap; i += threads) from[i] = -1;
+    copy_tracks(L, [&](int i) { return i; });
+    return;
   }
+  // ---- keys, the first count with them
   const long long after = (long long)s_newest - a.recent;  // positions above this are recent
-  const bool held = L <= KEYS_SMEM;
-  auto make_key = [&](int i) {
-    const size_t p = at(i);
+  auto make_key = [&](int i, bool have) {
+    uint32_t p;
+    if (a.recent > 0 || !have) at(i, p);
     if (a.recent > 0) {
-      const long long age = (long long)a.b_in[p] - after;
+      const long long age = (long long)__ldg(a.b_in + p) - after;
       if (age > 0) return KEY_RECENT + (uint32_t)age;
     }
-    return key_of(a.w_in[p]);
+    return have ? s_keys[i] : key_of(__ldg(a.w_in + p));
   };
-  if (held) {
-    for (int i = tid; i < L; i += SEL_THREADS) s_keys[i] = make_key(i);
-  }
-  auto key = [&](int i) { return held ? s_keys[i] : make_key(i); };
-  // ---- the keep-th largest key
+  auto key = [&](int i) { return held ? s_keys[i] : make_key(i, false); };
   uint32_t prefix = 0, mask = 0, want = (uint32_t)keep;  // keys of this prefix still wanted
 #pragma unroll 1
   for (int pass = 0; pass < 3 && keep > 0; ++pass) {
-    const int low = pass == 0 ? 21 : pass == 1 ? 10 : 0, bits = pass == 2 ? 10 : 11;
-    for (int i = tid; i < BINS; i += SEL_THREADS) s_hist[i] = 0;
-    __syncthreads();
-    for (int i = tid; i < L; i += SEL_THREADS) {
-      const uint32_t k = key(i);
-      if ((k & mask) == prefix) atomicAdd(&s_hist[(k >> low) & ((1u << bits) - 1u)], 1u);
+    const int low = pass == 0 ? 21 : pass == 1 ? 10 : 0, width = pass == 2 ? 10 : 11;
+    auto count = [&](bool in, uint32_t k) {
+      const uint32_t digit = in && (k & mask) == prefix ? (k >> low) & ((1u << width) - 1u) : BINS;
+      // many tokens may have one weight, 0 above all: a warp of them is one addition
+      const uint32_t first = __shfl_sync(0xFFFFFFFFu, digit, 0);
+      if (__all_sync(0xFFFFFFFFu, digit == first)) {
+        if (lane == 0 && first < BINS) atomicAdd(&s_hist[first], 32u);
+      } else if (digit < BINS) {
+        atomicAdd(&s_hist[digit], 1u);
+      }
+    };
+    if (pass == 0 && held) {
+#pragma unroll 4
+      for (int i0 = 32 * warp; i0 < L; i0 += threads) {
+        const int i = i0 + lane;
+        const uint32_t k = i < L ? make_key(i, true) : 0u;
+        if (i < L) s_keys[i] = k;
+        count(i < L, k);
+      }
+    } else {
+      for (int i0 = 32 * warp; i0 < L; i0 += threads) count(i0 + lane < L, i0 + lane < L ? key(i0 + lane) : 0u);
     }
     __syncthreads();
-    // the bin where the count from above reaches `want`: two bins a thread, from the top
-    const uint32_t c0 = s_hist[BINS - 1 - 2 * tid], c1 = s_hist[BINS - 2 - 2 * tid];
-    uint32_t inc = c0 + c1;
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-      const uint32_t v = __shfl_up_sync(0xFFFFFFFFu, inc, o);
-      if (lane >= o) inc += v;
+    // the bin where the count from above reaches `want`: some bins a thread, from the top
+    const int each = BINS / threads, top = BINS - 1 - each * tid;
+    uint32_t sum = 0;
+    for (int j = 0; j < each; ++j) sum += s_hist[top - j];
+    uint32_t above = block_scan(sum, s_sum) - sum;
+    for (int j = 0; j < each; ++j) {
+      const uint32_t c = s_hist[top - j];
+      if (above < want && want <= above + c) s_digit = top - j, s_left = want - above, s_in_bin = c;
+      above += c;
+      s_hist[top - j] = 0;
     }
-    if (lane == 31) s_sum[warp] = inc;
-    __syncthreads();
-    uint32_t base = 0;
-    for (int w = 0; w < warp; ++w) base += s_sum[w];
-    const uint32_t above = base + inc - c0 - c1;
-    if (above < want && want <= above + c0) s_digit = BINS - 1 - 2 * tid, s_left = want - above;
-    else if (above + c0 < want && want <= above + c0 + c1) s_digit = BINS - 2 - 2 * tid, s_left = want - above - c0;
     __syncthreads();
     prefix |= s_digit << low;
-    mask |= ((1u << bits) - 1u) << low;
+    mask |= ((1u << width) - 1u) << low;
     want = s_left;
-    __syncthreads();
+    // all of the bin's keys stay: the rest of the bits do not matter
+    if (want == s_in_bin) break;
   }
-  // prefix: the smallest key that stays; `want` of its ties do, the first ones
-  const uint32_t edge = keep > 0 ? prefix : 0xFFFFFFFFu;
-  const int seg = ((L + SEL_WARPS - 1) / SEL_WARPS + 31) & ~31, i0 = min(L, warp * seg), i1 = min(L, i0 + seg);
-  const uint32_t below = (1u << lane) - 1u;
-  int ties = 0;
-  for (int i = i0; i < i1; i += 32) ties += __popc(__ballot_sync(0xFFFFFFFFu, i + lane < i1 && key(i + lane) == edge));
-  if (lane == 0) s_warp[warp][0] = ties;
-  __syncthreads();
-  int ties0 = 0;
-  for (int w = 0; w < warp; ++w) ties0 += s_warp[w][0];
-  // which of 32 tokens from i on stay; t: ties met so far
-  auto stay = [&](int i, int& t) {
-    const uint32_t k = i + lane < i1 ? key(i + lane) : 0u;
-    const bool tie = i + lane < i1 && k == edge;
-    const uint32_t ts = __ballot_sync(0xFFFFFFFFu, tie);
-    const bool s = keep > 0 && i + lane < i1 && (k > edge || (tie && t + __popc(ts & below) < (int)want));
-    t += __popc(ts);
-    return __ballot_sync(0xFFFFFFFFu, s);
-  };
-  auto lows = [&](int i) { return keep <= i ? 0u : keep - i >= 32 ? 0xFFFFFFFFu : (1u << (keep - i)) - 1u; };  // places below keep
-  int holes = 0, sources = 0, t = ties0;
-  for (int i = i0; i < i1; i += 32) {
-    const uint32_t s = stay(i, t), lo = lows(i);
-    holes += __popc(~s & lo);
-    sources += __popc(s & ~lo);
-  }
-  if (lane == 0) s_warp[warp][1] = holes, s_warp[warp][2] = sources;
-  __syncthreads();
-  int hole0 = 0, source0 = 0;
-  for (int w = 0; w < warp; ++w) hole0 += s_warp[w][1], source0 += s_warp[w][2];
-  t = ties0;
-  for (int i = i0; i < i1; i += 32) {  // the sources, in order
-    const uint32_t s = stay(i, t) & ~lows(i);
-    if ((s >> lane) & 1u) list[source0 + __popc(s & below)] = i + lane;
-    source0 += __popc(s);
-  }
-  __syncthreads();
-  t = ties0;
-  for (int i = i0; i < min(i1, keep); i += 32) {
-    const uint32_t gone = ~stay(i, t) & lows(i);
-    if (i + lane < keep) {
-      const bool hole = (gone >> lane) & 1u;
-      const int src = hole ? list[hole0 + __popc(gone & below)] : -1;
-      from[i + lane] = src;
-      const size_t p = at(i + lane), q = hole ? at(src) : p;
-      a.w_out[p] = a.w_in[q];
-      a.b_out[p] = a.b_in[q];
+  // keys whose masked bits are above prefix stay, and the first `want` of those equal to it (all, if there are no more)
+  const bool all_ties = keep > 0 && want == s_in_bin;
+  const int groups = (L + 31) >> 5;
+  for (int g = warp; g < groups; g += warps) {
+    const int i = 32 * g + lane;
+    const uint32_t k = i < L && keep > 0 ? key(i) & mask : 0u;
+    const uint32_t up = __ballot_sync(0xFFFFFFFFu, i < L && keep > 0 && (all_ties ? k >= prefix : k > prefix));
+    const uint32_t tie = __ballot_sync(0xFFFFFFFFu, i < L && keep > 0 && k == prefix);
+    if (lane == 0) {
+      bits[2 * g] = up;
+      if (!all_ties) bits[2 * g + 1] = tie;
     }
-    hole0 += __popc(gone);
   }
-  for (int i = keep + tid; i < a.cap; i += SEL_THREADS) from[i] = -1;
+  __syncthreads();
+  const int each = (groups + threads - 1) / threads, g0 = min(groups, tid * each), g1 = min(groups, g0 + each);
+  if (!all_ties && keep > 0) {
+    uint32_t n = 0;
+    for (int g = g0; g < g1; ++g) n += __popc(bits[2 * g + 1]);
+    uint32_t rank = block_scan(n, s_sum) - n;
+    for (int g = g0; g < g1; ++g) {
+      uint32_t tie = bits[2 * g + 1];
+      const uint32_t c = __popc(tie), room = want > rank ? want - rank : 0u;
+      for (uint32_t x = room; x < c; ++x) tie &= ~(0x80000000u >> __clz(tie));  // the last ones go
+      bits[2 * g] |= tie;
+      rank += c;
+    }
+  }
+  // ---- holes (bits 0..15 of a sum) and sources; at most 2^31 tokens, so a sum each
+  auto lows = [&](int g) { return keep <= 32 * g ? 0u : keep - 32 * g >= 32 ? 0xFFFFFFFFu : (1u << (keep - 32 * g)) - 1u; };
+  uint32_t nh = 0, ns = 0;
+  for (int g = g0; g < g1; ++g) {
+    const uint32_t s = bits[2 * g], lo = lows(g);
+    nh += __popc(~s & lo);
+    ns += __popc(s & ~lo);
+  }
+  nh = block_scan(nh, s_sum) - nh;
+  ns = block_scan(ns, s_sum) - ns;
+  for (int g = g0; g < g1; ++g) {  // a group's second word: its first hole's or source's rank (of the group with both, the hole's)
+    const uint32_t s = bits[2 * g], lo = lows(g);
+    bits[2 * g + 1] = lo ? nh : ns;
+    for (uint32_t m = lo ? s & ~lo : 0u, r = ns; m; m &= m - 1, ++r) list[r] = 32 * g + __ffs(m) - 1;
+    nh += __popc(~s & lo);
+    ns += __popc(s & ~lo);
+  }
+  __syncthreads();
+  const uint32_t below = (1u << lane) - 1u;
+  for (int g = (keep + 31) / 32 + warp; g < groups; g += warps) {  // the sources, in order
+    const uint32_t s = bits[2 * g];
+    if ((s >> lane) & 1u) list[bits[2 * g + 1] + __popc(s & below)] = 32 * g + lane;
+  }
+  // ---- the blocks that take a token
+  int32_t* todo = a.todo + (size_t)unit * ((a.cap + KV8_BLOCK - 1) / KV8_BLOCK);
+  for (int t0 = 32 * warp; t0 < (keep + KV8_BLOCK - 1) / KV8_BLOCK; t0 += threads) {
+    const int t = t0 + lane;
+    const bool takes = t < (keep + KV8_BLOCK - 1) / KV8_BLOCK && (((~bits[t & ~1] & lows(t >> 1)) >> (16 * (t & 1))) & 0xFFFFu);
+    const uint32_t all = __ballot_sync(0xFFFFFFFFu, takes);
+    int at0 = 0;
+    if (lane == 0 && all) at0 = atomicAdd(&s_todo, __popc(all));
+    at0 = __shfl_sync(0xFFFFFFFFu, at0, 0);
+    if (takes) todo[at0 + __popc(all & below)] = t;
+  }
+  // ---- a copy of the block that holds both kinds
+  if (keep & (KV8_BLOCK - 1)) {
+    uint32_t p;
+    at(keep & ~(KV8_BLOCK - 1), p);
+    uint4* e = reinterpret_cast<uint4*>(a.edge + (size_t)unit * EDGE_BYTES);
+    for (int i = tid; i < 2 * KV8_BLOCK * HD / 16; i += threads)
+      e[i] = reinterpret_cast<const uint4*>((i < KV8_BLOCK * HD / 16 ? a.kc : a.vc) + (size_t)p * HD)[i % (KV8_BLOCK * HD / 16)];
+    if (tid < 2) reinterpret_cast<float*>(e + 2 * KV8_BLOCK * HD / 16)[tid] = (tid ? a.vs : a.ks)[p >> 4];
+  }
+  __syncthreads();
+  if (tid == 0) a.count[unit] = s_todo;
+  copy_tracks(keep, [&](int i) {
+    const int g = i >> 5;
+    const uint32_t gone = ~bits[2 * g] & lows(g);
+    const bool hole = (gone >> (i & 31)) & 1u;
+    const int src = hole ? list[bits[2 * g + 1] + __popc(gone & ((1u << (i & 31)) - 1u))] : -1;
+    from[i] = src;
+    return hole ? src : i;
+  });
+  for (int i = keep + tid; i < a.cap; i += threads) from[i] = -1;
 }
 
-// last = 0: every block but the one that holds index keep; 1: that one.
-__global__ void __launch_bounds__(MV_THREADS) k_move(EvictArgs a, int last, int blocks) {
-  const int lane = threadIdx.x & 31, half = lane >> 4, l16 = lane & 15;
-  const uint32_t group = 0xFFFFu << (lane & 16);
-  const long long item = (long long)blockIdx.x * MV_WARPS + (threadIdx.x >> 5), units = (long long)a.batch * a.Hkv;
-  if (item >= (last ? units : units * blocks)) return;
-  const long long unit = last ? item : item / blocks;
-  const int b = (int)(unit / a.Hkv), h = (int)(unit - (long long)b * a.Hkv);
+__global__ void __launch_bounds__(MV_THREADS, 5) k_move(EvictArgs a) {
+  const int lane = threadIdx.x & 31, l16 = lane & 15, half = (threadIdx.x >> 5) & 1;
+  const int unit = blockIdx.x, n = a.count[unit];
+  const int b = unit / a.Hkv, h = unit - b * a.Hkv;
   const int keep = a.keep[b], L = a.kv_len[b];
-  int t = last ? keep >> 4 : (int)(item - unit * blocks);
-  if (keep < 0 || keep >= L || keep > a.cap || t * KV8_BLOCK >= keep || (t == keep >> 4) != (last != 0)) return;
-  const int base = t * KV8_BLOCK;
   const int32_t* from = a.from + (size_t)unit * a.cap;
-  const int mine = l16 + base < keep ? from[base + l16] : -1;
-  if (!__any_sync(0xFFFFFFFFu, mine >= 0)) return;
+  const int32_t* todo = a.todo + (size_t)unit * ((a.cap + KV8_BLOCK - 1) / KV8_BLOCK);
   const int32_t* tab = a.table + (size_t)b * a.max_pages;
-  auto at = [&](int i) { return ((((size_t)tab[i >> a.shift]) * a.Hkv + h) << a.shift) + (i & ((1 << a.shift) - 1)); };
-  const size_t to = at(base);
+  const unsigned char* edge = a.edge + (size_t)unit * EDGE_BYTES;
+  auto at = [&](int i) { return (((uint32_t)tab[i >> a.shift] * (uint32_t)a.Hkv + (uint32_t)h) << a.shift) | ((uint32_t)i & ((1u << a.shift) - 1u)); };
   uint8_t* codes = half ? a.vc : a.kc;
   float* scales = half ? a.vs : a.ks;
-  const int live = min(KV8_BLOCK, L - base);
-  uint2 w[KV8_BLOCK];
-  const size_t row_at = mine >= 0 ? at(mine) : to + l16;  // lane l16: where row l16 comes from
-  const float row_scale = scales[row_at >> 4];
+  // a block's number and where its rows come from are asked for one block ahead
+  const int step = gridDim.y * (MV_WARPS / 2);
+  auto source = [&](int base) { return l16 + base < keep ? from[base + l16] : -1; };
+  int x = blockIdx.y * (MV_WARPS / 2) + (threadIdx.x >> 6);
+  int base_next = x < n ? todo[x] * KV8_BLOCK : 0, mine_next = x < n ? source(base_next) : -1;
+#pragma unroll 1
+  for (; x < n; x += step) {
+    const int base = base_next, mine = mine_next, live = min(KV8_BLOCK, L - base);
+    if (x + step < n) base_next = todo[x + step] * KV8_BLOCK;
+    const uint32_t to = at(base);
+    // lane l16: where row l16 is, and its scale
+    const bool copied = mine >= 0 && (keep & (KV8_BLOCK - 1)) && mine >> 4 == keep >> 4;
+    const uint32_t row = mine >= 0 && !copied ? at(mine) : to + l16;
+    const float row_scale = copied ? reinterpret_cast<const float*>(edge + 2 * KV8_BLOCK * HD)[half] : scales[row >> 4];
+    const uint32_t moved = __ballot_sync(0xFFFFFFFFu, mine >= 0), copies = __ballot_sync(0xFFFFFFFFu, copied);
+    const uint32_t* at_lane = reinterpret_cast<const uint32_t*>(codes) + lane;
+    uint32_t w[KV8_BLOCK];
 #pragma unroll
-  for (int j = 0; j < KV8_BLOCK; ++j) {
-    const size_t r = __shfl_sync(0xFFFFFFFFu, (unsigned long long)row_at, j);
-    w[j] = j < live ? reinterpret_cast<const uint2*>(codes + r * HD)[l16] : make_uint2(0, 0);
-  }
-  // the largest magnitude, by the bytes' order, times 2^-6 so that none overflows
-  float top = 0.f;
+    for (int j = 0; j < KV8_BLOCK; ++j) w[j] = at_lane[(size_t)__shfl_sync(0xFFFFFFFFu, row, j) * (HD / 4)];
+    if (copies) {
 #pragma unroll
-  for (int j = 0; j < KV8_BLOCK; ++j) {
-    const uint32_t m = __vmaxu4(w[j].x & 0x7F7F7F7Fu, w[j].y & 0x7F7F7F7Fu);
-    const uint32_t m2 = max(max(m & 255u, (m >> 8) & 255u), max((m >> 16) & 255u, m >> 24));
-    const float s = __shfl_sync(group, row_scale, j, 16);
-    top = fmaxf(top, e4m3x2_floats(m2).x * kv8_pow2(min(max(kv8_exp(s), KV8_MIN_EXP), KV8_MAX_EXP) - 6));
-  }
-#pragma unroll
-  for (int o = 1; o < 16; o <<= 1) top = fmaxf(top, __shfl_xor_sync(group, top, o));
-  const bool nan = __any_sync(group, l16 < live && kv8_nan(row_scale));
-  const int e = nan ? 0 : max(kv8_exp_for(top) + 6, KV8_MIN_EXP);
-  __syncwarp();
-#pragma unroll
-  for (int j = 0; j < KV8_BLOCK; ++j) {
-    const float s = __shfl_sync(group, row_scale, j, 16);
-    if (j >= live) continue;
-    const int d = nan ? 0 : kv8_exp(s) - e;
-    if (d != 0) {
-      w[j].x = kv8_rescale4(w[j].x, d);
-      w[j].y = kv8_rescale4(w[j].y, d);
+      for (int j = 0; j < KV8_BLOCK; ++j) {
+        const int k = __shfl_sync(0xFFFFFFFFu, mine, j) & 15;
+        if ((copies >> j) & 1u) w[j] = reinterpret_cast<const uint32_t*>(edge + (half * KV8_BLOCK + k) * HD)[lane];
+      }
     }
-    reinterpret_cast<uint2*>(codes + (to + j) * HD)[l16] = w[j];
+    if (x + step < n) mine_next = source(base_next);
+    // The largest magnitude, in fp16 relative to the largest scale: exact where it counts, as nothing
+    // below 2^-14 of that scale is the largest unless the block calls for a far smaller one.
+    const bool nan = __any_sync(0xFFFFFFFFu, l16 < live && kv8_nan(row_scale));
+    const int row_e = l16 < live ? min(max(kv8_exp(row_scale), KV8_MIN_EXP), KV8_MAX_EXP) : KV8_MIN_EXP;
+    const int ref = __reduce_max_sync(0xFFFFFFFFu, row_e);
+    const uint32_t to_ref = l16 < live ? half2_bits(kv8_half_pow2(row_e - ref)) : 0u;  // (a NaN is no maximum)
+    __half2 top2 = __float2half2_rn(0.f);
+#pragma unroll
+    for (int j = 0; j < KV8_BLOCK; ++j) {
+      const __half2 f = bits_half2(__shfl_sync(0xFFFFFFFFu, to_ref, j));
+      top2 = __hmax2(top2, __hmax2(__habs2(__hmul2(e4m3x2_halves(w[j] & 0xFFFFu), f)), __habs2(__hmul2(e4m3x2_halves(w[j] >> 16), f))));
+    }
+    // magnitudes order like their bits
+    float top = __uint_as_float(__reduce_max_sync(0xFFFFFFFFu, __float_as_uint(fmaxf(__low2float(top2), __high2float(top2)))));
+    int e = max(kv8_exp_for(top) + ref, KV8_MIN_EXP);
+    if (ref - e > 10) {  // from the numbers themselves, times 2^-6 so that none overflows
+      top = 0.f;
+#pragma unroll
+      for (int j = 0; j < KV8_BLOCK; ++j) {
+        const float s = kv8_pow2(__shfl_sync(0xFFFFFFFFu, row_e, j) - 6);
+        const float2 p = e4m3x2_floats(w[j] & 0xFFFFu), q = e4m3x2_floats(w[j] >> 16);
+        if (j < live) top = fmaxf(top, fmaxf(fmaxf(fabsf(p.x), fabsf(p.y)), fmaxf(fabsf(q.x), fabsf(q.y))) * s);
+      }
+      top = __uint_as_float(__reduce_max_sync(0xFFFFFFFFu, __float_as_uint(top)));
+      e = max(kv8_exp_for(top) + 6, KV8_MIN_EXP);
+    }
+    const int d = nan ? 0 : row_e - e;
+    const uint32_t by = half2_bits(kv8_half_pow2(d));
+    const uint32_t put = (moved | __ballot_sync(0xFFFFFFFFu, d != 0)) & ((1u << live) - 1u);  // rows that change
+    const bool large = __any_sync(0xFFFFFFFFu, l16 < live && d > 15);
+    uint32_t* out = reinterpret_cast<uint32_t*>(codes + (size_t)to * HD) + lane;
+#pragma unroll
+    for (int j = 0; j < KV8_BLOCK; ++j) {
+      const __half2 f = bits_half2(__shfl_sync(0xFFFFFFFFu, by, j));
+      uint32_t r = kv8_times4(w[j], f);
+      if (large) r = kv8_rescale4(w[j], __shfl_sync(0xFFFFFFFFu, d, j));
+      if ((put >> j) & 1u) out[j * 32] = r;
+    }
+    if (lane == 0) scales[to >> 4] = nan ? __uint_as_float(0x7FC00000u) : kv8_pow2(e);
   }
-  if (l16 == 0) scales[to >> 4] = nan ? __uint_as_float(0x7FC00000u) : kv8_pow2(e);
 }
+
+size_t up256(size_t n) { return (n + 255) & ~(size_t)255; }
 
 }  // namespace
 
 extern "C" size_t fc_kv8_evict_workspace(int batch, int Hkv, int cap) {
   if (batch < 1 || Hkv < 1 || cap < 0) return 0;
-  return (size_t)batch * Hkv * std::max(cap, 1) * sizeof(int32_t);
+  const size_t units = (size_t)batch * Hkv;
+  return up256(units * 4) + up256(units * ((cap + KV8_BLOCK - 1) / KV8_BLOCK) * 4) + up256(units * EDGE_BYTES) + up256(units * cap * 4);
 }
 
 extern "C" fc_status fc_kv8_evict(const fc_kv8_cache* cache, const int32_t* d_table, int max_pages, const int32_t* d_kv_len,
@@ -271,31 +403,41 @@ extern "C" fc_status fc_kv8_evict(const fc_kv8_cache* cache, const int32_t* d_ta
   if (const fc_status st = fc_kv8_check(cache)) return st;
   const int shift = kv8_page_shift(cache->page_size);
   if (batch < 0 || max_pages < 1 || recent < 0 || cap < 0) return FC_ERR_INVALID_ARG;
-  if (recent > MAX_RECENT || (long long)max_pages << shift > 0x7FFFFFFFll || (long long)batch * cache->Hkv > 1 << 24)
+  if (recent > MAX_RECENT || (long long)max_pages << shift > MAX_KEYS || (long long)batch * cache->Hkv > 1 << 24)
     return FC_ERR_UNSUPPORTED;
   if (batch == 0) return FC_OK;
   if (!d_table || !d_kv_len || !d_keep || !d_weight_in || !d_born_in || !d_weight_out || !d_born_out || (cap && !d_from) ||
       d_weight_in == d_weight_out || d_born_in == d_born_out)
     return FC_ERR_INVALID_ARG;
-  if (!d_ws || !kv8_aligned(d_ws, 4) || ws_bytes < fc_kv8_evict_workspace(batch, cache->Hkv, cap)) return FC_ERR_WORKSPACE;
+  const long long units = (long long)batch * cache->Hkv, longest = (long long)max_pages << shift;
+  if (!d_ws || !kv8_aligned(d_ws, 256) || ws_bytes < fc_kv8_evict_workspace(batch, cache->Hkv, cap)) return FC_ERR_WORKSPACE;
+  unsigned char* ws = static_cast<unsigned char*>(d_ws);
+  auto take = [&](size_t n) {
+    unsigned char* p = ws;
+    ws += up256(n);
+    return p;
+  };
+  const int blocks = (cap + KV8_BLOCK - 1) / KV8_BLOCK;
   EvictArgs a{d_table, d_kv_len, d_keep, max_pages, cache->n_pages, shift, cache->Hkv, batch, cap, recent, d_weight_in, d_born_in,
-              d_weight_out, d_born_out, d_from, static_cast<int32_t*>(d_ws), static_cast<uint8_t*>(cache->k_codes),
-              static_cast<uint8_t*>(cache->v_codes), static_cast<float*>(cache->k_scale), static_cast<float*>(cache->v_scale),
-              fc_error_slot()};
+              d_weight_out, d_born_out, d_from, nullptr, nullptr, nullptr, nullptr,
+              static_cast<uint8_t*>(cache->k_codes), static_cast<uint8_t*>(cache->v_codes), static_cast<float*>(cache->k_scale),
+              static_cast<float*>(cache->v_scale), fc_error_slot()};
+  a.count = reinterpret_cast<int32_t*>(take(units * 4));
+  a.todo = reinterpret_cast<int32_t*>(take(units * blocks * 4));
+  a.edge = take(units * EDGE_BYTES);
+  a.list = reinterpret_cast<int32_t*>(take(units * cap * 4));
   static std::atomic<unsigned long long> done{0};
   const fc_status st = fc_once_per_device(done, [](int) {
-    return fc_cuda_status(cudaFuncSetAttribute(k_select, cudaFuncAttributeMaxDynamicSharedMemorySize, KEYS_SMEM * 4));
+    return fc_cuda_status(cudaFuncSetAttribute(k_select, cudaFuncAttributeMaxDynamicSharedMemorySize, SEL_SMEM));
   });
   if (st != FC_OK) return st;
   cudaStream_t s = static_cast<cudaStream_t>(stream);
-  const long long units = (long long)batch * cache->Hkv, longest = (long long)max_pages << shift;
-  k_select<<<(unsigned)units, SEL_THREADS, (size_t)std::min<long long>(longest, KEYS_SMEM) * 4, s>>>(a);
+  const int held = (int)std::min<long long>((longest + 31) / 32 * 32, KEYS_SMEM), threads = longest <= 8192 ? 512 : SEL_THREADS;
+  k_select<<<(unsigned)units, threads, longest > KEYS_SMEM ? SEL_SMEM : held / 32 * 34 * 4, s>>>(a, held);
   if (cap > 0) {
-    const int blocks = (cap + KV8_BLOCK - 1) / KV8_BLOCK;
-    const long long warps = units * blocks;
-    if ((warps + MV_WARPS - 1) / MV_WARPS > 0x7FFFFFFFll) return FC_ERR_UNSUPPORTED;
-    k_move<<<(unsigned)((warps + MV_WARPS - 1) / MV_WARPS), MV_THREADS, 0, s>>>(a, 0, blocks);
-    k_move<<<(unsigned)((units + MV_WARPS - 1) / MV_WARPS), MV_THREADS, 0, s>>>(a, 1, blocks);
+    // CTAs a unit: enough for every SM's registers, while there are blocks for them
+    const int y = (int)std::max<long long>(1, std::min<long long>((152 * 20 + units - 1) / units, (2 * blocks + MV_WARPS - 1) / MV_WARPS));
+    k_move<<<dim3((unsigned)units, (unsigned)y), MV_THREADS, 0, s>>>(a);
   }
   return FC_CHECK_LAUNCH();
 }
