@@ -74,8 +74,10 @@ constexpr float M_START = -1e30f;  // a reference before any key
 // Exponents below count as this, so that the product of two is no fp32
 // underflow; such scores are 0 to fp32 all the same.
 constexpr int E_MIN = -50;
-// A unit's start and end in blocks of one tile, and the least share worth a CTA.
-constexpr int UNIT_COST = 8, LEAST = 6;
+// A unit's start and end in blocks of one tile: 8 where a unit is cut over CTAs
+// (4 trees of 64 nodes over 300 keys 29 us, with 12 32), 12 where a CTA has several
+// (16 ragged trees of 64 nodes 166 us, with 8 178).  And the least share worth a CTA.
+constexpr int CUT_COST = 8, WHOLE_COST = 12, LEAST = 6;
 
 // Registers a thread by warpgroup (setmaxnreg), of the launch's 96.  The shares must add up to the launch's
 // allocation, or the increase never returns; the host checks the compiled count.
@@ -105,6 +107,7 @@ struct ManyArgs {
   Kv8Args a;
   int chunks;      // most units a (sequence, kv head)
   int split;       // 0: whole units, CTA by CTA
+  int unit_cost;   // CUT_COST or WHOLE_COST
   int rows_cap;    // rows a piece's slot has room for
   int* list;       // [grid][8] cut units for k_kv8_join
   float* part_o;   // [grid][2][rows_cap][HD]
@@ -300,7 +303,7 @@ struct Walk {
     r.w = r.rows_each > BM ? 2 : 1;
     return r;
   }
-  __device__ __forceinline__ int unit_cost(const Req& r) const { return UNIT_COST + r.blocks * r.w; }
+  __device__ __forceinline__ int unit_cost(const Req& r) const { return f.unit_cost + r.blocks * r.w; }
 
   // every lane of a warp calls this
   __device__ __forceinline__ Walk(const ManyArgs& args) : f(args), cut(1, 1, 1) {
@@ -363,7 +366,7 @@ struct Walk {
         chunk = u - gh * r.n_chunks;
         unit_base = base + u * cost;
         // a block belongs to the share that holds its first cost
-        const int from = max(0, cur - unit_base - UNIT_COST), to = min(cost, end - unit_base) - UNIT_COST;
+        const int from = max(0, cur - unit_base - f.unit_cost), to = min(cost, end - unit_base) - f.unit_cost;
         s0 = (from + r.w - 1) / r.w;
         s1 = to <= 0 ? 0 : (to + r.w - 1) / r.w;
         cur = min(unit_base + cost, end);
@@ -388,9 +391,9 @@ struct Walk {
     }
   }
   __device__ __forceinline__ bool whole() const { return s0 == 0 && s1 == blocks; }
-  __device__ __forceinline__ int first_cta() const { return cut.share_of(unit_base + UNIT_COST); }
+  __device__ __forceinline__ int first_cta() const { return cut.share_of(unit_base + f.unit_cost); }
   __device__ __forceinline__ int last_cta() const {
-    return cut.share_of(unit_base + UNIT_COST + (blocks - 1) * (two ? 2 : 1));
+    return cut.share_of(unit_base + f.unit_cost + (blocks - 1) * (two ? 2 : 1));
   }
   __device__ __forceinline__ int slot(int c) const { return 2 * c + (cut.start(c) < unit_base ? 1 : 0); }
 };
@@ -436,7 +439,7 @@ __global__ void __launch_bounds__(THREADS, 1) k_kv8_attn_many(const __grid_const
     // e4m3 operands: format 0 where bf16 is 1 (bits 7..9, 10..12)
     constexpr uint32_t BF16 = (1u << 7) | (1u << 10);
     constexpr uint32_t IDESC_QK = idesc_bf16_f32(BM, BN, 0) & ~BF16, IDESC_PV = idesc_bf16_f32(BM, HD, 1);
-    uint32_t nb = 0, np = 0, t_of[2] = {0, 0};  // blocks, pieces, steps of each tile so far
+    uint32_t nb = 0, np = 0, t0 = 0, t1 = 0;  // blocks, pieces, steps of each tile so far
     bool ok = true;
     // descriptors' low words: a byte offset adds to them in units of 16
     const uint32_t q_lo = (uint32_t)smem_desc_sw128(sQ, 16, 1024), k_lo = (uint32_t)smem_desc_sw128(sK, 16, 1024);
@@ -466,8 +469,8 @@ __global__ void __launch_bounds__(THREADS, 1) k_kv8_attn_many(const __grid_const
         if (k >= 0) {  // O_x (+)= P_x V
           const uint32_t blk = nb + (k >> two), st = blk & 1;
           if (!(two & x) && !wait(B_VFULL + st, blk >> 1)) break;  // tile 1: waited for by tile 0
-          if (!wait(B_PFULL + x, t_of[x])) break;
-          ++t_of[x];
+          if (!wait(B_PFULL + x, x ? t1 : t0)) break;
+          t0 += 1 - x, t1 += x;
           if (k == 0 && np > 0 && !wait(B_OFREE, np - 1)) break;
           tc_fence_after();
           mma_pv(tmem + 256 + x * 128, tmem + x * 128, v_lo + st * (TILE_BYTES >> 4), IDESC_PV, k >= 2);
@@ -1079,13 +1082,14 @@ fc_status kv8_attn_many(const Kv8Args& a, void* ws, size_t ws_bytes, cudaStream_
     return fc_cuda_status(cudaFuncSetAttribute(k_kv8_attn_many, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM_BYTES));
   });
   if (st != FC_OK) return st;
-  ManyArgs f{a, 0, 1, rows_of_chunk(a.n_pad, a.G), nullptr, nullptr, nullptr};
+  ManyArgs f{a, 0, 1, CUT_COST, rows_of_chunk(a.n_pad, a.G), nullptr, nullptr, nullptr};
   f.chunks = (a.n_pad * a.G + ROWS - 1) / ROWS;
   const long long units = (long long)a.B * a.Hkv * f.chunks;
   if (units > 0x7FFFFFFFll) return FC_ERR_UNSUPPORTED;
+  if (units > 2 * FULL_GRID) f.unit_cost = WHOLE_COST;
   const long long longest = (((long long)a.max_pages << a.shift) + BN - 1) / BN + 1;
-  const bool fits = units * (UNIT_COST + 2 * longest) <= 0x7FFFFFFFll;
-  int grid = (int)std::min<long long>(FULL_GRID, units * ((UNIT_COST + 2 * longest) / LEAST));
+  const bool fits = units * (WHOLE_COST + 2 * longest) <= 0x7FFFFFFFll;
+  int grid = (int)std::min<long long>(FULL_GRID, units * ((CUT_COST + 2 * longest) / LEAST));
   auto need = [&] { return KV8_WS_COUNTERS + list_bytes(grid) + (size_t)grid * 2 * slot_bytes(f.rows_cap); };
   while (grid > 1 && ws && need() > ws_bytes) --grid;
   // a workspace for fewer CTAs than whole units would fill: whole units
