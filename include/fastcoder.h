@@ -833,7 +833,7 @@ typedef struct {
  * pass: for a head's row x of D values
  *   y = x / sqrt(mean(x^2) + eps) * w,   then (y_i, y_{i + D/2}) turned by
  *   pos * base^(-2i/D)   (fc_rope's pairing; a negative position: not turned),
- * fp32 inside, rounded once to bf16.
+ * fp32 inside (the squares' sum too), rounded once to bf16.
  *   d_q  row (b, i, h) at element b * q_seq_stride + i * q_row_stride + h *
  *        q_head_stride, so that parts of a projection's rows are read where
  *        they are; d_k and d_v likewise with the kv strides.  d_v may be NULL.
@@ -884,11 +884,22 @@ fc_status fc_kv8_read(const fc_kv8_cache* cache, const int32_t* d_slot, int rows
  *             is there.  For up to 16 rows a kv head (n_pad * H / Hkv, else
  *             FC_ERR_UNSUPPORTED), batch * Hkv <= 65535, with a workspace made
  *             for weight_keys = max_pages * page_size (else FC_ERR_WORKSPACE).
- * Sums and the softmax are fp32, products of cached numbers with queries exact;
- * probabilities are rounded to 16 bits for the second product.
+ * Sums, scales and the softmax are fp32.  What the tensor cores multiply is
+ * rounded so:
+ *   up to 16 rows a kv head: cached numbers exact; queries fp16 relative to the
+ *     largest of the request's rows of that kv head, exact down to 2^-27 of it;
+ *     probabilities times value scales fp16 relative to the row's largest, 11
+ *     bits down to 2^-25 of it;
+ *   more: cached numbers exact; queries, and new keys by 16, exact down to 2^-10
+ *     of the row's largest, to 2^-18 of it below; probabilities bf16.
+ * Scales and new values may lie anywhere between 2^-80 and 2^100 (or be 0), side
+ * by side; scores, scale * q k, of up to 2^24 in magnitude.
  * What a block holds past a request's end, and a scale of a block that begins
  * there, is not looked at.  A block that stands for NaN makes the rows of its
- * request and head NaN; new tokens and queries as in fc_kv4_attn.
+ * request and head NaN.  A new token with a NaN or an infinity in its key or its
+ * value makes NaN of the rows that see it, and of no others (up to 16 rows: an
+ * infinity in a key has no weight where its product with the query is
+ * -infinity).  A query with a NaN makes its own row NaN.
  */
 fc_status fc_kv8_attn(const void* d_q, const fc_kv8_cache* cache, const int32_t* d_table, int max_pages,
                       const int32_t* d_kv_len, const void* d_k_new, const void* d_v_new, const uint64_t* d_mask,

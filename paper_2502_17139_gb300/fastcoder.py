@@ -1074,7 +1074,7 @@ def fc_w4_matvec(x, w: W4Weight, out=None):
 # ------------------------------- serving from a cache in eight bits, kept to a budget
 def _rows_strides(x):
     """(b, i, h) strides of x [B, n, heads, D], 0 for a dimension of one."""
-    return [0 if m == 1 else s for m, s in zip(x.shape[:3], x.stride())]
+    return [0 if m == 1 else s for m, s in zip(x.shape[:3], x.stride())] if x.dim() == 4 else [0, 0, 0]
 
 
 def fc_qk_norm_rope(q, k, v, wq, wk, pos, base=10000.0, eps=1e-6, out=None):
@@ -1084,11 +1084,15 @@ def fc_qk_norm_rope(q, k, v, wq, wk, pos, base=10000.0, eps=1e-6, out=None):
     the same ones): parts of a projection's rows.  Returns q [B, n, H, D], k and
     v [B, Hkv, n, D] (``out``: these three)."""
     bf = torch.bfloat16
+    if not (isinstance(q, torch.Tensor) and isinstance(k, torch.Tensor)):
+        raise TypeError("q and k must be tensors")
     B, n, H, D = q.shape if q.dim() == 4 else (0, 0, 0, 0)
     qs, ks, kshape = q.stride(), k.stride(), k.shape
-    if not (q.dtype is bf and k.dtype is bf and q.is_cuda and k.is_cuda and len(kshape) == 4 and D > 1 and qs[3] == 1 and ks[3] == 1 and
+    if not (B > 1 and n > 1 and H > 1 and kshape[-2] > 1):  # a dimension of one has no stride that matters
+        qs, ks = _rows_strides(q), _rows_strides(k)
+    if not (q.dtype is bf and k.dtype is bf and q.is_cuda and k.is_cuda and len(kshape) == 4 and q.stride(3) == 1 and k.stride(3) == 1 and
             kshape[0] == B and kshape[1] == n and kshape[3] == D and
-            (v is None or (v.dtype is bf and v.is_cuda and v.shape == kshape and v.stride() == ks))):  # one test for the usual case
+            (v is None or (v.dtype is bf and v.is_cuda and v.shape == kshape and v.stride() == k.stride()))):  # one test for the usual case
         for t, name in ((q, "q"), (k, "k")) + (((v, "v"),) if v is not None else ()):
             if not isinstance(t, torch.Tensor) or t.dtype is not bf:
                 raise TypeError(f"{name} must be a torch.bfloat16 tensor")

@@ -1,16 +1,19 @@
 """Decoding in four bits: a LLaMA-family decoder whose weights are held in 4
-bits (fc_w4_pack) and whose KV cache is paged and held in 4 bits (Kv4Cache),
-for the few rows of a decoding step: single tokens of up to 16 sequences, or
-one small draft tree (batch * nodes <= 16).
+bits (fc_w4_pack) and whose KV cache is paged and held in 4 bits (Kv4Cache) or
+in 8 (Kv8Cache), for the few rows of a decoding step: single tokens of up to 16
+sequences, or one small draft tree (batch * nodes <= 16).  Weights with
+``q_norm`` and ``k_norm`` in a layer norm the queries and keys of each head.
 
 A step: forward() runs the rows against the caches, with the new tokens' own
 keys and values in bf16; append() plans where the kept ones go
 (fc_kv_pages_plan, once) and quantises them into every layer's pages
 (fc_kv4_write).  All on the current stream, no host round trip.  Both read and
 write the same tensors at every step, so that a step captured in a CUDA graph
-is good for all of them.
+is good for all of them.  A cache in 8 bits can be kept to a budget (``keep``):
+forward() adds up the weight that each cached token received, and evict() cuts
+every sequence down to the tokens that received most (fc_kv8_evict).
 
-    python -m paper_2502_17139_gb300.q4decoder [batch] [context]
+    python -m paper_2502_17139_gb300.q4decoder [batch] [context] [cache bits]
 
 times single-token steps of the 1.3B shape with random weights.
 """
@@ -28,12 +31,19 @@ class Q4Decoder:
     """W: bf16 weights in synth.decoder_weights' layout, quantised here (one
     scale for ``group`` weights).  ``nodes`` new tokens a sequence and step.
     The pool has ``n_pages`` pages of ``page_size`` tokens; a sequence holds at
-    most ``max_pages``."""
+    most ``max_pages``.  ``cache_bits`` 4 or 8; with 8, ``keep`` > 0: evict()
+    leaves a sequence that many tokens, the last ``recent`` positions' among them."""
 
     def __init__(self, shape: DecoderShape, W, batch, n_pages, max_pages, nodes=1, page_size=64, group=128,
-                 device="cuda"):
+                 device="cuda", cache_bits=4, keep=0, recent=0):
         if batch * nodes > MAX_ROWS:
             raise ValueError(f"a step has at most {MAX_ROWS} rows")
+        if cache_bits not in (4, 8):
+            raise ValueError("cache_bits must be 4 or 8")
+        if keep < 0 or recent < 0 or (keep and cache_bits == 4):
+            raise ValueError("keep and recent count tokens of a cache in 8 bits")
+        if keep and nodes * (shape.H // shape.Hkv) > 16:
+            raise ValueError("weights need at most 16 rows a kv head")
         s = shape
         self.s, self.B, self.n = s, batch, nodes
         pack = lambda w: fc.fc_w4_pack(w.contiguous(), group)
@@ -43,7 +53,9 @@ class Q4Decoder:
         i32 = dict(dtype=torch.int32, device=device)
         self.pages = fc.KvPages(page_size, torch.zeros((batch, max_pages), **i32),
                                 torch.arange(n_pages - 1, -1, -1, **i32))
-        self.caches = [fc.Kv4Cache.empty(n_pages, s.Hkv, page_size, s.D, device) for _ in range(s.layers)]
+        self.bits, self.keep, self.recent = cache_bits, keep, recent
+        kind = fc.Kv4Cache if cache_bits == 4 else fc.Kv8Cache
+        self.caches = [kind.empty(n_pages, s.Hkv, page_size, s.D, device) for _ in range(s.layers)]
         # lengths and the free count: the current ones, and a plan's results, which
         # are copied back (a plan's outputs are not its inputs)
         self.state = torch.zeros((2, batch + 1), **i32)
@@ -59,7 +71,21 @@ class Q4Decoder:
         self.gu, self.act, self.logits = bf(R, 2 * s.inter), bf(R, s.inter), bf(R, s.vocab)
         self.k_new = [bf(batch, s.Hkv, nodes, s.D) for _ in range(s.layers)]
         self.v_new = [bf(batch, s.Hkv, nodes, s.D) for _ in range(s.layers)]
-        self.ws = fc.kv4_attn_workspace(batch, nodes, s.H, s.Hkv, device)
+        if cache_bits == 4:
+            self.ws = fc.kv4_attn_workspace(batch, nodes, s.H, s.Hkv, device)
+        else:
+            self.ws = fc.kv8_attn_workspace(batch, nodes, s.H, s.Hkv, device, max_pages * page_size if keep else 0)
+        if "q_norm" in W["layers"][0]:
+            self.q_raw = bf(batch, nodes, s.H, s.D)
+            for mine, w in zip(self.layers, W["layers"]):
+                mine.update(q_norm=w["q_norm"], k_norm=w["k_norm"])
+        # how far a sequence's positions are ahead of its cached tokens
+        self.ahead = torch.zeros(batch, **i32)
+        if keep:
+            self.tracks = [[fc.Kv8Track.empty(c), fc.Kv8Track.empty(c)] for c in self.caches]
+            self.keeps = torch.full((batch,), keep, **i32)
+            self.from_ = torch.empty((batch, s.Hkv, keep), **i32)
+            self.evict_ws = fc.kv8_evict_workspace(batch, s.Hkv, keep, device)
         self.steps = torch.arange(nodes, **i32)[None, :]
         self.ones = torch.full((batch,), nodes, **i32)
 
@@ -69,19 +95,29 @@ class Q4Decoder:
         (None: each sees those before it), n_nodes [B]."""
         s, B, n, kv_len = self.s, self.B, self.n, self.kv_len[0]
         if pos is None:
-            pos = kv_len[:, None] + self.steps
+            pos = (kv_len + self.ahead if self.keep else kv_len)[:, None] + self.steps
         fc.fc_embed(tok.reshape(-1), self.embed, self.x)
         r = None
         for l, w in enumerate(self.layers):
             fc.fc_add_rmsnorm(self.x, r, w["attn_norm"], self.h, s.eps)
-            fc.fc_w4_matvec(self.h, w["wq"], out=self.q.view(B * n, -1))
-            fc.fc_rope(self.q, pos, s.rope_base, out=self.q)
+            normed = "q_norm" in w
+            fc.fc_w4_matvec(self.h, w["wq"], out=(self.q_raw if normed else self.q).view(B * n, -1))
             fc.fc_w4_matvec(self.h, w["wkv"], out=self.kv)
-            stride = 2 * s.Hkv * s.D
-            fc.fc_rope_heads(self.kv, 0, stride, self.k_new[l], B, n, s.Hkv, s.D, pos, s.rope_base)
-            fc.fc_rope_heads(self.kv, s.Hkv * s.D, stride, self.v_new[l], B, n, s.Hkv, s.D, pos, 0.0)
-            fc.fc_kv4_attn(self.q, self.caches[l], self.pages.table, kv_len, self.k_new[l], self.v_new[l], mask, n_nodes,
-                           out=self.attn, workspace=self.ws)
+            if normed:
+                kv = self.kv.view(B, n, 2, s.Hkv, s.D)
+                fc.fc_qk_norm_rope(self.q_raw, kv[:, :, 0], kv[:, :, 1], w["q_norm"], w["k_norm"], pos, s.rope_base, s.eps,
+                                   out=(self.q, self.k_new[l], self.v_new[l]))
+            else:
+                fc.fc_rope(self.q, pos, s.rope_base, out=self.q)
+                stride = 2 * s.Hkv * s.D
+                fc.fc_rope_heads(self.kv, 0, stride, self.k_new[l], B, n, s.Hkv, s.D, pos, s.rope_base)
+                fc.fc_rope_heads(self.kv, s.Hkv * s.D, stride, self.v_new[l], B, n, s.Hkv, s.D, pos, 0.0)
+            if self.bits == 4:
+                fc.fc_kv4_attn(self.q, self.caches[l], self.pages.table, kv_len, self.k_new[l], self.v_new[l], mask, n_nodes,
+                               out=self.attn, workspace=self.ws)
+            else:
+                fc.fc_kv8_attn(self.q, self.caches[l], self.pages.table, kv_len, self.k_new[l], self.v_new[l], mask, n_nodes,
+                               out=self.attn, workspace=self.ws, weight=self.tracks[l][0].weight if self.keep else None)
             fc.fc_w4_matvec(self.attn.view(B * n, -1), w["wo"], out=self.o)
             fc.fc_add_rmsnorm(self.x, self.o, w["mlp_norm"], self.h, s.eps)
             fc.fc_w4_matvec(self.h, w["wgu"], out=self.gu)
@@ -101,14 +137,42 @@ class Q4Decoder:
         fc.fc_kv_pages_plan(self.pages, self.kv_len[0], self.ones if n_keep is None else n_keep, self.n_free[0], path=path,
                             n_per_seq=self.n, out=out)
         self.state[0].copy_(self.state[1])
-        for cache, k, v in zip(self.caches, self.k_new, self.v_new):
-            fc.fc_kv4_write(cache, k.transpose(1, 2), v.transpose(1, 2), out["slot"], src=out["src"])
+        born = None
+        if self.keep:  # the rows' positions; out["pos"] are their places
+            born = out["pos"] + self.ahead[out["seq"].clamp(min=0).long()]
+        for l, (cache, k, v) in enumerate(zip(self.caches, self.k_new, self.v_new)):
+            if self.bits == 4:
+                fc.fc_kv4_write(cache, k.transpose(1, 2), v.transpose(1, 2), out["slot"], src=out["src"])
+            else:
+                fc.fc_kv8_write(cache, k.transpose(1, 2), v.transpose(1, 2), out["slot"], src=out["src"],
+                                track=self.tracks[l][0] if self.keep else None, pos=born)
+
+    def evict(self):
+        """Cuts every sequence down to ``keep`` tokens, each layer and kv head
+        choosing its own: those of the last ``recent`` positions, then those that
+        received the largest attention weights.  Emptied pages are free again;
+        positions go on.  For use between steps: a step captured in a CUDA graph
+        stays good, as everything stays where it is."""
+        if not self.keep:
+            raise ValueError("a budget of tokens (keep) was not given")
+        for l, cache in enumerate(self.caches):
+            now, then = self.tracks[l]
+            fc.fc_kv8_evict(cache, self.pages.table, self.kv_len[0], self.keeps, self.recent, now, then, out=self.from_,
+                            workspace=self.evict_ws)
+            now.weight.copy_(then.weight)
+            now.born.copy_(then.born)
+        had = self.kv_len[0].clone()
+        self.release(self.keeps)
+        self.ahead += had - self.kv_len[0]
 
     def release(self, keep):
-        """Sequence b keeps its first keep[b] tokens (0: it is finished); its
-        other pages are free again."""
+        """Sequence b keeps its first keep[b] tokens (0: it is finished; one that
+        takes its place starts at position 0); its other pages are free again.
+        After evict() its tokens are in no order."""
         fc.fc_kv_pages_release(self.pages, self.kv_len[0], keep, self.n_free[0], out=(self.kv_len[1], self.n_free[1]))
         self.state[0].copy_(self.state[1])
+        if self.keep:
+            self.ahead.mul_(self.kv_len[0] > 0)
 
     def generate(self, tok, steps):
         """Greedy decoding of ``steps`` tokens from tok [B] (nodes = 1): [B, steps].
@@ -127,13 +191,13 @@ class Q4Decoder:
         return torch.stack(out, 1)
 
 
-def main(batch=1, context=4096, steps=20):
+def main(batch=1, context=4096, cache_bits=4, steps=20):
     from . import synth
     from .decoder import DEEPSEEK_CODER_1_3B as shape
     s = shape
     W = synth.decoder_weights(s.hidden, s.layers, s.H, s.Hkv, s.D, s.inter, s.vocab, 7, device="cuda")
     held, most = -(-context // 64), -(-(context + 2 * steps + 4) // 64)
-    dec = Q4Decoder(s, W, batch, batch * most, most)
+    dec = Q4Decoder(s, W, batch, batch * most, most, cache_bits=cache_bits)
     # a context of random numbers, as if it had been decoded: the pages at the pool's end
     order = torch.arange(batch * most - 1, -1, -1, dtype=torch.int32, device="cuda")
     dec.pages.table[:, :held] = order[:batch * held].view(batch, held)
@@ -141,10 +205,10 @@ def main(batch=1, context=4096, steps=20):
     dec.n_free[dec.cur].fill_(batch * (most - held))
     dec.pages.free.copy_(torch.arange(batch * most, dtype=torch.int32))
     for c in dec.caches:
-        c.k_codes.random_(0x11, 0xFF)
-        c.v_codes.random_(0x11, 0xFF)
-        c.k_scale.fill_(0.1)
-        c.v_scale.fill_(0.1)
+        c.k_codes.random_(0x11, 0xFF if cache_bits == 4 else 0x7F)
+        c.v_codes.random_(0x11, 0xFF if cache_bits == 4 else 0x7F)
+        c.k_scale.fill_(0.1 if cache_bits == 4 else 2.0 ** -9)
+        c.v_scale.fill_(0.1 if cache_bits == 4 else 2.0 ** -9)
     tok = torch.zeros((batch, 1), dtype=torch.int32, device="cuda")
 
     def step():
@@ -166,7 +230,7 @@ def main(batch=1, context=4096, steps=20):
     assert fc.fc_get_error() == "FC_OK"
     assert dec.kv_len[dec.cur].tolist() == [context + 3 + steps] * batch
     ms = a.elapsed_time(b) / steps
-    print(f"batch {batch}, context {context}: {ms:.3f} ms a step, {batch / ms * 1e3:.0f} tokens/s (forward and append, from a graph)")
+    print(f"batch {batch}, context {context}, cache in {cache_bits} bits: {ms:.3f} ms a step, {batch / ms * 1e3:.0f} tokens/s (forward and append, from a graph)")
 
 
 if __name__ == "__main__":

@@ -81,6 +81,19 @@ def test_norm_rope(fc, B, n, H, Hkv, dim):
     assert two[2] is None and torch.equal(two[0], out[0]) and torch.equal(two[1], out[1])
 
 
+def test_norm_rope_dimensions_of_one(fc):
+    """One row, one head: their strides are not looked at."""
+    rng = np.random.default_rng(4)
+    x = bf(rng, 3, 64).cuda()
+    odd = lambda r: torch.as_strided(x, (1, 1, 1, 64), (7, 3, 5, 1), 64 * r)
+    w, pos = bf(rng, 64).cuda(), torch.full((1, 1), 9, dtype=torch.int32).cuda()
+    out = fc.fc_qk_norm_rope(odd(0), odd(1), odd(2), w, w, pos)
+    ref = fc.fc_qk_norm_rope(*(x[r].view(1, 1, 1, 64) for r in range(3)), w, w, pos)
+    assert all(torch.equal(a, b) for a, b in zip(out, ref))
+    got = fc.fc_qk_norm_rope(*(x[:0].view(0, 1, 1, 64) for _ in range(3)), w, w, pos[:0])
+    assert got[0].shape == (0, 1, 1, 64)
+
+
 def test_norm_rope_rows_that_are_not_finite_stay_alone(fc):
     rng = np.random.default_rng(3)
     q, k = bf(rng, 2, 4, 8, D).cuda(), bf(rng, 2, 4, 2, D).cuda()
@@ -404,6 +417,84 @@ def test_attention_many_small_weights_beside_a_large_one(fc, n, H, Hkv):
     got = call(fc, s, scale=0.6, workspace=fc.kv8_attn_workspace(1, n, H, Hkv, "cuda"))
     ref, tol, _, _ = reference(s, None, 0.6, causal=True)
     assert np.all(np.abs(num(got) - ref) <= tol)
+
+
+@pytest.mark.parametrize("n,H,Hkv", [(1, 8, 2), (64, 4, 2)])
+def test_scores_that_grow_and_fall_along_the_cache(fc, n, H, Hkv):
+    """Keys whose scores rise by 30 (base 2) a hundred tokens, then fall: the
+    reference of a row moves many times, within blocks too."""
+    rng = np.random.default_rng(13)
+    L = 1500
+    s = setup(rng, [L], n, H, Hkv, 64, stale=False)
+    s["q"][:] = 0
+    s["q"][..., 0] = 1
+    s["q"][:, :, 1::2, 0] = -1  # every second head the other way round
+    up = np.concatenate((np.linspace(-200, 200, 1000), np.linspace(200, 0, L - 1000)))
+    i = np.arange(L)
+    s["cache"][0][:] = 0
+    s["cache"][2][:] = 2.0 ** 0
+    s["cache"][0][s["table"][0][i // 64], :, i % 64, 0] = o8.encode(up)[:, None]
+    got = call(fc, s, scale=1.0, workspace=fc.kv8_attn_workspace(1, n, H, Hkv, "cuda"))
+    ref, tol, _, _ = reference(s, None, 1.0, causal=True)
+    assert np.all(np.abs(num(got) - ref) <= tol)
+    got = call(fc, s, scale=1.0)
+    assert np.all(np.abs(num(got) - ref) <= tol)
+
+
+@pytest.mark.parametrize("n,H,Hkv", [(1, 8, 2), (64, 4, 2)])
+def test_a_captured_call_is_good_for_other_lengths(fc, n, H, Hkv):
+    """A graph of write and attention, replayed after lengths, tables and rows changed."""
+    rng = np.random.default_rng(14)
+    s = setup(rng, [200, 90], n, H, Hkv, 32, stale=False)
+    cache = on_gpu(fc, s["cache"])
+    table, kv, q, k, v = dev(s["table"]), dev(s["kv"]), s["q"].cuda(), s["k"].cuda(), s["v"].cuda()
+    ws, out = fc.kv8_attn_workspace(2, n, H, Hkv, "cuda"), torch.empty_like(q)
+    slot = torch.full((2,), -1, dtype=torch.int32).cuda()
+    rows = [torch.zeros(2, Hkv, D, dtype=torch.bfloat16).cuda() for _ in range(2)]
+
+    def step():
+        fc.fc_kv8_write(cache, rows[0], rows[1], slot)
+        fc.fc_kv8_attn(q, cache, table, kv, k, v, out=out, workspace=ws)
+
+    step()
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()  # captured on another stream than the tensors'
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        step()
+    for kv_new in ([37, 90], [0, 1], [199, 64]):
+        s["kv"] = np.array(kv_new, np.int32)
+        x = [bf(rng, 2, Hkv, D) for _ in range(2)]
+        at = np.array([s["table"][b][L // 32] * 32 + L % 32 for b, L in enumerate(kv_new)], np.int32)
+        for d, h in zip(rows + [slot, kv], x + [torch.from_numpy(at), torch.from_numpy(s["kv"] + 1)]):
+            d.copy_(h)
+        graph.replay()
+        o8.write(s["cache"], num(x[0]), num(x[1]), at)
+        s["kv"] = s["kv"] + 1
+        ref, tol, _, _ = reference(s, None, D ** -0.5, causal=True)
+        assert np.all(np.abs(num(out) - ref) <= tol)
+    assert fc.fc_get_error() == "FC_OK"
+
+
+def test_attention_on_two_streams_at_once(fc):
+    """Two calls that overlap, with a workspace each."""
+    rng = np.random.default_rng(15)
+    for n, H, Hkv in ((1, 16, 4), (48, 8, 4)):
+        s = setup(rng, [3000, 700], n, H, Hkv, 64)
+        ref, tol, _, _ = reference(s, None, D ** -0.5, causal=True)
+        cache, table, kv = on_gpu(fc, s["cache"]), dev(s["table"]), dev(s["kv"])
+        q, k, v = s["q"].cuda(), s["k"].cuda(), s["v"].cuda()
+        streams = [torch.cuda.Stream() for _ in range(2)]
+        ws = [fc.kv8_attn_workspace(2, n, H, Hkv, "cuda") for _ in range(2)]
+        outs = [torch.empty_like(q) for _ in range(2)]
+        torch.cuda.synchronize()
+        for _ in range(5):
+            for st, w, o in zip(streams, ws, outs):
+                with torch.cuda.stream(st):
+                    fc.fc_kv8_attn(q, cache, table, kv, k, v, out=o, workspace=w)
+        torch.cuda.synchronize()
+        for o in outs:
+            assert np.all(np.abs(num(o) - ref) <= tol)
 
 
 @pytest.mark.parametrize("n,H,Hkv", [(1, 8, 2), (3, 4, 1), (64, 4, 2)])
