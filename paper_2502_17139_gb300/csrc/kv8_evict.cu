@@ -81,6 +81,233 @@ __device__ __forceinline__ uint32_t block_scan(uint32_t v, uint32_t* s_sum) {
 __device__ __forceinline__ uint32_t half2_bits(__half2 v) { return *reinterpret_cast<uint32_t*>(&v); }
 __device__ __forceinline__ __half2 bits_half2(uint32_t v) { return *reinterpret_cast<__half2*>(&v); }
 
+// A copy of the block that holds both places below keep and sources, by the block's threads.
+__device__ __forceinline__ void copy_edge(const EvictArgs& a, int unit, int h, int keep, const int32_t* tab, int threads) {
+  if (!(keep & (KV8_BLOCK - 1))) return;
+  const int first = keep & ~(KV8_BLOCK - 1);
+  const size_t p = ((((size_t)tab[first >> a.shift]) * a.Hkv + h) << a.shift) + (first & ((1 << a.shift) - 1));
+  uint4* e = reinterpret_cast<uint4*>(a.edge + (size_t)unit * EDGE_BYTES);
+  constexpr int N = KV8_BLOCK * HD / 16;
+  for (int i = threadIdx.x; i < 2 * N; i += threads) e[i] = reinterpret_cast<const uint4*>((i < N ? a.kc : a.vc) + p * HD)[i % N];
+  if (threadIdx.x < 2) reinterpret_cast<float*>(e + 2 * N)[threadIdx.x] = (threadIdx.x ? a.vs : a.ks)[p >> 4];
+}
+
+constexpr int HELD = 16;  // tokens a thread of k_select_held
+
+// k_select for requests of up to HELD * THREADS tokens, whose weights and
+// positions stay in registers from the first read on: only sources pass through
+// shared memory.  (32 requests of 8 heads and 4160 tokens: 25 us with keys in
+// shared memory and passes over them, most of it instructions.)
+template <int THREADS>
+__global__ void __launch_bounds__(THREADS, 1024 / THREADS) k_select_held(EvictArgs a) {
+  constexpr int WARPS = THREADS / 32, GROUPS = HELD * WARPS, MOST = HELD * THREADS / 2;  // moves are at most half
+  extern __shared__ uint32_t s_dyn[];
+  int* s_src = reinterpret_cast<int*>(s_dyn);  // [MOST] sources: index, weight, position
+  float* s_w = reinterpret_cast<float*>(s_dyn + MOST);
+  int* s_b = reinterpret_cast<int*>(s_dyn + 2 * MOST);
+  __shared__ __align__(16) uint32_t s_hist[BINS];
+  __shared__ uint32_t s_sum[32], s_bits[GROUPS], s_tie[GROUPS], s_rank[GROUPS];
+  __shared__ int s_bad, s_newest, s_todo;
+  __shared__ uint32_t s_digit, s_left, s_in_bin;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int unit = blockIdx.x, b = unit / a.Hkv, h = unit - b * a.Hkv;
+  const int L = a.kv_len[b], keep = a.keep[b];
+  const int32_t* tab = a.table + (size_t)b * a.max_pages;
+  int32_t* from = a.from + (size_t)unit * a.cap;
+  const bool wrong = L < 0 || keep < 0 || L > (long long)a.max_pages << a.shift;
+  const bool full = !wrong && keep < L && keep > a.cap;
+  if (tid == 0) s_bad = 0, s_newest = INT_MIN, s_todo = 0;
+  for (int i = tid; i < BINS; i += THREADS) s_hist[i] = 0;
+  __syncthreads();
+  auto at = [&](int i, uint32_t& p) {
+    const uint32_t page = (uint32_t)__ldg(tab + (i >> a.shift));
+    p = ((page * (uint32_t)a.Hkv + (uint32_t)h) << a.shift) | ((uint32_t)i & ((1u << a.shift) - 1u));
+    return page < (uint32_t)a.n_pages;
+  };
+  const bool fine = !wrong && !full;
+  float w[HELD];
+  int born[HELD];
+  {
+    bool bad = false;
+    int newest = INT_MIN;
+#pragma unroll
+    for (int u = 0; u < HELD; ++u) {
+      const int i = u * THREADS + tid;
+      w[u] = 0.f;
+      born[u] = INT_MIN;
+      uint32_t p;
+      if (fine && i < L) {
+        if (at(i, p)) {
+          w[u] = __ldg(a.w_in + p);
+          born[u] = __ldg(a.b_in + p);
+        } else {
+          bad = true;
+        }
+      }
+    }
+#pragma unroll
+    for (int u = 0; u < HELD; ++u) newest = max(newest, born[u]);
+    newest = __reduce_max_sync(0xFFFFFFFFu, newest);
+    if (lane == 0 && a.recent > 0) atomicMax(&s_newest, newest);
+    if (bad) s_bad = 1;
+  }
+  __syncthreads();
+  if (!fine || s_bad) {  // left as it is
+    if (tid == 0) {
+      a.count[unit] = 0;
+      if (h == 0) fc_flag(FC_ERR_WORD(a.err), full ? FC_EBIT_CAPACITY : FC_EBIT_INVALID);
+    }
+    for (int i = tid; i < a.cap; i += THREADS) from[i] = -1;
+    return;
+  }
+  const bool lose = keep < L;
+  const int kept = min(keep, L);
+  uint32_t below = (1u << lane) - 1u;
+  auto lows = [&](int g) { return kept <= 32 * g ? 0u : kept - 32 * g >= 32 ? 0xFFFFFFFFu : (1u << (kept - 32 * g)) - 1u; };
+  uint32_t stays = 0;  // bit u: token u * THREADS + tid does
+  if (lose && keep > 0) {
+    const long long after = (long long)s_newest - a.recent;  // positions above this are recent
+    uint32_t key[HELD];
+#pragma unroll
+    for (int u = 0; u < HELD; ++u) {
+      const long long age = (long long)born[u] - after;
+      key[u] = a.recent > 0 && age > 0 ? KEY_RECENT + (uint32_t)age : key_of(w[u]);
+    }
+    uint32_t prefix = 0, mask = 0, want = (uint32_t)keep;  // keys of this prefix still wanted
+#pragma unroll 1
+    for (int pass = 0; pass < 3; ++pass) {
+      const int low = pass == 0 ? 21 : pass == 1 ? 10 : 0;
+      const uint32_t digits = pass == 2 ? 1023u : 2047u;
+#pragma unroll
+      for (int u = 0; u < HELD; ++u) {
+        if (u * THREADS >= L) break;
+        const bool in = u * THREADS + tid < L && (key[u] & mask) == prefix;
+        if (pass > 0 && !__any_sync(0xFFFFFFFFu, in)) continue;
+        const uint32_t digit = in ? (key[u] >> low) & digits : BINS;
+        // many tokens may have one weight, 0 above all: a warp of them is one addition
+        const uint32_t first = __shfl_sync(0xFFFFFFFFu, digit, 0);
+        if (__all_sync(0xFFFFFFFFu, digit == first)) {
+          if (lane == 0 && first < BINS) atomicAdd(&s_hist[first], 32u);
+        } else if (digit < BINS) {
+          atomicAdd(&s_hist[digit], 1u);
+        }
+      }
+      __syncthreads();
+      // the bin where the count from above reaches `want`: some bins a thread, from the top
+      constexpr int EACH = BINS / THREADS;
+      const int top = BINS - 1 - EACH * tid;
+      uint32_t c[EACH], sum = 0;
+#pragma unroll
+      for (int j = 0; j < EACH; ++j) sum += c[j] = s_hist[top - j];
+      uint32_t above = block_scan(sum, s_sum) - sum;
+#pragma unroll
+      for (int j = 0; j < EACH; ++j) {
+        if (above < want && want <= above + c[j]) s_digit = top - j, s_left = want - above, s_in_bin = c[j];
+        above += c[j];
+        s_hist[top - j] = 0;
+      }
+      __syncthreads();
+      prefix |= s_digit << low;
+      mask |= digits << low;
+      want = s_left;
+      if (want == s_in_bin) break;  // all of the bin's keys stay: the rest of the bits do not matter
+    }
+    const bool all_ties = want == s_in_bin;
+    uint32_t ties = 0;
+#pragma unroll
+    for (int u = 0; u < HELD; ++u) {
+      if (u * THREADS >= L) break;
+      const bool in = u * THREADS + tid < L;
+      const uint32_t k = key[u] & mask;
+      if (in && (all_ties ? k >= prefix : k > prefix)) stays |= 1u << u;
+      if (!all_ties) {
+        const bool tie = in && k == prefix;
+        const uint32_t m = __ballot_sync(0xFFFFFFFFu, tie);
+        if (tie) ties |= 1u << u;
+        if (lane == 0) s_tie[u * WARPS + warp] = m;
+      }
+    }
+    if (!all_ties) {  // the first `want` of the ties stay
+      __syncthreads();
+      const uint32_t c = tid < GROUPS && 32 * tid < L ? __popc(s_tie[tid]) : 0u;
+      const uint32_t rank = block_scan(c, s_sum) - c;
+      if (tid < GROUPS) s_rank[tid] = rank;
+      __syncthreads();
+#pragma unroll
+      for (int u = 0; u < HELD; ++u) {
+        const int g = u * WARPS + warp;
+        if ((ties >> u) & 1u)
+          if (s_rank[g] + __popc(s_tie[g] & below) < want) stays |= 1u << u;
+      }
+      __syncthreads();
+    }
+  } else if (!lose) {
+    stays = 0xFFFFFFFFu;
+  }
+  // ---- ranks of holes (low half) and sources (high half), a group of 32 a thread
+#pragma unroll
+  for (int u = 0; u < HELD; ++u) {
+    if (u * THREADS >= L) break;
+    const uint32_t m = __ballot_sync(0xFFFFFFFFu, u * THREADS + tid < L && ((stays >> u) & 1u));
+    if (lane == 0) s_bits[u * WARPS + warp] = m;
+  }
+  __syncthreads();
+  if (lose) {
+    uint32_t c = 0;
+    if (tid < GROUPS && 32 * tid < L) {
+      const uint32_t s = s_bits[tid], lo = lows(tid);
+      c = __popc(~s & lo) | ((uint32_t)__popc(s & ~lo) << 16);
+    }
+    const uint32_t rank = block_scan(c, s_sum) - c;
+    if (tid < GROUPS) s_rank[tid] = rank;
+    __syncthreads();
+#pragma unroll
+    for (int u = 0; u < HELD; ++u) {  // the sources, in order
+      const int i = u * THREADS + tid, g = u * WARPS + warp;
+      if (i >= keep && i < L && ((stays >> u) & 1u)) {
+        const uint32_t r = (s_rank[g] >> 16) + __popc(s_bits[g] & ~lows(g) & below);
+        s_src[r] = i;
+        s_w[r] = w[u];
+        s_b[r] = born[u];
+      }
+    }
+    // the blocks that take a token
+    int32_t* todo = a.todo + (size_t)unit * ((a.cap + KV8_BLOCK - 1) / KV8_BLOCK);
+    const int blocks = (keep + KV8_BLOCK - 1) / KV8_BLOCK;
+    for (int t0 = 32 * warp; t0 < blocks; t0 += THREADS) {
+      const int t = t0 + lane;
+      const bool takes = t < blocks && (((~s_bits[t >> 1] & lows(t >> 1)) >> (16 * (t & 1))) & 0xFFFFu);
+      const uint32_t all = __ballot_sync(0xFFFFFFFFu, takes);
+      int at0 = 0;
+      if (lane == 0 && all) at0 = atomicAdd(&s_todo, __popc(all));
+      at0 = __shfl_sync(0xFFFFFFFFu, at0, 0);
+      if (takes) todo[at0 + __popc(all & below)] = t;
+    }
+    copy_edge(a, unit, h, keep, tab, THREADS);
+  }
+  __syncthreads();
+  if (tid == 0) a.count[unit] = s_todo;
+#pragma unroll
+  for (int u = 0; u < HELD; ++u) {
+    const int i = u * THREADS + tid, g = u * WARPS + warp;
+    if (i >= kept) break;
+    const uint32_t gone = lose ? ~s_bits[g] & lows(g) : 0u;
+    int src = -1;
+    if ((gone >> lane) & 1u) {
+      const uint32_t r = (s_rank[g] & 0xFFFFu) + __popc(gone & below);
+      src = s_src[r];
+      w[u] = s_w[r];
+      born[u] = s_b[r];
+    }
+    uint32_t p;
+    at(i, p);
+    a.w_out[p] = w[u];
+    a.b_out[p] = born[u];
+    if (i < a.cap) from[i] = src;
+  }
+  for (int i = kept + tid; i < a.cap; i += THREADS) from[i] = -1;
+}
+
 // Threads: a power of two, 512 to SEL_THREADS.  Shared memory: held_cap keys (the
 // sources' list takes their place) and two words a group of 32 tokens, or, of a
 // longer request, these words alone.
@@ -282,15 +509,7 @@ __global__ void __launch_bounds__(SEL_THREADS) k_select(EvictArgs a, int held_ca
     at0 = __shfl_sync(0xFFFFFFFFu, at0, 0);
     if (takes) todo[at0 + __popc(all & below)] = t;
   }
-  // ---- a copy of the block that holds both kinds
-  if (keep & (KV8_BLOCK - 1)) {
-    uint32_t p;
-    at(keep & ~(KV8_BLOCK - 1), p);
-    uint4* e = reinterpret_cast<uint4*>(a.edge + (size_t)unit * EDGE_BYTES);
-    for (int i = tid; i < 2 * KV8_BLOCK * HD / 16; i += threads)
-      e[i] = reinterpret_cast<const uint4*>((i < KV8_BLOCK * HD / 16 ? a.kc : a.vc) + (size_t)p * HD)[i % (KV8_BLOCK * HD / 16)];
-    if (tid < 2) reinterpret_cast<float*>(e + 2 * KV8_BLOCK * HD / 16)[tid] = (tid ? a.vs : a.ks)[p >> 4];
-  }
+  copy_edge(a, unit, h, keep, tab, threads);
   __syncthreads();
   if (tid == 0) a.count[unit] = s_todo;
   copy_tracks(keep, [&](int i) {
@@ -428,12 +647,18 @@ extern "C" fc_status fc_kv8_evict(const fc_kv8_cache* cache, const int32_t* d_ta
   a.list = reinterpret_cast<int32_t*>(take(units * cap * 4));
   static std::atomic<unsigned long long> done{0};
   const fc_status st = fc_once_per_device(done, [](int) {
+    if (cudaFuncSetAttribute(k_select_held<512>, cudaFuncAttributeMaxDynamicSharedMemorySize, HELD * 512 / 2 * 12) != cudaSuccess ||
+        cudaFuncSetAttribute(k_select_held<1024>, cudaFuncAttributeMaxDynamicSharedMemorySize, HELD * 1024 / 2 * 12) != cudaSuccess)
+      return FC_ERR_CUDA;
     return fc_cuda_status(cudaFuncSetAttribute(k_select, cudaFuncAttributeMaxDynamicSharedMemorySize, SEL_SMEM));
   });
   if (st != FC_OK) return st;
   cudaStream_t s = static_cast<cudaStream_t>(stream);
-  const int held = (int)std::min<long long>((longest + 31) / 32 * 32, KEYS_SMEM), threads = longest <= 8192 ? 512 : SEL_THREADS;
-  k_select<<<(unsigned)units, threads, longest > KEYS_SMEM ? SEL_SMEM : held / 32 * 34 * 4, s>>>(a, held);
+  const int held = (int)std::min<long long>((longest + 31) / 32 * 32, KEYS_SMEM);
+  if (longest <= HELD * 256) k_select_held<256><<<(unsigned)units, 256, HELD * 256 / 2 * 12, s>>>(a);
+  else if (longest <= HELD * 512) k_select_held<512><<<(unsigned)units, 512, HELD * 512 / 2 * 12, s>>>(a);
+  else if (longest <= HELD * 1024) k_select_held<1024><<<(unsigned)units, 1024, HELD * 1024 / 2 * 12, s>>>(a);
+  else k_select<<<(unsigned)units, SEL_THREADS, longest > KEYS_SMEM ? SEL_SMEM : held / 32 * 34 * 4, s>>>(a, held);
   if (cap > 0) {
     // CTAs a unit: enough for every SM's registers, while there are blocks for them
     const int y = (int)std::max<long long>(1, std::min<long long>((152 * 20 + units - 1) / units, (2 * blocks + MV_WARPS - 1) / MV_WARPS));

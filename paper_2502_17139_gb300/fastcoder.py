@@ -1088,8 +1088,9 @@ def fc_qk_norm_rope(q, k, v, wq, wk, pos, base=10000.0, eps=1e-6, out=None):
         raise TypeError("q and k must be tensors")
     B, n, H, D = q.shape if q.dim() == 4 else (0, 0, 0, 0)
     qs, ks, kshape = q.stride(), k.stride(), k.shape
-    if not (B > 1 and n > 1 and H > 1 and kshape[-2] > 1):  # a dimension of one has no stride that matters
-        qs, ks = _rows_strides(q), _rows_strides(k)
+    if (B == 1 or n == 1 or H == 1 or kshape[-2] == 1) and len(ks) == len(qs) == 4:  # whose stride does not matter
+        b, i = B > 1, n > 1
+        qs, ks = (b and qs[0], i and qs[1], H > 1 and qs[2]), (b and ks[0], i and ks[1], kshape[2] > 1 and ks[2])
     if not (q.dtype is bf and k.dtype is bf and q.is_cuda and k.is_cuda and len(kshape) == 4 and q.stride(3) == 1 and k.stride(3) == 1 and
             kshape[0] == B and kshape[1] == n and kshape[3] == D and
             (v is None or (v.dtype is bf and v.is_cuda and v.shape == kshape and v.stride() == k.stride()))):  # one test for the usual case
@@ -1251,19 +1252,34 @@ def fc_kv8_attn(q, cache: Kv8Cache, table, kv_len, k_new=None, v_new=None, mask=
     kv8_attn_workspace(...) or None (no key split).  weight fp32 [n_pages, Hkv,
     page_size]: becomes decay * weight + the softmax weights that the request's
     cached tokens received (up to 16 rows a kv head; needs the workspace)."""
-    _need(q, torch.bfloat16, "q")
+    bf, i32 = torch.bfloat16, torch.int32
+    if not (type(q) is torch.Tensor and q.dim() == 4):
+        _need(q, bf, "q")
+        raise ValueError("q must be [B, n_pad, H, D]")
     B, Np, H, D = q.shape
     Hkv = cache.Hkv
-    if D != cache.D:
-        raise ValueError("q and the cache differ in head dimension")
-    _need(table, torch.int32, "table")
-    if table.dim() != 2 or table.shape[0] != B:
-        raise ValueError("table must be [B, max_pages]")
-    _need(kv_len, torch.int32, "kv_len", (B,))
+    if out is None:
+        out = torch.empty_like(q)
+    new = (B, Hkv, Np, D)
+    if not (q.dtype is bf and out.dtype is bf and table.dtype is i32 and kv_len.dtype is i32 and q.is_cuda and out.is_cuda and
+            table.is_cuda and kv_len.is_cuda and q.is_contiguous() and out.is_contiguous() and table.is_contiguous() and
+            kv_len.is_contiguous() and out.shape == q.shape and table.dim() == 2 and table.shape[0] == B and kv_len.shape == (B,) and
+            D == cache.D and (k_new is None or (k_new.dtype is bf and v_new.dtype is bf and k_new.is_cuda and v_new.is_cuda and
+                                                k_new.is_contiguous() and v_new.is_contiguous() and k_new.shape == new and
+                                                v_new.shape == new))):  # one test for the usual case
+        _need(q, bf, "q")
+        if D != cache.D:
+            raise ValueError("q and the cache differ in head dimension")
+        _need(table, i32, "table")
+        if table.dim() != 2 or table.shape[0] != B:
+            raise ValueError("table must be [B, max_pages]")
+        _need(kv_len, i32, "kv_len", (B,))
+        if k_new is not None:
+            _need(k_new, bf, "k_new", new)
+            _need(v_new, bf, "v_new", new)
+        _need(out, bf, "out", q.shape)
     kp = vp = mp = np_ = wp = None
     if k_new is not None:
-        _need(k_new, torch.bfloat16, "k_new", (B, Hkv, Np, D))
-        _need(v_new, torch.bfloat16, "v_new", (B, Hkv, Np, D))
         kp, vp = k_new.data_ptr(), v_new.data_ptr()
     elif v_new is not None:
         raise ValueError("k_new and v_new go together")
@@ -1271,12 +1287,8 @@ def fc_kv8_attn(q, cache: Kv8Cache, table, kv_len, k_new=None, v_new=None, mask=
         _need(mask, torch.int64, "mask", (B, Np, (Np + 63) // 64))
         mp = mask.data_ptr()
     if n_nodes is not None:
-        _need(n_nodes, torch.int32, "n_nodes", (B,))
+        _need(n_nodes, i32, "n_nodes", (B,))
         np_ = n_nodes.data_ptr()
-    if out is None:
-        out = torch.empty_like(q)
-    else:
-        _need(out, torch.bfloat16, "out", q.shape)
     if weight is not None:
         _need(weight, torch.float32, "weight", cache.k_codes.shape[:3])
         wp = weight.data_ptr()

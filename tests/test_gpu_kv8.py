@@ -545,7 +545,8 @@ def test_bad_pages_and_lengths_are_recorded(fc):
 # ------------------------------------------------------------------ eviction
 @pytest.mark.parametrize("kv,keep,recent,H,page", [([20], [7], 0, 1, 16), ([64, 30], [40, 40], 8, 2, 32), ([1000, 333, 70], [500, 300, 1], 50, 3, 64),
                                                    ([100], [99], 100, 2, 16), ([300, 300], [16, 0], 5, 2, 128), ([2100], [2047], 64, 1, 256),
-                                                   ([50, 0, 49], [48, 48, 48], 1000, 2, 16)])
+                                                   ([50, 0, 49], [48, 48, 48], 1000, 2, 16), ([4096, 4000], [4095, 2000], 0, 1, 256),
+                                                   ([8192, 5], [4096, 5], 33, 1, 128), ([9000, 16384], [8999, 100], 64, 1, 64), ([17000], [8499], 100, 1, 256)])
 def test_evict(fc, kv, keep, recent, H, page):
     rng = np.random.default_rng(sum(kv) + recent)
     s = setup(rng, kv, 1, H, H, page, stale=False)
