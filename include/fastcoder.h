@@ -934,8 +934,8 @@ size_t fc_kv8_attn_workspace(int batch, int n_pad, int H, int Hkv, int64_t weigh
  * A request that loses tokens needs keep[b] <= cap: else it records
  * FC_ERR_CAPACITY, one with a negative length or keep, a length beyond its table
  * or a page id outside the pool FC_ERR_INVALID_ARG, and is left as it is (its
- * weights and positions are not carried over).  recent <= 2^22, batch * Hkv <=
- * 2^24, max_pages * page_size <= 696320.  Requests share no page that changes.
+ * weights and positions are not carried over).  recent <= 2^22, cap <= 2^30,
+ * batch * Hkv <= 2^24, max_pages * page_size <= 696320.  Requests share no page that changes.
  */
 fc_status fc_kv8_evict(const fc_kv8_cache* cache, const int32_t* d_table, int max_pages, const int32_t* d_kv_len,
                        const int32_t* d_keep, int batch, int recent, const float* d_weight_in, const int32_t* d_born_in,

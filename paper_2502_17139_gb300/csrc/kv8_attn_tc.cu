@@ -56,7 +56,7 @@ constexpr uint32_t OFF_V = OFF_K2 + HALF_BYTES;        // two stages
 constexpr uint32_t OFF_KEEP = OFF_V + 2 * TILE_BYTES;  // [slot][4] bits of the keys that count
 constexpr uint32_t OFF_BACK = OFF_KEEP + SLOTS * 16;   // [slot][8] what 16 keys' scores are to be multiplied by
 constexpr uint32_t OFF_RUN = OFF_BACK + SLOTS * 32;    // [slot][8] where 16 keys' rows are, in runs of 16 rows
-constexpr uint32_t OFF_VS = OFF_RUN + SLOTS * 32;      // [slot][8] 16 values' scale (new keys: what they are multiplied by)
+constexpr uint32_t OFF_VS = OFF_RUN + SLOTS * 32;      // [slot][8] 16 values' scale
 constexpr int PIECES = 4;                              // piece descriptions kept
 constexpr uint32_t OFF_QE = OFF_VS + SLOTS * 32;       // [PIECES][256] what a query row's scores are to be multiplied by
 constexpr uint32_t OFF_ML = OFF_QE + PIECES * ROWS * 4;  // [2 turns][2][128] (m, l) exchanged at a unit's end
@@ -207,6 +207,18 @@ __device__ __forceinline__ void mma_pv(uint32_t d, uint32_t a_tmem, uint32_t b_l
       "r"(a_tmem), "r"(b_lo), "r"(idesc), "r"(add), "n"(DESC_HI)
       : "memory");
 }
+__device__ __forceinline__ void cp_async8(uint32_t dst, const void* src) {
+  asm volatile("cp.async.ca.shared.global [%0], [%1], 8;\n" ::"r"(dst), "l"(src) : "memory");
+}
+__device__ __forceinline__ void cp_async16(uint32_t dst, const void* src) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;\n" ::"r"(dst), "l"(src) : "memory");
+}
+__device__ __forceinline__ void cp_async_commit() { asm volatile("cp.async.commit_group;\n" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void cp_async_wait() {
+  asm volatile("cp.async.wait_group %0;\n" ::"n"(N) : "memory");
+}
+__device__ __forceinline__ void cp_async_wait_all() { asm volatile("cp.async.wait_all;\n" ::: "memory"); }
 __device__ __forceinline__ void prefetch_l2(const void* p) { asm volatile("prefetch.global.L2 [%0];" ::"l"(p)); }
 __device__ __forceinline__ float pow2i(int e) { return __uint_as_float((uint32_t)(e + 127) << 23); }  // -126 <= e <= 127
 __device__ __forceinline__ float lo_f(uint32_t w) { return __uint_as_float(w << 16); }
@@ -584,7 +596,7 @@ __global__ void __launch_bounds__(THREADS, 1) k_kv8_attn_many(const __grid_const
           const bool fresh = blk >= pc.cached;
           const uint32_t run_now = run;
           int left;  // keys of the run that count
-          float back, mul;
+          float back = 1.f, mul = 0.f;
           if (!fresh) {
             const long long more = pc.kvl - ((long long)blk * BN + 16 * run_i);
             left = in ? (int)min(16ll, max(0ll, more)) : 0;
@@ -597,20 +609,7 @@ __global__ void __launch_bounds__(THREADS, 1) k_kv8_attn_many(const __grid_const
               id_next = look_up(blk + 2);
             }
           } else {
-            left = a.k_new ? min(16, max(0, pc.nn - 16 * run_i)) : 0;
-            const uint4* src = reinterpret_cast<const uint4*>(a.k_new + (((size_t)pc.b * a.Hkv + pc.gh) * a.n_pad + 16 * run_i) * HD);
-            uint32_t top = 0;
-#pragma unroll 8
-            for (int e = l4; e < left * (HD / 8); e += 4) {
-              const uint4 k = src[e];
-              top = top2(top2(top2(top2(top, k.x), k.y), k.z), k.w);
-            }
-            top = max(top & 0xFFFFu, top >> 16);
-            top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, 1));
-            top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, 2));
-            const int ek = expo_of(top);
-            back = pow2i(ek - E_TOP);
-            mul = pow2i(E_TOP - ek);
+            left = a.k_new ? min(16, max(0, pc.nn - 16 * run_i)) : 0;  // (their factors: by the warps that split them)
           }
           if (nb >= SLOTS && !(ok = warp_wait(bar(B_SLOT + slot), (nb / SLOTS - 1) & 1, &s_abort))) break;
           if (l4 == 0) {
@@ -659,49 +658,42 @@ __global__ void __launch_bounds__(THREADS, 1) k_kv8_attn_many(const __grid_const
       vr[2] = src[4];
       vr[3] = src[68];
     };
-    const size_t no_row = ~(size_t)0;
-    auto new_row = [&](int j) {
-      return a.k_new && j < pc.nn ? (((size_t)pc.b * a.Hkv + pc.gh) * a.n_pad + j) * HD : no_row;
+    // The piece's queries, a row 16 lanes: all of them asked for at once, a chunk of
+    // 8 values in two halves, each where a part of the chunk will be.  Rows past
+    // the last warp of the softmax that has some are not written.
+    auto q_at = [&](int r, int ch, int tile) {
+      return OFF_Q + (tile + (r >> 7)) * TILE_BYTES + (r & 127) * 128 + (((ch >> 1) ^ (r & 7)) << 4) + (ch & 1) * 8;
     };
-    // The piece's queries: a row 16 lanes, 16 rows at a time, times a power of two.
     auto stage_q = [&](uint32_t np, int tile) {
       float* back = reinterpret_cast<float*>(smem + OFF_QE) + np % PIECES * ROWS;
-      const int ch = lane & 15, passes = (pc.two ? 2 : 1) * BM / 16;
+      const int ch = lane & 15, rows = (pc.rows + 31) & ~31;
 #pragma unroll 1
-      for (int p0 = 0; p0 < passes; p0 += 2) {
-        uint4 v[2];
-#pragma unroll
-        for (int k = 0; k < 2; ++k) {
-          const int r = 16 * (p0 + k) + 2 * w + (lane >> 4);
-          v[k] = make_uint4(0, 0, 0, 0);
-          if (r < pc.rows) {
-            const int rr = pc.row0 + r, i = rr / a.G, hh = rr - i * a.G;
-            v[k] = reinterpret_cast<const uint4*>(a.q + (((size_t)pc.b * a.n_pad + i) * a.H + pc.gh * a.G + hh) * HD)[ch];
-          }
-        }
-#pragma unroll
-        for (int k = 0; k < 2; ++k) {
-          const int r = 16 * (p0 + k) + 2 * w + (lane >> 4);
-          const uint32_t sign = 0x7FFF7FFFu;
-          uint32_t top = __vmaxu2(__vmaxu2(v[k].x & sign, v[k].y & sign), __vmaxu2(v[k].z & sign, v[k].w & sign));
-#pragma unroll
-          for (int o = 1; o < 16; o <<= 1) top = __vmaxu2(top, __shfl_xor_sync(0xFFFFFFFFu, top, o));
-          const int ex = expo_of(max(top & 0xFFFFu, top >> 16));
-          if (ch == 0) back[r] = pow2i(ex - E_TOP);
-          uint2 p1, p2;
-          split8(v[k], pow2i(E_TOP - ex), p1, p2);
-          unsigned char* to = smem + OFF_Q + (tile + (r >> 7)) * TILE_BYTES + (r & 127) * 128 + (((ch >> 1) ^ (r & 7)) << 4) + (ch & 1) * 8;
-          *reinterpret_cast<uint2*>(to) = p1;
-          *reinterpret_cast<uint2*>(to + HALF_BYTES) = p2;
+      for (int r = 2 * w + (lane >> 4); r < rows; r += 16) {
+        const uint32_t to = q_at(r, ch, tile);
+        if (r < pc.rows) {
+          const int rr = pc.row0 + r, i = rr / a.G, hh = rr - i * a.G;
+          const __nv_bfloat16* src = a.q + (((size_t)pc.b * a.n_pad + i) * a.H + pc.gh * a.G + hh) * HD + ch * 8;
+          cp_async8(sbase + to, src);
+          cp_async8(sbase + to + HALF_BYTES, src + 4);
+        } else {
+          *reinterpret_cast<uint2*>(smem + to) = *reinterpret_cast<uint2*>(smem + to + HALF_BYTES) = make_uint2(0, 0);
         }
       }
-    };
-    auto store_new = [&](const __nv_bfloat16* src, auto&& put) {  // the new rows, zeros past them
+      cp_async_wait_all();
 #pragma unroll 2
-      for (int e = lane; e < 256; e += 32) {
-        const int j = 16 * w + (e >> 4), ch = e & 15;
-        const size_t row = new_row(j);
-        put(j, ch, row != no_row ? reinterpret_cast<const uint4*>(src + row)[ch] : make_uint4(0, 0, 0, 0));
+      for (int r = 2 * w + (lane >> 4); r < rows; r += 16) {
+        unsigned char* to = smem + q_at(r, ch, tile);
+        const uint2 lo = *reinterpret_cast<const uint2*>(to), hi = *reinterpret_cast<const uint2*>(to + HALF_BYTES);
+        const uint32_t sign = 0x7FFF7FFFu;
+        uint32_t top = __vmaxu2(__vmaxu2(lo.x & sign, lo.y & sign), __vmaxu2(hi.x & sign, hi.y & sign));
+#pragma unroll
+        for (int o = 1; o < 16; o <<= 1) top = __vmaxu2(top, __shfl_xor_sync(0xFFFFFFFFu, top, o));
+        const int ex = expo_of(max(top & 0xFFFFu, top >> 16));
+        if (ch == 0) back[r] = pow2i(ex - E_TOP);
+        uint2 p1, p2;
+        split8(make_uint4(lo.x, lo.y, hi.x, hi.y), pow2i(E_TOP - ex), p1, p2);
+        *reinterpret_cast<uint2*>(to) = p1;
+        *reinterpret_cast<uint2*>(to + HALF_BYTES) = p2;
       }
     };
     auto done = [&](int which) {  // this warp's part of a tile is written
@@ -758,34 +750,69 @@ __global__ void __launch_bounds__(THREADS, 1) k_kv8_attn_many(const __grid_const
         if (!(ok = info(nb))) break;
         // the second part's place: free once the last piece's first products are done
         if (np > 0 && !(ok = warp_wait(bar(B_QFREE), (np - 1) & 1, &s_abort))) break;
-        const float by = vscales[slot * (BN / 16)];
-        store_new(a.k_new, [&](int j, int ch, const uint4& v) {
-          uint2 p1, p2;
-          split8(v, by, p1, p2);
-          const uint32_t at = j * 128 + (((ch >> 1) ^ (j & 7)) << 4) + (ch & 1) * 8;
-          *reinterpret_cast<uint2*>(smem + OFF_K + slot * HALF_BYTES + at) = p1;
-          *reinterpret_cast<uint2*>(smem + OFF_K2 + at) = p2;
-        });
-        done(B_KFULL + slot);
+        // rows 16w .. of the new tokens; keys' halves where their parts will be, values in their place
+        const int live = a.k_new ? min(16, pc.nn - 16 * w) : 0;
+        const size_t from = (((size_t)pc.b * a.Hkv + pc.gh) * a.n_pad + 16 * w) * HD;
+        const uint32_t sK1 = OFF_K + slot * HALF_BYTES, ch = lane & 15;
+        auto k_at = [&](int j) { return (16 * w + j) * 128 + (((ch >> 1) ^ (j & 7)) << 4) + (ch & 1) * 8; };
+#pragma unroll 1
+        for (int j = lane >> 4; j < live; j += 2) {
+          cp_async8(sbase + sK1 + k_at(j), a.k_new + from + j * HD + ch * 8);
+          cp_async8(sbase + OFF_K2 + k_at(j), a.k_new + from + j * HD + ch * 8 + 4);
+        }
+        cp_async_commit();
         if (nb >= 2 && !(ok = warp_wait(bar(B_VEMPTY + st), ((nb >> 1) - 1) & 1, &s_abort))) break;
+        const uint32_t sV1 = OFF_V + st * TILE_BYTES + (ch >> 3) * HALF_BYTES;
+        auto v_at = [&](int j) { return sV1 + (16 * w + j) * 128 + (((ch & 7) ^ (j & 7)) << 4); };
+#pragma unroll 1
+        for (int j = lane >> 4; j < 16; j += 2) {
+          if (j < live) cp_async16(sbase + v_at(j), a.v_new + from + j * HD + ch * 8);
+          else *reinterpret_cast<uint4*>(smem + v_at(j)) = make_uint4(0, 0, 0, 0);
+        }
+        cp_async_commit();
+        cp_async_wait<1>();
+        uint32_t top = 0;
+#pragma unroll 1
+        for (int j = lane >> 4; j < live; j += 2) {
+          const uint2 lo = *reinterpret_cast<const uint2*>(smem + sK1 + k_at(j)), hi = *reinterpret_cast<const uint2*>(smem + OFF_K2 + k_at(j));
+          top = top2(top2(top2(top2(top, lo.x), lo.y), hi.x), hi.y);
+        }
+        const int ek = expo_of(__reduce_max_sync(0xFFFFFFFFu, max(top & 0xFFFFu, top >> 16)));
+        if (lane == 0) reinterpret_cast<float*>(smem + OFF_BACK)[slot * (BN / 16) + w] = pow2i(ek - E_TOP);
+#pragma unroll 1
+        for (int j = lane >> 4; j < live; j += 2) {
+          uint2 *k1 = reinterpret_cast<uint2*>(smem + sK1 + k_at(j)), *k2 = reinterpret_cast<uint2*>(smem + OFF_K2 + k_at(j));
+          const uint2 lo = *k1, hi = *k2;
+          split8(make_uint4(lo.x, lo.y, hi.x, hi.y), pow2i(E_TOP - ek), *k1, *k2);
+        }
+        done(B_KFULL + slot);
+        cp_async_wait<0>();
         // A value that is not finite becomes 0, as no weight of 0 would take it
         // out of the rows that do not see its token; those that do are NaN.
         uint32_t bad = 0;
-        store_new(a.v_new, [&](int j, int ch, const uint4& v) {
-          auto finite = [&](uint32_t x) {
-            const uint32_t not_finite = __vcmpgeu2(x & 0x7FFF7FFFu, 0x7F807F80u);
-            if (not_finite) bad |= 1u << (j & 15);
-            return x & ~not_finite;
-          };
-          *reinterpret_cast<uint4*>(smem + OFF_V + st * TILE_BYTES + (ch >> 3) * HALF_BYTES + j * 128 + (((ch & 7) ^ (j & 7)) << 4)) =
-              make_uint4(finite(v.x), finite(v.y), finite(v.z), finite(v.w));
-        });
+#pragma unroll 1
+        for (int j = lane >> 4; j < live; j += 2) {
+          uint4* at = reinterpret_cast<uint4*>(smem + v_at(j));
+          uint4 v = *at;
+          uint32_t any = 0;
+#pragma unroll
+          for (int u = 0; u < 4; ++u) {
+            const uint32_t not_finite = __vcmpgeu2((&v.x)[u] & 0x7FFF7FFFu, 0x7F807F80u);
+            any |= not_finite;
+            (&v.x)[u] &= ~not_finite;
+          }
+          if (any) {
+            *at = v;
+            bad |= 1u << j;
+          }
+        }
         bad = __reduce_or_sync(0xFFFFFFFFu, bad);
         if (lane == 0) reinterpret_cast<uint16_t*>(smem + OFF_BAD)[np % PIECES * NUM_WARPS + w] = (uint16_t)bad;
         done(B_VFULL + st);
         ++nb;
       }
     }
+    cp_async_wait_all();
   } else {
     // ---------------- softmax: warpgroup x, a row a thread ----------------
     // (A piece's description is read again where it is needed, not kept: the
@@ -831,11 +858,15 @@ __global__ void __launch_bounds__(THREADS, 1) k_kv8_attn_many(const __grid_const
         const float2* back = reinterpret_cast<const float2*>(smem + OFF_BACK) + slot * (NUM_WARPS / 2);
         const uint32_t* keep = reinterpret_cast<const uint32_t*>(smem + OFF_KEEP) + slot * 4;
         const bool masked = j >= n_cached || (keep[0] & keep[1] & keep[2] & keep[3]) != 0xFFFFFFFFu;  // in all rows alike
+        uint64_t sees[2] = {~0ull, ~0ull};
+        if (j >= n_cached) {
+          seen(pc, sees);
+          // the new keys' factors come with the keys
+          if (!(ok = warp_wait(bar(B_KFULL + slot), ((nb + j) / SLOTS) & 1, &s_abort))) break;
+        }
         if (!(ok = warp_wait(bar(B_SFULL + x), t & 1, &s_abort))) break;
         tc_fence_after();
         if (__builtin_expect(masked, 0)) {  // masked scores are overwritten by -inf
-          uint64_t sees[2] = {~0ull, ~0ull};
-          if (j >= n_cached) seen(pc, sees);
 #pragma unroll 1
           for (int q = 0; q < 4; ++q) {
             const uint32_t k = keep[q] & (uint32_t)(sees[q >> 1] >> (32 * (q & 1)));

@@ -35,6 +35,7 @@ constexpr int KEYS_SMEM = 40960;             // keys that fit in shared memory (
 constexpr int SEL_SMEM = KEYS_SMEM / 32 * 34 * 4;
 constexpr int MAX_KEYS = SEL_SMEM / 8 * 32;  // 696,320 tokens a request
 constexpr int MAX_RECENT = 1 << 22;
+constexpr int MAX_CAP = 1 << 30;  // places of d_from are counted in 32 bits
 constexpr uint32_t KEY_RECENT = 0xFF900000u;  // above every weight's key; recent tokens by age from here on
 constexpr int MV_THREADS = 256, MV_WARPS = MV_THREADS / 32;
 constexpr int EDGE_BYTES = 2 * KV8_BLOCK * HD + 16;  // a unit's copy: 16 rows of keys, of values, their scales
@@ -609,7 +610,7 @@ size_t up256(size_t n) { return (n + 255) & ~(size_t)255; }
 }  // namespace
 
 extern "C" size_t fc_kv8_evict_workspace(int batch, int Hkv, int cap) {
-  if (batch < 1 || Hkv < 1 || cap < 0) return 0;
+  if (batch < 1 || Hkv < 1 || cap < 0 || cap > MAX_CAP) return 0;
   const size_t units = (size_t)batch * Hkv;
   return up256(units * 4) + up256(units * ((cap + KV8_BLOCK - 1) / KV8_BLOCK) * 4) + up256(units * EDGE_BYTES) + up256(units * cap * 4);
 }
@@ -622,7 +623,7 @@ extern "C" fc_status fc_kv8_evict(const fc_kv8_cache* cache, const int32_t* d_ta
   if (const fc_status st = fc_kv8_check(cache)) return st;
   const int shift = kv8_page_shift(cache->page_size);
   if (batch < 0 || max_pages < 1 || recent < 0 || cap < 0) return FC_ERR_INVALID_ARG;
-  if (recent > MAX_RECENT || (long long)max_pages << shift > MAX_KEYS || (long long)batch * cache->Hkv > 1 << 24)
+  if (recent > MAX_RECENT || cap > MAX_CAP || (long long)max_pages << shift > MAX_KEYS || (long long)batch * cache->Hkv > 1 << 24)
     return FC_ERR_UNSUPPORTED;
   if (batch == 0) return FC_OK;
   if (!d_table || !d_kv_len || !d_keep || !d_weight_in || !d_born_in || !d_weight_out || !d_born_out || (cap && !d_from) ||
