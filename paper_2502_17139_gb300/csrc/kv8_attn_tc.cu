@@ -45,6 +45,7 @@ namespace {
 constexpr int HD = KV8_D;
 constexpr int THREADS = 640;  // warp 0 products, 1 pieces, 2 scales and keys, 4-7 / 8-11 softmax, 12-19 queries and values to tiles
 constexpr int NUM_WARPS = 8;
+constexpr int QN = 2;  // queries' rows in hand a lane
 constexpr int BM = 128, BN = 128, ROWS = 2 * BM;
 constexpr uint32_t HALF_BYTES = 128 * 128;             // 64 bf16 dims, or all 128 e4m3 ones, of 128 rows
 constexpr uint32_t TILE_BYTES = 2 * HALF_BYTES;        // a bf16 tile, or an e4m3 one's two parts
@@ -74,10 +75,11 @@ constexpr float M_START = -1e30f;  // a reference before any key
 // Exponents below count as this, so that the product of two is no fp32
 // underflow; such scores are 0 to fp32 all the same.
 constexpr int E_MIN = -50;
-// A unit's start and end in blocks of one tile: 8 where a unit is cut over CTAs
-// (4 trees of 64 nodes over 300 keys 29 us, with 12 32), 12 where a CTA has several
-// (16 ragged trees of 64 nodes 166 us, with 8 178).  And the least share worth a CTA.
-constexpr int CUT_COST = 8, WHOLE_COST = 12, LEAST = 6;
+// A unit's start and end in blocks of one tile: 4 where a unit is cut over CTAs (3
+// requests of 128 nodes, 32 heads of their own, over 3000 keys 36 us, with 8 39), 7
+// where a CTA has several (16 ragged trees of 64 nodes 121 us, with 12 128).  And
+// the least share worth a CTA (32 nodes over 2000 keys 22 us, with 6 25).
+constexpr int CUT_COST = 4, WHOLE_COST = 7, LEAST = 4;
 
 // Registers a thread by warpgroup (setmaxnreg), of the launch's 96.  The shares must add up to the launch's
 // allocation, or the increase never returns; the host checks the compiled count.
@@ -109,9 +111,11 @@ struct ManyArgs {
   int split;       // 0: whole units, CTA by CTA
   int unit_cost;   // CUT_COST or WHOLE_COST
   int rows_cap;    // rows a piece's slot has room for
+  uint32_t by_G;   // r / G is r * by_G >> 20 for r < 2048
   int* list;       // [grid][8] cut units for k_kv8_join
   float* part_o;   // [grid][2][rows_cap][HD]
   float2* part_ml; // [grid][2][rows_cap]
+  __device__ __forceinline__ int node_of(int r) const { return (int)((uint32_t)r * by_G >> 20); }
 };
 
 __device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, volatile int* abort) {
@@ -145,9 +149,10 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
   asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
   return d;
 }
-__device__ __forceinline__ void tmem_ld16(uint32_t taddr, uint32_t (&r)[16]) {
+// 16 rows of 32 columns: register 4i + 2k + e is column 8i + 2 (lane % 4) + e of row lane / 4 + 8k
+__device__ __forceinline__ void tmem_ld_rows(uint32_t taddr, uint32_t (&r)[16]) {
   asm volatile(
-      "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
+      "tcgen05.ld.sync.aligned.16x256b.x4.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
       : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
         "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
       : "r"(taddr));
@@ -248,16 +253,16 @@ __device__ __forceinline__ void split8(const uint4& v, float by, uint2& p1, uint
   p2 = make_uint2(b[0] | (b[1] << 16), b[2] | (b[3] << 16));
 }
 
-// 8 cached numbers (two words) times 2^-120 times f1 (times f2), as bf16
-__device__ __forceinline__ uint4 values8(uint32_t lo, uint32_t hi, uint32_t f1, uint32_t f2) {
-  auto two = [&](uint32_t w, uint32_t sel) {
+// The first (sel 0x1000) or last two (0x3020) cached numbers of each word, times 2^-120 times f1 (times f2), as bf16
+__device__ __forceinline__ uint4 values8(uint32_t a, uint32_t b, uint32_t c, uint32_t d, uint32_t sel, uint32_t f1, uint32_t f2) {
+  auto two = [&](uint32_t w) {
     const uint32_t x = __byte_perm(w, w, sel);
     uint32_t r = ((x >> 4) & 0x07F007F0u) | (x & 0x80008000u);
     asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(r), "r"(f1));
     if (f2 != 0x3F803F80u) asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(r), "r"(f2));
     return r;
   };
-  return make_uint4(two(lo, 0x1000), two(lo, 0x3020), two(hi, 0x1000), two(hi, 0x3020));
+  return make_uint4(two(a), two(b), two(c), two(d));
 }
 
 // A CTA's part of a unit: n blocks from s0 on (n = 0: there is no more).
@@ -636,14 +641,14 @@ __global__ void __launch_bounds__(THREADS, 1) k_kv8_attn_many(const __grid_const
   } else if (warp >= 12) {
     // ---------------- queries and values to tiles ----------------
     // Warp w has rows 16w .. 16w + 15 of a block, one run of a page: lane (rho,
-    // c) rows rho and rho + 8, 16 bytes c and c + 4 of their 128.  Eight lanes in
-    // turn have eight rows, so that their stores fall in different banks.
+    // c) rows rho and rho + 8, dimensions 32c .. 32c + 31.  Eight lanes in turn have
+    // eight rows, so that their stores fall in different banks.
+    // Column 8i + 2q + e of 32 is dimension 8q + 2i + e: so a thread that reads the
+    // sums back, columns 2q and 2q + 1 of every 8, has 8 dimensions that are neighbours.
     const int w = warp - 12, c = lane >> 3, rho = lane & 7;
-    uint32_t dst[2];
-#pragma unroll
-    for (int i = 0; i < 2; ++i) dst[i] = (16 * w + rho) * 128 + (((2 * c + i) ^ rho) << 4);
+    const uint32_t dst = (c >> 1) * HALF_BYTES + (16 * w + rho) * 128 + ((((c & 1) * 4) ^ rho) << 4);
     Piece pc = {};
-    uint4 vr[4];  // rows rho, rho + 8 of the first 64 dims, then of the others
+    uint4 vr[4];  // row rho, then row rho + 8
     uint32_t nb = 0;
     bool ok = true;
     auto info = [&](uint32_t blk) {
@@ -652,48 +657,61 @@ __global__ void __launch_bounds__(THREADS, 1) k_kv8_attn_many(const __grid_const
     const uint32_t* runs = reinterpret_cast<const uint32_t*>(smem + OFF_RUN) + w;
     const float* vscales = reinterpret_cast<const float*>(smem + OFF_VS) + w;
     auto fetch = [&](uint32_t run) {
-      const uint4* src = reinterpret_cast<const uint4*>(a.vc + (uint64_t)run * 2048u) + rho * 8 + c;
+      const uint4* src = reinterpret_cast<const uint4*>(a.vc + (uint64_t)run * 2048u) + rho * 8 + 2 * c;
       vr[0] = src[0];
-      vr[1] = src[64];
-      vr[2] = src[4];
-      vr[3] = src[68];
+      vr[1] = src[1];
+      vr[2] = src[64];
+      vr[3] = src[65];
     };
     // The piece's queries, a row 16 lanes: all of them asked for at once, a chunk of
     // 8 values in two halves, each where a part of the chunk will be.  Rows past
-    // the last warp of the softmax that has some are not written.
-    auto q_at = [&](int r, int ch, int tile) {
-      return OFF_Q + (tile + (r >> 7)) * TILE_BYTES + (r & 127) * 128 + (((ch >> 1) ^ (r & 7)) << 4) + (ch & 1) * 8;
-    };
+    // the last 32 of which some are in use are not written.
     auto stage_q = [&](uint32_t np, int tile) {
-      float* back = reinterpret_cast<float*>(smem + OFF_QE) + np % PIECES * ROWS;
-      const int ch = lane & 15, rows = (pc.rows + 31) & ~31;
+      const int ch = lane & 15, r0 = 2 * w + (lane >> 4), passes = ((pc.rows + 31) >> 5) * 2;  // 16 rows each
+      const uint32_t to0 = OFF_Q + tile * TILE_BYTES + r0 * 128 + (((ch >> 1) ^ (r0 & 7)) << 4) + (ch & 1) * 8;
+      auto at = [&](int p) { return to0 + p * 2048 + (p & 8) * 2048; };  // the second tile from pass 8 on
+      const __nv_bfloat16* q0 = a.q + ((size_t)pc.b * a.n_pad * a.H + pc.gh * a.G) * HD + ch * 8;
 #pragma unroll 1
-      for (int r = 2 * w + (lane >> 4); r < rows; r += 16) {
-        const uint32_t to = q_at(r, ch, tile);
+      for (int p = 0; p < passes; ++p) {
+        const uint32_t to = sbase + at(p);
+        const int r = r0 + 16 * p, rr = pc.row0 + r;
         if (r < pc.rows) {
-          const int rr = pc.row0 + r, i = rr / a.G, hh = rr - i * a.G;
-          const __nv_bfloat16* src = a.q + (((size_t)pc.b * a.n_pad + i) * a.H + pc.gh * a.G + hh) * HD + ch * 8;
-          cp_async8(sbase + to, src);
-          cp_async8(sbase + to + HALF_BYTES, src + 4);
+          const __nv_bfloat16* src = q0 + (size_t)(uint32_t)(f.node_of(rr) * (a.H - a.G) + rr) * HD;
+          cp_async8(to, src);
+          cp_async8(to + HALF_BYTES, src + 4);
         } else {
-          *reinterpret_cast<uint2*>(smem + to) = *reinterpret_cast<uint2*>(smem + to + HALF_BYTES) = make_uint2(0, 0);
+          unsigned char* z = smem + at(p);
+          *reinterpret_cast<uint2*>(z) = *reinterpret_cast<uint2*>(z + HALF_BYTES) = make_uint2(0, 0);
         }
       }
       cp_async_wait_all();
-#pragma unroll 2
-      for (int r = 2 * w + (lane >> 4); r < rows; r += 16) {
-        unsigned char* to = smem + q_at(r, ch, tile);
-        const uint2 lo = *reinterpret_cast<const uint2*>(to), hi = *reinterpret_cast<const uint2*>(to + HALF_BYTES);
-        const uint32_t sign = 0x7FFF7FFFu;
-        uint32_t top = __vmaxu2(__vmaxu2(lo.x & sign, lo.y & sign), __vmaxu2(hi.x & sign, hi.y & sign));
+      float* back = reinterpret_cast<float*>(smem + OFF_QE) + np % PIECES * ROWS + r0;
+#pragma unroll 1
+      for (int p0 = 0; p0 < passes; p0 += QN) {
+        uint2 lo[QN], hi[QN];
+        uint32_t top[QN];
 #pragma unroll
-        for (int o = 1; o < 16; o <<= 1) top = __vmaxu2(top, __shfl_xor_sync(0xFFFFFFFFu, top, o));
-        const int ex = expo_of(max(top & 0xFFFFu, top >> 16));
-        if (ch == 0) back[r] = pow2i(ex - E_TOP);
-        uint2 p1, p2;
-        split8(make_uint4(lo.x, lo.y, hi.x, hi.y), pow2i(E_TOP - ex), p1, p2);
-        *reinterpret_cast<uint2*>(to) = p1;
-        *reinterpret_cast<uint2*>(to + HALF_BYTES) = p2;
+        for (int k = 0; k < QN; ++k) {
+          const unsigned char* from = smem + at(p0 + k);
+          lo[k] = *reinterpret_cast<const uint2*>(from);
+          hi[k] = *reinterpret_cast<const uint2*>(from + HALF_BYTES);
+          const uint32_t sign = 0x7FFF7FFFu;
+          top[k] = __vmaxu2(__vmaxu2(lo[k].x & sign, lo[k].y & sign), __vmaxu2(hi[k].x & sign, hi[k].y & sign));
+        }
+#pragma unroll
+        for (int o = 1; o < 16; o <<= 1)
+#pragma unroll
+          for (int k = 0; k < QN; ++k) top[k] = __vmaxu2(top[k], __shfl_xor_sync(0xFFFFFFFFu, top[k], o));
+#pragma unroll
+        for (int k = 0; k < QN; ++k) {
+          const int ex = expo_of(max(top[k] & 0xFFFFu, top[k] >> 16));
+          if (ch == 0) back[16 * (p0 + k)] = pow2i(ex - E_TOP);
+          uint2 p1, p2;
+          split8(make_uint4(lo[k].x, lo[k].y, hi[k].x, hi[k].y), pow2i(E_TOP - ex), p1, p2);
+          unsigned char* to = smem + at(p0 + k);
+          *reinterpret_cast<uint2*>(to) = p1;
+          *reinterpret_cast<uint2*>(to + HALF_BYTES) = p2;
+        }
       }
     };
     auto done = [&](int which) {  // this warp's part of a tile is written
@@ -733,10 +751,13 @@ __global__ void __launch_bounds__(THREADS, 1) k_kv8_attn_many(const __grid_const
         const uint32_t f1 = pack_bf16x2(m1, m1), f2 = pack_bf16x2(pow2i(ex - e1), pow2i(ex - e1));
         if (nb >= 2 && !(ok = warp_wait(bar(B_VEMPTY + st), ((nb >> 1) - 1) & 1, &s_abort))) break;
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-          unsigned char* t = smem + OFF_V + st * TILE_BYTES + (k >> 1) * HALF_BYTES + (k & 1) * 1024;
-          *reinterpret_cast<uint4*>(t + dst[0]) = values8(vr[k].x, vr[k].y, f1, f2);
-          *reinterpret_cast<uint4*>(t + dst[1]) = values8(vr[k].z, vr[k].w, f1, f2);
+        for (int k = 0; k < 2; ++k) {
+          unsigned char* t = smem + OFF_V + st * TILE_BYTES + k * 1024;
+          const uint4 a0 = vr[2 * k], a1 = vr[2 * k + 1];
+          *reinterpret_cast<uint4*>(t + dst) = values8(a0.x, a0.z, a1.x, a1.z, 0x1000, f1, f2);
+          *reinterpret_cast<uint4*>(t + (dst ^ 16)) = values8(a0.x, a0.z, a1.x, a1.z, 0x3020, f1, f2);
+          *reinterpret_cast<uint4*>(t + (dst ^ 32)) = values8(a0.y, a0.w, a1.y, a1.w, 0x1000, f1, f2);
+          *reinterpret_cast<uint4*>(t + (dst ^ 48)) = values8(a0.y, a0.w, a1.y, a1.w, 0x3020, f1, f2);
         }
         done(B_VFULL + st);
         if (more) {
@@ -754,7 +775,10 @@ __global__ void __launch_bounds__(THREADS, 1) k_kv8_attn_many(const __grid_const
         const int live = a.k_new ? min(16, pc.nn - 16 * w) : 0;
         const size_t from = (((size_t)pc.b * a.Hkv + pc.gh) * a.n_pad + 16 * w) * HD;
         const uint32_t sK1 = OFF_K + slot * HALF_BYTES, ch = lane & 15;
-        auto k_at = [&](int j) { return (16 * w + j) * 128 + (((ch >> 1) ^ (j & 7)) << 4) + (ch & 1) * 8; };
+        const uint32_t k0 = (16 * w + (lane >> 4)) * 128 + (((ch >> 1) ^ (lane >> 4)) << 4) + (ch & 1) * 8;
+        auto k_at = [&](int j) { return (k0 ^ ((j & 6) << 4)) + (j >> 1) * 256; };  // of row j, lane >> 4 in its lowest bit
+        const uint32_t sV1 = OFF_V + st * TILE_BYTES + (ch >> 3) * HALF_BYTES;
+        auto v_at = [&](int j, int i) { return sV1 + (16 * w + j) * 128 + (((ch & 4) ^ i ^ (j & 7)) << 4); };
 #pragma unroll 1
         for (int j = lane >> 4; j < live; j += 2) {
           cp_async8(sbase + sK1 + k_at(j), a.k_new + from + j * HD + ch * 8);
@@ -762,12 +786,10 @@ __global__ void __launch_bounds__(THREADS, 1) k_kv8_attn_many(const __grid_const
         }
         cp_async_commit();
         if (nb >= 2 && !(ok = warp_wait(bar(B_VEMPTY + st), ((nb >> 1) - 1) & 1, &s_abort))) break;
-        const uint32_t sV1 = OFF_V + st * TILE_BYTES + (ch >> 3) * HALF_BYTES;
-        auto v_at = [&](int j) { return sV1 + (16 * w + j) * 128 + (((ch & 7) ^ (j & 7)) << 4); };
 #pragma unroll 1
         for (int j = lane >> 4; j < 16; j += 2) {
-          if (j < live) cp_async16(sbase + v_at(j), a.v_new + from + j * HD + ch * 8);
-          else *reinterpret_cast<uint4*>(smem + v_at(j)) = make_uint4(0, 0, 0, 0);
+          if (j < live) cp_async16(sbase + v_at(j, ch & 3), a.v_new + from + j * HD + ch * 8);
+          else *reinterpret_cast<uint4*>(smem + v_at(j, ch & 3)) = make_uint4(0, 0, 0, 0);
         }
         cp_async_commit();
         cp_async_wait<1>();
@@ -787,23 +809,20 @@ __global__ void __launch_bounds__(THREADS, 1) k_kv8_attn_many(const __grid_const
         }
         done(B_KFULL + slot);
         cp_async_wait<0>();
-        // A value that is not finite becomes 0, as no weight of 0 would take it
+        __syncwarp();
+        // Into their columns: four lanes exchange the words of 32 dimensions.  A
+        // value that is not finite becomes 0, as no weight of 0 would take it
         // out of the rows that do not see its token; those that do are NaN.
         uint32_t bad = 0;
 #pragma unroll 1
-        for (int j = lane >> 4; j < live; j += 2) {
-          uint4* at = reinterpret_cast<uint4*>(smem + v_at(j));
-          uint4 v = *at;
-          uint32_t any = 0;
+        for (int j = lane >> 4; j - (lane >> 4) < live; j += 2) {
+          const uint4 v = *reinterpret_cast<const uint4*>(smem + v_at(j, ch & 3));
+          __syncwarp();
 #pragma unroll
-          for (int u = 0; u < 4; ++u) {
-            const uint32_t not_finite = __vcmpgeu2((&v.x)[u] & 0x7FFF7FFFu, 0x7F807F80u);
-            any |= not_finite;
-            (&v.x)[u] &= ~not_finite;
-          }
-          if (any) {
-            *at = v;
-            bad |= 1u << j;
+          for (int i = 0; i < 4; ++i) {
+            const uint32_t x = (&v.x)[i], not_finite = __vcmpgeu2(x & 0x7FFF7FFFu, 0x7F807F80u);
+            *reinterpret_cast<uint32_t*>(smem + v_at(j, i) + (ch & 3) * 4) = x & ~not_finite;
+            if (not_finite) bad |= 1u << j;
           }
         }
         bad = __reduce_or_sync(0xFFFFFFFFu, bad);
@@ -823,7 +842,7 @@ __global__ void __launch_bounds__(THREADS, 1) k_kv8_attn_many(const __grid_const
     bool ok = true;
     auto row_of = [&](const Piece* pc) { return pc->two ? x * BM + r : r; };  // row of the piece
     auto seen = [&](const Piece* pc, uint64_t (&sees)[2]) {  // the new tokens that the row sees
-      const int lr = row_of(pc), i = (pc->row0 + lr) / a.G;
+      const int lr = row_of(pc), i = f.node_of(pc->row0 + lr);
       if (lr >= pc->rows) {
         sees[0] = sees[1] = 0;
       } else if (a.mask) {
@@ -954,10 +973,6 @@ __global__ void __launch_bounds__(THREADS, 1) k_kv8_attn_many(const __grid_const
       tc_fence_after();
       // ---- the piece's rows: this tile's, or half the dimensions of both halves' sum
       const bool two = pc->two, whole = pc->whole;
-      const int lr = row_of(pc), rr = pc->row0 + lr, i = rr / a.G, hh = rr - i * a.G;
-      const bool row_ok = lr < pc->rows;
-      __nv_bfloat16* dst = a.out + (((size_t)pc->b * a.n_pad + (row_ok ? i : 0)) * a.H + pc->gh * a.G + hh) * HD;
-      const size_t slot = (size_t)pc->slot * f.rows_cap + lr;
       if (n > n_cached) {  // new tokens: are all values finite?
         const uint64_t* bad = reinterpret_cast<const uint64_t*>(smem + OFF_BAD) + np % PIECES * 2;
         if (bad[0] | bad[1]) {
@@ -987,36 +1002,53 @@ __global__ void __launch_bounds__(THREADS, 1) k_kv8_attn_many(const __grid_const
       k0 *= inv;
       k1 *= inv;
       const bool both = !two && n > 1;
+      const int row_w = row_of(pc) - lane;  // the warp's first row
+      const size_t slot0 = (size_t)pc->slot * f.rows_cap;
+      // 16 rows and 32 dimensions at a time: a lane has 8 neighbours of two rows, four lanes 64 (a lane a row,
+      // its stores in 32 rows each, took 7000 cycles for 256 rows, this 3000)
 #pragma unroll 1
-      for (int cc = two ? 0 : 4 * x; cc < (two ? 8 : 4 * x + 4); ++cc) {
-        uint32_t o[16];
-        float v[16];
-        tmem_ld16(tO0 + cc * 16, o);
-        tc_wait_ld();
+      for (int half = idle ? 32 : 0; half < 32; half += 16) {
+        float ka[2], kb[2];
+        bool in[2];
+        __nv_bfloat16* dst[2];
+        float* po[2];
 #pragma unroll
-        for (int u = 0; u < 16; ++u) v[u] = __uint_as_float(o[u]) * k0;
-        if (both) {
-          tmem_ld16(tO0 + 128 + cc * 16, o);
+        for (int k = 0; k < 2; ++k) {
+          const int from = half + 8 * k + (lane >> 2), lr = row_w + from, rr = pc->row0 + lr;
+          ka[k] = __shfl_sync(0xFFFFFFFFu, k0, from);
+          kb[k] = __shfl_sync(0xFFFFFFFFu, k1, from);
+          in[k] = lr < pc->rows;
+          dst[k] = a.out + ((size_t)(uint32_t)(f.node_of(rr) * (a.H - a.G) + rr) + (size_t)pc->b * a.n_pad * a.H + pc->gh * a.G) * HD + (lane & 3) * 8;
+          po[k] = f.part_o + (slot0 + lr) * HD + (lane & 3) * 8;
+        }
+#pragma unroll 1
+        for (int cc = two ? 0 : 2 * x; cc < (two ? 4 : 2 * x + 2); ++cc) {
+          uint32_t o[16], o2[16];
+          tmem_ld_rows(tO0 + (half << 16) + cc * 32, o);
+          if (both) tmem_ld_rows(tO0 + (half << 16) + 128 + cc * 32, o2);
           tc_wait_ld();
 #pragma unroll
-          for (int u = 0; u < 16; ++u) v[u] = fmaf(__uint_as_float(o[u]), k1, v[u]);
-        }
-        if (row_ok) {
+          for (int k = 0; k < 2; ++k) {
+            float v[8];
 #pragma unroll
-          for (int u = 0; u < 16; u += 8) {
+            for (int u = 0; u < 8; ++u) {
+              const int i = 4 * (u >> 1) + 2 * k + (u & 1);
+              v[u] = __uint_as_float(o[i]) * ka[k];
+              if (both) v[u] = fmaf(__uint_as_float(o2[i]), kb[k], v[u]);
+            }
+            if (!in[k]) continue;
             if (whole) {
-              *reinterpret_cast<uint4*>(dst + cc * 16 + u) =
-                  make_uint4(pack_bf16x2(v[u], v[u + 1]), pack_bf16x2(v[u + 2], v[u + 3]),
-                             pack_bf16x2(v[u + 4], v[u + 5]), pack_bf16x2(v[u + 6], v[u + 7]));
+              *reinterpret_cast<uint4*>(dst[k] + cc * 32) =
+                  make_uint4(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), pack_bf16x2(v[4], v[5]), pack_bf16x2(v[6], v[7]));
             } else {
-              float4* po = reinterpret_cast<float4*>(f.part_o + slot * HD + cc * 16 + u);
-              po[0] = make_float4(v[u], v[u + 1], v[u + 2], v[u + 3]);
-              po[1] = make_float4(v[u + 4], v[u + 5], v[u + 6], v[u + 7]);
+              float4* p = reinterpret_cast<float4*>(po[k] + cc * 32);
+              p[0] = make_float4(v[0], v[1], v[2], v[3]);
+              p[1] = make_float4(v[4], v[5], v[6], v[7]);
             }
           }
         }
       }
-      if (!whole && row_ok && (two || x == 0)) f.part_ml[slot] = make_float2(m_all, l);
+      if (!whole && row_w + lane < pc->rows && (two || x == 0)) f.part_ml[slot0 + row_w + lane] = make_float2(m_all, l);
       tc_fence_before();
       mbar_arrive(bar(B_OFREE));
       nb += n;
@@ -1059,7 +1091,7 @@ __global__ void __launch_bounds__(256) k_kv8_join(ManyArgs f) {
     acc.x += v.x * k, acc.y += v.y * k, acc.z += v.z * k, acc.w += v.w * k;
   }
   const float inv = l == 0.f ? 0.f : 1.f / l;
-  const int i = (row0 + r) / a.G, hh = (row0 + r) - i * a.G;
+  const int i = f.node_of(row0 + r), hh = row0 + r - i * a.G;
   __nv_bfloat16* dst = a.out + (((size_t)b * a.n_pad + i) * a.H + gh * a.G + hh) * HD + 4 * lane;
   *reinterpret_cast<uint2*>(dst) =
       make_uint2(pack_bf16x2(acc.x * inv, acc.y * inv), pack_bf16x2(acc.z * inv, acc.w * inv));
@@ -1113,7 +1145,7 @@ fc_status kv8_attn_many(const Kv8Args& a, void* ws, size_t ws_bytes, cudaStream_
     return fc_cuda_status(cudaFuncSetAttribute(k_kv8_attn_many, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM_BYTES));
   });
   if (st != FC_OK) return st;
-  ManyArgs f{a, 0, 1, CUT_COST, rows_of_chunk(a.n_pad, a.G), nullptr, nullptr, nullptr};
+  ManyArgs f{a, 0, 1, CUT_COST, rows_of_chunk(a.n_pad, a.G), ((1u << 20) + a.G - 1) / a.G, nullptr, nullptr, nullptr};
   f.chunks = (a.n_pad * a.G + ROWS - 1) / ROWS;
   const long long units = (long long)a.B * a.Hkv * f.chunks;
   if (units > 0x7FFFFFFFll) return FC_ERR_UNSUPPORTED;
