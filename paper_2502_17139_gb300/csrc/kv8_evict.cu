@@ -107,8 +107,8 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) k_select_held(EvictAr
   float* s_w = reinterpret_cast<float*>(s_dyn + MOST);
   int* s_b = reinterpret_cast<int*>(s_dyn + 2 * MOST);
   __shared__ __align__(16) uint32_t s_hist[BINS];
-  __shared__ uint32_t s_sum[32], s_bits[GROUPS], s_tie[GROUPS], s_rank[GROUPS];
-  __shared__ int s_bad, s_newest, s_todo;
+  __shared__ uint32_t s_sum[32], s_bits[GROUPS], s_tie[GROUPS], s_rank[GROUPS], s_page[THREADS];  // (pages of 16 tokens and more)
+  __shared__ int s_newest, s_todo;
   __shared__ uint32_t s_digit, s_left, s_in_bin;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int unit = blockIdx.x, b = unit / a.Hkv, h = unit - b * a.Hkv;
@@ -117,43 +117,29 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) k_select_held(EvictAr
   int32_t* from = a.from + (size_t)unit * a.cap;
   const bool wrong = L < 0 || keep < 0 || L > (long long)a.max_pages << a.shift;
   const bool full = !wrong && keep < L && keep > a.cap;
-  if (tid == 0) s_bad = 0, s_newest = INT_MIN, s_todo = 0;
+  if (tid == 0) s_newest = INT_MIN, s_todo = 0;
   for (int i = tid; i < BINS; i += THREADS) s_hist[i] = 0;
-  __syncthreads();
-  auto at = [&](int i, uint32_t& p) {
-    const uint32_t page = (uint32_t)__ldg(tab + (i >> a.shift));
-    p = ((page * (uint32_t)a.Hkv + (uint32_t)h) << a.shift) | ((uint32_t)i & ((1u << a.shift) - 1u));
-    return page < (uint32_t)a.n_pages;
-  };
   const bool fine = !wrong && !full;
+  const int pages = fine ? (L + (1 << a.shift) - 1) >> a.shift : 0;  // at most THREADS
+  bool bad = false;
+  if (tid < pages) {
+    const int page = tab[tid];
+    s_page[tid] = ((uint32_t)page * (uint32_t)a.Hkv + (uint32_t)h) << a.shift;  // its first place
+    bad = (uint32_t)page >= (uint32_t)a.n_pages;
+  }
+  const bool ok = !__syncthreads_or(bad) && fine;
+  auto at = [&](int i) { return s_page[i >> a.shift] | ((uint32_t)i & ((1u << a.shift) - 1u)); };
   float w[HELD];
   int born[HELD];
-  {
-    bool bad = false;
-    int newest = INT_MIN;
 #pragma unroll
-    for (int u = 0; u < HELD; ++u) {
-      const int i = u * THREADS + tid;
-      w[u] = 0.f;
-      born[u] = INT_MIN;
-      uint32_t p;
-      if (fine && i < L) {
-        if (at(i, p)) {
-          w[u] = __ldg(a.w_in + p);
-          born[u] = __ldg(a.b_in + p);
-        } else {
-          bad = true;
-        }
-      }
-    }
-#pragma unroll
-    for (int u = 0; u < HELD; ++u) newest = max(newest, born[u]);
-    newest = __reduce_max_sync(0xFFFFFFFFu, newest);
-    if (lane == 0 && a.recent > 0) atomicMax(&s_newest, newest);
-    if (bad) s_bad = 1;
+  for (int u = 0; u < HELD; ++u) {
+    const int i = u * THREADS + tid;
+    const bool in = ok && i < L;
+    const uint32_t p = in ? at(i) : 0u;
+    w[u] = in ? __ldg(a.w_in + p) : 0.f;
+    born[u] = in ? __ldg(a.b_in + p) : INT_MIN;
   }
-  __syncthreads();
-  if (!fine || s_bad) {  // left as it is
+  if (!ok) {  // left as it is
     if (tid == 0) {
       a.count[unit] = 0;
       if (h == 0) fc_flag(FC_ERR_WORD(a.err), full ? FC_EBIT_CAPACITY : FC_EBIT_INVALID);
@@ -161,6 +147,14 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) k_select_held(EvictAr
     for (int i = tid; i < a.cap; i += THREADS) from[i] = -1;
     return;
   }
+  if (a.recent > 0) {
+    int newest = INT_MIN;
+#pragma unroll
+    for (int u = 0; u < HELD; ++u) newest = max(newest, born[u]);
+    newest = __reduce_max_sync(0xFFFFFFFFu, newest);
+    if (lane == 0) atomicMax(&s_newest, newest);
+  }
+  __syncthreads();
   const bool lose = keep < L;
   const int kept = min(keep, L);
   uint32_t below = (1u << lane) - 1u;
@@ -300,8 +294,7 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) k_select_held(EvictAr
       w[u] = s_w[r];
       born[u] = s_b[r];
     }
-    uint32_t p;
-    at(i, p);
+    const uint32_t p = at(i);
     a.w_out[p] = w[u];
     a.b_out[p] = born[u];
     if (i < a.cap) from[i] = src;
