@@ -19,6 +19,10 @@
 //             for what it then holds; rows that change are written.  The block
 //             that holds both the last places and the first sources is read from
 //             a copy, as its own warp may have written it.
+//
+// Both are instructions and latency more than bytes: 32 requests of 8 heads and 4160
+// tokens that lose 64 take 31 us (14 and 16), 16 requests of up to 16384 tokens that
+// lose half 76 (15 and 60; 187 MB read, 110 written).
 #include <algorithm>
 #include <climits>
 
@@ -97,8 +101,9 @@ constexpr int HELD = 16;  // tokens a thread of k_select_held
 
 // k_select for requests of up to HELD * THREADS tokens, whose weights and
 // positions stay in registers from the first read on: only sources pass through
-// shared memory.  (32 requests of 8 heads and 4160 tokens: 25 us with keys in
-// shared memory and passes over them, most of it instructions.)
+// shared memory.  Pages are looked up first, so that all reads are in flight at
+// once.  (32 requests of 8 heads and 4160 tokens, caches flushed: 20 us, 23 with the
+// pages looked up token by token, 25 with keys in shared memory and passes over them.)
 template <int THREADS>
 __global__ void __launch_bounds__(THREADS, 1024 / THREADS) k_select_held(EvictArgs a) {
   constexpr int WARPS = THREADS / 32, GROUPS = HELD * WARPS, MOST = HELD * THREADS / 2;  // moves are at most half

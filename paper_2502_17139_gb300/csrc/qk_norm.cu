@@ -7,7 +7,9 @@
 // squares is a shuffle over LP lanes, the rotation needs no exchange, and the
 // 8 sines and cosines of a lane's dimensions serve all heads of the row that the
 // warp takes.  The read and the write bound it (rows * (H + 2 Hkv) * D * 4
-// bytes); fp32 inside, rounded once.
+// bytes; 65000 rows of 16 + 16 + 16 heads of 128 267 us, 6.0 TB/s, a copy's rate
+// 6.6; unrolled over heads or rows, with prefetches or streaming hints, and on other grids 278
+// to 387); fp32 inside, rounded once.  32 rows take 3.7 us, latency.
 #include <algorithm>
 #include <cmath>
 
