@@ -1086,14 +1086,16 @@ def fc_qk_norm_rope(q, k, v, wq, wk, pos, base=10000.0, eps=1e-6, out=None):
     bf = torch.bfloat16
     if not (isinstance(q, torch.Tensor) and isinstance(k, torch.Tensor)):
         raise TypeError("q and k must be tensors")
-    B, n, H, D = q.shape if q.dim() == 4 else (0, 0, 0, 0)
     qs, ks, kshape = q.stride(), k.stride(), k.shape
-    if (B == 1 or n == 1 or H == 1 or kshape[-2] == 1) and len(ks) == len(qs) == 4:  # whose stride does not matter
+    if len(qs) != 4 or len(ks) != 4:
+        raise ValueError("q and k must be [B, n, heads, D]")
+    B, n, H, D = q.shape
+    if B == 1 or n == 1 or H == 1 or kshape[2] == 1:  # whose stride does not matter
         b, i = B > 1, n > 1
         qs, ks = (b and qs[0], i and qs[1], H > 1 and qs[2]), (b and ks[0], i and ks[1], kshape[2] > 1 and ks[2])
-    if not (q.dtype is bf and k.dtype is bf and q.is_cuda and k.is_cuda and len(kshape) == 4 and q.stride(3) == 1 and k.stride(3) == 1 and
+    if not (q.dtype is bf and k.dtype is bf and q.is_cuda and k.is_cuda and q.stride(3) == 1 and k.stride(3) == 1 and
             kshape[0] == B and kshape[1] == n and kshape[3] == D and
-            (v is None or (v.dtype is bf and v.is_cuda and v.shape == kshape and v.stride() == k.stride()))):  # one test for the usual case
+            (v is None or (isinstance(v, torch.Tensor) and v.dtype is bf and v.is_cuda and v.shape == kshape and v.stride() == k.stride()))):  # one test for the usual case
         for t, name in ((q, "q"), (k, "k")) + (((v, "v"),) if v is not None else ()):
             if not isinstance(t, torch.Tensor) or t.dtype is not bf:
                 raise TypeError(f"{name} must be a torch.bfloat16 tensor")
@@ -1261,6 +1263,8 @@ def fc_kv8_attn(q, cache: Kv8Cache, table, kv_len, k_new=None, v_new=None, mask=
     if out is None:
         out = torch.empty_like(q)
     new = (B, Hkv, Np, D)
+    if (k_new is None) != (v_new is None):
+        raise ValueError("k_new and v_new go together")
     if not (q.dtype is bf and out.dtype is bf and table.dtype is i32 and kv_len.dtype is i32 and q.is_cuda and out.is_cuda and
             table.is_cuda and kv_len.is_cuda and q.is_contiguous() and out.is_contiguous() and table.is_contiguous() and
             kv_len.is_contiguous() and out.shape == q.shape and table.dim() == 2 and table.shape[0] == B and kv_len.shape == (B,) and
@@ -1281,8 +1285,6 @@ def fc_kv8_attn(q, cache: Kv8Cache, table, kv_len, k_new=None, v_new=None, mask=
     kp = vp = mp = np_ = wp = None
     if k_new is not None:
         kp, vp = k_new.data_ptr(), v_new.data_ptr()
-    elif v_new is not None:
-        raise ValueError("k_new and v_new go together")
     if mask is not None:
         _need(mask, torch.int64, "mask", (B, Np, (Np + 63) // 64))
         mp = mask.data_ptr()
@@ -1338,7 +1340,8 @@ def fc_kv8_evict(cache: Kv8Cache, table, kv_len, keep, recent, track: Kv8Track, 
     elif not (workspace.is_cuda and workspace.is_contiguous()):
         raise ValueError("workspace must be a dense tensor on a CUDA device")
     _check("fc_kv8_evict", LIB.fc_kv8_evict(
-        cache.ref, table.data_ptr(), table.shape[1], kv_len.data_ptr(), keep.data_ptr(), B, int(recent), track.weight.data_ptr(),
+        cache.ref, table.data_ptr(), table.shape[1], kv_len.data_ptr(), keep.data_ptr(), B, max(-1, min(int(recent), 1 << 30)),
+        track.weight.data_ptr(),
         track.born.data_ptr(), track_out.weight.data_ptr(), track_out.born.data_ptr(), out.data_ptr(), out.shape[2],
         workspace.data_ptr(), workspace.numel() * workspace.element_size(), _stream()))
     return out

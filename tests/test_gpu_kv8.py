@@ -614,3 +614,28 @@ def test_evict_leaves_what_it_refuses(fc):
     assert np.array_equal(frm[3:].cpu().numpy(), ref)
     same_cache(got, good[1])
     assert np.array_equal(t_out.weight.cpu().numpy(), w0)
+
+
+def test_arguments_that_do_not_fit_are_refused(fc):
+    """Before anything runs: ranks, a missing partner, numbers past 32 bits."""
+    bf = torch.bfloat16
+    new = lambda *s: torch.zeros(s, dtype=bf, device="cuda")
+    ints = lambda *s: torch.zeros(s, dtype=torch.int32, device="cuda")
+    q, k, w, pos = new(1, 2, 4, 128), new(1, 2, 2, 128), new(128), ints(1, 2)
+    for bad in ((q[0], k, None), (q, k[0], None), (q, k[0, 0, 0], None), (q, k, new(1, 2, 2, 64)), (q, k[..., :64], None)):
+        with pytest.raises(ValueError):
+            fc.fc_qk_norm_rope(*bad, w, w, pos)
+    with pytest.raises(TypeError):
+        fc.fc_qk_norm_rope(q, k, [1], w, w, pos)
+    cache = fc.Kv8Cache.empty(2, 2, 16)
+    table, kv_len = ints(1, 2), ints(1)
+    kn = new(1, 2, 2, 128)
+    for pair in ((kn, None), (None, kn)):
+        with pytest.raises(ValueError):
+            fc.fc_kv8_attn(q, cache, table, kv_len, *pair)
+    now, then = fc.Kv8Track.empty(cache), fc.Kv8Track.empty(cache)
+    for recent in (-1, -(1 << 32), (1 << 22) + 1, 1 << 32):
+        with pytest.raises(fc.FastCoderError):
+            fc.fc_kv8_evict(cache, table, kv_len, kv_len, recent, now, then, cap=4)
+    with pytest.raises(fc.FastCoderError):  # the same arrays in and out
+        fc.fc_kv8_evict(cache, table, kv_len, kv_len, 0, now, now, cap=4)

@@ -135,3 +135,13 @@ def test_binding_refusals(fc):
         fc.fc_qk_norm_rope(x.float(), x, x, x, x, x)
     with pytest.raises(ValueError):
         fc.Kv8Cache.empty(2, 8, 64, device="cpu")
+
+
+def test_evict_refuses_more_places_than_it_counts(fc):
+    """d_from's places are counted in 32 bits: above 2^30 neither a workspace nor a call."""
+    L, nul = fc.LIB, None
+    cache = C.byref(fc.fc_kv8_cache(256, 256, 256, 256, 4, 16, 2, 128))
+    for cap in ((1 << 30) + 1, (1 << 31) - 16, (1 << 31) - 1):
+        assert L.fc_kv8_evict_workspace(1, 2, cap) == 0
+        assert L.fc_kv8_evict(cache, 256, 4, 256, 256, 1, 5, 256, 256, 512, 512, 256, cap, 256, 1 << 40, nul) == 2  # FC_ERR_UNSUPPORTED
+    assert L.fc_kv8_evict_workspace(1, 2, 1 << 30) > 2 << 32
