@@ -309,6 +309,25 @@ def test_attention(fc, kv, n, H, Hkv, page, workspace):
         assert torch.equal(call(fc, s, masks, workspace=ws), got)
 
 
+@pytest.mark.parametrize("workspace", [True, False])
+@pytest.mark.parametrize("new", [True, False])
+def test_attention_of_many_requests_of_all_sizes(fc, new, workspace):
+    """More units than CTAs: units of no rows, of 2 to 256, of no key, of new keys alone and of some blocks follow one another."""
+    rng = np.random.default_rng(31 + new)
+    nodes = [int(x) for x in rng.choice([0, 1, 8, 9, 31, 32, 33, 64, 65, 100, 128], 40)]
+    kv = [int(x) for x in rng.choice([0, 1, 16, 40, 127, 128, 129, 256, 290], 40)]
+    s = setup(rng, kv, 128, 16, 8, 16, nodes)
+    masks = trees(rng, nodes, 128)
+    ws = fc.kv8_attn_workspace(40, 128, 16, 8, "cuda") if workspace else None
+    got = call(fc, s, masks, new=new, workspace=ws)
+    assert fc.fc_get_error() == "FC_OK"
+    ref, tol, _, _ = reference(s, masks.view(np.uint64), D ** -0.5, new=new)
+    err = np.abs(num(got) - ref)
+    assert np.all(err <= tol), (err - tol).max()
+    for _ in range(3):
+        assert torch.equal(call(fc, s, masks, new=new, workspace=ws), got)
+
+
 @pytest.mark.parametrize("n,H,Hkv", [(1, 8, 2), (3, 4, 4), (64, 8, 2)])
 def test_attention_without_new_tokens_and_causal(fc, n, H, Hkv):
     rng = np.random.default_rng(n)
