@@ -77,8 +77,11 @@ constexpr float RESCALE_THRESHOLD = 8.f;  // O is rescaled when a row's maximum 
 constexpr int E_TOP = 7;  // a query row's largest value, 16 new keys' largest, is put at 2^7..2^8
 constexpr float M_START = -1e30f;  // a reference before any key
 // Exponents below count as this, so that the product of two is no fp32
-// underflow; such scores are 0 to fp32 all the same.
+// underflow; such scores are 0 to fp32 all the same.  And what a score is
+// multiplied by is at least FACTOR_MIN (a block of zeros has scale 2^-120, a row
+// of zeros 2^E_MIN): a factor of 0 would make NaN of masked scores, -infinity.
 constexpr int E_MIN = -50;
+constexpr float FACTOR_MIN = 0x1p-126f;
 // A unit's start and end in blocks of one tile: 4 where a unit is cut over CTAs (3
 // requests of 128 nodes, 32 heads of their own, over 3000 keys 36 us, with 8 39), 7
 // where a CTA has several (16 ragged trees of 64 nodes 121 us, with 12 128).  And
@@ -146,6 +149,11 @@ __device__ __forceinline__ uint64_t f2_fma(uint64_t a, uint64_t b, uint64_t c) {
 __device__ __forceinline__ uint64_t f2_add(uint64_t a, uint64_t b) {
   uint64_t d;
   asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+  return d;
+}
+__device__ __forceinline__ float max_nan(float a, float b) {  // NaN of either
+  float d;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(d) : "f"(a), "f"(b));
   return d;
 }
 __device__ __forceinline__ float max3(float a, float b, float c) {
@@ -866,7 +874,7 @@ __global__ void __launch_bounds__(THREADS, 1) k_kv8_attn_many(const __grid_const
       if (n == 0) break;
       float m = M_START, l = 0.f;  // m: the reference
       if (!(ok = warp_wait(bar(B_QE + np % PIECES), (np / PIECES) & 1, &s_abort))) break;
-      const float c_row = a.scale_log2 * reinterpret_cast<const float*>(smem + OFF_QE)[np % PIECES * ROWS + row_of(pc)];
+      const float c_row = fmaxf(a.scale_log2 * reinterpret_cast<const float*>(smem + OFF_QE)[np % PIECES * ROWS + row_of(pc)], FACTOR_MIN);
       const int every = pc->two ? 1 : 2, first = pc->two ? 0 : x, n_cached = pc->cached - pc->s0;
       const bool idle = row_of(pc) - lane >= pc->rows;  // none of the warp's rows is in use
 #pragma unroll 1
@@ -950,7 +958,7 @@ __global__ void __launch_bounds__(THREADS, 1) k_kv8_attn_many(const __grid_const
           const float2 bk = back[q];
 #pragma unroll
           for (int u = 0; u < 16; ++u) {
-            const float cz = c_row * (u < 8 ? bk.x : bk.y);
+            const float cz = max_nan(c_row * (u < 8 ? bk.x : bk.y), FACTOR_MIN);
             float p0, p1;
             f2_unpack(f2_fma(f2_pack(__uint_as_float(sv[2 * u]), __uint_as_float(sv[2 * u + 1])), f2_pack(cz, cz), neg), p0, p1);
             p0 = exp2_fast(p0), p1 = exp2_fast(p1);

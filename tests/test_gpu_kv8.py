@@ -419,6 +419,27 @@ def test_attention_subnormal_and_largest_numbers(fc, n, H, Hkv):
     assert np.all(np.abs(num(got) - ref) <= tol)
 
 
+@pytest.mark.parametrize("n,H,Hkv", [(1, 8, 2), (4, 8, 2), (20, 4, 4), (128, 8, 2)])
+@pytest.mark.parametrize("tiny", [0.0, 2.0 ** -40])
+def test_attention_of_rows_and_keys_that_are_zero(fc, n, H, Hkv, tiny):
+    """A padded batch: queries of zeros (or next to it) beside others, keys of zeros, whose blocks have the smallest
+    scale, with places past the end in the same block."""
+    rng = np.random.default_rng(12)
+    s = setup(rng, [5, 40, 131, 300], n, H, Hkv, 16)
+    for b, L in enumerate(s["kv"]):
+        i = np.arange(L)
+        p, o = s["table"][b][i // 16], i % 16
+        zero = (i // 16) % 2 == 0
+        s["cache"][0][p[zero], :, o[zero]] = 0
+        s["cache"][2][p[zero], :, 0] = 2.0 ** -120
+    s["q"][:, ::2] *= tiny
+    s["k"][1:3] = 0
+    got = call(fc, s, workspace=fc.kv8_attn_workspace(4, n, H, Hkv, "cuda"))
+    ref, tol, _, _ = reference(s, None, D ** -0.5, causal=True)
+    assert np.all(np.abs(num(got) - ref) <= tol)
+    assert fc.fc_get_error() == "FC_OK"
+
+
 @pytest.mark.parametrize("n,H,Hkv", [(1, 8, 2), (64, 4, 2)])
 def test_attention_many_small_weights_beside_a_large_one(fc, n, H, Hkv):
     """One key 14 above thousands of others that together outweigh it."""
