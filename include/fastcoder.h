@@ -818,7 +818,7 @@ fc_status fc_w4_matvec(const void* d_x, const void* d_codes, const void* d_scale
  * scale NaN: the block stands for NaN.
  * ------------------------------------------------------------------------ */
 typedef struct {
-  void* k_codes;     /* device, [n_pages][Hkv][page_size][D] e4m3 bytes, 16-byte aligned */
+  void* k_codes;     /* device, [n_pages][Hkv][page_size][D] e4m3 bytes, 32-byte aligned */
   void* v_codes;     /* (0x7F and 0xFF, e4m3's NaN, are not written and not expected) */
   float* k_scale;    /* device, [n_pages][Hkv][page_size / 16] powers of two, 2^-120 to 2^120, or NaN */
   float* v_scale;

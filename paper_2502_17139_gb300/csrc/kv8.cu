@@ -169,7 +169,7 @@ fc_status fc_kv8_check(const fc_kv8_cache* c) {
   if (c->D != HD || kv8_page_shift(c->page_size) < 0 || (long long)c->n_pages * c->page_size > 0x7FFFFFFFll ||
       (long long)c->n_pages * c->page_size * c->Hkv > 0x7FFFFFFFll)  // rows are counted in 32 bits (256 GB of codes)
     return FC_ERR_UNSUPPORTED;
-  if (!c->k_codes || !c->v_codes || !c->k_scale || !c->v_scale || !kv8_aligned(c->k_codes, 16) || !kv8_aligned(c->v_codes, 16) ||
+  if (!c->k_codes || !c->v_codes || !c->k_scale || !c->v_scale || !kv8_aligned(c->k_codes, 32) || !kv8_aligned(c->v_codes, 32) ||
       !kv8_aligned(c->k_scale, 4) || !kv8_aligned(c->v_scale, 4))
     return FC_ERR_INVALID_ARG;
   return FC_OK;

@@ -236,6 +236,12 @@ __device__ __forceinline__ void cp_async_wait() {
   asm volatile("cp.async.wait_group %0;\n" ::"n"(N) : "memory");
 }
 __device__ __forceinline__ void cp_async_wait_all() { asm volatile("cp.async.wait_all;\n" ::: "memory"); }
+// 32 bytes at once (by 16 each sector is asked for twice: 16 ragged trees of 64 nodes 121 us instead of 117)
+__device__ __forceinline__ void ld_global32(uint4& a, uint4& b, const void* p) {
+  asm volatile("ld.global.v8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
+               : "=r"(a.x), "=r"(a.y), "=r"(a.z), "=r"(a.w), "=r"(b.x), "=r"(b.y), "=r"(b.z), "=r"(b.w)
+               : "l"(p));
+}
 __device__ __forceinline__ void prefetch_l2(const void* p) { asm volatile("prefetch.global.L2 [%0];" ::"l"(p)); }
 __device__ __forceinline__ float pow2i(int e) { return __uint_as_float((uint32_t)(e + 127) << 23); }  // -126 <= e <= 127
 __device__ __forceinline__ float lo_f(uint32_t w) { return __uint_as_float(w << 16); }
@@ -669,11 +675,9 @@ __global__ void __launch_bounds__(THREADS, 1) k_kv8_attn_many(const __grid_const
     const uint32_t* runs = reinterpret_cast<const uint32_t*>(smem + OFF_RUN) + w;
     const float* vscales = reinterpret_cast<const float*>(smem + OFF_VS) + w;
     auto fetch = [&](uint32_t run) {
-      const uint4* src = reinterpret_cast<const uint4*>(a.vc + (uint64_t)run * 2048u) + rho * 8 + 2 * c;
-      vr[0] = src[0];
-      vr[1] = src[1];
-      vr[2] = src[64];
-      vr[3] = src[65];
+      const uint8_t* src = a.vc + (uint64_t)run * 2048u + rho * 128 + 32 * c;
+      ld_global32(vr[0], vr[1], src);
+      ld_global32(vr[2], vr[3], src + 8 * 128);
     };
     // The piece's queries, a row 16 lanes: all of them asked for at once, a chunk of
     // 8 values in two halves, each where a part of the chunk will be.  Rows past

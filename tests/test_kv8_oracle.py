@@ -145,3 +145,14 @@ def test_evict_refuses_more_places_than_it_counts(fc):
         assert L.fc_kv8_evict_workspace(1, 2, cap) == 0
         assert L.fc_kv8_evict(cache, 256, 4, 256, 256, 1, 5, 256, 256, 512, 512, 256, cap, 256, 1 << 40, nul) == 2  # FC_ERR_UNSUPPORTED
     assert L.fc_kv8_evict_workspace(1, 2, 1 << 30) > 2 << 32
+
+
+@pytest.mark.parametrize("field,offset", [("k_codes", 16), ("v_codes", 16), ("k_codes", 8), ("v_codes", 1), ("k_scale", 2), ("v_scale", 2)])
+def test_a_cache_off_its_alignment_is_refused(fc, field, offset):
+    """Numbers at multiples of 32 bytes, scales of 4: rows are read 32 bytes at a time."""
+    at = dict(k_codes=256, v_codes=256, k_scale=256, v_scale=256)
+    for shift, want in ((0, 0), (offset, 1)):
+        c = dict(at)
+        c[field] += shift
+        cache = C.byref(fc.fc_kv8_cache(c["k_codes"], c["v_codes"], c["k_scale"], c["v_scale"], 4, 16, 2, 128))
+        assert fc.LIB.fc_kv8_read(cache, None, 0, None, None, None) == want
