@@ -561,23 +561,23 @@ __global__ void __launch_bounds__(MV_THREADS, 5) k_move(EvictArgs a) {
       }
     }
     if (x + step < n) mine_next = source(base_next);
-    // The largest magnitude, in fp16 relative to the largest scale: exact where it counts, as nothing
-    // below 2^-14 of that scale is the largest unless the block calls for a far smaller one.
+    // The largest magnitude: the seven bits of a number's are 8 E + m, of (1 + m / 8) 2^(E - 7) from 8 on, so
+    // that 2^-d times it has them less 8 d.  (Below 8, subnormal, it is less than that says: none of these is
+    // the largest beside one of 8 or more.)  Two in 16 bits each, 0x4000 added.
     const bool nan = __any_sync(0xFFFFFFFFu, l16 < live && kv8_nan(row_scale));
     const int row_e = l16 < live ? min(max(kv8_exp(row_scale), KV8_MIN_EXP), KV8_MAX_EXP) : KV8_MIN_EXP;
     const int ref = __reduce_max_sync(0xFFFFFFFFu, row_e);
-    const uint32_t to_ref = l16 < live ? half2_bits(kv8_half_pow2(row_e - ref)) : 0u;  // (a NaN is no maximum)
-    __half2 top2 = __float2half2_rn(0.f);
+    const uint32_t bias = l16 < live ? 0x40004000u - (uint32_t)(ref - row_e) * 0x00080008u : 0u;
+    uint32_t top2 = 0;
 #pragma unroll
-    for (int j = 0; j < KV8_BLOCK; ++j) {
-      const __half2 f = bits_half2(__shfl_sync(0xFFFFFFFFu, to_ref, j));
-      top2 = __hmax2(top2, __hmax2(__habs2(__hmul2(e4m3x2_halves(w[j] & 0xFFFFu), f)), __habs2(__hmul2(e4m3x2_halves(w[j] >> 16), f))));
-    }
-    // magnitudes order like their bits
-    float top = __uint_as_float(__reduce_max_sync(0xFFFFFFFFu, __float_as_uint(fmaxf(__low2float(top2), __high2float(top2)))));
-    int e = max(kv8_exp_for(top) + ref, KV8_MIN_EXP);
-    if (ref - e > 10) {  // from the numbers themselves, times 2^-6 so that none overflows
-      top = 0.f;
+    for (int j = 0; j < KV8_BLOCK; ++j)
+      top2 = __vmaxu2(top2, __vmaxu2(w[j] & 0x007F007Fu, (w[j] >> 8) & 0x007F007Fu) + __shfl_sync(0xFFFFFFFFu, bias, j));
+    const int bits = (int)__reduce_max_sync(0xFFFFFFFFu, max(top2 & 0xFFFFu, top2 >> 16)) - 0x4000;
+    int e;  // the smallest with (1 + m / 8) 2^(E - 7) 2^ref <= 1.75 * 2^(e + 8)
+    if (bits >= 8) {
+      e = max(ref + (bits >> 3) - 15 + ((bits & 7) == 7 ? 1 : 0), KV8_MIN_EXP);
+    } else {  // from the numbers themselves, times 2^-6 so that none overflows
+      float top = 0.f;
 #pragma unroll
       for (int j = 0; j < KV8_BLOCK; ++j) {
         const float s = kv8_pow2(__shfl_sync(0xFFFFFFFFu, row_e, j) - 6);
@@ -589,15 +589,16 @@ __global__ void __launch_bounds__(MV_THREADS, 5) k_move(EvictArgs a) {
     }
     const int d = nan ? 0 : row_e - e;
     const uint32_t by = half2_bits(kv8_half_pow2(d));
-    const uint32_t put = (moved | __ballot_sync(0xFFFFFFFFu, d != 0)) & ((1u << live) - 1u);  // rows that change
+    const uint32_t again = __ballot_sync(0xFFFFFFFFu, d != 0);                // rows of another scale, rounded again
+    const uint32_t put = (moved | again) & ((1u << live) - 1u);  // rows that change
     const bool large = __any_sync(0xFFFFFFFFu, l16 < live && d > 15);
     uint32_t* out = reinterpret_cast<uint32_t*>(codes + (size_t)to * HD) + lane;
 #pragma unroll
     for (int j = 0; j < KV8_BLOCK; ++j) {
-      const __half2 f = bits_half2(__shfl_sync(0xFFFFFFFFu, by, j));
-      uint32_t r = kv8_times4(w[j], f);
-      if (large) r = kv8_rescale4(w[j], __shfl_sync(0xFFFFFFFFu, d, j));
-      if ((put >> j) & 1u) out[j * 32] = r;
+      if (!((put >> j) & 1u)) continue;
+      uint32_t r = w[j];
+      if ((again >> j) & 1u) r = large ? kv8_rescale4(r, __shfl_sync(0xFFFFFFFFu, d, j)) : kv8_times4(r, bits_half2(__shfl_sync(0xFFFFFFFFu, by, j)));
+      out[j * 32] = r;
     }
     if (lane == 0) scales[to >> 4] = nan ? __uint_as_float(0x7FC00000u) : kv8_pow2(e);
   }
