@@ -29,8 +29,8 @@
 // The CTAs (one an SM) share all units' blocks equally, cut anywhere; a cut
 // unit's pieces go through the workspace to k_kv8_join.
 // Several roles run at once from one instruction cache, so the loops are short.
-// Measured: 32 trees of 128 nodes, 4 query heads a kv head, over 16384 keys 898 us (1225
-// TFLOP/s), 16 ragged trees of 64 nodes, a kv head a query head, 120 us.  What bounds it is a
+// Measured: 32 trees of 128 nodes, 4 query heads a kv head, over 16384 keys 893 us (1231
+// TFLOP/s), 16 ragged trees of 64 nodes, a kv head a query head, 117 us.  What bounds it is a
 // block's chain: of 4.0 K cycles a block of two tiles, a tile's weights take 2.3 K (a warp's instructions one
 // after another, not a pipe), its products 1.0 K, hand-overs the rest; the tiles run side by side.
 // Every mbarrier wait is bounded: one that runs out raises FC_ERR_TIMEOUT, the

@@ -21,8 +21,8 @@
 //             a copy, as its own warp may have written it.
 //
 // Both are instructions and latency more than bytes: 32 requests of 8 heads and 4160
-// tokens that lose 64 take 31 us (14 and 16), 16 requests of up to 16384 tokens that
-// lose half 76 (15 and 60; 187 MB read, 110 written).
+// tokens that lose 64 take 30 us (14 and 15), 16 requests of up to 16384 tokens that
+// lose half 72 (15 and 56; 187 MB read, 110 written).
 #include <algorithm>
 #include <climits>
 
@@ -522,6 +522,8 @@ __global__ void __launch_bounds__(SEL_THREADS) k_select(EvictArgs a, int held_ca
   for (int i = keep + tid; i < a.cap; i += threads) from[i] = -1;
 }
 
+// Registers bound how many blocks are in flight (5 CTAs an SM at 48: half of 16 x
+// 16384 tokens 72 us, 4 81, 6 with spills 82), instructions what a block takes.
 __global__ void __launch_bounds__(MV_THREADS, 5) k_move(EvictArgs a) {
   const int lane = threadIdx.x & 31, l16 = lane & 15, half = (threadIdx.x >> 5) & 1;
   const int unit = blockIdx.x, n = a.count[unit];
