@@ -884,6 +884,7 @@ fc_status fc_kv8_read(const fc_kv8_cache* cache, const int32_t* d_slot, int rows
  *             is there.  For up to 16 rows a kv head (n_pad * H / Hkv, else
  *             FC_ERR_UNSUPPORTED), batch * Hkv <= 65535, with a workspace made
  *             for weight_keys = max_pages * page_size (else FC_ERR_WORKSPACE).
+ *             Requests then share no page.
  * Sums, scales and the softmax are fp32.  What the tensor cores multiply is
  * rounded so:
  *   up to 16 rows a kv head: cached numbers exact; queries fp16 relative to the

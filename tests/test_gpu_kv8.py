@@ -615,6 +615,39 @@ def test_evict(fc, kv, keep, recent, H, page):
     assert np.array_equal(t_in.weight.cpu().numpy(), w, equal_nan=True)
 
 
+def test_a_captured_eviction_is_good_for_other_lengths(fc):
+    """A graph of an eviction, captured on another stream, replayed over other caches, lengths and budgets, zero and nothing to do among them."""
+    H, page, cap = 2, 32, 200
+    kv = [500, 300]
+    s = setup(np.random.default_rng(3), kv, 1, H, H, page, stale=False)
+    got = on_gpu(fc, s["cache"])
+    tracks = [fc.Kv8Track.empty(got) for _ in range(2)]
+    table, lens, keep = dev(s["table"]), dev(s["kv"]), dev(np.array([200, 100], np.int32))
+    out = torch.empty((2, H, cap), dtype=torch.int32, device="cuda")
+    ws = fc.kv8_evict_workspace(2, H, cap, "cuda")
+    run = lambda: fc.fc_kv8_evict(got, table, lens, keep, 10, *tracks, out=out, workspace=ws)
+    run()
+    torch.cuda.synchronize()
+    graph, side = torch.cuda.CUDAGraph(), torch.cuda.Stream()
+    with torch.cuda.graph(graph, stream=side):
+        run()
+    for i, (L, K) in enumerate((([500, 300], [199, 1]), ([0, 17], [0, 16]), ([480, 290], [0, 290]), ([33, 256], [32, 128]))):
+        rng = np.random.default_rng(40 + i)
+        cache = random_cache(rng, got.n_pages, H, page)
+        w = np.exp(rng.standard_normal((got.n_pages, H, page))).astype(np.float32)
+        born = rng.permutation(w.size).reshape(w.shape).astype(np.int32)
+        w0, b0 = np.zeros_like(w), np.zeros_like(born)
+        for d, h in zip((got.k_codes, got.v_codes, got.k_scale, got.v_scale, tracks[0].weight, tracks[0].born, tracks[1].weight, tracks[1].born, lens, keep),
+                        cache + [w, born, w0, b0, np.array(L, np.int32), np.array(K, np.int32)]):
+            d.copy_(torch.from_numpy(h))
+        graph.replay()
+        ref = o8.evict(cache, s["table"], np.array(L), K, 10, [w, born], [w0, b0], cap)
+        assert np.array_equal(out.cpu().numpy(), ref)
+        same_cache(got, cache)
+        assert np.array_equal(tracks[1].weight.cpu().numpy(), w0) and np.array_equal(tracks[1].born.cpu().numpy(), b0)
+    assert fc.fc_get_error() == "FC_OK"
+
+
 def test_evict_long_request(fc):
     """More tokens than the keys' place in shared memory holds."""
     rng = np.random.default_rng(20)
@@ -654,6 +687,40 @@ def test_evict_leaves_what_it_refuses(fc):
     assert np.array_equal(frm[3:].cpu().numpy(), ref)
     same_cache(got, good[1])
     assert np.array_equal(t_out.weight.cpu().numpy(), w0)
+
+
+def test_pages_past_four_gigabytes(fc):
+    """The last pages of a pool of 5.2 GB of keys and as much of values do as those of a small one."""
+    rng = np.random.default_rng(17)
+    P, H, page = 40000, 8, 128
+    s = setup(rng, [700, 129, 0], 40, 16, H, page, stale=False)
+    few = on_gpu(fc, s["cache"])
+    n = few.n_pages
+    big = fc.Kv8Cache.empty(P, H, page)
+    last = slice(P - n, P)
+    for x in ("k_codes", "v_codes", "k_scale", "v_scale"):
+        getattr(big, x)[last].copy_(getattr(few, x))
+    tables = [dev(s["table"]), dev(np.where(s["table"] >= 0, s["table"] + P - n, s["table"]).astype(np.int32))]
+    tracks = [[fc.Kv8Track.empty(c) for _ in range(2)] for c in (few, big)]
+    born = rng.permutation(n * H * page).reshape(n, H, page).astype(np.int32)
+    tracks[0][0].born.copy_(dev(born))
+    tracks[1][0].born[last].copy_(dev(born))
+    kv, q, k, v = dev(s["kv"]), s["q"].cuda(), s["k"].cuda(), s["v"].cuda()
+    keep = dev(np.array([300, 128, 0], np.int32))
+    slots = torch.from_numpy(s["table"][[0, 0, 1]][:, 0] * page + np.array([1, 30, 3])).int().cuda()
+    got = []
+    for c, table, (now, then), off in zip((few, big), tables, tracks, (0, (P - n) * page)):
+        ws = fc.kv8_attn_workspace(3, 40, 16, H, "cuda")
+        out = [fc.fc_kv8_attn(q, c, table, kv, k, v, workspace=ws)]
+        ws = fc.kv8_attn_workspace(3, 1, 16, H, "cuda", table.shape[1] * page)
+        out.append(fc.fc_kv8_attn(q[:, :1].contiguous(), c, table, kv, workspace=ws, weight=now.weight))
+        out += [now.weight[c.n_pages - n:].clone(), fc.fc_kv8_evict(c, table, kv, keep, 20, now, then, cap=300)]
+        fc.fc_kv8_write(c, k[:, :, 0], v[:, :, 0], slots + off, track=then, pos=slots)
+        out += [*fc.fc_kv8_read(c, slots + off), then.weight[c.n_pages - n:], then.born[c.n_pages - n:]]
+        got.append(out + [getattr(c, x)[c.n_pages - n:] for x in ("k_codes", "v_codes", "k_scale", "v_scale")])
+    assert fc.fc_get_error() == "FC_OK"
+    assert all(torch.equal(x, y) for x, y in zip(*got))
+    assert got[1][2].any() and (got[1][3] >= 0).any() and got[1][4].any()
 
 
 def test_arguments_that_do_not_fit_are_refused(fc):
