@@ -401,6 +401,30 @@ def test_attention_scales_far_apart(fc, n, H, Hkv):
     assert np.all(np.abs(num(got) - ref) <= tol)
 
 
+@pytest.mark.parametrize("n,H,Hkv", [(1, 8, 2), (4, 2, 2), (2, 16, 2), (40, 4, 2)])
+@pytest.mark.parametrize("kv", [[300, 90], [3000, 17]])
+def test_attention_scales_as_far_apart_as_they_may_be(fc, kv, n, H, Hkv):
+    """Value scales of 2^-80 to 2^90 side by side: a row's sum and its output may be 2^170 apart."""
+    rng = np.random.default_rng(19)
+    s = setup(rng, kv, n, H, Hkv, 32, stale=False)
+    s["cache"][3][:] = (2.0 ** rng.choice([-80, -79, 0, 60, 89, 90], s["cache"][3].shape)).astype(np.float32)
+    got = call(fc, s, workspace=fc.kv8_attn_workspace(2, n, H, Hkv, "cuda"))
+    ref, tol, _, _ = reference(s, None, D ** -0.5, causal=True)
+    # up to 16 rows: a weight times its value scale is fp16, its error at most 2^-36 of the row's largest (at
+    # least 2^11 where a subnormal step is 2^-24), times numbers of up to 448
+    for b, L in enumerate(s["kv"]):
+        i = np.arange(L)
+        for h in range(H):
+            g = h // (H // Hkv)
+            K = np.concatenate((o8.cached(s["cache"], 0, s["table"][b], L, g), num(s["k"][b, g])))
+            scales = np.concatenate((s["cache"][3][s["table"][b][i // 32], g, i % 32 // 16], np.ones(n)))
+            for r in range(n):
+                z = K[:L + r + 1] @ num(s["q"][b, r, h]) * D ** -0.5
+                p = np.exp(z - z.max())
+                tol[b, r, h] += (p / p.sum() * scales[:L + r + 1]).max() * 448 * 2.0 ** -36 * (L + r + 1)
+    assert np.all(np.abs(num(got) - ref) <= tol)
+
+
 @pytest.mark.parametrize("n,H,Hkv", [(1, 8, 2), (40, 4, 2)])
 def test_attention_subnormal_and_largest_numbers(fc, n, H, Hkv):
     """Every e4m3 number: keys and values of each byte, e4m3's subnormal ones among them."""
