@@ -884,7 +884,9 @@ fc_status fc_kv8_read(const fc_kv8_cache* cache, const int32_t* d_slot, int rows
  *             is there.  For up to 16 rows a kv head (n_pad * H / Hkv, else
  *             FC_ERR_UNSUPPORTED), batch * Hkv <= 65535, with a workspace made
  *             for weight_keys = max_pages * page_size (else FC_ERR_WORKSPACE).
- *             Requests then share no page.
+ *             Requests then share no page.  Values have no part in it: a row
+ *             that a value makes NaN weighs its tokens as it does without; a
+ *             row with a NaN among its scores makes all its weights NaN.
  * Sums, scales and the softmax are fp32.  What the tensor cores multiply is
  * rounded so:
  *   up to 16 rows a kv head: cached numbers exact; queries fp16 relative to the

@@ -614,12 +614,21 @@ __global__ void __launch_bounds__(FEW_THREADS, FEW_CTAS) k_kv8_attn_few(FewArgs 
         }
       }
       bad = __reduce_or_sync(0xFFFFFFFFu, bad);
-      if (bad) {
+      if (bad) {  // NaN in the rows' sums of values, not in their sums of powers, which the weights go by
+        uint32_t rows_bad = 0;
 #pragma unroll
         for (int n = 0; n < NT; ++n)
 #pragma unroll
           for (int c = 0; c < 4; ++c)
-            if (((seen >> (4 * n + c)) & 1u) && ((bad >> (g + 8 * (c >> 1))) & 1u)) l[n][c & 1] = __uint_as_float(0x7FC00000u);
+            if (((seen >> (4 * n + c)) & 1u) && ((bad >> (g + 8 * (c >> 1))) & 1u)) rows_bad |= 1u << (8 * n + 2 * t + (c & 1));
+        rows_bad = __reduce_or_sync(0xFFFFFFFFu, rows_bad);
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+          for (int r = 0; r < 2; ++r)
+            if ((rows_bad >> (8 * n + 2 * t + r)) & 1u)
+#pragma unroll
+              for (int mt = 0; mt < 8; ++mt) o[n][mt][r] = o[n][mt][2 + r] = __uint_as_float(0x7FC00000u);
       }
     }
 

@@ -770,3 +770,26 @@ def test_arguments_that_do_not_fit_are_refused(fc):
             fc.fc_kv8_evict(cache, table, kv_len, kv_len, recent, now, then, cap=4)
     with pytest.raises(fc.FastCoderError):  # the same arrays in and out
         fc.fc_kv8_evict(cache, table, kv_len, kv_len, 0, now, now, cap=4)
+
+
+@pytest.mark.parametrize("n,H,Hkv", [(1, 8, 2), (3, 4, 1), (16, 1, 1)])
+@pytest.mark.parametrize("kv", [[200, 70], [9000, 40]])
+def test_weights_do_not_depend_on_new_values(fc, kv, n, H, Hkv):
+    """New tokens whose values are not finite: the rows that see them are NaN, the weights of the cached tokens what
+    they are without, bit for bit."""
+    rng = np.random.default_rng(21)
+    s = setup(rng, kv, n, H, Hkv, 32)
+    masks = trees(rng, [n] * 2, n)
+    ws = fc.kv8_attn_workspace(2, n, H, Hkv, "cuda", s["table"].shape[1] * 32)
+    before = dev(rng.random(s["cache"][0].shape[:3]).astype(np.float32))
+    clean, weight = before.clone(), before.clone()
+    ok = call(fc, s, masks, workspace=ws, weight=clean, decay=0.5)
+    s["v"][0, Hkv - 1, 0, 5] = float("nan")  # the root, which every row sees
+    s["v"][1, 0, n - 1, 3] = float("inf")
+    got = call(fc, s, masks, workspace=ws, weight=weight, decay=0.5)
+    assert torch.equal(weight, clean)
+    want = torch.zeros(2, n, H, dtype=torch.bool)
+    want[0, :, -(H // Hkv):] = True
+    want[1, :, :H // Hkv] = torch.from_numpy((masks[1, :, 0] >> (n - 1)) & 1 == 1)[:, None]
+    assert torch.equal(got.isnan().all(-1).cpu(), want) and torch.equal(got[~want.cuda()], ok[~want.cuda()])
+    assert fc.fc_get_error() == "FC_OK"
