@@ -422,7 +422,10 @@ __global__ void __launch_bounds__(FEW_THREADS, FEW_CTAS) k_kv8_attn_few(FewArgs 
         for (int r = 0; r < 2; ++r) {
           float top = M_START;
 #pragma unroll
-          for (int i = 0; i < 4; ++i) top = fmaxf(top, fmaf(d[i][r], ks[i], (float)(max(expo(vs[i]), VS_MIN_EXP) - 11)));
+          for (int i = 0; i < 4; ++i) {
+            const int e = expo(vs[i]);  // 128: NaN, whose row is NaN whatever the reference; its powers still count
+            top = fmaxf(top, fmaf(d[i][r], ks[i], (float)((e == 128 ? VS_MIN_EXP : max(e, VS_MIN_EXP)) - 11)));
+          }
 #pragma unroll
           for (int x = 4; x < 32; x <<= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, x));
           const float mn = fmaxf(m[n][r], top), al = exp2_fast(m[n][r] - mn);

@@ -793,3 +793,25 @@ def test_weights_do_not_depend_on_new_values(fc, kv, n, H, Hkv):
     want[1, :, :H // Hkv] = torch.from_numpy((masks[1, :, 0] >> (n - 1)) & 1 == 1)[:, None]
     assert torch.equal(got.isnan().all(-1).cpu(), want) and torch.equal(got[~want.cuda()], ok[~want.cuda()])
     assert fc.fc_get_error() == "FC_OK"
+
+
+@pytest.mark.parametrize("n,H,Hkv", [(1, 8, 2), (3, 4, 1), (16, 1, 1)])
+@pytest.mark.parametrize("kv", [[200, 70], [9000, 40]])
+def test_weights_beside_cached_values_that_stand_for_nan(fc, kv, n, H, Hkv):
+    """Blocks whose value scale is NaN: the rows of their request and head are NaN, the weights those of the scores,
+    which spread far here (queries times 2)."""
+    rng = np.random.default_rng(22)
+    s = setup(rng, kv, n, H, Hkv, 32)
+    s["q"] = s["q"] * 2
+    ws = fc.kv8_attn_workspace(2, n, H, Hkv, "cuda", s["table"].shape[1] * 32)
+    _, _, want, bound = reference(s, None, D ** -0.5, causal=True)
+    for t in range(0, kv[0] // 32, 3):
+        s["cache"][3][s["table"][0][t], 0, t % 2] = np.nan
+    s["cache"][3][s["table"][1][0], Hkv - 1, 1] = np.nan
+    weight = torch.zeros(s["cache"][0].shape[:3]).cuda()
+    got = call(fc, s, workspace=ws, weight=weight, decay=0.0)
+    assert np.all(np.abs(num(weight) - want) <= bound)
+    G = H // Hkv
+    nan = got.isnan().all(-1)
+    assert nan[0, :, :G].all() and nan[1, :, -G:].all() and nan.sum() == 2 * n * G
+    assert fc.fc_get_error() == "FC_OK"
