@@ -854,9 +854,10 @@ fc_status fc_qk_norm_rope(const void* d_q, int64_t q_seq_stride, int64_t q_row_s
 /*
  * Rounds rows of keys and values into the cache: fc_kv4_write's arguments, and
  * one more rule, as a block's rows share a scale.  The rows of a call that go
- * to one block of 16 lie within 32 rows of one another (left out rows may stand
- * between; fc_kv_pages_plan's are neighbours), and what the block holds before
- * the first of their places is kept, what it holds from there on is not
+ * to one block of 16 are at most 32 rows apart (row r and row r + 32 still are;
+ * left out rows may stand between; fc_kv_pages_plan's are neighbours; what a
+ * block with rows further apart holds is not defined), and what the block holds
+ * before the first of their places is kept, what it holds from there on is not
  * expected to be.
  * With d_weight and d_born (both or none, [n_pages][Hkv][page_size]) the rows'
  * places get weight 0 and position d_pos[r] there, for fc_kv8_attn and

@@ -33,7 +33,7 @@ struct Kv8Write {
 };
 
 // A warp takes `per` neighbouring rows of one head, keys or values.  A row begins a run when
-// none of the WINDOW rows before it goes to its block of 16; the run's rows are
+// none of the WINDOW rows before it goes to its block of 16; the run's rows are it and
 // those of the next WINDOW that do.  So the warp that meets a run's first row
 // knows the whole block's new tokens, and no two warps write one block.
 // Four dimensions a lane, the block's 16 places at once: their largest magnitude (bf16 bits as unsigned numbers order
@@ -71,14 +71,14 @@ __global__ void __launch_bounds__(WR_THREADS) k_kv8_write(Kv8Write a, int per) {
 #pragma unroll 1
   for (; starts; starts &= starts - 1) {
     const int i = __ffs(starts) - 1, mine = __shfl_sync(0xFFFFFFFFu, here, i), block = mine >> 4;
-    // rows r0 + i - WINDOW .. - 1, then r0 + i .. + WINDOW - 1
+    // rows r0 + i - WINDOW .. - 1, then r0 + i .. + WINDOW
     const uint32_t same_b = __ballot_sync(0xFFFFFFFFu, before >> 4 == block);
     const uint32_t same_h = __ballot_sync(0xFFFFFFFFu, here >> 4 == block);
     if ((same_b >> i) | (same_h & ((1u << i) - 1u))) continue;  // an earlier row's run
     if (lane < KV8_BLOCK) row_of[lane] = -1;
     __syncwarp();
     if (lane >= i && here >> 4 == block) row_of[here & 15] = r0 + lane;
-    if (lane < i && next >> 4 == block) row_of[next & 15] = r0 + WINDOW + lane;
+    if (lane <= i && next >> 4 == block) row_of[next & 15] = r0 + WINDOW + lane;
     __syncwarp();
     const int page = mine >> a.shift, in_page = (mine & ((1 << a.shift) - 1)) >> 4;
     const size_t row0 = (((size_t)page * a.Hkv + h) << a.shift) + in_page * KV8_BLOCK;

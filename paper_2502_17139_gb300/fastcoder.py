@@ -1188,7 +1188,7 @@ def fc_kv8_write(cache: Kv8Cache, k, v, slot, src=None, track: Kv8Track | None =
     """Rounds rows into the cache: k, v bf16 [rows, Hkv, D] or [B, n, Hkv, D] of
     equal strides (any, the last dimension dense), slot [rows] int32 (negative:
     left out); src [rows] int32: the row of k, v (of B * n) that goes to a slot.
-    The rows of one block of 16 places lie within 32 rows of one another.  With
+    The rows of one block of 16 places are at most 32 rows apart.  With
     ``track`` their places get weight 0 and position pos [rows] int32."""
     if k.dtype is not torch.bfloat16 or v.dtype is not torch.bfloat16:
         raise TypeError("k and v must be torch.bfloat16")

@@ -815,3 +815,28 @@ def test_weights_beside_cached_values_that_stand_for_nan(fc, kv, n, H, Hkv):
     nan = got.isnan().all(-1)
     assert nan[0, :, :G].all() and nan[1, :, -G:].all() and nan.sum() == 2 * n * G
     assert fc.fc_get_error() == "FC_OK"
+
+
+@pytest.mark.parametrize("apart", [1, 16, 30, 31, 32])
+@pytest.mark.parametrize("lead", [0, 1, 15, 16, 31])
+@pytest.mark.parametrize("many", [False, True])
+def test_write_of_rows_of_a_block_that_stand_apart(fc, apart, lead, many):
+    """Two rows of one block with rows between them that are left out or go to other blocks."""
+    rng = np.random.default_rng(apart + lead)
+    H, page = 4, 32
+    slot = np.full(lead + apart + 40, -1, np.int32)
+    slot[lead], slot[lead + apart] = 3 * page + 18, 3 * page + 21
+    if apart > 2:
+        slot[lead + 1], slot[lead + apart - 1] = 0, page + 16
+    if many:  # enough rows for a warp to take several
+        slot = np.concatenate([np.where(slot < 0, -1, slot + 4 * page * i) for i in range(60)]).astype(np.int32)
+    cache = random_cache(rng, 4 * (60 if many else 1), H, page)
+    got = on_gpu(fc, cache)
+    track = fc.Kv8Track(torch.full(cache[0].shape[:3], 3.5).cuda(), torch.full(cache[0].shape[:3], -7, dtype=torch.int32).cuda())
+    rt = [track.weight.cpu().numpy(), track.born.cpu().numpy()]
+    x, pos = bf(rng, len(slot), H, D), rng.integers(0, 99, len(slot)).astype(np.int32)
+    fc.fc_kv8_write(got, x.cuda(), x.cuda(), dev(slot), track=track, pos=dev(pos))
+    o8.write(cache, num(x), num(x), slot, None, rt, pos)
+    same_cache(got, cache)
+    assert np.array_equal(track.weight.cpu().numpy(), rt[0]) and np.array_equal(track.born.cpu().numpy(), rt[1])
+    assert fc.fc_get_error() == "FC_OK"
