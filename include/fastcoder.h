@@ -896,8 +896,9 @@ fc_status fc_kv8_read(const fc_kv8_cache* cache, const int32_t* d_slot, int rows
  *     bits down to 2^-25 of it;
  *   more: cached numbers exact; queries, and new keys by 16, exact down to 2^-10
  *     of the row's largest, to 2^-18 of it below; probabilities bf16.
- * Scales and new values may lie anywhere between 2^-80 and 2^100 (or be 0), side
- * by side; scores, scale * q k, of up to 2^24 in magnitude.
+ * Scales, new keys and new values may lie anywhere between 2^-80 and 2^100 (or be
+ * 0), side by side, and queries anywhere; scores, scale * q k, of up to 2^24 in
+ * magnitude.
  * What a block holds past a request's end, and a scale of a block that begins
  * there, is not looked at.  A block that stands for NaN makes the rows of its
  * request and head NaN.  A new token with a NaN or an infinity in its key or its

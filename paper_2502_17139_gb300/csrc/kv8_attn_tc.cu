@@ -76,12 +76,15 @@ constexpr uint64_t DRAIN_CYCLES = 400000000ull;
 constexpr float RESCALE_THRESHOLD = 8.f;  // O is rescaled when a row's maximum (base 2) grows by more
 constexpr int E_TOP = 7;  // a query row's largest value, 16 new keys' largest, is put at 2^7..2^8
 constexpr float M_START = -1e30f;  // a reference before any key
-// Exponents below count as this, so that the product of two is no fp32
-// underflow; such scores are 0 to fp32 all the same.  And what a score is
-// multiplied by is at least FACTOR_MIN (a block of zeros has scale 2^-120, a row
-// of zeros 2^E_MIN): a factor of 0 would make NaN of masked scores, -infinity.
-constexpr int E_MIN = -50;
-constexpr float FACTOR_MIN = 0x1p-126f;
+// Exponents of queries and new keys are taken as they are where 2^(e - E_TOP) and
+// its inverse are normal fp32 numbers; smaller ones count as E_MIN (what a row of
+// queries below it loses, 2^-136 a value, moves a score by less than 2^-23 beside
+// keys of 448 * 2^100).  What a score is multiplied by, the row's factor times
+// the keys', may underflow: it is at least FACTOR_MIN, and the row's at least
+// ROW_MIN, as a factor of 0 would make NaN of masked scores, -infinity.  (The sum
+// of two e4m3 products is below 2^25, so that such a score is 0 beside 1.)
+constexpr int E_MIN = -119, E_MAX = 127;
+constexpr float FACTOR_MIN = 0x1p-126f, ROW_MIN = 0x1p-149f, ROW_MAX = 0x1.fffffep127f;
 // A unit's start and end in blocks of one tile: 4 where a unit is cut over CTAs (3
 // requests of 128 nodes, 32 heads of their own, over 3000 keys 36 us, with 8 39), 7
 // where a CTA has several (16 ragged trees of 64 nodes 121 us, with 12 128).  And
@@ -251,8 +254,8 @@ __device__ __forceinline__ uint32_t top2(uint32_t top, uint32_t w) {
   const uint32_t mag = w & 0x7FFF7FFFu;
   return __vmaxu2(top, mag & ~__vcmpgeu2(mag, 0x7F807F80u));
 }
-// Exponent of a magnitude given as bf16 bits, in E_MIN..100.
-__device__ __forceinline__ int expo_of(uint32_t bits) { return min(max((int)(bits >> 7) - 127, E_MIN), 100); }
+// Exponent of a magnitude given as bf16 bits, in E_MIN..E_MAX.
+__device__ __forceinline__ int expo_of(uint32_t bits) { return min(max((int)(bits >> 7) - 127, E_MIN), E_MAX); }
 // 8 bf16 values times a power of two as the sum of two e4m3 rows' bytes.  The
 // nearest e4m3 number has four significant bits, so it leaves at most four of
 // the eight, in steps that e4m3 has down to 2^-9.
@@ -878,7 +881,8 @@ __global__ void __launch_bounds__(THREADS, 1) k_kv8_attn_many(const __grid_const
       if (n == 0) break;
       float m = M_START, l = 0.f;  // m: the reference
       if (!(ok = warp_wait(bar(B_QE + np % PIECES), (np / PIECES) & 1, &s_abort))) break;
-      const float c_row = fmaxf(a.scale_log2 * reinterpret_cast<const float*>(smem + OFF_QE)[np % PIECES * ROWS + row_of(pc)], FACTOR_MIN);
+      const float c_row =
+          fminf(fmaxf(a.scale_log2 * reinterpret_cast<const float*>(smem + OFF_QE)[np % PIECES * ROWS + row_of(pc)], ROW_MIN), ROW_MAX);
       const int every = pc->two ? 1 : 2, first = pc->two ? 0 : x, n_cached = pc->cached - pc->s0;
       const bool idle = row_of(pc) - lane >= pc->rows;  // none of the warp's rows is in use
 #pragma unroll 1

@@ -840,3 +840,26 @@ def test_write_of_rows_of_a_block_that_stand_apart(fc, apart, lead, many):
     same_cache(got, cache)
     assert np.array_equal(track.weight.cpu().numpy(), rt[0]) and np.array_equal(track.born.cpu().numpy(), rt[1])
     assert fc.fc_get_error() == "FC_OK"
+
+
+SIZES_APART = [(-60, 0), (-70, 68), (-112, 90), (-20, -60), (74, -70), (110, -60), (20, 88)]
+
+
+def sized(rng, kv, n, H, Hkv, q_exp, k_exp):
+    """Queries times 2^q_exp, keys, cached and new, times 2^k_exp, and the scale that takes both back."""
+    s = setup(rng, kv, n, H, Hkv, 32, stale=False)
+    s["q"] = (s["q"].float() * 2.0 ** q_exp).bfloat16()
+    s["k"] = (s["k"].float() * 2.0 ** k_exp).bfloat16()
+    s["cache"][2] *= np.float32(2.0 ** k_exp)
+    return s, D ** -0.5 * 2.0 ** -(q_exp + k_exp)
+
+
+@pytest.mark.parametrize("q_exp,k_exp", SIZES_APART)
+@pytest.mark.parametrize("n,H,Hkv", [(20, 4, 4), (40, 4, 2)])
+def test_trees_of_tiny_and_large_queries_and_keys(fc, n, H, Hkv, q_exp, k_exp):
+    """Scores of some units, whatever makes them up."""
+    s, scale = sized(np.random.default_rng(23), [300, 45], n, H, Hkv, q_exp, k_exp)
+    ref, tol, _, _ = reference(s, None, scale, causal=True)
+    got = call(fc, s, scale=scale, workspace=fc.kv8_attn_workspace(2, n, H, Hkv, "cuda"))
+    assert np.all(np.abs(num(got) - ref) <= tol)
+    assert fc.fc_get_error() == "FC_OK"
