@@ -375,7 +375,7 @@ __global__ void __launch_bounds__(FEW_THREADS, FEW_CTAS) k_kv8_attn_few(FewArgs 
         }
       }
     top = __reduce_max_sync(0xFFFFFFFFu, max(top & 0xFFFFu, top >> 16));
-    const int qe = top ? min(max((int)(top >> 7) - 127, -100), 100) : 0;  // largest |q| < 2^(qe + 1) (or it overflows)
+    const int qe = top ? max((int)(top >> 7) - 127, -100) : 0;  // largest |q| < 2^(qe + 1)
     const float q_mul = pow2i(14 - qe);
     const float z_mul = a.scale_log2 * pow2i(qe - 14);
     uint32_t qf[NT][8][2];

@@ -863,3 +863,13 @@ def test_trees_of_tiny_and_large_queries_and_keys(fc, n, H, Hkv, q_exp, k_exp):
     got = call(fc, s, scale=scale, workspace=fc.kv8_attn_workspace(2, n, H, Hkv, "cuda"))
     assert np.all(np.abs(num(got) - ref) <= tol)
     assert fc.fc_get_error() == "FC_OK"
+
+
+@pytest.mark.parametrize("q_exp,k_exp", SIZES_APART)
+@pytest.mark.parametrize("n,H,Hkv", [(1, 8, 2), (4, 16, 4)])
+def test_few_rows_of_tiny_and_large_queries_and_keys(fc, n, H, Hkv, q_exp, k_exp):
+    s, scale = sized(np.random.default_rng(24), [300, 45], n, H, Hkv, q_exp, k_exp)
+    ref, tol, _, _ = reference(s, None, scale, causal=True)
+    got = call(fc, s, scale=scale, workspace=fc.kv8_attn_workspace(2, n, H, Hkv, "cuda"))
+    assert np.all(np.abs(num(got) - ref) <= tol)
+    assert fc.fc_get_error() == "FC_OK"
