@@ -60,6 +60,7 @@ constexpr float VS_MIN = 0x1p-80f;
 // A reference before any key: 2^(z + 1e30) is infinite and not below W_MAX
 // whatever it is multiplied by, 2^(-1e30 - m) is 0.
 constexpr float M_START = -1e30f;
+constexpr float F32_MAX = 0x1.fffffep127f;
 template <int NT>
 struct FewSmem {
   static constexpr int ROWS = 8 * NT;
@@ -135,6 +136,11 @@ __device__ __forceinline__ float exp2_fast(float x) {
   float y;
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
+}
+__device__ __forceinline__ float min_nan(float a, float b) {  // NaN of either
+  float d;
+  asm("min.NaN.f32 %0, %1, %2;" : "=f"(d) : "f"(a), "f"(b));
+  return d;
 }
 // l * 2^d by two factors: a row's sum, relative to a reference that value scales move, may be 2^112 and d -180
 __device__ __forceinline__ float times_pow2(float l, float d) {
@@ -459,7 +465,9 @@ __global__ void __launch_bounds__(FEW_THREADS, FEW_CTAS) k_kv8_attn_few(FewArgs 
         issue(it + FEW_STAGES - 1, last, last * STEP_BYTES);
       }
       const float4 sc = *reinterpret_cast<const float4*>(st + OFF_SC);
-      float ks[4] = {sc.x * z_mul, sc.x * z_mul, sc.y * z_mul, sc.y * z_mul};
+      // (finite: a sum of 0 between large queries and large keys is a score of 0)
+      const float ka = min_nan(sc.x * z_mul, F32_MAX), kb = min_nan(sc.y * z_mul, F32_MAX);
+      float ks[4] = {ka, ka, kb, kb};
       float vs[4] = {sc.z, sc.z, sc.w, sc.w};
       float z[NT][4][2];
 #pragma unroll

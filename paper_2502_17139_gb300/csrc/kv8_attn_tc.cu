@@ -81,10 +81,11 @@ constexpr float M_START = -1e30f;  // a reference before any key
 // queries below it loses, 2^-136 a value, moves a score by less than 2^-23 beside
 // keys of 448 * 2^100).  What a score is multiplied by, the row's factor times
 // the keys', may underflow: it is at least FACTOR_MIN, and the row's at least
-// ROW_MIN, as a factor of 0 would make NaN of masked scores, -infinity.  (The sum
-// of two e4m3 products is below 2^25, so that such a score is 0 beside 1.)
+// ROW_MIN, as a factor of 0 would make NaN of masked scores, -infinity (sums of
+// products are below 2^26, so that such a score is 0 beside 1).  And it is finite, as
+// a sum of 0 between large queries and large keys is a score of 0.
 constexpr int E_MIN = -119, E_MAX = 127;
-constexpr float FACTOR_MIN = 0x1p-126f, ROW_MIN = 0x1p-149f, ROW_MAX = 0x1.fffffep127f;
+constexpr float FACTOR_MIN = 0x1p-126f, ROW_MIN = 0x1p-149f, FACTOR_MAX = 0x1.fffffep127f;
 // A unit's start and end in blocks of one tile: 4 where a unit is cut over CTAs (3
 // requests of 128 nodes, 32 heads of their own, over 3000 keys 36 us, with 8 39), 7
 // where a CTA has several (16 ragged trees of 64 nodes 121 us, with 12 128).  And
@@ -157,6 +158,11 @@ __device__ __forceinline__ uint64_t f2_add(uint64_t a, uint64_t b) {
 __device__ __forceinline__ float max_nan(float a, float b) {  // NaN of either
   float d;
   asm("max.NaN.f32 %0, %1, %2;" : "=f"(d) : "f"(a), "f"(b));
+  return d;
+}
+__device__ __forceinline__ float min_nan(float a, float b) {
+  float d;
+  asm("min.NaN.f32 %0, %1, %2;" : "=f"(d) : "f"(a), "f"(b));
   return d;
 }
 __device__ __forceinline__ float max3(float a, float b, float c) {
@@ -882,7 +888,7 @@ __global__ void __launch_bounds__(THREADS, 1) k_kv8_attn_many(const __grid_const
       float m = M_START, l = 0.f;  // m: the reference
       if (!(ok = warp_wait(bar(B_QE + np % PIECES), (np / PIECES) & 1, &s_abort))) break;
       const float c_row =
-          fminf(fmaxf(a.scale_log2 * reinterpret_cast<const float*>(smem + OFF_QE)[np % PIECES * ROWS + row_of(pc)], ROW_MIN), ROW_MAX);
+          fminf(fmaxf(a.scale_log2 * reinterpret_cast<const float*>(smem + OFF_QE)[np % PIECES * ROWS + row_of(pc)], ROW_MIN), FACTOR_MAX);
       const int every = pc->two ? 1 : 2, first = pc->two ? 0 : x, n_cached = pc->cached - pc->s0;
       const bool idle = row_of(pc) - lane >= pc->rows;  // none of the warp's rows is in use
 #pragma unroll 1
@@ -966,7 +972,7 @@ __global__ void __launch_bounds__(THREADS, 1) k_kv8_attn_many(const __grid_const
           const float2 bk = back[q];
 #pragma unroll
           for (int u = 0; u < 16; ++u) {
-            const float cz = max_nan(c_row * (u < 8 ? bk.x : bk.y), FACTOR_MIN);
+            const float cz = min_nan(max_nan(c_row * (u < 8 ? bk.x : bk.y), FACTOR_MIN), FACTOR_MAX);
             float p0, p1;
             f2_unpack(f2_fma(f2_pack(__uint_as_float(sv[2 * u]), __uint_as_float(sv[2 * u + 1])), f2_pack(cz, cz), neg), p0, p1);
             p0 = exp2_fast(p0), p1 = exp2_fast(p1);

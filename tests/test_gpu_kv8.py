@@ -873,3 +873,20 @@ def test_few_rows_of_tiny_and_large_queries_and_keys(fc, n, H, Hkv, q_exp, k_exp
     got = call(fc, s, scale=scale, workspace=fc.kv8_attn_workspace(2, n, H, Hkv, "cuda"))
     assert np.all(np.abs(num(got) - ref) <= tol)
     assert fc.fc_get_error() == "FC_OK"
+
+
+@pytest.mark.parametrize("n,H,Hkv", [(1, 8, 2), (2, 16, 2), (40, 4, 2)])
+def test_scores_of_zero_between_large_queries_and_keys(fc, n, H, Hkv):
+    """Queries of 2^100 in one half of the dimensions, keys of 2^60 in the other: every score is 0, every weight the same."""
+    s = setup(np.random.default_rng(25), [300, 45], n, H, Hkv, 32, stale=False)
+    s["q"][..., 64:] = 0
+    s["k"][..., :64] = 0
+    s["cache"][0][..., :64] = 0
+    zero = dict(s, q=torch.zeros_like(s["q"]))
+    ref, tol, _, _ = reference(zero, None, D ** -0.5, causal=True)
+    s["q"] = (s["q"].float() * 2.0 ** 100).bfloat16()
+    s["k"] = (s["k"].float() * 2.0 ** 20).bfloat16()
+    s["cache"][2] *= np.float32(2.0 ** 60)
+    got = call(fc, s, workspace=fc.kv8_attn_workspace(2, n, H, Hkv, "cuda"))
+    assert np.all(np.abs(num(got) - ref) <= tol)
+    assert fc.fc_get_error() == "FC_OK"
