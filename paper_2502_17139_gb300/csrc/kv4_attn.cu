@@ -140,6 +140,11 @@ __device__ __forceinline__ float exp2_fast(float x) {
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
 }
+// l * 2^d by two factors: a row's sum, relative to a reference that value scales move, may be 2^112 and d -180
+__device__ __forceinline__ float times_pow2(float l, float d) {
+  const float h = exp2_fast(0.5f * d);
+  return l * h * h;
+}
 __device__ __forceinline__ float pow2i(int e) { return __uint_as_float((uint32_t)(e + 127) << 23); }  // -126 <= e <= 127
 __device__ __forceinline__ int expo(float x) { return (int)((__float_as_uint(x) >> 23) & 255u) - 127; }
 __device__ __forceinline__ float lo_f(uint32_t w) { return __uint_as_float(w << 16); }
@@ -442,8 +447,8 @@ __global__ void __launch_bounds__(FEW_THREADS, NT == 1 ? 2 : 1) k_kv4_attn_few(F
 #pragma unroll
           for (int x = 4; x < 32; x <<= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, x));
           const float mn = fmaxf(m[n][r], top), al = exp2_fast(m[n][r] - mn);
+          l[n][r] = times_pow2(l[n][r], m[n][r] - mn);
           m[n][r] = mn;
-          l[n][r] *= al;
 #pragma unroll
           for (int mt = 0; mt < 8; ++mt) o[n][mt][r] *= al, o[n][mt][2 + r] *= al;
 #pragma unroll
@@ -673,7 +678,7 @@ __global__ void __launch_bounds__(FEW_THREADS, NT == 1 ? 2 : 1) k_kv4_attn_few(F
         const float2 ml = pml[w * L::ROWS + r];
         const float k = exp2_fast(ml.x - mx);
         const float4 v = *reinterpret_cast<const float4*>(po + (w * L::ROWS + r) * L::OUT_PITCH + 4 * d4);
-        sum += ml.y * k;
+        sum += times_pow2(ml.y, ml.x - mx);
         acc.x += v.x * k, acc.y += v.y * k, acc.z += v.z * k, acc.w += v.w * k;
       }
       if (whole) {
@@ -703,14 +708,14 @@ __global__ void __launch_bounds__(FEW_THREADS, NT == 1 ? 2 : 1) k_kv4_attn_few(F
           for (int c = lane; c < nc; c += 32) {
             const float2 ml = __ldcg(reinterpret_cast<const float2*>(piece(c0 + c) + L::ROWS * HD) + r);
             const float mn = fmaxf(mx, ml.x);
-            sum = sum * exp2_fast(mx - mn) + ml.y * exp2_fast(ml.x - mn);
+            sum = times_pow2(sum, mx - mn) + times_pow2(ml.y, ml.x - mn);
             mx = mn;
             wt[r * nc + c] = ml.x;
           }
           float all = mx;
 #pragma unroll
           for (int x = 16; x > 0; x >>= 1) all = fmaxf(all, __shfl_xor_sync(0xFFFFFFFFu, all, x));
-          sum *= exp2_fast(mx - all);
+          sum = times_pow2(sum, mx - all);
 #pragma unroll
           for (int x = 16; x > 0; x >>= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, x);
           const float inv = sum == 0.f ? 0.f : 1.f / sum;

@@ -849,3 +849,24 @@ def test_binding_refuses_outputs_that_are_too_small(fc):
     with pytest.raises(ValueError):
         fc.fc_w4_pack(torch.zeros((128, 40), dtype=torch.bfloat16, device="cuda"), 0)
     assert fc.fc_get_error() == "FC_OK"
+
+
+@pytest.mark.parametrize("n,H,G", [(1, 8, 2), (4, 2, 2), (2, 16, 2), (20, 4, 2)])
+@pytest.mark.parametrize("lens", [[300, 90], [3000, 17]])
+@pytest.mark.parametrize("low_first", [True, False])
+def test_attn_value_scales_as_far_apart_as_they_may_be(fc, low_first, lens, n, H, G):
+    """One half of a request's values under scales of 2^-80, the other under 2^90: the keys of both count in the row sum.
+    Tolerance: test_attn_scales_far_apart's."""
+    c = attn_case(n + 9, 2, n, H, G, lens, 32, stale=False)
+    for b, L in enumerate(lens):
+        at = np.arange(L)
+        low = (at < L // 2) == low_first
+        c["scales"][1][c["table"][b, at // 32], :, at % 32] = np.where(low, 2.0 ** -80, 2.0 ** 90)[:, None]
+    kn, vn = num(c["k_new"]), num(c["v_new"])
+    ref, size = o4.attn(num(c["q"]), *(o4.pack(x) for x in c["codes"]), *c["scales"], c["table"], c["lens"], kn, vn,
+                        c["sees"], c["nodes"], c["scale"])
+    floor = (c["lens"].max() + n) * 2.0 ** -33 * size.max(-1, keepdims=True)
+    for ws in (True, False):
+        got = num(run_attn(fc, c, ws=ws))
+        assert np.all(np.abs(got - ref) <= 2.0 ** -8 * np.abs(ref) + size * (2.0 ** -8 + 2.0 ** -10) + floor)
+    assert fc.fc_get_error() == "FC_OK"
