@@ -763,8 +763,10 @@ fc_status fc_kv4_read(const fc_kv4_cache* cache, const int32_t* d_slot, int rows
  *   more: cached and new keys fp16 relative to the largest of 16 neighbours,
  *     exact down to 2^-20 of it; queries fp16 relative to the row's largest,
  *     exact down to 2^-26 of it; probabilities times value scales bf16.
- * Scales and new values may lie anywhere between 2^-80 and 2^100 (or be 0), side
- * by side; scores, scale * q k, of up to 2^24 in magnitude.
+ * Scales, new keys and new values may lie anywhere between 2^-80 and 2^100 (or be
+ * 0), side by side, and queries anywhere; scores, scale * q k, of up to 2^24 in
+ * magnitude (their sums are fp32: with s a key's scale, its score is off by up to
+ * 2^-14 of scale * s * sum |q|, which is to be below 2^100).
  * A length or node count out of range, or a page id outside the pool, records
  * FC_ERR_INVALID_ARG (that request's rows are zeros; that page's keys are
  * left out).  What a page holds past a request's end is not looked at.  A new

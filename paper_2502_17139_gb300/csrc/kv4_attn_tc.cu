@@ -80,9 +80,15 @@ constexpr uint64_t DRAIN_CYCLES = 400000000ull;
 constexpr float RESCALE_THRESHOLD = 8.f;  // O is rescaled when a row's maximum (base 2) grows by more
 constexpr int E_TOP = 9;  // a query row's largest value, 16 keys' largest scale (or new value), is put at 2^9..2^10
 constexpr float M_START = -1e30f;  // a reference before any key
-// Exponents below count as this, so that the product of two is no fp32
-// underflow; such scores are 0 to fp32 all the same.
-constexpr int E_MIN = -50;
+// Exponents of queries, new keys and key scales are taken as they are where 2^(e -
+// E_TOP) and its inverse are normal fp32 numbers; smaller ones count as E_MIN (what
+// a row of queries below it loses, 2^-151 a value, is nothing beside keys of 7 *
+// 2^100).  What a score is multiplied by, the row's factor times the keys', may
+// underflow: it is at least FACTOR_MIN, and the row's at least ROW_MIN, as a
+// factor of 0 would make NaN of masked scores, -infinity.  (Sums of products are
+// below 2^30, so that such a score is 0 beside 1.)
+constexpr int E_MIN = -117, E_MAX = 127;
+constexpr float FACTOR_MIN = 0x1p-126f, ROW_MIN = 0x1p-149f, ROW_MAX = 0x1.fffffep127f;
 // A unit's start and end in blocks of one tile (4 takes 183 us where 8 takes 161,
 // 16 ragged trees of 64 nodes), and the least share worth a CTA: with 12 instead
 // of 6 a tree of 32 nodes over 2000 keys takes 37 us instead of 31, one of 64 over
@@ -250,8 +256,8 @@ __device__ __forceinline__ uint32_t top2(uint32_t top, uint32_t w) {
   const uint32_t mag = w & 0x7FFF7FFFu;
   return __vmaxu2(top, mag & ~__vcmpgeu2(mag, 0x7F807F80u));
 }
-// Exponent of a magnitude given as bf16 bits, in E_MIN..100.
-__device__ __forceinline__ int expo_of(uint32_t bits) { return min(max((int)(bits >> 7) - 127, E_MIN), 100); }
+// Exponent of a magnitude given as bf16 bits, in E_MIN..E_MAX.
+__device__ __forceinline__ int expo_of(uint32_t bits) { return min(max((int)(bits >> 7) - 127, E_MIN), E_MAX); }
 // 16 bytes of bf16 in the tiles' order times a power of two, as fp16
 __device__ __forceinline__ uint4 to_f16(const uint4& v, float by) {
   auto two = [&](uint32_t w) { return pack_f16x2(lo_f(w) * by, hi_f(w) * by); };
@@ -833,7 +839,8 @@ __global__ void __launch_bounds__(THREADS, 1) k_kv4_attn_many(ManyArgs f) {
       if (n == 0) break;
       float m = M_START, l = 0.f;  // m: the reference
       if (!(ok = warp_wait(bar(B_QE + np % PIECES), (np / PIECES) & 1, &s_abort))) break;
-      const float c_row = a.scale_log2 * reinterpret_cast<const float*>(smem + OFF_QE)[np % PIECES * ROWS + row_of(pc)];
+      const float c_row =
+          fminf(fmaxf(a.scale_log2 * reinterpret_cast<const float*>(smem + OFF_QE)[np % PIECES * ROWS + row_of(pc)], ROW_MIN), ROW_MAX);
       const int every = pc->two ? 1 : 2, first = pc->two ? 0 : x, n_cached = pc->cached - pc->s0;
       const bool idle = row_of(pc) - lane >= pc->rows;  // none of the warp's rows is in use
 #pragma unroll 1
@@ -915,7 +922,7 @@ __global__ void __launch_bounds__(THREADS, 1) k_kv4_attn_many(ManyArgs f) {
 #pragma unroll
           for (int g = 0; g < 8; ++g) {  // 4 keys, their value scales in one load
             const ulonglong2 v4 = vs4[q * 8 + g];
-            const float cz = c_row * (g < 4 ? bk.x : bk.y);
+            const float cz = fmaxf(c_row * (g < 4 ? bk.x : bk.y), FACTOR_MIN);
             const uint64_t c2 = f2_pack(cz, cz);
 #pragma unroll
             for (int u = 0; u < 2; ++u) {

@@ -870,3 +870,22 @@ def test_attn_value_scales_as_far_apart_as_they_may_be(fc, low_first, lens, n, H
         got = num(run_attn(fc, c, ws=ws))
         assert np.all(np.abs(got - ref) <= 2.0 ** -8 * np.abs(ref) + size * (2.0 ** -8 + 2.0 ** -10) + floor)
     assert fc.fc_get_error() == "FC_OK"
+
+
+SIZES_APART = [(-60, 0), (-70, 68), (-110, 90), (-20, -60), (74, -70), (110, -60), (20, 88)]
+
+
+def sized(n, H, G, q_exp, k_exp):
+    """Queries times 2^q_exp, keys, cached and new, times 2^k_exp, and the scale that takes both back."""
+    c = attn_case(n + 10, 2, n, H, G, [300, 45], 32, stale=False, scale=128 ** -0.5 * 2.0 ** -(q_exp + k_exp))
+    c["q"] = (c["q"].float() * 2.0 ** q_exp).bfloat16()
+    c["k_new"] = (c["k_new"].float() * 2.0 ** k_exp).bfloat16()
+    c["scales"][0] *= 2.0 ** k_exp
+    return c
+
+
+@pytest.mark.parametrize("q_exp,k_exp", SIZES_APART)
+@pytest.mark.parametrize("n,H,G", [(20, 4, 2), (128, 4, 2)])
+def test_attn_trees_of_tiny_and_large_queries_and_keys(fc, n, H, G, q_exp, k_exp):
+    """Scores of some units, whatever makes them up."""
+    check_attn(fc, sized(n, H, G, q_exp, k_exp))
