@@ -385,9 +385,9 @@ __global__ void __launch_bounds__(FEW_THREADS, NT == 1 ? 2 : 1) k_kv4_attn_few(F
         }
       }
     top = __reduce_max_sync(0xFFFFFFFFu, max(top & 0xFFFFu, top >> 16));
-    const int qe = top ? min(max((int)(top >> 7) - 127, -100), 100) : 0;  // largest |q| < 2^(qe + 1) (or it overflows)
+    const int qe = top ? max((int)(top >> 7) - 127, -100) : 0;  // largest |q| < 2^(qe + 1)
     const float q_mul = pow2i(14 - qe), q_odd = q_mul * 0.0625f;
-    const float z_mul = a.scale_log2 * pow2i(qe + 10);  // undoes 2^(14 - qe) 2^-24
+    const float z_mul = a.scale_log2 * pow2i(qe - 14) * 0x1p24f;  // undoes 2^(14 - qe) 2^-24
     uint32_t qf[NT][8][2];
     float s_init[NT][2];  // rows 8n + 2t, + 1: -8 2^-24 times the sum of the row
 #pragma unroll

@@ -889,3 +889,9 @@ def sized(n, H, G, q_exp, k_exp):
 def test_attn_trees_of_tiny_and_large_queries_and_keys(fc, n, H, G, q_exp, k_exp):
     """Scores of some units, whatever makes them up."""
     check_attn(fc, sized(n, H, G, q_exp, k_exp))
+
+
+@pytest.mark.parametrize("q_exp,k_exp", SIZES_APART)
+@pytest.mark.parametrize("n,H,G", [(1, 8, 2), (4, 16, 4)])
+def test_attn_few_rows_of_tiny_and_large_queries_and_keys(fc, n, H, G, q_exp, k_exp):
+    check_attn(fc, sized(n, H, G, q_exp, k_exp))
