@@ -896,8 +896,8 @@ fc_status fc_kv8_read(const fc_kv8_cache* cache, const int32_t* d_slot, int rows
  *     largest of the request's rows of that kv head, exact down to 2^-27 of it;
  *     probabilities times value scales fp16 relative to the row's largest, 11
  *     bits down to 2^-25 of it;
- *   more: cached numbers exact; queries, and new keys by 16, exact down to 2^-10
- *     of the row's largest, to 2^-18 of it below; probabilities bf16.
+ *   more: cached numbers exact; queries, and new keys by 16, exact down to 2^-9
+ *     of the row's largest, to 2^-17 of it below; probabilities bf16.
  * Scales, new keys and new values may lie anywhere between 2^-80 and 2^100 (or be
  * 0), side by side, and queries anywhere; scores, scale * q k, of up to 2^24 in
  * magnitude.

@@ -86,16 +86,22 @@ def cached(cache, which, table, n, h):
     return decode(cache[which][p, h, o]) * cache[2 + which][p, h, o // BLOCK].astype(np.float64)[:, None]
 
 
-def attend(q, k, v, sees, scale):
+def attend(q, k, v, sees, scale, new=0):
     """q [n, D], k, v [L, D], sees [n, L]: (out, weights [n, L], mean |v|, e): e
-    bounds a score's error where sums of 128 products round to fp32 and queries
-    to 2^-18 of their row's largest."""
+    bounds a score's error where sums of 128 products round to fp32 and queries,
+    and the last `new` keys by 16, are sums of two e4m3 numbers: 2^-17 of the
+    largest magnitude of their row, or 16 rows.  (That one is put at 2^7 to 2^8.
+    The nearest e4m3 number of x leaves at most four significant bits, of x's
+    last place or more; what is below 2^-9, e4m3's smallest step, is rounded to
+    it, by 2^-10 at most: 2^-17 of 2^7.)"""
     z = np.where(sees, (q @ k.T) * scale, -np.inf)
     top = z.max(1, keepdims=True, initial=-np.inf)
     w = np.where(sees, np.exp(z - np.where(np.isfinite(top), top, 0)), 0)
     total = w.sum(1, keepdims=True)
     w = np.divide(w, total, out=np.zeros_like(w), where=total > 0)
-    e = scale * (2.0 ** -16 * (np.abs(q) @ np.abs(k).T) + 2.0 ** -18 * np.abs(q).max(1, keepdims=True) * np.abs(k).sum(1)[None])
+    e = scale * (2.0 ** -16 * (np.abs(q) @ np.abs(k).T) + 2.0 ** -17 * np.abs(q).max(1, keepdims=True) * np.abs(k).sum(1)[None])
+    for j in range(len(k) - new, len(k), BLOCK):
+        e[:, j:j + BLOCK] += scale * 2.0 ** -17 * np.abs(k[j:j + BLOCK]).max() * np.abs(q).sum(1)[:, None]
     return w @ v, w, w @ np.abs(v), np.where(sees, e, 0).max(1, keepdims=True, initial=0.0)
 
 

@@ -8,7 +8,7 @@
 // from the pages into the operand's place, and no thread touches a key.  A query
 // row, bf16 times a power of two, is the sum of two e4m3 rows: the nearest e4m3
 // number leaves a remainder of at most four significant bits.  Two products at
-// twice bf16's rate take bf16's time, and are exact for values down to 2^-10 of
+// twice bf16's rate take bf16's time, and are exact for values down to 2^-9 of
 // the row's largest.  New keys are split likewise.  A block's scale, 16 keys',
 // multiplies scores.  The second product is in bf16, P needing its range: V's
 // numbers times their scale, exact, as scales are powers of two.

@@ -156,3 +156,40 @@ def test_a_cache_off_its_alignment_is_refused(fc, field, offset):
         c[field] += shift
         cache = C.byref(fc.fc_kv8_cache(c["k_codes"], c["v_codes"], c["k_scale"], c["v_scale"], 4, 16, 2, 128))
         assert fc.LIB.fc_kv8_read(cache, None, 0, None, None, None) == want
+
+
+def parts(x, largest):
+    """x as the sum of two e4m3 numbers, `largest` put at 2^7 to 2^8."""
+    by = 2.0 ** (7 - np.floor(np.log2(largest)))
+    near = o8.decode(o8.encode(x * by))
+    return (near + o8.decode(o8.encode(x * by - near))) / by
+
+
+@pytest.mark.parametrize("largest", [1.0, 1.75, 255 / 128, 2.0 ** 60, 2.0 ** -100])
+def test_two_parts_hold_what_the_header_says(largest):
+    """bf16 values, 8 significant bits, beside the largest of their row: exact down to 2^-9 of it, else to 2^-17 of it."""
+    x = np.arange(128, 256)[None] / 128 * 2.0 ** -np.arange(0.0, 30)[:, None] * 2.0 ** np.floor(np.log2(largest))
+    x = x[x <= largest]
+    err = np.abs(parts(x, largest) - x)
+    assert np.all(err[x >= 2.0 ** -9 * largest] == 0)
+    assert 0 < err.max() <= 2.0 ** -17 * largest
+
+
+def test_scores_of_two_parts_are_within_the_oracles_bound():
+    """Small numbers beside a large one that meets zeros: all of a score's error is the parts'."""
+    rng = np.random.default_rng(4)
+    small = lambda *s: rng.integers(128, 256, s) / 128 * 2.0 ** -12.0
+    q, k = small(3, 128), rng.standard_normal((40, 128))
+    q[0] = 129 / 128 * 2.0 ** -10  # just between two sums of parts, all on one side
+    k[0] = np.abs(k[0])
+    q[:, 0], k[:, 0] = 1, 0
+    k[8:] = small(32, 128)  # the last 32 are new
+    k[8::16, 1], q[:, 1] = 1, 0
+    k[8:, 0] = 0
+    qp = np.stack([parts(r, 1.0) for r in q])
+    kp = np.concatenate((k[:8], parts(k[8:], 1.0)))
+    sees = np.ones((3, 40), bool)
+    bound = lambda keys, new: o8.attend(q, k[keys], k[keys], sees[:, keys], 1.0, new)[3]
+    err = np.abs(qp @ kp.T - q @ k.T)
+    for keys, new in ((slice(0, 8), 0), (slice(8, 40), 32)):
+        assert np.all(err[:, keys] <= bound(keys, new))
