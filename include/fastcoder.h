@@ -925,9 +925,11 @@ size_t fc_kv8_attn_workspace(int batch, int n_pad, int H, int Hkv, int64_t weigh
  * NaN counts as larger than every number.  The tokens that stay at an index >=
  * keep move, in order, into the places below keep that come free; the others
  * stay where they are.  A block that takes a token gets the scale for what it
- * then holds.  Requests with keep[b] >= kv_len[b] keep all.  The caller then
- * has min(keep, kv_len) tokens a request (fc_kv_pages_release with d_keep gives
- * the length and the emptied pages).
+ * then holds, at all its places below kv_len[b]: in the block of place keep - 1
+ * the tokens past it, which are no longer the request's, count too and are
+ * rounded with the others.  Requests with keep[b] >= kv_len[b] keep all.  The
+ * caller then has min(keep, kv_len) tokens a request (fc_kv_pages_release with
+ * d_keep gives the length and the emptied pages).
  *   d_weight_in, d_born_in   [n_pages][Hkv][page_size]: weights and positions
  *                as fc_kv8_attn and fc_kv8_write leave them (the positions of a
  *                head's tokens differ)
@@ -942,7 +944,8 @@ size_t fc_kv8_attn_workspace(int batch, int n_pad, int H, int Hkv, int64_t weigh
  * FC_ERR_CAPACITY, one with a negative length or keep, a length beyond its table
  * or a page id outside the pool FC_ERR_INVALID_ARG, and is left as it is (its
  * weights and positions are not carried over).  recent <= 2^22, cap <= 2^30,
- * batch * Hkv <= 2^24, max_pages * page_size <= 696320.  Requests share no page that changes.
+ * batch * Hkv <= 2^24, max_pages * page_size <= 696320.  Requests share no page
+ * that changes.
  */
 fc_status fc_kv8_evict(const fc_kv8_cache* cache, const int32_t* d_table, int max_pages, const int32_t* d_kv_len,
                        const int32_t* d_keep, int batch, int recent, const float* d_weight_in, const int32_t* d_born_in,

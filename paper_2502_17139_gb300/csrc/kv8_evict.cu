@@ -16,7 +16,8 @@
 //             and a list of the blocks of 16 places that take a token.
 //   k_move    a warp a block on the list: put together in registers (8 bytes a
 //             lane of each row, lanes 0-15 keys, 16-31 values), it gets the scale
-//             for what it then holds; rows that change are written.  The block
+//             for what it then holds, below the old length (whose last block may
+//             hold more than what stays); rows that change are written.  The block
 //             that holds both the last places and the first sources is read from
 //             a copy, as its own warp may have written it.
 //

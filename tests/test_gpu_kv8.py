@@ -890,3 +890,27 @@ def test_scores_of_zero_between_large_queries_and_keys(fc, n, H, Hkv):
     got = call(fc, s, workspace=fc.kv8_attn_workspace(2, n, H, Hkv, "cuda"))
     assert np.all(np.abs(num(got) - ref) <= tol)
     assert fc.fc_get_error() == "FC_OK"
+
+
+@pytest.mark.parametrize("L", [30, 34, 500])
+def test_evict_the_last_block_counts_up_to_the_old_length(fc, L):
+    """20 tokens stay; place 17 takes one, and the scale of its block is the one for its 16 places below the old
+    length, an evicted token's large numbers at place 25 among them."""
+    rng = np.random.default_rng(L)
+    H, page, K = 2, 16, 20
+    s = setup(rng, [L], 1, H, H, page, stale=False)
+    at = lambda i: (s["table"][0][i // page], slice(None), i % page)
+    for i in range(2):
+        s["cache"][i][at(25)] = o8.encode(448.0)
+        s["cache"][2 + i][s["table"][0][1]] = 2.0 ** 10  # place 25's block
+    w, born = np.zeros(s["cache"][0].shape[:3], np.float32), np.zeros(s["cache"][0].shape[:3], np.int32)
+    for i in range(L):
+        w[at(i)], born[at(i)] = (2.0 if i < K and i != 17 or i == L - 1 else 1 / (i + 2)), i
+    w0, b0 = np.zeros_like(w), np.zeros_like(born)
+    got = on_gpu(fc, s["cache"])
+    t_out = fc.Kv8Track(dev(w0), dev(b0))
+    frm = fc.fc_kv8_evict(got, dev(s["table"]), dev(s["kv"]), dev(np.array([K], np.int32)), 0, fc.Kv8Track(dev(w), dev(born)), t_out, cap=K)
+    assert (frm[0, :, 17] == L - 1).all() and (frm >= 0).sum() == H
+    o8.evict(s["cache"], s["table"], s["kv"], [K], 0, [w, born], [w0, b0], K)
+    same_cache(got, s["cache"])
+    assert (got.k_scale[int(s["table"][0][1])] == 2.0 ** 10).all() and fc.fc_get_error() == "FC_OK"
