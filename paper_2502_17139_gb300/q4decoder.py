@@ -11,7 +11,9 @@ keys and values in bf16; append() plans where the kept ones go
 write the same tensors at every step, so that a step captured in a CUDA graph
 is good for all of them.  A cache in 8 bits can be kept to a budget (``keep``):
 forward() adds up the weight that each cached token received, and evict() cuts
-every sequence down to the tokens that received most (fc_kv8_evict).
+every sequence down to the tokens that received most (fc_kv8_evict).  Every
+forward() counts, a tree's rejected nodes and a call that no append() follows
+(a warm-up before a capture) among them.
 
     python -m paper_2502_17139_gb300.q4decoder [batch] [context] [cache bits]
 
@@ -92,7 +94,8 @@ class Q4Decoder:
     def forward(self, tok, pos=None, mask=None, n_nodes=None):
         """tok [B, n] int32 -> logits [B, n, vocab].  pos [B, n] (None: the
         tokens follow the cache in order), mask [B, n, 1] int64 ancestor bits
-        (None: each sees those before it), n_nodes [B]."""
+        (None: each sees those before it), n_nodes [B].  With ``keep`` the cached
+        tokens' weights grow by what this call gives them, each time it runs."""
         s, B, n, kv_len = self.s, self.B, self.n, self.kv_len[0]
         if pos is None:
             pos = (kv_len + self.ahead if self.keep else kv_len)[:, None] + self.steps
