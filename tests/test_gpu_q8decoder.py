@@ -174,3 +174,125 @@ def test_refusals(weights):
             Q4Decoder(shape, W, 1, 4, 4, page_size=PAGE, **kw)
     with pytest.raises(ValueError):
         Q4Decoder(shape, W, 1, 4, 4, page_size=PAGE, cache_bits=8).evict()
+
+
+def rope(x, pos, base):
+    """x [heads, D] turned by pos."""
+    a = pos * base ** (-2.0 * np.arange(D // 2) / D)
+    lo, hi = x[:, :D // 2], x[:, D // 2:]
+    return np.concatenate((lo * np.cos(a) - hi * np.sin(a), hi * np.cos(a) + lo * np.sin(a)), 1)
+
+
+class PlainTree(Plain):
+    """The decoder in 64 bits over some nodes at once, with or without norms of queries and keys."""
+
+    def heads(self, x, w, pos):
+        if w is not None:
+            x = x / np.sqrt((x * x).mean(1, keepdims=True) + self.s.eps) * w
+        return rope(x, pos, self.s.rope_base)
+
+    def step(self, tok, pos, sees, cached):
+        """tok, pos [m], sees [m, m]: logits [m], and by layer and head the weights that the cached tokens received."""
+        m, received = len(tok), []
+        x = self.W["embed"][tok]
+        for l, w in enumerate(self.L):
+            h = np.stack([self.norm(r, w["attn_norm"]) for r in x])
+            q = np.stack([self.heads(r.reshape(H, D), w.get("q_norm"), p) for r, p in zip(h @ w["wq"], pos)])
+            kv = (h @ w["wkv"]).reshape(m, 2, HKV, D)
+            k = np.stack([self.heads(r, w.get("k_norm"), p) for r, p in zip(kv[:, 0], pos)])
+            out, got = np.zeros((m, H, D)), []
+            for g in range(HKV):
+                K, V = cached(l, g)
+                seen = np.concatenate((np.ones((m, len(K)), bool), sees), 1)
+                total = np.zeros(len(K))
+                for i in range(g * (H // HKV), (g + 1) * (H // HKV)):
+                    out[:, i], p, _, _ = o8.attend(q[:, i], np.concatenate((K, k[:, g])), np.concatenate((V, kv[:, 1, g])), seen, D ** -0.5)
+                    total += p[:, :len(K)].sum(0)
+                got.append(total)
+            received.append(got)
+            x = x + out.reshape(m, -1) @ w["wo"]
+            h = np.stack([self.norm(r, w["mlp_norm"]) for r in x])
+            gu = h @ w["wgu"]
+            x = x + (gu[:, :INTER] / (1 + np.exp(-gu[:, :INTER])) * gu[:, INTER:]) @ w["wd"]
+        return np.stack([self.norm(r, self.W["final_norm"]) for r in x]) @ self.W["lm_head"], received
+
+
+@pytest.mark.parametrize("normed,keep,steps", [(True, 24, 80), (False, 24, 80), (False, 0, 30)])
+def test_trees_with_accepted_paths_and_evictions_follow_the_plain_decoder(weights, normed, keep, steps):
+    """Draft trees of up to four nodes of three sequences: each step a path of none to all of them is kept (rows
+    head-major by src, several a block, some left out), and whoever holds 32 tokens or more is cut to 24.  Logits,
+    weights and bounds as in test_steps_with_a_budget_follow_the_plain_decoder; written rows, weights and positions
+    equal to the oracle's."""
+    from paper_2502_17139_gb300 import fastcoder as fc
+    from paper_2502_17139_gb300.q4decoder import Q4Decoder
+    shape, W = weights
+    if not normed:
+        W = dict(W, layers=[{k: v for k, v in w.items() if k not in ("q_norm", "k_norm")} for w in W["layers"]])
+    B, N, RECENT, FULL = 3, 4, 6, 32
+    dec = Q4Decoder(shape, W, B, 15, 5, nodes=N, page_size=PAGE, group=64, cache_bits=8, keep=keep, recent=RECENT if keep else 0)
+    plain = PlainTree(shape, W, 64)
+    rng = np.random.default_rng(8)
+    held, ahead, evicted = np.zeros(B, int), np.zeros(B, int), 0
+    i32 = lambda a: torch.from_numpy(np.asarray(a, np.int32)).cuda()
+    for t in range(steps):
+        nodes = rng.integers(1, N + 1, B) if t % 3 else np.full(B, N)
+        tok, depth, sees = rng.integers(0, VOCAB, (B, N)), np.zeros((B, N), int), np.zeros((B, N, N), bool)
+        path, accepted = np.full((B, N), -1), np.zeros(B, int)
+        for b in range(B):
+            parent = [-1] + [int(rng.integers(0, i)) for i in range(1, N)]
+            for i in range(N):
+                if i:
+                    sees[b, i], depth[b, i] = sees[b, parent[i]], depth[b, parent[i]] + 1
+                sees[b, i, i] = True
+            tip = int(rng.integers(0, nodes[b]))
+            line = [j for j in range(N) if sees[b, tip, j]]
+            accepted[b] = rng.integers(0, len(line) + 1)
+            path[b, :len(line)] = line
+        pos = held[:, None] + ahead[:, None] + depth
+        bits = (sees * (1 << np.arange(N))).sum(-1)[..., None]
+        table, before = dec.pages.table.cpu().numpy(), [arrays(c) for c in dec.caches]
+        was = [(num(x.weight), x.born.cpu().numpy()) for x, _ in dec.tracks] if keep else None
+        got = num(dec.forward(i32(tok), i32(pos), torch.from_numpy(bits.astype(np.int64)).cuda(), i32(nodes)))
+        added = [num(x.weight) - y[0] for (x, _), y in zip(dec.tracks, was)] if keep else None
+        for b in range(B):
+            m, L = nodes[b], held[b]
+            cached = lambda l, g: tuple(o8.cached(before[l], w, table[b], L, g) for w in range(2))
+            want, received = plain.step(tok[b, :m], pos[b, :m], sees[b, :m, :m], cached)
+            for i in range(m):
+                assert np.linalg.norm(got[b, i] - want[i]) < 4 * 5 * 2.0 ** -8 / 3 * np.linalg.norm(want[i]), (t, b, i)
+            if keep and L:
+                j = np.arange(L)
+                p, o = table[b][j // PAGE], j % PAGE
+                for l in range(LAYERS):
+                    for g in range(HKV):
+                        assert np.abs(added[l][p, g, o] - received[l][g]).max() <= 2.0 ** -4 * received[l][g].max() + 2.0 ** -20 * was[l][0].max()
+        tracks = [[x.weight.cpu().numpy().copy(), x.born.cpu().numpy().copy()] for x, _ in dec.tracks] if keep else None
+        dec.append(i32(accepted), path=i32(path))
+        slot, src, seq, place = (dec.plan[x].cpu().numpy() for x in ("slot", "src", "seq", "pos"))
+        assert (slot >= 0).sum() == accepted.sum()
+        for l in range(LAYERS):
+            k, v = (num(x[l]).transpose(0, 2, 1, 3).reshape(B * N, HKV, D) for x in (dec.k_new, dec.v_new))
+            o8.write(before[l], k, v, slot, src, tracks[l] if keep else None, place + ahead[np.maximum(seq, 0)])
+            for x, y in zip(before[l], arrays(dec.caches[l])):
+                assert np.array_equal(x, y)
+            if keep:
+                assert np.array_equal(tracks[l][0], dec.tracks[l][0].weight.cpu().numpy()) and np.array_equal(tracks[l][1], dec.tracks[l][0].born.cpu().numpy())
+        held += accepted
+        assert dec.kv_len[0].tolist() == held.tolist()
+        if keep and held.max() >= FULL:
+            table, evicted = dec.pages.table.cpu().numpy(), evicted + 1
+            dec.evict()
+            for l in range(LAYERS):
+                after, outs = before[l], [x.copy() for x in tracks[l]]
+                o8.evict(after, table, held, [keep] * B, RECENT, tracks[l], outs, keep)
+                for x, y in zip(after, arrays(dec.caches[l])):
+                    assert np.array_equal(x, y)
+                for b in range(B):
+                    j = np.arange(min(keep, held[b]))
+                    p, o = table[b][j // PAGE], j % PAGE
+                    for x, y in zip(outs, (dec.tracks[l][0].weight, dec.tracks[l][0].born)):
+                        assert np.array_equal(x[p, :, o], y.cpu().numpy()[p, :, o])
+            ahead += held - np.minimum(held, keep)
+            held = np.minimum(held, keep)
+            assert dec.kv_len[0].tolist() == held.tolist() and dec.ahead.tolist() == ahead.tolist()
+    assert fc.fc_get_error() == "FC_OK" and (evicted > 1) == bool(keep)
