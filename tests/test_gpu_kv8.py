@@ -914,3 +914,98 @@ def test_evict_the_last_block_counts_up_to_the_old_length(fc, L):
     o8.evict(s["cache"], s["table"], s["kv"], [K], 0, [w, born], [w0, b0], K)
     same_cache(got, s["cache"])
     assert (got.k_scale[int(s["table"][0][1])] == 2.0 ** 10).all() and fc.fc_get_error() == "FC_OK"
+
+
+@pytest.mark.parametrize("pages", [300, 3000])
+def test_weights_and_evictions_under_a_wide_table(fc, pages):
+    """Short requests under tables for 19200 and 192000 tokens, as wide as their longest allowed request."""
+    rng = np.random.default_rng(26)
+    kv, n, H, Hkv, page, K = [700, 0, 333], 2, 8, 2, 64, 200
+    s = setup(rng, kv, n, H, Hkv, page)
+    s["table"] = np.concatenate((s["table"], np.full((3, pages - s["table"].shape[1]), -9, np.int32)), 1)
+    masks = trees(rng, [n] * 3, n)
+    weight, born = dev(np.zeros(s["cache"][0].shape[:3], np.float32)), np.zeros(s["cache"][0].shape[:3], np.int32)
+    for b, L in enumerate(kv):
+        i = np.arange(L)
+        born[s["table"][b][i // page], :, i % page] = i[:, None]
+    got = call(fc, s, masks, workspace=fc.kv8_attn_workspace(3, n, H, Hkv, "cuda", pages * page), weight=weight, decay=1.0)
+    ref, tol, want, bound = reference(s, masks.view(np.uint64), D ** -0.5)
+    assert np.all(np.abs(num(got) - ref) <= tol) and np.all(np.abs(num(weight) - want) <= bound)
+    w = weight.cpu().numpy()
+    w0, b0 = np.zeros_like(w), np.zeros_like(born)
+    cache, t_out = on_gpu(fc, s["cache"]), fc.Kv8Track(dev(w0), dev(b0))
+    frm = fc.fc_kv8_evict(cache, dev(s["table"]), dev(s["kv"]), dev(np.full(3, K, np.int32)), 16, fc.Kv8Track(weight, dev(born)), t_out, cap=K)
+    assert np.array_equal(frm.cpu().numpy(), o8.evict(s["cache"], s["table"], kv, [K] * 3, 16, [w, born], [w0, b0], K))
+    same_cache(cache, s["cache"])
+    assert np.array_equal(t_out.weight.cpu().numpy(), w0) and np.array_equal(t_out.born.cpu().numpy(), b0)
+    assert fc.fc_get_error() == "FC_OK"
+
+
+@pytest.mark.parametrize("chunk", [4, 48, 128])
+def test_prompts_in_chunks(fc, chunk):
+    """Prompts taken in by chunks: attention over what is cached, causal among the new, then the chunk is written.  Each
+    chunk against the oracle over the cache as it is."""
+    rng = np.random.default_rng(27)
+    H, Hkv, page, lens = 8, 4, 32, [300, 131, 17]
+    B, most = len(lens), 10
+    n_pages = B * most
+    table = rng.permutation(n_pages).astype(np.int32).reshape(B, most)
+    cache = [np.zeros((n_pages, Hkv, page, D), np.uint8) for _ in range(2)] + [np.ones((n_pages, Hkv, page // 16), np.float32) for _ in range(2)]
+    held = on_gpu(fc, cache)
+    ws = fc.kv8_attn_workspace(B, chunk, H, Hkv, "cuda")
+    for at in range(0, max(lens), chunk):
+        kv = np.minimum(at, lens).astype(np.int32)
+        nodes = np.clip(np.array(lens) - at, 0, chunk).astype(np.int32)
+        s = dict(kv=kv, nodes=nodes, table=table, cache=cache, q=bf(rng, B, chunk, H, D), k=bf(rng, B, Hkv, chunk, D), v=bf(rng, B, Hkv, chunk, D))
+        k, v = s["k"].cuda(), s["v"].cuda()
+        got = fc.fc_kv8_attn(s["q"].cuda(), held, dev(table), dev(kv), k, v, None, dev(nodes), workspace=ws)
+        ref, tol, _, _ = reference(s, None, D ** -0.5, causal=True)
+        assert np.all(np.abs(num(got) - ref) <= tol)
+        p = at + np.arange(chunk)
+        slot = np.where(np.arange(chunk) < nodes[:, None], table[:, np.minimum(p // page, most - 1)] * page + p % page, -1).astype(np.int32).reshape(-1)
+        fc.fc_kv8_write(held, k.transpose(1, 2), v.transpose(1, 2), dev(slot))
+        o8.write(cache, *(num(x).transpose(0, 2, 1, 3).reshape(-1, Hkv, D) for x in (s["k"], s["v"])), slot)
+        same_cache(held, cache)
+    assert fc.fc_get_error() == "FC_OK"
+
+
+def test_tracks_change_places_after_an_eviction(fc):
+    """Attention with weights, writes, an eviction whose output track is the next steps': three times over."""
+    rng = np.random.default_rng(28)
+    B, n, H, Hkv, page, K = 2, 1, 4, 2, 16, 40
+    s = setup(rng, [70, 41], n, H, Hkv, page, stale=False)
+    s["table"] = np.arange(2 * 6, dtype=np.int32).reshape(2, 6)
+    s["cache"] = random_cache(rng, 12, Hkv, page)
+    cache, table = on_gpu(fc, s["cache"]), dev(s["table"])
+    now, then = fc.Kv8Track.empty(cache), fc.Kv8Track.empty(cache)
+    t_now, t_then = ([x.weight.cpu().numpy().copy(), x.born.cpu().numpy().copy()] for x in (now, then))
+    ws = fc.kv8_attn_workspace(B, n, H, Hkv, "cuda", 6 * page)
+    born = 1000
+    for _ in range(3):
+        for _ in range(20):
+            s["k"], s["v"], s["q"] = bf(rng, B, Hkv, n, D), bf(rng, B, Hkv, n, D), bf(rng, B, n, H, D)
+            k, v = s["k"].cuda(), s["v"].cuda()
+            got = fc.fc_kv8_attn(s["q"].cuda(), cache, table, dev(s["kv"]), k, v, workspace=ws, weight=now.weight, decay=0.9)
+            ref, tol, want, bound = reference(s, None, D ** -0.5, causal=True)
+            assert np.all(np.abs(num(got) - ref) <= tol)
+            for b in range(B):  # the tokens' alone decay
+                i = np.arange(s["kv"][b])
+                p, o = s["table"][b][i // page], i % page
+                new = num(now.weight)[p, :, o]
+                assert np.all(np.abs(new - (0.9 * t_now[0][p, :, o] + want[p, :, o])) <= bound[p, :, o] + 2.0 ** -22 * new)
+            t_now[0] = now.weight.cpu().numpy().copy()
+            slot = np.array([s["table"][b][L // page] * page + L % page for b, L in enumerate(s["kv"])], np.int32)
+            pos = np.full(B, born, np.int32)
+            fc.fc_kv8_write(cache, k.transpose(1, 2), v.transpose(1, 2), dev(slot), track=now, pos=dev(pos))
+            o8.write(s["cache"], num(s["k"])[:, :, 0], num(s["v"])[:, :, 0], slot, None, t_now, pos)
+            s["kv"], born = s["kv"] + 1, born + 1
+        fc.fc_kv8_evict(cache, table, dev(s["kv"]), dev(np.full(B, K, np.int32)), 8, now, then, cap=K)
+        o8.evict(s["cache"], s["table"], s["kv"], [K] * B, 8, t_now, t_then, K)
+        same_cache(cache, s["cache"])
+        now, then, t_now, t_then = then, now, t_then, t_now
+        s["kv"] = np.minimum(s["kv"], K).astype(np.int32)
+        for x, y in zip((now.weight, now.born), t_now):
+            for b in range(B):
+                i = np.arange(K)
+                assert np.array_equal(x.cpu().numpy()[s["table"][b][i // page], :, i % page], y[s["table"][b][i // page], :, i % page])
+    assert fc.fc_get_error() == "FC_OK"
