@@ -835,7 +835,8 @@ typedef struct {
  * pass: for a head's row x of D values
  *   y = x / sqrt(mean(x^2) + eps) * w,   then (y_i, y_{i + D/2}) turned by
  *   pos * base^(-2i/D)   (fc_rope's pairing; a negative position: not turned),
- * fp32 inside (the squares' sum too), rounded once to bf16.
+ * fp32 inside (the squares' sum too, of x times a power of two where it would
+ * pass fp32's range), rounded once to bf16.
  *   d_q  row (b, i, h) at element b * q_seq_stride + i * q_row_stride + h *
  *        q_head_stride, so that parts of a projection's rows are read where
  *        they are; d_k and d_v likewise with the kv strides.  d_v may be NULL.

@@ -7,9 +7,10 @@
 // squares is a shuffle over LP lanes, the rotation needs no exchange, and the
 // 8 sines and cosines of a lane's dimensions serve all heads of the row that the
 // warp takes.  The read and the write bound it (rows * (H + 2 Hkv) * D * 4
-// bytes; 65000 rows of 16 + 16 + 16 heads of 128 267 us, 6.0 TB/s, a copy's rate
-// 6.6; unrolled over heads or rows, with prefetches or streaming hints, and on other grids 278
-// to 387); fp32 inside, rounded once.  32 rows take 3.7 us, latency.
+// bytes; 65000 rows of 16 + 16 + 16 heads of 128 272 us, 5.9 TB/s, a copy's rate
+// 6.6; 267 without the check of the squares' range; unrolled over heads or rows, with
+// prefetches or streaming hints, and on other grids 278 to 387); fp32 inside,
+// rounded once.  32 rows take 3.7 us, latency.
 #include <algorithm>
 #include <cmath>
 
@@ -21,6 +22,9 @@ namespace {
 
 constexpr int NR_THREADS = 256, NR_WARPS = NR_THREADS / 32;
 constexpr int MAX_D = 512;
+// Sums of squares that fp32 holds with all their parts: up to SS_MAX, and from
+// SS_MIN on unless eps is as much (it then outweighs what is lost).
+constexpr uint32_t SS_MAX = 0x7B800000u, SS_MIN = 0x17800000u;  // 2^120, 2^-80: fp32's bits, in the numbers' order
 
 struct NormArgs {
   const __nv_bfloat16 *q, *k, *v;
@@ -31,6 +35,7 @@ struct NormArgs {
   int n, H, Hkv, D, heads, slices, per;  // heads: H + Hkv (+ Hkv with values); a warp takes `per` of them
   long long items;                       // rows * slices
   float eps;
+  uint32_t ss_min;  // SS_MIN or 0
   double nl2f;  // -2 log2(base) / D
 };
 
@@ -79,9 +84,23 @@ __global__ void __launch_bounds__(NR_THREADS) k_qk_norm_rope(NormArgs a) {
       }
 #pragma unroll
       for (int o = 1; o < LP; o <<= 1) ss += __shfl_xor_sync(0xFFFFFFFFu, ss, o);
+      float by = 1.f, eps = a.eps;
+      if (__builtin_expect(__any_sync(0xFFFFFFFFu, __float_as_uint(ss) - a.ss_min > SS_MAX - a.ss_min), 0)) {  // once more, of x times a power of two
+        by = !(ss <= __uint_as_float(SS_MAX)) ? 0x1p-80f : ss < __uint_as_float(a.ss_min) ? 0x1p100f : 1.f;
+        ss = 0.f;
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+          const uint32_t l = (&lo.x)[u], m = (&hi.x)[u];
+          const float x0 = lo_f(l) * by, x1 = hi_f(l) * by, y0 = lo_f(m) * by, y1 = hi_f(m) * by;
+          ss = fmaf(x0, x0, fmaf(x1, x1, fmaf(y0, y0, fmaf(y1, y1, ss))));
+        }
+#pragma unroll
+        for (int o = 1; o < LP; o <<= 1) ss += __shfl_xor_sync(0xFFFFFFFFu, ss, o);
+        eps = eps * by * by;
+      }
       if (!in) continue;
       if (!value) {
-        const float inv = rsqrtf(ss / (float)a.D + a.eps);
+        const float inv = rsqrtf(ss / (float)a.D + eps) * by;
         const uint4* w = reinterpret_cast<const uint4*>(query ? a.wq : a.wk);
         const uint4 wl = w[c], wh = w[c + chunks];
 #pragma unroll
@@ -126,7 +145,7 @@ extern "C" fc_status fc_qk_norm_rope(const void* d_q, int64_t q_seq_stride, int6
   const int per = rows * ((heads + at_once - 1) / at_once) <= 152 * 64 ? at_once : heads, slices = (heads + per - 1) / per;
   NormArgs a{bf(d_q), bf(d_k), bf(d_v), q_seq_stride, q_row_stride, q_head_stride, kv_seq_stride, kv_row_stride, kv_head_stride,
              bf(d_wq), bf(d_wk), d_pos, static_cast<__nv_bfloat16*>(d_q_out), static_cast<__nv_bfloat16*>(d_k_out),
-             static_cast<__nv_bfloat16*>(d_v_out), n, H, Hkv, D, heads, slices, per, rows * slices, eps,
+             static_cast<__nv_bfloat16*>(d_v_out), n, H, Hkv, D, heads, slices, per, rows * slices, eps, eps < 0x1p-80f ? SS_MIN : 0u,
              -2.0 * std::log2((double)base) / D};
   const unsigned grid = (unsigned)std::min<long long>((a.items + NR_WARPS - 1) / NR_WARPS, 152 * 8);
   cudaStream_t s = static_cast<cudaStream_t>(stream);

@@ -1009,3 +1009,22 @@ def test_tracks_change_places_after_an_eviction(fc):
                 i = np.arange(K)
                 assert np.array_equal(x.cpu().numpy()[s["table"][b][i // page], :, i % page], y[s["table"][b][i // page], :, i % page])
     assert fc.fc_get_error() == "FC_OK"
+
+
+@pytest.mark.parametrize("dim", [16, 64, 128, 256, 512])
+@pytest.mark.parametrize("exp,eps", [(70, 1e-6), (110, 1e-6), (125, 0.0), (-70, 0.0), (-110, 0.0), (-70, 1e-6), (-45, 1e-26), (0, 1e30)])
+def test_norm_rope_of_large_and_small_rows(fc, dim, exp, eps):
+    """Rows whose squares pass fp32's range, beside ordinary ones and rows of zeros."""
+    rng = np.random.default_rng(dim)
+    q, k = bf(rng, 2, 5, 3, dim), bf(rng, 2, 5, 2, dim)
+    q[:, ::2], k[:, 1, 1] = (q[:, ::2].float().clamp(-2, 2) * 2.0 ** exp).bfloat16(), (k[:, 1, 1].float().clamp(-2, 2) * 2.0 ** exp).bfloat16()
+    if eps:
+        q[1, 1, 1] = 0
+    w, pos = bf(rng, dim), rng.integers(0, 9, (2, 5)).astype(np.int32)
+    got = fc.fc_qk_norm_rope(q.cuda(), k.cuda(), None, w.cuda(), w.cuda(), dev(pos), 1e4, eps)
+    for x, y, turn in ((q, got[0], False), (k, got[1], True)):
+        ref, mag = o8.norm_rope(num(x), num(w), pos.astype(np.float64), 1e4, eps)
+        if turn:
+            ref, mag = ref.transpose(0, 2, 1, 3), mag.transpose(0, 2, 1, 3)
+        assert np.all(np.abs(num(y) - ref) <= 2.0 ** -8 * np.abs(ref) + 2.0 ** -18 * mag + 2.0 ** -133)
+    assert fc.fc_get_error() == "FC_OK"
