@@ -764,9 +764,9 @@ fc_status fc_kv4_read(const fc_kv4_cache* cache, const int32_t* d_slot, int rows
  *     exact down to 2^-20 of it; queries fp16 relative to the row's largest,
  *     exact down to 2^-26 of it; probabilities times value scales bf16.
  * Scales, new keys and new values may lie anywhere between 2^-80 and 2^100 (or be
- * 0), side by side, and queries anywhere; scores, scale * q k, of up to 2^24 in
- * magnitude (their sums are fp32: with s a key's scale, its score is off by up to
- * 2^-14 of scale * s * sum |q|, which is to be below 2^100).
+ * 0), side by side, and queries anywhere; scores, scale * q k, of up to 2^24 and
+ * q k of up to 2^120 in magnitude, its terms among them (their sums are fp32: with
+ * s a key's scale, its score is off by up to 2^-14 of scale * s * sum |q|).
  * A length or node count out of range, or a page id outside the pool, records
  * FC_ERR_INVALID_ARG (that request's rows are zeros; that page's keys are
  * left out).  What a page holds past a request's end is not looked at.  A new
@@ -900,8 +900,8 @@ fc_status fc_kv8_read(const fc_kv8_cache* cache, const int32_t* d_slot, int rows
  *   more: cached numbers exact; queries, and new keys by 16, exact down to 2^-9
  *     of the row's largest, to 2^-17 of it below; probabilities bf16.
  * Scales, new keys and new values may lie anywhere between 2^-80 and 2^100 (or be
- * 0), side by side, and queries anywhere; scores, scale * q k, of up to 2^24 in
- * magnitude.
+ * 0), side by side, and queries anywhere; scores, scale * q k, of up to 2^24 and
+ * q k of up to 2^120 in magnitude, its terms among them.
  * What a block holds past a request's end, and a scale of a block that begins
  * there, is not looked at.  A block that stands for NaN makes the rows of its
  * request and head NaN.  A new token with a NaN or an infinity in its key or its

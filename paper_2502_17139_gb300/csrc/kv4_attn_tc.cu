@@ -31,7 +31,7 @@
 // The CTAs (one an SM) share all units' blocks equally, cut anywhere; a cut
 // unit's pieces go through the workspace to k_kv4_join.
 // Measured (kv heads x their query heads): 32 trees of 128 nodes over 16384 keys
-// (8 x 4) 1061 us, 1036 TFLOP/s of the tree's own products; 16 trees of 64 nodes
+// (8 x 4) 1070 us, 1028 TFLOP/s of the tree's own products; 16 trees of 64 nodes
 // over 4096 (32 x 1) 217 us; one of 128 over 500 keys 35 us.  With two tiles a
 // block takes 4.1 K cycles: 2.6 K of softmax, then the 1.1 K of that tile's two
 // products, waits the rest; the other tile runs beside it.  With one tile it

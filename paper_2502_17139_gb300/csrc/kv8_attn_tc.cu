@@ -29,8 +29,8 @@
 // The CTAs (one an SM) share all units' blocks equally, cut anywhere; a cut
 // unit's pieces go through the workspace to k_kv8_join.
 // Several roles run at once from one instruction cache, so the loops are short.
-// Measured: 32 trees of 128 nodes, 4 query heads a kv head, over 16384 keys 893 us (1231
-// TFLOP/s), 16 ragged trees of 64 nodes, a kv head a query head, 117 us.  What bounds it is a
+// Measured: 32 trees of 128 nodes, 4 query heads a kv head, over 16384 keys 899 us (1223
+// TFLOP/s), 16 ragged trees of 64 nodes, a kv head a query head, 118 us.  What bounds it is a
 // block's chain: of 4.0 K cycles a block of two tiles, a tile's weights take 2.3 K (a warp's instructions one
 // after another, not a pipe), its products 1.0 K, hand-overs the rest; the tiles run side by side.
 // Every mbarrier wait is bounded: one that runs out raises FC_ERR_TIMEOUT, the
@@ -87,9 +87,9 @@ constexpr float M_START = -1e30f;  // a reference before any key
 constexpr int E_MIN = -119, E_MAX = 127;
 constexpr float FACTOR_MIN = 0x1p-126f, ROW_MIN = 0x1p-149f, FACTOR_MAX = 0x1.fffffep127f;
 // A unit's start and end in blocks of one tile: 4 where a unit is cut over CTAs (3
-// requests of 128 nodes, 32 heads of their own, over 3000 keys 36 us, with 8 39), 7
-// where a CTA has several (16 ragged trees of 64 nodes 121 us, with 12 128).  And
-// the least share worth a CTA (32 nodes over 2000 keys 22 us, with 6 25).
+// requests of 128 nodes, 32 heads of their own, over 3000 keys 44 us, with 8 47), 7
+// where a CTA has several (16 ragged trees of 64 nodes 117 us, with 12 123).  And
+// the least share worth a CTA (32 nodes over 2000 keys 22.7 us, with 6 24).
 constexpr int CUT_COST = 4, WHOLE_COST = 7, LEAST = 4;
 
 // Registers a thread by warpgroup (setmaxnreg), of the launch's 96.  The shares must add up to the launch's
@@ -925,10 +925,10 @@ __global__ void __launch_bounds__(THREADS, 1) k_kv8_attn_many(const __grid_const
           }
           tc_wait_st();
         }
-        // The row's scores come 32 at a time, once for the maximum, once for P:
-        // one short loop each, as two bodies with loads in flight beside them
-        // took longer (1160 us where this takes 1100): the roles share the
-        // instruction cache and the other warps cover the loads.
+        // The row's scores come 32 at a time, once for the maximum, once for P, one
+        // short loop each: the roles share the instruction cache, and the other
+        // warps cover the loads.  (64 at a time, at a step where this took 893 us for
+        // 32 trees of 128 nodes and 121 for 16 of 64: 880 and 129.)
         uint32_t sa[32], sb[32];
         float top = -INFINITY;
         auto largest = [&](int q, const uint32_t (&sv)[32]) {
