@@ -834,6 +834,9 @@ bool shape_ok(int n_pad, int H, int Hkv) {
   return n_pad >= 1 && n_pad <= FC_MAX_NODES && H >= 1 && Hkv >= 1 && H % Hkv == 0 && H / Hkv <= 16;
 }
 
+// at most 2^30 query rows over all heads (the product of all three may pass 64 bits)
+bool rows_ok(int batch, int n_pad, int H) { return batch <= (1ll << 30) / ((long long)H * n_pad); }
+
 // bytes of the scores and of the rows' sums that the weights are made from
 size_t score_bytes(long long batch, int n_pad, int H, long long keys) {
   const size_t rows = (size_t)batch * n_pad * H;
@@ -843,7 +846,9 @@ size_t score_bytes(long long batch, int n_pad, int H, long long keys) {
 }  // namespace
 
 extern "C" size_t fc_kv8_attn_workspace(int batch, int n_pad, int H, int Hkv, int64_t weight_keys) {
-  if (batch < 1 || !shape_ok(n_pad, H, Hkv) || weight_keys < 0 || (weight_keys && n_pad * (H / Hkv) > 16)) return 0;
+  if (batch < 1 || !shape_ok(n_pad, H, Hkv) || !rows_ok(batch, n_pad, H) || weight_keys < 0 || weight_keys > 0x7FFFFFFFll ||
+      (weight_keys && n_pad * (H / Hkv) > 16))
+    return 0;
   if (n_pad * (H / Hkv) > 16) return kv8_attn_many_workspace(batch, n_pad, H, Hkv);
   return KV8_WS_COUNTERS + (size_t)FEW_GRID * 2 * FewSmem<2>::ROWS * (HD + 2) * sizeof(float) +
          (weight_keys ? score_bytes(batch, n_pad, H, weight_keys) : 0);
@@ -859,7 +864,7 @@ extern "C" fc_status fc_kv8_attn(const void* d_q, const fc_kv8_cache* cache, con
   if (batch < 0 || max_pages < 1 || !(scale > 0.f) || !std::isfinite(scale) || (d_weight && !std::isfinite(decay))) return FC_ERR_INVALID_ARG;
   if (!shape_ok(n_pad, H, cache->Hkv)) return FC_ERR_UNSUPPORTED;
   const int shift = kv8_page_shift(cache->page_size), G = H / cache->Hkv;
-  if ((long long)batch * H * n_pad > 1ll << 30 || (long long)max_pages << shift > 0x7FFFFFFFll || (d_weight && n_pad * G > 16))
+  if (!rows_ok(batch, n_pad, H) || (long long)max_pages << shift > 0x7FFFFFFFll || (d_weight && n_pad * G > 16))
     return FC_ERR_UNSUPPORTED;
   if (batch == 0) return FC_OK;
   if (!d_q || !d_table || !d_kv_len || !d_out || !kv8_aligned(d_q, 16) || !kv8_aligned(d_out, 16) || !d_k_new != !d_v_new ||

@@ -193,3 +193,14 @@ def test_scores_of_two_parts_are_within_the_oracles_bound():
     err = np.abs(qp @ kp.T - q @ k.T)
     for keys, new in ((slice(0, 8), 0), (slice(8, 40), 32)):
         assert np.all(err[:, keys] <= bound(keys, new))
+
+
+def test_more_query_rows_than_are_counted_are_refused(fc):
+    """2^30 over all heads; sizes whose product passes 64 bits among them."""
+    L, nul, f = fc.LIB, None, C.c_float
+    for Hkv, batch, n, H in ((1 << 26, 1 << 30, 16, 1 << 30), (1 << 26, (1 << 31) - 1, 128, 1 << 30), (8, 1 << 27, 1, 9 * 8), (8, (1 << 27) + 1, 1, 8),
+                             (1 << 26, 1, 16, 1 << 30)):
+        cache = C.byref(fc.fc_kv8_cache(256, 256, 256, 256, 1, 16, Hkv, 128))
+        assert L.fc_kv8_attn(256, cache, 256, 4, 256, nul, nul, nul, nul, batch, n, H, f(0.1), nul, f(1.0), 256, nul, 0, nul) == 2  # FC_ERR_UNSUPPORTED
+        assert L.fc_kv8_attn_workspace(batch, n, H, Hkv, 0) == 0
+    assert L.fc_kv8_attn_workspace(1 << 26, 1, 16, 8, 0) > 0 and L.fc_kv8_attn_workspace(1, 1, 8, 8, 1 << 31) == 0
