@@ -878,10 +878,10 @@ fc_status fc_kv8_read(const fc_kv8_cache* cache, const int32_t* d_slot, int rows
 /*
  * fc_tree_attn over the paged 8-bit cache, for 1 to 128 new tokens a request:
  * fc_kv4_attn's arguments and limits (D = 128, H a multiple of Hkv, H / Hkv <=
- * 16, and batch * n_pad * H <= 2^30; new tokens in bf16 by mask, rows past n_nodes and rows that see no key
- * zeros, page ids and lengths checked on the device, a workspace of
- * fc_kv8_attn_workspace() bytes, 256-byte aligned, ZEROED before its first use
- * and fit for the next call of any shape after each).
+ * 16, batch * n_pad * H <= 2^30; new tokens in bf16 by mask, rows past n_nodes
+ * and rows that see no key zeros, page ids and lengths checked on the device, a
+ * workspace of fc_kv8_attn_workspace() bytes, 256-byte aligned, ZEROED before its
+ * first use and fit for the next call of any shape after each).
  *   d_weight  optional [n_pages][Hkv][page_size] fp32: a cached token's becomes
  *             decay * (what is there) + the sum of its softmax weights over the
  *             request's query rows of that kv head; decay 0 does not read what
