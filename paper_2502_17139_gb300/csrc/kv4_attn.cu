@@ -140,10 +140,10 @@ __device__ __forceinline__ float exp2_fast(float x) {
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
 }
-// l * 2^d by two factors: a row's sum, relative to a reference that value scales move, may be 2^112 and d -180
+// l * 2^d by two factors, the first 1 from d = -100 on: a row's sum, relative to a
+// reference that value scales move, may be 2^112 and d -180
 __device__ __forceinline__ float times_pow2(float l, float d) {
-  const float h = exp2_fast(0.5f * d);
-  return l * h * h;
+  return l * exp2_fast(fminf(d + 100.f, 0.f)) * exp2_fast(fmaxf(d, -100.f));
 }
 __device__ __forceinline__ float pow2i(int e) { return __uint_as_float((uint32_t)(e + 127) << 23); }  // -126 <= e <= 127
 __device__ __forceinline__ int expo(float x) { return (int)((__float_as_uint(x) >> 23) & 255u) - 127; }
